@@ -555,6 +555,87 @@ int hcw_gemm_bf16(int M, int N, int K, const void* A, int ta, const void* B, int
 int hcw_gemm_bf16_batched(int M, int N, int K, const void* A, long long a_stride, const void* B,
                           long long b_stride, float* C, int batch, void* stream);
 
+/*
+ * Norms after one block and before the next, fused with the block's gate and the
+ * residual scale (the sandwich of norms around a sublayer of a language model, with the
+ * mixing stack or the feed-forward block as the sublayer):
+ *   v = N_post(f);  s = alpha r + gate_g(t) v;  r_out = s;  x_out = N_pre(s)
+ *   N(v) = vhat w + b;  HCW_NORM_RMS: vhat = v / sqrt(mean(v^2) + eps), b = 0;
+ *   HCW_NORM_LAYER: vhat = (v - mean(v)) / sqrt(var(v) + eps), biased variance;
+ *   HCW_NORM_NONE: N_post(f) = f (not allowed for N_pre when x_out is wanted).
+ *   r, f     [T][d] (dtype): residual stream and branch output; one of them may be NULL
+ *            (r: s is the branch alone; f: no branch, gate and post are not read).
+ *   gate     [G][d] fp32 or NULL (ones); rows_per_gate rows in a row share one, the last
+ *            group may be shorter (G = ceil(T / rows_per_gate)); 0: all rows share one.
+ *   post_w, post_b, pre_w, pre_b  [d] fp32; a NULL weight is ones, a NULL bias zeros, and a
+ *            bias is read under HCW_NORM_LAYER only.
+ *   r_out, x_out  [T][d] (dtype) outputs; either may be NULL.  x_out is the norm of s in
+ *            fp32, before r_out's rounding.
+ * Statistics, sums and products are fp32; each output is rounded once.  Rows of d elements
+ * one after the other, 1 <= d <= 8192 (HCW_ERR_UNSUPPORTED above), any T >= 0 (0 does
+ * nothing); pointers are 16-byte aligned.  An output that overlaps an input or another
+ * output is HCW_ERR_ALIASING.  One launch, no workspace.
+ */
+#define HCW_NORM_NONE  0
+#define HCW_NORM_RMS   1
+#define HCW_NORM_LAYER 2
+int hcw_residual_norm_fwd(const void* r, const void* f, const float* gate, int rows_per_gate,
+                          float alpha, int post, const float* post_w, const float* post_b, int pre,
+                          const float* pre_w, const float* pre_b, float eps, int T, int d,
+                          int dtype, void* r_out, void* x_out, void* stream);
+
+/*
+ * Its backward pass, which recomputes the statistics from the rows:
+ *   ds = dr_out + N_pre'(s)^T dx_out;  dr = alpha ds;  df = N_post'(f)^T (gate ds)
+ *   dgate_g = sum over the group's rows of ds v;  dpost_w = sum gate ds fhat,
+ *   dpost_b = sum gate ds;  dpre_w = sum dx_out shat;  dpre_b = sum dx_out
+ *   dr_out, dx_out  [T][d] (dtype): gradients of r_out and x_out; one may be NULL (zero).
+ *   s        [T][d] (dtype): r_out as the forward stored it (read with dx_out).
+ *   f, gate, rows_per_gate, alpha, post, post_w, post_b, pre, pre_w, eps as for the forward.
+ *   dr, df   [T][d] (dtype) outputs, dgate [G][d], dpost_w, dpost_b, dpre_w, dpre_b [d] fp32
+ *            outputs; each may be NULL (not wanted), one at least is given.  A norm that is
+ *            not there has no gradients, RMS no bias gradient (HCW_ERR_INVALID_ARG).  With
+ *            T = 0 the parameter gradients are zeros.
+ *   workspace  hcw_residual_norm_bwd_workspace_bytes(...) bytes for the parameter gradients'
+ *            partial sums; not needed without them.
+ * The sums over the rows have a fixed order: the same inputs give the same bits.
+ */
+size_t hcw_residual_norm_bwd_workspace_bytes(int T, int d, int rows_per_gate);
+int hcw_residual_norm_bwd(const void* dr_out, const void* dx_out, const void* s, const void* f,
+                          const float* gate, int rows_per_gate, float alpha, int post,
+                          const float* post_w, const float* post_b, int pre, const float* pre_w,
+                          float eps, int T, int d, int dtype, void* dr, void* df, float* dgate,
+                          float* dpost_w, float* dpost_b, float* dpre_w, float* dpre_b,
+                          void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * Distillation from a teacher's top logits: loss and gradient of every row in one pass.
+ *   p = softmax over the row's slots of teacher / temperature
+ *   q = softmax(z / temperature) and q1 = softmax(z) over the V symbols
+ *   loss = weight [ kl_scale temperature^2 sum_k p_k (log p_k - log q_{idx_k})
+ *                   + ce_scale (log sum_j exp(z_j) - z_target) ]
+ *   dz_j = weight [ kl_scale temperature (q_j - sum_{k: idx_k = j} p_k)
+ *                   + ce_scale (q1_j - [j = target]) ]
+ *   z        [T][V] (dtype): the student's logits.
+ *   idx, teacher  [T][K] int32 and fp32: symbols and logits of the teacher's slots, or both
+ *            NULL with K = 0.  A negative idx is an empty slot; a row without a slot (or with
+ *            teacher logits of -inf only) has no teacher part.  A symbol may occur twice (its
+ *            probabilities add up).
+ *   target   [T] int32 or NULL: the hard label; negative: the row has none.
+ *   weight   [T] fp32 or NULL (ones), e.g. 1 / (rows that count).  A row of weight 0 gives
+ *            loss and gradient 0 whatever its logits are, NaN included; they are not read.
+ *   loss     [T] fp32, dz [T][V] (dtype): outputs; one may be NULL.
+ * Logits of -inf are symbols that cannot occur (gradient 0 unless the teacher or the label
+ * names them, then the loss is +inf); a row of -inf alone gives 0 and 0.  NaN or +inf in a row
+ * that counts gives NaN.  idx or target >= V counts as empty and is reported by
+ * hcw_sync_status as HCW_ERR_INVALID_ARG.  Sums are fp32, dz is rounded once; no atomics: the
+ * same inputs give the same bits.  1 <= V <= 262144, K <= 1024 (HCW_ERR_UNSUPPORTED above), any V
+ * and T (T = 0 does nothing); temperature > 0.  One launch, no workspace.
+ */
+int hcw_distill_loss(const void* z, const int* idx, const float* teacher, const int* target,
+                     const float* weight, int T, int V, int K, int dtype, float temperature,
+                     float kl_scale, float ce_scale, float* loss, void* dz, void* stream);
+
 /* Number of kernels this library has launched in this process (all devices). */
 unsigned long long hcw_launch_count(void);
 

@@ -356,6 +356,10 @@ cudaError_t block_error_word_read_clear(int* word);
 // (the launch counter lives with the C API in hcw_api.cu).
 int count_launch(cudaError_t e, int kernels);
 
+// ---- Distillation loss (hcw_distill.cu) ----
+// Read its kernels' error word and reset it to 0 (synchronous).
+cudaError_t distill_error_word_read_clear(int* word);
+
 // Dynamic shared memory the tensor-core kernel uses for this N tile.
 size_t tc_smem_bytes(int BN);
 int tc_stages(int BN);

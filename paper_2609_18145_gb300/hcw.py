@@ -40,6 +40,10 @@ HCW_CAUSAL = 1
 HCW_RESIDUAL = 2
 HCW_ACT_RELU = 4
 
+HCW_NORM_NONE = 0
+HCW_NORM_RMS = 1
+HCW_NORM_LAYER = 2
+
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libhcw.so")
 
 _lock = threading.Lock()
@@ -50,6 +54,7 @@ _I = ctypes.c_int
 _U = ctypes.c_uint
 _SZ = ctypes.c_size_t
 _LL = ctypes.c_longlong
+_F = ctypes.c_float
 
 _SIGNATURES = {
     "hcw_version": ([], _I),
@@ -97,6 +102,12 @@ _SIGNATURES = {
     "hcw_gemm_bf16": ([_I, _I, _I, _P, _I, _P, _I, _P, _P, _SZ, _P], _I),
     "hcw_gemm_bf16_batched": ([_I, _I, _I, _P, ctypes.c_longlong, _P, ctypes.c_longlong, _P, _I,
                                _P], _I),
+    "hcw_residual_norm_fwd": ([_P, _P, _P, _I, _F, _I, _P, _P, _I, _P, _P, _F, _I, _I, _I, _P, _P,
+                               _P], _I),
+    "hcw_residual_norm_bwd_workspace_bytes": ([_I, _I, _I], _SZ),
+    "hcw_residual_norm_bwd": ([_P, _P, _P, _P, _P, _I, _F, _I, _P, _P, _I, _P, _F, _I, _I, _I, _P,
+                               _P, _P, _P, _P, _P, _P, _P, _SZ, _P], _I),
+    "hcw_distill_loss": ([_P, _P, _P, _P, _P, _I, _I, _I, _I, _F, _F, _F, _P, _P, _P], _I),
     "hcw_set_stack_kernels": ([_I], _I),
     "hcw_set_decode_kernel": ([_I], _I),
     "hcw_stack_kernels_used": ([_I, _I, _I, _I], _I),
@@ -384,6 +395,157 @@ def hcw_gemm_bf16_batched(A, B, C=None, stream=None):
     _check(lib().hcw_gemm_bf16_batched(M, N, K, _ptr(A), A.stride(0), _ptr(B), B.stride(0),
                                        _ptr(C), batch, _stream(stream)), "hcw_gemm_bf16_batched")
     return C
+
+
+def _rows(t):
+    """(T, d) of a row matrix [..., d]."""
+    d = t.shape[-1]
+    return (t.numel() // d if d else 0), d
+
+
+def _f32(what, *ts):
+    for t in ts:
+        if t is not None and t.dtype != torch.float32:
+            raise TypeError("%s must be float32, got %s" % (what, t.dtype))
+
+
+def _like(ref, what, *ts):
+    """ts (None allowed) have ref's dtype and number of elements."""
+    for t in ts:
+        if t is not None and (t.dtype != ref.dtype or t.numel() != ref.numel()):
+            raise ValueError("%s: %s %s does not match %s %s"
+                             % (what, tuple(t.shape), t.dtype, tuple(ref.shape), ref.dtype))
+
+
+def _numel(what, n, *ts):
+    for t in ts:
+        if t is not None and t.numel() != n:
+            raise ValueError("%s: expected %d elements, got %s" % (what, n, tuple(t.shape)))
+
+
+def _gates(T: int, rows_per_gate: int) -> int:
+    return -(-T // rows_per_gate) if rows_per_gate > 0 else 1
+
+
+def hcw_residual_norm_fwd(r, f, gate=None, rows_per_gate: int = 0, alpha: float = 1.0,
+                          post: int = HCW_NORM_NONE, post_w=None, post_b=None,
+                          pre: int = HCW_NORM_RMS, pre_w=None, pre_b=None, eps: float = 1e-5,
+                          r_out=None, x_out=None, want_r: bool = True, want_x: bool = True,
+                          stream=None):
+    """s = alpha r + gate N_post(f), x = N_pre(s) over rows [..., d]; returns
+    (r_out, x_out).  r or f may be None; gate [G, d] fp32 is shared by
+    rows_per_gate rows each (0: by all rows).  want_r / want_x = False leaves
+    an output out (None)."""
+    _dev(r, f, gate, post_w, post_b, pre_w, pre_b, r_out, x_out)
+    ref = f if r is None else r
+    if ref is None:
+        raise ValueError("hcw_residual_norm_fwd: r or f is needed")
+    T, d = _rows(ref)
+    _f32("hcw_residual_norm_fwd: gate, weights and biases", gate, post_w, post_b, pre_w, pre_b)
+    _numel("hcw_residual_norm_fwd: weights and biases", d, post_w, post_b, pre_w, pre_b)
+    _numel("hcw_residual_norm_fwd: gate", _gates(T, rows_per_gate) * d, gate)
+    if want_r and r_out is None:
+        r_out = torch.empty_like(ref)
+    if want_x and x_out is None:
+        x_out = torch.empty_like(ref)
+    _like(ref, "hcw_residual_norm_fwd", f, r_out, x_out)
+    _check(lib().hcw_residual_norm_fwd(_ptr(r), _ptr(f), _ptr(gate), rows_per_gate, alpha, post,
+                                       _ptr(post_w), _ptr(post_b), pre, _ptr(pre_w), _ptr(pre_b),
+                                       eps, T, d, _dtype_code(ref), _ptr(r_out), _ptr(x_out),
+                                       _stream(stream)), "hcw_residual_norm_fwd")
+    return r_out, x_out
+
+
+def hcw_residual_norm_bwd_workspace_bytes(T: int, d: int, rows_per_gate: int = 0) -> int:
+    return int(lib().hcw_residual_norm_bwd_workspace_bytes(T, d, rows_per_gate))
+
+
+def hcw_residual_norm_bwd(dr_out, dx_out, s, f, gate=None, rows_per_gate: int = 0,
+                          alpha: float = 1.0, post: int = HCW_NORM_NONE, post_w=None, post_b=None,
+                          pre: int = HCW_NORM_RMS, pre_w=None, eps: float = 1e-5, dr=None, df=None,
+                          want_dr: bool = True, want_params: bool = True, want_bias: bool = False,
+                          workspace=None, stream=None):
+    """Backward of hcw_residual_norm_fwd; s is the forward's r_out.  Returns a
+    dict: dr, df (with f), dgate (with gate), dpost_w, dpre_w (of the norms
+    there are) and, with want_bias, dpost_b, dpre_b of LayerNorms.  dr_out or
+    dx_out may be None (zero).  want_params=False: dr and df only."""
+    _dev(dr_out, dx_out, s, f, gate, post_w, post_b, pre_w, dr, df, workspace)
+    ref = dr_out if dx_out is None else dx_out
+    if ref is None:
+        raise ValueError("hcw_residual_norm_bwd: dr_out or dx_out is needed")
+    T, d = _rows(ref)
+    G = _gates(T, rows_per_gate)
+    _f32("hcw_residual_norm_bwd: gate, weights and biases", gate, post_w, post_b, pre_w)
+    _numel("hcw_residual_norm_bwd: weights and biases", d, post_w, post_b, pre_w)
+    _numel("hcw_residual_norm_bwd: gate", G * d, gate)
+    has_post = f is not None and post != HCW_NORM_NONE
+    has_pre = dx_out is not None and pre != HCW_NORM_NONE
+    out = {}
+    if want_dr:
+        out["dr"] = torch.empty_like(ref) if dr is None else dr
+    if f is not None:
+        out["df"] = torch.empty_like(ref) if df is None else df
+    _like(ref, "hcw_residual_norm_bwd", dr_out, s if dx_out is not None else None, f,
+          out.get("dr"), out.get("df"))
+    if want_params:
+        f32 = dict(dtype=torch.float32, device=ref.device)
+        if f is not None and gate is not None:
+            out["dgate"] = torch.empty(G, d, **f32)
+        if has_post:
+            out["dpost_w"] = torch.empty(d, **f32)
+            if want_bias and post == HCW_NORM_LAYER:
+                out["dpost_b"] = torch.empty(d, **f32)
+        if has_pre:
+            out["dpre_w"] = torch.empty(d, **f32)
+            if want_bias and pre == HCW_NORM_LAYER:
+                out["dpre_b"] = torch.empty(d, **f32)
+        if workspace is None:
+            workspace = _workspace(hcw_residual_norm_bwd_workspace_bytes(T, d, rows_per_gate),
+                                   ref.device, None)
+    get = lambda k: _ptr(out.get(k))  # noqa: E731
+    _check(lib().hcw_residual_norm_bwd(_ptr(dr_out), _ptr(dx_out), _ptr(s), _ptr(f), _ptr(gate),
+                                       rows_per_gate, alpha, post, _ptr(post_w), _ptr(post_b),
+                                       pre, _ptr(pre_w), eps, T, d, _dtype_code(ref), get("dr"),
+                                       get("df"), get("dgate"), get("dpost_w"), get("dpost_b"),
+                                       get("dpre_w"), get("dpre_b"), _ptr(workspace),
+                                       0 if workspace is None else workspace.numel(),
+                                       _stream(stream)), "hcw_residual_norm_bwd")
+    return out
+
+
+def hcw_distill_loss(z, idx=None, teacher=None, target=None, weight=None,
+                     temperature: float = 1.0, kl_scale: float = 1.0, ce_scale: float = 0.0,
+                     loss=None, dz=None, want_grad: bool = True, stream=None):
+    """Loss of every row of student logits z [..., V] against the teacher's top
+    logits (idx, teacher [..., K]: int32 symbols, -1 for an empty slot, and fp32
+    logits) and hard labels (target [...] int32, -1 for none), and its gradient.
+    Returns (loss [T] fp32, dz like z, or None with want_grad=False)."""
+    _dev(z, idx, teacher, target, weight, loss, dz)
+    T, V = _rows(z)
+    K = 0
+    if idx is not None:
+        if teacher is None or idx.shape != teacher.shape:
+            raise ValueError("hcw_distill_loss: idx and teacher must have the same shape")
+        if idx.dtype != torch.int32:
+            raise TypeError("hcw_distill_loss: idx must be int32, got %s" % idx.dtype)
+        K = idx.shape[-1]
+        _numel("hcw_distill_loss: idx and teacher", T * K, idx)
+    elif teacher is not None:
+        raise ValueError("hcw_distill_loss: teacher logits without their symbols")
+    if target is not None and target.dtype != torch.int32:
+        raise TypeError("hcw_distill_loss: target must be int32, got %s" % target.dtype)
+    _f32("hcw_distill_loss: teacher, weight and loss", teacher, weight, loss)
+    _numel("hcw_distill_loss: target, weight and loss", T, target, weight, loss)
+    if loss is None:
+        loss = torch.empty(T, dtype=torch.float32, device=z.device)
+    if want_grad and dz is None:
+        dz = torch.empty_like(z)
+    _like(z, "hcw_distill_loss", dz)
+    _check(lib().hcw_distill_loss(_ptr(z), _ptr(idx) if K else None, _ptr(teacher) if K else None,
+                                  _ptr(target), _ptr(weight), T, V, K, _dtype_code(z),
+                                  temperature, kl_scale, ce_scale, _ptr(loss), _ptr(dz),
+                                  _stream(stream)), "hcw_distill_loss")
+    return loss, dz
 
 
 def hcw_set_decode_kernel(mode: int) -> int:
