@@ -556,6 +556,47 @@ int hcw_gemm_bf16_batched(int M, int N, int K, const void* A, long long a_stride
                           long long b_stride, float* C, int batch, void* stream);
 
 /*
+ * Gated feed-forward block, bf16:
+ *   g = x Wg^T,  u = x Wu^T,  a = act(g) u (elementwise),  y = a W2^T
+ *   x   [T][d];  W1 [2h][d]: rows 0 .. h-1 are Wg, rows h .. 2h-1 Wu;  W2 [d][h]
+ *   act HCW_GATE_SILU g / (1 + exp(-g)), HCW_GATE_GELU g (1 + erf(g / sqrt 2)) / 2,
+ *       or HCW_GATE_RELU max(g, 0) (derivative 0 at 0)
+ *   y   [T][d] output (no residual: hcw_residual_norm_fwd adds it)
+ *   workspace  hcw_gated_ffn_fwd_workspace_bytes(...) bytes, contents need not be
+ *       initialised (HCW_ERR_WORKSPACE when NULL or smaller).
+ * Products accumulate in fp32; g and u stay in fp32, a is rounded to bf16 once (it is the
+ * second product's operand), y once.  T >= 0 (0 does nothing), d and h multiples of 8
+ * (HCW_ERR_UNSUPPORTED otherwise, and above 2^20); pointers are 16-byte aligned; an output
+ * or the workspace over an input is HCW_ERR_ALIASING.  The same inputs give the same bits.
+ */
+#define HCW_GATE_SILU 0
+#define HCW_GATE_GELU 1
+#define HCW_GATE_RELU 2
+size_t hcw_gated_ffn_fwd_workspace_bytes(int T, int d, int h);
+int hcw_gated_ffn_fwd(const void* x, const void* W1, const void* W2, int T, int d, int h, int act,
+                      void* y, void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * Its backward pass, from the block's inputs alone (g and u are computed again, so the
+ * forward saves nothing):
+ *   da = dy W2;  du = da act(g);  dg = da u act'(g)
+ *   dx = dg Wg + du Wu;  dW1 = [dg | du]^T x (gate rows, then up rows);  dW2 = dy^T a
+ *   dy  [T][d] bf16;  dx [T][d] bf16 output
+ *   dW1 [2h][d], dW2 [d][h] outputs in dw_dtype: HCW_BF16 (the weights' type, rounded once)
+ *       or HCW_F32 (to be accumulated further)
+ *   dx = NULL: the weight gradients alone; dW1 = dW2 = NULL: dx alone (frozen weights).
+ *       With T = 0 the weight gradients are zeros.
+ *   workspace  hcw_gated_ffn_bwd_workspace_bytes(...) bytes.
+ * dg, du and a are rounded to bf16 once, as the products' operands.  Partial sums of a
+ * split sum over the tokens are added in a fixed order: the same inputs give the same
+ * bits.  Requirements and errors as for the forward.
+ */
+size_t hcw_gated_ffn_bwd_workspace_bytes(int T, int d, int h);
+int hcw_gated_ffn_bwd(const void* x, const void* dy, const void* W1, const void* W2, int T, int d,
+                      int h, int act, int dw_dtype, void* dx, void* dW1, void* dW2,
+                      void* workspace, size_t ws_bytes, void* stream);
+
+/*
  * Norms after one block and before the next, fused with the block's gate and the
  * residual scale (the sandwich of norms around a sublayer of a language model, with the
  * mixing stack or the feed-forward block as the sublayer):
@@ -629,8 +670,8 @@ int hcw_residual_norm_bwd(const void* dr_out, const void* dx_out, const void* s,
  * names them, then the loss is +inf); a row of -inf alone gives 0 and 0.  NaN or +inf in a row
  * that counts gives NaN.  idx or target >= V counts as empty and is reported by
  * hcw_sync_status as HCW_ERR_INVALID_ARG.  Sums are fp32, dz is rounded once; no atomics: the
- * same inputs give the same bits.  1 <= V <= 262144, K <= 1024 (HCW_ERR_UNSUPPORTED above), any V
- * and T (T = 0 does nothing); temperature > 0.  One launch, no workspace.
+ * same inputs give the same bits.  1 <= V <= 262144, K <= 1024, T < 2^28 (HCW_ERR_UNSUPPORTED
+ * above; T = 0 does nothing); temperature > 0.  One launch, no workspace.
  */
 int hcw_distill_loss(const void* z, const int* idx, const float* teacher, const int* target,
                      const float* weight, int T, int V, int K, int dtype, float temperature,

@@ -537,7 +537,8 @@ extern "C" int hcw_distill_loss(const void* z, const int* idx, const float* teac
         !(temperature > 0.f) || !isfinite(temperature) || !isfinite(kl_scale) ||
         !isfinite(ce_scale))
         return HCW_ERR_INVALID_ARG;
-    if (V > kDMaxV || K > kDMaxK) return HCW_ERR_UNSUPPORTED;
+    // a grid holds the rows times the CTAs of a row
+    if (V > kDMaxV || K > kDMaxK || T > 0x7fffffff / 8) return HCW_ERR_UNSUPPORTED;
     const auto aligned = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; };
     if (!aligned(z) || !aligned(idx) || !aligned(teacher) || !aligned(target) || !aligned(weight) ||
         !aligned(loss) || !aligned(dz))
@@ -560,7 +561,6 @@ extern "C" int hcw_distill_loss(const void* z, const int* idx, const float* teac
     if (!z || (!loss && !dz) || (K > 0) != (idx != nullptr) ||
         (idx != nullptr) != (teacher != nullptr))
         return HCW_ERR_INVALID_ARG;
-    if ((long long)T * 8 > 0x7fffffffll) return HCW_ERR_UNSUPPORTED;   // rows x CTAs of a grid
     DistillArgs a = {};
     a.z = z;
     a.idx = kl_scale != 0.f ? idx : nullptr;

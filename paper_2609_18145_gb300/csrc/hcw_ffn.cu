@@ -1,0 +1,965 @@
+// hcw_ffn.cu -- the gated feed-forward block, bf16 (hcw_gated_ffn_fwd / _bwd):
+//
+//   [g | u] = x W1^T,  a = act(g) u,  y = a W2^T
+//   da = dy W2,  du = da act(g),  dg = da u act'(g)
+//   dx = [dg | du] W1,  dW1 = [dg | du]^T x,  dW2 = dy^T a
+//
+// with x [T][d], W1 [2h][d] (gate rows, then up rows), W2 [d][h].  Bound by the tensor
+// cores: 6 T d h flops forward, 12 T d h backward and 4 T d h more to compute g and u
+// again (the forward saves nothing: its 8 bytes a hidden value would be rounded to bf16
+// once more, or cost more traffic in fp32 than the products take at small d).
+//
+// All products run as pairs of SMs on tcgen05.mma.cta_group::2, operands by TMA
+// into a ring, fp32 accumulators in TMEM, results through shared-memory patches and TMA
+// stores.  A launch is persistent: the pairs take its units (output tiles) in turn.
+//   gate    256 rows x 128 hidden columns: the pair's first CTA loads the gate rows
+//           of W1, the second the up rows, so one MMA of N = 256 gives both projections
+//           of the tile side by side, and the epilogue writes act(g) u, rounded once.
+//           Two accumulators: a tile's epilogue runs under the next tile's products.
+//   grad    the same tile, three accumulators: da (128 columns), then g and u.  da has a
+//           second buffer (512 TMEM columns in all), so that the next tile's da
+//           products run under this tile's epilogue, which writes dg, du and a.
+//   gemm    y, or dx, dW1 and dW2 together: a list of up to three products in one launch,
+//           the units of the longest K first.  A product with few tiles and a long
+//           K splits it; the splits' fp32 partial sums are added in split order by
+//           a second kernel.
+//
+// g, u and da stay in fp32; a, dg and du are rounded to bf16 once, because they are the
+// next products' operands; y, dx, dW1 and dW2 once more when they are stored (dW in fp32
+// on request).  Every wait is bounded as in the library's other tensor-core kernels.
+#include "hcw.h"
+#include "hcw_internal.h"
+#include "hcw_ptx.cuh"
+
+#include <mutex>
+#include <string.h>
+
+namespace hcw {
+
+namespace {
+
+constexpr int kFM = 128;                     // tile rows per CTA (256 per pair)
+constexpr int kFK = 64;                      // K step: one 128-byte row of bf16
+constexpr int kFA = kFM * kFK * 2;           // 16 KB: a CTA's rows of A of a stage
+constexpr int kFStage = 2 * kFA;             // and its columns of B (128 at most)
+constexpr int kFWarps = 8;                   // epilogue warps, two per TMEM lane quarter
+constexpr int kFThreads = 64 + 32 * kFWarps;
+constexpr uint32_t kFTmem = 512;
+constexpr int kFPatch = 4096;                // 32 rows x 128 bytes
+constexpr int kFMaxStages = 5;
+constexpr unsigned long long kFTimeoutNs = 2000000000ull;
+
+enum FfnMode { FFN_GEMM = 0, FFN_GATE = 1, FFN_GRAD = 2 };
+
+// stages of the ring and patches of an epilogue warp
+constexpr int ffn_stages(int mode) { return mode == FFN_GRAD ? 4 : 5; }
+constexpr int ffn_patches(int mode) { return mode == FFN_GRAD ? 3 : 2; }
+
+struct __align__(8) FfnBars {
+    uint64_t full[kFMaxStages];    // leader: both CTAs' copies of a stage landed
+    uint64_t empty[kFMaxStages];   // each CTA: the pair's MMAs have read the stage
+    uint64_t tfull[2];             // each CTA: a unit's accumulators are complete
+    uint64_t tempty[2];            // leader: both CTAs have drained them
+    uint64_t drain;
+    uint32_t tmem_base;
+    int abort;
+};
+
+constexpr size_t ffn_smem(int mode) {
+    return 1024 + (size_t)ffn_stages(mode) * kFStage + (size_t)kFWarps * ffn_patches(mode) * kFPatch +
+           sizeof(FfnBars);
+}
+static_assert(ffn_smem(FFN_GEMM) <= 232448 && ffn_smem(FFN_GRAD) <= 232448, "shared memory");
+
+// A product C[M][N] = A B over K.  Operands as the library's GEMM reads them: K-major rows
+// (box 64 x 128), or MN-major (_mn: a row-major [K][cols] matrix in 64 x 64 boxes).
+struct FfnProd {
+    CUtensorMap mA, mB;
+    CUtensorMap mOut;     // bf16 (N, M) box (64, 32), or fp32 (N, M, splits) box (32, 32, 1)
+    int a_mn, b_mn;
+    int M, N;
+    int bn;               // tile columns: 256 or 128
+    int nkb, kps, splits; // K steps, K steps of a split, splits
+    int mt, nt;           // tiles
+    int unit0;            // first unit
+    int f32;              // fp32 output (mOut)
+};
+
+struct FfnArgs {
+    // FFN_GATE: p[0] = (x, W1) -> a.  FFN_GRAD: p[0] = (dy, W2) with mOut dg,
+    // p[1] = (x, W1) with mOut du, p[2].mOut a.
+    FfnProd p[3];
+    int n_prod, n_units;
+    int h;                // FFN_GATE / FFN_GRAD: hidden columns (first up row of W1)
+    unsigned long long timeout_ns;
+};
+
+__device__ __forceinline__ float ffn_ex2(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float ffn_rcp(float x) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
+// act(g), and in *d its derivative
+template <int ACT>
+__device__ __forceinline__ float ffn_act(float g, float* d) {
+    if (ACT == HCW_GATE_SILU) {
+        const float s = ffn_rcp(1.f + ffn_ex2(g * -1.4426950408889634f));
+        if (d) *d = s * (1.f + g * (1.f - s));
+        return g * s;
+    }
+    if (ACT == HCW_GATE_GELU) {
+        const float c = 0.5f + 0.5f * erff(g * 0.70710678118654752f);
+        if (d) *d = c + g * 0.39894228040143268f * ffn_ex2(g * g * -0.72134752044448170f);
+        return g * c;
+    }
+    if (d) *d = g > 0.f ? 1.f : 0.f;
+    return g > 0.f ? g : 0.f;
+}
+
+template <int MODE, int ACT>
+__global__ void __launch_bounds__(kFThreads, 1) ffn_pair_kernel(const __grid_constant__ FfnArgs a) {
+    constexpr int kStages = ffn_stages(MODE), kPatches = ffn_patches(MODE);
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>(
+        (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    uint8_t* staging = smem + (size_t)kStages * kFStage;
+    FfnBars* bars = reinterpret_cast<FfnBars*>(staging + kFWarps * kPatches * kFPatch);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_ctarank();
+    const int pair = (int)blockIdx.x >> 1, n_pairs = (int)gridDim.x >> 1;
+    const uint64_t tmo = a.timeout_ns;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kStages; ++s) {
+            mbar_init(&bars->full[s], 1);
+            mbar_init(&bars->empty[s], 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&bars->tfull[i], 1);
+            mbar_init(&bars->tempty[i], 2 * kFWarps);
+        }
+        mbar_init(&bars->drain, 1);
+        bars->abort = 0;
+        fence_mbar_init();
+    }
+    if (warp == 1) {
+        tmem_alloc_pair(&bars->tmem_base, kFTmem);
+        tmem_relinquish_pair();
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync_all();   // both CTAs' barriers exist before any cross-CTA arrive
+    tc_fence_after();
+    // nothing before this touches global memory
+    pdl_wait();
+    pdl_trigger();
+    const uint32_t tmem_base = bars->tmem_base;
+    volatile int* abort = &bars->abort;
+
+    // unit -> product, split, row tile, column tile (columns fastest: the pairs that run
+    // together share rows of A)
+    struct Unit {
+        int q, s, mi, ni;
+    };
+    auto unit = [&](int v) {
+        Unit t;
+        t.q = 0;
+        if (MODE == FFN_GEMM)
+            while (t.q + 1 < a.n_prod && v >= a.p[t.q + 1].unit0) ++t.q;
+        const FfnProd& p = a.p[t.q];
+        if (MODE == FFN_GEMM) v -= p.unit0;
+        const int tiles = p.mt * p.nt;
+        t.s = v / tiles;
+        const int rem = v - t.s * tiles;
+        t.mi = rem / p.nt;
+        t.ni = rem - t.mi * p.nt;
+        return t;
+    };
+    // A unit's passes over K: one product, or two for FFN_GRAD.
+    constexpr int kPasses = MODE == FFN_GRAD ? 2 : 1;
+    auto k_range = [&](const FfnProd& p, int s, int& kb0, int& kb1) {
+        kb0 = MODE == FFN_GEMM ? s * p.kps : 0;
+        kb1 = MODE == FFN_GEMM && kb0 + p.kps < p.nkb ? kb0 + p.kps : p.nkb;
+    };
+
+    if (warp == 0) {
+        // ------------------------------------------------------------ producer (both CTAs)
+        if (lane == 0) {
+            int stage = 0;
+            uint32_t phase = 0, issued_mask = 0, issued_phase = 0;
+            bool ok = true;
+            for (int v = pair; v < a.n_units && ok; v += n_pairs) {
+                const Unit t = unit(v);
+                for (int pass = 0; pass < kPasses && ok; ++pass) {
+                    const FfnProd& p = a.p[MODE == FFN_GEMM ? t.q : pass];
+                    int kb0, kb1;
+                    k_range(p, t.s, kb0, kb1);
+                    const int a_mn = p.a_mn, b_mn = p.b_mn;
+                    const int bc = p.bn / 2;   // this CTA's columns of B
+                    // FFN_GATE and the second pass of FFN_GRAD: gate rows on one CTA, up
+                    // rows on the other
+                    const bool split_b = MODE == FFN_GATE || (MODE == FFN_GRAD && pass == 1);
+                    const int a_row = (2 * t.mi + (int)rank) * kFM;
+                    const int b_row = split_b ? (int)rank * a.h + t.ni * 128
+                                              : t.ni * p.bn + (int)rank * bc;
+                    const uint32_t tx = 2u * (uint32_t)(kFA + bc * kFK * 2);
+                    for (int kb = kb0; kb < kb1; ++kb) {
+                        if (!mbar_wait(&bars->empty[stage], phase ^ 1, abort, tmo)) {
+                            ok = false;
+                            break;
+                        }
+                        uint8_t* sA = smem + (size_t)stage * kFStage;
+                        uint8_t* sB = sA + kFA;
+                        if (rank == 0) mbar_arrive_expect_tx(&bars->full[stage], tx);
+                        issued_mask |= 1u << stage;
+                        issued_phase = (issued_phase & ~(1u << stage)) | (phase << stage);
+                        const uint32_t fb = mapa_shared(&bars->full[stage], 0);
+                        const int k = kb * kFK;
+                        if (a_mn) {
+                            tma_load_2d_pair(sA, &p.mA, fb, a_row, k);
+                            tma_load_2d_pair(sA + 8192, &p.mA, fb, a_row + 64, k);
+                        } else {
+                            tma_load_2d_pair(sA, &p.mA, fb, k, a_row);
+                        }
+                        if (b_mn) {
+                            tma_load_2d_pair(sB, &p.mB, fb, b_row, k);
+                            if (bc > 64) tma_load_2d_pair(sB + 8192, &p.mB, fb, b_row + 64, k);
+                        } else {
+                            tma_load_2d_pair(sB, &p.mB, fb, k, b_row);
+                        }
+                        if (++stage == kStages) {
+                            stage = 0;
+                            phase ^= 1;
+                        }
+                    }
+                }
+            }
+            if (!ok && rank == 0)
+                // every copy of the pair completes on the leader's barriers
+                for (int s = 0; s < kStages; ++s)
+                    if (issued_mask & (1u << s))
+                        mbar_wait_drain(&bars->full[s], (issued_phase >> s) & 1u, tmo);
+        }
+    } else if (warp == 1) {
+        // ------------------------------------------------------------ MMA issuer (leader)
+        if (lane == 0 && rank == 0) {
+            int stage = 0, it = 0;
+            uint32_t phase = 0;
+            bool ok = true, any = false;
+            for (int v = pair; v < a.n_units && ok; v += n_pairs, ++it) {
+                const Unit t = unit(v);
+                for (int pass = 0; pass < kPasses && ok; ++pass) {
+                    const FfnProd& p = a.p[MODE == FFN_GEMM ? t.q : pass];
+                    int kb0, kb1;
+                    k_range(p, t.s, kb0, kb1);
+                    const uint32_t idesc = idesc_bf16_f32(2 * kFM, p.bn, p.a_mn, p.b_mn);
+                    // bytes from one 16-deep step to the next within a stage
+                    const uint32_t a_step = p.a_mn ? 2048 : 32, b_step = p.b_mn ? 2048 : 32;
+                    const uint32_t a_lbo = p.a_mn ? 8192 : 16, b_lbo = p.b_mn ? 8192 : 16;
+                    uint32_t d_tmem;
+                    if (MODE != FFN_GRAD) {
+                        // accumulator it % 2: drained of unit it - 2
+                        if (!mbar_wait(&bars->tempty[it & 1], ((it >> 1) & 1) ^ 1, abort, tmo))
+                            ok = false;
+                        d_tmem = tmem_base + (uint32_t)(it & 1) * 256;
+                    } else if (pass == 0) {
+                        // da, buffer it % 2: its unit it - 2 was drained before the g, u
+                        // products of unit it - 1 began
+                        d_tmem = tmem_base + (uint32_t)(it & 1) * 128;
+                    } else {
+                        // g and u: drained of unit it - 1
+                        if (!mbar_wait(&bars->tempty[0], (it & 1) ^ 1, abort, tmo)) ok = false;
+                        d_tmem = tmem_base + 256;
+                    }
+                    if (!ok) break;
+                    tc_fence_after();
+                    for (int kb = kb0; kb < kb1; ++kb) {
+                        if (!mbar_wait(&bars->full[stage], phase, abort, tmo)) {
+                            ok = false;
+                            break;
+                        }
+                        tc_fence_after();
+                        const uint32_t sa = smem_u32(smem + (size_t)stage * kFStage);
+                        const uint32_t sb = sa + kFA;
+#pragma unroll
+                        for (int kk = 0; kk < kFK / 16; ++kk)
+                            mma_bf16_f32_pair(d_tmem, smem_desc_sw128(sa + kk * a_step, a_lbo, 1024),
+                                              smem_desc_sw128(sb + kk * b_step, b_lbo, 1024), idesc,
+                                              (kb != kb0 || kk != 0) ? 1u : 0u);
+                        any = true;
+                        mma_commit_pair(&bars->empty[stage], 3);
+                        if (++stage == kStages) {
+                            stage = 0;
+                            phase ^= 1;
+                        }
+                    }
+                }
+                if (ok) mma_commit_pair(&bars->tfull[it & 1], 3);
+            }
+            if (any) {
+                // the pair's MMAs have completed before TMEM can be freed
+                mma_commit_pair(&bars->drain, 1);
+                mbar_wait_drain(&bars->drain, 0, tmo);
+            }
+        }
+    } else {
+        // ------------------------------------------------------------ epilogue (both CTAs)
+        // warp e drains TMEM lane quarter warp % 4 (rows 32 q .. 32 q + 31 of this CTA's
+        // 128) and half e / 4 of the unit's columns
+        const int e = warp - 2;
+        const int quarter = warp & 3, chalf = e >> 2;
+        const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+        uint8_t* const patches = staging + (size_t)e * kPatches * kFPatch;
+        // 16-byte chunk m of row r of a 128-byte-swizzled patch
+        auto chunk = [](uint8_t* buf, int r, int m) {
+            return reinterpret_cast<uint4*>(buf + r * 128 + ((m ^ (r & 7)) << 4));
+        };
+        int it = 0, nbuf = 0;
+        for (int v = pair; v < a.n_units; v += n_pairs, ++it) {
+            const Unit t = unit(v);
+            const FfnProd& p = a.p[MODE == FFN_GEMM ? t.q : 0];
+            const int row0 = (2 * t.mi + (int)rank) * kFM + quarter * 32;
+            const bool okw = mbar_wait(&bars->tfull[it & 1], (it >> 1) & 1, abort, tmo);
+            if (!__all_sync(0xffffffffu, okw)) break;
+            tc_fence_after();
+            const uint32_t tempty =
+                mapa_shared(&bars->tempty[MODE == FFN_GRAD ? 0 : it & 1], 0);
+            auto release = [&]() {   // this warp has read the unit's accumulators
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_remote_tmem(tempty);
+            };
+            if (MODE == FFN_GEMM) {
+                const int cw = p.bn / 2;                       // the warp's columns
+                const int colw = t.ni * p.bn + chalf * cw;
+                const uint32_t tb = tmem_base + lanes + (uint32_t)((it & 1) * 256 + chalf * cw);
+#pragma unroll 1
+                for (int c = 0; c < cw; c += 32) {
+                    const bool st = row0 < p.M && colw + c < p.N;   // warp-uniform
+                    uint32_t r[32];
+                    if (st) {
+                        __syncwarp();
+                        tmem_ld_32x32b_x32(tb + (uint32_t)c, r);
+                        tmem_ld_wait_regs(r);
+                    }
+                    if (c + 32 == cw) release();
+                    if (!st) continue;
+                    // fp32: a patch of 32 columns each time; bf16: of 64, filled in two
+                    const int part = p.f32 ? 0 : (c >> 5) & 1;
+                    uint8_t* buf = patches + nbuf * kFPatch;
+                    if (part == 0) {
+                        if (lane == 0) bulk_wait_read<1>();   // its store of two patches ago
+                        __syncwarp();
+                    }
+                    if (p.f32) {
+#pragma unroll
+                        for (int m = 0; m < 8; ++m)
+                            *chunk(buf, lane, m) =
+                                make_uint4(r[4 * m], r[4 * m + 1], r[4 * m + 2], r[4 * m + 3]);
+                    } else {
+#pragma unroll
+                        for (int m = 0; m < 4; ++m) {
+                            uint32_t w[4];
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
+                                w[j] = pack_bf16x2(__uint_as_float(r[8 * m + 2 * j]),
+                                                   __uint_as_float(r[8 * m + 2 * j + 1]));
+                            *chunk(buf, lane, 4 * part + m) = make_uint4(w[0], w[1], w[2], w[3]);
+                        }
+                    }
+                    // a bf16 patch whose second half holds no column of C goes out half full
+                    // (TMA drops the columns past C's end)
+                    if (!p.f32 && part == 0 && colw + c + 32 < p.N) continue;
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) {
+                        if (p.f32)
+                            tma_store_3d(&p.mOut, buf, colw + c, row0, t.s);
+                        else
+                            tma_store_2d(&p.mOut, buf, colw + (c & ~63), row0);
+                        bulk_commit();
+                    }
+                    nbuf ^= 1;
+                }
+                continue;
+            }
+            const int col = t.ni * 128 + chalf * 64;   // the warp's 64 hidden columns
+            const bool st = row0 < p.M && col < a.h;
+            if (!st) {
+                release();
+                continue;
+            }
+            if (MODE == FFN_GATE) {
+                const uint32_t tg = tmem_base + lanes + (uint32_t)((it & 1) * 256 + chalf * 64);
+                uint8_t* buf = patches + nbuf * kFPatch;
+                nbuf ^= 1;
+                if (lane == 0) bulk_wait_read<1>();
+                __syncwarp();
+#pragma unroll 1
+                for (int c = 0; c < 64; c += 32) {
+                    uint32_t g[32], u[32];
+                    __syncwarp();
+                    tmem_ld_32x32b_x32(tg + (uint32_t)c, g);
+                    tmem_ld_32x32b_x32(tg + (uint32_t)(128 + c), u);
+                    tmem_ld_wait_regs(g);
+                    tmem_ld_wait_regs(u);
+                    if (c) release();
+#pragma unroll
+                    for (int m = 0; m < 4; ++m) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const int i = 8 * m + 2 * j;
+                            w[j] = pack_bf16x2(
+                                ffn_act<ACT>(__uint_as_float(g[i]), nullptr) * __uint_as_float(u[i]),
+                                ffn_act<ACT>(__uint_as_float(g[i + 1]), nullptr) *
+                                    __uint_as_float(u[i + 1]));
+                        }
+                        *chunk(buf, lane, (c >> 3) + m) = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
+                }
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) {
+                    tma_store_2d(&p.mOut, buf, col, row0);
+                    bulk_commit();
+                }
+            } else {
+                const uint32_t td = tmem_base + lanes + (uint32_t)((it & 1) * 128 + chalf * 64);
+                const uint32_t tg = tmem_base + lanes + (uint32_t)(256 + chalf * 64);
+                if (lane == 0) bulk_wait_read<0>();   // the last unit's three patches
+                __syncwarp();
+#pragma unroll 1
+                for (int c = 0; c < 64; c += 32) {
+                    uint32_t d[32], g[32], u[32];
+                    __syncwarp();
+                    tmem_ld_32x32b_x32(td + (uint32_t)c, d);
+                    tmem_ld_32x32b_x32(tg + (uint32_t)c, g);
+                    tmem_ld_32x32b_x32(tg + (uint32_t)(128 + c), u);
+                    tmem_ld_wait_regs(d);
+                    tmem_ld_wait_regs(g);
+                    tmem_ld_wait_regs(u);
+                    if (c) release();
+#pragma unroll
+                    for (int m = 0; m < 4; ++m) {
+                        uint32_t wg[4], wu[4], wa[4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            float og[2], ou[2], oa[2];
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) {
+                                const int q = 8 * m + 2 * j + i;
+                                const float da = __uint_as_float(d[q]), uu = __uint_as_float(u[q]);
+                                float dact;
+                                const float ag = ffn_act<ACT>(__uint_as_float(g[q]), &dact);
+                                og[i] = da * uu * dact;
+                                ou[i] = da * ag;
+                                oa[i] = ag * uu;
+                            }
+                            wg[j] = pack_bf16x2(og[0], og[1]);
+                            wu[j] = pack_bf16x2(ou[0], ou[1]);
+                            wa[j] = pack_bf16x2(oa[0], oa[1]);
+                        }
+                        const int k = (c >> 3) + m;
+                        *chunk(patches, lane, k) = make_uint4(wg[0], wg[1], wg[2], wg[3]);
+                        *chunk(patches + kFPatch, lane, k) = make_uint4(wu[0], wu[1], wu[2], wu[3]);
+                        *chunk(patches + 2 * kFPatch, lane, k) =
+                            make_uint4(wa[0], wa[1], wa[2], wa[3]);
+                    }
+                }
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) {
+                    tma_store_2d(&a.p[0].mOut, patches, col, row0);
+                    tma_store_2d(&a.p[1].mOut, patches + kFPatch, col, row0);
+                    tma_store_2d(&a.p[2].mOut, patches + 2 * kFPatch, col, row0);
+                    bulk_commit();
+                }
+            }
+        }
+        // every store of this warp is complete before the CTA exits
+        if (lane == 0) bulk_wait<0>();
+        __syncwarp();
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync_all();   // neither CTA frees the pair's TMEM while the other uses it
+    if (warp == 1) {
+        __syncwarp();
+        tc_fence_after();
+        tmem_dealloc_pair(tmem_base, kFTmem);
+    }
+}
+
+// out[i] = sum over the splits, in order, of part[s][i] (zero without splits), for up to
+// three matrices of a multiple of four elements, one after the other.
+struct FfnReduce {
+    struct {
+        const float* part;
+        void* out;
+        size_t count4;   // groups of four
+        int splits, f32;
+    } m[3];
+};
+
+__global__ void __launch_bounds__(256) ffn_reduce_kernel(const FfnReduce a) {
+    pdl_wait();
+    pdl_trigger();
+    for (int q = 0; q < 3; ++q) {
+        const auto& m = a.m[q];
+        for (size_t i = blockIdx.x * (size_t)blockDim.x + threadIdx.x; i < m.count4;
+             i += (size_t)gridDim.x * blockDim.x) {
+            float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int s = 0; s < m.splits; ++s) {
+                const float4 v = reinterpret_cast<const float4*>(m.part)[(size_t)s * m.count4 + i];
+                t.x += v.x;
+                t.y += v.y;
+                t.z += v.z;
+                t.w += v.w;
+            }
+            if (m.f32)
+                reinterpret_cast<float4*>(m.out)[i] = t;
+            else
+                reinterpret_cast<uint2*>(m.out)[i] =
+                    make_uint2(pack_bf16x2(t.x, t.y), pack_bf16x2(t.z, t.w));
+        }
+    }
+}
+
+// ------------------------------------------------------------------ host
+typedef CUresult (*FfnEncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*,
+                                const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+FfnEncodeFn ffn_encode() {
+    static FfnEncodeFn fn = nullptr;
+    static std::once_flag once;
+    std::call_once(once, [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000,
+                                             cudaEnableDefault, &q) == cudaSuccess &&
+            q == cudaDriverEntryPointSuccess)
+            fn = reinterpret_cast<FfnEncodeFn>(p);
+    });
+    return fn;
+}
+
+// bf16 [rows][cols], ld elements from row to row, in boxes of box_c x box_r
+bool ffn_map(CUtensorMap* m, const void* base, long long rows, long long cols, long long ld,
+             int box_c, int box_r) {
+    FfnEncodeFn enc = ffn_encode();
+    if (!enc) return false;
+    cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+    cuuint64_t strides[1] = {(cuuint64_t)ld * 2};
+    cuuint32_t box[2] = {(cuuint32_t)box_c, (cuuint32_t)box_r};
+    cuuint32_t estr[2] = {1, 1};
+    return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box,
+               estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+               CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// fp32 [splits][M][N] in patches of 32 x 32
+bool ffn_map_f32(CUtensorMap* m, void* base, int M, int N, int splits) {
+    FfnEncodeFn enc = ffn_encode();
+    if (!enc) return false;
+    cuuint64_t dims[3] = {(cuuint64_t)N, (cuuint64_t)M, (cuuint64_t)splits};
+    cuuint64_t strides[2] = {(cuuint64_t)N * 4, (cuuint64_t)M * N * 4};
+    cuuint32_t box[3] = {32, 32, 1};
+    cuuint32_t estr[3] = {1, 1, 1};
+    return enc(m, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, base, dims, strides, box, estr,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+               CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+int ffn_sms() {
+    int dev = 0, n = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess ||
+        cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 2)
+        return 148;
+    return n;
+}
+
+// An operand: K-major (the row-major [outer][K] matrix) or MN-major (row-major [K][outer]).
+bool ffn_operand(CUtensorMap* m, const void* base, long long outer, long long K, bool mn, int rows) {
+    return mn ? ffn_map(m, base, K, outer, outer, 64, 64) : ffn_map(m, base, outer, K, K, 64, rows);
+}
+
+template <int MODE, int ACT>
+cudaError_t ffn_launch(const FfnArgs& a, int pairs, cudaStream_t st) {
+    auto kern = ffn_pair_kernel<MODE, ACT>;
+    static std::once_flag once[64];
+    static cudaError_t set_err[64];
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+    std::call_once(once[dev], [&] {
+        set_err[dev] = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                            (int)ffn_smem(MODE));
+    });
+    if (set_err[dev] != cudaSuccess) return set_err[dev];
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(2 * pairs));
+    cfg.blockDim = dim3((unsigned)kFThreads);
+    cfg.dynamicSmemBytes = ffn_smem(MODE);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 2;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, kern, a);
+}
+
+template <int MODE>
+cudaError_t ffn_launch_act(int act, const FfnArgs& a, int pairs, cudaStream_t st) {
+    switch (act) {
+        case HCW_GATE_SILU: return ffn_launch<MODE, HCW_GATE_SILU>(a, pairs, st);
+        case HCW_GATE_GELU: return ffn_launch<MODE, HCW_GATE_GELU>(a, pairs, st);
+        default: return ffn_launch<MODE, HCW_GATE_RELU>(a, pairs, st);
+    }
+}
+
+// One product of a gemm launch, as the planner sees it.
+struct FfnShape {
+    long long M, N, K;
+    int out_f32;       // the output itself is fp32
+    // filled by the plan
+    int bn, nkb, kps, splits;
+};
+
+// Tile columns and K splits of the products of one launch on `pairs` pairs: over a range of
+// unit lengths L (K steps), the least of
+//   the units' K steps spread over the pairs, half a longest unit for the uneven end, no
+//   less than one longest unit, at 0.3 us a step (256 columns), and
+//   the fp32 partials written and read at 6 TB/s, and 3 us for the kernel that adds them.
+void ffn_plan(FfnShape* s, int n, int pairs) {
+    double best = 1e30;
+    for (int L = 4; L <= 1 << 20; L = L < 64 ? L + 4 : L * 2) {
+        double total = 0, longest = 0, bytes = 0;
+        bool capped = true;
+        FfnShape t[3];
+        for (int i = 0; i < n; ++i) {
+            t[i] = s[i];
+            t[i].bn = s[i].N <= 128 ? 128 : 256;
+            t[i].nkb = (int)((s[i].K + kFK - 1) / kFK);
+            int sp = (t[i].nkb + L - 1) / L;
+            if (sp > 64) sp = 64;
+            t[i].kps = (t[i].nkb + sp - 1) / sp;
+            t[i].splits = (t[i].nkb + t[i].kps - 1) / t[i].kps;
+            const double tiles = (double)((s[i].M + 255) / 256) * ((s[i].N + t[i].bn - 1) / t[i].bn);
+            const double step = t[i].bn == 256 ? 1.0 : 0.75;
+            total += tiles * t[i].nkb * step + tiles * t[i].splits * 2;   // 2: a unit's own part
+            if (t[i].kps * step + 2 > longest) longest = t[i].kps * step + 2;
+            if (t[i].splits > 1) {
+                bytes += (double)t[i].splits * s[i].M * s[i].N * 8;
+                capped = false;
+            }
+        }
+        double us = total / pairs + 0.5 * longest;
+        if (us < longest) us = longest;
+        us = us * 0.3 + bytes / 6.0e6 + (bytes > 0 ? 3.0 : 0.0);
+        if (us < best) {
+            best = us;
+            for (int i = 0; i < n; ++i) s[i] = t[i];
+        }
+        if (capped) break;   // longer units change nothing
+    }
+}
+
+size_t ffn_round(size_t n) { return (n + 255) & ~(size_t)255; }
+
+size_t ffn_part_bytes(const FfnShape* s, int n) {
+    size_t b = 0;
+    for (int i = 0; i < n; ++i)
+        if (s[i].splits > 1) b += ffn_round((size_t)s[i].splits * s[i].M * s[i].N * 4);
+    return b;
+}
+
+struct FfnOperands {
+    const void* A;
+    bool a_mn;
+    const void* B;
+    bool b_mn;
+    void* out;
+};
+
+// The products of one launch (planned), and the launch that adds their splits.
+int ffn_gemms(const FfnShape* s, const FfnOperands* o, int n, uint8_t* part, cudaStream_t st) {
+    FfnArgs a;
+    memset(&a, 0, sizeof(a));
+    FfnReduce r;
+    memset(&r, 0, sizeof(r));
+    // the products with the longest units first
+    int order[3] = {0, 1, 2};
+    for (int i = 0; i < n; ++i)
+        for (int j = i + 1; j < n; ++j)
+            if (s[order[j]].kps > s[order[i]].kps) {
+                const int k = order[i];
+                order[i] = order[j];
+                order[j] = k;
+            }
+    int units = 0, n_red = 0;
+    size_t most = 0;
+    for (int i = 0; i < n; ++i) {
+        const FfnShape& t = s[order[i]];
+        const FfnOperands& q = o[order[i]];
+        FfnProd& p = a.p[i];
+        p.a_mn = q.a_mn;
+        p.b_mn = q.b_mn;
+        p.M = (int)t.M;
+        p.N = (int)t.N;
+        p.bn = t.bn;
+        p.nkb = t.nkb;
+        p.kps = t.kps;
+        p.splits = t.splits;
+        p.mt = (int)((t.M + 255) / 256);
+        p.nt = (int)((t.N + t.bn - 1) / t.bn);
+        p.unit0 = units;
+        units += p.mt * p.nt * p.splits;
+        void* out = q.out;
+        p.f32 = t.out_f32 || t.splits > 1;
+        if (t.splits > 1) {
+            auto& m = r.m[n_red++];
+            m.part = reinterpret_cast<const float*>(part);
+            m.out = q.out;
+            m.count4 = (size_t)t.M * t.N / 4;
+            m.splits = t.splits;
+            m.f32 = t.out_f32;
+            most = m.count4 > most ? m.count4 : most;
+            out = part;
+            part += ffn_round((size_t)t.splits * t.M * t.N * 4);
+        }
+        if (!ffn_operand(&p.mA, q.A, t.M, t.K, q.a_mn, kFM) ||
+            !ffn_operand(&p.mB, q.B, t.N, t.K, q.b_mn, t.bn / 2) ||
+            !(p.f32 ? ffn_map_f32(&p.mOut, out, p.M, p.N, p.splits)
+                    : ffn_map(&p.mOut, out, p.M, p.N, p.N, 64, 32)))
+            return HCW_ERR_CUDA;
+    }
+    a.n_prod = n;
+    a.n_units = units;
+    a.timeout_ns = kFTimeoutNs;
+    const int sms = ffn_sms();
+    int rc = count_launch(ffn_launch<FFN_GEMM, 0>(a, units < sms / 2 ? units : sms / 2, st), 1);
+    if (rc || !n_red) return rc;
+    const size_t want = (most + 255) / 256, cap = (size_t)sms * 8;
+    return count_launch(launch_pdl(ffn_reduce_kernel, dim3((unsigned)(want < cap ? want : cap)),
+                                   dim3(256), 0, st, r), 1);
+}
+
+// Forward workspace: a [T][h] bf16, then the partial sums of y.
+FfnShape ffn_down_shape(int T, int d, int h) {
+    FfnShape s = {T, d, h, 0, 0, 0, 0, 0};
+    ffn_plan(&s, 1, ffn_sms() / 2);
+    return s;
+}
+
+struct FfnBwdWs {
+    size_t act, part, bytes;   // dgu at 0
+    FfnShape s[3];
+    int n;
+};
+
+FfnBwdWs ffn_bwd_ws(int T, int d, int h, bool dx, bool dw, bool f32) {
+    FfnBwdWs w;
+    w.n = 0;
+    if (dx) w.s[w.n++] = {T, d, 2ll * h, 0, 0, 0, 0, 0};
+    if (dw) {
+        w.s[w.n++] = {2ll * h, d, T, f32, 0, 0, 0, 0};
+        w.s[w.n++] = {d, h, T, f32, 0, 0, 0, 0};
+    }
+    ffn_plan(w.s, w.n, ffn_sms() / 2);
+    w.act = ffn_round((size_t)T * 2 * h * 2);
+    w.part = w.act + ffn_round((size_t)T * h * 2);
+    w.bytes = w.part + ffn_part_bytes(w.s, w.n);
+    return w;
+}
+
+bool ffn_aligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+struct FfnSpan {
+    const void* p;
+    size_t n;
+};
+
+bool ffn_meet(const FfnSpan& a, const FfnSpan& b) {
+    if (!a.p || !b.p || !a.n || !b.n) return false;
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+    return x < y + b.n && y < x + a.n;
+}
+
+int ffn_sizes(int T, int d, int h, int act) {
+    if (T < 0 || d < 1 || h < 1 || (act != HCW_GATE_SILU && act != HCW_GATE_GELU && act != HCW_GATE_RELU))
+        return HCW_ERR_INVALID_ARG;
+    // TMA reads rows of a multiple of 16 bytes; the tiles of a product are counted in ints
+    if (d % 8 || h % 8 || d > (1 << 20) || h > (1 << 20)) return HCW_ERR_UNSUPPORTED;
+    return HCW_OK;
+}
+
+int ffn_check(const FfnSpan* in, int n_in, const FfnSpan* out, int n_out) {
+    for (int i = 0; i < n_in; ++i)
+        if (!ffn_aligned(in[i].p)) return HCW_ERR_ALIGNMENT;
+    for (int i = 0; i < n_out; ++i)
+        if (!ffn_aligned(out[i].p)) return HCW_ERR_ALIGNMENT;
+    for (int i = 0; i < n_out; ++i) {
+        for (int j = 0; j < n_in; ++j)
+            if (ffn_meet(out[i], in[j])) return HCW_ERR_ALIASING;
+        for (int j = i + 1; j < n_out; ++j)
+            if (ffn_meet(out[i], out[j])) return HCW_ERR_ALIASING;
+    }
+    return HCW_OK;
+}
+
+}  // namespace
+
+cudaError_t ffn_error_word_read_clear(int* word) {
+    const int zero = 0;
+    cudaError_t e = cudaMemcpyFromSymbol(word, g_error_word, sizeof(int));
+    if (e == cudaSuccess && *word) e = cudaMemcpyToSymbol(g_error_word, &zero, sizeof(int));
+    return e;
+}
+
+}  // namespace hcw
+
+using namespace hcw;
+
+extern "C" {
+
+size_t hcw_gated_ffn_fwd_workspace_bytes(int T, int d, int h) {
+    if (T < 1 || ffn_sizes(T, d, h, HCW_GATE_SILU)) return 0;
+    const FfnShape s = ffn_down_shape(T, d, h);
+    return ffn_round((size_t)T * h * 2) + ffn_part_bytes(&s, 1);
+}
+
+int hcw_gated_ffn_fwd(const void* x, const void* W1, const void* W2, int T, int d, int h, int act,
+                      void* y, void* workspace, size_t ws_bytes, void* stream) {
+    int rc = ffn_sizes(T, d, h, act);
+    if (rc) return rc;
+    const size_t xb = (size_t)T * d * 2, wb = (size_t)d * h * 2;
+    const FfnSpan in[] = {{x, xb}, {W1, 2 * wb}, {W2, wb}};
+    const FfnSpan out[] = {{y, xb}, {workspace, workspace ? ws_bytes : 0}};
+    rc = ffn_check(in, 3, out, 2);
+    if (rc) return rc;
+    if (T == 0) return HCW_OK;
+    if (!x || !W1 || !W2 || !y) return HCW_ERR_INVALID_ARG;
+    FfnShape s = ffn_down_shape(T, d, h);
+    const size_t act_bytes = ffn_round((size_t)T * h * 2);
+    if (!workspace || ws_bytes < act_bytes + ffn_part_bytes(&s, 1)) return HCW_ERR_WORKSPACE;
+    const cudaStream_t st = (cudaStream_t)stream;
+    const int pairs = ffn_sms() / 2;
+    FfnArgs a;
+    memset(&a, 0, sizeof(a));
+    FfnProd& p = a.p[0];
+    p.M = T;
+    p.N = h;
+    p.bn = 256;
+    p.nkb = (d + kFK - 1) / kFK;
+    p.mt = (T + 255) / 256;
+    p.nt = (h + 127) / 128;
+    a.n_prod = 1;
+    a.n_units = p.mt * p.nt;
+    a.h = h;
+    a.timeout_ns = kFTimeoutNs;
+    if (!ffn_operand(&p.mA, x, T, d, false, kFM) || !ffn_operand(&p.mB, W1, 2ll * h, d, false, 128) ||
+        !ffn_map(&p.mOut, workspace, T, h, h, 64, 32))
+        return HCW_ERR_CUDA;
+    rc = count_launch(ffn_launch_act<FFN_GATE>(act, a, a.n_units < pairs ? a.n_units : pairs, st), 1);
+    if (rc) return rc;
+    const FfnOperands o = {workspace, false, W2, false, y};
+    return ffn_gemms(&s, &o, 1, static_cast<uint8_t*>(workspace) + act_bytes, st);
+}
+
+size_t hcw_gated_ffn_bwd_workspace_bytes(int T, int d, int h) {
+    if (T < 1 || ffn_sizes(T, d, h, HCW_GATE_SILU)) return 0;
+    size_t most = 0;
+    // whichever outputs a call asks for
+    for (int k = 1; k < 4; ++k) {
+        const size_t b = ffn_bwd_ws(T, d, h, k & 1, k & 2, false).bytes;
+        most = b > most ? b : most;
+    }
+    return most;
+}
+
+int hcw_gated_ffn_bwd(const void* x, const void* dy, const void* W1, const void* W2, int T, int d,
+                      int h, int act, int dw_dtype, void* dx, void* dW1, void* dW2,
+                      void* workspace, size_t ws_bytes, void* stream) {
+    int rc = ffn_sizes(T, d, h, act);
+    if (rc) return rc;
+    if (dw_dtype != HCW_BF16 && dw_dtype != HCW_F32) return HCW_ERR_INVALID_ARG;
+    const bool f32 = dw_dtype == HCW_F32;
+    const size_t xb = (size_t)T * d * 2, wb = (size_t)d * h * 2, gb = f32 ? 2 * wb : wb;
+    const FfnSpan in[] = {{x, xb}, {dy, xb}, {W1, 2 * wb}, {W2, wb}};
+    const FfnSpan out[] = {{dx, xb}, {dW1, 2 * gb}, {dW2, gb}, {workspace, workspace ? ws_bytes : 0}};
+    rc = ffn_check(in, 4, out, 4);
+    if (rc) return rc;
+    if (!dW1 != !dW2) return HCW_ERR_INVALID_ARG;
+    const cudaStream_t st = (cudaStream_t)stream;
+    if (T == 0) {
+        if (!dW1) return HCW_OK;
+        FfnReduce r;   // no tokens: the weight gradients are zero
+        memset(&r, 0, sizeof(r));
+        r.m[0].out = dW1;
+        r.m[0].count4 = (size_t)2 * d * h / 4;
+        r.m[1].out = dW2;
+        r.m[1].count4 = (size_t)d * h / 4;
+        r.m[0].f32 = r.m[1].f32 = f32;
+        return count_launch(launch_pdl(ffn_reduce_kernel, dim3((unsigned)ffn_sms() * 4), dim3(256), 0,
+                                       st, r), 1);
+    }
+    if (!x || !dy || !W1 || !W2 || (!dx && !dW1)) return HCW_ERR_INVALID_ARG;
+    const FfnBwdWs w = ffn_bwd_ws(T, d, h, dx != nullptr, dW1 != nullptr, f32);
+    if (!workspace || ws_bytes < w.bytes) return HCW_ERR_WORKSPACE;
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    const int pairs = ffn_sms() / 2;
+    FfnArgs a;
+    memset(&a, 0, sizeof(a));
+    for (int i = 0; i < 2; ++i) {
+        FfnProd& p = a.p[i];
+        p.M = T;
+        p.N = h;
+        p.bn = i == 0 ? 128 : 256;
+        p.b_mn = i == 0;
+        p.nkb = (d + kFK - 1) / kFK;
+        p.mt = (T + 255) / 256;
+        p.nt = (h + 127) / 128;
+    }
+    a.n_prod = 2;
+    a.n_units = a.p[0].mt * a.p[0].nt;
+    a.h = h;
+    a.timeout_ns = kFTimeoutNs;
+    if (!ffn_operand(&a.p[0].mA, dy, T, d, false, kFM) ||
+        !ffn_operand(&a.p[0].mB, W2, h, d, true, 0) ||
+        !ffn_operand(&a.p[1].mA, x, T, d, false, kFM) ||
+        !ffn_operand(&a.p[1].mB, W1, 2ll * h, d, false, 128) ||
+        !ffn_map(&a.p[0].mOut, ws, T, h, 2ll * h, 64, 32) ||
+        !ffn_map(&a.p[1].mOut, ws + (size_t)h * 2, T, h, 2ll * h, 64, 32) ||
+        !ffn_map(&a.p[2].mOut, ws + w.act, T, h, h, 64, 32))
+        return HCW_ERR_CUDA;
+    rc = count_launch(ffn_launch_act<FFN_GRAD>(act, a, a.n_units < pairs ? a.n_units : pairs, st), 1);
+    if (rc) return rc;
+    FfnOperands o[3];
+    int n = 0;
+    if (dx) o[n++] = {ws, false, W1, true, dx};
+    if (dW1) {
+        o[n++] = {ws, true, x, true, dW1};
+        o[n++] = {dy, true, ws + w.act, true, dW2};
+    }
+    return ffn_gemms(w.s, o, n, ws + w.part, st);
+}
+
+}  // extern "C"

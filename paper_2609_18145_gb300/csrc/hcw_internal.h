@@ -356,6 +356,10 @@ cudaError_t block_error_word_read_clear(int* word);
 // (the launch counter lives with the C API in hcw_api.cu).
 int count_launch(cudaError_t e, int kernels);
 
+// ---- Gated feed-forward block (hcw_ffn.cu) ----
+// Read its kernels' error word and reset it to 0 (synchronous).
+cudaError_t ffn_error_word_read_clear(int* word);
+
 // ---- Distillation loss (hcw_distill.cu) ----
 // Read its kernels' error word and reset it to 0 (synchronous).
 cudaError_t distill_error_word_read_clear(int* word);

@@ -40,6 +40,10 @@ HCW_CAUSAL = 1
 HCW_RESIDUAL = 2
 HCW_ACT_RELU = 4
 
+HCW_GATE_SILU = 0
+HCW_GATE_GELU = 1
+HCW_GATE_RELU = 2
+
 HCW_NORM_NONE = 0
 HCW_NORM_RMS = 1
 HCW_NORM_LAYER = 2
@@ -102,6 +106,10 @@ _SIGNATURES = {
     "hcw_gemm_bf16": ([_I, _I, _I, _P, _I, _P, _I, _P, _P, _SZ, _P], _I),
     "hcw_gemm_bf16_batched": ([_I, _I, _I, _P, ctypes.c_longlong, _P, ctypes.c_longlong, _P, _I,
                                _P], _I),
+    "hcw_gated_ffn_fwd_workspace_bytes": ([_I, _I, _I], _SZ),
+    "hcw_gated_ffn_fwd": ([_P, _P, _P, _I, _I, _I, _I, _P, _P, _SZ, _P], _I),
+    "hcw_gated_ffn_bwd_workspace_bytes": ([_I, _I, _I], _SZ),
+    "hcw_gated_ffn_bwd": ([_P, _P, _P, _P, _I, _I, _I, _I, _I, _P, _P, _P, _P, _SZ, _P], _I),
     "hcw_residual_norm_fwd": ([_P, _P, _P, _I, _F, _I, _P, _P, _I, _P, _P, _F, _I, _I, _I, _P, _P,
                                _P], _I),
     "hcw_residual_norm_bwd_workspace_bytes": ([_I, _I, _I], _SZ),
@@ -421,6 +429,76 @@ def _numel(what, n, *ts):
     for t in ts:
         if t is not None and t.numel() != n:
             raise ValueError("%s: expected %d elements, got %s" % (what, n, tuple(t.shape)))
+
+
+def _bf16(what, *ts):
+    for t in ts:
+        if t is not None and t.dtype != torch.bfloat16:
+            raise TypeError("%s must be bfloat16, got %s" % (what, t.dtype))
+
+
+def _ffn_sizes(what, x, W1, W2):
+    """(T, d, h) of the gated block's tensors."""
+    T, d = _rows(x)
+    if W1.dim() != 2 or W2.dim() != 2 or W1.shape != (2 * W2.shape[1], d) or W2.shape[0] != d:
+        raise ValueError("%s: x %s, W1 %s and W2 %s do not match ([.., d], [2h, d], [d, h])"
+                         % (what, tuple(x.shape), tuple(W1.shape), tuple(W2.shape)))
+    return T, d, W2.shape[1]
+
+
+def hcw_gated_ffn_fwd_workspace_bytes(T: int, d: int, h: int) -> int:
+    return int(lib().hcw_gated_ffn_fwd_workspace_bytes(T, d, h))
+
+
+def hcw_gated_ffn_fwd(x, W1, W2, act: int = HCW_GATE_SILU, y=None, workspace=None, stream=None):
+    """y = (act(x Wg^T) * (x Wu^T)) W2^T over rows x [..., d] bf16; W1 [2h, d]
+    holds Wg and Wu one after the other, W2 is [d, h].  Returns y."""
+    _dev(x, W1, W2, y, workspace)
+    _bf16("hcw_gated_ffn_fwd: tensors", x, W1, W2, y)
+    T, d, h = _ffn_sizes("hcw_gated_ffn_fwd", x, W1, W2)
+    y = torch.empty_like(x) if y is None else y
+    _like(x, "hcw_gated_ffn_fwd", y)
+    if workspace is None:
+        workspace = _workspace(hcw_gated_ffn_fwd_workspace_bytes(T, d, h), x.device, None)
+    _check(lib().hcw_gated_ffn_fwd(_ptr(x), _ptr(W1), _ptr(W2), T, d, h, act, _ptr(y),
+                                   _ptr(workspace), workspace.numel(), _stream(stream)),
+           "hcw_gated_ffn_fwd")
+    return y
+
+
+def hcw_gated_ffn_bwd_workspace_bytes(T: int, d: int, h: int) -> int:
+    return int(lib().hcw_gated_ffn_bwd_workspace_bytes(T, d, h))
+
+
+def hcw_gated_ffn_bwd(x, dy, W1, W2, act: int = HCW_GATE_SILU, dx=None, dW1=None, dW2=None,
+                      dw_dtype=torch.float32, want_dx: bool = True, want_dw: bool = True,
+                      workspace=None, stream=None):
+    """Backward of hcw_gated_ffn_fwd from its inputs and dy; returns (dx, dW1,
+    dW2), None for what is not wanted.  The weight gradients are fp32 or, by
+    dw_dtype or the tensors given, bf16."""
+    _dev(x, dy, W1, W2, dx, dW1, dW2, workspace)
+    _bf16("hcw_gated_ffn_bwd: tensors", x, dy, W1, W2, dx)
+    T, d, h = _ffn_sizes("hcw_gated_ffn_bwd", x, W1, W2)
+    if want_dx and dx is None:
+        dx = torch.empty_like(x)
+    _like(x, "hcw_gated_ffn_bwd", dy, dx)
+    if want_dw:
+        if dW1 is not None or dW2 is not None:
+            dw_dtype = (dW1 if dW1 is not None else dW2).dtype
+        dW1 = torch.empty(2 * h, d, dtype=dw_dtype, device=x.device) if dW1 is None else dW1
+        dW2 = torch.empty(d, h, dtype=dw_dtype, device=x.device) if dW2 is None else dW2
+        if dW1.shape != W1.shape or dW2.shape != W2.shape or dW1.dtype != dW2.dtype:
+            raise ValueError("hcw_gated_ffn_bwd: dW1 and dW2 have the weights' shapes and one dtype")
+        code = _dtype_code(dW1)
+    else:
+        dW1 = dW2 = None
+        code = HCW_BF16
+    if workspace is None:
+        workspace = _workspace(hcw_gated_ffn_bwd_workspace_bytes(T, d, h), x.device, None)
+    _check(lib().hcw_gated_ffn_bwd(_ptr(x), _ptr(dy), _ptr(W1), _ptr(W2), T, d, h, act, code,
+                                   _ptr(dx), _ptr(dW1), _ptr(dW2), _ptr(workspace),
+                                   workspace.numel(), _stream(stream)), "hcw_gated_ffn_bwd")
+    return dx, dW1, dW2
 
 
 def _gates(T: int, rows_per_gate: int) -> int:
