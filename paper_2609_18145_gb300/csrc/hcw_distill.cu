@@ -7,31 +7,31 @@
 //   dz_j = w [ a tau (P q_j - sum_{k: i_k = j} p_k) + b (q1_j - [j = y]) ]
 //
 // (P = 1, or 0 for a row without slots).  Bound by memory: the logits are read once and
-// the gradient is written once, 4 bytes a symbol in bf16.  A row stays in registers
-// between the sums and the gradient: a cluster of up to 8 CTAs shares a long row (or the
-// few rows of a short batch), each CTA summing its part against its own maximum and the
-// parts being joined through distributed shared memory.  Short rows (V <= 1024) take a
-// warp each.  The dense part of the gradient goes out first; then the symbols that the
-// teacher or the label names are written again with their share taken off, each by the
-// one thread that owns the symbol's first slot, so no atomics and no fixed-up rounding:
-// every output is rounded once, from fp32.
+// the gradient is written once, 4 bytes a symbol in bf16.  A row stays on chip between
+// its sums and its gradient: short rows (V <= 1024) in a warp's registers, long ones in
+// the shared memory of a cluster of up to 8 CTAs, each summing its slice against its own
+// maximum, the parts joined through distributed shared memory.  The dense part
+// of the gradient goes out first; then the symbols that the teacher or the label names
+// are written again with their share taken off, each by the one thread that owns the
+// symbol's first slot, so nothing depends on the order of atomics and every output is
+// rounded once, from fp32.
 //
-// A row starts anywhere (V may be odd): its whole 16-byte vectors go to the threads in
-// turn and the up to seven symbols on either side of them to the first threads of the
-// row's first CTA.
+// A row starts anywhere (V may be odd): its first and last 16-byte vectors may hold symbols
+// of its neighbours, which are masked when read and left alone when written.
 #include "hcw.h"
 #include "hcw_internal.h"
 #include "hcw_ptx.cuh"
 
 #include <math.h>
+#include <mutex>
 
 namespace hcw {
 
 namespace {
 
 constexpr int kDMaxK = 1024;          // slots of a row
-constexpr int kDMaxV = 262144;        // 8 CTAs x 512 threads x 64 symbols
-constexpr int kDThreads = 512;
+constexpr int kDMaxV = 262144;        // 8 CTAs x 128 KB of fp32 logits
+constexpr size_t kDSmem = 232448;     // shared memory of an SM
 constexpr int kDWarpV = 1024;         // a warp a row up to here,
 constexpr int kDWarpK = 64;           // and up to this many slots
 constexpr int kDWarps = 8;            // rows of a CTA of the warp kernel
@@ -179,6 +179,51 @@ __device__ __forceinline__ float slot_owned(const Slots& s, int K, int k) {
     return t;
 }
 
+// One warp: fills own through a table of the symbols (open addressing, `size` a power of two
+// of at least 2 K entries of symbol and first slot).  Which entry a symbol gets depends on
+// the order of the threads, what is found there does not.
+__device__ __forceinline__ void slots_own(const Slots& s, int K, int* table, int size, int lane) {
+    int* const key = table;
+    int* const low = table + size;
+    for (int i = lane; i < size; i += 32) {
+        key[i] = -1;
+        low[i] = 0x7fffffff;
+    }
+    __syncwarp();
+    for (int k = lane; k < K; k += 32) {
+        const int id = s.id[k];
+        if (id < 0) continue;
+        int h = (int)(((uint32_t)id * 2654435761u) >> 7) & (size - 1);
+        for (;;) {
+            const int was = atomicCAS(&key[h], -1, id);
+            if (was == -1 || was == id) break;
+            h = (h + 1) & (size - 1);
+        }
+        atomicMin(&low[h], k);
+        s.own[k] = __int_as_float(h);
+    }
+    __syncwarp();
+    // a symbol with a second slot: its entry's sign bit
+    for (int k = lane; k < K; k += 32) {
+        if (s.id[k] < 0) continue;
+        const int h = __float_as_int(s.own[k]);
+        if ((low[h] & 0x7fffffff) != k) atomicOr(&low[h], (int)0x80000000);
+    }
+    __syncwarp();
+    for (int k = lane; k < K; k += 32) {
+        if (s.id[k] < 0) {
+            s.own[k] = -1.f;
+            continue;
+        }
+        const int l = low[__float_as_int(s.own[k])];
+        if ((l & 0x7fffffff) != k)
+            s.own[k] = -1.f;
+        else
+            s.own[k] = l < 0 ? slot_owned(s, K, k) : s.p[k];
+    }
+    __syncwarp();
+}
+
 // ------------------------------------------------------------------ a warp a row
 // NE symbols a lane, symbol lane + 32 e: coalesced whatever the row's alignment.
 template <typename T, int NE, bool TWO>
@@ -270,197 +315,477 @@ __global__ void __launch_bounds__(32 * kDWarps) distill_warp_kernel(const Distil
 }
 
 // ------------------------------------------------------------------ a cluster a row
-// NV 16-byte vectors a thread.  The cluster's CTAs take the row's vectors in equal runs.
-template <typename T, int NV, bool TWO>
-__global__ void __launch_bounds__(kDThreads) distill_row_kernel(const DistillArgs a, int C) {
+// Long rows: a persistent cluster of C CTAs takes rows in turn, each CTA a slice of the row's
+// 16-byte vectors.  A CTA's roles:
+//   producer      bulk copies of the slices of the next rows into a ring of NB buffers
+//   NT compute    pass A (row n + 1): maximum and sum of the slice, each warp sending
+//     threads     its part to every CTA of the cluster (st.async, counted by an mbarrier);
+//                 then pass B (row n), whose parts arrived meanwhile: the gradient, from
+//                 the slice in shared memory
+//   slot warps    rows in turn: the teacher's probabilities and the named symbols' logits;
+//                 the loss; and, behind the dense values of pass B, those symbols
+// so that no role waits for another CTA's current row.  Rows of weight 0 are not read.
+constexpr int kDSlotWarps = 2;
+// Stat buffers.  A CTA sends row n + R's parts when every warp of the cluster has been
+// through pass A of row n + R - 2, so through pass B of n + R - 4, whose slot flags say that
+// row n + R - 4 - kDSlotWarps has left the slot warps: nobody reads row n's parts any more.
+constexpr int kDStats = 8;
+static_assert(kDStats >= 4 + kDSlotWarps, "stat ring");
+constexpr int kDMaxBufs = 4;
+constexpr unsigned long long kDTimeoutNs = 2000000000ull;
+
+struct __align__(8) DistillBars {
+    uint64_t full[kDMaxBufs];        // a row's slice has landed
+    uint64_t empty[kDMaxBufs];       // pass B has read it
+    uint64_t stat[kDStats];          // every warp of the cluster has sent its part
+    uint64_t ready[kDSlotWarps];     // the slot warp's flags for its row are set
+    uint64_t dense[kDSlotWarps];     // the dense values of its row are stored
+    int any[kDSlotWarps], label[kDSlotWarps];
+    int abort;
+};
+
+struct DistillPlan {
+    int C, clusters, bufs, look, slice;   // slice: bytes of a buffer
+    int table;                            // entries of a slot warp's symbol table
+    size_t smem;
+};
+
+// A warp's rows: first + i * step, i = 0, 1, ...; their weights come 32 at a time.
+struct RowCursor {
+    const float* weight;
+    int row, T, step, i, lane;
+    float mine;
+    __device__ __forceinline__ RowCursor(const DistillArgs& a, int first, int step_, int lane_)
+        : weight(a.weight), row(first), T(a.T), step(step_), i(0), lane(lane_), mine(1.f) {
+        fetch();
+    }
+    __device__ __forceinline__ void fetch() {
+        const long long r = (long long)row + (long long)lane * step;
+        mine = weight && r < T ? weight[r] : 1.f;
+    }
+    __device__ __forceinline__ bool more() const { return row < T; }
+    __device__ __forceinline__ float w() const { return __shfl_sync(0xffffffffu, mine, i); }
+    __device__ __forceinline__ void next() {
+        row = row <= T - step ? row + step : T;
+        if (++i == 32) {
+            i = 0;
+            fetch();
+        }
+    }
+    // to the first row from here on that counts; false when there is none
+    __device__ __forceinline__ bool seek() {
+        while (more() && w() == 0.f) next();
+        return more();
+    }
+};
+
+__device__ __forceinline__ float2 ex2_pair(uint64_t x) {
+    const float2 f = f32x2_unpack(x);
+    return make_float2(ex2(f.x), ex2(f.y));
+}
+
+// Sends one 16-byte value to the same place of CTA `rank`'s shared memory, counted by its
+// mbarrier `bar`.
+__device__ __forceinline__ void send16(const void* at, const uint64_t* bar, uint32_t rank, float x,
+                                       float y, float z) {
+    asm volatile(
+        "st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%1, %2, %3, %4}, [%5];"
+        ::"r"(mapa_shared(at, rank)), "r"(__float_as_uint(x)), "r"(__float_as_uint(y)),
+        "r"(__float_as_uint(z)), "r"(0u), "r"(mapa_shared(bar, rank))
+        : "memory");
+}
+
+// The joined statistic of a row from its n parts, on every lane, in a fixed order.
+template <bool TWO>
+__device__ __forceinline__ Stat stat_read(const float4* part, int n, int lane, float c) {
+    Stat v = {-INFINITY, 0.f, 0.f};
+    for (int i = lane; i < n; i += 32) {
+        const float4 q = part[i];
+        v = stat_join<TWO>(v, Stat{q.x, q.y, q.z}, c);
+    }
+    return stat_warp<TWO>(v, c);
+}
+
+template <typename T, int NT, bool TWO>
+__global__ void __launch_bounds__(NT + 32 + 32 * kDSlotWarps, NT == 512 ? 1 : NT == 256 ? 2 : 4)
+    distill_row_kernel(const DistillArgs a, const DistillPlan pl) {
     constexpr int VE = 16 / (int)sizeof(T);   // symbols of a vector
-    extern __shared__ __align__(16) uint8_t dyn[];
-    __shared__ Stat warp_stat[kDThreads / 32];
-    __shared__ Stat cta_stat;   // read by the cluster
-    __shared__ float s_ent;
-    __shared__ int s_any;
+    constexpr int NW = NT / 32;
+    constexpr int G = 8;                      // vectors a thread holds at once
+    extern __shared__ __align__(128) uint8_t dsm[];
+    uint8_t* p = dsm + (size_t)pl.bufs * pl.slice;
+    float4* const stats = reinterpret_cast<float4*>(p);   // [kDStats][C * NW]
+    const int parts = pl.C * NW;
+    p += (size_t)kDStats * parts * sizeof(float4);
+    uint8_t* const slot_mem = p;
+    const size_t slot_bytes = (size_t)a.K * 16 + (size_t)pl.table * 8;
+    DistillBars* const bars =
+        reinterpret_cast<DistillBars*>(p + kDSlotWarps * ((slot_bytes + 15) & ~(size_t)15));
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, tid = threadIdx.x;
-    const int n_warps = (int)blockDim.x >> 5, nt = (int)blockDim.x;
-    const int rank = (int)blockIdx.x % C;
-    const long long row = blockIdx.x / C;
-    Slots sl;
-    sl.p = reinterpret_cast<float*>(dyn);
-    sl.own = sl.p + a.K;
-    sl.zk = sl.own + a.K;
-    sl.id = reinterpret_cast<int*>(sl.zk + a.K);
+    const int rank = (int)blockIdx.x % pl.C, first = (int)blockIdx.x / pl.C;
+    const float c = a.inv_tau * kLog2e;
+    volatile int* abort = &bars->abort;
+    if (tid == 0) {
+        for (int i = 0; i < pl.bufs; ++i) {
+            mbar_init(&bars->full[i], 1);
+            mbar_init(&bars->empty[i], NW);
+        }
+        for (int i = 0; i < kDStats; ++i) mbar_init(&bars->stat[i], 1);
+        for (int i = 0; i < kDSlotWarps; ++i) {
+            mbar_init(&bars->ready[i], 1);
+            mbar_init(&bars->dense[i], NW);
+        }
+        bars->abort = 0;
+        fence_mbar_init();
+    }
+    __syncthreads();
+    cluster_sync_all();
     pdl_wait();
     pdl_trigger();
-    const T* z = static_cast<const T*>(a.z) + (size_t)row * a.V;
-    T* dz = a.dz ? static_cast<T*>(a.dz) + (size_t)row * a.V : nullptr;
-    // symbols before the row's first whole vector, the vectors, this CTA's run of them
-    const int skew = (int)(((size_t)row * a.V) % VE);
-    int head = skew ? VE - skew : 0;
-    if (head > a.V) head = a.V;
-    const int n_vec = (a.V - head) / VE;
-    const int per = (n_vec + C - 1) / C;
-    const int v0 = rank * per < n_vec ? rank * per : n_vec;
-    const int v1 = v0 + per < n_vec ? v0 + per : n_vec;
-    const int tail0 = head + n_vec * VE;
-    // and this thread's symbol beside the vectors
-    int edge = -1;
-    if (rank == 0 && tid < VE && tid < head) edge = tid;
-    if (rank == 0 && tid >= VE && tid < 2 * VE && tail0 + tid - VE < a.V) edge = tail0 + tid - VE;
-    const uint4* zv = reinterpret_cast<const uint4*>(z + head);
-    uint4* dv = dz ? reinterpret_cast<uint4*>(dz + head) : nullptr;
-    const float w = a.weight ? a.weight[row] : 1.f;
-    if (w == 0.f) {   // whatever the row holds; the whole cluster leaves here
-        if (dz) {
-            for (int i = v0 + tid; i < v1; i += nt) dv[i] = make_uint4(0u, 0u, 0u, 0u);
-            if (edge >= 0) put(dz + edge, 0.f);
-        }
-        if (rank == 0 && tid == 0 && a.loss) a.loss[row] = 0.f;
-        return;
-    }
-    const uint32_t ninf = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;
-    uint4 q[NV];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int j = v0 + tid + i * nt;
-        q[i] = j < v1 ? zv[j] : make_uint4(ninf, ninf, ninf, ninf);
-    }
-    const float ze = edge >= 0 ? logit(z + edge) : -INFINITY;
-    int y = a.target ? a.target[row] : -1;
-    if (y >= a.V) {
-        if (tid == 0) atomicExch(&g_error_word, kErrInvalid);
-        y = -1;
-    }
-    const float zy = y >= 0 ? logit(z + y) : 0.f;
-    // the slots, while the row is on its way
-    if (a.idx && warp == 0) {
-        bool any;
-        const float ent = slots_read(a, (size_t)row, sl, lane, &any);
-        if (lane == 0) {
-            s_ent = ent;
-            s_any = any;
-        }
-    }
-    if (!a.idx && tid == 0) s_any = 0;
-    __syncthreads();
-    if (a.idx)
-        for (int k = tid; k < a.K; k += nt) {
-            sl.own[k] = slot_owned(sl, a.K, k);
-            sl.zk[k] = sl.id[k] >= 0 ? logit(z + sl.id[k]) : 0.f;
-        }
 
-    auto elem = [&](const uint4& u, int e) {
-        const uint32_t ws[4] = {u.x, u.y, u.z, u.w};
-        if (sizeof(T) == 4) return __uint_as_float(ws[e]);
-        return __uint_as_float(e & 1 ? ws[e >> 1] & 0xFFFF0000u : ws[e >> 1] << 16);
+    // A row's vectors: those its symbols touch, the first and the last perhaps shared with
+    // the rows beside it.  [v0, v1): this CTA's.
+    struct Row {
+        size_t at;       // the row's first symbol
+        int skew;        // symbols of vector 0 before it
+        int n, v0, v1;
     };
-    const float c = a.inv_tau * kLog2e;
-    Stat st = {ze, 0.f, 0.f};
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-        for (int e = 0; e < VE; ++e) st.m = fmaxf(st.m, elem(q[i], e));
-    {
-        const float b = stat_base(st.m);
-        st.s = ex2((ze - b) * c);
-        if (TWO) st.s1 = ex2((ze - b) * kLog2e);
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-#pragma unroll
-            for (int e = 0; e < VE; ++e) {
-                const float x = elem(q[i], e) - b;
-                st.s += ex2(x * c);
-                if (TWO) st.s1 += ex2(x * kLog2e);
+    auto row_of = [&](int row) {
+        Row r;
+        r.at = (size_t)row * a.V;
+        r.skew = (int)(r.at % VE);
+        r.n = (r.skew + a.V + VE - 1) / VE;
+        const int per = (r.n + pl.C - 1) / pl.C;
+        r.v0 = rank * per < r.n ? rank * per : r.n;
+        r.v1 = r.v0 + per < r.n ? r.v0 + per : r.n;
+        return r;
+    };
+    const T* const zb = static_cast<const T*>(a.z);
+    T* const gb = static_cast<T*>(a.dz);
+
+    if (warp == NW) {
+        // ------------------------------------------------------------ producer
+        const size_t end = (size_t)a.T * a.V;   // symbols
+        int n = 0;
+        uint32_t issued = 0;
+        bool ok = true;
+        RowCursor cur(a, first, pl.clusters, lane);
+        for (; ok && cur.seek(); cur.next(), ++n) {
+            const int b = n % pl.bufs;
+            bool w = true;
+            if (n >= pl.bufs)
+                w = mbar_wait(&bars->empty[b], ((n / pl.bufs) & 1) ^ 1, abort, kDTimeoutNs);
+            ok = __all_sync(0xffffffffu, w);
+            if (!ok) break;
+            const Row r = row_of(cur.row);
+            uint8_t* dst = dsm + (size_t)b * pl.slice;
+            const size_t s0 = r.at - r.skew + (size_t)r.v0 * VE;
+            // whole vectors inside the tensor; the symbols after them one by one
+            size_t whole = (size_t)(r.v1 - r.v0);
+            if (whole && s0 + whole * VE > end) {
+                --whole;
+                const size_t s1 = s0 + whole * VE;
+                if (s1 + lane < end)
+                    reinterpret_cast<T*>(dst + whole * 16)[lane] = zb[s1 + lane];
+                __syncwarp();
             }
-    }
-    st = stat_warp<TWO>(st, c);
-    if (lane == 0) warp_stat[warp] = st;
-    __syncthreads();
-    if (warp == 0) {
-        Stat u = {-INFINITY, 0.f, 0.f};
-        if (lane < n_warps) u = warp_stat[lane];
-        u = stat_warp<TWO>(u, c);
-        if (lane == 0) cta_stat = u;
-    }
-    __syncwarp();
-    if (C > 1) {
-        cluster_sync_all();
-        // every thread joins the CTAs' parts, in rank order
-        st = Stat{-INFINITY, 0.f, 0.f};
-        for (int r = 0; r < C; ++r) {
-            const uint32_t at = mapa_shared(&cta_stat, (uint32_t)r);
-            Stat u;
-            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(u.m) : "r"(at) : "memory");
-            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(u.s) : "r"(at + 4) : "memory");
-            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(u.s1) : "r"(at + 8) : "memory");
-            st = stat_join<TWO>(st, u, c);
+            if (lane == 0) {
+                mbar_arrive_expect_tx(&bars->full[b], (uint32_t)(whole * 16));
+                issued |= 1u << b;
+                if (whole)
+                    asm volatile(
+                        "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes "
+                        "[%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)),
+                        "l"(zb + s0), "r"((uint32_t)(whole * 16)), "r"(smem_u32(&bars->full[b]))
+                        : "memory");
+            }
         }
-        // no CTA leaves while another may still read its part
-        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+        if (lane == 0)
+            // every copy has landed before the CTA leaves, also when the others gave up
+            for (int b = 0; b < pl.bufs; ++b)
+                if (issued & (1u << b)) {
+                    const int last = (n - 1 - b) / pl.bufs;   // the buffer's last round
+                    mbar_wait_drain(&bars->full[b], last & 1, kDTimeoutNs);
+                }
+    } else if (warp > NW) {
+        // ------------------------------------------------------------ slot warps
+        const int sw = warp - NW - 1;
+        Slots sl;
+        sl.p = reinterpret_cast<float*>(slot_mem + sw * ((slot_bytes + 15) & ~(size_t)15));
+        sl.own = sl.p + a.K;
+        sl.zk = sl.own + a.K;
+        sl.id = reinterpret_cast<int*>(sl.zk + a.K);
+        int* const table = sl.id + a.K;
+        RowCursor cur(a, first, pl.clusters, lane);
+        int n = 0;
+        bool ok = true;
+        for (; ok && cur.seek(); cur.next(), ++n) {
+            if (n % kDSlotWarps != sw) continue;
+            const uint32_t phase = (n / kDSlotWarps) & 1;
+            const float w = cur.w();
+            const Row r = row_of(cur.row);
+            const T* z = zb + r.at;
+            T* dz = gb ? gb + r.at : nullptr;
+            auto mine = [&](int j) {
+                const int v = (r.skew + j) / VE;
+                return v >= r.v0 && v < r.v1;
+            };
+            int y = a.target ? a.target[cur.row] : -1;
+            if (y >= a.V) {
+                if (lane == 0) atomicExch(&g_error_word, kErrInvalid);
+                y = -1;
+            }
+            bool any = false;
+            float ent = 0.f;
+            if (a.K) ent = slots_read(a, (size_t)cur.row, sl, lane, &any);
+            if (lane == 0) {
+                bars->any[sw] = any;
+                bars->label[sw] = y >= 0;
+                mbar_arrive(&bars->ready[sw]);
+            }
+            const float zy = y >= 0 && (rank == 0 || mine(y)) ? logit(z + y) : 0.f;
+            for (int k = lane; k < a.K; k += 32) {
+                const int i = sl.id[k];
+                sl.zk[k] = i >= 0 && (rank == 0 || mine(i)) ? logit(z + i) : 0.f;
+            }
+            if (any && dz) slots_own(sl, a.K, table, pl.table, lane);
+            const bool w1 = mbar_wait_cluster(&bars->stat[n % kDStats], (n / kDStats) & 1, abort,
+                                              kDTimeoutNs);
+            ok = __all_sync(0xffffffffu, w1);
+            if (!ok) break;
+            Stat st = stat_read<TWO>(stats + (n % kDStats) * parts, parts, lane, c);
+            const float base = stat_base(st.m);
+            if (st.s == 0.f) {   // no logit above -inf: nothing to learn from
+                any = false;
+                y = -1;
+                st.s = st.s1 = 1.f;
+            }
+            if (rank == 0 && a.loss) {
+                // log-sums relative to the maximum, as the logits are: the row's own size
+                // cancels first
+                const float ls = logf(st.s), ls1 = logf(st.s1);
+                float l = 0.f;
+                if (any)
+                    for (int k = lane; k < a.K; k += 32)
+                        if (sl.p[k] != 0.f) l -= sl.p[k] * ((sl.zk[k] - base) * a.inv_tau - ls);
+                l = warp_sum(l) + (any ? ent : 0.f);
+                if (lane == 0)
+                    a.loss[cur.row] =
+                        w * (a.kl * l + (y >= 0 ? a.ce * (ls1 - (zy - base)) : 0.f));
+            }
+            const bool w2 = mbar_wait(&bars->dense[sw], phase, abort, kDTimeoutNs);
+            ok = __all_sync(0xffffffffu, w2);
+            if (!ok) break;
+            if (!dz) continue;
+            const float fq = any ? w * a.kl_tau / st.s : 0.f, f1 = y >= 0 ? w * a.ce / st.s1 : 0.f;
+            auto dense = [&](float x) {
+                const float e = ex2((x - base) * c);
+                return TWO ? fq * e + f1 * ex2((x - base) * kLog2e) : (fq + f1) * e;
+            };
+            bool named = false;   // the label, by a slot
+            if (any)
+                for (int k = lane; k < a.K; k += 32) {
+                    const float t = sl.own[k];
+                    if (t < 0.f) continue;
+                    const bool is_y = sl.id[k] == y;
+                    named |= is_y;
+                    if (mine(sl.id[k]))
+                        put(dz + sl.id[k], dense(sl.zk[k]) - w * (a.kl_tau * t + (is_y ? a.ce : 0.f)));
+                }
+            named = __any_sync(0xffffffffu, named);
+            if (y >= 0 && !named && lane == 0 && mine(y)) put(dz + y, dense(zy) - w * a.ce);
+        }
     } else {
-        __syncthreads();
-        st = cta_stat;
-    }
-    const float base = stat_base(st.m);
-    bool any = s_any != 0;
-    if (st.s == 0.f) {   // no logit above -inf: nothing to learn from
-        any = false;
-        y = -1;
-        st.s = st.s1 = 1.f;
-    }
-    if (rank == 0 && warp == 0 && a.loss) {
-        // log-sums relative to the maximum, as the logits are: the row's own size cancels first
-        const float ls = logf(st.s), ls1 = logf(st.s1);
-        float l = 0.f;
-        if (any)
-            for (int k = lane; k < a.K; k += 32)
-                if (sl.p[k] != 0.f) l -= sl.p[k] * ((sl.zk[k] - base) * a.inv_tau - ls);
-        l = warp_sum(l) + (any ? s_ent : 0.f);
-        if (lane == 0) a.loss[row] = w * (a.kl * l + (y >= 0 ? a.ce * (ls1 - (zy - base)) : 0.f));
-    }
-    if (dz) {
-        const float fq = any ? w * a.kl_tau / st.s : 0.f, f1 = y >= 0 ? w * a.ce / st.s1 : 0.f;
-        auto dense = [&](float x) {
-            const float e = ex2((x - base) * c);
-            return TWO ? fq * e + f1 * ex2((x - base) * kLog2e) : (fq + f1) * e;
+        // ------------------------------------------------------------ compute warps
+        auto elem = [](const uint4& u, int e) {
+            const uint32_t ws[4] = {u.x, u.y, u.z, u.w};
+            if (sizeof(T) == 4) return __uint_as_float(ws[e]);
+            return __uint_as_float(e & 1 ? ws[e >> 1] & 0xFFFF0000u : ws[e >> 1] << 16);
         };
+        // two neighbouring symbols of a vector
+        auto pair = [](const uint4& u, int i) {
+            const uint32_t ws[4] = {u.x, u.y, u.z, u.w};
+            return sizeof(T) == 2
+                       ? bf16x2_to_f32x2(ws[i])
+                       : f32x2_pack(__uint_as_float(ws[2 * i]), __uint_as_float(ws[2 * i + 1]));
+        };
+        const uint32_t ninf = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;
+        const uint64_t cc = f32x2_pack(c, c), ll = f32x2_pack(kLog2e, kLog2e);
+        // vector v of the row as it lies in shared memory, symbols of other rows masked
+        auto vec = [&](const Row& r, const uint4* buf, int v) {
+            uint4 u = buf[v - r.v0];
+            if (v == 0 || v == r.n - 1) {
+                uint32_t ws[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int j = v0 + tid + i * nt;
-            if (j >= v1) continue;
-            uint32_t o[4];
-            if (sizeof(T) == 4) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[e] = __float_as_uint(dense(elem(q[i], e)));
-            } else {
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    o[e] = pack_bf16x2(dense(elem(q[i], 2 * e)), dense(elem(q[i], 2 * e + 1)));
+                for (int e = 0; e < VE; ++e) {
+                    const int j = v * VE + e - r.skew;
+                    if (j >= 0 && j < a.V) continue;
+                    if (sizeof(T) == 4)
+                        ws[e] = ninf;
+                    else
+                        ws[e >> 1] = e & 1 ? (ws[e >> 1] & 0xFFFFu) | 0xFF800000u
+                                           : (ws[e >> 1] & 0xFFFF0000u) | 0xFF80u;
+                }
+                u = make_uint4(ws[0], ws[1], ws[2], ws[3]);
             }
-            dv[j] = make_uint4(o[0], o[1], o[2], o[3]);
+            return u;
+        };
+        bool ok = true;
+        auto wait = [&](uint64_t* bar, uint32_t parity, bool cluster = false) {
+            const bool w = cluster ? mbar_wait_cluster(bar, parity, abort, kDTimeoutNs)
+                                   : mbar_wait(bar, parity, abort, kDTimeoutNs);
+            ok = __all_sync(0xffffffffu, w);
+            return ok;
+        };
+        auto pass_a = [&](int row, int n) {
+            const int b = n % pl.bufs;
+            if (!wait(&bars->full[b], (n / pl.bufs) & 1)) return;
+            const Row r = row_of(row);
+            const uint4* buf = reinterpret_cast<const uint4*>(dsm + (size_t)b * pl.slice);
+            Stat st = {-INFINITY, 0.f, 0.f};
+            for (int g = r.v0 + tid; g < r.v1; g += G * NT) {
+                uint4 q[G];
+#pragma unroll
+                for (int k = 0; k < G; ++k)
+                    q[k] = g + k * NT < r.v1 ? vec(r, buf, g + k * NT)
+                                             : make_uint4(ninf, ninf, ninf, ninf);
+                Stat u = {-INFINITY, 0.f, 0.f};
+                if (sizeof(T) == 2) {
+                    __nv_bfloat162 m = *reinterpret_cast<const __nv_bfloat162*>(&ninf);
+#pragma unroll
+                    for (int k = 0; k < G; ++k) {
+                        const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&q[k]);
+                        m = __hmax2(m, __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3])));
+                    }
+                    u.m = fmaxf(__low2float(m), __high2float(m));
+                } else {
+#pragma unroll
+                    for (int k = 0; k < G; ++k)
+#pragma unroll
+                        for (int e = 0; e < VE; ++e) u.m = fmaxf(u.m, elem(q[k], e));
+                }
+                const float nb = -stat_base(u.m);
+                const uint64_t nbb = f32x2_pack(nb, nb);
+                uint64_t s = 0, s1 = 0;   // two sums side by side
+#pragma unroll
+                for (int k = 0; k < G; ++k)
+#pragma unroll
+                    for (int i = 0; i < VE / 2; ++i) {
+                        const uint64_t d = f32x2_add(pair(q[k], i), nbb);
+                        const float2 e = ex2_pair(f32x2_mul(d, cc));
+                        s = f32x2_add(s, f32x2_pack(e.x, e.y));
+                        if (TWO) {
+                            const float2 f = ex2_pair(f32x2_mul(d, ll));
+                            s1 = f32x2_add(s1, f32x2_pack(f.x, f.y));
+                        }
+                    }
+                const float2 sf = f32x2_unpack(s), sf1 = f32x2_unpack(s1);
+                u.s = sf.x + sf.y;
+                u.s1 = TWO ? sf1.x + sf1.y : u.s;
+                st = stat_join<TWO>(st, u, c);
+            }
+            st = stat_warp<TWO>(st, c);
+            uint64_t* const bar = &bars->stat[n % kDStats];
+            float4* const at = stats + (n % kDStats) * parts + rank * NW + warp;
+            if (tid == 0) mbar_arrive_expect_tx(bar, (uint32_t)(parts * sizeof(float4)));
+            if (lane < pl.C) send16(at, bar, (uint32_t)lane, st.m, st.s, st.s1);
+        };
+        auto pass_b = [&](int row, int n, float w) {
+            const int sw = n % kDSlotWarps, b = n % pl.bufs;
+            if (!wait(&bars->stat[n % kDStats], (n / kDStats) & 1, true)) return;
+            if (!wait(&bars->ready[sw], (n / kDSlotWarps) & 1)) return;
+            Stat st = stat_read<TWO>(stats + (n % kDStats) * parts, parts, lane, c);
+            bool any = bars->any[sw] != 0, label = bars->label[sw] != 0;
+            if (st.s == 0.f) {
+                any = label = false;
+                st.s = st.s1 = 1.f;
+            }
+            if (gb) {
+                const Row r = row_of(row);
+                const uint4* buf = reinterpret_cast<const uint4*>(dsm + (size_t)b * pl.slice);
+                T* const dz = gb + r.at;
+                uint4* const dv = reinterpret_cast<uint4*>(gb + (r.at - r.skew));
+                const float nb = -stat_base(st.m);
+                const float fq = any ? w * a.kl_tau / st.s : 0.f;
+                const float f1 = label ? w * a.ce / st.s1 : 0.f;
+                const uint64_t nbb = f32x2_pack(nb, nb);
+                const uint64_t ff = TWO ? f32x2_pack(fq, fq) : f32x2_pack(fq + f1, fq + f1);
+                const uint64_t ff1 = f32x2_pack(f1, f1);
+#pragma unroll 4
+                for (int v = r.v0 + tid; v < r.v1; v += NT) {
+                    const uint4 q = buf[v - r.v0];
+                    uint32_t o[4];
+#pragma unroll
+                    for (int i = 0; i < VE / 2; ++i) {
+                        const uint64_t d = f32x2_add(pair(q, i), nbb);
+                        const float2 e = ex2_pair(f32x2_mul(d, cc));
+                        uint64_t g = f32x2_mul(f32x2_pack(e.x, e.y), ff);
+                        if (TWO) {
+                            const float2 f = ex2_pair(f32x2_mul(d, ll));
+                            g = f32x2_fma(f32x2_pack(f.x, f.y), ff1, g);
+                        }
+                        const float2 h = f32x2_unpack(g);
+                        if (sizeof(T) == 2) {
+                            o[i] = pack_bf16x2(h.x, h.y);
+                        } else {
+                            o[2 * i] = __float_as_uint(h.x);
+                            o[2 * i + 1] = __float_as_uint(h.y);
+                        }
+                    }
+                    const uint4 u = make_uint4(o[0], o[1], o[2], o[3]);
+                    if (v != 0 && v != r.n - 1) {
+                        dv[v] = u;
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < VE; ++e) {
+                            const int j = v * VE + e - r.skew;
+                            if (j >= 0 && j < a.V) put(dz + j, elem(u, e));
+                        }
+                    }
+                }
+            }
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive(&bars->empty[b]);
+                mbar_arrive(&bars->dense[sw]);
+            }
+        };
+        RowCursor ca(a, first, pl.clusters, lane), cb(a, first, pl.clusters, lane);
+        int na = 0, nb = 0;
+        for (; ok && cb.more(); cb.next()) {
+            const float w = cb.w();
+            if (w == 0.f) {   // whatever the row holds
+                if (gb) {
+                    const Row r = row_of(cb.row);
+                    uint4* const dv = reinterpret_cast<uint4*>(gb + (r.at - r.skew));
+                    for (int v = r.v0 + tid; v < r.v1; v += NT) {
+                        if (v != 0 && v != r.n - 1) {
+                            dv[v] = make_uint4(0u, 0u, 0u, 0u);
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < VE; ++e) {
+                                const int j = v * VE + e - r.skew;
+                                if (j >= 0 && j < a.V) put(gb + r.at + j, 0.f);
+                            }
+                        }
+                    }
+                }
+                if (rank == 0 && tid == 0 && a.loss) a.loss[cb.row] = 0.f;
+                continue;
+            }
+            while (ok && na <= nb + pl.look && ca.seek()) {
+                pass_a(ca.row, na);
+                ++na;
+                ca.next();
+            }
+            if (!ok) break;
+            pass_b(cb.row, nb, w);
+            ++nb;
         }
-        if (edge >= 0) put(dz + edge, dense(ze));
-        __syncthreads();   // the CTA's dense values are in place
-        // the named symbols of this CTA's part of the row
-        auto mine = [&](int j) {
-            if (j < head || j >= tail0) return rank == 0;
-            const int v = (j - head) / VE;
-            return v >= v0 && v < v1;
-        };
-        // (the label itself where no slot names it)
-        bool y_named = false;
-        if (any)
-            for (int k = tid; k < a.K; k += nt) {
-                const float t = sl.own[k];
-                if (t < 0.f) continue;
-                const bool is_y = sl.id[k] == y;
-                y_named |= is_y;
-                if (mine(sl.id[k]))
-                    put(dz + sl.id[k], dense(sl.zk[k]) - w * (a.kl_tau * t + (is_y ? a.ce : 0.f)));
-            }
-        y_named = __syncthreads_or(y_named);
-        if (y >= 0 && !y_named && tid == 0 && mine(y)) put(dz + y, dense(zy) - w * a.ce);
     }
+    // no CTA leaves while another may still send to it
     __syncwarp();
-    if (C > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    cluster_sync_all();
 }
 
 int distill_sms() {
@@ -471,23 +796,57 @@ int distill_sms() {
     return n;
 }
 
-template <typename T, int NV, bool TWO>
-cudaError_t launch_distill_rows(const DistillArgs& a, int C, int threads, cudaStream_t st) {
+template <typename T, int NT, bool TWO>
+cudaError_t launch_distill_rows(const DistillArgs& a, DistillPlan pl, cudaStream_t st) {
+    auto kern = distill_row_kernel<T, NT, TWO>;
+    static std::once_flag once[64];
+    static cudaError_t set_err[64];
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+    std::call_once(once[dev], [&] {
+        set_err[dev] = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                            (int)kDSmem);
+    });
+    if (set_err[dev] != cudaSuccess) return set_err[dev];
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)a.T * (unsigned)C);
-    cfg.blockDim = dim3((unsigned)threads);
-    cfg.dynamicSmemBytes = (size_t)a.K * 16;
+    cfg.gridDim = dim3((unsigned)pl.C);
+    cfg.blockDim = dim3(NT + 32 + 32 * kDSlotWarps);
+    cfg.dynamicSmemBytes = pl.smem;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = (unsigned)C;
-    attr[1].val.clusterDim.y = 1;
-    attr[1].val.clusterDim.z = 1;
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)pl.C;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = C > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, distill_row_kernel<T, NV, TWO>, a, C);
+    cfg.numAttrs = 2;
+    // no more clusters than run at once (their SMs have to lie together, so this is not the
+    // SMs over C): rows are dealt out in turn, and a late cluster's would come late.  Asked
+    // once for a device, cluster size and shared memory, in steps of 4 KB.
+    static std::mutex lock;
+    static int fit[64][4][64];
+    const int step = (int)((pl.smem + 4095) / 4096), lc = pl.C == 1 ? 0 : pl.C == 2 ? 1 : pl.C == 4 ? 2 : 3;
+    int n;
+    {
+        std::lock_guard<std::mutex> hold(lock);
+        int& f = fit[dev][lc][step];
+        if (!f) {
+            cudaLaunchConfig_t q = cfg;
+            q.numAttrs = 1;
+            q.dynamicSmemBytes = (size_t)step * 4096 < kDSmem ? (size_t)step * 4096 : kDSmem;
+            e = cudaOccupancyMaxActiveClusters(&n, kern, &q);
+            if (e != cudaSuccess) return e;
+            f = n > 0 ? n : 1;
+        }
+        n = f;
+    }
+    pl.clusters = a.T < n ? a.T : n;
+    cfg.gridDim = dim3((unsigned)(pl.clusters * pl.C));
+    return cudaLaunchKernelEx(&cfg, kern, a, pl);
 }
 
 template <typename T, bool TWO>
@@ -497,23 +856,36 @@ cudaError_t launch_distill(const DistillArgs& a, cudaStream_t st) {
         if (a.V <= 256) return launch_pdl(distill_warp_kernel<T, 8, TWO>, grid, block, 0, st, a);
         return launch_pdl(distill_warp_kernel<T, 32, TWO>, grid, block, 0, st, a);
     }
-    constexpr int VE = 16 / (int)sizeof(T);
-    constexpr int kMost = 64 / VE;   // vectors a thread: 64 symbols
-    // the fewest CTAs a row whose threads hold it, and more while the rows alone leave SMs
-    // without a CTA and each thread has two vectors or more
-    const long long n_vec = a.V / VE;
-    int C = 1;
-    while (C < 8 && n_vec > (long long)C * kDThreads * kMost) C *= 2;
     const int sms = distill_sms();
-    while (C < 8 && (long long)a.T * C * 2 <= sms && n_vec > (long long)C * kDThreads * 2) C *= 2;
-    const int per = (int)((n_vec + C - 1) / C);
-    int threads = 128;
-    while (threads < kDThreads && per > threads * 2) threads *= 2;
-    const int nv = (per + threads - 1) / threads;
-    if (nv <= 2) return launch_distill_rows<T, 2, TWO>(a, C, threads, st);
-    if (nv <= 4) return launch_distill_rows<T, 4, TWO>(a, C, threads, st);
-    if (nv <= 8 || kMost == 8) return launch_distill_rows<T, 8, TWO>(a, C, threads, st);
-    return launch_distill_rows<T, kMost, TWO>(a, C, threads, st);
+    const long long bytes = (long long)a.V * (int)sizeof(T) + 32;
+    DistillPlan pl;
+    // the fewest CTAs a row whose slices fit 64 KB (8 at most); more while the rows alone
+    // leave SMs without a CTA and a slice has 8 KB or more
+    pl.C = 1;
+    while (pl.C < 8 && bytes > pl.C * 65536ll) pl.C *= 2;
+    while (pl.C < 8 && (long long)a.T * pl.C * 2 <= sms && bytes > pl.C * 8192ll) pl.C *= 2;
+    // a slice: the row's vectors shared out, as a multiple of 128 bytes
+    const long long vecs = ((long long)a.V + 16 / sizeof(T) - 1) / (16 / sizeof(T)) + 1;
+    pl.slice = (int)(((vecs + pl.C - 1) / pl.C * 16 + 127) / 128 * 128);
+    // eight vectors a thread: 512 threads and one CTA an SM for 64 KB, and so on down
+    const int nt = pl.slice <= 16384 ? 128 : pl.slice <= 32768 ? 256 : 512;
+    const int per_sm = nt == 128 ? 4 : nt == 256 ? 2 : 1;
+    pl.table = 64;
+    while (pl.table < 2 * a.K) pl.table *= 2;
+    if (!a.K) pl.table = 0;
+    const size_t slots = (((size_t)a.K * 16 + (size_t)pl.table * 8) + 15) & ~(size_t)15;
+    const size_t fixed = (size_t)kDStats * pl.C * (nt / 32) * 16 + kDSlotWarps * slots +
+                         sizeof(DistillBars);
+    const size_t room = kDSmem / per_sm - (per_sm > 1 ? 1024 : 0);
+    pl.bufs = 3;
+    while (pl.bufs > 1 && fixed + (size_t)pl.bufs * pl.slice > room) --pl.bufs;
+    if (pl.bufs == 1 && 2 * (size_t)pl.slice + fixed <= kDSmem) pl.bufs = 2;
+    pl.look = pl.bufs > 1;
+    pl.smem = fixed + (size_t)pl.bufs * pl.slice;
+    pl.clusters = 0;   // the launch's
+    if (nt == 128) return launch_distill_rows<T, 128, TWO>(a, pl, st);
+    if (nt == 256) return launch_distill_rows<T, 256, TWO>(a, pl, st);
+    return launch_distill_rows<T, 512, TWO>(a, pl, st);
 }
 
 }  // namespace
