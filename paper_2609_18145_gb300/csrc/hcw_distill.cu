@@ -32,6 +32,7 @@ namespace {
 constexpr int kDMaxK = 1024;          // slots of a row
 constexpr int kDMaxV = 262144;        // 8 CTAs x 128 KB of fp32 logits
 constexpr size_t kDSmem = 232448;     // shared memory of an SM
+constexpr long long kDSlice = 65536;  // bytes of a row a CTA takes by choice
 constexpr int kDWarpV = 1024;         // a warp a row up to here,
 constexpr int kDWarpK = 64;           // and up to this many slots
 constexpr int kDWarps = 8;            // rows of a CTA of the warp kernel
@@ -86,17 +87,27 @@ __device__ __forceinline__ Stat stat_join(const Stat& x, const Stat& y, float c)
     return r;
 }
 
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+__device__ __forceinline__ float warp_max(float v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+    return v;
+}
+
+// The lanes' parts joined, on every lane: the maximum first, then one exponential a lane.
 template <bool TWO>
 __device__ __forceinline__ Stat stat_warp(Stat v, float c) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        Stat u;
-        u.m = __shfl_xor_sync(0xffffffffu, v.m, o);
-        u.s = __shfl_xor_sync(0xffffffffu, v.s, o);
-        u.s1 = TWO ? __shfl_xor_sync(0xffffffffu, v.s1, o) : u.s;
-        v = stat_join<TWO>(v, u, c);
-    }
-    return v;
+    Stat r;
+    r.m = warp_max(v.m);
+    // a part without symbols has no sum (one with NaN keeps it)
+    const float d = v.m == -INFINITY ? 0.f : v.m - stat_base(r.m);
+    r.s = warp_sum(v.s * ex2(d * c));
+    r.s1 = TWO ? warp_sum(v.s1 * ex2(d * kLog2e)) : r.s;
+    return r;
 }
 
 template <typename T>
@@ -117,17 +128,6 @@ struct Slots {
     float *p, *own, *zk;
     int* id;
 };
-
-__device__ __forceinline__ float warp_sum(float v) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    return v;
-}
-__device__ __forceinline__ float warp_max(float v) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
-    return v;
-}
 
 // One warp: fills p and id from the row's slots; returns sum_k p_k log p_k, and in *any
 // whether there is a slot with any probability.
@@ -325,7 +325,7 @@ __global__ void __launch_bounds__(32 * kDWarps) distill_warp_kernel(const Distil
 //   slot warps    rows in turn: the teacher's probabilities and the named symbols' logits;
 //                 the loss; and, behind the dense values of pass B, those symbols
 // so that no role waits for another CTA's current row.  Rows of weight 0 are not read.
-constexpr int kDSlotWarps = 2;
+constexpr int kDSlotWarps = 4;   // at most
 // Stat buffers.  A CTA sends row n + R's parts when every warp of the cluster has been
 // through pass A of row n + R - 2, so through pass B of n + R - 4, whose slot flags say that
 // row n + R - 4 - kDSlotWarps has left the slot warps: nobody reads row n's parts any more.
@@ -347,6 +347,7 @@ struct __align__(8) DistillBars {
 struct DistillPlan {
     int C, clusters, bufs, look, slice;   // slice: bytes of a buffer
     int table;                            // entries of a slot warp's symbol table
+    int sw_log2;                          // log2 of the slot warps that take rows
     size_t smem;
 };
 
@@ -395,13 +396,23 @@ __device__ __forceinline__ void send16(const void* at, const uint64_t* bar, uint
         : "memory");
 }
 
-// The joined statistic of a row from its n parts, on every lane, in a fixed order.
+// The joined statistic of a row from its n parts (at most 4 a lane), on every lane, in a
+// fixed order.
 template <bool TWO>
 __device__ __forceinline__ Stat stat_read(const float4* part, int n, int lane, float c) {
+    float4 q[4];
     Stat v = {-INFINITY, 0.f, 0.f};
-    for (int i = lane; i < n; i += 32) {
-        const float4 q = part[i];
-        v = stat_join<TWO>(v, Stat{q.x, q.y, q.z}, c);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        q[i] = lane + 32 * i < n ? part[lane + 32 * i] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+        v.m = fmaxf(v.m, q[i].x);
+    }
+    const float b = stat_base(v.m);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float d = q[i].x == -INFINITY ? 0.f : q[i].x - b;
+        v.s += q[i].y * ex2(d * c);
+        if (TWO) v.s1 += q[i].z * ex2(d * kLog2e);
     }
     return stat_warp<TWO>(v, c);
 }
@@ -420,7 +431,7 @@ __global__ void __launch_bounds__(NT + 32 + 32 * kDSlotWarps, NT == 512 ? 1 : NT
     uint8_t* const slot_mem = p;
     const size_t slot_bytes = (size_t)a.K * 16 + (size_t)pl.table * 8;
     DistillBars* const bars =
-        reinterpret_cast<DistillBars*>(p + kDSlotWarps * ((slot_bytes + 15) & ~(size_t)15));
+        reinterpret_cast<DistillBars*>(p + ((slot_bytes + 15) & ~(size_t)15) * ((size_t)1 << pl.sw_log2));
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, tid = threadIdx.x;
     const int rank = (int)blockIdx.x % pl.C, first = (int)blockIdx.x / pl.C;
     const float c = a.inv_tau * kLog2e;
@@ -444,11 +455,11 @@ __global__ void __launch_bounds__(NT + 32 + 32 * kDSlotWarps, NT == 512 ? 1 : NT
     pdl_trigger();
 
     // A row's vectors: those its symbols touch, the first and the last perhaps shared with
-    // the rows beside it.  [v0, v1): this CTA's.
+    // the rows beside it.  [v0, v1): this CTA's; [i0, i1): those wholly of the row.
     struct Row {
         size_t at;       // the row's first symbol
         int skew;        // symbols of vector 0 before it
-        int n, v0, v1;
+        int n, v0, v1, i0, i1;
     };
     auto row_of = [&](int row) {
         Row r;
@@ -458,7 +469,19 @@ __global__ void __launch_bounds__(NT + 32 + 32 * kDSlotWarps, NT == 512 ? 1 : NT
         const int per = (r.n + pl.C - 1) / pl.C;
         r.v0 = rank * per < r.n ? rank * per : r.n;
         r.v1 = r.v0 + per < r.n ? r.v0 + per : r.n;
+        r.i0 = r.v0 == 0 && r.skew ? 1 : r.v0;
+        r.i1 = r.v1 == r.n && (r.skew + a.V) % VE ? r.n - 1 : r.v1;
         return r;
+    };
+    // The symbol of a shared vector of this CTA's that a lane looks after (the first
+    // vector's with lanes 0 .. VE - 1, the last one's with the next VE), or -1.
+    auto edge_of = [&](const Row& r) {
+        const bool last = lane >= VE;
+        const int v = last ? r.n - 1 : 0;
+        const int j = v * VE + (lane & (VE - 1)) - r.skew;
+        const bool shared = last ? r.v1 == r.n && r.i1 < r.n && (r.n > 1 || !r.skew)
+                                 : r.v0 == 0 && r.skew != 0;
+        return lane < 2 * VE && shared && r.v0 < r.v1 && j >= 0 && j < a.V ? j : -1;
     };
     const T* const zb = static_cast<const T*>(a.z);
     T* const gb = static_cast<T*>(a.dz);
@@ -509,7 +532,7 @@ __global__ void __launch_bounds__(NT + 32 + 32 * kDSlotWarps, NT == 512 ? 1 : NT
                 }
     } else if (warp > NW) {
         // ------------------------------------------------------------ slot warps
-        const int sw = warp - NW - 1;
+        const int sw = warp - NW - 1, sw_n = 1 << pl.sw_log2;
         Slots sl;
         sl.p = reinterpret_cast<float*>(slot_mem + sw * ((slot_bytes + 15) & ~(size_t)15));
         sl.own = sl.p + a.K;
@@ -518,10 +541,10 @@ __global__ void __launch_bounds__(NT + 32 + 32 * kDSlotWarps, NT == 512 ? 1 : NT
         int* const table = sl.id + a.K;
         RowCursor cur(a, first, pl.clusters, lane);
         int n = 0;
-        bool ok = true;
+        bool ok = sw < sw_n;
         for (; ok && cur.seek(); cur.next(), ++n) {
-            if (n % kDSlotWarps != sw) continue;
-            const uint32_t phase = (n / kDSlotWarps) & 1;
+            if ((n & (sw_n - 1)) != sw) continue;
+            const uint32_t phase = (n >> pl.sw_log2) & 1;
             const float w = cur.w();
             const Row r = row_of(cur.row);
             const T* z = zb + r.at;
@@ -611,25 +634,6 @@ __global__ void __launch_bounds__(NT + 32 + 32 * kDSlotWarps, NT == 512 ? 1 : NT
         };
         const uint32_t ninf = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;
         const uint64_t cc = f32x2_pack(c, c), ll = f32x2_pack(kLog2e, kLog2e);
-        // vector v of the row as it lies in shared memory, symbols of other rows masked
-        auto vec = [&](const Row& r, const uint4* buf, int v) {
-            uint4 u = buf[v - r.v0];
-            if (v == 0 || v == r.n - 1) {
-                uint32_t ws[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-                for (int e = 0; e < VE; ++e) {
-                    const int j = v * VE + e - r.skew;
-                    if (j >= 0 && j < a.V) continue;
-                    if (sizeof(T) == 4)
-                        ws[e] = ninf;
-                    else
-                        ws[e >> 1] = e & 1 ? (ws[e >> 1] & 0xFFFFu) | 0xFF800000u
-                                           : (ws[e >> 1] & 0xFFFF0000u) | 0xFF80u;
-                }
-                u = make_uint4(ws[0], ws[1], ws[2], ws[3]);
-            }
-            return u;
-        };
         bool ok = true;
         auto wait = [&](uint64_t* bar, uint32_t parity, bool cluster = false) {
             const bool w = cluster ? mbar_wait_cluster(bar, parity, abort, kDTimeoutNs)
@@ -643,11 +647,11 @@ __global__ void __launch_bounds__(NT + 32 + 32 * kDSlotWarps, NT == 512 ? 1 : NT
             const Row r = row_of(row);
             const uint4* buf = reinterpret_cast<const uint4*>(dsm + (size_t)b * pl.slice);
             Stat st = {-INFINITY, 0.f, 0.f};
-            for (int g = r.v0 + tid; g < r.v1; g += G * NT) {
+            for (int g = r.i0 + tid; g < r.i1; g += G * NT) {
                 uint4 q[G];
 #pragma unroll
                 for (int k = 0; k < G; ++k)
-                    q[k] = g + k * NT < r.v1 ? vec(r, buf, g + k * NT)
+                    q[k] = g + k * NT < r.i1 ? buf[g + k * NT - r.v0]
                                              : make_uint4(ninf, ninf, ninf, ninf);
                 Stat u = {-INFINITY, 0.f, 0.f};
                 if (sizeof(T) == 2) {
@@ -684,6 +688,14 @@ __global__ void __launch_bounds__(NT + 32 + 32 * kDSlotWarps, NT == 512 ? 1 : NT
                 u.s1 = TWO ? sf1.x + sf1.y : u.s;
                 st = stat_join<TWO>(st, u, c);
             }
+            if (warp == 0) {
+                const int j = edge_of(r);
+                if (j >= 0) {
+                    const float x = logit(reinterpret_cast<const T*>(buf) + (j + r.skew - r.v0 * VE));
+                    const float d = x - stat_base(x);
+                    st = stat_join<TWO>(st, Stat{x, ex2(d * c), ex2(d * kLog2e)}, c);
+                }
+            }
             st = stat_warp<TWO>(st, c);
             uint64_t* const bar = &bars->stat[n % kDStats];
             float4* const at = stats + (n % kDStats) * parts + rank * NW + warp;
@@ -691,9 +703,9 @@ __global__ void __launch_bounds__(NT + 32 + 32 * kDSlotWarps, NT == 512 ? 1 : NT
             if (lane < pl.C) send16(at, bar, (uint32_t)lane, st.m, st.s, st.s1);
         };
         auto pass_b = [&](int row, int n, float w) {
-            const int sw = n % kDSlotWarps, b = n % pl.bufs;
+            const int sw = n & ((1 << pl.sw_log2) - 1), b = n % pl.bufs;
             if (!wait(&bars->stat[n % kDStats], (n / kDStats) & 1, true)) return;
-            if (!wait(&bars->ready[sw], (n / kDSlotWarps) & 1)) return;
+            if (!wait(&bars->ready[sw], (n >> pl.sw_log2) & 1)) return;
             Stat st = stat_read<TWO>(stats + (n % kDStats) * parts, parts, lane, c);
             bool any = bars->any[sw] != 0, label = bars->label[sw] != 0;
             if (st.s == 0.f) {
@@ -703,7 +715,6 @@ __global__ void __launch_bounds__(NT + 32 + 32 * kDSlotWarps, NT == 512 ? 1 : NT
             if (gb) {
                 const Row r = row_of(row);
                 const uint4* buf = reinterpret_cast<const uint4*>(dsm + (size_t)b * pl.slice);
-                T* const dz = gb + r.at;
                 uint4* const dv = reinterpret_cast<uint4*>(gb + (r.at - r.skew));
                 const float nb = -stat_base(st.m);
                 const float fq = any ? w * a.kl_tau / st.s : 0.f;
@@ -712,7 +723,7 @@ __global__ void __launch_bounds__(NT + 32 + 32 * kDSlotWarps, NT == 512 ? 1 : NT
                 const uint64_t ff = TWO ? f32x2_pack(fq, fq) : f32x2_pack(fq + f1, fq + f1);
                 const uint64_t ff1 = f32x2_pack(f1, f1);
 #pragma unroll 4
-                for (int v = r.v0 + tid; v < r.v1; v += NT) {
+                for (int v = r.i0 + tid; v < r.i1; v += NT) {
                     const uint4 q = buf[v - r.v0];
                     uint32_t o[4];
 #pragma unroll
@@ -732,15 +743,15 @@ __global__ void __launch_bounds__(NT + 32 + 32 * kDSlotWarps, NT == 512 ? 1 : NT
                             o[2 * i + 1] = __float_as_uint(h.y);
                         }
                     }
-                    const uint4 u = make_uint4(o[0], o[1], o[2], o[3]);
-                    if (v != 0 && v != r.n - 1) {
-                        dv[v] = u;
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < VE; ++e) {
-                            const int j = v * VE + e - r.skew;
-                            if (j >= 0 && j < a.V) put(dz + j, elem(u, e));
-                        }
+                    dv[v] = make_uint4(o[0], o[1], o[2], o[3]);
+                }
+                if (warp == 0) {
+                    const int j = edge_of(r);
+                    if (j >= 0) {
+                        const float d =
+                            logit(reinterpret_cast<const T*>(buf) + (j + r.skew - r.v0 * VE)) + nb;
+                        put(gb + r.at + j, TWO ? fq * ex2(d * c) + f1 * ex2(d * kLog2e)
+                                               : (fq + f1) * ex2(d * c));
                     }
                 }
             }
@@ -758,16 +769,10 @@ __global__ void __launch_bounds__(NT + 32 + 32 * kDSlotWarps, NT == 512 ? 1 : NT
                 if (gb) {
                     const Row r = row_of(cb.row);
                     uint4* const dv = reinterpret_cast<uint4*>(gb + (r.at - r.skew));
-                    for (int v = r.v0 + tid; v < r.v1; v += NT) {
-                        if (v != 0 && v != r.n - 1) {
-                            dv[v] = make_uint4(0u, 0u, 0u, 0u);
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < VE; ++e) {
-                                const int j = v * VE + e - r.skew;
-                                if (j >= 0 && j < a.V) put(gb + r.at + j, 0.f);
-                            }
-                        }
+                    for (int v = r.i0 + tid; v < r.i1; v += NT) dv[v] = make_uint4(0u, 0u, 0u, 0u);
+                    if (warp == 0) {
+                        const int j = edge_of(r);
+                        if (j >= 0) put(gb + r.at + j, 0.f);
                     }
                 }
                 if (rank == 0 && tid == 0 && a.loss) a.loss[cb.row] = 0.f;
@@ -862,21 +867,24 @@ cudaError_t launch_distill(const DistillArgs& a, cudaStream_t st) {
     // the fewest CTAs a row whose slices fit 64 KB (8 at most); more while the rows alone
     // leave SMs without a CTA and a slice has 8 KB or more
     pl.C = 1;
-    while (pl.C < 8 && bytes > pl.C * 65536ll) pl.C *= 2;
+    while (pl.C < 8 && bytes > pl.C * (kDSlice + 1024)) pl.C *= 2;
     while (pl.C < 8 && (long long)a.T * pl.C * 2 <= sms && bytes > pl.C * 8192ll) pl.C *= 2;
     // a slice: the row's vectors shared out, as a multiple of 128 bytes
     const long long vecs = ((long long)a.V + 16 / sizeof(T) - 1) / (16 / sizeof(T)) + 1;
     pl.slice = (int)(((vecs + pl.C - 1) / pl.C * 16 + 127) / 128 * 128);
     // eight vectors a thread: 512 threads and one CTA an SM for 64 KB, and so on down
-    const int nt = pl.slice <= 16384 ? 128 : pl.slice <= 32768 ? 256 : 512;
+    const int nt = pl.slice <= 17408 ? 128 : pl.slice <= 33792 ? 256 : 512;
     const int per_sm = nt == 128 ? 4 : nt == 256 ? 2 : 1;
     pl.table = 64;
     while (pl.table < 2 * a.K) pl.table *= 2;
     if (!a.K) pl.table = 0;
     const size_t slots = (((size_t)a.K * 16 + (size_t)pl.table * 8) + 15) & ~(size_t)15;
-    const size_t fixed = (size_t)kDStats * pl.C * (nt / 32) * 16 + kDSlotWarps * slots +
-                         sizeof(DistillBars);
     const size_t room = kDSmem / per_sm - (per_sm > 1 ? 1024 : 0);
+    // four slot warps, fewer where their slots would take a quarter of the room
+    pl.sw_log2 = 2;
+    while (pl.sw_log2 && (slots << pl.sw_log2) > room / 4) --pl.sw_log2;
+    const size_t fixed = (size_t)kDStats * pl.C * (nt / 32) * 16 + (slots << pl.sw_log2) +
+                         sizeof(DistillBars);
     pl.bufs = 3;
     while (pl.bufs > 1 && fixed + (size_t)pl.bufs * pl.slice > room) --pl.bufs;
     if (pl.bufs == 1 && 2 * (size_t)pl.slice + fixed <= kDSmem) pl.bufs = 2;
