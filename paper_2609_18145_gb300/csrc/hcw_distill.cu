@@ -317,35 +317,38 @@ __global__ void __launch_bounds__(32 * kDWarps) distill_warp_kernel(const Distil
 // ------------------------------------------------------------------ a cluster a row
 // Long rows: a persistent cluster of C CTAs takes rows in turn, each CTA a slice of the row's
 // 16-byte vectors.  A CTA's roles:
-//   producer      bulk copies of the slices of the next rows into a ring of NB buffers
+//   producer      bulk copies of the slices of the next rows into a ring of buffers
 //   NT compute    pass A (row n + 1): maximum and sum of the slice, each warp sending
 //     threads     its part to every CTA of the cluster (st.async, counted by an mbarrier);
-//                 then pass B (row n), whose parts arrived meanwhile: the gradient, from
+//                 then pass B (row n), whose factors are there by now: the gradient, from
 //                 the slice in shared memory
 //   slot warps    rows in turn: the teacher's probabilities and the named symbols' logits;
-//                 the loss; and, behind the dense values of pass B, those symbols
-// so that no role waits for another CTA's current row.  Rows of weight 0 are not read.
+//                 the row's parts joined, and its factors for pass B; the loss; and, behind
+//                 the dense values of pass B, the named symbols
+// so that no compute warp waits for another CTA's current row.  Rows of weight 0 are not
+// read.
 constexpr int kDSlotWarps = 4;   // at most
-// Stat buffers.  A CTA sends row n + R's parts when every warp of the cluster has been
-// through pass A of row n + R - 2, so through pass B of n + R - 4, whose slot flags say that
-// row n + R - 4 - kDSlotWarps has left the slot warps: nobody reads row n's parts any more.
-constexpr int kDStats = 8;
-static_assert(kDStats >= 4 + kDSlotWarps, "stat ring");
+// Buffers of parts.  A CTA sends row m's parts after its pass B of row m - 2, whose factors
+// need every warp's pass A of row m - 2, which comes after that warp's pass B of row m - 4
+// and so after row m - 4 was joined: four buffers hold all rows that may still be read.
+constexpr int kDStats = 4;
 constexpr int kDMaxBufs = 4;
 constexpr unsigned long long kDTimeoutNs = 2000000000ull;
 
-struct __align__(8) DistillBars {
+struct __align__(16) DistillBars {
     uint64_t full[kDMaxBufs];        // a row's slice has landed
     uint64_t empty[kDMaxBufs];       // pass B has read it
     uint64_t stat[kDStats];          // every warp of the cluster has sent its part
-    uint64_t ready[kDSlotWarps];     // the slot warp's flags for its row are set
+    uint64_t ready[kDSlotWarps];     // the slot warp's factors for its row are set
     uint64_t dense[kDSlotWarps];     // the dense values of its row are stored
-    int any[kDSlotWarps], label[kDSlotWarps];
+    // pass B's subtrahend of the exponents, factor at the teacher's temperature (of both
+    // softmaxes where they are one) and factor at temperature 1
+    float4 factor[kDSlotWarps];
     int abort;
 };
 
 struct DistillPlan {
-    int C, clusters, bufs, look, slice;   // slice: bytes of a buffer
+    int C, C_log2, clusters, bufs, look, slice;   // slice: bytes of a buffer
     int table;                            // entries of a slot warp's symbol table
     int sw_log2;                          // log2 of the slot warps that take rows
     size_t smem;
@@ -466,7 +469,7 @@ __global__ void __launch_bounds__(NT + 32 + 32 * kDSlotWarps, NT == 512 ? 1 : NT
         r.at = (size_t)row * a.V;
         r.skew = (int)(r.at % VE);
         r.n = (r.skew + a.V + VE - 1) / VE;
-        const int per = (r.n + pl.C - 1) / pl.C;
+        const int per = (r.n + pl.C - 1) >> pl.C_log2;
         r.v0 = rank * per < r.n ? rank * per : r.n;
         r.v1 = r.v0 + per < r.n ? r.v0 + per : r.n;
         r.i0 = r.v0 == 0 && r.skew ? 1 : r.v0;
@@ -561,11 +564,6 @@ __global__ void __launch_bounds__(NT + 32 + 32 * kDSlotWarps, NT == 512 ? 1 : NT
             bool any = false;
             float ent = 0.f;
             if (a.K) ent = slots_read(a, (size_t)cur.row, sl, lane, &any);
-            if (lane == 0) {
-                bars->any[sw] = any;
-                bars->label[sw] = y >= 0;
-                mbar_arrive(&bars->ready[sw]);
-            }
             const float zy = y >= 0 && (rank == 0 || mine(y)) ? logit(z + y) : 0.f;
             for (int k = lane; k < a.K; k += 32) {
                 const int i = sl.id[k];
@@ -582,6 +580,11 @@ __global__ void __launch_bounds__(NT + 32 + 32 * kDSlotWarps, NT == 512 ? 1 : NT
                 any = false;
                 y = -1;
                 st.s = st.s1 = 1.f;
+            }
+            const float fq = any ? w * a.kl_tau / st.s : 0.f, f1 = y >= 0 ? w * a.ce / st.s1 : 0.f;
+            if (lane == 0) {
+                bars->factor[sw] = make_float4(-base, TWO ? fq : fq + f1, f1, 0.f);
+                mbar_arrive(&bars->ready[sw]);
             }
             if (rank == 0 && a.loss) {
                 // log-sums relative to the maximum, as the logits are: the row's own size
@@ -600,7 +603,6 @@ __global__ void __launch_bounds__(NT + 32 + 32 * kDSlotWarps, NT == 512 ? 1 : NT
             ok = __all_sync(0xffffffffu, w2);
             if (!ok) break;
             if (!dz) continue;
-            const float fq = any ? w * a.kl_tau / st.s : 0.f, f1 = y >= 0 ? w * a.ce / st.s1 : 0.f;
             auto dense = [&](float x) {
                 const float e = ex2((x - base) * c);
                 return TWO ? fq * e + f1 * ex2((x - base) * kLog2e) : (fq + f1) * e;
@@ -635,15 +637,20 @@ __global__ void __launch_bounds__(NT + 32 + 32 * kDSlotWarps, NT == 512 ? 1 : NT
         const uint32_t ninf = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;
         const uint64_t cc = f32x2_pack(c, c), ll = f32x2_pack(kLog2e, kLog2e);
         bool ok = true;
-        auto wait = [&](uint64_t* bar, uint32_t parity, bool cluster = false) {
-            const bool w = cluster ? mbar_wait_cluster(bar, parity, abort, kDTimeoutNs)
-                                   : mbar_wait(bar, parity, abort, kDTimeoutNs);
+        auto wait = [&](uint64_t* bar, uint32_t parity) {
+            const bool w = mbar_wait(bar, parity, abort, kDTimeoutNs);
             ok = __all_sync(0xffffffffu, w);
             return ok;
         };
+        // buffers of the next row of either pass, and pass A's parity
+        int ba = 0, bb = 0, pa = 0;
         auto pass_a = [&](int row, int n) {
-            const int b = n % pl.bufs;
-            if (!wait(&bars->full[b], (n / pl.bufs) & 1)) return;
+            const int b = ba;
+            if (!wait(&bars->full[b], pa)) return;
+            if (++ba == pl.bufs) {
+                ba = 0;
+                pa ^= 1;
+            }
             const Row r = row_of(row);
             const uint4* buf = reinterpret_cast<const uint4*>(dsm + (size_t)b * pl.slice);
             Stat st = {-INFINITY, 0.f, 0.f};
@@ -697,31 +704,24 @@ __global__ void __launch_bounds__(NT + 32 + 32 * kDSlotWarps, NT == 512 ? 1 : NT
                 }
             }
             st = stat_warp<TWO>(st, c);
+            if (!gb && lane == 0) mbar_arrive(&bars->empty[b]);   // read once
             uint64_t* const bar = &bars->stat[n % kDStats];
             float4* const at = stats + (n % kDStats) * parts + rank * NW + warp;
             if (tid == 0) mbar_arrive_expect_tx(bar, (uint32_t)(parts * sizeof(float4)));
             if (lane < pl.C) send16(at, bar, (uint32_t)lane, st.m, st.s, st.s1);
         };
-        auto pass_b = [&](int row, int n, float w) {
-            const int sw = n & ((1 << pl.sw_log2) - 1), b = n % pl.bufs;
-            if (!wait(&bars->stat[n % kDStats], (n / kDStats) & 1, true)) return;
+        auto pass_b = [&](int row, int n) {
+            const int sw = n & ((1 << pl.sw_log2) - 1), b = bb;
+            if (++bb == pl.bufs) bb = 0;
             if (!wait(&bars->ready[sw], (n >> pl.sw_log2) & 1)) return;
-            Stat st = stat_read<TWO>(stats + (n % kDStats) * parts, parts, lane, c);
-            bool any = bars->any[sw] != 0, label = bars->label[sw] != 0;
-            if (st.s == 0.f) {
-                any = label = false;
-                st.s = st.s1 = 1.f;
-            }
             if (gb) {
                 const Row r = row_of(row);
                 const uint4* buf = reinterpret_cast<const uint4*>(dsm + (size_t)b * pl.slice);
                 uint4* const dv = reinterpret_cast<uint4*>(gb + (r.at - r.skew));
-                const float nb = -stat_base(st.m);
-                const float fq = any ? w * a.kl_tau / st.s : 0.f;
-                const float f1 = label ? w * a.ce / st.s1 : 0.f;
-                const uint64_t nbb = f32x2_pack(nb, nb);
-                const uint64_t ff = TWO ? f32x2_pack(fq, fq) : f32x2_pack(fq + f1, fq + f1);
-                const uint64_t ff1 = f32x2_pack(f1, f1);
+                const float4 f = bars->factor[sw];
+                const float nb = f.x;
+                const uint64_t nbb = f32x2_pack(nb, nb), ff = f32x2_pack(f.y, f.y),
+                               ff1 = f32x2_pack(f.z, f.z);
 #pragma unroll 4
                 for (int v = r.i0 + tid; v < r.i1; v += NT) {
                     const uint4 q = buf[v - r.v0];
@@ -732,8 +732,8 @@ __global__ void __launch_bounds__(NT + 32 + 32 * kDSlotWarps, NT == 512 ? 1 : NT
                         const float2 e = ex2_pair(f32x2_mul(d, cc));
                         uint64_t g = f32x2_mul(f32x2_pack(e.x, e.y), ff);
                         if (TWO) {
-                            const float2 f = ex2_pair(f32x2_mul(d, ll));
-                            g = f32x2_fma(f32x2_pack(f.x, f.y), ff1, g);
+                            const float2 e1 = ex2_pair(f32x2_mul(d, ll));
+                            g = f32x2_fma(f32x2_pack(e1.x, e1.y), ff1, g);
                         }
                         const float2 h = f32x2_unpack(g);
                         if (sizeof(T) == 2) {
@@ -750,14 +750,14 @@ __global__ void __launch_bounds__(NT + 32 + 32 * kDSlotWarps, NT == 512 ? 1 : NT
                     if (j >= 0) {
                         const float d =
                             logit(reinterpret_cast<const T*>(buf) + (j + r.skew - r.v0 * VE)) + nb;
-                        put(gb + r.at + j, TWO ? fq * ex2(d * c) + f1 * ex2(d * kLog2e)
-                                               : (fq + f1) * ex2(d * c));
+                        put(gb + r.at + j, TWO ? f.y * ex2(d * c) + f.z * ex2(d * kLog2e)
+                                               : f.y * ex2(d * c));
                     }
                 }
             }
             __syncwarp();
             if (lane == 0) {
-                mbar_arrive(&bars->empty[b]);
+                if (gb) mbar_arrive(&bars->empty[b]);
                 mbar_arrive(&bars->dense[sw]);
             }
         };
@@ -784,7 +784,7 @@ __global__ void __launch_bounds__(NT + 32 + 32 * kDSlotWarps, NT == 512 ? 1 : NT
                 ca.next();
             }
             if (!ok) break;
-            pass_b(cb.row, nb, w);
+            pass_b(cb.row, nb);
             ++nb;
         }
     }
@@ -834,7 +834,7 @@ cudaError_t launch_distill_rows(const DistillArgs& a, DistillPlan pl, cudaStream
     // once for a device, cluster size and shared memory, in steps of 4 KB.
     static std::mutex lock;
     static int fit[64][4][64];
-    const int step = (int)((pl.smem + 4095) / 4096), lc = pl.C == 1 ? 0 : pl.C == 2 ? 1 : pl.C == 4 ? 2 : 3;
+    const int step = (int)((pl.smem + 4095) / 4096), lc = pl.C_log2;
     int n;
     {
         std::lock_guard<std::mutex> hold(lock);
@@ -869,6 +869,7 @@ cudaError_t launch_distill(const DistillArgs& a, cudaStream_t st) {
     pl.C = 1;
     while (pl.C < 8 && bytes > pl.C * (kDSlice + 1024)) pl.C *= 2;
     while (pl.C < 8 && (long long)a.T * pl.C * 2 <= sms && bytes > pl.C * 8192ll) pl.C *= 2;
+    pl.C_log2 = pl.C == 1 ? 0 : pl.C == 2 ? 1 : pl.C == 4 ? 2 : 3;
     // a slice: the row's vectors shared out, as a multiple of 128 bytes
     const long long vecs = ((long long)a.V + 16 / sizeof(T) - 1) / (16 / sizeof(T)) + 1;
     pl.slice = (int)(((vecs + pl.C - 1) / pl.C * 16 + 127) / 128 * 128);
