@@ -54,6 +54,11 @@ struct DistillArgs {
 
 constexpr float kLog2e = 1.4426950408889634f;
 
+// The exponentials of a symbol: one (a single temperature in use), one at each of two
+// temperatures, or, where the teacher's is 2, the one at temperature 1 as the square of the
+// other.
+enum DistillExps { kOne = 0, kTwo = 1, kSquare = 2 };
+
 __device__ __forceinline__ float ex2(float x) {
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
@@ -69,7 +74,7 @@ struct Stat {
 // all -inf (exp2(-inf - 0) = 0, where -inf - -inf would be NaN).
 __device__ __forceinline__ float stat_base(float m) { return m == -INFINITY ? 0.f : m; }
 
-template <bool TWO>
+template <int EXPS>
 __device__ __forceinline__ Stat stat_join(const Stat& x, const Stat& y, float c) {
     Stat r;
     r.m = fmaxf(x.m, y.m);
@@ -78,7 +83,7 @@ __device__ __forceinline__ Stat stat_join(const Stat& x, const Stat& y, float c)
     // a part without symbols has no sum; one with NaN keeps it
     const float fx = ex2(dx * c), fy = ex2(dy * c);
     r.s = (x.m == -INFINITY ? x.s : x.s * fx) + (y.m == -INFINITY ? y.s : y.s * fy);
-    if (TWO) {
+    if (EXPS != kOne) {
         const float gx = ex2(dx * kLog2e), gy = ex2(dy * kLog2e);
         r.s1 = (x.m == -INFINITY ? x.s1 : x.s1 * gx) + (y.m == -INFINITY ? y.s1 : y.s1 * gy);
     } else {
@@ -99,14 +104,14 @@ __device__ __forceinline__ float warp_max(float v) {
 }
 
 // The lanes' parts joined, on every lane: the maximum first, then one exponential a lane.
-template <bool TWO>
+template <int EXPS>
 __device__ __forceinline__ Stat stat_warp(Stat v, float c) {
     Stat r;
     r.m = warp_max(v.m);
     // a part without symbols has no sum (one with NaN keeps it)
     const float d = v.m == -INFINITY ? 0.f : v.m - stat_base(r.m);
     r.s = warp_sum(v.s * ex2(d * c));
-    r.s1 = TWO ? warp_sum(v.s1 * ex2(d * kLog2e)) : r.s;
+    r.s1 = EXPS != kOne ? warp_sum(v.s1 * ex2(d * kLog2e)) : r.s;
     return r;
 }
 
@@ -137,28 +142,40 @@ __device__ __forceinline__ float slots_read(const DistillArgs& a, size_t row, co
     const float* tl = a.teacher + row * a.K;
     const float c = a.inv_tau;
     float m = -INFINITY;
-    for (int k = lane; k < a.K; k += 32) {
-        int i = idx[k];
-        if (i >= a.V) {
-            atomicExch(&g_error_word, kErrInvalid);
-            i = -1;
+    for (int k0 = lane; k0 < a.K; k0 += 64) {   // two of each on their way at once
+        int i[2];
+        float t[2];
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            const int k = k0 + 32 * q;
+            i[q] = k < a.K ? idx[k] : -1;
+            t[q] = k < a.K ? tl[k] : 0.f;
         }
-        const float t = i >= 0 ? tl[k] * c : -INFINITY;
-        s.id[k] = i;
-        s.p[k] = t;
-        m = fmaxf(m, t);
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            const int k = k0 + 32 * q;
+            if (k >= a.K) continue;
+            if (i[q] >= a.V) {
+                atomicExch(&g_error_word, kErrInvalid);
+                i[q] = -1;
+            }
+            const float x = i[q] >= 0 ? t[q] * c : -INFINITY;
+            s.id[k] = i[q];
+            s.p[k] = x;
+            m = fmaxf(m, x);
+        }
     }
     m = warp_max(m);
     const float b = stat_base(m);
     float sum = 0.f;
-    for (int k = lane; k < a.K; k += 32) sum += s.id[k] >= 0 ? expf(s.p[k] - b) : 0.f;
+    for (int k = lane; k < a.K; k += 32) sum += s.id[k] >= 0 ? ex2((s.p[k] - b) * kLog2e) : 0.f;
     sum = warp_sum(sum);
     *any = sum != 0.f;   // NaN counts: it belongs in the result
     const float lse = *any ? b + logf(sum) : 0.f, inv = *any ? 1.f / sum : 0.f;
     float ent = 0.f;
     for (int k = lane; k < a.K; k += 32) {
         const float t = s.p[k];
-        const float p = *any && s.id[k] >= 0 ? expf(t - b) * inv : 0.f;
+        const float p = *any && s.id[k] >= 0 ? ex2((t - b) * kLog2e) * inv : 0.f;
         s.p[k] = p;
         if (p != 0.f) ent += p * (t - lse);
     }
@@ -179,10 +196,24 @@ __device__ __forceinline__ float slot_owned(const Slots& s, int K, int k) {
     return t;
 }
 
-// One warp: fills own through a table of the symbols (open addressing, `size` a power of two
+// One warp: fills own, above 32 slots through a table of the symbols (open addressing, `size` a power of two
 // of at least 2 K entries of symbol and first slot).  Which entry a symbol gets depends on
 // the order of the threads, what is found there does not.
 __device__ __forceinline__ void slots_own(const Slots& s, int K, int* table, int size, int lane) {
+    if (K <= 32) {   // a slot a lane: the lanes with the same symbol
+        const int id = lane < K ? s.id[lane] : -1;
+        const uint32_t same = __match_any_sync(0xffffffffu, id);
+        if (lane < K) {
+            float t = -1.f;
+            if (id >= 0 && __ffs(same) - 1 == lane) {
+                t = 0.f;
+                for (uint32_t m = same; m; m &= m - 1) t += s.p[__ffs(m) - 1];
+            }
+            s.own[lane] = t;
+        }
+        __syncwarp();
+        return;
+    }
     int* const key = table;
     int* const low = table + size;
     for (int i = lane; i < size; i += 32) {
@@ -226,7 +257,7 @@ __device__ __forceinline__ void slots_own(const Slots& s, int K, int* table, int
 
 // ------------------------------------------------------------------ a warp a row
 // NE symbols a lane, symbol lane + 32 e: coalesced whatever the row's alignment.
-template <typename T, int NE, bool TWO>
+template <typename T, int NE, int EXPS>
 __global__ void __launch_bounds__(32 * kDWarps) distill_warp_kernel(const DistillArgs a) {
     __shared__ float sp[kDWarps][kDWarpK], so[kDWarps][kDWarpK], sz[kDWarps][kDWarpK];
     __shared__ int si[kDWarps][kDWarpK];
@@ -274,10 +305,10 @@ __global__ void __launch_bounds__(32 * kDWarps) distill_warp_kernel(const Distil
 #pragma unroll
     for (int e = 0; e < NE; ++e) {
         st.s += ex2((v[e] - base) * c);
-        if (TWO) st.s1 += ex2((v[e] - base) * kLog2e);
+        if (EXPS != kOne) st.s1 += ex2((v[e] - base) * kLog2e);
     }
     st.s = warp_sum(st.s);
-    st.s1 = TWO ? warp_sum(st.s1) : st.s;
+    st.s1 = EXPS != kOne ? warp_sum(st.s1) : st.s;
     if (st.s == 0.f) {   // no logit above -inf: nothing to learn from
         any = false;
         y = -1;
@@ -295,7 +326,7 @@ __global__ void __launch_bounds__(32 * kDWarps) distill_warp_kernel(const Distil
     const float fq = any ? w * a.kl_tau / st.s : 0.f, f1 = y >= 0 ? w * a.ce / st.s1 : 0.f;
     auto dense = [&](float x) {
         const float e = ex2((x - base) * c);
-        return TWO ? fq * e + f1 * ex2((x - base) * kLog2e) : (fq + f1) * e;
+        return EXPS != kOne ? fq * e + f1 * ex2((x - base) * kLog2e) : (fq + f1) * e;
     };
 #pragma unroll
     for (int e = 0; e < NE; ++e)
@@ -327,11 +358,19 @@ __global__ void __launch_bounds__(32 * kDWarps) distill_warp_kernel(const Distil
 //                 the dense values of pass B, the named symbols
 // so that no compute warp waits for another CTA's current row.  Rows of weight 0 are not
 // read.
-constexpr int kDSlotWarps = 4;   // at most
-// Buffers of parts.  A CTA sends row m's parts after its pass B of row m - 2, whose factors
-// need every warp's pass A of row m - 2, which comes after that warp's pass B of row m - 4
-// and so after row m - 4 was joined: four buffers hold all rows that may still be read.
-constexpr int kDStats = 4;
+// At most this many slot warps: a row's slots take about 10 us from their first load to the
+// last named symbol, of which a slot warp waits half for the row itself; 64 KB of logits
+// and as much gradient pass through an SM in 3 us.
+constexpr int slot_warps(int nt) { return nt == 512 ? 8 : nt == 256 ? 4 : 2; }
+constexpr int kDMaxSlotWarps = 8;   // slot warps in use: a power of two up to this
+// Buffers of parts, row n's in buffer n % kDStats.  A CTA sends row m's parts after its
+// pass B of row m - 2, whose factors need every warp's pass A of row m - 2, which comes after
+// that warp's pass B of row m - 4 and so after row m - 4 was joined: four buffers would hold
+// all rows that may still be read.  A wait for a buffer's barrier tells only odd from even
+// rounds, so the slot warp that waits for row n has to have seen row n - kDStats: the
+// buffers are a multiple of the slot warps, which makes it the same warp.
+constexpr int kDStats = 8;
+static_assert(kDStats >= 4 && kDStats % kDMaxSlotWarps == 0, "buffers of parts");
 constexpr int kDMaxBufs = 4;
 constexpr unsigned long long kDTimeoutNs = 2000000000ull;
 
@@ -339,11 +378,11 @@ struct __align__(16) DistillBars {
     uint64_t full[kDMaxBufs];        // a row's slice has landed
     uint64_t empty[kDMaxBufs];       // pass B has read it
     uint64_t stat[kDStats];          // every warp of the cluster has sent its part
-    uint64_t ready[kDSlotWarps];     // the slot warp's factors for its row are set
-    uint64_t dense[kDSlotWarps];     // the dense values of its row are stored
+    uint64_t ready[kDMaxSlotWarps];     // the slot warp's factors for its row are set
+    uint64_t dense[kDMaxSlotWarps];     // the dense values of its row are stored
     // pass B's subtrahend of the exponents, factor at the teacher's temperature (of both
     // softmaxes where they are one) and factor at temperature 1
-    float4 factor[kDSlotWarps];
+    float4 factor[kDMaxSlotWarps];
     int abort;
 };
 
@@ -401,7 +440,7 @@ __device__ __forceinline__ void send16(const void* at, const uint64_t* bar, uint
 
 // The joined statistic of a row from its n parts (at most 4 a lane), on every lane, in a
 // fixed order.
-template <bool TWO>
+template <int EXPS>
 __device__ __forceinline__ Stat stat_read(const float4* part, int n, int lane, float c) {
     float4 q[4];
     Stat v = {-INFINITY, 0.f, 0.f};
@@ -415,17 +454,17 @@ __device__ __forceinline__ Stat stat_read(const float4* part, int n, int lane, f
     for (int i = 0; i < 4; ++i) {
         const float d = q[i].x == -INFINITY ? 0.f : q[i].x - b;
         v.s += q[i].y * ex2(d * c);
-        if (TWO) v.s1 += q[i].z * ex2(d * kLog2e);
+        if (EXPS != kOne) v.s1 += q[i].z * ex2(d * kLog2e);
     }
-    return stat_warp<TWO>(v, c);
+    return stat_warp<EXPS>(v, c);
 }
 
-template <typename T, int NT, bool TWO>
-__global__ void __launch_bounds__(NT + 32 + 32 * kDSlotWarps, NT == 512 ? 1 : NT == 256 ? 2 : 4)
+template <typename T, int NT, int EXPS>
+__global__ void __launch_bounds__(NT + 32 + 32 * slot_warps(NT), NT == 512 ? 1 : NT == 256 ? 2 : 4)
     distill_row_kernel(const DistillArgs a, const DistillPlan pl) {
     constexpr int VE = 16 / (int)sizeof(T);   // symbols of a vector
     constexpr int NW = NT / 32;
-    constexpr int G = 8;                      // vectors a thread holds at once
+    constexpr int G = 4;                      // vectors a thread holds at once
     extern __shared__ __align__(128) uint8_t dsm[];
     uint8_t* p = dsm + (size_t)pl.bufs * pl.slice;
     float4* const stats = reinterpret_cast<float4*>(p);   // [kDStats][C * NW]
@@ -445,7 +484,7 @@ __global__ void __launch_bounds__(NT + 32 + 32 * kDSlotWarps, NT == 512 ? 1 : NT
             mbar_init(&bars->empty[i], NW);
         }
         for (int i = 0; i < kDStats; ++i) mbar_init(&bars->stat[i], 1);
-        for (int i = 0; i < kDSlotWarps; ++i) {
+        for (int i = 0; i < slot_warps(NT); ++i) {
             mbar_init(&bars->ready[i], 1);
             mbar_init(&bars->dense[i], NW);
         }
@@ -557,24 +596,30 @@ __global__ void __launch_bounds__(NT + 32 + 32 * kDSlotWarps, NT == 512 ? 1 : NT
                 return v >= r.v0 && v < r.v1;
             };
             int y = a.target ? a.target[cur.row] : -1;
+            bool any = false;
+            float ent = 0.f;
+            if (a.K) ent = slots_read(a, (size_t)cur.row, sl, lane, &any);
             if (y >= a.V) {
                 if (lane == 0) atomicExch(&g_error_word, kErrInvalid);
                 y = -1;
             }
-            bool any = false;
-            float ent = 0.f;
-            if (a.K) ent = slots_read(a, (size_t)cur.row, sl, lane, &any);
+            // the named symbols' logits, on their way while the symbols are sorted out
+            auto named_logit = [&](int k) {
+                const int i = k < a.K ? sl.id[k] : -1;
+                return i >= 0 && (rank == 0 || mine(i)) ? logit(z + i) : 0.f;
+            };
             const float zy = y >= 0 && (rank == 0 || mine(y)) ? logit(z + y) : 0.f;
-            for (int k = lane; k < a.K; k += 32) {
-                const int i = sl.id[k];
-                sl.zk[k] = i >= 0 && (rank == 0 || mine(i)) ? logit(z + i) : 0.f;
-            }
+            const float x0 = named_logit(lane), x1 = named_logit(lane + 32);
             if (any && dz) slots_own(sl, a.K, table, pl.table, lane);
+            if (lane < a.K) sl.zk[lane] = x0;
+            if (lane + 32 < a.K) sl.zk[lane + 32] = x1;
+#pragma unroll 4
+            for (int k = lane + 64; k < a.K; k += 32) sl.zk[k] = named_logit(k);
             const bool w1 = mbar_wait_cluster(&bars->stat[n % kDStats], (n / kDStats) & 1, abort,
                                               kDTimeoutNs);
             ok = __all_sync(0xffffffffu, w1);
             if (!ok) break;
-            Stat st = stat_read<TWO>(stats + (n % kDStats) * parts, parts, lane, c);
+            Stat st = stat_read<EXPS>(stats + (n % kDStats) * parts, parts, lane, c);
             const float base = stat_base(st.m);
             if (st.s == 0.f) {   // no logit above -inf: nothing to learn from
                 any = false;
@@ -583,7 +628,7 @@ __global__ void __launch_bounds__(NT + 32 + 32 * kDSlotWarps, NT == 512 ? 1 : NT
             }
             const float fq = any ? w * a.kl_tau / st.s : 0.f, f1 = y >= 0 ? w * a.ce / st.s1 : 0.f;
             if (lane == 0) {
-                bars->factor[sw] = make_float4(-base, TWO ? fq : fq + f1, f1, 0.f);
+                bars->factor[sw] = make_float4(-base, EXPS != kOne ? fq : fq + f1, f1, 0.f);
                 mbar_arrive(&bars->ready[sw]);
             }
             if (rank == 0 && a.loss) {
@@ -605,7 +650,7 @@ __global__ void __launch_bounds__(NT + 32 + 32 * kDSlotWarps, NT == 512 ? 1 : NT
             if (!dz) continue;
             auto dense = [&](float x) {
                 const float e = ex2((x - base) * c);
-                return TWO ? fq * e + f1 * ex2((x - base) * kLog2e) : (fq + f1) * e;
+                return EXPS != kOne ? fq * e + f1 * ex2((x - base) * kLog2e) : (fq + f1) * e;
             };
             bool named = false;   // the label, by a slot
             if (any)
@@ -685,25 +730,29 @@ __global__ void __launch_bounds__(NT + 32 + 32 * kDSlotWarps, NT == 512 ? 1 : NT
                         const uint64_t d = f32x2_add(pair(q[k], i), nbb);
                         const float2 e = ex2_pair(f32x2_mul(d, cc));
                         s = f32x2_add(s, f32x2_pack(e.x, e.y));
-                        if (TWO) {
+                        if (EXPS == kTwo) {
                             const float2 f = ex2_pair(f32x2_mul(d, ll));
                             s1 = f32x2_add(s1, f32x2_pack(f.x, f.y));
+                        }
+                        if (EXPS == kSquare) {
+                            const uint64_t f = f32x2_pack(e.x, e.y);
+                            s1 = f32x2_fma(f, f, s1);
                         }
                     }
                 const float2 sf = f32x2_unpack(s), sf1 = f32x2_unpack(s1);
                 u.s = sf.x + sf.y;
-                u.s1 = TWO ? sf1.x + sf1.y : u.s;
-                st = stat_join<TWO>(st, u, c);
+                u.s1 = EXPS != kOne ? sf1.x + sf1.y : u.s;
+                st = stat_join<EXPS>(st, u, c);
             }
             if (warp == 0) {
                 const int j = edge_of(r);
                 if (j >= 0) {
                     const float x = logit(reinterpret_cast<const T*>(buf) + (j + r.skew - r.v0 * VE));
                     const float d = x - stat_base(x);
-                    st = stat_join<TWO>(st, Stat{x, ex2(d * c), ex2(d * kLog2e)}, c);
+                    st = stat_join<EXPS>(st, Stat{x, ex2(d * c), ex2(d * kLog2e)}, c);
                 }
             }
-            st = stat_warp<TWO>(st, c);
+            st = stat_warp<EXPS>(st, c);
             if (!gb && lane == 0) mbar_arrive(&bars->empty[b]);   // read once
             uint64_t* const bar = &bars->stat[n % kDStats];
             float4* const at = stats + (n % kDStats) * parts + rank * NW + warp;
@@ -730,11 +779,13 @@ __global__ void __launch_bounds__(NT + 32 + 32 * kDSlotWarps, NT == 512 ? 1 : NT
                     for (int i = 0; i < VE / 2; ++i) {
                         const uint64_t d = f32x2_add(pair(q, i), nbb);
                         const float2 e = ex2_pair(f32x2_mul(d, cc));
-                        uint64_t g = f32x2_mul(f32x2_pack(e.x, e.y), ff);
-                        if (TWO) {
+                        const uint64_t ee = f32x2_pack(e.x, e.y);
+                        uint64_t g = f32x2_mul(ee, ff);
+                        if (EXPS == kTwo) {
                             const float2 e1 = ex2_pair(f32x2_mul(d, ll));
                             g = f32x2_fma(f32x2_pack(e1.x, e1.y), ff1, g);
                         }
+                        if (EXPS == kSquare) g = f32x2_fma(f32x2_mul(ee, ee), ff1, g);
                         const float2 h = f32x2_unpack(g);
                         if (sizeof(T) == 2) {
                             o[i] = pack_bf16x2(h.x, h.y);
@@ -750,7 +801,7 @@ __global__ void __launch_bounds__(NT + 32 + 32 * kDSlotWarps, NT == 512 ? 1 : NT
                     if (j >= 0) {
                         const float d =
                             logit(reinterpret_cast<const T*>(buf) + (j + r.skew - r.v0 * VE)) + nb;
-                        put(gb + r.at + j, TWO ? f.y * ex2(d * c) + f.z * ex2(d * kLog2e)
+                        put(gb + r.at + j, EXPS != kOne ? f.y * ex2(d * c) + f.z * ex2(d * kLog2e)
                                                : f.y * ex2(d * c));
                     }
                 }
@@ -801,9 +852,9 @@ int distill_sms() {
     return n;
 }
 
-template <typename T, int NT, bool TWO>
+template <typename T, int NT, int EXPS>
 cudaError_t launch_distill_rows(const DistillArgs& a, DistillPlan pl, cudaStream_t st) {
-    auto kern = distill_row_kernel<T, NT, TWO>;
+    auto kern = distill_row_kernel<T, NT, EXPS>;
     static std::once_flag once[64];
     static cudaError_t set_err[64];
     int dev = 0;
@@ -817,7 +868,7 @@ cudaError_t launch_distill_rows(const DistillArgs& a, DistillPlan pl, cudaStream
     if (set_err[dev] != cudaSuccess) return set_err[dev];
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)pl.C);
-    cfg.blockDim = dim3(NT + 32 + 32 * kDSlotWarps);
+    cfg.blockDim = dim3(NT + 32 + 32 * slot_warps(NT));
     cfg.dynamicSmemBytes = pl.smem;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
@@ -854,12 +905,12 @@ cudaError_t launch_distill_rows(const DistillArgs& a, DistillPlan pl, cudaStream
     return cudaLaunchKernelEx(&cfg, kern, a, pl);
 }
 
-template <typename T, bool TWO>
+template <typename T, int EXPS>
 cudaError_t launch_distill(const DistillArgs& a, cudaStream_t st) {
     if (a.V <= kDWarpV && a.K <= kDWarpK) {
         const dim3 grid((unsigned)((a.T + kDWarps - 1) / kDWarps)), block(32 * kDWarps);
-        if (a.V <= 256) return launch_pdl(distill_warp_kernel<T, 8, TWO>, grid, block, 0, st, a);
-        return launch_pdl(distill_warp_kernel<T, 32, TWO>, grid, block, 0, st, a);
+        if (a.V <= 256) return launch_pdl(distill_warp_kernel<T, 8, EXPS>, grid, block, 0, st, a);
+        return launch_pdl(distill_warp_kernel<T, 32, EXPS>, grid, block, 0, st, a);
     }
     const int sms = distill_sms();
     const long long bytes = (long long)a.V * (int)sizeof(T) + 32;
@@ -881,8 +932,8 @@ cudaError_t launch_distill(const DistillArgs& a, cudaStream_t st) {
     if (!a.K) pl.table = 0;
     const size_t slots = (((size_t)a.K * 16 + (size_t)pl.table * 8) + 15) & ~(size_t)15;
     const size_t room = kDSmem / per_sm - (per_sm > 1 ? 1024 : 0);
-    // four slot warps, fewer where their slots would take a quarter of the room
-    pl.sw_log2 = 2;
+    // fewer slot warps where their slots would take a quarter of the room
+    pl.sw_log2 = nt == 512 ? 3 : nt == 256 ? 2 : 1;
     while (pl.sw_log2 && (slots << pl.sw_log2) > room / 4) --pl.sw_log2;
     const size_t fixed = (size_t)kDStats * pl.C * (nt / 32) * 16 + (slots << pl.sw_log2) +
                          sizeof(DistillBars);
@@ -892,9 +943,9 @@ cudaError_t launch_distill(const DistillArgs& a, cudaStream_t st) {
     pl.look = pl.bufs > 1;
     pl.smem = fixed + (size_t)pl.bufs * pl.slice;
     pl.clusters = 0;   // the launch's
-    if (nt == 128) return launch_distill_rows<T, 128, TWO>(a, pl, st);
-    if (nt == 256) return launch_distill_rows<T, 256, TWO>(a, pl, st);
-    return launch_distill_rows<T, 512, TWO>(a, pl, st);
+    if (nt == 128) return launch_distill_rows<T, 128, EXPS>(a, pl, st);
+    if (nt == 256) return launch_distill_rows<T, 256, EXPS>(a, pl, st);
+    return launch_distill_rows<T, 512, EXPS>(a, pl, st);
 }
 
 }  // namespace
@@ -959,14 +1010,19 @@ extern "C" int hcw_distill_loss(const void* z, const int* idx, const float* teac
     a.ce = ce_scale;
     const cudaStream_t st = (cudaStream_t)stream;
     // the label's softmax is at temperature 1: a second sum where the teacher's is not
-    const bool two = a.idx && a.target && temperature != 1.f;
+    const int exps = !(a.idx && a.target) || temperature == 1.f ? kOne
+                     : temperature == 2.f                        ? kSquare
+                                                                 : kTwo;
     // without the teacher's part only the label's softmax is left
     if (!a.idx) a.inv_tau = 1.f;
     cudaError_t e;
     if (dtype == HCW_BF16)
-        e = two ? launch_distill<__nv_bfloat16, true>(a, st)
-                : launch_distill<__nv_bfloat16, false>(a, st);
+        e = exps == kOne   ? launch_distill<__nv_bfloat16, kOne>(a, st)
+            : exps == kTwo ? launch_distill<__nv_bfloat16, kTwo>(a, st)
+                           : launch_distill<__nv_bfloat16, kSquare>(a, st);
     else
-        e = two ? launch_distill<float, true>(a, st) : launch_distill<float, false>(a, st);
+        e = exps == kOne   ? launch_distill<float, kOne>(a, st)
+            : exps == kTwo ? launch_distill<float, kTwo>(a, st)
+                           : launch_distill<float, kSquare>(a, st);
     return count_launch(e, 1);
 }
