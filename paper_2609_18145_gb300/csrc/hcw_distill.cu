@@ -256,10 +256,12 @@ __device__ __forceinline__ void slots_own(const Slots& s, int K, int* table, int
 }
 
 // ------------------------------------------------------------------ a warp a row
-// NE symbols a lane, symbol lane + 32 e: coalesced whatever the row's alignment.
+// NE symbols a lane, symbol lane + 32 e: coalesced whatever the row's alignment.  Everything
+// the row needs from its index alone is loaded at once; the named symbols' logits come
+// after the row, from L1.  Slots lane and lane + 32 stay in registers.
 template <typename T, int NE, int EXPS>
 __global__ void __launch_bounds__(32 * kDWarps) distill_warp_kernel(const DistillArgs a) {
-    __shared__ float sp[kDWarps][kDWarpK], so[kDWarps][kDWarpK], sz[kDWarps][kDWarpK];
+    __shared__ float sp[kDWarps][kDWarpK];
     __shared__ int si[kDWarps][kDWarpK];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     pdl_wait();
@@ -269,80 +271,130 @@ __global__ void __launch_bounds__(32 * kDWarps) distill_warp_kernel(const Distil
     const T* z = static_cast<const T*>(a.z) + (size_t)row * a.V;
     T* dz = a.dz ? static_cast<T*>(a.dz) + (size_t)row * a.V : nullptr;
     const float w = a.weight ? a.weight[row] : 1.f;
+    int y = a.target ? a.target[row] : -1;
+    int id[2];
+    float p[2];
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        const int k = lane + 32 * q;
+        id[q] = k < a.K ? a.idx[row * a.K + k] : -1;
+        p[q] = k < a.K ? a.teacher[row * a.K + k] : 0.f;
+    }
+    float v[NE];
+#pragma unroll
+    for (int e = 0; e < NE; ++e) v[e] = lane + 32 * e < a.V ? logit(z + lane + 32 * e) : -INFINITY;
     if (w == 0.f) {   // whatever the row holds
         if (dz)
             for (int j = lane; j < a.V; j += 32) put(dz + j, 0.f);
         if (lane == 0 && a.loss) a.loss[row] = 0.f;
         return;
     }
-    float v[NE];
+    if (y >= a.V || id[0] >= a.V || id[1] >= a.V) atomicExch(&g_error_word, kErrInvalid);
+    if (y >= a.V) y = -1;
+    // maxima of the row and of the teacher's logits
+    float mz = -INFINITY, mt = -INFINITY;
 #pragma unroll
-    for (int e = 0; e < NE; ++e) v[e] = lane + 32 * e < a.V ? logit(z + lane + 32 * e) : -INFINITY;
-    const Slots sl = {sp[warp], so[warp], sz[warp], si[warp]};
-    bool any = false;
-    float ent = 0.f;
-    if (a.idx) {
-        ent = slots_read(a, (size_t)row, sl, lane, &any);
-        __syncwarp();
-        for (int k = lane; k < a.K; k += 32) {
-            sl.own[k] = slot_owned(sl, a.K, k);
-            sl.zk[k] = sl.id[k] >= 0 ? logit(z + sl.id[k]) : 0.f;
-        }
-        __syncwarp();
+    for (int q = 0; q < 2; ++q) {
+        if (id[q] >= a.V) id[q] = -1;
+        p[q] = id[q] >= 0 ? p[q] * a.inv_tau : -INFINITY;
+        mt = fmaxf(mt, p[q]);
     }
-    int y = a.target ? a.target[row] : -1;
-    if (y >= a.V) {
-        if (lane == 0) atomicExch(&g_error_word, kErrInvalid);
-        y = -1;
+#pragma unroll
+    for (int e = 0; e < NE; ++e) mz = fmaxf(mz, v[e]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        mz = fmaxf(mz, __shfl_xor_sync(0xffffffffu, mz, o));
+        mt = fmaxf(mt, __shfl_xor_sync(0xffffffffu, mt, o));
     }
-    const float zy = y >= 0 ? logit(z + y) : 0.f;
     const float c = a.inv_tau * kLog2e;
-    Stat st = {-INFINITY, 0.f, 0.f};
+    const float base = stat_base(mz), bt = stat_base(mt);
+    const float zy = y >= 0 ? logit(z + y) : 0.f;
+    float zk[2];
 #pragma unroll
-    for (int e = 0; e < NE; ++e) st.m = fmaxf(st.m, v[e]);
-    st.m = warp_max(st.m);
-    const float base = stat_base(st.m);
+    for (int q = 0; q < 2; ++q) zk[q] = id[q] >= 0 ? logit(z + id[q]) : 0.f;
+    // sums: the row's exponentials, the teacher's, and its sum of exp(t) t
+    float s = 0.f, s1 = 0.f, st = 0.f, stt = 0.f;
 #pragma unroll
     for (int e = 0; e < NE; ++e) {
-        st.s += ex2((v[e] - base) * c);
-        if (EXPS != kOne) st.s1 += ex2((v[e] - base) * kLog2e);
+        const float x = ex2((v[e] - base) * c);
+        s += x;
+        if (EXPS == kTwo) s1 += ex2((v[e] - base) * kLog2e);
+        if (EXPS == kSquare) s1 += x * x;
     }
-    st.s = warp_sum(st.s);
-    st.s1 = EXPS != kOne ? warp_sum(st.s1) : st.s;
-    if (st.s == 0.f) {   // no logit above -inf: nothing to learn from
+    float et[2];
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        et[q] = id[q] >= 0 ? ex2((p[q] - bt) * kLog2e) : 0.f;
+        st += et[q];
+        if (et[q] != 0.f) stt += et[q] * (p[q] - bt - (zk[q] - base) * a.inv_tau);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        s += __shfl_xor_sync(0xffffffffu, s, o);
+        st += __shfl_xor_sync(0xffffffffu, st, o);
+        stt += __shfl_xor_sync(0xffffffffu, stt, o);
+        if (EXPS != kOne) s1 += __shfl_xor_sync(0xffffffffu, s1, o);
+    }
+    if (EXPS == kOne) s1 = s;
+    bool any = st != 0.f;   // NaN counts: it belongs in the result
+    if (s == 0.f) {         // no logit above -inf: nothing to learn from
         any = false;
         y = -1;
-        st.s = st.s1 = 1.f;
+        s = s1 = 1.f;
     }
-    // log-sums relative to the maximum, as the logits are: the row's own size cancels first
-    const float ls = logf(st.s), ls1 = logf(st.s1);
-    float l = 0.f;
-    if (any)
-        for (int k = lane; k < a.K; k += 32)
-            if (sl.p[k] != 0.f) l -= sl.p[k] * ((sl.zk[k] - base) * a.inv_tau - ls);
-    l = warp_sum(l) + (any ? ent : 0.f);
-    if (lane == 0 && a.loss) a.loss[row] = w * (a.kl * l + (y >= 0 ? a.ce * (ls1 - (zy - base)) : 0.f));
+    const float inv_t = any ? 1.f / st : 0.f;
+    if (lane == 0 && a.loss) {
+        // sum p (log p - log q) with log p = t - bt - log st, log q = (z - base) / tau - log s
+        const float kl = any ? stt * inv_t - logf(st) + logf(s) : 0.f;
+        a.loss[row] = w * (a.kl * kl + (y >= 0 ? a.ce * (logf(s1) - (zy - base)) : 0.f));
+    }
     if (!dz) return;
-    const float fq = any ? w * a.kl_tau / st.s : 0.f, f1 = y >= 0 ? w * a.ce / st.s1 : 0.f;
+    const float fq = any ? w * a.kl_tau / s : 0.f, f1 = y >= 0 ? w * a.ce / s1 : 0.f;
     auto dense = [&](float x) {
         const float e = ex2((x - base) * c);
-        return EXPS != kOne ? fq * e + f1 * ex2((x - base) * kLog2e) : (fq + f1) * e;
+        if (EXPS == kOne) return (fq + f1) * e;
+        return fq * e + f1 * (EXPS == kSquare ? e * e : ex2((x - base) * kLog2e));
     };
 #pragma unroll
     for (int e = 0; e < NE; ++e)
         if (lane + 32 * e < a.V) put(dz + lane + 32 * e, dense(v[e]));
-    __syncwarp();   // the dense values are in place
-    bool y_done = false;
-    if (any)
-        for (int k = lane; k < a.K; k += 32) {
-            const float t = sl.own[k];
-            if (t < 0.f) continue;
-            const bool is_y = sl.id[k] == y;
-            y_done |= is_y;
-            put(dz + sl.id[k], dense(sl.zk[k]) - w * (a.kl_tau * t + (is_y ? a.ce : 0.f)));
+    bool named = false;
+    if (any) {
+        // a slot's share of its symbol: every slot its own, as a rule
+        const uint32_t m0 = __match_any_sync(0xffffffffu, id[0]);
+        bool twice = id[0] >= 0 && (m0 & (m0 - 1));
+        float own[2] = {id[0] >= 0 ? et[0] * inv_t : -1.f, id[1] >= 0 ? et[1] * inv_t : -1.f};
+        if (a.K > 32) {
+            const uint32_t m1 = __match_any_sync(0xffffffffu, id[1]);
+            twice |= id[1] >= 0 && (m1 & (m1 - 1));
+#pragma unroll 8
+            for (int r = 0; r < 32; ++r) {
+                const int o = __shfl_sync(0xffffffffu, id[1], lane ^ r);
+                twice |= id[0] >= 0 && o == id[0];
+            }
         }
-    y_done = __any_sync(0xffffffffu, y_done);
-    if (y >= 0 && !y_done && lane == 0) put(dz + y, dense(zy) - w * a.ce);
+        if (__any_sync(0xffffffffu, twice)) {
+            const Slots sl = {sp[warp], nullptr, nullptr, si[warp]};
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                si[warp][lane + 32 * q] = id[q];
+                sp[warp][lane + 32 * q] = et[q] * inv_t;
+            }
+            __syncwarp();
+#pragma unroll
+            for (int q = 0; q < 2; ++q) own[q] = slot_owned(sl, kDWarpK, lane + 32 * q);
+        }
+        __syncwarp();   // the dense values are in place
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            if (own[q] < 0.f) continue;
+            const bool is_y = id[q] == y;
+            named |= is_y;
+            put(dz + id[q], dense(zk[q]) - w * (a.kl_tau * own[q] + (is_y ? a.ce : 0.f)));
+        }
+    }
+    named = __any_sync(0xffffffffu, named);
+    if (y >= 0 && !named && lane == 0) put(dz + y, dense(zy) - w * a.ce);
 }
 
 // ------------------------------------------------------------------ a cluster a row
@@ -771,7 +823,7 @@ __global__ void __launch_bounds__(NT + 32 + 32 * slot_warps(NT), NT == 512 ? 1 :
                 const float nb = f.x;
                 const uint64_t nbb = f32x2_pack(nb, nb), ff = f32x2_pack(f.y, f.y),
                                ff1 = f32x2_pack(f.z, f.z);
-#pragma unroll 4
+#pragma unroll 2
                 for (int v = r.i0 + tid; v < r.i1; v += NT) {
                     const uint4 q = buf[v - r.v0];
                     uint32_t o[4];
