@@ -11,38 +11,44 @@
 // v / sqrt(mean(v^2) + eps) (RMS), and the row gradient of either
 //   N'(v)^T e = (e w - vhat mean(e w vhat) - [LayerNorm] mean(e w)) / sqrt(var + eps).
 //
-// Bound by memory: the forward reads two rows and writes two, the backward reads
-// four and writes two; each row is read once and stays in registers through its
-// two or three reductions.  W warps share a row (8 elements a thread and chunk: a
-// 16-byte access in bf16), so that a thread's share of the parameter gradients
-// stays in registers over all rows its CTA takes; the row sums go through
-// shuffles and, between the warps of a row, shared memory.  The next row is
-// loaded while a row is worked on.  Parameter gradients: each CTA writes one
-// row of partial sums, a second kernel adds the rows in a fixed order, so the
-// same inputs give the same bits.
+// Bound by memory: the forward reads two rows and writes two, the backward reads four and
+// writes two.  Runs of consecutive rows are always on their way into a ring in shared memory
+// (bulk copies: consecutive rows are one piece, whatever their width and alignment), so the
+// reductions of one row never hold up the loads of the next.  A row belongs to `nl`
+// threads (8 columns each, 16 above 4096 columns), whose columns stay the same from row to
+// row: the parameters and a thread's share of the parameter gradients stay in registers
+// over all rows of its CTA.  Several rows are reduced at once: the sums go through shuffles
+// that halve the number of values at each step and, between the warps of a row, through
+// shared memory behind a barrier of those warps.  The arithmetic is in packed pairs (two fp32
+// operations an instruction).  Parameter gradients: each CTA writes one row of partial
+// sums, a second kernel adds the rows in a fixed order, so the same inputs give the same
+// bits.
 //
 // All statistics, sums and products are fp32; only r_out, x_out, dr and df are
 // rounded to the storage type, once.  LayerNorm takes the mean first and sums the
 // squares of the centred values (no cancellation under a large common offset).
 #include "hcw.h"
 #include "hcw_internal.h"
+#include "hcw_ptx.cuh"
 
 #include <math.h>
+#include <mutex>
 
 namespace hcw {
 
 namespace {
 
-constexpr int kNormThreads = 512;   // most threads of a CTA (16 warps on one row)
+constexpr int kNormThreads = 512;   // most threads of a CTA
 constexpr int kNormMaxD = 8192;
-constexpr int kNormRed = 4;         // sums of one reduction round
 constexpr int kNormPar = 4;         // parameter sums of a CTA: post_w, post_b, pre_w, pre_b
+constexpr int kNormRed = 8;         // values of one reduction round
+constexpr int kNormMaxBufs = 8;
+constexpr size_t kNormSmem = 232448;
+constexpr unsigned long long kNormTimeoutNs = 2000000000ull;
 
 struct NormArgs {
-    const void* r;        // forward: residual stream or null; backward: dr_out or null
-    const void* f;        // branch output or null
-    const void* s;        // backward: the stored stream
-    const void* dx;       // backward: dx_out or null
+    // the tensors of a ring buffer: forward r, f; backward dr_out, f, s, dx_out (null: not there)
+    const void* in[4];
     void* o0;             // r_out / dr, or null
     void* o1;             // x_out / df, or null
     const float* gate;    // [groups][d] or null (ones)
@@ -57,136 +63,16 @@ struct NormArgs {
     int rows_per_gate;    // rows of a group (the last may be shorter)
     int groups, slices;   // an item is one of `slices` runs of rows of a group
     int post, pre;
-    int W;                // warps a row
+    int nl;               // threads a row
+    int rows;             // rows of a buffer
+    int bufs;
+    int piece;            // bytes of a tensor in a buffer
 };
 
-// A thread's 8 * NC elements of a row.  VEC (d a multiple of 8): chunk k is the 8 elements
-// from 8 (l + 32 W k) on, l the thread's place in the row; else element j is l + 32 W j.
-template <typename T, bool VEC, int NC>
-struct RowRegs {
-    static constexpr int kQ = 8 * NC * (int)sizeof(T) / 16;
-    uint4 q[kQ];
-    __device__ __forceinline__ static int col(int l, int nl, int j) {
-        return VEC ? 8 * (l + nl * (j >> 3)) + (j & 7) : l + nl * j;
-    }
-    __device__ __forceinline__ void clear() {
-#pragma unroll
-        for (int i = 0; i < kQ; ++i) q[i] = make_uint4(0u, 0u, 0u, 0u);
-    }
-    __device__ __forceinline__ void load(const void* base, size_t row, int l, int nl, int d) {
-        const T* p = static_cast<const T*>(base) + row * (size_t)d;
-        if (VEC) {
-#pragma unroll
-            for (int k = 0; k < NC; ++k) {
-                const int c = 8 * (l + nl * k);
-#pragma unroll
-                for (int i = 0; i < kQ / NC; ++i)
-                    q[k * (kQ / NC) + i] = c < d ? reinterpret_cast<const uint4*>(p + c)[i]
-                                                 : make_uint4(0u, 0u, 0u, 0u);
-            }
-        } else {
-            uint32_t* w = reinterpret_cast<uint32_t*>(q);
-            if (sizeof(T) == 4) {
-#pragma unroll
-                for (int j = 0; j < 8 * NC; ++j) {
-                    const int c = l + nl * j;
-                    w[j] = c < d ? reinterpret_cast<const uint32_t*>(p)[c] : 0u;
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < 4 * NC; ++j) {
-                    const int c0 = l + nl * 2 * j, c1 = c0 + nl;
-                    const uint32_t a = c0 < d ? reinterpret_cast<const unsigned short*>(p)[c0] : 0u;
-                    const uint32_t b = c1 < d ? reinterpret_cast<const unsigned short*>(p)[c1] : 0u;
-                    w[j] = a | b << 16;
-                }
-            }
-        }
-    }
-    __device__ __forceinline__ float get(int j) const {
-        const uint32_t* w = reinterpret_cast<const uint32_t*>(q);
-        if (sizeof(T) == 4) return __uint_as_float(w[j]);
-        return __uint_as_float(j & 1 ? w[j >> 1] & 0xFFFF0000u : w[j >> 1] << 16);
-    }
-    __device__ __forceinline__ static void store(void* base, size_t row, int l, int nl, int d,
-                                                 const float (&v)[8 * NC]) {
-        T* p = static_cast<T*>(base) + row * (size_t)d;
-#pragma unroll
-        for (int k = 0; k < NC; ++k) {
-            if (VEC) {
-                const int c = 8 * (l + nl * k);
-                if (c >= d) continue;
-                if (sizeof(T) == 4) {
-                    reinterpret_cast<float4*>(p + c)[0] =
-                        make_float4(v[8 * k], v[8 * k + 1], v[8 * k + 2], v[8 * k + 3]);
-                    reinterpret_cast<float4*>(p + c)[1] =
-                        make_float4(v[8 * k + 4], v[8 * k + 5], v[8 * k + 6], v[8 * k + 7]);
-                } else {
-                    uint32_t w[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const __nv_bfloat162 h =
-                            __floats2bfloat162_rn(v[8 * k + 2 * i], v[8 * k + 2 * i + 1]);
-                        w[i] = *reinterpret_cast<const uint32_t*>(&h);
-                    }
-                    *reinterpret_cast<uint4*>(p + c) = make_uint4(w[0], w[1], w[2], w[3]);
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int c = l + nl * (8 * k + i);
-                    if (c >= d) continue;
-                    if (sizeof(T) == 4)
-                        reinterpret_cast<float*>(p)[c] = v[8 * k + i];
-                    else
-                        reinterpret_cast<__nv_bfloat16*>(p)[c] = __float2bfloat16_rn(v[8 * k + i]);
-                }
-            }
-        }
-    }
-};
-
-// The parameter vector at the thread's columns (null: `none` everywhere).
-template <bool VEC, int NC>
-__device__ __forceinline__ void load_par(float (&v)[8 * NC], const float* p, float none, int l,
-                                         int nl, int d) {
-#pragma unroll
-    for (int j = 0; j < 8 * NC; ++j) {
-        const int c = RowRegs<float, VEC, NC>::col(l, nl, j);
-        v[j] = c < d ? (p ? p[c] : none) : 0.f;
-    }
-}
-
-// Sums over a row of N values of each of its threads, on every one of them.  Between the
-// warps of a row through red[parity][warp]: the parity alternates from round to round, so a
-// round's values are read before the round after the next overwrites them (a barrier of the
-// row's warps lies between).
-struct RowSum {
-    float (*red)[kNormThreads / 32][kNormRed];   // [2][warps of the CTA]
-    int parity, W, warp;
-    template <int N>
-    __device__ __forceinline__ void sum(float (&v)[N]) {
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1)
-#pragma unroll
-            for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
-        if (W == 1) return;
-        const int lane = threadIdx.x & 31, first = warp / W * W;
-        float(*buf)[kNormRed] = red[parity];
-        parity ^= 1;
-        if (lane == 0)
-#pragma unroll
-            for (int i = 0; i < N; ++i) buf[warp][i] = v[i];
-        asm volatile("bar.sync %0, %1;" ::"r"(1 + warp / W), "r"(32 * W) : "memory");
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = 0.f;
-        for (int w = 0; w < W; ++w) {
-            const float4 q = *reinterpret_cast<const float4*>(buf[first + w]);
-            const float t[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-            for (int i = 0; i < N; ++i) v[i] += t[i];
-        }
-    }
+struct __align__(16) NormShared {
+    float red[2][kNormThreads / 32][kNormRed];
+    uint64_t full[kNormMaxBufs], empty[kNormMaxBufs];
+    int abort;
 };
 
 // Rows [r0, r1) of an item.
@@ -200,290 +86,698 @@ __device__ __forceinline__ void item_rows(const NormArgs& a, int item, int& g, i
     r1 = first + (sl * len < n - len ? sl * len + len : n);
 }
 
-// LN: some norm is a LayerNorm (means and centred squares in rounds of their own).
-template <typename T, bool VEC, int NC, bool LN>
-__global__ void __launch_bounds__(kNormThreads) norm_fwd_kernel(const NormArgs a) {
-    __shared__ __align__(16) float red[2][kNormThreads / 32][kNormRed];
-    constexpr int E = 8 * NC;
-    using Row = RowRegs<T, VEC, NC>;
-    const int warp = threadIdx.x >> 5, W = a.W;
-    const int nl = 32 * W, l = (int)threadIdx.x % nl;
-    const int grp = warp / W, n_grp = (int)(blockDim.x >> 5) / W;
-    const float inv_d = 1.f / (float)a.d;
-    RowSum rs = {red, 0, W, warp};
-    pdl_wait();
-    pdl_trigger();
-    const int items = a.groups * a.slices;
-    float pw[E], pb[E];
-    load_par<VEC, NC>(pw, a.pre_w, 1.f, l, nl, a.d);
-    load_par<VEC, NC>(pb, LN ? a.pre_b : nullptr, 0.f, l, nl, a.d);
-    for (int item = blockIdx.x; item < items; item += gridDim.x) {
-        int g, r0, r1;
-        item_rows(a, item, g, r0, r1);
-        float gw[E], gb[E];   // gate * post_w, gate * post_b
-        {
-            float t[E];
-            load_par<VEC, NC>(t, a.gate ? a.gate + (size_t)g * a.d : nullptr, 1.f, l, nl, a.d);
-            load_par<VEC, NC>(gw, a.post_w, 1.f, l, nl, a.d);
-            load_par<VEC, NC>(gb, LN ? a.post_b : nullptr, 0.f, l, nl, a.d);
-#pragma unroll
-            for (int j = 0; j < E; ++j) {
-                gw[j] *= t[j];
-                gb[j] *= t[j];
-            }
+// The ring's source: thread 0 walks the same items and rows as the CTA works through, up
+// to `bufs` buffers ahead.
+struct NormFeed {
+    int item, row, r1;     // next rows to fetch
+    int b;                 // buffer they go to
+    uint32_t round;        // how often the ring has been gone through
+    __device__ __forceinline__ void start(const NormArgs& a) {
+        item = blockIdx.x;
+        b = 0;
+        round = 0;
+        row = r1 = 0;
+        if (item < a.groups * a.slices) {
+            int g;
+            item_rows(a, item, g, row, r1);
         }
-        Row rr, fr;
-        rr.clear();
-        fr.clear();
-        int row = r0 + grp;
-        if (row < r1) {
-            if (a.r) rr.load(a.r, row, l, nl, a.d);
-            if (a.f) fr.load(a.f, row, l, nl, a.d);
+        settle(a);
+    }
+    // on to an item with rows left
+    __device__ __forceinline__ void settle(const NormArgs& a) {
+        const int items = a.groups * a.slices;
+        while (item < items && row >= r1) {
+            item += gridDim.x;
+            int g;
+            if (item < items) item_rows(a, item, g, row, r1);
         }
-        for (; row < r1; row += n_grp) {
-            const Row rc = rr, fc = fr;
-            if (row + n_grp < r1) {
-                if (a.r) rr.load(a.r, row + n_grp, l, nl, a.d);
-                if (a.f) fr.load(a.f, row + n_grp, l, nl, a.d);
+    }
+    // Fetches the next rows into the next buffer, which must be free (false: gave up).
+    template <typename T, int NIN>
+    __device__ __forceinline__ bool fetch(const NormArgs& a, uint8_t* ring, NormShared* sh) {
+        if (item >= a.groups * a.slices) return true;
+        if (round && !mbar_wait(&sh->empty[b], (round & 1) ^ 1, &sh->abort, kNormTimeoutNs))
+            return false;
+        const int n = r1 - row < a.rows ? r1 - row : a.rows;
+        // the 16-byte pieces the rows touch, those wholly inside the tensor in one copy and
+        // the last few bytes of the tensor element by element
+        const size_t end = (size_t)a.T * a.d * sizeof(T);
+        const size_t from = (size_t)row * a.d * sizeof(T) & ~(size_t)15;
+        size_t to = ((size_t)(row + n) * a.d * sizeof(T) + 15) & ~(size_t)15;
+        const bool cut = to > end;
+        if (cut) to = end & ~(size_t)15;
+        const uint32_t bytes = to > from ? (uint32_t)(to - from) : 0;
+        uint8_t* dst = ring + (size_t)b * NIN * a.piece;
+        uint32_t total = 0;
+#pragma unroll 1
+        for (int i = 0; i < NIN; ++i) {
+            if (!a.in[i]) continue;
+            total += bytes;
+            if (cut)
+                for (size_t at = from + bytes; at < end; at += sizeof(T))
+                    *reinterpret_cast<T*>(dst + (size_t)i * a.piece + (at - from)) =
+                        *reinterpret_cast<const T*>(static_cast<const uint8_t*>(a.in[i]) + at);
+        }
+        mbar_arrive_expect_tx(&sh->full[b], total);
+        if (bytes)
+#pragma unroll 1
+            for (int i = 0; i < NIN; ++i)
+                if (a.in[i])
+                    asm volatile(
+                        "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes "
+                        "[%0], [%1], %2, [%3];" ::"r"(smem_u32(dst + (size_t)i * a.piece)),
+                        "l"(static_cast<const uint8_t*>(a.in[i]) + from), "r"(bytes),
+                        "r"(smem_u32(&sh->full[b]))
+                        : "memory");
+        row += n;
+        settle(a);
+        if (++b == a.bufs) {
+            b = 0;
+            ++round;
+        }
+        return true;
+    }
+    // Every copy has landed before the CTA leaves, also after giving up.
+    __device__ __forceinline__ void drain(const NormArgs& a, NormShared* sh) const {
+        for (int i = 0; i < a.bufs; ++i)
+            if (round || i < b)
+                mbar_wait_drain(&sh->full[i], (i < b ? round : round - 1) & 1, kNormTimeoutNs);
+    }
+};
+
+// A thread's E columns of a row, as pairs: VW neighbours at a time, nl threads apart.
+template <typename T, int VW, int E>
+struct Cols {
+    static constexpr int H = E / 2;
+    __device__ __forceinline__ static int col(int l, int nl, int j) {
+        return VW * (l + nl * (j / VW)) + j % VW;
+    }
+    // from shared memory, zeros past the row's end
+    __device__ __forceinline__ static void load(uint64_t (&v)[H], const uint8_t* row, int l, int nl,
+                                                int d) {
+        const T* p = reinterpret_cast<const T*>(row);
+        if (sizeof(T) == 2 && VW == 8) {
+#pragma unroll
+            for (int k = 0; k < E / 8; ++k) {
+                const int c = 8 * (l + nl * k);
+                const uint4 q = c < d ? *reinterpret_cast<const uint4*>(p + c)
+                                      : make_uint4(0u, 0u, 0u, 0u);
+                v[4 * k] = bf16x2_to_f32x2(q.x);
+                v[4 * k + 1] = bf16x2_to_f32x2(q.y);
+                v[4 * k + 2] = bf16x2_to_f32x2(q.z);
+                v[4 * k + 3] = bf16x2_to_f32x2(q.w);
             }
-            float s[E];
-            if (a.f) {
-                float mean = 0.f, rstd = 1.f;
-                if (LN && a.post == HCW_NORM_LAYER) {
-                    float t[1] = {0.f};
+        } else if (sizeof(T) == 2 && VW == 2) {
 #pragma unroll
-                    for (int j = 0; j < E; ++j) t[0] += fc.get(j);
-                    rs.sum(t);
-                    mean = t[0] * inv_d;
-                }
-                if (a.post != HCW_NORM_NONE) {
-                    float t[1] = {0.f};
-#pragma unroll
-                    for (int j = 0; j < E; ++j) {
-                        const float c = Row::col(l, nl, j) < a.d ? fc.get(j) - mean : 0.f;
-                        t[0] += c * c;
-                    }
-                    rs.sum(t);
-                    rstd = 1.f / sqrtf(t[0] * inv_d + a.eps);
-                }
-#pragma unroll
-                for (int j = 0; j < E; ++j)
-                    s[j] = a.alpha * rc.get(j) + ((fc.get(j) - mean) * rstd * gw[j] + gb[j]);
-            } else {
-#pragma unroll
-                for (int j = 0; j < E; ++j) s[j] = a.alpha * rc.get(j);
+            for (int k = 0; k < H; ++k) {
+                const int c = 2 * (l + nl * k);
+                v[k] = bf16x2_to_f32x2(c < d ? *reinterpret_cast<const uint32_t*>(p + c) : 0u);
             }
-            if (a.o0) Row::store(a.o0, row, l, nl, a.d, s);
-            if (a.o1) {
-                float mean = 0.f;
-                if (LN && a.pre == HCW_NORM_LAYER) {
-                    float t[1] = {0.f};
+        } else if (sizeof(T) == 2) {
+            const unsigned short* h = reinterpret_cast<const unsigned short*>(p);
 #pragma unroll
-                    for (int j = 0; j < E; ++j) t[0] += s[j];
-                    rs.sum(t);
-                    mean = t[0] * inv_d;
-                }
-                float t[1] = {0.f};
+            for (int k = 0; k < H; ++k) {
+                const int c0 = l + nl * 2 * k, c1 = c0 + nl;
+                v[k] = f32x2_pack(c0 < d ? __uint_as_float((uint32_t)h[c0] << 16) : 0.f,
+                                  c1 < d ? __uint_as_float((uint32_t)h[c1] << 16) : 0.f);
+            }
+        } else if (VW == 4) {
 #pragma unroll
-                for (int j = 0; j < E; ++j) {
-                    s[j] = Row::col(l, nl, j) < a.d ? s[j] - mean : 0.f;
-                    t[0] += s[j] * s[j];
-                }
-                rs.sum(t);
-                const float rstd = 1.f / sqrtf(t[0] * inv_d + a.eps);
+            for (int k = 0; k < E / 4; ++k) {
+                const int c = 4 * (l + nl * k);
+                const float4 q = c < d ? *reinterpret_cast<const float4*>(p + c)
+                                       : make_float4(0.f, 0.f, 0.f, 0.f);
+                v[2 * k] = f32x2_pack(q.x, q.y);
+                v[2 * k + 1] = f32x2_pack(q.z, q.w);
+            }
+        } else {
+            const float* h = reinterpret_cast<const float*>(p);
 #pragma unroll
-                for (int j = 0; j < E; ++j) s[j] = s[j] * rstd * pw[j] + pb[j];
-                Row::store(a.o1, row, l, nl, a.d, s);
+            for (int k = 0; k < H; ++k) {
+                const int c0 = l + nl * 2 * k, c1 = c0 + nl;
+                v[k] = f32x2_pack(c0 < d ? h[c0] : 0.f, c1 < d ? h[c1] : 0.f);
             }
         }
     }
+    __device__ __forceinline__ static void store(void* base, size_t row, int l, int nl, int d,
+                                                 const uint64_t (&v)[H]) {
+        T* p = static_cast<T*>(base) + row * (size_t)d;
+        auto pack = [&](int i) {
+            const float2 f = f32x2_unpack(v[i]);
+            return pack_bf16x2(f.x, f.y);
+        };
+        if (sizeof(T) == 2 && VW == 8) {
+#pragma unroll
+            for (int k = 0; k < E / 8; ++k) {
+                const int c = 8 * (l + nl * k);
+                if (c < d)
+                    *reinterpret_cast<uint4*>(p + c) =
+                        make_uint4(pack(4 * k), pack(4 * k + 1), pack(4 * k + 2), pack(4 * k + 3));
+            }
+        } else if (sizeof(T) == 2 && VW == 2) {
+#pragma unroll
+            for (int k = 0; k < H; ++k) {
+                const int c = 2 * (l + nl * k);
+                if (c < d) *reinterpret_cast<uint32_t*>(p + c) = pack(k);
+            }
+        } else if (VW == 4) {
+#pragma unroll
+            for (int k = 0; k < E / 4; ++k) {
+                const int c = 4 * (l + nl * k);
+                const float2 x = f32x2_unpack(v[2 * k]), y = f32x2_unpack(v[2 * k + 1]);
+                if (c < d) *reinterpret_cast<float4*>(p + c) = make_float4(x.x, x.y, y.x, y.y);
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < H; ++k) {
+                const int c0 = l + nl * 2 * k, c1 = c0 + nl;
+                const float2 f = f32x2_unpack(v[k]);
+                if (sizeof(T) == 2) {
+                    __nv_bfloat16* h = reinterpret_cast<__nv_bfloat16*>(p);
+                    if (c0 < d) h[c0] = __float2bfloat16_rn(f.x);
+                    if (c1 < d) h[c1] = __float2bfloat16_rn(f.y);
+                } else {
+                    float* h = reinterpret_cast<float*>(p);
+                    if (c0 < d) h[c0] = f.x;
+                    if (c1 < d) h[c1] = f.y;
+                }
+            }
+        }
+    }
+    // a parameter vector (null: `none` everywhere; 0 past the row's end)
+    __device__ __forceinline__ static void param(uint64_t (&v)[H], const float* p, float none, int l,
+                                                 int nl, int d) {
+#pragma unroll
+        for (int k = 0; k < H; ++k) {
+            const int c0 = col(l, nl, 2 * k), c1 = col(l, nl, 2 * k + 1);
+            v[k] = f32x2_pack(c0 < d ? (p ? p[c0] : none) : 0.f, c1 < d ? (p ? p[c1] : none) : 0.f);
+        }
+    }
+    // v - m, zero past the row's end (`ragged`: the row ends inside the threads' columns)
+    __device__ __forceinline__ static void centre(uint64_t (&v)[H], float m, bool ragged, int l,
+                                                  int nl, int d) {
+        const uint64_t mm = f32x2_pack(-m, -m);
+#pragma unroll
+        for (int k = 0; k < H; ++k) v[k] = f32x2_add(v[k], mm);
+        if (ragged)
+#pragma unroll
+            for (int k = 0; k < H; ++k) {
+                const float2 f = f32x2_unpack(v[k]);
+                v[k] = f32x2_pack(col(l, nl, 2 * k) < d ? f.x : 0.f,
+                                  col(l, nl, 2 * k + 1) < d ? f.y : 0.f);
+            }
+    }
+};
+
+template <int H>
+__device__ __forceinline__ void pairs_zero(uint64_t (&v)[H]) {
+#pragma unroll
+    for (int j = 0; j < H; ++j) v[j] = 0;
+}
+__device__ __forceinline__ float pair_sum(uint64_t v) {
+    const float2 f = f32x2_unpack(v);
+    return f.x + f.y;
+}
+__device__ __forceinline__ uint64_t both(float x) { return f32x2_pack(x, x); }
+
+// Sums of N <= 8 values over the nl threads of a row, on every one of them.
+struct RowSum {
+    NormShared* sh;
+    int parity, nl, warp, lane;
+    template <int N>
+    __device__ __forceinline__ void sum(float (&v)[N]) {
+        if (nl < 32) {   // several rows in a warp
+            for (int o = nl >> 1; o > 0; o >>= 1)
+#pragma unroll
+                for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+            return;
+        }
+        // each step sends half of the values away and takes in the partner's other half;
+        // value i ends on the lanes whose upper bits spell it
+        constexpr int M = N <= 1 ? 1 : N <= 2 ? 2 : N <= 4 ? 4 : 8;
+        float t[M];
+#pragma unroll
+        for (int i = 0; i < M; ++i) t[i] = i < N ? v[i] : 0.f;
+        int o = 16;
+#pragma unroll
+        for (int m = M >> 1; m > 0; m >>= 1, o >>= 1) {
+            const bool up = lane & o;
+#pragma unroll
+            for (int i = 0; i < m; ++i) {
+                const float give = up ? t[i] : t[i + m];
+                const float keep = up ? t[i + m] : t[i];
+                t[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+            }
+        }
+#pragma unroll
+        for (int k = 16 / M; k > 0; k >>= 1) t[0] += __shfl_xor_sync(0xffffffffu, t[0], k);
+        // lanes i * (32 / M) .. hold value i
+        if (nl == 32) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = __shfl_sync(0xffffffffu, t[0], i * (32 / M));
+            return;
+        }
+        // Between the row's warps.  The parity alternates from round to round: a round's
+        // values are read before the round after the next overwrites them, a barrier of the
+        // row's warps lies between.
+        const int W = nl >> 5, first = warp / W * W;
+        float(*buf)[kNormRed] = sh->red[parity];
+        parity ^= 1;
+        if ((lane & (32 / M - 1)) == 0) buf[warp][lane / (32 / M)] = t[0];
+        asm volatile("bar.sync %0, %1;" ::"r"(1 + warp / W), "r"(nl) : "memory");
+        // lane l adds value l % M of every (32 / M)-th warp
+        float x = 0.f;
+        for (int w = lane / M; w < W; w += 32 / M) x += buf[first + w][lane % M];
+#pragma unroll
+        for (int k = M; k < 32; k <<= 1) x += __shfl_xor_sync(0xffffffffu, x, k);
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = __shfl_sync(0xffffffffu, x, i);
+    }
+};
+
+// LN: some norm is a LayerNorm (means, centred values and biases).  R: rows a row group works
+// on at once.
+template <typename T, int VW, int NC, bool LN, int R>
+__global__ void __launch_bounds__(kNormThreads) norm_fwd_kernel(const NormArgs a) {
+    extern __shared__ __align__(128) uint8_t norm_smem[];
+    __shared__ NormShared sh;
+    constexpr int E = 8 * NC, H = E / 2;
+    using C = Cols<T, VW, E>;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int nt = (int)blockDim.x, nl = a.nl, d = a.d;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < a.bufs; ++i) {
+            mbar_init(&sh.full[i], 1);
+            mbar_init(&sh.empty[i], nt >> 5);
+        }
+        sh.abort = 0;
+        fence_mbar_init();
+    }
+    __syncthreads();
+    pdl_wait();
+    pdl_trigger();
+    NormFeed feed;
+    bool fed = true;
+    if (threadIdx.x == 0) {
+        feed.start(a);
+        for (int i = 0; i < a.bufs; ++i) fed = fed && feed.fetch<T, 2>(a, norm_smem, &sh);
+    }
+    const int l = (int)threadIdx.x % nl, grp = (int)threadIdx.x / nl, n_grp = nt / nl;
+    const float inv_d = 1.f / (float)d;
+    const bool ragged = d != nl * E;
+    const bool has_r = a.in[0], has_f = a.in[1];
+    const int row_bytes = d * (int)sizeof(T), first = grp * row_bytes, step = n_grp * row_bytes;
+    const int items = a.groups * a.slices;
+    RowSum rs = {&sh, 0, nl, warp, lane};
+    const uint64_t alpha = both(a.alpha);
+    uint64_t pw[H], pb[LN ? H : 1];
+    C::param(pw, a.pre_w, 1.f, l, nl, d);
+    if constexpr (LN) C::param(pb, a.pre_b, 0.f, l, nl, d);
+    int b = 0;
+    uint32_t round = 0;
+    bool ok = true;
+    for (int item = blockIdx.x; item < items && ok; item += gridDim.x) {
+        int g, r0, r1;
+        item_rows(a, item, g, r0, r1);
+        uint64_t gw[H], gb[LN ? H : 1];   // gate * post_w, gate * post_b
+        {
+            uint64_t t[H];
+            C::param(t, a.gate ? a.gate + (size_t)g * d : nullptr, 1.f, l, nl, d);
+            C::param(gw, a.post_w, 1.f, l, nl, d);
+            if constexpr (LN) C::param(gb, a.post_b, 0.f, l, nl, d);
+#pragma unroll
+            for (int j = 0; j < H; ++j) {
+                gw[j] = f32x2_mul(gw[j], t[j]);
+                if constexpr (LN) gb[j] = f32x2_mul(gb[j], t[j]);
+            }
+        }
+        for (int row0 = r0; row0 < r1; row0 += a.rows) {
+            const bool okw = mbar_wait(&sh.full[b], round & 1, &sh.abort, kNormTimeoutNs);
+            ok = __all_sync(0xffffffffu, okw && fed);
+            if (!ok) break;
+            // a group's rows past the buffer's n hold what was there before: they are worked
+            // on and not stored
+            const int n = r1 - row0 < a.rows ? r1 - row0 : a.rows;
+            const uint8_t* buf = norm_smem + (size_t)b * 2 * a.piece +
+                                 ((uint32_t)((size_t)row0 * d * sizeof(T)) & 15) + first;
+            uint64_t v[R][H];
+            float q[R];
+#pragma unroll
+            for (int k = 0; k < R; ++k) {
+                q[k] = 1.f;
+                if (has_f)
+                    C::load(v[k], buf + a.piece + k * step, l, nl, d);
+                else
+                    pairs_zero(v[k]);
+            }
+            if (has_f && a.post != HCW_NORM_NONE) {
+                if (LN && a.post == HCW_NORM_LAYER) {
+#pragma unroll
+                    for (int k = 0; k < R; ++k) {
+                        uint64_t t = v[k][0];
+#pragma unroll
+                        for (int j = 1; j < H; ++j) t = f32x2_add(t, v[k][j]);
+                        q[k] = pair_sum(t);
+                    }
+                    rs.sum(q);
+#pragma unroll
+                    for (int k = 0; k < R; ++k) C::centre(v[k], q[k] * inv_d, ragged, l, nl, d);
+                }
+#pragma unroll
+                for (int k = 0; k < R; ++k) {
+                    uint64_t t = 0;
+#pragma unroll
+                    for (int j = 0; j < H; ++j) t = f32x2_fma(v[k][j], v[k][j], t);
+                    q[k] = pair_sum(t);
+                }
+                rs.sum(q);
+#pragma unroll
+                for (int k = 0; k < R; ++k) q[k] = rsqrtf(q[k] * inv_d + a.eps);
+            }
+#pragma unroll
+            for (int k = 0; k < R; ++k) {
+                uint64_t r[H];
+                if (has_r)
+                    C::load(r, buf + k * step, l, nl, d);
+                else
+                    pairs_zero(r);
+                const uint64_t qq = both(q[k]);
+#pragma unroll
+                for (int j = 0; j < H; ++j) {
+                    uint64_t t = f32x2_mul(r[j], alpha);
+                    if constexpr (LN) t = f32x2_add(t, gb[j]);
+                    v[k][j] = f32x2_fma(f32x2_mul(v[k][j], qq), gw[j], t);
+                }
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sh.empty[b]);   // the buffer has been read
+            if (a.o0)
+#pragma unroll
+                for (int k = 0; k < R; ++k)
+                    if (grp + n_grp * k < n) C::store(a.o0, row0 + grp + n_grp * k, l, nl, d, v[k]);
+            if (a.o1) {
+                if (LN && a.pre == HCW_NORM_LAYER) {
+#pragma unroll
+                    for (int k = 0; k < R; ++k) {
+                        uint64_t t = v[k][0];
+#pragma unroll
+                        for (int j = 1; j < H; ++j) t = f32x2_add(t, v[k][j]);
+                        q[k] = pair_sum(t);
+                    }
+                    rs.sum(q);
+#pragma unroll
+                    for (int k = 0; k < R; ++k) C::centre(v[k], q[k] * inv_d, ragged, l, nl, d);
+                }
+#pragma unroll
+                for (int k = 0; k < R; ++k) {
+                    uint64_t t = 0;
+#pragma unroll
+                    for (int j = 0; j < H; ++j) t = f32x2_fma(v[k][j], v[k][j], t);
+                    q[k] = pair_sum(t);
+                }
+                rs.sum(q);
+#pragma unroll
+                for (int k = 0; k < R; ++k) {
+                    const uint64_t qq = both(rsqrtf(q[k] * inv_d + a.eps));
+#pragma unroll
+                    for (int j = 0; j < H; ++j) {
+                        v[k][j] = f32x2_mul(v[k][j], qq);
+                        if constexpr (LN)
+                            v[k][j] = f32x2_fma(v[k][j], pw[j], pb[j]);
+                        else
+                            v[k][j] = f32x2_mul(v[k][j], pw[j]);
+                    }
+                    if (grp + n_grp * k < n) C::store(a.o1, row0 + grp + n_grp * k, l, nl, d, v[k]);
+                }
+            }
+            if (threadIdx.x == 0) fed = feed.fetch<T, 2>(a, norm_smem, &sh);
+            __syncwarp();
+            if (++b == a.bufs) {
+                b = 0;
+                ++round;
+            }
+        }
+    }
+    if (threadIdx.x == 0) feed.drain(a, &sh);
 }
 
 // Adds the row groups' values v of a CTA into group 0's, in group order, through `buf`
-// ([n_grp - 1][E][32 W] floats).
-template <int E>
-__device__ __forceinline__ void group_add(float (&v)[E], float* buf, int grp, int n_grp, int l,
+// ([n_grp - 1][H][nl] pairs).
+template <int H>
+__device__ __forceinline__ void group_add(uint64_t (&v)[H], uint64_t* buf, int grp, int n_grp, int l,
                                           int nl) {
     if (n_grp == 1) return;
     __syncthreads();
     if (grp > 0)
 #pragma unroll
-        for (int j = 0; j < E; ++j) buf[((size_t)(grp - 1) * E + j) * nl + l] = v[j];
+        for (int j = 0; j < H; ++j) buf[((grp - 1) * H + j) * nl + l] = v[j];
     __syncthreads();
     if (grp == 0)
         for (int q = 0; q < n_grp - 1; ++q)
 #pragma unroll
-            for (int j = 0; j < E; ++j) v[j] += buf[((size_t)q * E + j) * nl + l];
+            for (int j = 0; j < H; ++j) v[j] = f32x2_add(v[j], buf[(q * H + j) * nl + l]);
 }
 
-template <typename T, bool VEC, int NC, bool LN>
+template <typename T, int VW, int NC, bool LN, int R>
 __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const NormArgs a) {
-    __shared__ __align__(16) float red[2][kNormThreads / 32][kNormRed];
-    extern __shared__ __align__(16) float gbuf[];
-    constexpr int E = 8 * NC;
-    using Row = RowRegs<T, VEC, NC>;
-    const int warp = threadIdx.x >> 5, W = a.W;
-    const int nl = 32 * W, l = (int)threadIdx.x % nl;
-    const int grp = warp / W, n_grp = (int)(blockDim.x >> 5) / W;
-    const float inv_d = 1.f / (float)a.d;
-    RowSum rs = {red, 0, W, warp};
+    extern __shared__ __align__(128) uint8_t norm_smem[];
+    __shared__ NormShared sh;
+    constexpr int E = 8 * NC, H = E / 2;
+    using C = Cols<T, VW, E>;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int nt = (int)blockDim.x, nl = a.nl, d = a.d;
+    uint64_t* const gbuf = reinterpret_cast<uint64_t*>(norm_smem + (size_t)a.bufs * 4 * a.piece);
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < a.bufs; ++i) {
+            mbar_init(&sh.full[i], 1);
+            mbar_init(&sh.empty[i], nt >> 5);
+        }
+        sh.abort = 0;
+        fence_mbar_init();
+    }
+    __syncthreads();
     pdl_wait();
     pdl_trigger();
+    NormFeed feed;
+    bool fed = true;
+    if (threadIdx.x == 0) {
+        feed.start(a);
+        for (int i = 0; i < a.bufs; ++i) fed = fed && feed.fetch<T, 4>(a, norm_smem, &sh);
+    }
+    const int l = (int)threadIdx.x % nl, grp = (int)threadIdx.x / nl, n_grp = nt / nl;
+    const float inv_d = 1.f / (float)d;
+    const bool ragged = d != nl * E;
+    const bool has_dr = a.in[0], has_f = a.in[1], has_dx = a.in[3];
+    const int row_bytes = d * (int)sizeof(T), first = grp * row_bytes, step = n_grp * row_bytes;
     const int items = a.groups * a.slices;
-    float pw[E];
-    load_par<VEC, NC>(pw, a.pre_w, 1.f, l, nl, a.d);
-    // sums over all of the CTA's rows: gate ds fhat, gate ds, dx shat, dx
-    float c_w[E], c_b[E], c_pw[E], c_pb[E];
-#pragma unroll
-    for (int j = 0; j < E; ++j) c_w[j] = c_b[j] = c_pw[j] = c_pb[j] = 0.f;
+    RowSum rs = {&sh, 0, nl, warp, lane};
+    uint64_t pw[H];
+    C::param(pw, a.pre_w, 1.f, l, nl, d);
+    // sums over all of the CTA's rows: dx shat, dx
+    uint64_t c_w[H], c_b[LN ? H : 1];
+    pairs_zero(c_w);
+    if constexpr (LN) pairs_zero(c_b);
+    float* const crow = a.cpart ? a.cpart + (size_t)blockIdx.x * kNormPar * d : nullptr;
+    int b = 0;
+    uint32_t round = 0;
+    bool ok = true;
     for (int item = blockIdx.x; item < items; item += gridDim.x) {
         int g, r0, r1;
         item_rows(a, item, g, r0, r1);
-        const float* gate = a.gate ? a.gate + (size_t)g * a.d : nullptr;
-        float gp[E];   // gate * post_w
+        const float* gate = a.gate ? a.gate + (size_t)g * d : nullptr;
+        uint64_t gp[H];   // gate * post_w
         {
-            float t[E];
-            load_par<VEC, NC>(t, gate, 1.f, l, nl, a.d);
-            load_par<VEC, NC>(gp, a.post_w, 1.f, l, nl, a.d);
+            uint64_t t[H];
+            C::param(t, gate, 1.f, l, nl, d);
+            C::param(gp, a.post_w, 1.f, l, nl, d);
 #pragma unroll
-            for (int j = 0; j < E; ++j) gp[j] *= t[j];
+            for (int j = 0; j < H; ++j) gp[j] = f32x2_mul(gp[j], t[j]);
         }
         // sums over the item's rows: ds fhat, ds
-        float i_w[E], i_b[E];
+        uint64_t i_w[H], i_b[LN ? H : 1];
+        pairs_zero(i_w);
+        if constexpr (LN) pairs_zero(i_b);
+        for (int row0 = r0; row0 < r1 && ok; row0 += a.rows) {
+            const bool okw = mbar_wait(&sh.full[b], round & 1, &sh.abort, kNormTimeoutNs);
+            ok = __all_sync(0xffffffffu, okw && fed);
+            if (!ok) break;
+            const int n = r1 - row0 < a.rows ? r1 - row0 : a.rows;
+            const uint8_t* buf = norm_smem + (size_t)b * 4 * a.piece +
+                                 ((uint32_t)((size_t)row0 * d * sizeof(T)) & 15) + first;
+            // a group's rows past the buffer's n: zeros
+            uint64_t S[R][H], F[R][H], X[R][H];
 #pragma unroll
-        for (int j = 0; j < E; ++j) i_w[j] = i_b[j] = 0.f;
-        Row nr, nf, ns, nx;
-        nr.clear();
-        nf.clear();
-        ns.clear();
-        nx.clear();
-        auto load = [&](int row) {
-            if (a.r) nr.load(a.r, row, l, nl, a.d);
-            if (a.f) nf.load(a.f, row, l, nl, a.d);
-            if (a.dx) {
-                ns.load(a.s, row, l, nl, a.d);
-                nx.load(a.dx, row, l, nl, a.d);
+            for (int k = 0; k < R; ++k) {
+                const bool in = grp + n_grp * k < n;
+                if (in && has_dx) {
+                    C::load(S[k], buf + 2 * a.piece + k * step, l, nl, d);
+                    C::load(X[k], buf + 3 * a.piece + k * step, l, nl, d);
+                } else {
+                    pairs_zero(S[k]);
+                    pairs_zero(X[k]);
+                }
+                if (in && has_f)
+                    C::load(F[k], buf + a.piece + k * step, l, nl, d);
+                else
+                    pairs_zero(F[k]);
             }
-        };
-        int row = r0 + grp;
-        if (row < r1) load(row);
-        for (; row < r1; row += n_grp) {
-            const Row cr = nr, cf = nf, cs = ns, cx = nx;
-            if (row + n_grp < r1) load(row + n_grp);
-            float mean_s = 0.f, mean_f = 0.f;
             if (LN) {
-                float t[2] = {0.f, 0.f};
+                float t[2 * R];
 #pragma unroll
-                for (int j = 0; j < E; ++j) {
-                    t[0] += cs.get(j);
-                    t[1] += cf.get(j);
+                for (int k = 0; k < R; ++k) {
+                    uint64_t x = S[k][0], y = F[k][0];
+#pragma unroll
+                    for (int j = 1; j < H; ++j) {
+                        x = f32x2_add(x, S[k][j]);
+                        y = f32x2_add(y, F[k][j]);
+                    }
+                    t[2 * k] = pair_sum(x);
+                    t[2 * k + 1] = pair_sum(y);
                 }
                 rs.sum(t);
-                mean_s = a.pre == HCW_NORM_LAYER ? t[0] * inv_d : 0.f;
-                mean_f = a.post == HCW_NORM_LAYER ? t[1] * inv_d : 0.f;
-            }
-            // sums of (s - mean)^2, (f - mean)^2, e (s - mean), e  with e = dx pre_w
-            float t[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int j = 0; j < E; ++j) {
-                const bool in = Row::col(l, nl, j) < a.d;
-                const float sc = in ? cs.get(j) - mean_s : 0.f;
-                const float fc = in ? cf.get(j) - mean_f : 0.f;
-                const float e = cx.get(j) * pw[j];
-                t[0] += sc * sc;
-                t[1] += fc * fc;
-                t[2] += e * sc;
-                t[3] += e;
+                for (int k = 0; k < R; ++k) {
+                    if (a.pre == HCW_NORM_LAYER) C::centre(S[k], t[2 * k] * inv_d, ragged, l, nl, d);
+                    if (a.post == HCW_NORM_LAYER)
+                        C::centre(F[k], t[2 * k + 1] * inv_d, ragged, l, nl, d);
+                }
+            }
+            // sums of s^2, e s, f^2, e  with e = dx pre_w (s and f centred)
+            float t[4 * R];
+#pragma unroll
+            for (int k = 0; k < R; ++k) {
+                uint64_t ss = 0, es = 0, ff = 0, e1 = 0;
+#pragma unroll
+                for (int j = 0; j < H; ++j) {
+                    const uint64_t e = f32x2_mul(X[k][j], pw[j]);
+                    ss = f32x2_fma(S[k][j], S[k][j], ss);
+                    es = f32x2_fma(e, S[k][j], es);
+                    ff = f32x2_fma(F[k][j], F[k][j], ff);
+                    if (LN) e1 = f32x2_add(e1, e);
+                }
+                t[4 * k] = pair_sum(ss);
+                t[4 * k + 1] = pair_sum(es);
+                t[4 * k + 2] = pair_sum(ff);
+                t[4 * k + 3] = LN ? pair_sum(e1) : 0.f;
             }
             rs.sum(t);
-            const float rs_s = 1.f / sqrtf(t[0] * inv_d + a.eps);
-            const float rs_f = a.post != HCW_NORM_NONE ? 1.f / sqrtf(t[1] * inv_d + a.eps) : 1.f;
-            const float m2 = t[2] * inv_d * rs_s;   // mean(e shat)
-            const float m1 = LN && a.pre == HCW_NORM_LAYER ? t[3] * inv_d : 0.f;
-            float ds[E];
+            float u[2 * R], qf[R];   // sums of h fhat, h  with h = gate ds post_w
 #pragma unroll
-            for (int j = 0; j < E; ++j) {
-                ds[j] = cr.get(j);
-                if (a.dx) {
-                    const float x = cx.get(j);
-                    const float sh = (cs.get(j) - mean_s) * rs_s;
-                    ds[j] += (x * pw[j] - sh * m2 - m1) * rs_s;
-                    c_pw[j] += x * sh;
-                    if (LN) c_pb[j] += x;
+            for (int k = 0; k < R; ++k) {
+                const float rstd = has_dx ? rsqrtf(t[4 * k] * inv_d + a.eps) : 0.f;
+                const float m2 = t[4 * k + 1] * inv_d * rstd;   // mean(e shat)
+                const float m1 = LN && a.pre == HCW_NORM_LAYER ? t[4 * k + 3] * inv_d : 0.f;
+                qf[k] = a.post != HCW_NORM_NONE ? rsqrtf(t[4 * k + 2] * inv_d + a.eps) : 1.f;
+                uint64_t D[H];
+                if (has_dr && grp + n_grp * k < n)
+                    C::load(D, buf + k * step, l, nl, d);
+                else
+                    pairs_zero(D);
+                const uint64_t rr = both(rstd), nm2 = both(-m2), nm1 = both(-m1), qq = both(qf[k]);
+                uint64_t hf = 0, h1 = 0;
+#pragma unroll
+                for (int j = 0; j < H; ++j) {
+                    // ds, from here on in place of dx
+                    const uint64_t sh_ = f32x2_mul(S[k][j], rr);
+                    uint64_t e = f32x2_fma(sh_, nm2, f32x2_mul(X[k][j], pw[j]));
+                    if (LN) e = f32x2_add(e, nm1);
+                    c_w[j] = f32x2_fma(X[k][j], sh_, c_w[j]);
+                    if constexpr (LN) c_b[j] = f32x2_add(c_b[j], X[k][j]);
+                    X[k][j] = f32x2_fma(e, rr, D[j]);
+                    // fhat, in place of f; h is 0 past the row's end
+                    F[k][j] = f32x2_mul(F[k][j], qq);
+                    const uint64_t h = f32x2_mul(X[k][j], gp[j]);
+                    i_w[j] = f32x2_fma(X[k][j], F[k][j], i_w[j]);
+                    if constexpr (LN) i_b[j] = f32x2_add(i_b[j], X[k][j]);
+                    hf = f32x2_fma(h, F[k][j], hf);
+                    if (LN) h1 = f32x2_add(h1, h);
                 }
+                u[2 * k] = pair_sum(hf);
+                u[2 * k + 1] = LN ? pair_sum(h1) : 0.f;
             }
-            if (a.f) {
-                float u[2] = {0.f, 0.f};   // sums of h fhat, h  with h = gate ds post_w
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sh.empty[b]);   // the buffer has been read
+            if (a.o1) {
+                if (a.post != HCW_NORM_NONE) rs.sum(u);
 #pragma unroll
-                for (int j = 0; j < E; ++j) {
-                    const float fh = (cf.get(j) - mean_f) * rs_f;
-                    const float h = ds[j] * gp[j];   // 0 past the row's end
-                    i_w[j] += ds[j] * fh;
-                    if (LN) i_b[j] += ds[j];
-                    u[0] += h * fh;
-                    u[1] += h;
-                }
-                if (a.o1) {
-                    if (a.post != HCW_NORM_NONE) rs.sum(u);
-                    const float m4 = a.post != HCW_NORM_NONE ? u[0] * inv_d : 0.f;
-                    const float m3 = LN && a.post == HCW_NORM_LAYER ? u[1] * inv_d : 0.f;
-                    float o[E];
+                for (int k = 0; k < R; ++k) {
+                    const uint64_t m4 = both(a.post != HCW_NORM_NONE ? -u[2 * k] * inv_d : 0.f);
+                    const uint64_t m3 =
+                        both(LN && a.post == HCW_NORM_LAYER ? -u[2 * k + 1] * inv_d : 0.f);
+                    const uint64_t qq = both(qf[k]);
 #pragma unroll
-                    for (int j = 0; j < E; ++j) {
-                        const float fh = (cf.get(j) - mean_f) * rs_f;
-                        o[j] = (ds[j] * gp[j] - fh * m4 - m3) * rs_f;
+                    for (int j = 0; j < H; ++j) {
+                        uint64_t o = f32x2_fma(F[k][j], m4, f32x2_mul(X[k][j], gp[j]));
+                        if (LN) o = f32x2_add(o, m3);
+                        F[k][j] = f32x2_mul(o, qq);
                     }
-                    Row::store(a.o1, row, l, nl, a.d, o);
+                    if (grp + n_grp * k < n) C::store(a.o1, row0 + grp + n_grp * k, l, nl, d, F[k]);
                 }
             }
             if (a.o0) {
+                const uint64_t alpha = both(a.alpha);
 #pragma unroll
-                for (int j = 0; j < E; ++j) ds[j] *= a.alpha;
-                Row::store(a.o0, row, l, nl, a.d, ds);
+                for (int k = 0; k < R; ++k) {
+#pragma unroll
+                    for (int j = 0; j < H; ++j) X[k][j] = f32x2_mul(X[k][j], alpha);
+                    if (grp + n_grp * k < n) C::store(a.o0, row0 + grp + n_grp * k, l, nl, d, X[k]);
+                }
+            }
+            if (threadIdx.x == 0) fed = feed.fetch<T, 4>(a, norm_smem, &sh);
+            __syncwarp();
+            if (++b == a.bufs) {
+                b = 0;
+                ++round;
             }
         }
         if (a.cpart || a.gpart) {
-            group_add<E>(i_w, gbuf, grp, n_grp, l, nl);
-            if (LN) group_add<E>(i_b, gbuf, grp, n_grp, l, nl);
+            group_add(i_w, gbuf, grp, n_grp, l, nl);
+            if constexpr (LN) group_add(i_b, gbuf, grp, n_grp, l, nl);
             if (grp == 0) {
-                float t[E], q[E];
-                load_par<VEC, NC>(t, gate, 1.f, l, nl, a.d);
+                // the CTA's sums of gate ds fhat and gate ds build up in its partial row
+                const bool fresh = item == (int)blockIdx.x;
 #pragma unroll
                 for (int j = 0; j < E; ++j) {
-                    c_w[j] += t[j] * i_w[j];
-                    if (LN) c_b[j] += t[j] * i_b[j];
-                }
-                if (a.gpart) {   // ds v = ds (fhat post_w + post_b)
-                    load_par<VEC, NC>(t, a.post_w, 1.f, l, nl, a.d);
-                    load_par<VEC, NC>(q, LN ? a.post_b : nullptr, 0.f, l, nl, a.d);
-#pragma unroll
-                    for (int j = 0; j < E; ++j) {
-                        const int c = Row::col(l, nl, j);
-                        if (c < a.d)
-                            a.gpart[(size_t)item * a.d + c] = i_w[j] * t[j] + (LN ? i_b[j] * q[j] : 0.f);
+                    const int c = C::col(l, nl, j);
+                    if (c >= d) continue;
+                    const float2 w2 = f32x2_unpack(i_w[j / 2]);
+                    const float w = j & 1 ? w2.y : w2.x;
+                    float bb = 0.f;
+                    if constexpr (LN) {
+                        const float2 b2 = f32x2_unpack(i_b[j / 2]);
+                        bb = j & 1 ? b2.y : b2.x;
+                    }
+                    if (crow) {
+                        const float t = gate ? gate[c] : 1.f;
+                        crow[c] = (fresh ? 0.f : crow[c]) + t * w;
+                        if constexpr (LN) crow[d + c] = (fresh ? 0.f : crow[d + c]) + t * bb;
+                    }
+                    if (a.gpart) {   // ds v = ds (fhat post_w + post_b)
+                        float v = w * (a.post_w ? a.post_w[c] : 1.f);
+                        if constexpr (LN) v += bb * (a.post_b ? a.post_b[c] : 0.f);
+                        a.gpart[(size_t)item * d + c] = v;
                     }
                 }
             }
         }
     }
-    if (a.cpart) {
-        group_add<E>(c_pw, gbuf, grp, n_grp, l, nl);
-        if (LN) group_add<E>(c_pb, gbuf, grp, n_grp, l, nl);
-        if (grp == 0) {
-            float* out = a.cpart + (size_t)blockIdx.x * kNormPar * a.d;
+    if (crow) {
+        group_add(c_w, gbuf, grp, n_grp, l, nl);
+        if constexpr (LN) group_add(c_b, gbuf, grp, n_grp, l, nl);
+        if (grp == 0)
 #pragma unroll
             for (int j = 0; j < E; ++j) {
-                const int c = Row::col(l, nl, j);
-                if (c >= a.d) continue;
-                out[c] = c_w[j];
-                out[(size_t)2 * a.d + c] = c_pw[j];
-                if (LN) {
-                    out[(size_t)a.d + c] = c_b[j];
-                    out[(size_t)3 * a.d + c] = c_pb[j];
+                const int c = C::col(l, nl, j);
+                if (c >= d) continue;
+                const float2 w2 = f32x2_unpack(c_w[j / 2]);
+                crow[(size_t)2 * d + c] = j & 1 ? w2.y : w2.x;
+                if constexpr (LN) {
+                    const float2 b2 = f32x2_unpack(c_b[j / 2]);
+                    crow[(size_t)3 * d + c] = j & 1 ? b2.y : b2.x;
                 }
             }
-        }
     }
+    if (threadIdx.x == 0) feed.drain(a, &sh);
 }
 
 // Column sums of the partial rows, 32 columns a block, 32 rows at a time, in a fixed order.
@@ -536,9 +830,11 @@ __global__ void __launch_bounds__(1024) norm_reduce_kernel(const NormReduceArgs 
     if (tx == 0 && co < a.d) dst[co] = t;
 }
 
-// Warps a row and CTA size for a width.
+// Threads a row and a CTA, buffers and items for a call.
 struct NormPlan {
-    int W, threads, nc, grid, slices, groups;
+    int nl, threads, nc, grid, slices, groups;
+    int rows, bufs, piece;
+    size_t smem;
 };
 
 int norm_sms() {
@@ -553,16 +849,35 @@ int norm_groups(int T, int rows_per_gate) {
     return rows_per_gate > 0 ? (int)(((long long)T + rows_per_gate - 1) / rows_per_gate) : 1;
 }
 
-NormPlan norm_plan(int T, int d, int rows_per_gate, int ctas_per_sm) {
+// rows a row group works on at once
+constexpr int norm_rows(bool bwd, int nc) { return bwd ? (nc == 1 ? 2 : 1) : (nc == 1 ? 4 : 2); }
+
+// elem: bytes of an element (grid, slices and groups do not depend on it).
+NormPlan norm_plan(bool bwd, int T, int d, int elem, int rows_per_gate) {
     NormPlan p;
     p.nc = d <= 4096 ? 1 : 2;
-    p.W = 1;
-    while (p.W * 256 * p.nc < d) p.W *= 2;
-    p.threads = p.W <= 8 ? 256 : 32 * p.W;
-    const int n_grp = p.threads / 32 / p.W;
+    const int E = 8 * p.nc;
+    // a power of two up to a warp, whole warps above
+    p.nl = 8;
+    while (p.nl < 32 && p.nl * E < d) p.nl *= 2;
+    if (p.nl * E < d) p.nl = (d + 32 * E - 1) / (32 * E) * 32;
+    // row groups of 256 threads in all, as many CTAs an SM as make 512
+    const int n_grp = p.nl < 256 ? 256 / p.nl : 1, n_in = bwd ? 4 : 2;
+    p.threads = n_grp * p.nl;
+    const int per_sm = 512 / p.threads > 0 ? 512 / p.threads : 1;
+    int r = norm_rows(bwd, p.nc);
+    const size_t sums = bwd ? (size_t)(n_grp - 1) * E * p.nl * sizeof(float) : 0;
+    const size_t room = kNormSmem / per_sm - 4096 - sums;
+    auto piece = [&](int rows) { return (int)(((size_t)rows * d * elem + 32 + 127) / 128 * 128); };
+    p.rows = n_grp * r;
+    p.piece = piece(p.rows);
+    p.bufs = (int)(room / ((size_t)n_in * p.piece));
+    if (p.bufs > 4) p.bufs = 4;
+    if (p.bufs < 1) p.bufs = 1;
+    p.smem = (size_t)p.bufs * n_in * p.piece + sums;
     p.groups = norm_groups(T, rows_per_gate);
     const int rows = rows_per_gate > 0 && rows_per_gate < T ? rows_per_gate : T;
-    const int most = norm_sms() * ctas_per_sm;
+    const int most = norm_sms() * per_sm;
     // enough runs of rows for every CTA, each with a row for every row group
     p.slices = p.groups > 0 ? (most + p.groups - 1) / p.groups : 1;
     const int runs = (rows + n_grp - 1) / n_grp;
@@ -573,32 +888,44 @@ NormPlan norm_plan(int T, int d, int rows_per_gate, int ctas_per_sm) {
     return p;
 }
 
-template <typename T, bool VEC, int NC, bool LN>
+template <typename T, int VW, int NC, bool LN>
 cudaError_t launch_norm(bool bwd, const NormPlan& p, const NormArgs& a, cudaStream_t st) {
-    if (!bwd)
-        return launch_pdl(norm_fwd_kernel<T, VEC, NC, LN>, dim3(p.grid), dim3(p.threads), 0, st, a);
-    const int n_grp = p.threads / 32 / p.W;
-    const size_t smem = (size_t)(n_grp - 1) * 8 * NC * 32 * p.W * sizeof(float);
-    return launch_pdl(norm_bwd_kernel<T, VEC, NC, LN>, dim3(p.grid), dim3(p.threads), smem, st, a);
+    auto kern = bwd ? norm_bwd_kernel<T, VW, NC, LN, norm_rows(true, NC)>
+                    : norm_fwd_kernel<T, VW, NC, LN, norm_rows(false, NC)>;
+    static std::once_flag once[64][2];
+    static cudaError_t set_err[64][2];
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+    std::call_once(once[dev][bwd], [&] {
+        set_err[dev][bwd] = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                 (int)(kNormSmem - 4096));
+    });
+    if (set_err[dev][bwd] != cudaSuccess) return set_err[dev][bwd];
+    return launch_pdl(kern, dim3((unsigned)p.grid), dim3((unsigned)p.threads), p.smem, st, a);
 }
 
-template <typename T>
-cudaError_t launch_norm_any(bool bwd, const NormPlan& p, const NormArgs& a, cudaStream_t st) {
+template <typename T, int VW>
+cudaError_t launch_norm_vw(bool bwd, const NormPlan& p, const NormArgs& a, cudaStream_t st) {
     const bool ln = a.post == HCW_NORM_LAYER || a.pre == HCW_NORM_LAYER;
-    const bool vec = a.d % 8 == 0;   // every row starts 16-byte aligned
     if (p.nc == 1)
-        return vec ? (ln ? launch_norm<T, true, 1, true>(bwd, p, a, st)
-                         : launch_norm<T, true, 1, false>(bwd, p, a, st))
-                   : (ln ? launch_norm<T, false, 1, true>(bwd, p, a, st)
-                         : launch_norm<T, false, 1, false>(bwd, p, a, st));
-    return vec ? (ln ? launch_norm<T, true, 2, true>(bwd, p, a, st)
-                     : launch_norm<T, true, 2, false>(bwd, p, a, st))
-               : (ln ? launch_norm<T, false, 2, true>(bwd, p, a, st)
-                     : launch_norm<T, false, 2, false>(bwd, p, a, st));
+        return ln ? launch_norm<T, VW, 1, true>(bwd, p, a, st)
+                  : launch_norm<T, VW, 1, false>(bwd, p, a, st);
+    return ln ? launch_norm<T, VW, 2, true>(bwd, p, a, st)
+              : launch_norm<T, VW, 2, false>(bwd, p, a, st);
 }
 
-constexpr int kNormBwdCtas = 2;   // backward CTAs per SM (kNormThreads / 2 threads each)
-constexpr int kNormFwdCtas = 4;
+// The widest access every row's start allows.
+cudaError_t launch_norm_any(bool bwd, int dtype, const NormPlan& p, const NormArgs& a,
+                            cudaStream_t st) {
+    if (dtype == HCW_F32)
+        return a.d % 4 == 0 ? launch_norm_vw<float, 4>(bwd, p, a, st)
+                            : launch_norm_vw<float, 1>(bwd, p, a, st);
+    return a.d % 8 == 0   ? launch_norm_vw<__nv_bfloat16, 8>(bwd, p, a, st)
+           : a.d % 2 == 0 ? launch_norm_vw<__nv_bfloat16, 2>(bwd, p, a, st)
+                          : launch_norm_vw<__nv_bfloat16, 1>(bwd, p, a, st);
+}
 
 size_t round256(size_t n) { return (n + 255) & ~(size_t)255; }
 
@@ -638,7 +965,15 @@ int norm_check(int T, int d, int dtype, int post, int pre, int rows_per_gate, fl
     return HCW_OK;
 }
 
-// The backward's partial sums: the CTAs' parameter rows, then dgate's rows.
+void norm_geometry(NormArgs& a, const NormPlan& p) {
+    a.nl = p.nl;
+    a.rows = p.rows;
+    a.bufs = p.bufs;
+    a.piece = p.piece;
+}
+
+// The backward's partial sums (of a size that does not depend on the type: the plan's grid
+// and slices do not): the CTAs' parameter rows, then dgate's rows.
 struct NormWs {
     size_t gpart, bytes;
 };
@@ -673,10 +1008,10 @@ int hcw_residual_norm_fwd(const void* r, const void* f, const float* gate, int r
     if (x_out && pre == HCW_NORM_NONE) return HCW_ERR_INVALID_ARG;
     if (T == 0) return HCW_OK;
     if ((!r && !f) || (!r_out && !x_out)) return HCW_ERR_INVALID_ARG;
-    const NormPlan p = norm_plan(T, d, rows_per_gate, kNormFwdCtas);
+    const NormPlan p = norm_plan(false, T, d, dtype == HCW_F32 ? 4 : 2, rows_per_gate);
     NormArgs a = {};
-    a.r = r;
-    a.f = f;
+    a.in[0] = r;
+    a.in[1] = f;
     a.o0 = r_out;
     a.o1 = x_out;
     a.gate = gate;
@@ -693,15 +1028,13 @@ int hcw_residual_norm_fwd(const void* r, const void* f, const float* gate, int r
     a.slices = p.slices;
     a.post = f ? post : HCW_NORM_NONE;
     a.pre = x_out ? pre : HCW_NORM_NONE;
-    a.W = p.W;
-    const cudaStream_t st = (cudaStream_t)stream;
-    return count_launch(dtype == HCW_BF16 ? launch_norm_any<__nv_bfloat16>(false, p, a, st)
-                                          : launch_norm_any<float>(false, p, a, st), 1);
+    norm_geometry(a, p);
+    return count_launch(launch_norm_any(false, dtype, p, a, (cudaStream_t)stream), 1);
 }
 
 size_t hcw_residual_norm_bwd_workspace_bytes(int T, int d, int rows_per_gate) {
     if (T < 1 || d < 1 || d > kNormMaxD || rows_per_gate < 0) return 0;
-    return norm_ws(norm_plan(T, d, rows_per_gate, kNormBwdCtas), d).bytes;
+    return norm_ws(norm_plan(true, T, d, 2, rows_per_gate), d).bytes;
 }
 
 int hcw_residual_norm_bwd(const void* dr_out, const void* dx_out, const void* s, const void* f,
@@ -733,7 +1066,7 @@ int hcw_residual_norm_bwd(const void* dr_out, const void* dx_out, const void* s,
                   ((dpre_w || dpre_b) && !dx_out) || (branch && !f)))
         return HCW_ERR_INVALID_ARG;
     const cudaStream_t st = (cudaStream_t)stream;
-    NormPlan p = norm_plan(T, d, rows_per_gate, kNormBwdCtas);
+    NormPlan p = norm_plan(true, T, d, dtype == HCW_F32 ? 4 : 2, rows_per_gate);
     NormWs w = {};
     const bool ws_needed = T > 0 && (params || (dgate && p.slices > 1));
     if (ws_needed) {
@@ -744,10 +1077,10 @@ int hcw_residual_norm_bwd(const void* dr_out, const void* dx_out, const void* s,
     float* gpart = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + w.gpart);
     if (T > 0) {
         NormArgs a = {};
-        a.r = dr_out;
-        a.f = branch ? f : nullptr;
-        a.s = s;
-        a.dx = dx_out;
+        a.in[0] = dr_out;
+        a.in[1] = branch ? f : nullptr;
+        a.in[2] = dx_out ? s : nullptr;
+        a.in[3] = dx_out;
         a.o0 = dr;
         a.o1 = df;
         a.gate = gate;
@@ -765,10 +1098,8 @@ int hcw_residual_norm_bwd(const void* dr_out, const void* dx_out, const void* s,
         a.slices = p.slices;
         a.post = branch ? post : HCW_NORM_NONE;
         a.pre = dx_out ? pre : HCW_NORM_NONE;
-        a.W = p.W;
-        const int e = count_launch(dtype == HCW_BF16
-                                       ? launch_norm_any<__nv_bfloat16>(true, p, a, st)
-                                       : launch_norm_any<float>(true, p, a, st), 1);
+        norm_geometry(a, p);
+        const int e = count_launch(launch_norm_any(true, dtype, p, a, st), 1);
         if (e) return e;
     }
     // without rows the sums are zero: the same kernel over no partial rows
