@@ -15,11 +15,11 @@
 // writes two.  Runs of consecutive rows are always on their way into a ring in shared memory
 // (bulk copies: consecutive rows are one piece, whatever their width and alignment), so the
 // reductions of one row never hold up the loads of the next.  A row belongs to `nl`
-// threads (8 columns each, 16 above 4096 columns), whose columns stay the same from row to
-// row: the parameters and a thread's share of the parameter gradients stay in registers
-// over all rows of its CTA.  Several rows are reduced at once: the sums go through shuffles
-// that halve the number of values at each step and, between the warps of a row, through
-// shared memory behind a barrier of those warps.  The arithmetic is in packed pairs (two fp32
+// threads (16 columns each: up to 512 columns no two warps share a row), whose columns stay
+// the same from row to row: a thread's share of the parameter gradients stays in registers
+// over all rows of its CTA, the parameters in shared memory.  The sums of a row go through
+// shuffles that halve the number of values at each step and, between the warps of a row,
+// through shared memory behind a barrier of those warps.  The arithmetic is in packed pairs (two fp32
 // operations an instruction).  Parameter gradients: each CTA writes one row of partial
 // sums, a second kernel adds the rows in a fixed order, so the same inputs give the same
 // bits.
@@ -42,6 +42,8 @@ constexpr int kNormThreads = 512;   // most threads of a CTA
 constexpr int kNormMaxD = 8192;
 constexpr int kNormPar = 4;         // parameter sums of a CTA: post_w, post_b, pre_w, pre_b
 constexpr int kNormRed = 8;         // values of one reduction round
+constexpr int kNormCols = 16;       // columns a thread, in parts of 8:
+constexpr int kNormPart = 4;        // pairs of a part
 constexpr int kNormMaxBufs = 8;
 constexpr size_t kNormSmem = 232448;
 constexpr unsigned long long kNormTimeoutNs = 2000000000ull;
@@ -63,6 +65,7 @@ struct NormArgs {
     int rows_per_gate;    // rows of a group (the last may be shorter)
     int groups, slices;   // an item is one of `slices` runs of rows of a group
     int post, pre;
+    int ln;               // a LayerNorm among them
     int nl;               // threads a row
     int rows;             // rows of a buffer
     int bufs;
@@ -172,86 +175,88 @@ struct Cols {
     __device__ __forceinline__ static int col(int l, int nl, int j) {
         return VW * (l + nl * (j / VW)) + j % VW;
     }
-    // from shared memory, zeros past the row's end
-    __device__ __forceinline__ static void load(uint64_t (&v)[H], const uint8_t* row, int l, int nl,
-                                                int d) {
+    // Part k (8 columns) from shared memory, zeros past the row's end.
+    __device__ __forceinline__ static void load8(uint64_t (&v)[kNormPart], const uint8_t* row, int k,
+                                                 int l, int nl, int d) {
         const T* p = reinterpret_cast<const T*>(row);
         if (sizeof(T) == 2 && VW == 8) {
-#pragma unroll
-            for (int k = 0; k < E / 8; ++k) {
-                const int c = 8 * (l + nl * k);
-                const uint4 q = c < d ? *reinterpret_cast<const uint4*>(p + c)
-                                      : make_uint4(0u, 0u, 0u, 0u);
-                v[4 * k] = bf16x2_to_f32x2(q.x);
-                v[4 * k + 1] = bf16x2_to_f32x2(q.y);
-                v[4 * k + 2] = bf16x2_to_f32x2(q.z);
-                v[4 * k + 3] = bf16x2_to_f32x2(q.w);
-            }
+            const int c = 8 * (l + nl * k);
+            const uint4 q = c < d ? *reinterpret_cast<const uint4*>(p + c) : make_uint4(0u, 0u, 0u, 0u);
+            v[0] = bf16x2_to_f32x2(q.x);
+            v[1] = bf16x2_to_f32x2(q.y);
+            v[2] = bf16x2_to_f32x2(q.z);
+            v[3] = bf16x2_to_f32x2(q.w);
         } else if (sizeof(T) == 2 && VW == 2) {
 #pragma unroll
-            for (int k = 0; k < H; ++k) {
-                const int c = 2 * (l + nl * k);
-                v[k] = bf16x2_to_f32x2(c < d ? *reinterpret_cast<const uint32_t*>(p + c) : 0u);
+            for (int j = 0; j < 4; ++j) {
+                const int c = 2 * (l + nl * (4 * k + j));
+                v[j] = bf16x2_to_f32x2(c < d ? *reinterpret_cast<const uint32_t*>(p + c) : 0u);
             }
         } else if (sizeof(T) == 2) {
             const unsigned short* h = reinterpret_cast<const unsigned short*>(p);
 #pragma unroll
-            for (int k = 0; k < H; ++k) {
-                const int c0 = l + nl * 2 * k, c1 = c0 + nl;
-                v[k] = f32x2_pack(c0 < d ? __uint_as_float((uint32_t)h[c0] << 16) : 0.f,
+            for (int j = 0; j < 4; ++j) {
+                const int c0 = l + nl * (8 * k + 2 * j), c1 = c0 + nl;
+                v[j] = f32x2_pack(c0 < d ? __uint_as_float((uint32_t)h[c0] << 16) : 0.f,
                                   c1 < d ? __uint_as_float((uint32_t)h[c1] << 16) : 0.f);
             }
         } else if (VW == 4) {
 #pragma unroll
-            for (int k = 0; k < E / 4; ++k) {
-                const int c = 4 * (l + nl * k);
+            for (int j = 0; j < 2; ++j) {
+                const int c = 4 * (l + nl * (2 * k + j));
                 const float4 q = c < d ? *reinterpret_cast<const float4*>(p + c)
                                        : make_float4(0.f, 0.f, 0.f, 0.f);
-                v[2 * k] = f32x2_pack(q.x, q.y);
-                v[2 * k + 1] = f32x2_pack(q.z, q.w);
+                v[2 * j] = f32x2_pack(q.x, q.y);
+                v[2 * j + 1] = f32x2_pack(q.z, q.w);
             }
         } else {
             const float* h = reinterpret_cast<const float*>(p);
 #pragma unroll
-            for (int k = 0; k < H; ++k) {
-                const int c0 = l + nl * 2 * k, c1 = c0 + nl;
-                v[k] = f32x2_pack(c0 < d ? h[c0] : 0.f, c1 < d ? h[c1] : 0.f);
+            for (int j = 0; j < 4; ++j) {
+                const int c0 = l + nl * (8 * k + 2 * j), c1 = c0 + nl;
+                v[j] = f32x2_pack(c0 < d ? h[c0] : 0.f, c1 < d ? h[c1] : 0.f);
             }
         }
     }
-    __device__ __forceinline__ static void store(void* base, size_t row, int l, int nl, int d,
-                                                 const uint64_t (&v)[H]) {
+    __device__ __forceinline__ static void load(uint64_t (&v)[H], const uint8_t* row, int l, int nl,
+                                                int d) {
+#pragma unroll
+        for (int k = 0; k < H / kNormPart; ++k) {
+            uint64_t q[kNormPart];
+            load8(q, row, k, l, nl, d);
+#pragma unroll
+            for (int j = 0; j < kNormPart; ++j) v[k * kNormPart + j] = q[j];
+        }
+    }
+    __device__ __forceinline__ static void store8(void* base, size_t row, int k, int l, int nl, int d,
+                                                  const uint64_t (&v)[kNormPart]) {
         T* p = static_cast<T*>(base) + row * (size_t)d;
         auto pack = [&](int i) {
             const float2 f = f32x2_unpack(v[i]);
             return pack_bf16x2(f.x, f.y);
         };
         if (sizeof(T) == 2 && VW == 8) {
-#pragma unroll
-            for (int k = 0; k < E / 8; ++k) {
-                const int c = 8 * (l + nl * k);
-                if (c < d)
-                    *reinterpret_cast<uint4*>(p + c) =
-                        make_uint4(pack(4 * k), pack(4 * k + 1), pack(4 * k + 2), pack(4 * k + 3));
-            }
+            const int c = 8 * (l + nl * k);
+            if (c < d)
+                *reinterpret_cast<uint4*>(p + c) = make_uint4(pack(0), pack(1), pack(2), pack(3));
         } else if (sizeof(T) == 2 && VW == 2) {
 #pragma unroll
-            for (int k = 0; k < H; ++k) {
-                const int c = 2 * (l + nl * k);
-                if (c < d) *reinterpret_cast<uint32_t*>(p + c) = pack(k);
+            for (int j = 0; j < 4; ++j) {
+                const int c = 2 * (l + nl * (4 * k + j));
+                if (c < d) *reinterpret_cast<uint32_t*>(p + c) = pack(j);
             }
         } else if (VW == 4) {
 #pragma unroll
-            for (int k = 0; k < E / 4; ++k) {
-                const int c = 4 * (l + nl * k);
-                const float2 x = f32x2_unpack(v[2 * k]), y = f32x2_unpack(v[2 * k + 1]);
+            for (int j = 0; j < 2; ++j) {
+                const int c = 4 * (l + nl * (2 * k + j));
+                const float2 x = f32x2_unpack(v[2 * j]), y = f32x2_unpack(v[2 * j + 1]);
                 if (c < d) *reinterpret_cast<float4*>(p + c) = make_float4(x.x, x.y, y.x, y.y);
             }
         } else {
 #pragma unroll
-            for (int k = 0; k < H; ++k) {
-                const int c0 = l + nl * 2 * k, c1 = c0 + nl;
-                const float2 f = f32x2_unpack(v[k]);
+            for (int j = 0; j < 4; ++j) {
+                const int c0 = l + nl * (8 * k + 2 * j), c1 = c0 + nl;
+                const float2 f = f32x2_unpack(v[j]);
                 if (sizeof(T) == 2) {
                     __nv_bfloat16* h = reinterpret_cast<__nv_bfloat16*>(p);
                     if (c0 < d) h[c0] = __float2bfloat16_rn(f.x);
@@ -264,6 +269,16 @@ struct Cols {
             }
         }
     }
+    __device__ __forceinline__ static void store(void* base, size_t row, int l, int nl, int d,
+                                                 const uint64_t (&v)[H]) {
+#pragma unroll
+        for (int k = 0; k < H / kNormPart; ++k) {
+            uint64_t q[kNormPart];
+#pragma unroll
+            for (int j = 0; j < kNormPart; ++j) q[j] = v[k * kNormPart + j];
+            store8(base, row, k, l, nl, d, q);
+        }
+    }
     // a parameter vector (null: `none` everywhere; 0 past the row's end)
     __device__ __forceinline__ static void param(uint64_t (&v)[H], const float* p, float none, int l,
                                                  int nl, int d) {
@@ -273,19 +288,55 @@ struct Cols {
             v[k] = f32x2_pack(c0 < d ? (p ? p[c0] : none) : 0.f, c1 < d ? (p ? p[c1] : none) : 0.f);
         }
     }
-    // v - m, zero past the row's end (`ragged`: the row ends inside the threads' columns)
-    __device__ __forceinline__ static void centre(uint64_t (&v)[H], float m, bool ragged, int l,
-                                                  int nl, int d) {
+    // the product of two parameter vectors (or one) into shared memory, as `fetch` reads it
+    __device__ __forceinline__ static void fill(ulonglong2* to, const float* p, const float* q,
+                                                float none, int l, int nl, int d) {
+        uint64_t v[H];
+        param(v, p, none, l, nl, d);
+        if (q) {
+            uint64_t w[H];
+            param(w, q, 1.f, l, nl, d);
+#pragma unroll
+            for (int k = 0; k < H; ++k) v[k] = f32x2_mul(v[k], w[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < H / 2; ++k) to[k * nl + l] = make_ulonglong2(v[2 * k], v[2 * k + 1]);
+    }
+    __device__ __forceinline__ static void fetch(uint64_t (&v)[H], const ulonglong2* from, int l,
+                                                 int nl) {
+#pragma unroll
+        for (int k = 0; k < H / 2; ++k) {
+            const ulonglong2 x = from[k * nl + l];
+            v[2 * k] = x.x;
+            v[2 * k + 1] = x.y;
+        }
+    }
+    // part k of v - m, zero past the row's end (`ragged`: the row ends inside the threads'
+    // columns)
+    __device__ __forceinline__ static void centre8(uint64_t (&v)[kNormPart], float m, bool ragged,
+                                                   int k, int l, int nl, int d) {
         const uint64_t mm = f32x2_pack(-m, -m);
 #pragma unroll
-        for (int k = 0; k < H; ++k) v[k] = f32x2_add(v[k], mm);
+        for (int j = 0; j < kNormPart; ++j) v[j] = f32x2_add(v[j], mm);
         if (ragged)
 #pragma unroll
-            for (int k = 0; k < H; ++k) {
-                const float2 f = f32x2_unpack(v[k]);
-                v[k] = f32x2_pack(col(l, nl, 2 * k) < d ? f.x : 0.f,
-                                  col(l, nl, 2 * k + 1) < d ? f.y : 0.f);
+            for (int j = 0; j < kNormPart; ++j) {
+                const float2 f = f32x2_unpack(v[j]);
+                v[j] = f32x2_pack(col(l, nl, 8 * k + 2 * j) < d ? f.x : 0.f,
+                                  col(l, nl, 8 * k + 2 * j + 1) < d ? f.y : 0.f);
             }
+    }
+    __device__ __forceinline__ static void centre(uint64_t (&v)[H], float m, bool ragged, int l,
+                                                  int nl, int d) {
+#pragma unroll
+        for (int k = 0; k < H / kNormPart; ++k) {
+            uint64_t q[kNormPart];
+#pragma unroll
+            for (int j = 0; j < kNormPart; ++j) q[j] = v[k * kNormPart + j];
+            centre8(q, m, ragged, k, l, nl, d);
+#pragma unroll
+            for (int j = 0; j < kNormPart; ++j) v[k * kNormPart + j] = q[j];
+        }
     }
 };
 
@@ -357,11 +408,11 @@ struct RowSum {
 
 // LN: some norm is a LayerNorm (means, centred values and biases).  R: rows a row group works
 // on at once.
-template <typename T, int VW, int NC, bool LN, int R>
+template <typename T, int VW, bool LN, int R>
 __global__ void __launch_bounds__(kNormThreads) norm_fwd_kernel(const NormArgs a) {
     extern __shared__ __align__(128) uint8_t norm_smem[];
     __shared__ NormShared sh;
-    constexpr int E = 8 * NC, H = E / 2;
+    constexpr int E = kNormCols, H = E / 2;
     using C = Cols<T, VW, E>;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int nt = (int)blockDim.x, nl = a.nl, d = a.d;
@@ -390,28 +441,27 @@ __global__ void __launch_bounds__(kNormThreads) norm_fwd_kernel(const NormArgs a
     const int items = a.groups * a.slices;
     RowSum rs = {&sh, 0, nl, warp, lane};
     const uint64_t alpha = both(a.alpha);
-    uint64_t pw[H], pb[LN ? H : 1];
-    C::param(pw, a.pre_w, 1.f, l, nl, d);
-    if constexpr (LN) C::param(pb, a.pre_b, 0.f, l, nl, d);
+    // parameters: pre_w, gate * post_w, pre_b, gate * post_b
+    ulonglong2* const pw = reinterpret_cast<ulonglong2*>(norm_smem + (size_t)a.bufs * 2 * a.piece);
+    ulonglong2 *const gw = pw + H / 2 * nl, *const pb = gw + H / 2 * nl, *const gb = pb + H / 2 * nl;
+    if (grp == 0) {
+        C::fill(pw, a.pre_w, nullptr, 1.f, l, nl, d);
+        if (LN) C::fill(pb, a.pre_b, nullptr, 0.f, l, nl, d);
+    }
     int b = 0;
     uint32_t round = 0;
     bool ok = true;
-    for (int item = blockIdx.x; item < items && ok; item += gridDim.x) {
+    for (int item = blockIdx.x; item < items; item += gridDim.x) {
         int g, r0, r1;
         item_rows(a, item, g, r0, r1);
-        uint64_t gw[H], gb[LN ? H : 1];   // gate * post_w, gate * post_b
-        {
-            uint64_t t[H];
-            C::param(t, a.gate ? a.gate + (size_t)g * d : nullptr, 1.f, l, nl, d);
-            C::param(gw, a.post_w, 1.f, l, nl, d);
-            if constexpr (LN) C::param(gb, a.post_b, 0.f, l, nl, d);
-#pragma unroll
-            for (int j = 0; j < H; ++j) {
-                gw[j] = f32x2_mul(gw[j], t[j]);
-                if constexpr (LN) gb[j] = f32x2_mul(gb[j], t[j]);
-            }
+        const float* gate = a.gate ? a.gate + (size_t)g * d : nullptr;
+        __syncthreads();   // the item before has been worked through
+        if (grp == 0) {
+            C::fill(gw, a.post_w, gate, 1.f, l, nl, d);
+            if (LN) C::fill(gb, a.post_b, gate, 0.f, l, nl, d);
         }
-        for (int row0 = r0; row0 < r1; row0 += a.rows) {
+        __syncthreads();
+        for (int row0 = r0; row0 < r1 && ok; row0 += a.rows) {
             const bool okw = mbar_wait(&sh.full[b], round & 1, &sh.abort, kNormTimeoutNs);
             ok = __all_sync(0xffffffffu, okw && fed);
             if (!ok) break;
@@ -462,11 +512,15 @@ __global__ void __launch_bounds__(kNormThreads) norm_fwd_kernel(const NormArgs a
                 else
                     pairs_zero(r);
                 const uint64_t qq = both(q[k]);
+                uint64_t w[H];
+                C::fetch(w, gw, l, nl);
 #pragma unroll
-                for (int j = 0; j < H; ++j) {
-                    uint64_t t = f32x2_mul(r[j], alpha);
-                    if constexpr (LN) t = f32x2_add(t, gb[j]);
-                    v[k][j] = f32x2_fma(f32x2_mul(v[k][j], qq), gw[j], t);
+                for (int j = 0; j < H; ++j)
+                    v[k][j] = f32x2_fma(f32x2_mul(v[k][j], qq), w[j], f32x2_mul(r[j], alpha));
+                if (LN) {
+                    C::fetch(w, gb, l, nl);
+#pragma unroll
+                    for (int j = 0; j < H; ++j) v[k][j] = f32x2_add(v[k][j], w[j]);
                 }
             }
             __syncwarp();
@@ -499,13 +553,14 @@ __global__ void __launch_bounds__(kNormThreads) norm_fwd_kernel(const NormArgs a
 #pragma unroll
                 for (int k = 0; k < R; ++k) {
                     const uint64_t qq = both(rsqrtf(q[k] * inv_d + a.eps));
+                    uint64_t w[H];
+                    C::fetch(w, pw, l, nl);
 #pragma unroll
-                    for (int j = 0; j < H; ++j) {
-                        v[k][j] = f32x2_mul(v[k][j], qq);
-                        if constexpr (LN)
-                            v[k][j] = f32x2_fma(v[k][j], pw[j], pb[j]);
-                        else
-                            v[k][j] = f32x2_mul(v[k][j], pw[j]);
+                    for (int j = 0; j < H; ++j) v[k][j] = f32x2_mul(f32x2_mul(v[k][j], qq), w[j]);
+                    if (LN) {
+                        C::fetch(w, pb, l, nl);
+#pragma unroll
+                        for (int j = 0; j < H; ++j) v[k][j] = f32x2_add(v[k][j], w[j]);
                     }
                     if (grp + n_grp * k < n) C::store(a.o1, row0 + grp + n_grp * k, l, nl, d, v[k]);
                 }
@@ -538,15 +593,18 @@ __device__ __forceinline__ void group_add(uint64_t (&v)[H], uint64_t* buf, int g
             for (int j = 0; j < H; ++j) v[j] = f32x2_add(v[j], buf[(q * H + j) * nl + l]);
 }
 
-template <typename T, int VW, int NC, bool LN, int R>
+template <typename T, int VW, bool LN>
 __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const NormArgs a) {
     extern __shared__ __align__(128) uint8_t norm_smem[];
     __shared__ NormShared sh;
-    constexpr int E = 8 * NC, H = E / 2;
+    constexpr int E = kNormCols, H = E / 2, Q = kNormPart;   // pairs in all, and at a time
     using C = Cols<T, VW, E>;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int nt = (int)blockDim.x, nl = a.nl, d = a.d;
-    uint64_t* const gbuf = reinterpret_cast<uint64_t*>(norm_smem + (size_t)a.bufs * 4 * a.piece);
+    // parameters: pre_w, gate * post_w; then the row groups' sums on their way to group 0
+    ulonglong2* const pw = reinterpret_cast<ulonglong2*>(norm_smem + (size_t)a.bufs * 4 * a.piece);
+    ulonglong2* const gp = pw + H / 2 * nl;
+    uint64_t* const gbuf = reinterpret_cast<uint64_t*>(gp + H / 2 * nl);
     if (threadIdx.x == 0) {
         for (int i = 0; i < a.bufs; ++i) {
             mbar_init(&sh.full[i], 1);
@@ -568,11 +626,10 @@ __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const NormArgs a
     const float inv_d = 1.f / (float)d;
     const bool ragged = d != nl * E;
     const bool has_dr = a.in[0], has_f = a.in[1], has_dx = a.in[3];
-    const int row_bytes = d * (int)sizeof(T), first = grp * row_bytes, step = n_grp * row_bytes;
+    const int first = grp * d * (int)sizeof(T);
     const int items = a.groups * a.slices;
     RowSum rs = {&sh, 0, nl, warp, lane};
-    uint64_t pw[H];
-    C::param(pw, a.pre_w, 1.f, l, nl, d);
+    if (grp == 0) C::fill(pw, a.pre_w, nullptr, 1.f, l, nl, d);
     // sums over all of the CTA's rows: dx shat, dx
     uint64_t c_w[H], c_b[LN ? H : 1];
     pairs_zero(c_w);
@@ -585,14 +642,9 @@ __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const NormArgs a
         int g, r0, r1;
         item_rows(a, item, g, r0, r1);
         const float* gate = a.gate ? a.gate + (size_t)g * d : nullptr;
-        uint64_t gp[H];   // gate * post_w
-        {
-            uint64_t t[H];
-            C::param(t, gate, 1.f, l, nl, d);
-            C::param(gp, a.post_w, 1.f, l, nl, d);
-#pragma unroll
-            for (int j = 0; j < H; ++j) gp[j] = f32x2_mul(gp[j], t[j]);
-        }
+        __syncthreads();   // the item before has been worked through
+        if (grp == 0) C::fill(gp, a.post_w, gate, 1.f, l, nl, d);
+        __syncthreads();
         // sums over the item's rows: ds fhat, ds
         uint64_t i_w[H], i_b[LN ? H : 1];
         pairs_zero(i_w);
@@ -604,123 +656,163 @@ __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const NormArgs a
             const int n = r1 - row0 < a.rows ? r1 - row0 : a.rows;
             const uint8_t* buf = norm_smem + (size_t)b * 4 * a.piece +
                                  ((uint32_t)((size_t)row0 * d * sizeof(T)) & 15) + first;
-            // a group's rows past the buffer's n: zeros
-            uint64_t S[R][H], F[R][H], X[R][H];
-#pragma unroll
-            for (int k = 0; k < R; ++k) {
-                const bool in = grp + n_grp * k < n;
-                if (in && has_dx) {
-                    C::load(S[k], buf + 2 * a.piece + k * step, l, nl, d);
-                    C::load(X[k], buf + 3 * a.piece + k * step, l, nl, d);
-                } else {
-                    pairs_zero(S[k]);
-                    pairs_zero(X[k]);
-                }
-                if (in && has_f)
-                    C::load(F[k], buf + a.piece + k * step, l, nl, d);
+            // one row a group; a group past the buffer's n works on zeros
+            const bool in = grp < n;
+            const int row = row0 + grp;
+            // 8 columns at a time, read again in each pass: the sums over the rows take the
+            // registers
+            auto part = [&](uint64_t (&v)[Q], int i, int k) {
+                if (in)
+                    C::load8(v, buf + i * a.piece, k, l, nl, d);
                 else
-                    pairs_zero(F[k]);
-            }
+                    pairs_zero(v);
+            };
+            auto param = [&](uint64_t (&v)[Q], const ulonglong2* from, int k) {
+#pragma unroll
+                for (int j = 0; j < Q / 2; ++j) {
+                    const ulonglong2 x = from[(k * (Q / 2) + j) * nl + l];
+                    v[2 * j] = x.x;
+                    v[2 * j + 1] = x.y;
+                }
+            };
+            float ms = 0.f, mf = 0.f;
             if (LN) {
-                float t[2 * R];
+                float t[2] = {0.f, 0.f};
+                uint64_t x = 0, y = 0;
 #pragma unroll
-                for (int k = 0; k < R; ++k) {
-                    uint64_t x = S[k][0], y = F[k][0];
+                for (int k = 0; k < H / Q; ++k) {
+                    uint64_t v[Q];
+                    if (has_dx && a.pre == HCW_NORM_LAYER) {
+                        part(v, 2, k);
 #pragma unroll
-                    for (int j = 1; j < H; ++j) {
-                        x = f32x2_add(x, S[k][j]);
-                        y = f32x2_add(y, F[k][j]);
+                        for (int j = 0; j < Q; ++j) x = f32x2_add(x, v[j]);
                     }
-                    t[2 * k] = pair_sum(x);
-                    t[2 * k + 1] = pair_sum(y);
+                    if (has_f && a.post == HCW_NORM_LAYER) {
+                        part(v, 1, k);
+#pragma unroll
+                        for (int j = 0; j < Q; ++j) y = f32x2_add(y, v[j]);
+                    }
                 }
+                t[0] = pair_sum(x);
+                t[1] = pair_sum(y);
                 rs.sum(t);
+                ms = t[0] * inv_d;
+                mf = t[1] * inv_d;
+            }
+            // s or f, centred where its norm is a LayerNorm
+            auto centred = [&](uint64_t (&v)[Q], int i, int k, float m) {
+                part(v, i, k);
+                if (LN) C::centre8(v, m, ragged, k, l, nl, d);
+            };
+            // sums of s^2, e s, f^2, e  with e = dx pre_w
+            uint64_t ss = 0, es = 0, ff = 0, e1 = 0;
 #pragma unroll
-                for (int k = 0; k < R; ++k) {
-                    if (a.pre == HCW_NORM_LAYER) C::centre(S[k], t[2 * k] * inv_d, ragged, l, nl, d);
-                    if (a.post == HCW_NORM_LAYER)
-                        C::centre(F[k], t[2 * k + 1] * inv_d, ragged, l, nl, d);
+            for (int k = 0; k < H / Q; ++k) {
+                uint64_t v[Q], x[Q], w[Q];
+                if (has_dx) {
+                    centred(v, 2, k, ms);
+                    part(x, 3, k);
+                    param(w, pw, k);
+#pragma unroll
+                    for (int j = 0; j < Q; ++j) {
+                        const uint64_t e = f32x2_mul(x[j], w[j]);
+                        ss = f32x2_fma(v[j], v[j], ss);
+                        es = f32x2_fma(e, v[j], es);
+                        if (LN) e1 = f32x2_add(e1, e);
+                    }
+                }
+                if (has_f) {
+                    centred(v, 1, k, mf);
+#pragma unroll
+                    for (int j = 0; j < Q; ++j) ff = f32x2_fma(v[j], v[j], ff);
                 }
             }
-            // sums of s^2, e s, f^2, e  with e = dx pre_w (s and f centred)
-            float t[4 * R];
-#pragma unroll
-            for (int k = 0; k < R; ++k) {
-                uint64_t ss = 0, es = 0, ff = 0, e1 = 0;
-#pragma unroll
-                for (int j = 0; j < H; ++j) {
-                    const uint64_t e = f32x2_mul(X[k][j], pw[j]);
-                    ss = f32x2_fma(S[k][j], S[k][j], ss);
-                    es = f32x2_fma(e, S[k][j], es);
-                    ff = f32x2_fma(F[k][j], F[k][j], ff);
-                    if (LN) e1 = f32x2_add(e1, e);
-                }
-                t[4 * k] = pair_sum(ss);
-                t[4 * k + 1] = pair_sum(es);
-                t[4 * k + 2] = pair_sum(ff);
-                t[4 * k + 3] = LN ? pair_sum(e1) : 0.f;
-            }
+            float t[4] = {pair_sum(ss), pair_sum(es), pair_sum(ff), LN ? pair_sum(e1) : 0.f};
             rs.sum(t);
-            float u[2 * R], qf[R];   // sums of h fhat, h  with h = gate ds post_w
+            // (a group without a row: factors of 0, not of 1 / sqrt(0))
+            const float rstd = in && has_dx ? rsqrtf(t[0] * inv_d + a.eps) : 0.f;
+            const float m2 = t[1] * inv_d * rstd;   // mean(e shat)
+            const float m1 = LN && a.pre == HCW_NORM_LAYER ? t[3] * inv_d : 0.f;
+            const float qf =
+                !in ? 0.f : a.post != HCW_NORM_NONE ? rsqrtf(t[2] * inv_d + a.eps) : 1.f;
+            const uint64_t rr = both(rstd), nm2 = both(-m2), nm1 = both(-m1), qq = both(qf);
+            uint64_t ds[H], hf = 0, h1 = 0;   // sums of h fhat, h  with h = gate ds post_w
 #pragma unroll
-            for (int k = 0; k < R; ++k) {
-                const float rstd = has_dx ? rsqrtf(t[4 * k] * inv_d + a.eps) : 0.f;
-                const float m2 = t[4 * k + 1] * inv_d * rstd;   // mean(e shat)
-                const float m1 = LN && a.pre == HCW_NORM_LAYER ? t[4 * k + 3] * inv_d : 0.f;
-                qf[k] = a.post != HCW_NORM_NONE ? rsqrtf(t[4 * k + 2] * inv_d + a.eps) : 1.f;
-                uint64_t D[H];
-                if (has_dr && grp + n_grp * k < n)
-                    C::load(D, buf + k * step, l, nl, d);
+            for (int k = 0; k < H / Q; ++k) {
+                uint64_t v[Q], x[Q], w[Q];
+                if (has_dr)
+                    part(w, 0, k);
                 else
-                    pairs_zero(D);
-                const uint64_t rr = both(rstd), nm2 = both(-m2), nm1 = both(-m1), qq = both(qf[k]);
-                uint64_t hf = 0, h1 = 0;
+                    pairs_zero(w);
 #pragma unroll
-                for (int j = 0; j < H; ++j) {
-                    // ds, from here on in place of dx
-                    const uint64_t sh_ = f32x2_mul(S[k][j], rr);
-                    uint64_t e = f32x2_fma(sh_, nm2, f32x2_mul(X[k][j], pw[j]));
-                    if (LN) e = f32x2_add(e, nm1);
-                    c_w[j] = f32x2_fma(X[k][j], sh_, c_w[j]);
-                    if constexpr (LN) c_b[j] = f32x2_add(c_b[j], X[k][j]);
-                    X[k][j] = f32x2_fma(e, rr, D[j]);
-                    // fhat, in place of f; h is 0 past the row's end
-                    F[k][j] = f32x2_mul(F[k][j], qq);
-                    const uint64_t h = f32x2_mul(X[k][j], gp[j]);
-                    i_w[j] = f32x2_fma(X[k][j], F[k][j], i_w[j]);
-                    if constexpr (LN) i_b[j] = f32x2_add(i_b[j], X[k][j]);
-                    hf = f32x2_fma(h, F[k][j], hf);
-                    if (LN) h1 = f32x2_add(h1, h);
+                for (int j = 0; j < Q; ++j) ds[k * Q + j] = w[j];
+                if (has_dx) {
+                    centred(v, 2, k, ms);
+                    part(x, 3, k);
+                    param(w, pw, k);
+#pragma unroll
+                    for (int j = 0; j < Q; ++j) {
+                        const uint64_t h = f32x2_mul(v[j], rr);
+                        uint64_t e = f32x2_fma(h, nm2, f32x2_mul(x[j], w[j]));
+                        if (LN) e = f32x2_add(e, nm1);
+                        c_w[k * Q + j] = f32x2_fma(x[j], h, c_w[k * Q + j]);
+                        if constexpr (LN) c_b[k * Q + j] = f32x2_add(c_b[k * Q + j], x[j]);
+                        ds[k * Q + j] = f32x2_fma(e, rr, ds[k * Q + j]);
+                    }
                 }
-                u[2 * k] = pair_sum(hf);
-                u[2 * k + 1] = LN ? pair_sum(h1) : 0.f;
+                if (has_f) {
+                    centred(v, 1, k, mf);
+                    param(w, gp, k);
+#pragma unroll
+                    for (int j = 0; j < Q; ++j) {
+                        const uint64_t g_ = ds[k * Q + j], fh = f32x2_mul(v[j], qq);
+                        const uint64_t h = f32x2_mul(g_, w[j]);   // 0 past the row's end
+                        i_w[k * Q + j] = f32x2_fma(g_, fh, i_w[k * Q + j]);
+                        if constexpr (LN) i_b[k * Q + j] = f32x2_add(i_b[k * Q + j], g_);
+                        hf = f32x2_fma(h, fh, hf);
+                        if (LN) h1 = f32x2_add(h1, h);
+                    }
+                }
+            }
+            if (a.o1) {
+                float m4 = 0.f, m3 = 0.f;
+                if (a.post != HCW_NORM_NONE) {
+                    if (LN) {
+                        float u[2] = {pair_sum(hf), pair_sum(h1)};
+                        rs.sum(u);
+                        m4 = u[0] * inv_d;
+                        m3 = a.post == HCW_NORM_LAYER ? u[1] * inv_d : 0.f;
+                    } else {
+                        float u[1] = {pair_sum(hf)};
+                        rs.sum(u);
+                        m4 = u[0] * inv_d;
+                    }
+                }
+                const uint64_t n4 = both(-m4 * qf), n3 = both(-m3);   // fhat m4 = f qf m4
+#pragma unroll
+                for (int k = 0; k < H / Q; ++k) {
+                    uint64_t v[Q], w[Q];
+                    centred(v, 1, k, mf);
+                    param(w, gp, k);
+#pragma unroll
+                    for (int j = 0; j < Q; ++j) {
+                        uint64_t o = f32x2_fma(v[j], n4, f32x2_mul(ds[k * Q + j], w[j]));
+                        if (LN) o = f32x2_add(o, n3);
+                        v[j] = f32x2_mul(o, qq);
+                    }
+                    if (in) C::store8(a.o1, row, k, l, nl, d, v);
+                }
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(&sh.empty[b]);   // the buffer has been read
-            if (a.o1) {
-                if (a.post != HCW_NORM_NONE) rs.sum(u);
-#pragma unroll
-                for (int k = 0; k < R; ++k) {
-                    const uint64_t m4 = both(a.post != HCW_NORM_NONE ? -u[2 * k] * inv_d : 0.f);
-                    const uint64_t m3 =
-                        both(LN && a.post == HCW_NORM_LAYER ? -u[2 * k + 1] * inv_d : 0.f);
-                    const uint64_t qq = both(qf[k]);
-#pragma unroll
-                    for (int j = 0; j < H; ++j) {
-                        uint64_t o = f32x2_fma(F[k][j], m4, f32x2_mul(X[k][j], gp[j]));
-                        if (LN) o = f32x2_add(o, m3);
-                        F[k][j] = f32x2_mul(o, qq);
-                    }
-                    if (grp + n_grp * k < n) C::store(a.o1, row0 + grp + n_grp * k, l, nl, d, F[k]);
-                }
-            }
             if (a.o0) {
                 const uint64_t alpha = both(a.alpha);
 #pragma unroll
-                for (int k = 0; k < R; ++k) {
+                for (int k = 0; k < H / Q; ++k) {
+                    uint64_t v[Q];
 #pragma unroll
-                    for (int j = 0; j < H; ++j) X[k][j] = f32x2_mul(X[k][j], alpha);
-                    if (grp + n_grp * k < n) C::store(a.o0, row0 + grp + n_grp * k, l, nl, d, X[k]);
+                    for (int j = 0; j < Q; ++j) v[j] = f32x2_mul(ds[k * Q + j], alpha);
+                    if (in) C::store8(a.o0, row, k, l, nl, d, v);
                 }
             }
             if (threadIdx.x == 0) fed = feed.fetch<T, 4>(a, norm_smem, &sh);
@@ -832,7 +924,7 @@ __global__ void __launch_bounds__(1024) norm_reduce_kernel(const NormReduceArgs 
 
 // Threads a row and a CTA, buffers and items for a call.
 struct NormPlan {
-    int nl, threads, nc, grid, slices, groups;
+    int nl, threads, grid, slices, groups;
     int rows, bufs, piece;
     size_t smem;
 };
@@ -850,48 +942,64 @@ int norm_groups(int T, int rows_per_gate) {
 }
 
 // rows a row group works on at once
-constexpr int norm_rows(bool bwd, int nc) { return bwd ? (nc == 1 ? 2 : 1) : (nc == 1 ? 4 : 2); }
+constexpr int norm_rows(bool bwd) { return bwd ? 1 : 2; }
 
-// elem: bytes of an element (grid, slices and groups do not depend on it).
-NormPlan norm_plan(bool bwd, int T, int d, int elem, int rows_per_gate) {
+// elem: bytes of an element, ln: a LayerNorm (grid, slices and groups depend on neither).
+NormPlan norm_plan(bool bwd, bool ln, int T, int d, int elem, int rows_per_gate) {
     NormPlan p;
-    p.nc = d <= 4096 ? 1 : 2;
-    const int E = 8 * p.nc;
+    const int sms = norm_sms(), E = kNormCols;
     // a power of two up to a warp, whole warps above
     p.nl = 8;
     while (p.nl < 32 && p.nl * E < d) p.nl *= 2;
     if (p.nl * E < d) p.nl = (d + 32 * E - 1) / (32 * E) * 32;
-    // row groups of 256 threads in all, as many CTAs an SM as make 512
-    const int n_grp = p.nl < 256 ? 256 / p.nl : 1, n_in = bwd ? 4 : 2;
+    // one CTA an SM, row groups of 512 threads in all; fewer where the rows do not go round,
+    // but whole warps
+    int n_grp = p.nl < kNormThreads ? kNormThreads / p.nl : 1;
+    const int least = p.nl < 32 ? 32 / p.nl : 1, share = (T + sms - 1) / sms;
+    while (n_grp / 2 >= least && n_grp / 2 >= share) n_grp /= 2;
     p.threads = n_grp * p.nl;
-    const int per_sm = 512 / p.threads > 0 ? 512 / p.threads : 1;
-    int r = norm_rows(bwd, p.nc);
-    const size_t sums = bwd ? (size_t)(n_grp - 1) * E * p.nl * sizeof(float) : 0;
-    const size_t room = kNormSmem / per_sm - 4096 - sums;
+    const int n_in = bwd ? 4 : 2;
+    int r = norm_rows(bwd);
+    const size_t vec = (size_t)E * p.nl * sizeof(float);
+    const size_t fixed = (bwd || !ln ? 2 : 4) * vec + (bwd ? (size_t)(n_grp - 1) * vec : 0);
+    const size_t room = kNormSmem - 4096 - fixed;
     auto piece = [&](int rows) { return (int)(((size_t)rows * d * elem + 32 + 127) / 128 * 128); };
+    // (a buffer of one row a group where two do not fit: the kernel's second row is then
+    // past the buffer's rows)
+    while (r > 1 && 2 * (size_t)n_in * piece(n_grp * r) > room) r /= 2;
     p.rows = n_grp * r;
     p.piece = piece(p.rows);
     p.bufs = (int)(room / ((size_t)n_in * p.piece));
     if (p.bufs > 4) p.bufs = 4;
     if (p.bufs < 1) p.bufs = 1;
-    p.smem = (size_t)p.bufs * n_in * p.piece + sums;
+    p.smem = (size_t)p.bufs * n_in * p.piece + fixed;
     p.groups = norm_groups(T, rows_per_gate);
     const int rows = rows_per_gate > 0 && rows_per_gate < T ? rows_per_gate : T;
-    const int most = norm_sms() * per_sm;
-    // enough runs of rows for every CTA, each with a row for every row group
-    p.slices = p.groups > 0 ? (most + p.groups - 1) / p.groups : 1;
-    const int runs = (rows + n_grp - 1) / n_grp;
-    if (p.slices > runs) p.slices = runs;
-    if (p.slices < 1) p.slices = 1;
+    const int most = sms;
+    // runs of rows of a group: as many as make the busiest CTA's work least, in row groups'
+    // steps and 4 steps a run
+    p.slices = 1;
+    if (p.groups > 0 && p.groups < 4 * most) {
+        long long best = -1;
+        const int runs = (rows + n_grp - 1) / n_grp;
+        for (int k = 1; k <= runs && (long long)k * p.groups <= 8ll * most; ++k) {
+            const long long per = ((long long)p.groups * k + most - 1) / most;
+            const long long len = ((rows + k - 1) / k + n_grp - 1) / n_grp;
+            if (best < 0 || per * (len + 4) < best) {
+                best = per * (len + 4);
+                p.slices = k;
+            }
+        }
+    }
     const long long items = (long long)p.groups * p.slices;
     p.grid = (int)(items < most ? items : most);
     return p;
 }
 
-template <typename T, int VW, int NC, bool LN>
+template <typename T, int VW, bool LN>
 cudaError_t launch_norm(bool bwd, const NormPlan& p, const NormArgs& a, cudaStream_t st) {
-    auto kern = bwd ? norm_bwd_kernel<T, VW, NC, LN, norm_rows(true, NC)>
-                    : norm_fwd_kernel<T, VW, NC, LN, norm_rows(false, NC)>;
+    auto kern = bwd ? norm_bwd_kernel<T, VW, LN>
+                    : norm_fwd_kernel<T, VW, LN, norm_rows(false)>;
     static std::once_flag once[64][2];
     static cudaError_t set_err[64][2];
     int dev = 0;
@@ -908,12 +1016,8 @@ cudaError_t launch_norm(bool bwd, const NormPlan& p, const NormArgs& a, cudaStre
 
 template <typename T, int VW>
 cudaError_t launch_norm_vw(bool bwd, const NormPlan& p, const NormArgs& a, cudaStream_t st) {
-    const bool ln = a.post == HCW_NORM_LAYER || a.pre == HCW_NORM_LAYER;
-    if (p.nc == 1)
-        return ln ? launch_norm<T, VW, 1, true>(bwd, p, a, st)
-                  : launch_norm<T, VW, 1, false>(bwd, p, a, st);
-    return ln ? launch_norm<T, VW, 2, true>(bwd, p, a, st)
-              : launch_norm<T, VW, 2, false>(bwd, p, a, st);
+    const bool ln = a.ln;
+    return ln ? launch_norm<T, VW, true>(bwd, p, a, st) : launch_norm<T, VW, false>(bwd, p, a, st);
 }
 
 // The widest access every row's start allows.
@@ -966,6 +1070,7 @@ int norm_check(int T, int d, int dtype, int post, int pre, int rows_per_gate, fl
 }
 
 void norm_geometry(NormArgs& a, const NormPlan& p) {
+    a.ln = a.post == HCW_NORM_LAYER || a.pre == HCW_NORM_LAYER;
     a.nl = p.nl;
     a.rows = p.rows;
     a.bufs = p.bufs;
@@ -1008,7 +1113,8 @@ int hcw_residual_norm_fwd(const void* r, const void* f, const float* gate, int r
     if (x_out && pre == HCW_NORM_NONE) return HCW_ERR_INVALID_ARG;
     if (T == 0) return HCW_OK;
     if ((!r && !f) || (!r_out && !x_out)) return HCW_ERR_INVALID_ARG;
-    const NormPlan p = norm_plan(false, T, d, dtype == HCW_F32 ? 4 : 2, rows_per_gate);
+    const NormPlan p = norm_plan(false, post == HCW_NORM_LAYER || pre == HCW_NORM_LAYER, T, d,
+                                 dtype == HCW_F32 ? 4 : 2, rows_per_gate);
     NormArgs a = {};
     a.in[0] = r;
     a.in[1] = f;
@@ -1034,7 +1140,7 @@ int hcw_residual_norm_fwd(const void* r, const void* f, const float* gate, int r
 
 size_t hcw_residual_norm_bwd_workspace_bytes(int T, int d, int rows_per_gate) {
     if (T < 1 || d < 1 || d > kNormMaxD || rows_per_gate < 0) return 0;
-    return norm_ws(norm_plan(true, T, d, 2, rows_per_gate), d).bytes;
+    return norm_ws(norm_plan(true, false, T, d, 2, rows_per_gate), d).bytes;
 }
 
 int hcw_residual_norm_bwd(const void* dr_out, const void* dx_out, const void* s, const void* f,
@@ -1066,7 +1172,7 @@ int hcw_residual_norm_bwd(const void* dr_out, const void* dx_out, const void* s,
                   ((dpre_w || dpre_b) && !dx_out) || (branch && !f)))
         return HCW_ERR_INVALID_ARG;
     const cudaStream_t st = (cudaStream_t)stream;
-    NormPlan p = norm_plan(true, T, d, dtype == HCW_F32 ? 4 : 2, rows_per_gate);
+    NormPlan p = norm_plan(true, false, T, d, dtype == HCW_F32 ? 4 : 2, rows_per_gate);
     NormWs w = {};
     const bool ws_needed = T > 0 && (params || (dgate && p.slices > 1));
     if (ws_needed) {
