@@ -44,8 +44,11 @@ constexpr int kNormPar = 4;         // parameter sums of a CTA: post_w, post_b, 
 constexpr int kNormRed = 8;         // values of one reduction round
 constexpr int kNormCols = 16;       // columns a thread, in parts of 8:
 constexpr int kNormPart = 4;        // pairs of a part
+// 16-byte pieces from a thread's parameters in shared memory to the next thread's: 80 bytes,
+// so that 8 neighbours' 16-byte accesses fall into different banks
+constexpr int kNormStride = 5;
 constexpr int kNormMaxBufs = 8;
-constexpr size_t kNormSmem = 232448;
+constexpr size_t kNormSmem = 232448 - 2048;   // dynamic, beside NormShared
 constexpr unsigned long long kNormTimeoutNs = 2000000000ull;
 
 struct NormArgs {
@@ -74,6 +77,7 @@ struct NormArgs {
 
 struct __align__(16) NormShared {
     float red[2][kNormThreads / 32][kNormRed];
+    float zero[4];
     uint64_t full[kNormMaxBufs], empty[kNormMaxBufs];
     int abort;
 };
@@ -171,171 +175,137 @@ struct NormFeed {
 // A thread's E columns of a row, as pairs: VW neighbours at a time, nl threads apart.
 template <typename T, int VW, int E>
 struct Cols {
-    static constexpr int H = E / 2;
-    __device__ __forceinline__ static int col(int l, int nl, int j) {
-        return VW * (l + nl * (j / VW)) + j % VW;
+    static constexpr int H = E / 2, N = E / VW;   // pairs, runs of neighbours
+    int l, nl, d;
+    uint32_t in;             // bit i: run i lies inside the row
+    const uint8_t* zero;     // 16 bytes of zeros in shared memory, read in place of the others
+    __device__ __forceinline__ Cols(int l_, int nl_, int d_, const void* zero_)
+        : l(l_), nl(nl_), d(d_), in(0), zero(static_cast<const uint8_t*>(zero_)) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) in |= (uint32_t)(col(VW * i) < d) << i;
+    }
+    __device__ __forceinline__ int col(int j) const { return VW * (l + nl * (j / VW)) + j % VW; }
+    __device__ __forceinline__ bool has(int run) const { return in >> run & 1; }
+    __device__ __forceinline__ const uint8_t* run(const uint8_t* row, int i) const {
+        return has(i) ? row + VW * (int)sizeof(T) * (l + nl * i) : zero;
     }
     // Part k (8 columns) from shared memory, zeros past the row's end.
-    __device__ __forceinline__ static void load8(uint64_t (&v)[kNormPart], const uint8_t* row, int k,
-                                                 int l, int nl, int d) {
-        const T* p = reinterpret_cast<const T*>(row);
+    __device__ __forceinline__ void load8(uint64_t (&v)[kNormPart], const uint8_t* row, int k) const {
         if (sizeof(T) == 2 && VW == 8) {
-            const int c = 8 * (l + nl * k);
-            const uint4 q = c < d ? *reinterpret_cast<const uint4*>(p + c) : make_uint4(0u, 0u, 0u, 0u);
+            const uint4 q = *reinterpret_cast<const uint4*>(run(row, k));
             v[0] = bf16x2_to_f32x2(q.x);
             v[1] = bf16x2_to_f32x2(q.y);
             v[2] = bf16x2_to_f32x2(q.z);
             v[3] = bf16x2_to_f32x2(q.w);
         } else if (sizeof(T) == 2 && VW == 2) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int c = 2 * (l + nl * (4 * k + j));
-                v[j] = bf16x2_to_f32x2(c < d ? *reinterpret_cast<const uint32_t*>(p + c) : 0u);
-            }
+            for (int j = 0; j < 4; ++j)
+                v[j] = bf16x2_to_f32x2(*reinterpret_cast<const uint32_t*>(run(row, 4 * k + j)));
         } else if (sizeof(T) == 2) {
-            const unsigned short* h = reinterpret_cast<const unsigned short*>(p);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const int c0 = l + nl * (8 * k + 2 * j), c1 = c0 + nl;
-                v[j] = f32x2_pack(c0 < d ? __uint_as_float((uint32_t)h[c0] << 16) : 0.f,
-                                  c1 < d ? __uint_as_float((uint32_t)h[c1] << 16) : 0.f);
+                const uint32_t x = *reinterpret_cast<const unsigned short*>(run(row, 8 * k + 2 * j)),
+                               y = *reinterpret_cast<const unsigned short*>(run(row, 8 * k + 2 * j + 1));
+                v[j] = bf16x2_to_f32x2(x | y << 16);
             }
         } else if (VW == 4) {
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                const int c = 4 * (l + nl * (2 * k + j));
-                const float4 q = c < d ? *reinterpret_cast<const float4*>(p + c)
-                                       : make_float4(0.f, 0.f, 0.f, 0.f);
-                v[2 * j] = f32x2_pack(q.x, q.y);
-                v[2 * j + 1] = f32x2_pack(q.z, q.w);
+                const ulonglong2 q = *reinterpret_cast<const ulonglong2*>(run(row, 2 * k + j));
+                v[2 * j] = q.x;
+                v[2 * j + 1] = q.y;
             }
         } else {
-            const float* h = reinterpret_cast<const float*>(p);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int c0 = l + nl * (8 * k + 2 * j), c1 = c0 + nl;
-                v[j] = f32x2_pack(c0 < d ? h[c0] : 0.f, c1 < d ? h[c1] : 0.f);
-            }
+            for (int j = 0; j < 4; ++j)
+                v[j] = f32x2_pack(*reinterpret_cast<const float*>(run(row, 8 * k + 2 * j)),
+                                  *reinterpret_cast<const float*>(run(row, 8 * k + 2 * j + 1)));
         }
     }
-    __device__ __forceinline__ static void load(uint64_t (&v)[H], const uint8_t* row, int l, int nl,
-                                                int d) {
+    __device__ __forceinline__ void load(uint64_t (&v)[H], const uint8_t* row) const {
 #pragma unroll
         for (int k = 0; k < H / kNormPart; ++k) {
             uint64_t q[kNormPart];
-            load8(q, row, k, l, nl, d);
+            load8(q, row, k);
 #pragma unroll
             for (int j = 0; j < kNormPart; ++j) v[k * kNormPart + j] = q[j];
         }
     }
-    __device__ __forceinline__ static void store8(void* base, size_t row, int k, int l, int nl, int d,
-                                                  const uint64_t (&v)[kNormPart]) {
+    // Part k of row `row` of a global tensor.
+    __device__ __forceinline__ void store8(void* base, size_t row, int k,
+                                           const uint64_t (&v)[kNormPart]) const {
         T* p = static_cast<T*>(base) + row * (size_t)d;
         auto pack = [&](int i) {
             const float2 f = f32x2_unpack(v[i]);
             return pack_bf16x2(f.x, f.y);
         };
         if (sizeof(T) == 2 && VW == 8) {
-            const int c = 8 * (l + nl * k);
-            if (c < d)
-                *reinterpret_cast<uint4*>(p + c) = make_uint4(pack(0), pack(1), pack(2), pack(3));
+            if (has(k))
+                *reinterpret_cast<uint4*>(p + col(8 * k)) =
+                    make_uint4(pack(0), pack(1), pack(2), pack(3));
         } else if (sizeof(T) == 2 && VW == 2) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int c = 2 * (l + nl * (4 * k + j));
-                if (c < d) *reinterpret_cast<uint32_t*>(p + c) = pack(j);
-            }
+            for (int j = 0; j < 4; ++j)
+                if (has(4 * k + j)) *reinterpret_cast<uint32_t*>(p + col(8 * k + 2 * j)) = pack(j);
         } else if (VW == 4) {
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                const int c = 4 * (l + nl * (2 * k + j));
                 const float2 x = f32x2_unpack(v[2 * j]), y = f32x2_unpack(v[2 * j + 1]);
-                if (c < d) *reinterpret_cast<float4*>(p + c) = make_float4(x.x, x.y, y.x, y.y);
+                if (has(2 * k + j))
+                    *reinterpret_cast<float4*>(p + col(8 * k + 4 * j)) = make_float4(x.x, x.y, y.x, y.y);
             }
         } else {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const int c0 = l + nl * (8 * k + 2 * j), c1 = c0 + nl;
                 const float2 f = f32x2_unpack(v[j]);
+                const int i = 8 * k + 2 * j;
                 if (sizeof(T) == 2) {
                     __nv_bfloat16* h = reinterpret_cast<__nv_bfloat16*>(p);
-                    if (c0 < d) h[c0] = __float2bfloat16_rn(f.x);
-                    if (c1 < d) h[c1] = __float2bfloat16_rn(f.y);
+                    if (has(i)) h[col(i)] = __float2bfloat16_rn(f.x);
+                    if (has(i + 1)) h[col(i + 1)] = __float2bfloat16_rn(f.y);
                 } else {
                     float* h = reinterpret_cast<float*>(p);
-                    if (c0 < d) h[c0] = f.x;
-                    if (c1 < d) h[c1] = f.y;
+                    if (has(i)) h[col(i)] = f.x;
+                    if (has(i + 1)) h[col(i + 1)] = f.y;
                 }
             }
         }
     }
-    __device__ __forceinline__ static void store(void* base, size_t row, int l, int nl, int d,
-                                                 const uint64_t (&v)[H]) {
+    __device__ __forceinline__ void store(void* base, size_t row, const uint64_t (&v)[H]) const {
 #pragma unroll
         for (int k = 0; k < H / kNormPart; ++k) {
             uint64_t q[kNormPart];
 #pragma unroll
             for (int j = 0; j < kNormPart; ++j) q[j] = v[k * kNormPart + j];
-            store8(base, row, k, l, nl, d, q);
+            store8(base, row, k, q);
         }
     }
-    // a parameter vector (null: `none` everywhere; 0 past the row's end)
-    __device__ __forceinline__ static void param(uint64_t (&v)[H], const float* p, float none, int l,
-                                                 int nl, int d) {
-#pragma unroll
-        for (int k = 0; k < H; ++k) {
-            const int c0 = col(l, nl, 2 * k), c1 = col(l, nl, 2 * k + 1);
-            v[k] = f32x2_pack(c0 < d ? (p ? p[c0] : none) : 0.f, c1 < d ? (p ? p[c1] : none) : 0.f);
+    // The product of a parameter vector (null: `none`) and, if given, another into shared
+    // memory at this thread's place, zeros past the row's end.
+    __device__ __forceinline__ void fill(ulonglong2* to, const float* p, const float* q,
+                                         float none) const {
+        float* o = reinterpret_cast<float*>(to + l * kNormStride);
+        for (int j = 0; j < E; ++j) {
+            const int c = col(j);
+            o[j] = c < d ? (p ? p[c] : none) * (q ? q[c] : 1.f) : 0.f;
         }
     }
-    // the product of two parameter vectors (or one) into shared memory, as `fetch` reads it
-    __device__ __forceinline__ static void fill(ulonglong2* to, const float* p, const float* q,
-                                                float none, int l, int nl, int d) {
-        uint64_t v[H];
-        param(v, p, none, l, nl, d);
-        if (q) {
-            uint64_t w[H];
-            param(w, q, 1.f, l, nl, d);
+    // part k of such a vector
+    __device__ __forceinline__ void fetch8(uint64_t (&v)[kNormPart], const ulonglong2* from,
+                                           int k) const {
 #pragma unroll
-            for (int k = 0; k < H; ++k) v[k] = f32x2_mul(v[k], w[k]);
-        }
-#pragma unroll
-        for (int k = 0; k < H / 2; ++k) to[k * nl + l] = make_ulonglong2(v[2 * k], v[2 * k + 1]);
-    }
-    __device__ __forceinline__ static void fetch(uint64_t (&v)[H], const ulonglong2* from, int l,
-                                                 int nl) {
-#pragma unroll
-        for (int k = 0; k < H / 2; ++k) {
-            const ulonglong2 x = from[k * nl + l];
-            v[2 * k] = x.x;
-            v[2 * k + 1] = x.y;
+        for (int j = 0; j < kNormPart / 2; ++j) {
+            const ulonglong2 x = from[l * kNormStride + k * (kNormPart / 2) + j];
+            v[2 * j] = x.x;
+            v[2 * j + 1] = x.y;
         }
     }
-    // part k of v - m, zero past the row's end (`ragged`: the row ends inside the threads'
-    // columns)
-    __device__ __forceinline__ static void centre8(uint64_t (&v)[kNormPart], float m, bool ragged,
-                                                   int k, int l, int nl, int d) {
-        const uint64_t mm = f32x2_pack(-m, -m);
+    // part k of v - m (past the row's end v stays 0)
+    __device__ __forceinline__ void centre8(uint64_t (&v)[kNormPart], float m, int k) const {
 #pragma unroll
-        for (int j = 0; j < kNormPart; ++j) v[j] = f32x2_add(v[j], mm);
-        if (ragged)
-#pragma unroll
-            for (int j = 0; j < kNormPart; ++j) {
-                const float2 f = f32x2_unpack(v[j]);
-                v[j] = f32x2_pack(col(l, nl, 8 * k + 2 * j) < d ? f.x : 0.f,
-                                  col(l, nl, 8 * k + 2 * j + 1) < d ? f.y : 0.f);
-            }
-    }
-    __device__ __forceinline__ static void centre(uint64_t (&v)[H], float m, bool ragged, int l,
-                                                  int nl, int d) {
-#pragma unroll
-        for (int k = 0; k < H / kNormPart; ++k) {
-            uint64_t q[kNormPart];
-#pragma unroll
-            for (int j = 0; j < kNormPart; ++j) q[j] = v[k * kNormPart + j];
-            centre8(q, m, ragged, k, l, nl, d);
-#pragma unroll
-            for (int j = 0; j < kNormPart; ++j) v[k * kNormPart + j] = q[j];
+        for (int j = 0; j < kNormPart; ++j) {
+            const int i = 8 * k + 2 * j;
+            v[j] = f32x2_add(v[j], f32x2_pack(has(i / VW) ? -m : 0.f, has((i + 1) / VW) ? -m : 0.f));
         }
     }
 };
@@ -354,7 +324,12 @@ __device__ __forceinline__ uint64_t both(float x) { return f32x2_pack(x, x); }
 // Sums of N <= 8 values over the nl threads of a row, on every one of them.
 struct RowSum {
     NormShared* sh;
-    int parity, nl, warp, lane;
+    int nl, warp, lane;
+    int parity, W, first;   // warps of the row and the first of them
+    __device__ __forceinline__ RowSum(NormShared* sh_, int nl_, int warp_, int lane_)
+        : sh(sh_), nl(nl_), warp(warp_), lane(lane_), parity(0), W(nl_ >> 5), first(0) {
+        if (W > 1) first = warp / W * W;
+    }
     template <int N>
     __device__ __forceinline__ void sum(float (&v)[N]) {
         if (nl < 32) {   // several rows in a warp
@@ -391,11 +366,10 @@ struct RowSum {
         // Between the row's warps.  The parity alternates from round to round: a round's
         // values are read before the round after the next overwrites them, a barrier of the
         // row's warps lies between.
-        const int W = nl >> 5, first = warp / W * W;
         float(*buf)[kNormRed] = sh->red[parity];
         parity ^= 1;
         if ((lane & (32 / M - 1)) == 0) buf[warp][lane / (32 / M)] = t[0];
-        asm volatile("bar.sync %0, %1;" ::"r"(1 + warp / W), "r"(nl) : "memory");
+        asm volatile("bar.sync %0, %1;" ::"r"(1 + first), "r"(nl) : "memory");
         // lane l adds value l % M of every (32 / M)-th warp
         float x = 0.f;
         for (int w = lane / M; w < W; w += 32 / M) x += buf[first + w][lane % M];
@@ -412,8 +386,7 @@ template <typename T, int VW, bool LN, int R>
 __global__ void __launch_bounds__(kNormThreads) norm_fwd_kernel(const NormArgs a) {
     extern __shared__ __align__(128) uint8_t norm_smem[];
     __shared__ NormShared sh;
-    constexpr int E = kNormCols, H = E / 2;
-    using C = Cols<T, VW, E>;
+    constexpr int E = kNormCols, H = E / 2, Q = kNormPart;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int nt = (int)blockDim.x, nl = a.nl, d = a.d;
     if (threadIdx.x == 0) {
@@ -422,6 +395,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_fwd_kernel(const NormArgs a
             mbar_init(&sh.empty[i], nt >> 5);
         }
         sh.abort = 0;
+        sh.zero[0] = sh.zero[1] = sh.zero[2] = sh.zero[3] = 0.f;
         fence_mbar_init();
     }
     __syncthreads();
@@ -433,20 +407,21 @@ __global__ void __launch_bounds__(kNormThreads) norm_fwd_kernel(const NormArgs a
         feed.start(a);
         for (int i = 0; i < a.bufs; ++i) fed = fed && feed.fetch<T, 2>(a, norm_smem, &sh);
     }
-    const int l = (int)threadIdx.x % nl, grp = (int)threadIdx.x / nl, n_grp = nt / nl;
+    const int grp = (int)threadIdx.x / nl, n_grp = nt / nl;
     const float inv_d = 1.f / (float)d;
-    const bool ragged = d != nl * E;
     const bool has_r = a.in[0], has_f = a.in[1];
-    const int row_bytes = d * (int)sizeof(T), first = grp * row_bytes, step = n_grp * row_bytes;
+    const int first = grp * d * (int)sizeof(T), step = n_grp * d * (int)sizeof(T);
     const int items = a.groups * a.slices;
-    RowSum rs = {&sh, 0, nl, warp, lane};
+    RowSum rs(&sh, nl, warp, lane);
+    const Cols<T, VW, E> C((int)threadIdx.x % nl, nl, d, sh.zero);
     const uint64_t alpha = both(a.alpha);
     // parameters: pre_w, gate * post_w, pre_b, gate * post_b
     ulonglong2* const pw = reinterpret_cast<ulonglong2*>(norm_smem + (size_t)a.bufs * 2 * a.piece);
-    ulonglong2 *const gw = pw + H / 2 * nl, *const pb = gw + H / 2 * nl, *const gb = pb + H / 2 * nl;
+    ulonglong2 *const gw = pw + kNormStride * nl, *const pb = gw + kNormStride * nl,
+                     *const gb = pb + kNormStride * nl;
     if (grp == 0) {
-        C::fill(pw, a.pre_w, nullptr, 1.f, l, nl, d);
-        if (LN) C::fill(pb, a.pre_b, nullptr, 0.f, l, nl, d);
+        C.fill(pw, a.pre_w, nullptr, 1.f);
+        if (LN) C.fill(pb, a.pre_b, nullptr, 0.f);
     }
     int b = 0;
     uint32_t round = 0;
@@ -457,8 +432,8 @@ __global__ void __launch_bounds__(kNormThreads) norm_fwd_kernel(const NormArgs a
         const float* gate = a.gate ? a.gate + (size_t)g * d : nullptr;
         __syncthreads();   // the item before has been worked through
         if (grp == 0) {
-            C::fill(gw, a.post_w, gate, 1.f, l, nl, d);
-            if (LN) C::fill(gb, a.post_b, gate, 0.f, l, nl, d);
+            C.fill(gw, a.post_w, gate, 1.f);
+            if (LN) C.fill(gb, a.post_b, gate, 0.f);
         }
         __syncthreads();
         for (int row0 = r0; row0 < r1 && ok; row0 += a.rows) {
@@ -472,97 +447,95 @@ __global__ void __launch_bounds__(kNormThreads) norm_fwd_kernel(const NormArgs a
                                  ((uint32_t)((size_t)row0 * d * sizeof(T)) & 15) + first;
             uint64_t v[R][H];
             float q[R];
+            // mean out of v (a LayerNorm), then 1 / sqrt(mean square + eps) into q
+            auto statistics = [&](bool layer) {
+                if (LN && layer) {
 #pragma unroll
-            for (int k = 0; k < R; ++k) {
-                q[k] = 1.f;
-                if (has_f)
-                    C::load(v[k], buf + a.piece + k * step, l, nl, d);
-                else
-                    pairs_zero(v[k]);
-            }
-            if (has_f && a.post != HCW_NORM_NONE) {
-                if (LN && a.post == HCW_NORM_LAYER) {
+                    for (int r = 0; r < R; ++r) {
+                        uint64_t t = v[r][0];
 #pragma unroll
-                    for (int k = 0; k < R; ++k) {
-                        uint64_t t = v[k][0];
-#pragma unroll
-                        for (int j = 1; j < H; ++j) t = f32x2_add(t, v[k][j]);
-                        q[k] = pair_sum(t);
+                        for (int j = 1; j < H; ++j) t = f32x2_add(t, v[r][j]);
+                        q[r] = pair_sum(t);
                     }
                     rs.sum(q);
 #pragma unroll
-                    for (int k = 0; k < R; ++k) C::centre(v[k], q[k] * inv_d, ragged, l, nl, d);
+                    for (int r = 0; r < R; ++r)
+#pragma unroll
+                        for (int k = 0; k < H / Q; ++k) {
+                            uint64_t x[Q];
+#pragma unroll
+                            for (int j = 0; j < Q; ++j) x[j] = v[r][k * Q + j];
+                            C.centre8(x, q[r] * inv_d, k);
+#pragma unroll
+                            for (int j = 0; j < Q; ++j) v[r][k * Q + j] = x[j];
+                        }
                 }
 #pragma unroll
-                for (int k = 0; k < R; ++k) {
+                for (int r = 0; r < R; ++r) {
                     uint64_t t = 0;
 #pragma unroll
-                    for (int j = 0; j < H; ++j) t = f32x2_fma(v[k][j], v[k][j], t);
-                    q[k] = pair_sum(t);
+                    for (int j = 0; j < H; ++j) t = f32x2_fma(v[r][j], v[r][j], t);
+                    q[r] = pair_sum(t);
                 }
                 rs.sum(q);
 #pragma unroll
-                for (int k = 0; k < R; ++k) q[k] = rsqrtf(q[k] * inv_d + a.eps);
-            }
+                for (int r = 0; r < R; ++r) q[r] = rsqrtf(q[r] * inv_d + a.eps);
+            };
 #pragma unroll
-            for (int k = 0; k < R; ++k) {
-                uint64_t r[H];
-                if (has_r)
-                    C::load(r, buf + k * step, l, nl, d);
+            for (int r = 0; r < R; ++r) {
+                q[r] = 1.f;
+                if (has_f)
+                    C.load(v[r], buf + a.piece + r * step);
                 else
-                    pairs_zero(r);
-                const uint64_t qq = both(q[k]);
-                uint64_t w[H];
-                C::fetch(w, gw, l, nl);
+                    pairs_zero(v[r]);
+            }
+            if (has_f && a.post != HCW_NORM_NONE) statistics(a.post == HCW_NORM_LAYER);
 #pragma unroll
-                for (int j = 0; j < H; ++j)
-                    v[k][j] = f32x2_fma(f32x2_mul(v[k][j], qq), w[j], f32x2_mul(r[j], alpha));
-                if (LN) {
-                    C::fetch(w, gb, l, nl);
+            for (int k = 0; k < H / Q; ++k) {
+                uint64_t w[Q], wb[Q];
+                C.fetch8(w, gw, k);
+                if (LN) C.fetch8(wb, gb, k);
 #pragma unroll
-                    for (int j = 0; j < H; ++j) v[k][j] = f32x2_add(v[k][j], w[j]);
+                for (int r = 0; r < R; ++r) {
+                    uint64_t x[Q];
+                    if (has_r)
+                        C.load8(x, buf + r * step, k);
+                    else
+                        pairs_zero(x);
+                    const uint64_t qq = both(q[r]);
+#pragma unroll
+                    for (int j = 0; j < Q; ++j) {
+                        const int i = k * Q + j;
+                        uint64_t t = f32x2_mul(x[j], alpha);
+                        if (LN) t = f32x2_add(t, wb[j]);
+                        v[r][i] = f32x2_fma(f32x2_mul(v[r][i], qq), w[j], t);
+                    }
                 }
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(&sh.empty[b]);   // the buffer has been read
             if (a.o0)
 #pragma unroll
-                for (int k = 0; k < R; ++k)
-                    if (grp + n_grp * k < n) C::store(a.o0, row0 + grp + n_grp * k, l, nl, d, v[k]);
+                for (int r = 0; r < R; ++r)
+                    if (grp + n_grp * r < n) C.store(a.o0, row0 + grp + n_grp * r, v[r]);
             if (a.o1) {
-                if (LN && a.pre == HCW_NORM_LAYER) {
+                statistics(a.pre == HCW_NORM_LAYER);
 #pragma unroll
-                    for (int k = 0; k < R; ++k) {
-                        uint64_t t = v[k][0];
+                for (int k = 0; k < H / Q; ++k) {
+                    uint64_t w[Q], wb[Q];
+                    C.fetch8(w, pw, k);
+                    if (LN) C.fetch8(wb, pb, k);
 #pragma unroll
-                        for (int j = 1; j < H; ++j) t = f32x2_add(t, v[k][j]);
-                        q[k] = pair_sum(t);
+                    for (int r = 0; r < R; ++r) {
+                        const uint64_t qq = both(q[r]);
+                        uint64_t x[Q];
+#pragma unroll
+                        for (int j = 0; j < Q; ++j) {
+                            x[j] = f32x2_mul(v[r][k * Q + j], qq);
+                            x[j] = LN ? f32x2_fma(x[j], w[j], wb[j]) : f32x2_mul(x[j], w[j]);
+                        }
+                        if (grp + n_grp * r < n) C.store8(a.o1, row0 + grp + n_grp * r, k, x);
                     }
-                    rs.sum(q);
-#pragma unroll
-                    for (int k = 0; k < R; ++k) C::centre(v[k], q[k] * inv_d, ragged, l, nl, d);
-                }
-#pragma unroll
-                for (int k = 0; k < R; ++k) {
-                    uint64_t t = 0;
-#pragma unroll
-                    for (int j = 0; j < H; ++j) t = f32x2_fma(v[k][j], v[k][j], t);
-                    q[k] = pair_sum(t);
-                }
-                rs.sum(q);
-#pragma unroll
-                for (int k = 0; k < R; ++k) {
-                    const uint64_t qq = both(rsqrtf(q[k] * inv_d + a.eps));
-                    uint64_t w[H];
-                    C::fetch(w, pw, l, nl);
-#pragma unroll
-                    for (int j = 0; j < H; ++j) v[k][j] = f32x2_mul(f32x2_mul(v[k][j], qq), w[j]);
-                    if (LN) {
-                        C::fetch(w, pb, l, nl);
-#pragma unroll
-                        for (int j = 0; j < H; ++j) v[k][j] = f32x2_add(v[k][j], w[j]);
-                    }
-                    if (grp + n_grp * k < n) C::store(a.o1, row0 + grp + n_grp * k, l, nl, d, v[k]);
                 }
             }
             if (threadIdx.x == 0) fed = feed.fetch<T, 2>(a, norm_smem, &sh);
@@ -598,19 +571,19 @@ __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const NormArgs a
     extern __shared__ __align__(128) uint8_t norm_smem[];
     __shared__ NormShared sh;
     constexpr int E = kNormCols, H = E / 2, Q = kNormPart;   // pairs in all, and at a time
-    using C = Cols<T, VW, E>;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int nt = (int)blockDim.x, nl = a.nl, d = a.d;
     // parameters: pre_w, gate * post_w; then the row groups' sums on their way to group 0
     ulonglong2* const pw = reinterpret_cast<ulonglong2*>(norm_smem + (size_t)a.bufs * 4 * a.piece);
-    ulonglong2* const gp = pw + H / 2 * nl;
-    uint64_t* const gbuf = reinterpret_cast<uint64_t*>(gp + H / 2 * nl);
+    ulonglong2* const gp = pw + kNormStride * nl;
+    uint64_t* const gbuf = reinterpret_cast<uint64_t*>(gp + kNormStride * nl);
     if (threadIdx.x == 0) {
         for (int i = 0; i < a.bufs; ++i) {
             mbar_init(&sh.full[i], 1);
             mbar_init(&sh.empty[i], nt >> 5);
         }
         sh.abort = 0;
+        sh.zero[0] = sh.zero[1] = sh.zero[2] = sh.zero[3] = 0.f;
         fence_mbar_init();
     }
     __syncthreads();
@@ -624,12 +597,12 @@ __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const NormArgs a
     }
     const int l = (int)threadIdx.x % nl, grp = (int)threadIdx.x / nl, n_grp = nt / nl;
     const float inv_d = 1.f / (float)d;
-    const bool ragged = d != nl * E;
     const bool has_dr = a.in[0], has_f = a.in[1], has_dx = a.in[3];
     const int first = grp * d * (int)sizeof(T);
     const int items = a.groups * a.slices;
-    RowSum rs = {&sh, 0, nl, warp, lane};
-    if (grp == 0) C::fill(pw, a.pre_w, nullptr, 1.f, l, nl, d);
+    RowSum rs(&sh, nl, warp, lane);
+    const Cols<T, VW, E> C(l, nl, d, sh.zero);
+    if (grp == 0) C.fill(pw, a.pre_w, nullptr, 1.f);
     // sums over all of the CTA's rows: dx shat, dx
     uint64_t c_w[H], c_b[LN ? H : 1];
     pairs_zero(c_w);
@@ -643,7 +616,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const NormArgs a
         item_rows(a, item, g, r0, r1);
         const float* gate = a.gate ? a.gate + (size_t)g * d : nullptr;
         __syncthreads();   // the item before has been worked through
-        if (grp == 0) C::fill(gp, a.post_w, gate, 1.f, l, nl, d);
+        if (grp == 0) C.fill(gp, a.post_w, gate, 1.f);
         __syncthreads();
         // sums over the item's rows: ds fhat, ds
         uint64_t i_w[H], i_b[LN ? H : 1];
@@ -656,163 +629,160 @@ __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const NormArgs a
             const int n = r1 - row0 < a.rows ? r1 - row0 : a.rows;
             const uint8_t* buf = norm_smem + (size_t)b * 4 * a.piece +
                                  ((uint32_t)((size_t)row0 * d * sizeof(T)) & 15) + first;
-            // one row a group; a group past the buffer's n works on zeros
+            // One row a group (a group past the buffer's n adds nothing), 8 columns at a time,
+            // read again in each pass: the sums over the rows take the registers.
             const bool in = grp < n;
             const int row = row0 + grp;
-            // 8 columns at a time, read again in each pass: the sums over the rows take the
-            // registers
-            auto part = [&](uint64_t (&v)[Q], int i, int k) {
-                if (in)
-                    C::load8(v, buf + i * a.piece, k, l, nl, d);
-                else
-                    pairs_zero(v);
-            };
-            auto param = [&](uint64_t (&v)[Q], const ulonglong2* from, int k) {
-#pragma unroll
-                for (int j = 0; j < Q / 2; ++j) {
-                    const ulonglong2 x = from[(k * (Q / 2) + j) * nl + l];
-                    v[2 * j] = x.x;
-                    v[2 * j + 1] = x.y;
-                }
-            };
+            const uint8_t *const dr_row = buf, *const f_row = buf + a.piece,
+                                *const s_row = buf + 2 * a.piece, *const x_row = buf + 3 * a.piece;
             float ms = 0.f, mf = 0.f;
             if (LN) {
-                float t[2] = {0.f, 0.f};
                 uint64_t x = 0, y = 0;
+                if (in) {
 #pragma unroll
-                for (int k = 0; k < H / Q; ++k) {
-                    uint64_t v[Q];
-                    if (has_dx && a.pre == HCW_NORM_LAYER) {
-                        part(v, 2, k);
+                    for (int k = 0; k < H / Q; ++k) {
+                        uint64_t v[Q];
+                        if (has_dx && a.pre == HCW_NORM_LAYER) {
+                            C.load8(v, s_row, k);
 #pragma unroll
-                        for (int j = 0; j < Q; ++j) x = f32x2_add(x, v[j]);
-                    }
-                    if (has_f && a.post == HCW_NORM_LAYER) {
-                        part(v, 1, k);
+                            for (int j = 0; j < Q; ++j) x = f32x2_add(x, v[j]);
+                        }
+                        if (has_f && a.post == HCW_NORM_LAYER) {
+                            C.load8(v, f_row, k);
 #pragma unroll
-                        for (int j = 0; j < Q; ++j) y = f32x2_add(y, v[j]);
+                            for (int j = 0; j < Q; ++j) y = f32x2_add(y, v[j]);
+                        }
                     }
                 }
-                t[0] = pair_sum(x);
-                t[1] = pair_sum(y);
+                float t[2] = {pair_sum(x), pair_sum(y)};
                 rs.sum(t);
                 ms = t[0] * inv_d;
                 mf = t[1] * inv_d;
             }
             // s or f, centred where its norm is a LayerNorm
-            auto centred = [&](uint64_t (&v)[Q], int i, int k, float m) {
-                part(v, i, k);
-                if (LN) C::centre8(v, m, ragged, k, l, nl, d);
+            auto centred = [&](uint64_t (&v)[Q], const uint8_t* at, int k, float m) {
+                C.load8(v, at, k);
+                if (LN) C.centre8(v, m, k);
             };
             // sums of s^2, e s, f^2, e  with e = dx pre_w
-            uint64_t ss = 0, es = 0, ff = 0, e1 = 0;
+            constexpr int NS = LN ? 4 : 3;
+            float t[NS];
+            {
+                uint64_t ss = 0, es = 0, ff = 0, e1 = 0;
+                if (in) {
 #pragma unroll
-            for (int k = 0; k < H / Q; ++k) {
-                uint64_t v[Q], x[Q], w[Q];
-                if (has_dx) {
-                    centred(v, 2, k, ms);
-                    part(x, 3, k);
-                    param(w, pw, k);
+                    for (int k = 0; k < H / Q; ++k) {
+                        uint64_t v[Q], x[Q], w[Q];
+                        if (has_dx) {
+                            centred(v, s_row, k, ms);
+                            C.load8(x, x_row, k);
+                            C.fetch8(w, pw, k);
 #pragma unroll
-                    for (int j = 0; j < Q; ++j) {
-                        const uint64_t e = f32x2_mul(x[j], w[j]);
-                        ss = f32x2_fma(v[j], v[j], ss);
-                        es = f32x2_fma(e, v[j], es);
-                        if (LN) e1 = f32x2_add(e1, e);
+                            for (int j = 0; j < Q; ++j) {
+                                const uint64_t e = f32x2_mul(x[j], w[j]);
+                                ss = f32x2_fma(v[j], v[j], ss);
+                                es = f32x2_fma(e, v[j], es);
+                                if (LN) e1 = f32x2_add(e1, e);
+                            }
+                        }
+                        if (has_f) {
+                            centred(v, f_row, k, mf);
+#pragma unroll
+                            for (int j = 0; j < Q; ++j) ff = f32x2_fma(v[j], v[j], ff);
+                        }
                     }
                 }
-                if (has_f) {
-                    centred(v, 1, k, mf);
-#pragma unroll
-                    for (int j = 0; j < Q; ++j) ff = f32x2_fma(v[j], v[j], ff);
-                }
+                t[0] = pair_sum(ss);
+                t[1] = pair_sum(es);
+                t[2] = pair_sum(ff);
+                if (LN) t[NS - 1] = pair_sum(e1);
             }
-            float t[4] = {pair_sum(ss), pair_sum(es), pair_sum(ff), LN ? pair_sum(e1) : 0.f};
             rs.sum(t);
-            // (a group without a row: factors of 0, not of 1 / sqrt(0))
-            const float rstd = in && has_dx ? rsqrtf(t[0] * inv_d + a.eps) : 0.f;
-            const float m2 = t[1] * inv_d * rstd;   // mean(e shat)
-            const float m1 = LN && a.pre == HCW_NORM_LAYER ? t[3] * inv_d : 0.f;
-            const float qf =
-                !in ? 0.f : a.post != HCW_NORM_NONE ? rsqrtf(t[2] * inv_d + a.eps) : 1.f;
-            const uint64_t rr = both(rstd), nm2 = both(-m2), nm1 = both(-m1), qq = both(qf);
+            const float rstd = has_dx ? rsqrtf(t[0] * inv_d + a.eps) : 0.f;
+            const float qf = a.post != HCW_NORM_NONE ? rsqrtf(t[2] * inv_d + a.eps) : 1.f;
+            const uint64_t qq = both(qf);
             uint64_t ds[H], hf = 0, h1 = 0;   // sums of h fhat, h  with h = gate ds post_w
+            if (in) {
+                const uint64_t rr = both(rstd);
+                const uint64_t nm2 = both(-t[1] * inv_d * rstd);   // mean(e shat)
+                const uint64_t nm1 =
+                    both(LN && a.pre == HCW_NORM_LAYER ? -t[NS - 1] * inv_d : 0.f);
 #pragma unroll
-            for (int k = 0; k < H / Q; ++k) {
-                uint64_t v[Q], x[Q], w[Q];
-                if (has_dr)
-                    part(w, 0, k);
-                else
-                    pairs_zero(w);
+                for (int k = 0; k < H / Q; ++k) {
+                    uint64_t v[Q], x[Q], w[Q], g_[Q];
+                    if (has_dr)
+                        C.load8(g_, dr_row, k);
+                    else
+                        pairs_zero(g_);
+                    if (has_dx) {
+                        centred(v, s_row, k, ms);
+                        C.load8(x, x_row, k);
+                        C.fetch8(w, pw, k);
 #pragma unroll
-                for (int j = 0; j < Q; ++j) ds[k * Q + j] = w[j];
-                if (has_dx) {
-                    centred(v, 2, k, ms);
-                    part(x, 3, k);
-                    param(w, pw, k);
-#pragma unroll
-                    for (int j = 0; j < Q; ++j) {
-                        const uint64_t h = f32x2_mul(v[j], rr);
-                        uint64_t e = f32x2_fma(h, nm2, f32x2_mul(x[j], w[j]));
-                        if (LN) e = f32x2_add(e, nm1);
-                        c_w[k * Q + j] = f32x2_fma(x[j], h, c_w[k * Q + j]);
-                        if constexpr (LN) c_b[k * Q + j] = f32x2_add(c_b[k * Q + j], x[j]);
-                        ds[k * Q + j] = f32x2_fma(e, rr, ds[k * Q + j]);
+                        for (int j = 0; j < Q; ++j) {
+                            const int i = k * Q + j;
+                            const uint64_t h = f32x2_mul(v[j], rr);
+                            uint64_t e = f32x2_fma(h, nm2, f32x2_mul(x[j], w[j]));
+                            if (LN) e = f32x2_add(e, nm1);
+                            c_w[i] = f32x2_fma(x[j], h, c_w[i]);
+                            if constexpr (LN) c_b[i] = f32x2_add(c_b[i], x[j]);
+                            g_[j] = f32x2_fma(e, rr, g_[j]);
+                        }
                     }
-                }
-                if (has_f) {
-                    centred(v, 1, k, mf);
-                    param(w, gp, k);
+                    if (has_f) {
+                        centred(v, f_row, k, mf);
+                        C.fetch8(w, gp, k);
 #pragma unroll
-                    for (int j = 0; j < Q; ++j) {
-                        const uint64_t g_ = ds[k * Q + j], fh = f32x2_mul(v[j], qq);
-                        const uint64_t h = f32x2_mul(g_, w[j]);   // 0 past the row's end
-                        i_w[k * Q + j] = f32x2_fma(g_, fh, i_w[k * Q + j]);
-                        if constexpr (LN) i_b[k * Q + j] = f32x2_add(i_b[k * Q + j], g_);
-                        hf = f32x2_fma(h, fh, hf);
-                        if (LN) h1 = f32x2_add(h1, h);
+                        for (int j = 0; j < Q; ++j) {
+                            const int i = k * Q + j;
+                            const uint64_t fh = f32x2_mul(v[j], qq);
+                            const uint64_t h = f32x2_mul(g_[j], w[j]);   // 0 past the row's end
+                            i_w[i] = f32x2_fma(g_[j], fh, i_w[i]);
+                            if constexpr (LN) i_b[i] = f32x2_add(i_b[i], g_[j]);
+                            hf = f32x2_fma(h, fh, hf);
+                            if (LN) h1 = f32x2_add(h1, h);
+                        }
                     }
+#pragma unroll
+                    for (int j = 0; j < Q; ++j) ds[k * Q + j] = g_[j];
                 }
             }
             if (a.o1) {
-                float m4 = 0.f, m3 = 0.f;
+                float u[LN ? 2 : 1] = {};
                 if (a.post != HCW_NORM_NONE) {
-                    if (LN) {
-                        float u[2] = {pair_sum(hf), pair_sum(h1)};
-                        rs.sum(u);
-                        m4 = u[0] * inv_d;
-                        m3 = a.post == HCW_NORM_LAYER ? u[1] * inv_d : 0.f;
-                    } else {
-                        float u[1] = {pair_sum(hf)};
-                        rs.sum(u);
-                        m4 = u[0] * inv_d;
-                    }
+                    u[0] = pair_sum(hf);
+                    if (LN) u[LN ? 1 : 0] = pair_sum(h1);
+                    rs.sum(u);
                 }
-                const uint64_t n4 = both(-m4 * qf), n3 = both(-m3);   // fhat m4 = f qf m4
+                if (in) {
+                    const uint64_t n4 = both(-u[0] * inv_d * qf);   // fhat mean(h fhat) = f qf mean
+                    const uint64_t n3 =
+                        both(LN && a.post == HCW_NORM_LAYER ? -u[LN ? 1 : 0] * inv_d : 0.f);
 #pragma unroll
-                for (int k = 0; k < H / Q; ++k) {
-                    uint64_t v[Q], w[Q];
-                    centred(v, 1, k, mf);
-                    param(w, gp, k);
+                    for (int k = 0; k < H / Q; ++k) {
+                        uint64_t v[Q], w[Q];
+                        centred(v, f_row, k, mf);
+                        C.fetch8(w, gp, k);
 #pragma unroll
-                    for (int j = 0; j < Q; ++j) {
-                        uint64_t o = f32x2_fma(v[j], n4, f32x2_mul(ds[k * Q + j], w[j]));
-                        if (LN) o = f32x2_add(o, n3);
-                        v[j] = f32x2_mul(o, qq);
+                        for (int j = 0; j < Q; ++j) {
+                            uint64_t o = f32x2_fma(v[j], n4, f32x2_mul(ds[k * Q + j], w[j]));
+                            if (LN) o = f32x2_add(o, n3);
+                            v[j] = f32x2_mul(o, qq);
+                        }
+                        C.store8(a.o1, row, k, v);
                     }
-                    if (in) C::store8(a.o1, row, k, l, nl, d, v);
                 }
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(&sh.empty[b]);   // the buffer has been read
-            if (a.o0) {
+            if (a.o0 && in) {
                 const uint64_t alpha = both(a.alpha);
 #pragma unroll
                 for (int k = 0; k < H / Q; ++k) {
                     uint64_t v[Q];
 #pragma unroll
                     for (int j = 0; j < Q; ++j) v[j] = f32x2_mul(ds[k * Q + j], alpha);
-                    if (in) C::store8(a.o0, row, k, l, nl, d, v);
+                    C.store8(a.o0, row, k, v);
                 }
             }
             if (threadIdx.x == 0) fed = feed.fetch<T, 4>(a, norm_smem, &sh);
@@ -830,7 +800,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const NormArgs a
                 const bool fresh = item == (int)blockIdx.x;
 #pragma unroll
                 for (int j = 0; j < E; ++j) {
-                    const int c = C::col(l, nl, j);
+                    const int c = C.col(j);
                     if (c >= d) continue;
                     const float2 w2 = f32x2_unpack(i_w[j / 2]);
                     const float w = j & 1 ? w2.y : w2.x;
@@ -859,7 +829,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const NormArgs a
         if (grp == 0)
 #pragma unroll
             for (int j = 0; j < E; ++j) {
-                const int c = C::col(l, nl, j);
+                const int c = C.col(j);
                 if (c >= d) continue;
                 const float2 w2 = f32x2_unpack(c_w[j / 2]);
                 crow[(size_t)2 * d + c] = j & 1 ? w2.y : w2.x;
@@ -924,6 +894,7 @@ __global__ void __launch_bounds__(1024) norm_reduce_kernel(const NormReduceArgs 
 
 // Threads a row and a CTA, buffers and items for a call.
 struct NormPlan {
+    bool ln;
     int nl, threads, grid, slices, groups;
     int rows, bufs, piece;
     size_t smem;
@@ -941,12 +912,13 @@ int norm_groups(int T, int rows_per_gate) {
     return rows_per_gate > 0 ? (int)(((long long)T + rows_per_gate - 1) / rows_per_gate) : 1;
 }
 
-// rows a row group works on at once
-constexpr int norm_rows(bool bwd) { return bwd ? 1 : 2; }
+// rows a row group works on at once in the forward (the backward: one)
+constexpr int kNormRows = 2;
 
 // elem: bytes of an element, ln: a LayerNorm (grid, slices and groups depend on neither).
 NormPlan norm_plan(bool bwd, bool ln, int T, int d, int elem, int rows_per_gate) {
     NormPlan p;
+    p.ln = ln;
     const int sms = norm_sms(), E = kNormCols;
     // a power of two up to a warp, whole warps above
     p.nl = 8;
@@ -959,14 +931,15 @@ NormPlan norm_plan(bool bwd, bool ln, int T, int d, int elem, int rows_per_gate)
     while (n_grp / 2 >= least && n_grp / 2 >= share) n_grp /= 2;
     p.threads = n_grp * p.nl;
     const int n_in = bwd ? 4 : 2;
-    int r = norm_rows(bwd);
-    const size_t vec = (size_t)E * p.nl * sizeof(float);
-    const size_t fixed = (bwd || !ln ? 2 : 4) * vec + (bwd ? (size_t)(n_grp - 1) * vec : 0);
-    const size_t room = kNormSmem - 4096 - fixed;
+    int r = bwd ? 1 : kNormRows;
+    const size_t vec = (size_t)kNormStride * 16 * p.nl;
+    const size_t fixed = (bwd || !ln ? 2 : 4) * vec +
+                         (bwd ? (size_t)(n_grp - 1) * E * p.nl * sizeof(float) : 0);
+    const size_t room = kNormSmem - fixed;
     auto piece = [&](int rows) { return (int)(((size_t)rows * d * elem + 32 + 127) / 128 * 128); };
     // (a buffer of one row a group where two do not fit: the kernel's second row is then
     // past the buffer's rows)
-    while (r > 1 && 2 * (size_t)n_in * piece(n_grp * r) > room) r /= 2;
+    while (r > 1 && (size_t)n_in * piece(n_grp * r) > room) r /= 2;
     p.rows = n_grp * r;
     p.piece = piece(p.rows);
     p.bufs = (int)(room / ((size_t)n_in * p.piece));
@@ -999,7 +972,7 @@ NormPlan norm_plan(bool bwd, bool ln, int T, int d, int elem, int rows_per_gate)
 template <typename T, int VW, bool LN>
 cudaError_t launch_norm(bool bwd, const NormPlan& p, const NormArgs& a, cudaStream_t st) {
     auto kern = bwd ? norm_bwd_kernel<T, VW, LN>
-                    : norm_fwd_kernel<T, VW, LN, norm_rows(false)>;
+                    : norm_fwd_kernel<T, VW, LN, kNormRows>;
     static std::once_flag once[64][2];
     static cudaError_t set_err[64][2];
     int dev = 0;
@@ -1008,7 +981,7 @@ cudaError_t launch_norm(bool bwd, const NormPlan& p, const NormArgs& a, cudaStre
     if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
     std::call_once(once[dev][bwd], [&] {
         set_err[dev][bwd] = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                 (int)(kNormSmem - 4096));
+                                                 (int)kNormSmem);
     });
     if (set_err[dev][bwd] != cudaSuccess) return set_err[dev][bwd];
     return launch_pdl(kern, dim3((unsigned)p.grid), dim3((unsigned)p.threads), p.smem, st, a);
@@ -1070,7 +1043,7 @@ int norm_check(int T, int d, int dtype, int post, int pre, int rows_per_gate, fl
 }
 
 void norm_geometry(NormArgs& a, const NormPlan& p) {
-    a.ln = a.post == HCW_NORM_LAYER || a.pre == HCW_NORM_LAYER;
+    a.ln = p.ln;
     a.nl = p.nl;
     a.rows = p.rows;
     a.bufs = p.bufs;
@@ -1172,7 +1145,8 @@ int hcw_residual_norm_bwd(const void* dr_out, const void* dx_out, const void* s,
                   ((dpre_w || dpre_b) && !dx_out) || (branch && !f)))
         return HCW_ERR_INVALID_ARG;
     const cudaStream_t st = (cudaStream_t)stream;
-    NormPlan p = norm_plan(true, false, T, d, dtype == HCW_F32 ? 4 : 2, rows_per_gate);
+    NormPlan p = norm_plan(true, post == HCW_NORM_LAYER || pre == HCW_NORM_LAYER, T, d,
+                           dtype == HCW_F32 ? 4 : 2, rows_per_gate);
     NormWs w = {};
     const bool ws_needed = T > 0 && (params || (dgate && p.slices > 1));
     if (ws_needed) {
