@@ -99,6 +99,7 @@ struct NormFeed {
     int item, row, r1;     // next rows to fetch
     int b;                 // buffer they go to
     uint32_t round;        // how often the ring has been gone through
+    size_t at;             // where they start in a tensor, in elements
     __device__ __forceinline__ void start(const NormArgs& a) {
         item = blockIdx.x;
         b = 0;
@@ -109,6 +110,7 @@ struct NormFeed {
             item_rows(a, item, g, row, r1);
         }
         settle(a);
+        at = (size_t)row * a.d;
     }
     // on to an item with rows left
     __device__ __forceinline__ void settle(const NormArgs& a) {
@@ -129,8 +131,9 @@ struct NormFeed {
         // the 16-byte pieces the rows touch, those wholly inside the tensor in one copy and
         // the last few bytes of the tensor element by element
         const size_t end = (size_t)a.T * a.d * sizeof(T);
-        const size_t from = (size_t)row * a.d * sizeof(T) & ~(size_t)15;
-        size_t to = ((size_t)(row + n) * a.d * sizeof(T) + 15) & ~(size_t)15;
+        const size_t from = at * sizeof(T) & ~(size_t)15;
+        at += (size_t)n * a.d;
+        size_t to = (at * sizeof(T) + 15) & ~(size_t)15;
         const bool cut = to > end;
         if (cut) to = end & ~(size_t)15;
         const uint32_t bytes = to > from ? (uint32_t)(to - from) : 0;
@@ -141,9 +144,9 @@ struct NormFeed {
             if (!a.in[i]) continue;
             total += bytes;
             if (cut)
-                for (size_t at = from + bytes; at < end; at += sizeof(T))
-                    *reinterpret_cast<T*>(dst + (size_t)i * a.piece + (at - from)) =
-                        *reinterpret_cast<const T*>(static_cast<const uint8_t*>(a.in[i]) + at);
+                for (size_t q = from + bytes; q < end; q += sizeof(T))
+                    *reinterpret_cast<T*>(dst + (size_t)i * a.piece + (q - from)) =
+                        *reinterpret_cast<const T*>(static_cast<const uint8_t*>(a.in[i]) + q);
         }
         mbar_arrive_expect_tx(&sh->full[b], total);
         if (bytes)
@@ -157,7 +160,10 @@ struct NormFeed {
                         "r"(smem_u32(&sh->full[b]))
                         : "memory");
         row += n;
-        settle(a);
+        if (row >= r1) {
+            settle(a);
+            at = (size_t)row * a.d;
+        }
         if (++b == a.bufs) {
             b = 0;
             ++round;
@@ -172,27 +178,47 @@ struct NormFeed {
     }
 };
 
+// Shared memory by its 32-bit address.
+__device__ __forceinline__ uint4 lds128(uint32_t at) {
+    uint4 q;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w) : "r"(at));
+    return q;
+}
+__device__ __forceinline__ uint32_t lds32(uint32_t at) {
+    uint32_t q;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(q) : "r"(at));
+    return q;
+}
+__device__ __forceinline__ uint32_t lds16(uint32_t at) {
+    unsigned short q;
+    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(q) : "r"(at));
+    return q;
+}
+
 // A thread's E columns of a row, as pairs: VW neighbours at a time, nl threads apart.
 template <typename T, int VW, int E>
 struct Cols {
     static constexpr int H = E / 2, N = E / VW;   // pairs, runs of neighbours
+    static constexpr int B = VW * (int)sizeof(T);   // bytes of a run
     int l, nl, d;
     uint32_t in;             // bit i: run i lies inside the row
-    const uint8_t* zero;     // 16 bytes of zeros in shared memory, read in place of the others
+    uint32_t zero;           // 16 bytes of zeros in shared memory, read in place of the others
+    int at0, gap;            // bytes from a row's start to run 0, and from run to run
     __device__ __forceinline__ Cols(int l_, int nl_, int d_, const void* zero_)
-        : l(l_), nl(nl_), d(d_), in(0), zero(static_cast<const uint8_t*>(zero_)) {
+        : l(l_), nl(nl_), d(d_), in(0), zero(smem_u32(zero_)), at0(B * l_), gap(B * nl_) {
 #pragma unroll
         for (int i = 0; i < N; ++i) in |= (uint32_t)(col(VW * i) < d) << i;
     }
     __device__ __forceinline__ int col(int j) const { return VW * (l + nl * (j / VW)) + j % VW; }
     __device__ __forceinline__ bool has(int run) const { return in >> run & 1; }
-    __device__ __forceinline__ const uint8_t* run(const uint8_t* row, int i) const {
-        return has(i) ? row + VW * (int)sizeof(T) * (l + nl * i) : zero;
+    __device__ __forceinline__ uint32_t run(uint32_t row, int i) const {
+        return has(i) ? row + at0 + i * gap : zero;
     }
-    // Part k (8 columns) from shared memory, zeros past the row's end.
-    __device__ __forceinline__ void load8(uint64_t (&v)[kNormPart], const uint8_t* row, int k) const {
+    // Part k (8 columns) of a row in shared memory, zeros past its end.
+    __device__ __forceinline__ void load8(uint64_t (&v)[kNormPart], uint32_t row, int k) const {
         if (sizeof(T) == 2 && VW == 8) {
-            const uint4 q = *reinterpret_cast<const uint4*>(run(row, k));
+            const uint4 q = lds128(run(row, k));
             v[0] = bf16x2_to_f32x2(q.x);
             v[1] = bf16x2_to_f32x2(q.y);
             v[2] = bf16x2_to_f32x2(q.z);
@@ -200,29 +226,28 @@ struct Cols {
         } else if (sizeof(T) == 2 && VW == 2) {
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                v[j] = bf16x2_to_f32x2(*reinterpret_cast<const uint32_t*>(run(row, 4 * k + j)));
+                v[j] = bf16x2_to_f32x2(lds32(run(row, 4 * k + j)));
         } else if (sizeof(T) == 2) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const uint32_t x = *reinterpret_cast<const unsigned short*>(run(row, 8 * k + 2 * j)),
-                               y = *reinterpret_cast<const unsigned short*>(run(row, 8 * k + 2 * j + 1));
-                v[j] = bf16x2_to_f32x2(x | y << 16);
+                const uint32_t x = lds16(run(row, 8 * k + 2 * j)), y = lds16(run(row, 8 * k + 2 * j + 1));
+                v[j] = f32x2_pack(__uint_as_float(x << 16), __uint_as_float(y << 16));
             }
         } else if (VW == 4) {
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                const ulonglong2 q = *reinterpret_cast<const ulonglong2*>(run(row, 2 * k + j));
-                v[2 * j] = q.x;
-                v[2 * j + 1] = q.y;
+                const uint4 q = lds128(run(row, 2 * k + j));
+                v[2 * j] = f32x2_pack(__uint_as_float(q.x), __uint_as_float(q.y));
+                v[2 * j + 1] = f32x2_pack(__uint_as_float(q.z), __uint_as_float(q.w));
             }
         } else {
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                v[j] = f32x2_pack(*reinterpret_cast<const float*>(run(row, 8 * k + 2 * j)),
-                                  *reinterpret_cast<const float*>(run(row, 8 * k + 2 * j + 1)));
+                v[j] = f32x2_pack(__uint_as_float(lds32(run(row, 8 * k + 2 * j))),
+                                  __uint_as_float(lds32(run(row, 8 * k + 2 * j + 1))));
         }
     }
-    __device__ __forceinline__ void load(uint64_t (&v)[H], const uint8_t* row) const {
+    __device__ __forceinline__ void load(uint64_t (&v)[H], uint32_t row) const {
 #pragma unroll
         for (int k = 0; k < H / kNormPart; ++k) {
             uint64_t q[kNormPart];
@@ -291,14 +316,16 @@ struct Cols {
         }
     }
     // part k of such a vector
-    __device__ __forceinline__ void fetch8(uint64_t (&v)[kNormPart], const ulonglong2* from,
-                                           int k) const {
+    // (`from`: the address of the thread's own)
+    __device__ __forceinline__ static void fetch8(uint64_t (&v)[kNormPart], uint32_t from, int k) {
 #pragma unroll
-        for (int j = 0; j < kNormPart / 2; ++j) {
-            const ulonglong2 x = from[l * kNormStride + k * (kNormPart / 2) + j];
-            v[2 * j] = x.x;
-            v[2 * j + 1] = x.y;
-        }
+        for (int j = 0; j < kNormPart / 2; ++j)
+            asm volatile("ld.shared.v2.u64 {%0, %1}, [%2];"
+                         : "=l"(v[2 * j]), "=l"(v[2 * j + 1])
+                         : "r"(from + 16 * (k * (kNormPart / 2) + j)));
+    }
+    __device__ __forceinline__ uint32_t place(const ulonglong2* vec) const {
+        return smem_u32(vec + l * kNormStride);
     }
     // part k of v - m (past the row's end v stays 0)
     __device__ __forceinline__ void centre8(uint64_t (&v)[kNormPart], float m, int k) const {
@@ -372,7 +399,11 @@ struct RowSum {
         asm volatile("bar.sync %0, %1;" ::"r"(1 + first), "r"(nl) : "memory");
         // lane l adds value l % M of every (32 / M)-th warp
         float x = 0.f;
-        for (int w = lane / M; w < W; w += 32 / M) x += buf[first + w][lane % M];
+#pragma unroll
+        for (int k = 0; k * (32 / M) < kNormThreads / 32; ++k) {
+            const int w = lane / M + k * (32 / M);
+            if (w < W) x += buf[first + w][lane % M];
+        }
 #pragma unroll
         for (int k = M; k < 32; k <<= 1) x += __shfl_xor_sync(0xffffffffu, x, k);
 #pragma unroll
@@ -423,6 +454,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_fwd_kernel(const NormArgs a
         C.fill(pw, a.pre_w, nullptr, 1.f);
         if (LN) C.fill(pb, a.pre_b, nullptr, 0.f);
     }
+    const uint32_t pw_ = C.place(pw), gw_ = C.place(gw), pb_ = C.place(pb), gb_ = C.place(gb);
     int b = 0;
     uint32_t round = 0;
     bool ok = true;
@@ -443,8 +475,8 @@ __global__ void __launch_bounds__(kNormThreads) norm_fwd_kernel(const NormArgs a
             // a group's rows past the buffer's n hold what was there before: they are worked
             // on and not stored
             const int n = r1 - row0 < a.rows ? r1 - row0 : a.rows;
-            const uint8_t* buf = norm_smem + (size_t)b * 2 * a.piece +
-                                 ((uint32_t)((size_t)row0 * d * sizeof(T)) & 15) + first;
+            const uint32_t buf = smem_u32(norm_smem) + b * 2 * a.piece +
+                                 ((uint32_t)row0 * (uint32_t)d * (uint32_t)sizeof(T) & 15) + first;
             uint64_t v[R][H];
             float q[R];
             // mean out of v (a LayerNorm), then 1 / sqrt(mean square + eps) into q
@@ -493,8 +525,8 @@ __global__ void __launch_bounds__(kNormThreads) norm_fwd_kernel(const NormArgs a
 #pragma unroll
             for (int k = 0; k < H / Q; ++k) {
                 uint64_t w[Q], wb[Q];
-                C.fetch8(w, gw, k);
-                if (LN) C.fetch8(wb, gb, k);
+                C.fetch8(w, gw_, k);
+                if (LN) C.fetch8(wb, gb_, k);
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
                     uint64_t x[Q];
@@ -523,8 +555,8 @@ __global__ void __launch_bounds__(kNormThreads) norm_fwd_kernel(const NormArgs a
 #pragma unroll
                 for (int k = 0; k < H / Q; ++k) {
                     uint64_t w[Q], wb[Q];
-                    C.fetch8(w, pw, k);
-                    if (LN) C.fetch8(wb, pb, k);
+                    C.fetch8(w, pw_, k);
+                    if (LN) C.fetch8(wb, pb_, k);
 #pragma unroll
                     for (int r = 0; r < R; ++r) {
                         const uint64_t qq = both(q[r]);
@@ -603,6 +635,12 @@ __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const NormArgs a
     RowSum rs(&sh, nl, warp, lane);
     const Cols<T, VW, E> C(l, nl, d, sh.zero);
     if (grp == 0) C.fill(pw, a.pre_w, nullptr, 1.f);
+    const uint32_t pw_ = C.place(pw), gp_ = C.place(gp);
+    // a tensor that is not there reads the zeros
+    Cols<T, VW, E> Cr = C, Cf = C, Cx = C;
+    if (!has_dr) Cr.in = 0;
+    if (!has_f) Cf.in = 0;
+    if (!has_dx) Cx.in = 0;
     // sums over all of the CTA's rows: dx shat, dx
     uint64_t c_w[H], c_b[LN ? H : 1];
     pairs_zero(c_w);
@@ -627,14 +665,14 @@ __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const NormArgs a
             ok = __all_sync(0xffffffffu, okw && fed);
             if (!ok) break;
             const int n = r1 - row0 < a.rows ? r1 - row0 : a.rows;
-            const uint8_t* buf = norm_smem + (size_t)b * 4 * a.piece +
-                                 ((uint32_t)((size_t)row0 * d * sizeof(T)) & 15) + first;
+            const uint32_t buf = smem_u32(norm_smem) + b * 4 * a.piece +
+                                 ((uint32_t)row0 * (uint32_t)d * (uint32_t)sizeof(T) & 15) + first;
             // One row a group (a group past the buffer's n adds nothing), 8 columns at a time,
             // read again in each pass: the sums over the rows take the registers.
             const bool in = grp < n;
             const int row = row0 + grp;
-            const uint8_t *const dr_row = buf, *const f_row = buf + a.piece,
-                                *const s_row = buf + 2 * a.piece, *const x_row = buf + 3 * a.piece;
+            const uint32_t dr_row = buf, f_row = buf + a.piece, s_row = buf + 2 * a.piece,
+                           x_row = buf + 3 * a.piece;
             float ms = 0.f, mf = 0.f;
             if (LN) {
                 uint64_t x = 0, y = 0;
@@ -642,27 +680,27 @@ __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const NormArgs a
 #pragma unroll
                     for (int k = 0; k < H / Q; ++k) {
                         uint64_t v[Q];
-                        if (has_dx && a.pre == HCW_NORM_LAYER) {
-                            C.load8(v, s_row, k);
+                        Cx.load8(v, s_row, k);
 #pragma unroll
-                            for (int j = 0; j < Q; ++j) x = f32x2_add(x, v[j]);
-                        }
-                        if (has_f && a.post == HCW_NORM_LAYER) {
-                            C.load8(v, f_row, k);
+                        for (int j = 0; j < Q; ++j) x = f32x2_add(x, v[j]);
+                        Cf.load8(v, f_row, k);
 #pragma unroll
-                            for (int j = 0; j < Q; ++j) y = f32x2_add(y, v[j]);
-                        }
+                        for (int j = 0; j < Q; ++j) y = f32x2_add(y, v[j]);
                     }
                 }
                 float t[2] = {pair_sum(x), pair_sum(y)};
                 rs.sum(t);
-                ms = t[0] * inv_d;
-                mf = t[1] * inv_d;
+                ms = a.pre == HCW_NORM_LAYER ? t[0] * inv_d : 0.f;
+                mf = a.post == HCW_NORM_LAYER ? t[1] * inv_d : 0.f;
             }
             // s or f, centred where its norm is a LayerNorm
-            auto centred = [&](uint64_t (&v)[Q], const uint8_t* at, int k, float m) {
-                C.load8(v, at, k);
-                if (LN) C.centre8(v, m, k);
+            auto centred_s = [&](uint64_t (&v)[Q], int k) {
+                Cx.load8(v, s_row, k);
+                if (LN) C.centre8(v, ms, k);
+            };
+            auto centred_f = [&](uint64_t (&v)[Q], int k) {
+                Cf.load8(v, f_row, k);
+                if (LN) C.centre8(v, mf, k);
             };
             // sums of s^2, e s, f^2, e  with e = dx pre_w
             constexpr int NS = LN ? 4 : 3;
@@ -673,23 +711,19 @@ __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const NormArgs a
 #pragma unroll
                     for (int k = 0; k < H / Q; ++k) {
                         uint64_t v[Q], x[Q], w[Q];
-                        if (has_dx) {
-                            centred(v, s_row, k, ms);
-                            C.load8(x, x_row, k);
-                            C.fetch8(w, pw, k);
+                        centred_s(v, k);
+                        Cx.load8(x, x_row, k);
+                        C.fetch8(w, pw_, k);
 #pragma unroll
-                            for (int j = 0; j < Q; ++j) {
-                                const uint64_t e = f32x2_mul(x[j], w[j]);
-                                ss = f32x2_fma(v[j], v[j], ss);
-                                es = f32x2_fma(e, v[j], es);
-                                if (LN) e1 = f32x2_add(e1, e);
-                            }
+                        for (int j = 0; j < Q; ++j) {
+                            const uint64_t e = f32x2_mul(x[j], w[j]);
+                            ss = f32x2_fma(v[j], v[j], ss);
+                            es = f32x2_fma(e, v[j], es);
+                            if (LN) e1 = f32x2_add(e1, e);
                         }
-                        if (has_f) {
-                            centred(v, f_row, k, mf);
+                        centred_f(v, k);
 #pragma unroll
-                            for (int j = 0; j < Q; ++j) ff = f32x2_fma(v[j], v[j], ff);
-                        }
+                        for (int j = 0; j < Q; ++j) ff = f32x2_fma(v[j], v[j], ff);
                     }
                 }
                 t[0] = pair_sum(ss);
@@ -699,7 +733,8 @@ __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const NormArgs a
             }
             rs.sum(t);
             const float rstd = has_dx ? rsqrtf(t[0] * inv_d + a.eps) : 0.f;
-            const float qf = a.post != HCW_NORM_NONE ? rsqrtf(t[2] * inv_d + a.eps) : 1.f;
+            const float qf =
+                a.post != HCW_NORM_NONE && has_f ? rsqrtf(t[2] * inv_d + a.eps) : 1.f;
             const uint64_t qq = both(qf);
             uint64_t ds[H], hf = 0, h1 = 0;   // sums of h fhat, h  with h = gate ds post_w
             if (in) {
@@ -710,38 +745,31 @@ __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const NormArgs a
 #pragma unroll
                 for (int k = 0; k < H / Q; ++k) {
                     uint64_t v[Q], x[Q], w[Q], g_[Q];
-                    if (has_dr)
-                        C.load8(g_, dr_row, k);
-                    else
-                        pairs_zero(g_);
-                    if (has_dx) {
-                        centred(v, s_row, k, ms);
-                        C.load8(x, x_row, k);
-                        C.fetch8(w, pw, k);
+                    Cr.load8(g_, dr_row, k);
+                    centred_s(v, k);
+                    Cx.load8(x, x_row, k);
+                    C.fetch8(w, pw_, k);
 #pragma unroll
-                        for (int j = 0; j < Q; ++j) {
-                            const int i = k * Q + j;
-                            const uint64_t h = f32x2_mul(v[j], rr);
-                            uint64_t e = f32x2_fma(h, nm2, f32x2_mul(x[j], w[j]));
-                            if (LN) e = f32x2_add(e, nm1);
-                            c_w[i] = f32x2_fma(x[j], h, c_w[i]);
-                            if constexpr (LN) c_b[i] = f32x2_add(c_b[i], x[j]);
-                            g_[j] = f32x2_fma(e, rr, g_[j]);
-                        }
+                    for (int j = 0; j < Q; ++j) {
+                        const int i = k * Q + j;
+                        const uint64_t h = f32x2_mul(v[j], rr);
+                        uint64_t e = f32x2_fma(h, nm2, f32x2_mul(x[j], w[j]));
+                        if (LN) e = f32x2_add(e, nm1);
+                        c_w[i] = f32x2_fma(x[j], h, c_w[i]);
+                        if constexpr (LN) c_b[i] = f32x2_add(c_b[i], x[j]);
+                        g_[j] = f32x2_fma(e, rr, g_[j]);
                     }
-                    if (has_f) {
-                        centred(v, f_row, k, mf);
-                        C.fetch8(w, gp, k);
+                    centred_f(v, k);
+                    C.fetch8(w, gp_, k);
 #pragma unroll
-                        for (int j = 0; j < Q; ++j) {
-                            const int i = k * Q + j;
-                            const uint64_t fh = f32x2_mul(v[j], qq);
-                            const uint64_t h = f32x2_mul(g_[j], w[j]);   // 0 past the row's end
-                            i_w[i] = f32x2_fma(g_[j], fh, i_w[i]);
-                            if constexpr (LN) i_b[i] = f32x2_add(i_b[i], g_[j]);
-                            hf = f32x2_fma(h, fh, hf);
-                            if (LN) h1 = f32x2_add(h1, h);
-                        }
+                    for (int j = 0; j < Q; ++j) {
+                        const int i = k * Q + j;
+                        const uint64_t fh = f32x2_mul(v[j], qq);
+                        const uint64_t h = f32x2_mul(g_[j], w[j]);   // 0 past the row's end
+                        i_w[i] = f32x2_fma(g_[j], fh, i_w[i]);
+                        if constexpr (LN) i_b[i] = f32x2_add(i_b[i], g_[j]);
+                        hf = f32x2_fma(h, fh, hf);
+                        if (LN) h1 = f32x2_add(h1, h);
                     }
 #pragma unroll
                     for (int j = 0; j < Q; ++j) ds[k * Q + j] = g_[j];
@@ -761,8 +789,8 @@ __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const NormArgs a
 #pragma unroll
                     for (int k = 0; k < H / Q; ++k) {
                         uint64_t v[Q], w[Q];
-                        centred(v, f_row, k, mf);
-                        C.fetch8(w, gp, k);
+                        centred_f(v, k);
+                        C.fetch8(w, gp_, k);
 #pragma unroll
                         for (int j = 0; j < Q; ++j) {
                             uint64_t o = f32x2_fma(v[j], n4, f32x2_mul(ds[k * Q + j], w[j]));
