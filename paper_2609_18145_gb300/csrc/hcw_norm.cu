@@ -44,9 +44,10 @@ constexpr int kNormPar = 4;         // parameter sums of a CTA: post_w, post_b, 
 constexpr int kNormRed = 8;         // values of one reduction round
 constexpr int kNormCols = 16;       // columns a thread, in parts of 8:
 constexpr int kNormPart = 4;        // pairs of a part
-// 16-byte pieces from a thread's parameters in shared memory to the next thread's: 80 bytes,
-// so that 8 neighbours' 16-byte accesses fall into different banks
-constexpr int kNormStride = 5;
+// A thread's 16 floats in shared memory are 64 bytes, its 16-byte pieces in an order of its
+// own (piece c at c ^ (l / 2 & 3)), so that 8 neighbours' accesses to one piece fall into
+// different banks.
+constexpr int kNormOwn = kNormCols * (int)sizeof(float);
 constexpr int kNormMaxBufs = 8;
 constexpr size_t kNormSmem = 232448 - 2048;   // dynamic, beside NormShared
 constexpr unsigned long long kNormTimeoutNs = 2000000000ull;
@@ -305,27 +306,47 @@ struct Cols {
             store8(base, row, k, q);
         }
     }
-    // The product of a parameter vector (null: `none`) and, if given, another into shared
-    // memory at this thread's place, zeros past the row's end.
-    __device__ __forceinline__ void fill(ulonglong2* to, const float* p, const float* q,
+    // Address of a thread's own 16 floats of a vector in shared memory (`i`: its place).
+    __device__ __forceinline__ static uint32_t own(const void* vec, int i) {
+        return smem_u32(vec) + (uint32_t)(i * kNormOwn + ((i >> 1 & 3) << 4));
+    }
+    __device__ __forceinline__ static uint32_t piece(uint32_t own, int c) {
+        return own ^ (uint32_t)(c << 4);
+    }
+    // The product of a parameter vector (null: `none`) and, if given, another into its own
+    // floats, zeros past the row's end.
+    __device__ __forceinline__ void fill(uint32_t to, const float* p, const float* q,
                                          float none) const {
-        float* o = reinterpret_cast<float*>(to + l * kNormStride);
+        float v[E], w[E];
+#pragma unroll
         for (int j = 0; j < E; ++j) {
             const int c = col(j);
-            o[j] = c < d ? (p ? p[c] : none) * (q ? q[c] : 1.f) : 0.f;
+            v[j] = c < d ? (p ? p[c] : none) : 0.f;
+            w[j] = c < d && q ? q[c] : 1.f;
         }
+#pragma unroll
+        for (int c = 0; c < E / 4; ++c)
+            asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(piece(to, c)),
+                         "f"(v[4 * c] * w[4 * c]), "f"(v[4 * c + 1] * w[4 * c + 1]),
+                         "f"(v[4 * c + 2] * w[4 * c + 2]), "f"(v[4 * c + 3] * w[4 * c + 3])
+                         : "memory");
     }
-    // part k of such a vector
-    // (`from`: the address of the thread's own)
-    __device__ __forceinline__ static void fetch8(uint64_t (&v)[kNormPart], uint32_t from, int k) {
+    // part k of own floats
+    __device__ __forceinline__ static void fetch8(uint64_t (&v)[kNormPart], uint32_t own, int k) {
 #pragma unroll
         for (int j = 0; j < kNormPart / 2; ++j)
             asm volatile("ld.shared.v2.u64 {%0, %1}, [%2];"
                          : "=l"(v[2 * j]), "=l"(v[2 * j + 1])
-                         : "r"(from + 16 * (k * (kNormPart / 2) + j)));
+                         : "r"(piece(own, k * (kNormPart / 2) + j))
+                         : "memory");
     }
-    __device__ __forceinline__ uint32_t place(const ulonglong2* vec) const {
-        return smem_u32(vec + l * kNormStride);
+    __device__ __forceinline__ static void put8(uint32_t own, int k, const uint64_t (&v)[kNormPart]) {
+#pragma unroll
+        for (int j = 0; j < kNormPart / 2; ++j)
+            asm volatile("st.shared.v2.u64 [%0], {%1, %2};" ::"r"(
+                             piece(own, k * (kNormPart / 2) + j)),
+                         "l"(v[2 * j]), "l"(v[2 * j + 1])
+                         : "memory");
     }
     // part k of v - m (past the row's end v stays 0)
     __device__ __forceinline__ void centre8(uint64_t (&v)[kNormPart], float m, int k) const {
@@ -447,14 +468,13 @@ __global__ void __launch_bounds__(kNormThreads) norm_fwd_kernel(const NormArgs a
     const Cols<T, VW, E> C((int)threadIdx.x % nl, nl, d, sh.zero);
     const uint64_t alpha = both(a.alpha);
     // parameters: pre_w, gate * post_w, pre_b, gate * post_b
-    ulonglong2* const pw = reinterpret_cast<ulonglong2*>(norm_smem + (size_t)a.bufs * 2 * a.piece);
-    ulonglong2 *const gw = pw + kNormStride * nl, *const pb = gw + kNormStride * nl,
-                     *const gb = pb + kNormStride * nl;
-    if (grp == 0) {
+    const uint8_t* const par = norm_smem + (size_t)a.bufs * 2 * a.piece;
+    const uint32_t pw = C.own(par, C.l), gw = pw + kNormOwn * nl, pb = gw + kNormOwn * nl,
+                   gb = pb + kNormOwn * nl;
+    if (grp == n_grp - 1) {
         C.fill(pw, a.pre_w, nullptr, 1.f);
         if (LN) C.fill(pb, a.pre_b, nullptr, 0.f);
     }
-    const uint32_t pw_ = C.place(pw), gw_ = C.place(gw), pb_ = C.place(pb), gb_ = C.place(gb);
     int b = 0;
     uint32_t round = 0;
     bool ok = true;
@@ -463,7 +483,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_fwd_kernel(const NormArgs a
         item_rows(a, item, g, r0, r1);
         const float* gate = a.gate ? a.gate + (size_t)g * d : nullptr;
         __syncthreads();   // the item before has been worked through
-        if (grp == 0) {
+        if (grp == n_grp - 1) {
             C.fill(gw, a.post_w, gate, 1.f);
             if (LN) C.fill(gb, a.post_b, gate, 0.f);
         }
@@ -525,8 +545,8 @@ __global__ void __launch_bounds__(kNormThreads) norm_fwd_kernel(const NormArgs a
 #pragma unroll
             for (int k = 0; k < H / Q; ++k) {
                 uint64_t w[Q], wb[Q];
-                C.fetch8(w, gw_, k);
-                if (LN) C.fetch8(wb, gb_, k);
+                C.fetch8(w, gw, k);
+                if (LN) C.fetch8(wb, gb, k);
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
                     uint64_t x[Q];
@@ -555,8 +575,8 @@ __global__ void __launch_bounds__(kNormThreads) norm_fwd_kernel(const NormArgs a
 #pragma unroll
                 for (int k = 0; k < H / Q; ++k) {
                     uint64_t w[Q], wb[Q];
-                    C.fetch8(w, pw_, k);
-                    if (LN) C.fetch8(wb, pb_, k);
+                    C.fetch8(w, pw, k);
+                    if (LN) C.fetch8(wb, pb, k);
 #pragma unroll
                     for (int r = 0; r < R; ++r) {
                         const uint64_t qq = both(q[r]);
@@ -581,34 +601,46 @@ __global__ void __launch_bounds__(kNormThreads) norm_fwd_kernel(const NormArgs a
     if (threadIdx.x == 0) feed.drain(a, &sh);
 }
 
-// Adds the row groups' values v of a CTA into group 0's, in group order, through `buf`
-// ([n_grp - 1][H][nl] pairs).
-template <int H>
-__device__ __forceinline__ void group_add(uint64_t (&v)[H], uint64_t* buf, int grp, int n_grp, int l,
-                                          int nl) {
-    if (n_grp == 1) return;
+// The sums of the row groups' values v, in group order, column by column: emit(c, sum) on
+// the thread that has column c.  Through `buf` ([n_grp][nl * E] floats, one after the
+// other by column).
+template <typename C, int H, typename F>
+__device__ __forceinline__ void group_sum(const C& cols, const uint64_t (&v)[H], float* buf, int grp,
+                                          int n_grp, F emit) {
+    const int ld = cols.nl * 2 * H;
     __syncthreads();
-    if (grp > 0)
 #pragma unroll
-        for (int j = 0; j < H; ++j) buf[((grp - 1) * H + j) * nl + l] = v[j];
+    for (int j = 0; j < H; ++j) {
+        const float2 f = f32x2_unpack(v[j]);
+        buf[grp * ld + cols.col(2 * j)] = f.x;
+        buf[grp * ld + cols.col(2 * j + 1)] = f.y;
+    }
     __syncthreads();
-    if (grp == 0)
-        for (int q = 0; q < n_grp - 1; ++q)
-#pragma unroll
-            for (int j = 0; j < H; ++j) v[j] = f32x2_add(v[j], buf[(q * H + j) * nl + l]);
+    for (int c = threadIdx.x; c < cols.d; c += blockDim.x) {
+        float t = buf[c];
+#pragma unroll 4
+        for (int g = 1; g < n_grp; ++g) t += buf[g * ld + c];
+        emit(c, t);
+    }
 }
 
-template <typename T, int VW, bool LN>
+// SM: with LayerNorms, the sums of dx and ds in shared memory (the registers have no room for
+// them; without SM they are there all the same, for rows whose ring leaves no room either).
+template <typename T, int VW, bool LN, bool SM>
 __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const NormArgs a) {
     extern __shared__ __align__(128) uint8_t norm_smem[];
     __shared__ NormShared sh;
     constexpr int E = kNormCols, H = E / 2, Q = kNormPart;   // pairs in all, and at a time
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int nt = (int)blockDim.x, nl = a.nl, d = a.d;
-    // parameters: pre_w, gate * post_w; then the row groups' sums on their way to group 0
-    ulonglong2* const pw = reinterpret_cast<ulonglong2*>(norm_smem + (size_t)a.bufs * 4 * a.piece);
-    ulonglong2* const gp = pw + kNormStride * nl;
-    uint64_t* const gbuf = reinterpret_cast<uint64_t*>(gp + kNormStride * nl);
+    // parameters: pre_w, gate * post_w; the sums of dx and ds (SM); the row groups' sums on
+    // their way together (through the sums of ds, which are in registers by then)
+    const uint8_t* const par = norm_smem + (size_t)a.bufs * 4 * a.piece;
+    const uint32_t pw = Cols<T, VW, E>::own(par, (int)threadIdx.x % nl), gp = pw + kNormOwn * nl;
+    const uint32_t c_b = Cols<T, VW, E>::own(par + 2 * kNormOwn * nl, threadIdx.x),
+                   i_b = c_b + kNormOwn * nt;
+    float* const gbuf = reinterpret_cast<float*>(
+        norm_smem + (size_t)a.bufs * 4 * a.piece + kNormOwn * (2 * nl + (SM ? nt : 0)));
     if (threadIdx.x == 0) {
         for (int i = 0; i < a.bufs; ++i) {
             mbar_init(&sh.full[i], 1);
@@ -634,17 +666,29 @@ __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const NormArgs a
     const int items = a.groups * a.slices;
     RowSum rs(&sh, nl, warp, lane);
     const Cols<T, VW, E> C(l, nl, d, sh.zero);
-    if (grp == 0) C.fill(pw, a.pre_w, nullptr, 1.f);
-    const uint32_t pw_ = C.place(pw), gp_ = C.place(gp);
+    if (grp == n_grp - 1) C.fill(pw, a.pre_w, nullptr, 1.f);
     // a tensor that is not there reads the zeros
     Cols<T, VW, E> Cr = C, Cf = C, Cx = C;
     if (!has_dr) Cr.in = 0;
     if (!has_f) Cf.in = 0;
     if (!has_dx) Cx.in = 0;
     // sums over all of the CTA's rows: dx shat, dx
-    uint64_t c_w[H], c_b[LN ? H : 1];
+    uint64_t c_w[H];
     pairs_zero(c_w);
-    if constexpr (LN) pairs_zero(c_b);
+    const uint64_t none[Q] = {};
+    uint64_t c_r[LN && !SM ? H : 1] = {}, i_r[LN && !SM ? H : 1];   // dx and ds without SM
+    if (SM)
+#pragma unroll
+        for (int k = 0; k < H / Q; ++k) C.put8(c_b, k, none);
+    auto own_sums = [&](uint64_t (&v)[H], uint32_t own) {
+#pragma unroll
+        for (int k = 0; k < H / Q; ++k) {
+            uint64_t q[Q];
+            C.fetch8(q, own, k);
+#pragma unroll
+            for (int j = 0; j < Q; ++j) v[k * Q + j] = q[j];
+        }
+    };
     float* const crow = a.cpart ? a.cpart + (size_t)blockIdx.x * kNormPar * d : nullptr;
     int b = 0;
     uint32_t round = 0;
@@ -654,12 +698,15 @@ __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const NormArgs a
         item_rows(a, item, g, r0, r1);
         const float* gate = a.gate ? a.gate + (size_t)g * d : nullptr;
         __syncthreads();   // the item before has been worked through
-        if (grp == 0) C.fill(gp, a.post_w, gate, 1.f);
+        if (grp == n_grp - 1) C.fill(gp, a.post_w, gate, 1.f);
         __syncthreads();
         // sums over the item's rows: ds fhat, ds
-        uint64_t i_w[H], i_b[LN ? H : 1];
+        uint64_t i_w[H];
         pairs_zero(i_w);
-        if constexpr (LN) pairs_zero(i_b);
+        if (SM)
+#pragma unroll
+            for (int k = 0; k < H / Q; ++k) C.put8(i_b, k, none);
+        if constexpr (LN && !SM) pairs_zero(i_r);
         for (int row0 = r0; row0 < r1 && ok; row0 += a.rows) {
             const bool okw = mbar_wait(&sh.full[b], round & 1, &sh.abort, kNormTimeoutNs);
             ok = __all_sync(0xffffffffu, okw && fed);
@@ -713,7 +760,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const NormArgs a
                         uint64_t v[Q], x[Q], w[Q];
                         centred_s(v, k);
                         Cx.load8(x, x_row, k);
-                        C.fetch8(w, pw_, k);
+                        C.fetch8(w, pw, k);
 #pragma unroll
                         for (int j = 0; j < Q; ++j) {
                             const uint64_t e = f32x2_mul(x[j], w[j]);
@@ -748,7 +795,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const NormArgs a
                     Cr.load8(g_, dr_row, k);
                     centred_s(v, k);
                     Cx.load8(x, x_row, k);
-                    C.fetch8(w, pw_, k);
+                    C.fetch8(w, pw, k);
 #pragma unroll
                     for (int j = 0; j < Q; ++j) {
                         const int i = k * Q + j;
@@ -756,18 +803,32 @@ __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const NormArgs a
                         uint64_t e = f32x2_fma(h, nm2, f32x2_mul(x[j], w[j]));
                         if (LN) e = f32x2_add(e, nm1);
                         c_w[i] = f32x2_fma(x[j], h, c_w[i]);
-                        if constexpr (LN) c_b[i] = f32x2_add(c_b[i], x[j]);
                         g_[j] = f32x2_fma(e, rr, g_[j]);
                     }
+                    if constexpr (LN && !SM)
+#pragma unroll
+                        for (int j = 0; j < Q; ++j) {
+                            c_r[k * Q + j] = f32x2_add(c_r[k * Q + j], x[j]);
+                            i_r[k * Q + j] = f32x2_add(i_r[k * Q + j], g_[j]);
+                        }
+                    if (SM) {
+                        C.fetch8(w, c_b, k);
+#pragma unroll
+                        for (int j = 0; j < Q; ++j) w[j] = f32x2_add(w[j], x[j]);
+                        C.put8(c_b, k, w);
+                        C.fetch8(w, i_b, k);
+#pragma unroll
+                        for (int j = 0; j < Q; ++j) w[j] = f32x2_add(w[j], g_[j]);
+                        C.put8(i_b, k, w);
+                    }
                     centred_f(v, k);
-                    C.fetch8(w, gp_, k);
+                    C.fetch8(w, gp, k);
 #pragma unroll
                     for (int j = 0; j < Q; ++j) {
                         const int i = k * Q + j;
                         const uint64_t fh = f32x2_mul(v[j], qq);
                         const uint64_t h = f32x2_mul(g_[j], w[j]);   // 0 past the row's end
                         i_w[i] = f32x2_fma(g_[j], fh, i_w[i]);
-                        if constexpr (LN) i_b[i] = f32x2_add(i_b[i], g_[j]);
                         hf = f32x2_fma(h, fh, hf);
                         if (LN) h1 = f32x2_add(h1, h);
                     }
@@ -790,7 +851,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const NormArgs a
                     for (int k = 0; k < H / Q; ++k) {
                         uint64_t v[Q], w[Q];
                         centred_f(v, k);
-                        C.fetch8(w, gp_, k);
+                        C.fetch8(w, gp, k);
 #pragma unroll
                         for (int j = 0; j < Q; ++j) {
                             uint64_t o = f32x2_fma(v[j], n4, f32x2_mul(ds[k * Q + j], w[j]));
@@ -821,51 +882,37 @@ __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const NormArgs a
             }
         }
         if (a.cpart || a.gpart) {
-            group_add(i_w, gbuf, grp, n_grp, l, nl);
-            if constexpr (LN) group_add(i_b, gbuf, grp, n_grp, l, nl);
-            if (grp == 0) {
-                // the CTA's sums of gate ds fhat and gate ds build up in its partial row
-                const bool fresh = item == (int)blockIdx.x;
+            // the CTA's sums of gate ds fhat and gate ds build up in its partial row; dgate's of
+            // ds v = ds (fhat post_w + post_b) are the item's alone
+            const bool fresh = item == (int)blockIdx.x;
+            float* const grow = a.gpart ? a.gpart + (size_t)item * d : nullptr;
+            uint64_t b_[H];
+            if (SM) own_sums(b_, i_b);
+            group_sum(C, i_w, gbuf, grp, n_grp, [&](int c, float v) {
+                if (crow) crow[c] = (fresh ? 0.f : crow[c]) + (gate ? gate[c] : 1.f) * v;
+                if (grow) grow[c] = v * (a.post_w ? a.post_w[c] : 1.f);
+            });
+            if (LN) {
+                if constexpr (LN && !SM)
 #pragma unroll
-                for (int j = 0; j < E; ++j) {
-                    const int c = C.col(j);
-                    if (c >= d) continue;
-                    const float2 w2 = f32x2_unpack(i_w[j / 2]);
-                    const float w = j & 1 ? w2.y : w2.x;
-                    float bb = 0.f;
-                    if constexpr (LN) {
-                        const float2 b2 = f32x2_unpack(i_b[j / 2]);
-                        bb = j & 1 ? b2.y : b2.x;
-                    }
-                    if (crow) {
-                        const float t = gate ? gate[c] : 1.f;
-                        crow[c] = (fresh ? 0.f : crow[c]) + t * w;
-                        if constexpr (LN) crow[d + c] = (fresh ? 0.f : crow[d + c]) + t * bb;
-                    }
-                    if (a.gpart) {   // ds v = ds (fhat post_w + post_b)
-                        float v = w * (a.post_w ? a.post_w[c] : 1.f);
-                        if constexpr (LN) v += bb * (a.post_b ? a.post_b[c] : 0.f);
-                        a.gpart[(size_t)item * d + c] = v;
-                    }
-                }
+                    for (int j = 0; j < H; ++j) b_[j] = i_r[j];
+                group_sum(C, b_, gbuf, grp, n_grp, [&](int c, float v) {
+                    if (crow) crow[d + c] = (fresh ? 0.f : crow[d + c]) + (gate ? gate[c] : 1.f) * v;
+                    if (grow && a.post_b) grow[c] += v * a.post_b[c];
+                });
             }
         }
     }
     if (crow) {
-        group_add(c_w, gbuf, grp, n_grp, l, nl);
-        if constexpr (LN) group_add(c_b, gbuf, grp, n_grp, l, nl);
-        if (grp == 0)
+        uint64_t b_[H];
+        if (SM) own_sums(b_, c_b);
+        group_sum(C, c_w, gbuf, grp, n_grp, [&](int c, float v) { crow[(size_t)2 * d + c] = v; });
+        if (LN) {
+            if constexpr (LN && !SM)
 #pragma unroll
-            for (int j = 0; j < E; ++j) {
-                const int c = C.col(j);
-                if (c >= d) continue;
-                const float2 w2 = f32x2_unpack(c_w[j / 2]);
-                crow[(size_t)2 * d + c] = j & 1 ? w2.y : w2.x;
-                if constexpr (LN) {
-                    const float2 b2 = f32x2_unpack(c_b[j / 2]);
-                    crow[(size_t)3 * d + c] = j & 1 ? b2.y : b2.x;
-                }
-            }
+                for (int j = 0; j < H; ++j) b_[j] = c_r[j];
+            group_sum(C, b_, gbuf, grp, n_grp, [&](int c, float v) { crow[(size_t)3 * d + c] = v; });
+        }
     }
     if (threadIdx.x == 0) feed.drain(a, &sh);
 }
@@ -922,7 +969,7 @@ __global__ void __launch_bounds__(1024) norm_reduce_kernel(const NormReduceArgs 
 
 // Threads a row and a CTA, buffers and items for a call.
 struct NormPlan {
-    bool ln;
+    bool ln, sm;
     int nl, threads, grid, slices, groups;
     int rows, bufs, piece;
     size_t smem;
@@ -960,11 +1007,15 @@ NormPlan norm_plan(bool bwd, bool ln, int T, int d, int elem, int rows_per_gate)
     p.threads = n_grp * p.nl;
     const int n_in = bwd ? 4 : 2;
     int r = bwd ? 1 : kNormRows;
-    const size_t vec = (size_t)kNormStride * 16 * p.nl;
-    const size_t fixed = (bwd || !ln ? 2 : 4) * vec +
-                         (bwd ? (size_t)(n_grp - 1) * E * p.nl * sizeof(float) : 0);
-    const size_t room = kNormSmem - fixed;
+    const size_t vec = (size_t)kNormOwn * p.nl;
+    size_t fixed = !bwd ? (ln ? 4 : 2) * vec : (2 + (ln ? 2 : 1) * n_grp) * vec;
     auto piece = [&](int rows) { return (int)(((size_t)rows * d * elem + 32 + 127) / 128 * 128); };
+    p.sm = bwd && ln;
+    if (p.sm && fixed + (size_t)n_in * piece(n_grp) > kNormSmem) {
+        p.sm = false;
+        fixed = (2 + n_grp) * vec;
+    }
+    const size_t room = kNormSmem - fixed;
     // (a buffer of one row a group where two do not fit: the kernel's second row is then
     // past the buffer's rows)
     while (r > 1 && (size_t)n_in * piece(n_grp * r) > room) r /= 2;
@@ -999,19 +1050,22 @@ NormPlan norm_plan(bool bwd, bool ln, int T, int d, int elem, int rows_per_gate)
 
 template <typename T, int VW, bool LN>
 cudaError_t launch_norm(bool bwd, const NormPlan& p, const NormArgs& a, cudaStream_t st) {
-    auto kern = bwd ? norm_bwd_kernel<T, VW, LN>
-                    : norm_fwd_kernel<T, VW, LN, kNormRows>;
-    static std::once_flag once[64][2];
-    static cudaError_t set_err[64][2];
+    auto kern = bwd ? norm_bwd_kernel<T, VW, LN, LN> : norm_fwd_kernel<T, VW, LN, kNormRows>;
+    // (a row of bf16 always leaves the sums room: 192 KB in all at 8192 columns)
+    if constexpr (LN && sizeof(T) == 4)
+        if (bwd && !p.sm) kern = norm_bwd_kernel<T, VW, LN, false>;
+    const int which = !bwd ? 0 : p.sm == LN ? 1 : 2;
+    static std::once_flag once[64][3];
+    static cudaError_t set_err[64][3];
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
-    std::call_once(once[dev][bwd], [&] {
-        set_err[dev][bwd] = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
+    std::call_once(once[dev][which], [&] {
+        set_err[dev][which] = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                  (int)kNormSmem);
     });
-    if (set_err[dev][bwd] != cudaSuccess) return set_err[dev][bwd];
+    if (set_err[dev][which] != cudaSuccess) return set_err[dev][which];
     return launch_pdl(kern, dim3((unsigned)p.grid), dim3((unsigned)p.threads), p.smem, st, a);
 }
 
