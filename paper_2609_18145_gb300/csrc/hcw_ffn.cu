@@ -45,15 +45,17 @@ constexpr int kFStage = 2 * kFA;             // and its columns of B (128 at mos
 constexpr int kFWarps = 8;                   // epilogue warps, two per TMEM lane quarter
 constexpr int kFThreads = 64 + 32 * kFWarps;
 constexpr uint32_t kFTmem = 512;
-constexpr int kFPatch = 4096;                // 32 rows x 128 bytes
-constexpr int kFMaxStages = 5;
+constexpr int kFPatch = 2048;                // 32 rows x 64 bytes
+constexpr int kFMaxStages = 6;
 constexpr unsigned long long kFTimeoutNs = 2000000000ull;
 
 enum FfnMode { FFN_GEMM = 0, FFN_GATE = 1, FFN_GRAD = 2 };
 
-// stages of the ring and patches of an epilogue warp
-constexpr int ffn_stages(int mode) { return mode == FFN_GRAD ? 4 : 5; }
-constexpr int ffn_patches(int mode) { return mode == FFN_GRAD ? 3 : 2; }
+// Stages of the ring and patches of an epilogue warp.  A stage takes about 2,000 cycles from
+// its copies' start to their landing, its products 256 to 512: the ring takes the
+// shared memory, the patches the rest.
+constexpr int ffn_stages(int mode) { return mode == FFN_GRAD ? 5 : 6; }
+constexpr int ffn_patches(int mode) { return mode == FFN_GRAD ? 4 : 2; }
 
 struct __align__(8) FfnBars {
     uint64_t full[kFMaxStages];    // leader: both CTAs' copies of a stage landed
@@ -75,7 +77,7 @@ static_assert(ffn_smem(FFN_GEMM) <= 232448 && ffn_smem(FFN_GRAD) <= 232448, "sha
 // (box 64 x 128), or MN-major (_mn: a row-major [K][cols] matrix in 64 x 64 boxes).
 struct FfnProd {
     CUtensorMap mA, mB;
-    CUtensorMap mOut;     // bf16 (N, M) box (64, 32), or fp32 (N, M, splits) box (32, 32, 1)
+    CUtensorMap mOut;     // bf16 (N, M) box (32, 32), or fp32 (N, M, splits) box (16, 32, 1)
     int a_mn, b_mn;
     int M, N;
     int bn;               // tile columns: 256 or 128
@@ -315,12 +317,30 @@ __global__ void __launch_bounds__(kFThreads, 1) ffn_pair_kernel(const __grid_con
         const int e = warp - 2;
         const int quarter = warp & 3, chalf = e >> 2;
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+        // Patches of 32 rows x 64 bytes (64-byte swizzle) in a ring: one is filled when the
+        // store that was issued from it kPatches stores ago has read it.
         uint8_t* const patches = staging + (size_t)e * kPatches * kFPatch;
-        // 16-byte chunk m of row r of a 128-byte-swizzled patch
-        auto chunk = [](uint8_t* buf, int r, int m) {
-            return reinterpret_cast<uint4*>(buf + r * 128 + ((m ^ (r & 7)) << 4));
+        int nbuf = 0;
+        auto patch = [&]() {
+            if (lane == 0) bulk_wait_read<kPatches - 1>();
+            __syncwarp();
+            uint8_t* buf = patches + nbuf * kFPatch;
+            nbuf = nbuf + 1 == kPatches ? 0 : nbuf + 1;
+            return buf;
         };
-        int it = 0, nbuf = 0;
+        // 16-byte chunk m of this lane's row
+        auto chunk = [&](uint8_t* buf, int m) {
+            return reinterpret_cast<uint4*>(buf + lane * 64 + ((m ^ (lane >> 1 & 3)) << 4));
+        };
+        auto store_2d = [&](const CUtensorMap* m, uint8_t* buf, int c, int r) {
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+                tma_store_2d(m, buf, c, r);
+                bulk_commit();
+            }
+        };
+        int it = 0;
         for (int v = pair; v < a.n_units; v += n_pairs, ++it) {
             const Unit t = unit(v);
             const FfnProd& p = a.p[MODE == FFN_GEMM ? t.q : 0];
@@ -350,19 +370,24 @@ __global__ void __launch_bounds__(kFThreads, 1) ffn_pair_kernel(const __grid_con
                     }
                     if (c + 32 == cw) release();
                     if (!st) continue;
-                    // fp32: a patch of 32 columns each time; bf16: of 64, filled in two
-                    const int part = p.f32 ? 0 : (c >> 5) & 1;
-                    uint8_t* buf = patches + nbuf * kFPatch;
-                    if (part == 0) {
-                        if (lane == 0) bulk_wait_read<1>();   // its store of two patches ago
-                        __syncwarp();
-                    }
                     if (p.f32) {
 #pragma unroll
-                        for (int m = 0; m < 8; ++m)
-                            *chunk(buf, lane, m) =
-                                make_uint4(r[4 * m], r[4 * m + 1], r[4 * m + 2], r[4 * m + 3]);
+                        for (int h = 0; h < 2; ++h) {
+                            if (colw + c + 16 * h >= p.N) break;   // warp-uniform
+                            uint8_t* buf = patch();
+#pragma unroll
+                            for (int m = 0; m < 4; ++m)
+                                *chunk(buf, m) = make_uint4(r[16 * h + 4 * m], r[16 * h + 4 * m + 1],
+                                                            r[16 * h + 4 * m + 2], r[16 * h + 4 * m + 3]);
+                            fence_proxy_async_smem();
+                            __syncwarp();
+                            if (lane == 0) {
+                                tma_store_3d(&p.mOut, buf, colw + c + 16 * h, row0, t.s);
+                                bulk_commit();
+                            }
+                        }
                     } else {
+                        uint8_t* buf = patch();
 #pragma unroll
                         for (int m = 0; m < 4; ++m) {
                             uint32_t w[4];
@@ -370,22 +395,10 @@ __global__ void __launch_bounds__(kFThreads, 1) ffn_pair_kernel(const __grid_con
                             for (int j = 0; j < 4; ++j)
                                 w[j] = pack_bf16x2(__uint_as_float(r[8 * m + 2 * j]),
                                                    __uint_as_float(r[8 * m + 2 * j + 1]));
-                            *chunk(buf, lane, 4 * part + m) = make_uint4(w[0], w[1], w[2], w[3]);
+                            *chunk(buf, m) = make_uint4(w[0], w[1], w[2], w[3]);
                         }
+                        store_2d(&p.mOut, buf, colw + c, row0);
                     }
-                    // a bf16 patch whose second half holds no column of C goes out half full
-                    // (TMA drops the columns past C's end)
-                    if (!p.f32 && part == 0 && colw + c + 32 < p.N) continue;
-                    fence_proxy_async_smem();
-                    __syncwarp();
-                    if (lane == 0) {
-                        if (p.f32)
-                            tma_store_3d(&p.mOut, buf, colw + c, row0, t.s);
-                        else
-                            tma_store_2d(&p.mOut, buf, colw + (c & ~63), row0);
-                        bulk_commit();
-                    }
-                    nbuf ^= 1;
                 }
                 continue;
             }
@@ -397,10 +410,6 @@ __global__ void __launch_bounds__(kFThreads, 1) ffn_pair_kernel(const __grid_con
             }
             if (MODE == FFN_GATE) {
                 const uint32_t tg = tmem_base + lanes + (uint32_t)((it & 1) * 256 + chalf * 64);
-                uint8_t* buf = patches + nbuf * kFPatch;
-                nbuf ^= 1;
-                if (lane == 0) bulk_wait_read<1>();
-                __syncwarp();
 #pragma unroll 1
                 for (int c = 0; c < 64; c += 32) {
                     uint32_t g[32], u[32];
@@ -410,6 +419,8 @@ __global__ void __launch_bounds__(kFThreads, 1) ffn_pair_kernel(const __grid_con
                     tmem_ld_wait_regs(g);
                     tmem_ld_wait_regs(u);
                     if (c) release();
+                    if (col + c >= a.h) continue;   // warp-uniform
+                    uint8_t* buf = patch();
 #pragma unroll
                     for (int m = 0; m < 4; ++m) {
                         uint32_t w[4];
@@ -421,20 +432,13 @@ __global__ void __launch_bounds__(kFThreads, 1) ffn_pair_kernel(const __grid_con
                                 ffn_act<ACT>(__uint_as_float(g[i + 1]), nullptr) *
                                     __uint_as_float(u[i + 1]));
                         }
-                        *chunk(buf, lane, (c >> 3) + m) = make_uint4(w[0], w[1], w[2], w[3]);
+                        *chunk(buf, m) = make_uint4(w[0], w[1], w[2], w[3]);
                     }
-                }
-                fence_proxy_async_smem();
-                __syncwarp();
-                if (lane == 0) {
-                    tma_store_2d(&p.mOut, buf, col, row0);
-                    bulk_commit();
+                    store_2d(&p.mOut, buf, col + c, row0);
                 }
             } else {
                 const uint32_t td = tmem_base + lanes + (uint32_t)((it & 1) * 128 + chalf * 64);
                 const uint32_t tg = tmem_base + lanes + (uint32_t)(256 + chalf * 64);
-                if (lane == 0) bulk_wait_read<0>();   // the last unit's three patches
-                __syncwarp();
 #pragma unroll 1
                 for (int c = 0; c < 64; c += 32) {
                     uint32_t d[32], g[32], u[32];
@@ -446,6 +450,8 @@ __global__ void __launch_bounds__(kFThreads, 1) ffn_pair_kernel(const __grid_con
                     tmem_ld_wait_regs(g);
                     tmem_ld_wait_regs(u);
                     if (c) release();
+                    if (col + c >= a.h) continue;   // warp-uniform
+                    uint8_t *const bg = patch(), *const bu = patch(), *const ba = patch();
 #pragma unroll
                     for (int m = 0; m < 4; ++m) {
                         uint32_t wg[4], wu[4], wa[4];
@@ -466,20 +472,13 @@ __global__ void __launch_bounds__(kFThreads, 1) ffn_pair_kernel(const __grid_con
                             wu[j] = pack_bf16x2(ou[0], ou[1]);
                             wa[j] = pack_bf16x2(oa[0], oa[1]);
                         }
-                        const int k = (c >> 3) + m;
-                        *chunk(patches, lane, k) = make_uint4(wg[0], wg[1], wg[2], wg[3]);
-                        *chunk(patches + kFPatch, lane, k) = make_uint4(wu[0], wu[1], wu[2], wu[3]);
-                        *chunk(patches + 2 * kFPatch, lane, k) =
-                            make_uint4(wa[0], wa[1], wa[2], wa[3]);
+                        *chunk(bg, m) = make_uint4(wg[0], wg[1], wg[2], wg[3]);
+                        *chunk(bu, m) = make_uint4(wu[0], wu[1], wu[2], wu[3]);
+                        *chunk(ba, m) = make_uint4(wa[0], wa[1], wa[2], wa[3]);
                     }
-                }
-                fence_proxy_async_smem();
-                __syncwarp();
-                if (lane == 0) {
-                    tma_store_2d(&a.p[0].mOut, patches, col, row0);
-                    tma_store_2d(&a.p[1].mOut, patches + kFPatch, col, row0);
-                    tma_store_2d(&a.p[2].mOut, patches + 2 * kFPatch, col, row0);
-                    bulk_commit();
+                    store_2d(&a.p[0].mOut, bg, col + c, row0);
+                    store_2d(&a.p[1].mOut, bu, col + c, row0);
+                    store_2d(&a.p[2].mOut, ba, col + c, row0);
                 }
             }
         }
@@ -555,7 +554,7 @@ FfnEncodeFn ffn_encode() {
 
 // bf16 [rows][cols], ld elements from row to row, in boxes of box_c x box_r
 bool ffn_map(CUtensorMap* m, const void* base, long long rows, long long cols, long long ld,
-             int box_c, int box_r) {
+             int box_c, int box_r, CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B) {
     FfnEncodeFn enc = ffn_encode();
     if (!enc) return false;
     cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
@@ -563,21 +562,25 @@ bool ffn_map(CUtensorMap* m, const void* base, long long rows, long long cols, l
     cuuint32_t box[2] = {(cuuint32_t)box_c, (cuuint32_t)box_r};
     cuuint32_t estr[2] = {1, 1};
     return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box,
-               estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-               CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// fp32 [splits][M][N] in patches of 32 x 32
+// an output in patches of 32 x 32
+bool ffn_map_out(CUtensorMap* m, void* base, long long rows, long long cols, long long ld) {
+    return ffn_map(m, base, rows, cols, ld, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B);
+}
+
+// fp32 [splits][M][N] in patches of 32 rows x 16 columns
 bool ffn_map_f32(CUtensorMap* m, void* base, int M, int N, int splits) {
     FfnEncodeFn enc = ffn_encode();
     if (!enc) return false;
     cuuint64_t dims[3] = {(cuuint64_t)N, (cuuint64_t)M, (cuuint64_t)splits};
     cuuint64_t strides[2] = {(cuuint64_t)N * 4, (cuuint64_t)M * N * 4};
-    cuuint32_t box[3] = {32, 32, 1};
+    cuuint32_t box[3] = {16, 32, 1};
     cuuint32_t estr[3] = {1, 1, 1};
     return enc(m, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, base, dims, strides, box, estr,
-               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B,
                CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -748,7 +751,7 @@ int ffn_gemms(const FfnShape* s, const FfnOperands* o, int n, uint8_t* part, cud
         if (!ffn_operand(&p.mA, q.A, t.M, t.K, q.a_mn, kFM) ||
             !ffn_operand(&p.mB, q.B, t.N, t.K, q.b_mn, t.bn / 2) ||
             !(p.f32 ? ffn_map_f32(&p.mOut, out, p.M, p.N, p.splits)
-                    : ffn_map(&p.mOut, out, p.M, p.N, p.N, 64, 32)))
+                    : ffn_map_out(&p.mOut, out, p.M, p.N, p.N)))
             return HCW_ERR_CUDA;
     }
     a.n_prod = n;
@@ -876,7 +879,7 @@ int hcw_gated_ffn_fwd(const void* x, const void* W1, const void* W2, int T, int 
     a.h = h;
     a.timeout_ns = kFTimeoutNs;
     if (!ffn_operand(&p.mA, x, T, d, false, kFM) || !ffn_operand(&p.mB, W1, 2ll * h, d, false, 128) ||
-        !ffn_map(&p.mOut, workspace, T, h, h, 64, 32))
+        !ffn_map_out(&p.mOut, workspace, T, h, h))
         return HCW_ERR_CUDA;
     rc = count_launch(ffn_launch_act<FFN_GATE>(act, a, a.n_units < pairs ? a.n_units : pairs, st), 1);
     if (rc) return rc;
@@ -946,9 +949,9 @@ int hcw_gated_ffn_bwd(const void* x, const void* dy, const void* W1, const void*
         !ffn_operand(&a.p[0].mB, W2, h, d, true, 0) ||
         !ffn_operand(&a.p[1].mA, x, T, d, false, kFM) ||
         !ffn_operand(&a.p[1].mB, W1, 2ll * h, d, false, 128) ||
-        !ffn_map(&a.p[0].mOut, ws, T, h, 2ll * h, 64, 32) ||
-        !ffn_map(&a.p[1].mOut, ws + (size_t)h * 2, T, h, 2ll * h, 64, 32) ||
-        !ffn_map(&a.p[2].mOut, ws + w.act, T, h, h, 64, 32))
+        !ffn_map_out(&a.p[0].mOut, ws, T, h, 2ll * h) ||
+        !ffn_map_out(&a.p[1].mOut, ws + (size_t)h * 2, T, h, 2ll * h) ||
+        !ffn_map_out(&a.p[2].mOut, ws + w.act, T, h, h))
         return HCW_ERR_CUDA;
     rc = count_launch(ffn_launch_act<FFN_GRAD>(act, a, a.n_units < pairs ? a.n_units : pairs, st), 1);
     if (rc) return rc;
