@@ -532,6 +532,123 @@ __global__ void __launch_bounds__(256) ffn_reduce_kernel(const FfnReduce a) {
     }
 }
 
+// ------------------------------------------------------------------ few tokens
+// out[t][n] = sum_k A[t][k] B[n][k] over T <= 16 MT rows, or with GATED the gate and up
+// sums of B's rows n and n_cols + n and act(g) u.  Bound by reading B once (the weights), and
+// for narrow blocks by latency: a CTA takes 8 columns, its 8 warps a slice of K each with the
+// warp-level MMA (16 rows x 8 columns x 16; a slab of tcgen05's 128 rows would be empty
+// but for a few), four 32-wide blocks of weights in flight a lane; the warps' sums are added
+// in warp order.  A lane's 16 bytes of 8 neighbouring k stand for the MMA's k in any order,
+// the same for both operands.  The second product's launch reads its first weights before it
+// waits for the first's.
+constexpr int kRowWarps = 8;
+constexpr int kRowBlocks = 4;      // 32-wide blocks of K a lane has in flight
+constexpr int kRowMax = 32;        // tokens
+
+struct FfnRowArgs {
+    const __nv_bfloat16* A;   // [T][K]
+    const __nv_bfloat16* B;   // [n_cols][K], GATED: [2 n_cols][K]
+    __nv_bfloat16* out;       // [T][n_cols]
+    int T, K, n_cols;
+};
+
+__device__ __forceinline__ void ffn_mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2,
+                                        uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, "
+        "{%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+template <int MT, bool GATED, int ACT>
+__global__ void __launch_bounds__(32 * kRowWarps) ffn_rows_kernel(const FfnRowArgs a) {
+    constexpr int NB = GATED ? 2 : 1;
+    __shared__ float red[kRowWarps][MT][NB][16][9];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int g = lane >> 2, q = lane & 3;   // MMA row (and column of B), and 8 k of a block
+    const int blocks = (a.K + 31) / 32, per = (blocks + kRowWarps - 1) / kRowWarps;
+    const int b0 = warp * per, b1 = b0 + per < blocks ? b0 + per : blocks;
+    const int tiles = a.n_cols / 8;
+    const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+    uint4 w[kRowBlocks][NB];
+    auto weights = [&](int tile, int blk) {
+#pragma unroll
+        for (int i = 0; i < kRowBlocks; ++i) {
+            const int k = (blk + i) * 32 + q * 8;
+            const bool in = blk + i < b1 && k < a.K && tile < tiles;
+#pragma unroll
+            for (int n = 0; n < NB; ++n)
+                w[i][n] = in ? *reinterpret_cast<const uint4*>(
+                                   a.B + ((size_t)n * a.n_cols + tile * 8 + g) * a.K + k)
+                             : zero;
+        }
+    };
+    if (!GATED) weights(blockIdx.x, b0);   // written by nobody since the launch before began
+    pdl_wait();
+    pdl_trigger();
+    if (GATED) weights(blockIdx.x, b0);
+    for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        float acc[MT][NB][4] = {};
+        for (int blk = b0; blk < b1; blk += kRowBlocks) {
+            uint4 x[kRowBlocks][MT][2];
+#pragma unroll
+            for (int i = 0; i < kRowBlocks; ++i) {
+                const int k = (blk + i) * 32 + q * 8;
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int t = 16 * m + 8 * h + g;
+                        x[i][m][h] = blk + i < b1 && k < a.K && t < a.T
+                                         ? *reinterpret_cast<const uint4*>(a.A + (size_t)t * a.K + k)
+                                         : zero;
+                    }
+            }
+            uint4 v[kRowBlocks][NB];
+#pragma unroll
+            for (int i = 0; i < kRowBlocks; ++i)
+#pragma unroll
+                for (int n = 0; n < NB; ++n) v[i][n] = w[i][n];
+            // the next blocks' weights, of this tile or the next
+            const bool more = blk + kRowBlocks < b1;
+            weights(more ? tile : tile + (int)gridDim.x, more ? blk + kRowBlocks : b0);
+#pragma unroll
+            for (int i = 0; i < kRowBlocks; ++i)
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int n = 0; n < NB; ++n) {
+                        ffn_mma(acc[m][n], x[i][m][0].x, x[i][m][1].x, x[i][m][0].y, x[i][m][1].y,
+                                v[i][n].x, v[i][n].y);
+                        ffn_mma(acc[m][n], x[i][m][0].z, x[i][m][1].z, x[i][m][0].w, x[i][m][1].w,
+                                v[i][n].z, v[i][n].w);
+                    }
+        }
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int n = 0; n < NB; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    red[warp][m][n][g + 8 * (i >> 1)][2 * q + (i & 1)] = acc[m][n][i];
+        __syncthreads();
+        for (int o = threadIdx.x; o < MT * 128; o += 32 * kRowWarps) {
+            const int m = o >> 7, r = o >> 3 & 15, c = o & 7, t = 16 * m + r;
+            float s[NB];
+#pragma unroll
+            for (int n = 0; n < NB; ++n) {
+                s[n] = red[0][m][n][r][c];
+#pragma unroll
+                for (int k = 1; k < kRowWarps; ++k) s[n] += red[k][m][n][r][c];
+            }
+            const float v = GATED ? ffn_act<ACT>(s[0], nullptr) * s[NB - 1] : s[0];
+            if (t < a.T) a.out[(size_t)t * a.n_cols + tile * 8 + c] = __float2bfloat16_rn(v);
+        }
+        __syncthreads();
+    }
+}
+
 // ------------------------------------------------------------------ host
 typedef CUresult (*FfnEncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*,
                                 const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
@@ -636,6 +753,29 @@ cudaError_t ffn_launch_act(int act, const FfnArgs& a, int pairs, cudaStream_t st
         case HCW_GATE_GELU: return ffn_launch<MODE, HCW_GATE_GELU>(a, pairs, st);
         default: return ffn_launch<MODE, HCW_GATE_RELU>(a, pairs, st);
     }
+}
+
+template <bool GATED, int ACT>
+cudaError_t ffn_rows_launch(const FfnRowArgs& a, cudaStream_t st) {
+    const int tiles = a.n_cols / 8, most = 2 * ffn_sms();
+    const dim3 grid((unsigned)(tiles < most ? tiles : most)), block(32 * kRowWarps);
+    return a.T <= 16 ? launch_pdl(ffn_rows_kernel<1, GATED, ACT>, grid, block, 0, st, a)
+                     : launch_pdl(ffn_rows_kernel<2, GATED, ACT>, grid, block, 0, st, a);
+}
+
+// The forward of a few tokens: two launches.
+int ffn_rows_fwd(const void* x, const void* W1, const void* W2, int T, int d, int h, int act,
+                 void* y, void* ws, cudaStream_t st) {
+    FfnRowArgs a = {static_cast<const __nv_bfloat16*>(x), static_cast<const __nv_bfloat16*>(W1),
+                    static_cast<__nv_bfloat16*>(ws), T, d, h};
+    const int rc = count_launch(act == HCW_GATE_SILU   ? ffn_rows_launch<true, HCW_GATE_SILU>(a, st)
+                                : act == HCW_GATE_GELU ? ffn_rows_launch<true, HCW_GATE_GELU>(a, st)
+                                                       : ffn_rows_launch<true, HCW_GATE_RELU>(a, st),
+                                1);
+    if (rc) return rc;
+    FfnRowArgs b = {static_cast<const __nv_bfloat16*>(ws), static_cast<const __nv_bfloat16*>(W2),
+                    static_cast<__nv_bfloat16*>(y), T, h, d};
+    return count_launch(ffn_rows_launch<false, 0>(b, st), 1);
 }
 
 // One product of a gemm launch, as the planner sees it.
@@ -845,6 +985,7 @@ extern "C" {
 
 size_t hcw_gated_ffn_fwd_workspace_bytes(int T, int d, int h) {
     if (T < 1 || ffn_sizes(T, d, h, HCW_GATE_SILU)) return 0;
+    if (T <= kRowMax) return ffn_round((size_t)T * h * 2);
     const FfnShape s = ffn_down_shape(T, d, h);
     return ffn_round((size_t)T * h * 2) + ffn_part_bytes(&s, 1);
 }
@@ -860,10 +1001,14 @@ int hcw_gated_ffn_fwd(const void* x, const void* W1, const void* W2, int T, int 
     if (rc) return rc;
     if (T == 0) return HCW_OK;
     if (!x || !W1 || !W2 || !y) return HCW_ERR_INVALID_ARG;
-    FfnShape s = ffn_down_shape(T, d, h);
     const size_t act_bytes = ffn_round((size_t)T * h * 2);
-    if (!workspace || ws_bytes < act_bytes + ffn_part_bytes(&s, 1)) return HCW_ERR_WORKSPACE;
     const cudaStream_t st = (cudaStream_t)stream;
+    if (T <= kRowMax) {
+        if (!workspace || ws_bytes < act_bytes) return HCW_ERR_WORKSPACE;
+        return ffn_rows_fwd(x, W1, W2, T, d, h, act, y, workspace, st);
+    }
+    FfnShape s = ffn_down_shape(T, d, h);
+    if (!workspace || ws_bytes < act_bytes + ffn_part_bytes(&s, 1)) return HCW_ERR_WORKSPACE;
     const int pairs = ffn_sms() / 2;
     FfnArgs a;
     memset(&a, 0, sizeof(a));
