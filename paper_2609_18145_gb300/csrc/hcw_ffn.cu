@@ -317,13 +317,17 @@ __global__ void __launch_bounds__(kFThreads, 1) ffn_pair_kernel(const __grid_con
         const int e = warp - 2;
         const int quarter = warp & 3, chalf = e >> 2;
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
-        // Patches of 32 rows x 64 bytes (64-byte swizzle) in a ring: one is filled when the
-        // store that was issued from it kPatches stores ago has read it.
+        // Patches of 32 rows x 64 bytes (64-byte swizzle) in a ring.  kTaken of them are
+        // filled before the next store is issued, so all but the last kPatches - kTaken stores
+        // have to have read theirs first.
         uint8_t* const patches = staging + (size_t)e * kPatches * kFPatch;
         int nbuf = 0;
-        auto patch = [&]() {
-            if (lane == 0) bulk_wait_read<kPatches - 1>();
+        constexpr int kTaken = MODE == FFN_GRAD ? 3 : 1;
+        auto patches_free = [&]() {
+            if (lane == 0) bulk_wait_read<kPatches - kTaken>();
             __syncwarp();
+        };
+        auto patch = [&]() {
             uint8_t* buf = patches + nbuf * kFPatch;
             nbuf = nbuf + 1 == kPatches ? 0 : nbuf + 1;
             return buf;
@@ -374,6 +378,7 @@ __global__ void __launch_bounds__(kFThreads, 1) ffn_pair_kernel(const __grid_con
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
                             if (colw + c + 16 * h >= p.N) break;   // warp-uniform
+                            patches_free();
                             uint8_t* buf = patch();
 #pragma unroll
                             for (int m = 0; m < 4; ++m)
@@ -387,6 +392,7 @@ __global__ void __launch_bounds__(kFThreads, 1) ffn_pair_kernel(const __grid_con
                             }
                         }
                     } else {
+                        patches_free();
                         uint8_t* buf = patch();
 #pragma unroll
                         for (int m = 0; m < 4; ++m) {
@@ -420,6 +426,7 @@ __global__ void __launch_bounds__(kFThreads, 1) ffn_pair_kernel(const __grid_con
                     tmem_ld_wait_regs(u);
                     if (c) release();
                     if (col + c >= a.h) continue;   // warp-uniform
+                    patches_free();
                     uint8_t* buf = patch();
 #pragma unroll
                     for (int m = 0; m < 4; ++m) {
@@ -451,6 +458,7 @@ __global__ void __launch_bounds__(kFThreads, 1) ffn_pair_kernel(const __grid_con
                     tmem_ld_wait_regs(u);
                     if (c) release();
                     if (col + c >= a.h) continue;   // warp-uniform
+                    patches_free();
                     uint8_t *const bg = patch(), *const bu = patch(), *const ba = patch();
 #pragma unroll
                     for (int m = 0; m < 4; ++m) {
@@ -535,22 +543,30 @@ __global__ void __launch_bounds__(256) ffn_reduce_kernel(const FfnReduce a) {
 // ------------------------------------------------------------------ few tokens
 // out[t][n] = sum_k A[t][k] B[n][k] over T <= 16 MT rows, or with GATED the gate and up
 // sums of B's rows n and n_cols + n and act(g) u.  Bound by reading B once (the weights), and
-// for narrow blocks by latency: a CTA takes 8 columns, its 8 warps a slice of K each with the
-// warp-level MMA (16 rows x 8 columns x 16; a slab of tcgen05's 128 rows would be empty
-// but for a few), four 32-wide blocks of weights in flight a lane; the warps' sums are added
-// in warp order.  A lane's 16 bytes of 8 neighbouring k stand for the MMA's k in any order,
-// the same for both operands.  The second product's launch reads its first weights before it
-// waits for the first's.
-constexpr int kRowWarps = 8;
-constexpr int kRowBlocks = 4;      // 32-wide blocks of K a lane has in flight
+// for narrow blocks by latency.  A CTA (one an SM) takes 8 columns at a time; their weights
+// come through a ring in shared memory (bulk copies of row pieces of up to 1024 k, as many on
+// their way as fit), and its 16 warps contract a slice of each piece with the warp-level MMA
+// (16 rows x 8 columns x 16; of tcgen05's 128 rows all but a few would be empty).  The warps'
+// sums are added in warp order.  A lane's 16 bytes of 8 neighbouring k stand for the MMA's
+// k in an order of their own, the same for both operands.  The second product's launch
+// starts its ring before it waits for the first's.
+constexpr int kRowWarps = 16;
 constexpr int kRowMax = 32;        // tokens
+constexpr int kRowPiece = 1024;    // k of a piece at most
+constexpr int kRowMaxBufs = 8;
 
 struct FfnRowArgs {
     const __nv_bfloat16* A;   // [T][K]
     const __nv_bfloat16* B;   // [n_cols][K], GATED: [2 n_cols][K]
     __nv_bfloat16* out;       // [T][n_cols]
     int T, K, n_cols;
+    int kc, pieces;           // k of a piece (a multiple of 32), pieces of a row
+    int bufs;
 };
+
+// shared memory bytes from one row of a piece to the next: 64 beside the row, so that the MMA
+// lanes' 16-byte reads of neighbouring rows fall into different banks
+__host__ __device__ constexpr int ffn_row_stride(int kc) { return kc * 2 + 64; }
 
 __device__ __forceinline__ void ffn_mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2,
                                         uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -562,90 +578,145 @@ __device__ __forceinline__ void ffn_mma(float (&c)[4], uint32_t a0, uint32_t a1,
 }
 
 template <int MT, bool GATED, int ACT>
-__global__ void __launch_bounds__(32 * kRowWarps) ffn_rows_kernel(const FfnRowArgs a) {
+__global__ void __launch_bounds__(32 * kRowWarps + 32) ffn_rows_kernel(const FfnRowArgs a) {
     constexpr int NB = GATED ? 2 : 1;
-    __shared__ float red[kRowWarps][MT][NB][16][9];
+    constexpr int kRed = MT * NB * 16 * 9;        // floats of a warp's sums
+    extern __shared__ __align__(128) uint8_t row_smem[];
+    __shared__ uint64_t full[kRowMaxBufs], empty[kRowMaxBufs];
+    __shared__ volatile int gave_up, verdict[2];   // verdict: gave_up as a tile's barrier saw it
+    float* const sums = reinterpret_cast<float*>(row_smem);   // [2][kRowWarps][kRed]
+    uint8_t* const ring = row_smem + 2 * kRowWarps * kRed * sizeof(float);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int g = lane >> 2, q = lane & 3;   // MMA row (and column of B), and 8 k of a block
-    const int blocks = (a.K + 31) / 32, per = (blocks + kRowWarps - 1) / kRowWarps;
-    const int b0 = warp * per, b1 = b0 + per < blocks ? b0 + per : blocks;
     const int tiles = a.n_cols / 8;
-    const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-    uint4 w[kRowBlocks][NB];
-    auto weights = [&](int tile, int blk) {
-#pragma unroll
-        for (int i = 0; i < kRowBlocks; ++i) {
-            const int k = (blk + i) * 32 + q * 8;
-            const bool in = blk + i < b1 && k < a.K && tile < tiles;
-#pragma unroll
-            for (int n = 0; n < NB; ++n)
-                w[i][n] = in ? *reinterpret_cast<const uint4*>(
-                                   a.B + ((size_t)n * a.n_cols + tile * 8 + g) * a.K + k)
-                             : zero;
+    const int stride = ffn_row_stride(a.kc), buf_bytes = NB * 8 * stride;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < a.bufs; ++i) {
+            mbar_init(&full[i], 1);
+            mbar_init(&empty[i], kRowWarps);
         }
-    };
-    if (!GATED) weights(blockIdx.x, b0);   // written by nobody since the launch before began
+        gave_up = 0;
+        fence_mbar_init();
+    }
+    __syncthreads();
+    if (warp == kRowWarps) {
+        // producer: a lane a row
+        int buf = 0, n_bufs = 0, done = 0;
+        uint32_t round = 0;
+        bool ok = true;
+        if (GATED) pdl_wait();   // (without: weights, written by nobody since the launch before began)
+        for (int tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x)
+            for (int piece = 0; piece < a.pieces; ++piece) {
+                bool w = true;
+                if (round) w = mbar_wait(&empty[buf], (round & 1) ^ 1, &gave_up, kFTimeoutNs);
+                ok = __all_sync(0xffffffffu, w);
+                if (!ok) break;
+                const int k = piece * a.kc, n = a.K - k < a.kc ? a.K - k : a.kc;
+                if (lane == 0) mbar_arrive_expect_tx(&full[buf], (uint32_t)(NB * 8 * n * 2));
+                __syncwarp();
+                if (lane < NB * 8)
+                    asm volatile(
+                        "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes "
+                        "[%0], [%1], %2, [%3];" ::"r"(smem_u32(ring + buf * buf_bytes + lane * stride)),
+                        "l"(a.B + ((size_t)(lane >> 3) * a.n_cols + tile * 8 + (lane & 7)) * a.K + k),
+                        "r"((uint32_t)(n * 2)), "r"(smem_u32(&full[buf]))
+                        : "memory");
+                if (n_bufs < a.bufs) ++n_bufs;
+                ++done;
+                if (++buf == a.bufs) {
+                    buf = 0;
+                    ++round;
+                }
+            }
+        if (!GATED) pdl_wait();
+        // every copy has landed before the CTA leaves, also when the others gave up
+        if (lane == 0)
+            for (int i = 0; i < n_bufs; ++i)
+                mbar_wait_drain(&full[i], ((done - 1 - i) / a.bufs) & 1, kFTimeoutNs);
+        return;
+    }
     pdl_wait();
     pdl_trigger();
-    if (GATED) weights(blockIdx.x, b0);
-    for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+    const int per = a.kc / 32 + kRowWarps - 1 >> 4;   // blocks of 32 k of a piece a warp takes
+    const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+    int b = 0, round = 0, parity = 0;
+    bool ok = true;
+    for (int tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x, parity ^= 1) {
         float acc[MT][NB][4] = {};
-        for (int blk = b0; blk < b1; blk += kRowBlocks) {
-            uint4 x[kRowBlocks][MT][2];
-#pragma unroll
-            for (int i = 0; i < kRowBlocks; ++i) {
-                const int k = (blk + i) * 32 + q * 8;
+        for (int piece = 0; piece < a.pieces; ++piece) {
+            const int k0 = piece * a.kc + warp * per * 32 + q * 8;
+            const uint8_t* buf = ring + b * buf_bytes + g * stride + (warp * per * 32 + q * 8) * 2;
+            // this warp's rows of A: from L1 after the first tile
+            auto rows = [&](uint4 (&x)[MT][2], int i) {
 #pragma unroll
                 for (int m = 0; m < MT; ++m)
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        const int t = 16 * m + 8 * h + g;
-                        x[i][m][h] = blk + i < b1 && k < a.K && t < a.T
-                                         ? *reinterpret_cast<const uint4*>(a.A + (size_t)t * a.K + k)
-                                         : zero;
+                        const int t = 16 * m + 8 * h + g, k = k0 + 32 * i;
+                        x[m][h] = i < per && warp * per + i < a.kc / 32 && k < a.K && t < a.T
+                                      ? *reinterpret_cast<const uint4*>(a.A + (size_t)t * a.K + k)
+                                      : zero;
                     }
-            }
-            uint4 v[kRowBlocks][NB];
+            };
+            uint4 x[MT][2];
+            rows(x, 0);
+            const bool okw = mbar_wait(&full[b], round & 1, &gave_up, kFTimeoutNs);
+            ok = __all_sync(0xffffffffu, okw);
+            if (!ok) break;
+            for (int i = 0; i < per; ++i) {
+                uint4 y[MT][2];
+                rows(y, i + 1);
+                // past the row's end (or the warp's share) A is zero, B nothing that was read
+                const bool in = warp * per + i < a.kc / 32 && k0 + 32 * i < a.K;
 #pragma unroll
-            for (int i = 0; i < kRowBlocks; ++i)
+                for (int n = 0; n < NB; ++n) {
+                    const uint4 v = in ? *reinterpret_cast<const uint4*>(buf + n * 8 * stride + i * 64)
+                                       : zero;
 #pragma unroll
-                for (int n = 0; n < NB; ++n) v[i][n] = w[i][n];
-            // the next blocks' weights, of this tile or the next
-            const bool more = blk + kRowBlocks < b1;
-            weights(more ? tile : tile + (int)gridDim.x, more ? blk + kRowBlocks : b0);
-#pragma unroll
-            for (int i = 0; i < kRowBlocks; ++i)
+                    for (int m = 0; m < MT; ++m) {
+                        ffn_mma(acc[m][n], x[m][0].x, x[m][1].x, x[m][0].y, x[m][1].y, v.x, v.y);
+                        ffn_mma(acc[m][n], x[m][0].z, x[m][1].z, x[m][0].w, x[m][1].w, v.z, v.w);
+                    }
+                }
 #pragma unroll
                 for (int m = 0; m < MT; ++m)
 #pragma unroll
-                    for (int n = 0; n < NB; ++n) {
-                        ffn_mma(acc[m][n], x[i][m][0].x, x[i][m][1].x, x[i][m][0].y, x[i][m][1].y,
-                                v[i][n].x, v[i][n].y);
-                        ffn_mma(acc[m][n], x[i][m][0].z, x[i][m][1].z, x[i][m][0].w, x[i][m][1].w,
-                                v[i][n].z, v[i][n].w);
-                    }
+                    for (int h = 0; h < 2; ++h) x[m][h] = y[m][h];
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&empty[b]);
+            if (++b == a.bufs) {
+                b = 0;
+                ++round;
+            }
         }
+        float* const red = sums + parity * kRowWarps * kRed;
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
             for (int n = 0; n < NB; ++n)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    red[warp][m][n][g + 8 * (i >> 1)][2 * q + (i & 1)] = acc[m][n][i];
-        __syncthreads();
-        for (int o = threadIdx.x; o < MT * 128; o += 32 * kRowWarps) {
-            const int m = o >> 7, r = o >> 3 & 15, c = o & 7, t = 16 * m + r;
+                    red[warp * kRed + ((m * NB + n) * 16 + g + 8 * (i >> 1)) * 9 + 2 * q + (i & 1)] =
+                        acc[m][n][i];
+        // (two buffers: whoever fills this one again has passed the next tile's barrier, which
+        // this tile's readers pass after reading)
+        if (threadIdx.x == 0) verdict[parity] = gave_up;
+        named_bar_sync(1, 32 * kRowWarps);
+        ok = !verdict[parity];
+        if (ok && (int)threadIdx.x < MT * 128) {
+            const int o = threadIdx.x, m = o >> 7, r = o >> 3 & 15, c = o & 7, t = 16 * m + r;
             float s[NB];
 #pragma unroll
             for (int n = 0; n < NB; ++n) {
-                s[n] = red[0][m][n][r][c];
+                const float* p = red + ((m * NB + n) * 16 + r) * 9 + c;
+                s[n] = p[0];
 #pragma unroll
-                for (int k = 1; k < kRowWarps; ++k) s[n] += red[k][m][n][r][c];
+                for (int k = 1; k < kRowWarps; ++k) s[n] += p[k * kRed];
             }
             const float v = GATED ? ffn_act<ACT>(s[0], nullptr) * s[NB - 1] : s[0];
             if (t < a.T) a.out[(size_t)t * a.n_cols + tile * 8 + c] = __float2bfloat16_rn(v);
         }
-        __syncthreads();
     }
 }
 
@@ -755,26 +826,54 @@ cudaError_t ffn_launch_act(int act, const FfnArgs& a, int pairs, cudaStream_t st
     }
 }
 
+template <int MT, bool GATED, int ACT>
+cudaError_t ffn_rows_launch_mt(FfnRowArgs a, cudaStream_t st) {
+    auto kern = ffn_rows_kernel<MT, GATED, ACT>;
+    constexpr size_t sums = 2 * kRowWarps * MT * (GATED ? 2 : 1) * 16 * 9 * sizeof(float);
+    constexpr size_t room = 232448 - 1024;   // beside the barriers
+    static std::once_flag once[64];
+    static cudaError_t set_err[64];
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+    std::call_once(once[dev], [&] {
+        set_err[dev] =
+            cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)room);
+    });
+    if (set_err[dev] != cudaSuccess) return set_err[dev];
+    a.pieces = (a.K + kRowPiece - 1) / kRowPiece;
+    a.kc = ((a.K + a.pieces - 1) / a.pieces + 31) / 32 * 32;
+    a.pieces = (a.K + a.kc - 1) / a.kc;
+    const size_t buf = (size_t)(GATED ? 16 : 8) * ffn_row_stride(a.kc);
+    const int tiles = a.n_cols / 8, most = ffn_sms();
+    const int grid = tiles < most ? tiles : most;
+    const int work = (tiles + grid - 1) / grid * a.pieces;   // pieces of a CTA
+    a.bufs = (int)((room - sums) / buf);
+    if (a.bufs > work) a.bufs = work;
+    if (a.bufs > kRowMaxBufs) a.bufs = kRowMaxBufs;
+    return launch_pdl(kern, dim3((unsigned)grid), dim3(32 * kRowWarps + 32),
+                      sums + a.bufs * buf, st, a);
+}
+
 template <bool GATED, int ACT>
 cudaError_t ffn_rows_launch(const FfnRowArgs& a, cudaStream_t st) {
-    const int tiles = a.n_cols / 8, most = 2 * ffn_sms();
-    const dim3 grid((unsigned)(tiles < most ? tiles : most)), block(32 * kRowWarps);
-    return a.T <= 16 ? launch_pdl(ffn_rows_kernel<1, GATED, ACT>, grid, block, 0, st, a)
-                     : launch_pdl(ffn_rows_kernel<2, GATED, ACT>, grid, block, 0, st, a);
+    return a.T <= 16 ? ffn_rows_launch_mt<1, GATED, ACT>(a, st)
+                     : ffn_rows_launch_mt<2, GATED, ACT>(a, st);
 }
 
 // The forward of a few tokens: two launches.
 int ffn_rows_fwd(const void* x, const void* W1, const void* W2, int T, int d, int h, int act,
                  void* y, void* ws, cudaStream_t st) {
     FfnRowArgs a = {static_cast<const __nv_bfloat16*>(x), static_cast<const __nv_bfloat16*>(W1),
-                    static_cast<__nv_bfloat16*>(ws), T, d, h};
+                    static_cast<__nv_bfloat16*>(ws), T, d, h, 0, 0, 0};
     const int rc = count_launch(act == HCW_GATE_SILU   ? ffn_rows_launch<true, HCW_GATE_SILU>(a, st)
                                 : act == HCW_GATE_GELU ? ffn_rows_launch<true, HCW_GATE_GELU>(a, st)
                                                        : ffn_rows_launch<true, HCW_GATE_RELU>(a, st),
                                 1);
     if (rc) return rc;
     FfnRowArgs b = {static_cast<const __nv_bfloat16*>(ws), static_cast<const __nv_bfloat16*>(W2),
-                    static_cast<__nv_bfloat16*>(y), T, h, d};
+                    static_cast<__nv_bfloat16*>(y), T, h, d, 0, 0, 0};
     return count_launch(ffn_rows_launch<false, 0>(b, st), 1);
 }
 
