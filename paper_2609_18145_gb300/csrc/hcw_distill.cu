@@ -896,14 +896,6 @@ __global__ void __launch_bounds__(NT + 32 + 32 * slot_warps(NT), NT == 512 ? 1 :
     cluster_sync_all();
 }
 
-int distill_sms() {
-    int dev = 0, n = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess ||
-        cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1)
-        return 148;
-    return n;
-}
-
 template <typename T, int NT, int EXPS>
 cudaError_t launch_distill_rows(const DistillArgs& a, DistillPlan pl, cudaStream_t st) {
     auto kern = distill_row_kernel<T, NT, EXPS>;
@@ -964,7 +956,7 @@ cudaError_t launch_distill(const DistillArgs& a, cudaStream_t st) {
         if (a.V <= 256) return launch_pdl(distill_warp_kernel<T, 8, EXPS>, grid, block, 0, st, a);
         return launch_pdl(distill_warp_kernel<T, 32, EXPS>, grid, block, 0, st, a);
     }
-    const int sms = distill_sms();
+    const int sms = device_sms();
     const long long bytes = (long long)a.V * (int)sizeof(T) + 32;
     DistillPlan pl;
     // the fewest CTAs a row whose slices fit 64 KB (8 at most); more while the rows alone

@@ -544,15 +544,15 @@ __global__ void __launch_bounds__(256) ffn_reduce_kernel(const FfnReduce a) {
 // out[t][n] = sum_k A[t][k] B[n][k] over T <= 16 MT rows, or with GATED the gate and up
 // sums of B's rows n and n_cols + n and act(g) u.  Bound by reading B once (the weights), and
 // for narrow blocks by latency.  A CTA (one an SM) takes 8 columns at a time; their weights
-// come through a ring in shared memory (bulk copies of row pieces of up to 1024 k, as many on
+// come through a ring in shared memory (bulk copies of row pieces of up to 2048 k, as many on
 // their way as fit), and its 16 warps contract a slice of each piece with the warp-level MMA
 // (16 rows x 8 columns x 16; of tcgen05's 128 rows all but a few would be empty).  The warps'
 // sums are added in warp order.  A lane's 16 bytes of 8 neighbouring k stand for the MMA's
 // k in an order of their own, the same for both operands.  The second product's launch
 // starts its ring before it waits for the first's.
 constexpr int kRowWarps = 16;
-constexpr int kRowMax = 32;        // tokens
-constexpr int kRowPiece = 1024;    // k of a piece at most
+constexpr int kRowMax = 32;        // tokens at most
+constexpr int kRowPiece = 2048;    // k of a piece at most
 constexpr int kRowMaxBufs = 8;
 
 struct FfnRowArgs {
@@ -562,6 +562,8 @@ struct FfnRowArgs {
     int T, K, n_cols;
     int kc, pieces;           // k of a piece (a multiple of 32), pieces of a row
     int bufs;
+    int resident;             // A in shared memory, its rows a_stride bytes apart
+    int a_stride;
 };
 
 // shared memory bytes from one row of a piece to the next: 64 beside the row, so that the MMA
@@ -582,7 +584,7 @@ __global__ void __launch_bounds__(32 * kRowWarps + 32) ffn_rows_kernel(const Ffn
     constexpr int NB = GATED ? 2 : 1;
     constexpr int kRed = MT * NB * 16 * 9;        // floats of a warp's sums
     extern __shared__ __align__(128) uint8_t row_smem[];
-    __shared__ uint64_t full[kRowMaxBufs], empty[kRowMaxBufs];
+    __shared__ uint64_t full[kRowMaxBufs], empty[kRowMaxBufs], a_full;
     __shared__ volatile int gave_up, verdict[2];   // verdict: gave_up as a tile's barrier saw it
     float* const sums = reinterpret_cast<float*>(row_smem);   // [2][kRowWarps][kRed]
     uint8_t* const ring = row_smem + 2 * kRowWarps * kRed * sizeof(float);
@@ -595,20 +597,42 @@ __global__ void __launch_bounds__(32 * kRowWarps + 32) ffn_rows_kernel(const Ffn
             mbar_init(&full[i], 1);
             mbar_init(&empty[i], kRowWarps);
         }
+        mbar_init(&a_full, 1);
         gave_up = 0;
         fence_mbar_init();
     }
     __syncthreads();
+    uint8_t* const a_mem = ring + a.bufs * buf_bytes;
     if (warp == kRowWarps) {
         // producer: a lane a row
         int buf = 0, n_bufs = 0, done = 0;
         uint32_t round = 0;
-        bool ok = true;
-        if (GATED) pdl_wait();   // (without: weights, written by nobody since the launch before began)
+        bool ok = true, a_done = false;
+        // the rows of A, which the kernel before may still be writing
+        auto rows_of_a = [&]() {
+            if (a_done) return;
+            a_done = true;
+            pdl_wait();
+            if (!a.resident) return;
+            if (lane == 0) mbar_arrive_expect_tx(&a_full, (uint32_t)(a.T * a.K * 2));
+            __syncwarp();
+            if (lane < a.T)
+                asm volatile(
+                    "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes "
+                    "[%0], [%1], %2, [%3];" ::"r"(smem_u32(a_mem + lane * a.a_stride)),
+                    "l"(a.A + (size_t)lane * a.K), "r"((uint32_t)(a.K * 2)), "r"(smem_u32(&a_full))
+                    : "memory");
+        };
+        // (the second product: first as many weights as the ring holds, which nobody has
+        // written since the launch before this one began)
+        if (GATED) rows_of_a();
         for (int tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x)
             for (int piece = 0; piece < a.pieces; ++piece) {
                 bool w = true;
-                if (round) w = mbar_wait(&empty[buf], (round & 1) ^ 1, &gave_up, kFTimeoutNs);
+                if (round) {
+                    rows_of_a();
+                    w = mbar_wait(&empty[buf], (round & 1) ^ 1, &gave_up, kFTimeoutNs);
+                }
                 ok = __all_sync(0xffffffffu, w);
                 if (!ok) break;
                 const int k = piece * a.kc, n = a.K - k < a.kc ? a.K - k : a.kc;
@@ -628,11 +652,13 @@ __global__ void __launch_bounds__(32 * kRowWarps + 32) ffn_rows_kernel(const Ffn
                     ++round;
                 }
             }
-        if (!GATED) pdl_wait();
+        rows_of_a();
         // every copy has landed before the CTA leaves, also when the others gave up
-        if (lane == 0)
+        if (lane == 0) {
             for (int i = 0; i < n_bufs; ++i)
                 mbar_wait_drain(&full[i], ((done - 1 - i) / a.bufs) & 1, kFTimeoutNs);
+            if (a.resident) mbar_wait_drain(&a_full, 0, kFTimeoutNs);
+        }
         return;
     }
     pdl_wait();
@@ -641,12 +667,14 @@ __global__ void __launch_bounds__(32 * kRowWarps + 32) ffn_rows_kernel(const Ffn
     const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
     int b = 0, round = 0, parity = 0;
     bool ok = true;
-    for (int tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x, parity ^= 1) {
+    const uint8_t* const rows_at = a.resident ? a_mem : reinterpret_cast<const uint8_t*>(a.A);
+    if (a.resident) ok = __all_sync(0xffffffffu, mbar_wait(&a_full, 0, &gave_up, kFTimeoutNs));
+    for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x, parity ^= 1) {
         float acc[MT][NB][4] = {};
-        for (int piece = 0; piece < a.pieces; ++piece) {
+        for (int piece = 0; piece < a.pieces && ok; ++piece) {
             const int k0 = piece * a.kc + warp * per * 32 + q * 8;
             const uint8_t* buf = ring + b * buf_bytes + g * stride + (warp * per * 32 + q * 8) * 2;
-            // this warp's rows of A: from L1 after the first tile
+            // this warp's part of the rows of A
             auto rows = [&](uint4 (&x)[MT][2], int i) {
 #pragma unroll
                 for (int m = 0; m < MT; ++m)
@@ -654,7 +682,7 @@ __global__ void __launch_bounds__(32 * kRowWarps + 32) ffn_rows_kernel(const Ffn
                     for (int h = 0; h < 2; ++h) {
                         const int t = 16 * m + 8 * h + g, k = k0 + 32 * i;
                         x[m][h] = i < per && warp * per + i < a.kc / 32 && k < a.K && t < a.T
-                                      ? *reinterpret_cast<const uint4*>(a.A + (size_t)t * a.K + k)
+                                      ? *reinterpret_cast<const uint4*>(rows_at + t * a.a_stride + k * 2)
                                       : zero;
                     }
             };
@@ -704,7 +732,8 @@ __global__ void __launch_bounds__(32 * kRowWarps + 32) ffn_rows_kernel(const Ffn
         if (threadIdx.x == 0) verdict[parity] = gave_up;
         named_bar_sync(1, 32 * kRowWarps);
         ok = !verdict[parity];
-        if (ok && (int)threadIdx.x < MT * 128) {
+        if (!ok) break;
+        if ((int)threadIdx.x < MT * 128) {
             const int o = threadIdx.x, m = o >> 7, r = o >> 3 & 15, c = o & 7, t = 16 * m + r;
             float s[NB];
 #pragma unroll
@@ -773,14 +802,6 @@ bool ffn_map_f32(CUtensorMap* m, void* base, int M, int N, int splits) {
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-int ffn_sms() {
-    int dev = 0, n = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess ||
-        cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 2)
-        return 148;
-    return n;
-}
-
 // An operand: K-major (the row-major [outer][K] matrix) or MN-major (row-major [K][outer]).
 bool ffn_operand(CUtensorMap* m, const void* base, long long outer, long long K, bool mn, int rows) {
     return mn ? ffn_map(m, base, K, outer, outer, 64, 64) : ffn_map(m, base, outer, K, K, 64, rows);
@@ -845,15 +866,21 @@ cudaError_t ffn_rows_launch_mt(FfnRowArgs a, cudaStream_t st) {
     a.pieces = (a.K + kRowPiece - 1) / kRowPiece;
     a.kc = ((a.K + a.pieces - 1) / a.pieces + 31) / 32 * 32;
     a.pieces = (a.K + a.kc - 1) / a.kc;
+    // A stays in shared memory where it leaves the ring half of it
+    a.a_stride = ffn_row_stride(a.K);
+    const size_t rows = (size_t)a.T * a.a_stride;
+    a.resident = rows <= (room - sums) / 2;
+    if (!a.resident) a.a_stride = a.K * 2;
+    const size_t kept = a.resident ? rows : 0;
     const size_t buf = (size_t)(GATED ? 16 : 8) * ffn_row_stride(a.kc);
-    const int tiles = a.n_cols / 8, most = ffn_sms();
+    const int tiles = a.n_cols / 8, most = device_sms();
     const int grid = tiles < most ? tiles : most;
     const int work = (tiles + grid - 1) / grid * a.pieces;   // pieces of a CTA
-    a.bufs = (int)((room - sums) / buf);
+    a.bufs = (int)((room - sums - kept) / buf);
     if (a.bufs > work) a.bufs = work;
     if (a.bufs > kRowMaxBufs) a.bufs = kRowMaxBufs;
     return launch_pdl(kern, dim3((unsigned)grid), dim3(32 * kRowWarps + 32),
-                      sums + a.bufs * buf, st, a);
+                      sums + a.bufs * buf + kept, st, a);
 }
 
 template <bool GATED, int ACT>
@@ -862,18 +889,27 @@ cudaError_t ffn_rows_launch(const FfnRowArgs& a, cudaStream_t st) {
                      : ffn_rows_launch_mt<2, GATED, ACT>(a, st);
 }
 
+// Whether the rows kernels are the faster way (us a forward, rows kernels and SM pairs:
+// T = 1, d = 512, h = 1024: 6.2, 14.9; 32, 512, 1024: 8.3, 15.2; 1, 2048, 5632: 18, 33;
+// 16, 2048, 5632: 22, 27; 32, 2048, 5632: 38, 25; 32, 1024, 4096: 18.6, 19.4;
+// 8, 4096, 14336: 88, 88; 16, 4096, 14336: 102, 78).
+bool ffn_few(int T, int d, int h) {
+    const double work = (double)T * d * h;
+    return T <= 16 ? work <= 1 << 28 : T <= kRowMax && work <= 1 << 27;
+}
+
 // The forward of a few tokens: two launches.
 int ffn_rows_fwd(const void* x, const void* W1, const void* W2, int T, int d, int h, int act,
                  void* y, void* ws, cudaStream_t st) {
     FfnRowArgs a = {static_cast<const __nv_bfloat16*>(x), static_cast<const __nv_bfloat16*>(W1),
-                    static_cast<__nv_bfloat16*>(ws), T, d, h, 0, 0, 0};
+                    static_cast<__nv_bfloat16*>(ws), T, d, h, 0, 0, 0, 0, 0};
     const int rc = count_launch(act == HCW_GATE_SILU   ? ffn_rows_launch<true, HCW_GATE_SILU>(a, st)
                                 : act == HCW_GATE_GELU ? ffn_rows_launch<true, HCW_GATE_GELU>(a, st)
                                                        : ffn_rows_launch<true, HCW_GATE_RELU>(a, st),
                                 1);
     if (rc) return rc;
     FfnRowArgs b = {static_cast<const __nv_bfloat16*>(ws), static_cast<const __nv_bfloat16*>(W2),
-                    static_cast<__nv_bfloat16*>(y), T, h, d, 0, 0, 0};
+                    static_cast<__nv_bfloat16*>(y), T, h, d, 0, 0, 0, 0, 0};
     return count_launch(ffn_rows_launch<false, 0>(b, st), 1);
 }
 
@@ -996,7 +1032,7 @@ int ffn_gemms(const FfnShape* s, const FfnOperands* o, int n, uint8_t* part, cud
     a.n_prod = n;
     a.n_units = units;
     a.timeout_ns = kFTimeoutNs;
-    const int sms = ffn_sms();
+    const int sms = device_sms();
     int rc = count_launch(ffn_launch<FFN_GEMM, 0>(a, units < sms / 2 ? units : sms / 2, st), 1);
     if (rc || !n_red) return rc;
     const size_t want = (most + 255) / 256, cap = (size_t)sms * 8;
@@ -1004,10 +1040,37 @@ int ffn_gemms(const FfnShape* s, const FfnOperands* o, int n, uint8_t* part, cud
                                    dim3(256), 0, st, r), 1);
 }
 
+// The plan of these products, kept by its sizes: the thread's last few (a plan costs a few us
+// of the host's time, and a training step or a served model repeats the same ones).
+void ffn_plan_kept(FfnShape* s, int n, int pairs) {
+    struct Entry {
+        FfnShape s[3];
+        int n, pairs;
+    };
+    constexpr int kEntries = 8;
+    thread_local Entry kept[kEntries];
+    thread_local int next = 0;
+    for (const Entry& e : kept) {
+        bool same = e.n == n && e.pairs == pairs;
+        for (int i = 0; i < n && same; ++i)
+            same = e.s[i].M == s[i].M && e.s[i].N == s[i].N && e.s[i].K == s[i].K &&
+                   e.s[i].out_f32 == s[i].out_f32;
+        if (!same) continue;
+        for (int i = 0; i < n; ++i) s[i] = e.s[i];
+        return;
+    }
+    ffn_plan(s, n, pairs);
+    Entry& e = kept[next];
+    next = (next + 1) % kEntries;
+    e.n = n;
+    e.pairs = pairs;
+    for (int i = 0; i < n; ++i) e.s[i] = s[i];
+}
+
 // Forward workspace: a [T][h] bf16, then the partial sums of y.
 FfnShape ffn_down_shape(int T, int d, int h) {
     FfnShape s = {T, d, h, 0, 0, 0, 0, 0};
-    ffn_plan(&s, 1, ffn_sms() / 2);
+    ffn_plan_kept(&s, 1, device_sms() / 2);
     return s;
 }
 
@@ -1025,7 +1088,7 @@ FfnBwdWs ffn_bwd_ws(int T, int d, int h, bool dx, bool dw, bool f32) {
         w.s[w.n++] = {2ll * h, d, T, f32, 0, 0, 0, 0};
         w.s[w.n++] = {d, h, T, f32, 0, 0, 0, 0};
     }
-    ffn_plan(w.s, w.n, ffn_sms() / 2);
+    ffn_plan_kept(w.s, w.n, device_sms() / 2);
     w.act = ffn_round((size_t)T * 2 * h * 2);
     w.part = w.act + ffn_round((size_t)T * h * 2);
     w.bytes = w.part + ffn_part_bytes(w.s, w.n);
@@ -1084,7 +1147,7 @@ extern "C" {
 
 size_t hcw_gated_ffn_fwd_workspace_bytes(int T, int d, int h) {
     if (T < 1 || ffn_sizes(T, d, h, HCW_GATE_SILU)) return 0;
-    if (T <= kRowMax) return ffn_round((size_t)T * h * 2);
+    if (ffn_few(T, d, h)) return ffn_round((size_t)T * h * 2);
     const FfnShape s = ffn_down_shape(T, d, h);
     return ffn_round((size_t)T * h * 2) + ffn_part_bytes(&s, 1);
 }
@@ -1102,13 +1165,13 @@ int hcw_gated_ffn_fwd(const void* x, const void* W1, const void* W2, int T, int 
     if (!x || !W1 || !W2 || !y) return HCW_ERR_INVALID_ARG;
     const size_t act_bytes = ffn_round((size_t)T * h * 2);
     const cudaStream_t st = (cudaStream_t)stream;
-    if (T <= kRowMax) {
+    if (ffn_few(T, d, h)) {
         if (!workspace || ws_bytes < act_bytes) return HCW_ERR_WORKSPACE;
         return ffn_rows_fwd(x, W1, W2, T, d, h, act, y, workspace, st);
     }
     FfnShape s = ffn_down_shape(T, d, h);
     if (!workspace || ws_bytes < act_bytes + ffn_part_bytes(&s, 1)) return HCW_ERR_WORKSPACE;
-    const int pairs = ffn_sms() / 2;
+    const int pairs = device_sms() / 2;
     FfnArgs a;
     memset(&a, 0, sizeof(a));
     FfnProd& p = a.p[0];
@@ -1165,14 +1228,14 @@ int hcw_gated_ffn_bwd(const void* x, const void* dy, const void* W1, const void*
         r.m[1].out = dW2;
         r.m[1].count4 = (size_t)d * h / 4;
         r.m[0].f32 = r.m[1].f32 = f32;
-        return count_launch(launch_pdl(ffn_reduce_kernel, dim3((unsigned)ffn_sms() * 4), dim3(256), 0,
+        return count_launch(launch_pdl(ffn_reduce_kernel, dim3((unsigned)device_sms() * 4), dim3(256), 0,
                                        st, r), 1);
     }
     if (!x || !dy || !W1 || !W2 || (!dx && !dW1)) return HCW_ERR_INVALID_ARG;
     const FfnBwdWs w = ffn_bwd_ws(T, d, h, dx != nullptr, dW1 != nullptr, f32);
     if (!workspace || ws_bytes < w.bytes) return HCW_ERR_WORKSPACE;
     uint8_t* ws = static_cast<uint8_t*>(workspace);
-    const int pairs = ffn_sms() / 2;
+    const int pairs = device_sms() / 2;
     FfnArgs a;
     memset(&a, 0, sizeof(a));
     for (int i = 0; i < 2; ++i) {

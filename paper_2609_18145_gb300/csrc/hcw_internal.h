@@ -8,6 +8,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <atomic>
+
 namespace hcw {
 
 // MODE_DWF: weight gradients of a run of layers, one unit per (layer, output
@@ -355,6 +357,20 @@ cudaError_t block_error_word_read_clear(int* word);
 // HCW_OK after counting `kernels` launches if e is cudaSuccess, else HCW_ERR_CUDA
 // (the launch counter lives with the C API in hcw_api.cu).
 int count_launch(cudaError_t e, int kernels);
+
+// SMs of the current device (an even number of 2 or more; 148 where there is none), asked of
+// the runtime once a device.
+inline int device_sms() {
+    static std::atomic<int> known[64];
+    int dev = 0, n = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 148;
+    n = known[dev].load(std::memory_order_relaxed);
+    if (n) return n;
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 2)
+        return 148;
+    known[dev].store(n & ~1, std::memory_order_relaxed);
+    return n & ~1;
+}
 
 // ---- Gated feed-forward block (hcw_ffn.cu) ----
 // Read its kernels' error word and reset it to 0 (synchronous).

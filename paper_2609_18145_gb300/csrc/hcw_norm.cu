@@ -975,14 +975,6 @@ struct NormPlan {
     size_t smem;
 };
 
-int norm_sms() {
-    int dev = 0, n = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess ||
-        cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1)
-        return 148;
-    return n;
-}
-
 int norm_groups(int T, int rows_per_gate) {
     return rows_per_gate > 0 ? (int)(((long long)T + rows_per_gate - 1) / rows_per_gate) : 1;
 }
@@ -994,7 +986,7 @@ constexpr int kNormRows = 2;
 NormPlan norm_plan(bool bwd, bool ln, int T, int d, int elem, int rows_per_gate) {
     NormPlan p;
     p.ln = ln;
-    const int sms = norm_sms(), E = kNormCols;
+    const int sms = device_sms(), E = kNormCols;
     // a power of two up to a warp, whole warps above
     p.nl = 8;
     while (p.nl < 32 && p.nl * E < d) p.nl *= 2;
@@ -1028,19 +1020,22 @@ NormPlan norm_plan(bool bwd, bool ln, int T, int d, int elem, int rows_per_gate)
     p.groups = norm_groups(T, rows_per_gate);
     const int rows = rows_per_gate > 0 && rows_per_gate < T ? rows_per_gate : T;
     const int most = sms;
-    // runs of rows of a group: as many as make the busiest CTA's work least, in row groups'
-    // steps and 4 steps a run
+    // Runs of rows of a group: as many as make the busiest CTA's work least, in row groups'
+    // steps and 4 steps a run; for each number of runs a CTA takes, the shortest runs.
     p.slices = 1;
-    if (p.groups > 0 && p.groups < 4 * most) {
+    if (p.groups > 0) {
         long long best = -1;
         const int runs = (rows + n_grp - 1) / n_grp;
-        for (int k = 1; k <= runs && (long long)k * p.groups <= 8ll * most; ++k) {
-            const long long per = ((long long)p.groups * k + most - 1) / most;
+        for (int per = 1; per <= 8; ++per) {
+            long long k = (long long)most * per / p.groups;
+            k = k < 1 ? 1 : k < runs ? k : runs;
+            const long long busiest = (p.groups * k + most - 1) / most;
             const long long len = ((rows + k - 1) / k + n_grp - 1) / n_grp;
-            if (best < 0 || per * (len + 4) < best) {
-                best = per * (len + 4);
-                p.slices = k;
+            if (best < 0 || busiest * (len + 4) < best) {
+                best = busiest * (len + 4);
+                p.slices = (int)k;
             }
+            if (k == runs) break;
         }
     }
     const long long items = (long long)p.groups * p.slices;

@@ -165,10 +165,17 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+# torch's handle of the current stream without the Stream object around it (2 of the 3 us
+# that torch.cuda.current_stream() takes), where this torch has it
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream):
-    if stream is None:
-        stream = torch.cuda.current_stream()
-    return stream.cuda_stream
+    if stream is not None:
+        return stream.cuda_stream
+    if _raw_stream is None:
+        return torch.cuda.current_stream().cuda_stream
+    return _raw_stream(torch.cuda.current_device())
 
 
 def _dtype_code(t: torch.Tensor) -> int:
@@ -411,18 +418,22 @@ def _rows(t):
     return (t.numel() // d if d else 0), d
 
 
-def _f32(what, *ts):
-    for t in ts:
-        if t is not None and t.dtype != torch.float32:
-            raise TypeError("%s must be float32, got %s" % (what, t.dtype))
-
-
 def _like(ref, what, *ts):
     """ts (None allowed) have ref's dtype and number of elements."""
     for t in ts:
         if t is not None and (t.dtype != ref.dtype or t.numel() != ref.numel()):
             raise ValueError("%s: %s %s does not match %s %s"
                              % (what, tuple(t.shape), t.dtype, tuple(ref.shape), ref.dtype))
+
+
+def _params(what, n, *ts):
+    """ts (None allowed) are fp32 with n elements."""
+    for t in ts:
+        if t is not None:
+            if t.dtype != torch.float32:
+                raise TypeError("%s must be float32, got %s" % (what, t.dtype))
+            if t.numel() != n:
+                raise ValueError("%s: expected %d elements, got %s" % (what, n, tuple(t.shape)))
 
 
 def _numel(what, n, *ts):
@@ -519,9 +530,9 @@ def hcw_residual_norm_fwd(r, f, gate=None, rows_per_gate: int = 0, alpha: float 
     if ref is None:
         raise ValueError("hcw_residual_norm_fwd: r or f is needed")
     T, d = _rows(ref)
-    _f32("hcw_residual_norm_fwd: gate, weights and biases", gate, post_w, post_b, pre_w, pre_b)
-    _numel("hcw_residual_norm_fwd: weights and biases", d, post_w, post_b, pre_w, pre_b)
-    _numel("hcw_residual_norm_fwd: gate", _gates(T, rows_per_gate) * d, gate)
+    _params("hcw_residual_norm_fwd: weights and biases", d, post_w, post_b, pre_w, pre_b)
+    if gate is not None:
+        _params("hcw_residual_norm_fwd: gate", _gates(T, rows_per_gate) * d, gate)
     if want_r and r_out is None:
         r_out = torch.empty_like(ref)
     if want_x and x_out is None:
@@ -553,9 +564,8 @@ def hcw_residual_norm_bwd(dr_out, dx_out, s, f, gate=None, rows_per_gate: int = 
         raise ValueError("hcw_residual_norm_bwd: dr_out or dx_out is needed")
     T, d = _rows(ref)
     G = _gates(T, rows_per_gate)
-    _f32("hcw_residual_norm_bwd: gate, weights and biases", gate, post_w, post_b, pre_w)
-    _numel("hcw_residual_norm_bwd: weights and biases", d, post_w, post_b, pre_w)
-    _numel("hcw_residual_norm_bwd: gate", G * d, gate)
+    _params("hcw_residual_norm_bwd: weights and biases", d, post_w, post_b, pre_w)
+    _params("hcw_residual_norm_bwd: gate", G * d, gate)
     has_post = f is not None and post != HCW_NORM_NONE
     has_pre = dx_out is not None and pre != HCW_NORM_NONE
     out = {}
@@ -607,13 +617,13 @@ def hcw_distill_loss(z, idx=None, teacher=None, target=None, weight=None,
         if idx.dtype != torch.int32:
             raise TypeError("hcw_distill_loss: idx must be int32, got %s" % idx.dtype)
         K = idx.shape[-1]
-        _numel("hcw_distill_loss: idx and teacher", T * K, idx)
     elif teacher is not None:
         raise ValueError("hcw_distill_loss: teacher logits without their symbols")
     if target is not None and target.dtype != torch.int32:
         raise TypeError("hcw_distill_loss: target must be int32, got %s" % target.dtype)
-    _f32("hcw_distill_loss: teacher, weight and loss", teacher, weight, loss)
-    _numel("hcw_distill_loss: target, weight and loss", T, target, weight, loss)
+    _params("hcw_distill_loss: teacher", T * K, teacher)
+    _params("hcw_distill_loss: weight and loss", T, weight, loss)
+    _numel("hcw_distill_loss: target", T, target)
     if loss is None:
         loss = torch.empty(T, dtype=torch.float32, device=z.device)
     if want_grad and dz is None:
