@@ -550,15 +550,20 @@ __global__ void __launch_bounds__(256) ffn_reduce_kernel(const FfnReduce a) {
 // sums are added in warp order.  A lane's 16 bytes of 8 neighbouring k stand for the MMA's
 // k in an order of their own, the same for both operands.  The second product's launch
 // starts its ring before it waits for the first's.
+// Up to 8 tokens (LO) half of the MMA's rows would be empty; they hold what the rounding of a
+// to bf16 leaves, itself in bf16, so that a carries 16 bits into the second product at no cost
+// and y is rounded once: the first product writes the tokens' rows and, after them, the rows of
+// the remainders, the second adds the sums of both.
 constexpr int kRowWarps = 16;
 constexpr int kRowMax = 32;        // tokens at most
+constexpr int kRowLo = 8;          // tokens whose a is kept in two parts, at most
 constexpr int kRowPiece = 2048;    // k of a piece at most
 constexpr int kRowMaxBufs = 8;
 
 struct FfnRowArgs {
-    const __nv_bfloat16* A;   // [T][K]
+    const __nv_bfloat16* A;   // [T][K]; the second product with LO: [2 T][K]
     const __nv_bfloat16* B;   // [n_cols][K], GATED: [2 n_cols][K]
-    __nv_bfloat16* out;       // [T][n_cols]
+    __nv_bfloat16* out;       // [T][n_cols]; the first product with LO: [2 T][n_cols]
     int T, K, n_cols;
     int kc, pieces;           // k of a piece (a multiple of 32), pieces of a row
     int bufs;
@@ -579,9 +584,11 @@ __device__ __forceinline__ void ffn_mma(float (&c)[4], uint32_t a0, uint32_t a1,
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-template <int MT, bool GATED, int ACT>
+template <int MT, bool GATED, int ACT, bool LO>
 __global__ void __launch_bounds__(32 * kRowWarps + 32) ffn_rows_kernel(const FfnRowArgs a) {
+    static_assert(!LO || MT == 1, "the remainders take the second 8 rows of one MMA");
     constexpr int NB = GATED ? 2 : 1;
+    constexpr bool kTwo = LO && !GATED;           // two rows of A a token
     constexpr int kRed = MT * NB * 16 * 9;        // floats of a warp's sums
     extern __shared__ __align__(128) uint8_t row_smem[];
     __shared__ uint64_t full[kRowMaxBufs], empty[kRowMaxBufs], a_full;
@@ -591,6 +598,7 @@ __global__ void __launch_bounds__(32 * kRowWarps + 32) ffn_rows_kernel(const Ffn
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int g = lane >> 2, q = lane & 3;   // MMA row (and column of B), and 8 k of a block
     const int tiles = a.n_cols / 8;
+    const int n_rows = kTwo ? 2 * a.T : a.T;
     const int stride = ffn_row_stride(a.kc), buf_bytes = NB * 8 * stride;
     if (threadIdx.x == 0) {
         for (int i = 0; i < a.bufs; ++i) {
@@ -614,9 +622,9 @@ __global__ void __launch_bounds__(32 * kRowWarps + 32) ffn_rows_kernel(const Ffn
             a_done = true;
             pdl_wait();
             if (!a.resident) return;
-            if (lane == 0) mbar_arrive_expect_tx(&a_full, (uint32_t)(a.T * a.K * 2));
+            if (lane == 0) mbar_arrive_expect_tx(&a_full, (uint32_t)(n_rows * a.K * 2));
             __syncwarp();
-            if (lane < a.T)
+            if (lane < n_rows)
                 asm volatile(
                     "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes "
                     "[%0], [%1], %2, [%3];" ::"r"(smem_u32(a_mem + lane * a.a_stride)),
@@ -680,8 +688,9 @@ __global__ void __launch_bounds__(32 * kRowWarps + 32) ffn_rows_kernel(const Ffn
                 for (int m = 0; m < MT; ++m)
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        const int t = 16 * m + 8 * h + g, k = k0 + 32 * i;
-                        x[m][h] = i < per && warp * per + i < a.kc / 32 && k < a.K && t < a.T
+                        const int t = kTwo ? a.T * h + g : 16 * m + 8 * h + g, k = k0 + 32 * i;
+                        const bool row = kTwo ? g < a.T : t < a.T;
+                        x[m][h] = i < per && warp * per + i < a.kc / 32 && k < a.K && row
                                       ? *reinterpret_cast<const uint4*>(rows_at + t * a.a_stride + k * 2)
                                       : zero;
                     }
@@ -742,9 +751,23 @@ __global__ void __launch_bounds__(32 * kRowWarps + 32) ffn_rows_kernel(const Ffn
                 s[n] = p[0];
 #pragma unroll
                 for (int k = 1; k < kRowWarps; ++k) s[n] += p[k * kRed];
+                if (kTwo && r < 8) {
+                    float lo = p[8 * 9];
+#pragma unroll
+                    for (int k = 1; k < kRowWarps; ++k) lo += p[k * kRed + 8 * 9];
+                    s[n] += lo;
+                }
             }
             const float v = GATED ? ffn_act<ACT>(s[0], nullptr) * s[NB - 1] : s[0];
-            if (t < a.T) a.out[(size_t)t * a.n_cols + tile * 8 + c] = __float2bfloat16_rn(v);
+            if (t < a.T) {
+                const __nv_bfloat16 hi = __float2bfloat16_rn(v);
+                a.out[(size_t)t * a.n_cols + tile * 8 + c] = hi;
+                // (an infinite a has no remainder)
+                if (LO && GATED)
+                    a.out[(size_t)(a.T + t) * a.n_cols + tile * 8 + c] =
+                        __float2bfloat16_rn(fabsf(__bfloat162float(hi)) < INFINITY
+                                                ? v - __bfloat162float(hi) : 0.f);
+            }
         }
     }
 }
@@ -847,9 +870,9 @@ cudaError_t ffn_launch_act(int act, const FfnArgs& a, int pairs, cudaStream_t st
     }
 }
 
-template <int MT, bool GATED, int ACT>
+template <int MT, bool GATED, int ACT, bool LO>
 cudaError_t ffn_rows_launch_mt(FfnRowArgs a, cudaStream_t st) {
-    auto kern = ffn_rows_kernel<MT, GATED, ACT>;
+    auto kern = ffn_rows_kernel<MT, GATED, ACT, LO>;
     constexpr size_t sums = 2 * kRowWarps * MT * (GATED ? 2 : 1) * 16 * 9 * sizeof(float);
     constexpr size_t room = 232448 - 1024;   // beside the barriers
     static std::once_flag once[64];
@@ -868,7 +891,7 @@ cudaError_t ffn_rows_launch_mt(FfnRowArgs a, cudaStream_t st) {
     a.pieces = (a.K + a.kc - 1) / a.kc;
     // A stays in shared memory where it leaves the ring half of it
     a.a_stride = ffn_row_stride(a.K);
-    const size_t rows = (size_t)a.T * a.a_stride;
+    const size_t rows = (size_t)(LO && !GATED ? 2 * a.T : a.T) * a.a_stride;
     a.resident = rows <= (room - sums) / 2;
     if (!a.resident) a.a_stride = a.K * 2;
     const size_t kept = a.resident ? rows : 0;
@@ -885,8 +908,9 @@ cudaError_t ffn_rows_launch_mt(FfnRowArgs a, cudaStream_t st) {
 
 template <bool GATED, int ACT>
 cudaError_t ffn_rows_launch(const FfnRowArgs& a, cudaStream_t st) {
-    return a.T <= 16 ? ffn_rows_launch_mt<1, GATED, ACT>(a, st)
-                     : ffn_rows_launch_mt<2, GATED, ACT>(a, st);
+    return a.T <= kRowLo ? ffn_rows_launch_mt<1, GATED, ACT, true>(a, st)
+           : a.T <= 16   ? ffn_rows_launch_mt<1, GATED, ACT, false>(a, st)
+                         : ffn_rows_launch_mt<2, GATED, ACT, false>(a, st);
 }
 
 // Whether the rows kernels are the faster way (us a forward, rows kernels and SM pairs:
@@ -897,6 +921,11 @@ bool ffn_few(int T, int d, int h) {
     const double work = (double)T * d * h;
     return T <= 16 ? work <= 1 << 28 : T <= kRowMax && work <= 1 << 27;
 }
+
+size_t ffn_round(size_t n) { return (n + 255) & ~(size_t)255; }
+
+// a of a few tokens, and its remainders
+size_t ffn_rows_ws(int T, int h) { return ffn_round((size_t)(T <= kRowLo ? 2 * T : T) * h * 2); }
 
 // The forward of a few tokens: two launches.
 int ffn_rows_fwd(const void* x, const void* W1, const void* W2, int T, int d, int h, int act,
@@ -959,8 +988,6 @@ void ffn_plan(FfnShape* s, int n, int pairs) {
         if (capped) break;   // longer units change nothing
     }
 }
-
-size_t ffn_round(size_t n) { return (n + 255) & ~(size_t)255; }
 
 size_t ffn_part_bytes(const FfnShape* s, int n) {
     size_t b = 0;
@@ -1147,7 +1174,7 @@ extern "C" {
 
 size_t hcw_gated_ffn_fwd_workspace_bytes(int T, int d, int h) {
     if (T < 1 || ffn_sizes(T, d, h, HCW_GATE_SILU)) return 0;
-    if (ffn_few(T, d, h)) return ffn_round((size_t)T * h * 2);
+    if (ffn_few(T, d, h)) return ffn_rows_ws(T, h);
     const FfnShape s = ffn_down_shape(T, d, h);
     return ffn_round((size_t)T * h * 2) + ffn_part_bytes(&s, 1);
 }
@@ -1166,7 +1193,7 @@ int hcw_gated_ffn_fwd(const void* x, const void* W1, const void* W2, int T, int 
     const size_t act_bytes = ffn_round((size_t)T * h * 2);
     const cudaStream_t st = (cudaStream_t)stream;
     if (ffn_few(T, d, h)) {
-        if (!workspace || ws_bytes < act_bytes) return HCW_ERR_WORKSPACE;
+        if (!workspace || ws_bytes < ffn_rows_ws(T, h)) return HCW_ERR_WORKSPACE;
         return ffn_rows_fwd(x, W1, W2, T, d, h, act, y, workspace, st);
     }
     FfnShape s = ffn_down_shape(T, d, h);
