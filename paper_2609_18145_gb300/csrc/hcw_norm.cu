@@ -44,10 +44,9 @@ constexpr int kNormPar = 4;         // parameter sums of a CTA: post_w, post_b, 
 constexpr int kNormRed = 8;         // values of one reduction round
 constexpr int kNormCols = 16;       // columns a thread, in parts of 8:
 constexpr int kNormPart = 4;        // pairs of a part
-// A thread's 16 floats in shared memory are 64 bytes, its 16-byte pieces in an order of its
-// own (piece c at c ^ (l / 2 & 3)), so that 8 neighbours' accesses to one piece fall into
-// different banks.
-constexpr int kNormOwn = kNormCols * (int)sizeof(float);
+// A thread's 16 (8) floats in shared memory are 64 (32) bytes, its 16-byte pieces in an order
+// of its own (piece c at c ^ (l / 2 & 3), c ^ (l / 4 & 1)), so that 8 neighbours' accesses to
+// one piece fall into different banks.
 constexpr int kNormMaxBufs = 8;
 constexpr size_t kNormSmem = 232448 - 2048;   // dynamic, beside NormShared
 constexpr unsigned long long kNormTimeoutNs = 2000000000ull;
@@ -248,6 +247,22 @@ struct Cols {
                                   __uint_as_float(lds32(run(row, 8 * k + 2 * j + 1))));
         }
     }
+    // Part k of a row of bf16 as it is stored.
+    __device__ __forceinline__ void raw8(uint32_t (&v)[kNormPart], uint32_t row, int k) const {
+        if (VW == 8) {
+            const uint4 q = lds128(run(row, k));
+            v[0] = q.x;
+            v[1] = q.y;
+            v[2] = q.z;
+            v[3] = q.w;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                v[j] = VW == 2 ? lds32(run(row, 4 * k + j))
+                               : lds16(run(row, 8 * k + 2 * j)) |
+                                     lds16(run(row, 8 * k + 2 * j + 1)) << 16;
+        }
+    }
     __device__ __forceinline__ void load(uint64_t (&v)[H], uint32_t row) const {
 #pragma unroll
         for (int k = 0; k < H / kNormPart; ++k) {
@@ -306,9 +321,10 @@ struct Cols {
             store8(base, row, k, q);
         }
     }
-    // Address of a thread's own 16 floats of a vector in shared memory (`i`: its place).
+    // Address of a thread's own E floats of a vector in shared memory (`i`: its place).
+    static constexpr int OWN = E * (int)sizeof(float);
     __device__ __forceinline__ static uint32_t own(const void* vec, int i) {
-        return smem_u32(vec) + (uint32_t)(i * kNormOwn + ((i >> 1 & 3) << 4));
+        return smem_u32(vec) + (uint32_t)(i * OWN + (E == 16 ? (i >> 1 & 3) << 4 : (i >> 2 & 1) << 4));
     }
     __device__ __forceinline__ static uint32_t piece(uint32_t own, int c) {
         return own ^ (uint32_t)(c << 4);
@@ -469,8 +485,8 @@ __global__ void __launch_bounds__(kNormThreads) norm_fwd_kernel(const NormArgs a
     const uint64_t alpha = both(a.alpha);
     // parameters: pre_w, gate * post_w, pre_b, gate * post_b
     const uint8_t* const par = norm_smem + (size_t)a.bufs * 2 * a.piece;
-    const uint32_t pw = C.own(par, C.l), gw = pw + kNormOwn * nl, pb = gw + kNormOwn * nl,
-                   gb = pb + kNormOwn * nl;
+    const uint32_t pw = C.own(par, C.l), gw = pw + C.OWN * nl, pb = gw + C.OWN * nl,
+                   gb = pb + C.OWN * nl;
     if (grp == n_grp - 1) {
         C.fill(pw, a.pre_w, nullptr, 1.f);
         if (LN) C.fill(pb, a.pre_b, nullptr, 0.f);
@@ -624,23 +640,30 @@ __device__ __forceinline__ void group_sum(const C& cols, const uint64_t (&v)[H],
     }
 }
 
-// SM: with LayerNorms, the sums of dx and ds in shared memory (the registers have no room for
-// them; without SM they are there all the same, for rows whose ring leaves no room either).
-template <typename T, int VW, bool LN, bool SM>
+// E columns a thread, R rows a row group works on at once: 8 and 2 where a row then fits the
+// CTA, which reads the parameters once for two rows, adds up both rows' sums in one go and has
+// two rows' work between waits; 16 and 1 for wider rows.
+// SM: with LayerNorms, the sums of dx and ds in shared memory (16 columns' sums have no room in
+// the registers; without SM they are there all the same, for rows whose ring leaves no room
+// either).
+template <typename T, int VW, bool LN, bool SM, int E, int R>
 __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const NormArgs a) {
     extern __shared__ __align__(128) uint8_t norm_smem[];
     __shared__ NormShared sh;
-    constexpr int E = kNormCols, H = E / 2, Q = kNormPart;   // pairs in all, and at a time
+    constexpr int H = E / 2, Q = kNormPart;   // pairs in all, and at a time
+    // bf16 rows are read from shared memory once and kept as they are, where the sums leave
+    // room in the registers: f, and without LayerNorms s and dx
+    constexpr bool KF = sizeof(T) == 2 && E == 8, KX = KF && !LN;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int nt = (int)blockDim.x, nl = a.nl, d = a.d;
     // parameters: pre_w, gate * post_w; the sums of dx and ds (SM); the row groups' sums on
     // their way together (through the sums of ds, which are in registers by then)
     const uint8_t* const par = norm_smem + (size_t)a.bufs * 4 * a.piece;
-    const uint32_t pw = Cols<T, VW, E>::own(par, (int)threadIdx.x % nl), gp = pw + kNormOwn * nl;
-    const uint32_t c_b = Cols<T, VW, E>::own(par + 2 * kNormOwn * nl, threadIdx.x),
-                   i_b = c_b + kNormOwn * nt;
+    const uint32_t pw = Cols<T, VW, E>::own(par, (int)threadIdx.x % nl), gp = pw + Cols<T, VW, E>::OWN * nl;
+    const uint32_t c_b = Cols<T, VW, E>::own(par + 2 * Cols<T, VW, E>::OWN * nl, threadIdx.x),
+                   i_b = c_b + Cols<T, VW, E>::OWN * nt;
     float* const gbuf = reinterpret_cast<float*>(
-        norm_smem + (size_t)a.bufs * 4 * a.piece + kNormOwn * (2 * nl + (SM ? nt : 0)));
+        norm_smem + (size_t)a.bufs * 4 * a.piece + Cols<T, VW, E>::OWN * (2 * nl + (SM ? nt : 0)));
     if (threadIdx.x == 0) {
         for (int i = 0; i < a.bufs; ++i) {
             mbar_init(&sh.full[i], 1);
@@ -662,16 +685,11 @@ __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const NormArgs a
     const int l = (int)threadIdx.x % nl, grp = (int)threadIdx.x / nl, n_grp = nt / nl;
     const float inv_d = 1.f / (float)d;
     const bool has_dr = a.in[0], has_f = a.in[1], has_dx = a.in[3];
-    const int first = grp * d * (int)sizeof(T);
+    const int first = grp * d * (int)sizeof(T), step = n_grp * d * (int)sizeof(T);
     const int items = a.groups * a.slices;
     RowSum rs(&sh, nl, warp, lane);
     const Cols<T, VW, E> C(l, nl, d, sh.zero);
     if (grp == n_grp - 1) C.fill(pw, a.pre_w, nullptr, 1.f);
-    // a tensor that is not there reads the zeros
-    Cols<T, VW, E> Cr = C, Cf = C, Cx = C;
-    if (!has_dr) Cr.in = 0;
-    if (!has_f) Cf.in = 0;
-    if (!has_dx) Cx.in = 0;
     // sums over all of the CTA's rows: dx shat, dx
     uint64_t c_w[H];
     pairs_zero(c_w);
@@ -714,88 +732,144 @@ __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const NormArgs a
             const int n = r1 - row0 < a.rows ? r1 - row0 : a.rows;
             const uint32_t buf = smem_u32(norm_smem) + b * 4 * a.piece +
                                  ((uint32_t)row0 * (uint32_t)d * (uint32_t)sizeof(T) & 15) + first;
-            // One row a group (a group past the buffer's n adds nothing), 8 columns at a time,
-            // read again in each pass: the sums over the rows take the registers.
-            const bool in = grp < n;
-            const int row = row0 + grp;
-            const uint32_t dr_row = buf, f_row = buf + a.piece, s_row = buf + 2 * a.piece,
-                           x_row = buf + 3 * a.piece;
-            float ms = 0.f, mf = 0.f;
+            // 8 columns at a time, in passes over the rows: the sums over the rows take the
+            // registers.  A row past the buffer's n reads zeros and has zero factors.
+            uint32_t mr[R], mf_[R], mx[R];   // columns to read: dr, f, s and dx
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const bool in = grp + n_grp * r < n;
+                mr[r] = in && has_dr ? C.in : 0u;
+                mf_[r] = in && has_f ? C.in : 0u;
+                mx[r] = in && has_dx ? C.in : 0u;
+            }
+            const uint32_t f_row = buf + a.piece, s_row = buf + 2 * a.piece, x_row = buf + 3 * a.piece;
+            uint32_t kf[KF ? R : 1][Q], ks[KX ? R : 1][Q], kx[KX ? R : 1][Q];
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                Cols<T, VW, E> c = C;
+                c.in = mf_[r];
+                if constexpr (KF) c.raw8(kf[r], f_row + r * step, 0);
+                c.in = mx[r];
+                if constexpr (KX) {
+                    c.raw8(ks[r], s_row + r * step, 0);
+                    c.raw8(kx[r], x_row + r * step, 0);
+                }
+            }
+            // part k of row r
+            auto kept = [&](uint64_t (&v)[Q], const uint32_t (&raw)[Q]) {
+#pragma unroll
+                for (int j = 0; j < Q; ++j) v[j] = bf16x2_to_f32x2(raw[j]);
+            };
+            auto part = [&](uint64_t (&v)[Q], uint32_t row, uint32_t mask, int r, int k) {
+                Cols<T, VW, E> c = C;
+                c.in = mask;
+                c.load8(v, row + r * step, k);
+            };
+            auto part_s = [&](uint64_t (&v)[Q], int r, int k) {
+                if constexpr (KX) kept(v, ks[r]);
+                else part(v, s_row, mx[r], r, k);
+            };
+            auto part_x = [&](uint64_t (&v)[Q], int r, int k) {
+                if constexpr (KX) kept(v, kx[r]);
+                else part(v, x_row, mx[r], r, k);
+            };
+            auto part_f = [&](uint64_t (&v)[Q], int r, int k) {
+                if constexpr (KF) kept(v, kf[r]);
+                else part(v, f_row, mf_[r], r, k);
+            };
+            float ms[R] = {}, mf[R] = {};
             if (LN) {
-                uint64_t x = 0, y = 0;
-                if (in) {
+                float t[2 * R];
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    uint64_t x = 0, y = 0;
 #pragma unroll
                     for (int k = 0; k < H / Q; ++k) {
                         uint64_t v[Q];
-                        Cx.load8(v, s_row, k);
+                        part_s(v, r, k);
 #pragma unroll
                         for (int j = 0; j < Q; ++j) x = f32x2_add(x, v[j]);
-                        Cf.load8(v, f_row, k);
+                        part_f(v, r, k);
 #pragma unroll
                         for (int j = 0; j < Q; ++j) y = f32x2_add(y, v[j]);
                     }
+                    t[2 * r] = pair_sum(x);
+                    t[2 * r + 1] = pair_sum(y);
                 }
-                float t[2] = {pair_sum(x), pair_sum(y)};
                 rs.sum(t);
-                ms = a.pre == HCW_NORM_LAYER ? t[0] * inv_d : 0.f;
-                mf = a.post == HCW_NORM_LAYER ? t[1] * inv_d : 0.f;
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    ms[r] = a.pre == HCW_NORM_LAYER ? t[2 * r] * inv_d : 0.f;
+                    mf[r] = a.post == HCW_NORM_LAYER ? t[2 * r + 1] * inv_d : 0.f;
+                }
             }
             // s or f, centred where its norm is a LayerNorm
-            auto centred_s = [&](uint64_t (&v)[Q], int k) {
-                Cx.load8(v, s_row, k);
-                if (LN) C.centre8(v, ms, k);
+            auto centred_s = [&](uint64_t (&v)[Q], int r, int k) {
+                part_s(v, r, k);
+                if (LN) C.centre8(v, ms[r], k);
             };
-            auto centred_f = [&](uint64_t (&v)[Q], int k) {
-                Cf.load8(v, f_row, k);
-                if (LN) C.centre8(v, mf, k);
+            auto centred_f = [&](uint64_t (&v)[Q], int r, int k) {
+                part_f(v, r, k);
+                if (LN) C.centre8(v, mf[r], k);
             };
             // sums of s^2, e s, f^2, e  with e = dx pre_w
             constexpr int NS = LN ? 4 : 3;
-            float t[NS];
+            float t[NS * R];
             {
-                uint64_t ss = 0, es = 0, ff = 0, e1 = 0;
-                if (in) {
+                uint64_t ss[R] = {}, es[R] = {}, ff[R] = {}, e1[R] = {};
 #pragma unroll
-                    for (int k = 0; k < H / Q; ++k) {
-                        uint64_t v[Q], x[Q], w[Q];
-                        centred_s(v, k);
-                        Cx.load8(x, x_row, k);
-                        C.fetch8(w, pw, k);
+                for (int k = 0; k < H / Q; ++k) {
+                    uint64_t w[Q];
+                    C.fetch8(w, pw, k);
+#pragma unroll
+                    for (int r = 0; r < R; ++r) {
+                        uint64_t v[Q], x[Q];
+                        centred_s(v, r, k);
+                        part_x(x, r, k);
 #pragma unroll
                         for (int j = 0; j < Q; ++j) {
                             const uint64_t e = f32x2_mul(x[j], w[j]);
-                            ss = f32x2_fma(v[j], v[j], ss);
-                            es = f32x2_fma(e, v[j], es);
-                            if (LN) e1 = f32x2_add(e1, e);
+                            ss[r] = f32x2_fma(v[j], v[j], ss[r]);
+                            es[r] = f32x2_fma(e, v[j], es[r]);
+                            if (LN) e1[r] = f32x2_add(e1[r], e);
                         }
-                        centred_f(v, k);
+                        centred_f(v, r, k);
 #pragma unroll
-                        for (int j = 0; j < Q; ++j) ff = f32x2_fma(v[j], v[j], ff);
+                        for (int j = 0; j < Q; ++j) ff[r] = f32x2_fma(v[j], v[j], ff[r]);
                     }
                 }
-                t[0] = pair_sum(ss);
-                t[1] = pair_sum(es);
-                t[2] = pair_sum(ff);
-                if (LN) t[NS - 1] = pair_sum(e1);
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    t[NS * r] = pair_sum(ss[r]);
+                    t[NS * r + 1] = pair_sum(es[r]);
+                    t[NS * r + 2] = pair_sum(ff[r]);
+                    if (LN) t[NS * r + NS - 1] = pair_sum(e1[r]);
+                }
             }
             rs.sum(t);
-            const float rstd = has_dx ? rsqrtf(t[0] * inv_d + a.eps) : 0.f;
-            const float qf =
-                a.post != HCW_NORM_NONE && has_f ? rsqrtf(t[2] * inv_d + a.eps) : 1.f;
-            const uint64_t qq = both(qf);
-            uint64_t ds[H], hf = 0, h1 = 0;   // sums of h fhat, h  with h = gate ds post_w
-            if (in) {
-                const uint64_t rr = both(rstd);
-                const uint64_t nm2 = both(-t[1] * inv_d * rstd);   // mean(e shat)
-                const uint64_t nm1 =
-                    both(LN && a.pre == HCW_NORM_LAYER ? -t[NS - 1] * inv_d : 0.f);
+            float rstd[R], qf[R];
 #pragma unroll
-                for (int k = 0; k < H / Q; ++k) {
-                    uint64_t v[Q], x[Q], w[Q], g_[Q];
-                    Cr.load8(g_, dr_row, k);
-                    centred_s(v, k);
-                    Cx.load8(x, x_row, k);
-                    C.fetch8(w, pw, k);
+            for (int r = 0; r < R; ++r) {
+                rstd[r] = mx[r] ? rsqrtf(t[NS * r] * inv_d + a.eps) : 0.f;
+                qf[r] = a.post != HCW_NORM_NONE && mf_[r] ? rsqrtf(t[NS * r + 2] * inv_d + a.eps) : 1.f;
+            }
+            uint64_t ds[R][H], hf[R] = {}, h1[R] = {};   // sums of h fhat, h  with h = gate ds post_w
+#pragma unroll
+            for (int k = 0; k < H / Q; ++k) {
+                uint64_t w[Q];
+                C.fetch8(w, pw, k);
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    const uint64_t rr = both(rstd[r]);
+                    const uint64_t nm2 = both(-t[NS * r + 1] * inv_d * rstd[r]);   // mean(e shat)
+                    const uint64_t nm1 =
+                        both(LN && a.pre == HCW_NORM_LAYER ? -t[NS * r + NS - 1] * inv_d : 0.f);
+                    uint64_t v[Q], x[Q], g_[Q];
+                    Cols<T, VW, E> c = C;
+                    c.in = mr[r];
+                    c.load8(g_, buf + r * step, k);
+                    centred_s(v, r, k);
+                    part_x(x, r, k);
 #pragma unroll
                     for (int j = 0; j < Q; ++j) {
                         const int i = k * Q + j;
@@ -803,76 +877,98 @@ __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const NormArgs a
                         uint64_t e = f32x2_fma(h, nm2, f32x2_mul(x[j], w[j]));
                         if (LN) e = f32x2_add(e, nm1);
                         c_w[i] = f32x2_fma(x[j], h, c_w[i]);
-                        g_[j] = f32x2_fma(e, rr, g_[j]);
+                        ds[r][i] = f32x2_fma(e, rr, g_[j]);
                     }
                     if constexpr (LN && !SM)
 #pragma unroll
                         for (int j = 0; j < Q; ++j) {
                             c_r[k * Q + j] = f32x2_add(c_r[k * Q + j], x[j]);
-                            i_r[k * Q + j] = f32x2_add(i_r[k * Q + j], g_[j]);
+                            i_r[k * Q + j] = f32x2_add(i_r[k * Q + j], ds[r][k * Q + j]);
                         }
                     if (SM) {
-                        C.fetch8(w, c_b, k);
+                        uint64_t u[Q];
+                        C.fetch8(u, c_b, k);
 #pragma unroll
-                        for (int j = 0; j < Q; ++j) w[j] = f32x2_add(w[j], x[j]);
-                        C.put8(c_b, k, w);
-                        C.fetch8(w, i_b, k);
+                        for (int j = 0; j < Q; ++j) u[j] = f32x2_add(u[j], x[j]);
+                        C.put8(c_b, k, u);
+                        C.fetch8(u, i_b, k);
 #pragma unroll
-                        for (int j = 0; j < Q; ++j) w[j] = f32x2_add(w[j], g_[j]);
-                        C.put8(i_b, k, w);
+                        for (int j = 0; j < Q; ++j) u[j] = f32x2_add(u[j], ds[r][k * Q + j]);
+                        C.put8(i_b, k, u);
                     }
-                    centred_f(v, k);
-                    C.fetch8(w, gp, k);
+                }
+            }
+            auto read = [&]() {   // the buffer has been read
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sh.empty[b]);
+            };
+            if (KF) read();
+#pragma unroll
+            for (int k = 0; k < H / Q; ++k) {
+                uint64_t w[Q];
+                C.fetch8(w, gp, k);
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    const uint64_t qq = both(qf[r]);
+                    uint64_t v[Q];
+                    centred_f(v, r, k);
 #pragma unroll
                     for (int j = 0; j < Q; ++j) {
                         const int i = k * Q + j;
                         const uint64_t fh = f32x2_mul(v[j], qq);
-                        const uint64_t h = f32x2_mul(g_[j], w[j]);   // 0 past the row's end
-                        i_w[i] = f32x2_fma(g_[j], fh, i_w[i]);
-                        hf = f32x2_fma(h, fh, hf);
-                        if (LN) h1 = f32x2_add(h1, h);
+                        const uint64_t h = f32x2_mul(ds[r][i], w[j]);   // 0 past the row's end
+                        i_w[i] = f32x2_fma(ds[r][i], fh, i_w[i]);
+                        hf[r] = f32x2_fma(h, fh, hf[r]);
+                        if (LN) h1[r] = f32x2_add(h1[r], h);
                     }
-#pragma unroll
-                    for (int j = 0; j < Q; ++j) ds[k * Q + j] = g_[j];
                 }
             }
             if (a.o1) {
-                float u[LN ? 2 : 1] = {};
+                constexpr int NU = LN ? 2 : 1;
+                float u[NU * R] = {};
                 if (a.post != HCW_NORM_NONE) {
-                    u[0] = pair_sum(hf);
-                    if (LN) u[LN ? 1 : 0] = pair_sum(h1);
+#pragma unroll
+                    for (int r = 0; r < R; ++r) {
+                        u[NU * r] = pair_sum(hf[r]);
+                        if (LN) u[NU * r + NU - 1] = pair_sum(h1[r]);
+                    }
                     rs.sum(u);
                 }
-                if (in) {
-                    const uint64_t n4 = both(-u[0] * inv_d * qf);   // fhat mean(h fhat) = f qf mean
-                    const uint64_t n3 =
-                        both(LN && a.post == HCW_NORM_LAYER ? -u[LN ? 1 : 0] * inv_d : 0.f);
 #pragma unroll
-                    for (int k = 0; k < H / Q; ++k) {
-                        uint64_t v[Q], w[Q];
-                        centred_f(v, k);
-                        C.fetch8(w, gp, k);
+                for (int k = 0; k < H / Q; ++k) {
+                    uint64_t w[Q];
+                    C.fetch8(w, gp, k);
+#pragma unroll
+                    for (int r = 0; r < R; ++r) {
+                        const uint64_t qq = both(qf[r]);
+                        // fhat mean(h fhat) = f qf mean
+                        const uint64_t n4 = both(-u[NU * r] * inv_d * qf[r]);
+                        const uint64_t n3 = both(
+                            LN && a.post == HCW_NORM_LAYER ? -u[NU * r + NU - 1] * inv_d : 0.f);
+                        uint64_t v[Q];
+                        centred_f(v, r, k);
 #pragma unroll
                         for (int j = 0; j < Q; ++j) {
-                            uint64_t o = f32x2_fma(v[j], n4, f32x2_mul(ds[k * Q + j], w[j]));
+                            uint64_t o = f32x2_fma(v[j], n4, f32x2_mul(ds[r][k * Q + j], w[j]));
                             if (LN) o = f32x2_add(o, n3);
                             v[j] = f32x2_mul(o, qq);
                         }
-                        C.store8(a.o1, row, k, v);
+                        if (grp + n_grp * r < n) C.store8(a.o1, row0 + grp + n_grp * r, k, v);
                     }
                 }
             }
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&sh.empty[b]);   // the buffer has been read
-            if (a.o0 && in) {
+            if (!KF) read();
+            if (a.o0) {
                 const uint64_t alpha = both(a.alpha);
 #pragma unroll
-                for (int k = 0; k < H / Q; ++k) {
-                    uint64_t v[Q];
+                for (int k = 0; k < H / Q; ++k)
 #pragma unroll
-                    for (int j = 0; j < Q; ++j) v[j] = f32x2_mul(ds[k * Q + j], alpha);
-                    C.store8(a.o0, row, k, v);
-                }
+                    for (int r = 0; r < R; ++r) {
+                        uint64_t v[Q];
+#pragma unroll
+                        for (int j = 0; j < Q; ++j) v[j] = f32x2_mul(ds[r][k * Q + j], alpha);
+                        if (grp + n_grp * r < n) C.store8(a.o0, row0 + grp + n_grp * r, k, v);
+                    }
             }
             if (threadIdx.x == 0) fed = feed.fetch<T, 4>(a, norm_smem, &sh);
             __syncwarp();
@@ -970,6 +1066,7 @@ __global__ void __launch_bounds__(1024) norm_reduce_kernel(const NormReduceArgs 
 // Threads a row and a CTA, buffers and items for a call.
 struct NormPlan {
     bool ln, sm;
+    int cols;   // columns a thread
     int nl, threads, grid, slices, groups;
     int rows, bufs, piece;
     size_t smem;
@@ -979,14 +1076,15 @@ int norm_groups(int T, int rows_per_gate) {
     return rows_per_gate > 0 ? (int)(((long long)T + rows_per_gate - 1) / rows_per_gate) : 1;
 }
 
-// rows a row group works on at once in the forward (the backward: one)
+// rows a row group works on at once in the forward, and in the backward with 8 columns a thread
 constexpr int kNormRows = 2;
 
 // elem: bytes of an element, ln: a LayerNorm (grid, slices and groups depend on neither).
 NormPlan norm_plan(bool bwd, bool ln, int T, int d, int elem, int rows_per_gate) {
     NormPlan p;
     p.ln = ln;
-    const int sms = device_sms(), E = kNormCols;
+    p.cols = bwd && d <= kNormThreads * kNormCols / 2 ? kNormCols / 2 : kNormCols;
+    const int sms = device_sms(), E = p.cols;
     // a power of two up to a warp, whole warps above
     p.nl = 8;
     while (p.nl < 32 && p.nl * E < d) p.nl *= 2;
@@ -998,11 +1096,11 @@ NormPlan norm_plan(bool bwd, bool ln, int T, int d, int elem, int rows_per_gate)
     while (n_grp / 2 >= least && n_grp / 2 >= share) n_grp /= 2;
     p.threads = n_grp * p.nl;
     const int n_in = bwd ? 4 : 2;
-    int r = bwd ? 1 : kNormRows;
-    const size_t vec = (size_t)kNormOwn * p.nl;
-    size_t fixed = !bwd ? (ln ? 4 : 2) * vec : (2 + (ln ? 2 : 1) * n_grp) * vec;
+    int r = bwd && E == kNormCols ? 1 : kNormRows;
+    const size_t vec = (size_t)E * sizeof(float) * p.nl;
+    size_t fixed = !bwd ? (ln ? 4 : 2) * vec : (2 + (ln && E == kNormCols ? 2 : 1) * n_grp) * vec;
     auto piece = [&](int rows) { return (int)(((size_t)rows * d * elem + 32 + 127) / 128 * 128); };
-    p.sm = bwd && ln;
+    p.sm = bwd && ln && E == kNormCols;
     if (p.sm && fixed + (size_t)n_in * piece(n_grp) > kNormSmem) {
         p.sm = false;
         fixed = (2 + n_grp) * vec;
@@ -1045,13 +1143,18 @@ NormPlan norm_plan(bool bwd, bool ln, int T, int d, int elem, int rows_per_gate)
 
 template <typename T, int VW, bool LN>
 cudaError_t launch_norm(bool bwd, const NormPlan& p, const NormArgs& a, cudaStream_t st) {
-    auto kern = bwd ? norm_bwd_kernel<T, VW, LN, LN> : norm_fwd_kernel<T, VW, LN, kNormRows>;
+    auto kern = !bwd                    ? norm_fwd_kernel<T, VW, LN, kNormRows>
+                : p.cols == kNormCols ? norm_bwd_kernel<T, VW, LN, LN, kNormCols, 1>
+                                      : norm_bwd_kernel<T, VW, LN, false, kNormCols / 2, kNormRows>;
+    int which = !bwd ? 0 : p.cols == kNormCols ? 1 : 2;
     // (a row of bf16 always leaves the sums room: 192 KB in all at 8192 columns)
     if constexpr (LN && sizeof(T) == 4)
-        if (bwd && !p.sm) kern = norm_bwd_kernel<T, VW, LN, false>;
-    const int which = !bwd ? 0 : p.sm == LN ? 1 : 2;
-    static std::once_flag once[64][3];
-    static cudaError_t set_err[64][3];
+        if (which == 1 && !p.sm) {
+            kern = norm_bwd_kernel<T, VW, LN, false, kNormCols, 1>;
+            which = 3;
+        }
+    static std::once_flag once[64][4];
+    static cudaError_t set_err[64][4];
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
