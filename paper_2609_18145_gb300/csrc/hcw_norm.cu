@@ -1013,9 +1013,10 @@ __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const NormArgs a
     if (threadIdx.x == 0) feed.drain(a, &sh);
 }
 
-// Column sums of the partial rows, 32 columns a block, 32 rows at a time, in a fixed order.
-// Blocks [0, par * ncb): parameter vector par (out[par], if wanted) over the CTAs' rows;
-// then one run of ncb blocks a group: dgate over the group's slices.
+// Column sums of the partial rows, in a fixed order, by blocks of 1024 threads: 32 columns and 32
+// rows at a time, or up to 32 rows by more columns.  Blocks [0, kNormPar * ncb): parameter vector
+// (out[], if wanted) over the CTAs' rows; then a run of ncg blocks a group: dgate over the
+// group's slices.
 struct NormReduceArgs {
     const float* cpart;
     const float* gpart;
@@ -1023,45 +1024,64 @@ struct NormReduceArgs {
     float* dgate;
     int rows;        // rows of cpart
     int slices;      // rows of gpart a group
-    int d, ncb;
+    int d;
+    int ncb, ncg;    // column blocks of a vector
+    int c_log2, g_log2;   // columns of a block
 };
+constexpr int kReduceThreads = 1024;   // 1 << 10
 
-__global__ void __launch_bounds__(1024) norm_reduce_kernel(const NormReduceArgs a) {
-    __shared__ float sh[32][33];
+__global__ void __launch_bounds__(kReduceThreads) norm_reduce_kernel(const NormReduceArgs a) {
+    __shared__ float sh[32 * 33];
     pdl_wait();
     pdl_trigger();
-    const int which = (int)(blockIdx.x / a.ncb), cb = (int)(blockIdx.x - (unsigned)which * a.ncb);
-    const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
-    const int c = cb * 32 + tx;
+    const bool par = (int)blockIdx.x < kNormPar * a.ncb;
+    const int b = par ? blockIdx.x : (int)blockIdx.x - kNormPar * a.ncb, nc = par ? a.ncb : a.ncg;
+    const int which = b / nc, cb = b - which * nc;
+    const int log2 = par ? a.c_log2 : a.g_log2, tx = threadIdx.x & ((1 << log2) - 1);
+    const int ty = threadIdx.x >> log2, step = kReduceThreads >> log2;
+    const int c = (cb << log2) + tx;
     const float* src;
     float* dst;
     size_t ld;
     int rows;
-    if (which < kNormPar) {
+    if (par) {
         if (!a.out[which]) return;
         src = a.cpart + (size_t)which * a.d;
         ld = (size_t)kNormPar * a.d;
         dst = a.out[which];
         rows = a.rows;
     } else {
-        const int g = which - kNormPar;
-        src = a.gpart + (size_t)g * a.slices * a.d;
+        src = a.gpart + (size_t)which * a.slices * a.d;
         ld = a.d;
-        dst = a.dgate + (size_t)g * a.d;
+        dst = a.dgate + (size_t)which * a.d;
         rows = a.slices;
     }
     float t = 0.f;
     if (c < a.d)
 #pragma unroll 4
-        for (int r = ty; r < rows; r += 32) t += src[(size_t)r * ld + c];
-    sh[ty][tx] = t;
-    __syncthreads();
-    t = sh[tx][ty];   // row tx of column ty
+        for (int r = ty; r < rows; r += step) t += src[(size_t)r * ld + c];
+    if (log2 == 5) {
+        sh[ty * 33 + tx] = t;
+        __syncthreads();
+        t = sh[tx * 33 + ty];   // row tx of column ty
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
-    const int co = cb * 32 + ty;
-    if (tx == 0 && co < a.d) dst[co] = t;
+        for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
+        const int co = (cb << 5) + ty;
+        if (tx == 0 && co < a.d) dst[co] = t;
+        return;
+    }
+    if (step > 1) {
+        sh[threadIdx.x] = t;
+        __syncthreads();
+        if (ty) return;
+        for (int k = 1; k < step; ++k) t += sh[(k << log2) + tx];
+    }
+    if (c < a.d) dst[c] = t;
 }
+
+// Columns (their log2) of a block that adds so many rows: 8 rows a thread at most up to 32 rows.
+// (4099 x 777 fp32, 8 slices of 17 groups: the backward 29.0 us with 32 columns, 27.2 so.)
+int reduce_cols(int rows) { return rows > 32 ? 5 : rows > 16 ? 8 : rows > 8 ? 9 : 10; }
 
 // Threads a row and a CTA, buffers and items for a call.
 struct NormPlan {
@@ -1106,9 +1126,11 @@ NormPlan norm_plan(bool bwd, bool ln, int T, int d, int elem, int rows_per_gate)
         fixed = (2 + n_grp) * vec;
     }
     const size_t room = kNormSmem - fixed;
-    // (a buffer of one row a group where two do not fit: the kernel's second row is then
-    // past the buffer's rows)
-    while (r > 1 && (size_t)n_in * piece(n_grp * r) > room) r /= 2;
+    // One row a group where the ring would have but one buffer of two rows and other groups
+    // fill its waits (forward of 16384 x 2048 fp32, LayerNorms, 4 groups: 102 -> 89 us; of
+    // 16384 x 8192 bf16, one group: 290 -> 323), or not one buffer.  (The backward's second
+    // row is then past the buffer's rows.)
+    while (r > 1 && (size_t)n_in * piece(n_grp * r) * (bwd || n_grp == 1 ? 1 : 2) > room) r /= 2;
     p.rows = n_grp * r;
     p.piece = piece(p.rows);
     p.bufs = (int)(room / ((size_t)n_in * p.piece));
@@ -1143,18 +1165,19 @@ NormPlan norm_plan(bool bwd, bool ln, int T, int d, int elem, int rows_per_gate)
 
 template <typename T, int VW, bool LN>
 cudaError_t launch_norm(bool bwd, const NormPlan& p, const NormArgs& a, cudaStream_t st) {
-    auto kern = !bwd                    ? norm_fwd_kernel<T, VW, LN, kNormRows>
+    auto kern = !bwd                    ? (p.rows * p.nl > p.threads ? norm_fwd_kernel<T, VW, LN, kNormRows>
+                                                                     : norm_fwd_kernel<T, VW, LN, 1>)
                 : p.cols == kNormCols ? norm_bwd_kernel<T, VW, LN, LN, kNormCols, 1>
                                       : norm_bwd_kernel<T, VW, LN, false, kNormCols / 2, kNormRows>;
-    int which = !bwd ? 0 : p.cols == kNormCols ? 1 : 2;
+    int which = !bwd ? (p.rows * p.nl > p.threads ? 0 : 4) : p.cols == kNormCols ? 1 : 2;
     // (a row of bf16 always leaves the sums room: 192 KB in all at 8192 columns)
     if constexpr (LN && sizeof(T) == 4)
         if (which == 1 && !p.sm) {
             kern = norm_bwd_kernel<T, VW, LN, false, kNormCols, 1>;
             which = 3;
         }
-    static std::once_flag once[64][4];
-    static cudaError_t set_err[64][4];
+    static std::once_flag once[64][5];
+    static cudaError_t set_err[64][5];
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
@@ -1376,10 +1399,14 @@ int hcw_residual_norm_bwd(const void* dr_out, const void* dx_out, const void* s,
     q.rows = T > 0 ? p.grid : 0;
     q.slices = T > 0 ? p.slices : 0;
     q.d = d;
-    q.ncb = (d + 31) / 32;
-    const unsigned blocks =
-        (unsigned)q.ncb * (unsigned)(kNormPar + (gate_sum ? (T > 0 ? p.groups : 1) : 0));
-    return count_launch(launch_pdl(norm_reduce_kernel, dim3(blocks), dim3(1024), 0, st, q), 1);
+    q.c_log2 = reduce_cols(q.rows);
+    q.g_log2 = reduce_cols(q.slices);
+    q.ncb = (d + (1 << q.c_log2) - 1) >> q.c_log2;
+    q.ncg = (d + (1 << q.g_log2) - 1) >> q.g_log2;
+    const unsigned blocks = (unsigned)q.ncb * kNormPar +
+                            (unsigned)q.ncg * (gate_sum ? (unsigned)(T > 0 ? p.groups : 1) : 0u);
+    return count_launch(
+        launch_pdl(norm_reduce_kernel, dim3(blocks), dim3(kReduceThreads), 0, st, q), 1);
 }
 
 }  // extern "C"
