@@ -60,7 +60,7 @@ constexpr int ffn_patches(int mode) { return mode == FFN_GRAD ? 4 : 2; }
 struct __align__(8) FfnBars {
     uint64_t full[kFMaxStages];    // leader: both CTAs' copies of a stage landed
     uint64_t empty[kFMaxStages];   // each CTA: the pair's MMAs have read the stage
-    uint64_t tfull[2];             // each CTA: a unit's accumulators are complete
+    uint64_t tfull[2];             // each CTA: accumulators are complete (FFN_GRAD: g, u; da)
     uint64_t tempty[2];            // leader: both CTAs have drained them
     uint64_t drain;
     uint32_t tmem_base;
@@ -93,6 +93,7 @@ struct FfnArgs {
     FfnProd p[3];
     int n_prod, n_units;
     int h;                // FFN_GATE / FFN_GRAD: hidden columns (first up row of W1)
+    int wide, cut;        // FFN_GRAD: units of 256 hidden columns, and those cut into two of 128
     unsigned long long timeout_ns;
 };
 
@@ -168,10 +169,26 @@ __global__ void __launch_bounds__(kFThreads, 1) ffn_pair_kernel(const __grid_con
     // together share rows of A)
     struct Unit {
         int q, s, mi, ni;
+        bool wide;
     };
     auto unit = [&](int v) {
         Unit t;
-        t.q = 0;
+        t.q = t.s = 0;
+        t.wide = false;
+        if (MODE == FFN_GRAD) {
+            // ni: the first block of 128 hidden columns; last the odd block of each row tile
+            const int cols = a.p[0].nt / 2, k = v - a.wide;
+            if (k < 2 * a.cut) {
+                t.wide = k < 0;
+                const int w = t.wide ? v : a.wide + (k >> 1);
+                t.mi = w / cols;
+                t.ni = 2 * (w - t.mi * cols) + (t.wide ? 0 : k & 1);
+            } else {
+                t.mi = k - 2 * a.cut;
+                t.ni = a.p[0].nt - 1;
+            }
+            return t;
+        }
         if (MODE == FFN_GEMM)
             while (t.q + 1 < a.n_prod && v >= a.p[t.q + 1].unit0) ++t.q;
         const FfnProd& p = a.p[t.q];
@@ -183,8 +200,15 @@ __global__ void __launch_bounds__(kFThreads, 1) ffn_pair_kernel(const __grid_con
         t.ni = rem - t.mi * p.nt;
         return t;
     };
-    // A unit's passes over K: one product, or two for FFN_GRAD.
-    constexpr int kPasses = MODE == FFN_GRAD ? 2 : 1;
+    // A unit's passes over K: one product; FFN_GRAD: g and u of the first 128 hidden columns,
+    // da of all (under which the first g and u are drained), g and u of the second 128.
+    auto passes = [&](const Unit& t) { return MODE != FFN_GRAD ? 1 : t.wide ? 3 : 2; };
+    auto product = [&](const Unit& t, int pass) -> const FfnProd& {
+        return a.p[MODE == FFN_GEMM ? t.q : MODE == FFN_GRAD && pass != 1 ? 1 : 0];
+    };
+    auto tile_cols = [&](const Unit& t, int pass, const FfnProd& p) {
+        return MODE == FFN_GRAD && pass == 1 ? (t.wide ? 256 : 128) : p.bn;
+    };
     auto k_range = [&](const FfnProd& p, int s, int& kb0, int& kb1) {
         kb0 = MODE == FFN_GEMM ? s * p.kps : 0;
         kb1 = MODE == FFN_GEMM && kb0 + p.kps < p.nkb ? kb0 + p.kps : p.nkb;
@@ -198,18 +222,17 @@ __global__ void __launch_bounds__(kFThreads, 1) ffn_pair_kernel(const __grid_con
             bool ok = true;
             for (int v = pair; v < a.n_units && ok; v += n_pairs) {
                 const Unit t = unit(v);
-                for (int pass = 0; pass < kPasses && ok; ++pass) {
-                    const FfnProd& p = a.p[MODE == FFN_GEMM ? t.q : pass];
+                for (int pass = 0; pass < passes(t) && ok; ++pass) {
+                    const FfnProd& p = product(t, pass);
                     int kb0, kb1;
                     k_range(p, t.s, kb0, kb1);
                     const int a_mn = p.a_mn, b_mn = p.b_mn;
-                    const int bc = p.bn / 2;   // this CTA's columns of B
-                    // FFN_GATE and the second pass of FFN_GRAD: gate rows on one CTA, up
-                    // rows on the other
-                    const bool split_b = MODE == FFN_GATE || (MODE == FFN_GRAD && pass == 1);
+                    const int bc = tile_cols(t, pass, p) / 2;   // this CTA's columns of B
+                    // g and u: gate rows on one CTA, up rows on the other
+                    const bool split_b = MODE == FFN_GATE || (MODE == FFN_GRAD && pass != 1);
                     const int a_row = (2 * t.mi + (int)rank) * kFM;
-                    const int b_row = split_b ? (int)rank * a.h + t.ni * 128
-                                              : t.ni * p.bn + (int)rank * bc;
+                    const int b_row = split_b ? (int)rank * a.h + (t.ni + (pass >> 1)) * 128
+                                              : t.ni * (MODE == FFN_GRAD ? 128 : p.bn) + (int)rank * bc;
                     const uint32_t tx = 2u * (uint32_t)(kFA + bc * kFK * 2);
                     for (int kb = kb0; kb < kb1; ++kb) {
                         if (!mbar_wait(&bars->empty[stage], phase ^ 1, abort, tmo)) {
@@ -251,34 +274,26 @@ __global__ void __launch_bounds__(kFThreads, 1) ffn_pair_kernel(const __grid_con
     } else if (warp == 1) {
         // ------------------------------------------------------------ MMA issuer (leader)
         if (lane == 0 && rank == 0) {
-            int stage = 0, it = 0;
+            int stage = 0, it = 0, ig = 0;   // ig: passes of g and u
             uint32_t phase = 0;
             bool ok = true, any = false;
             for (int v = pair; v < a.n_units && ok; v += n_pairs, ++it) {
                 const Unit t = unit(v);
-                for (int pass = 0; pass < kPasses && ok; ++pass) {
-                    const FfnProd& p = a.p[MODE == FFN_GEMM ? t.q : pass];
+                for (int pass = 0; pass < passes(t) && ok; ++pass) {
+                    const FfnProd& p = product(t, pass);
                     int kb0, kb1;
                     k_range(p, t.s, kb0, kb1);
-                    const uint32_t idesc = idesc_bf16_f32(2 * kFM, p.bn, p.a_mn, p.b_mn);
+                    const uint32_t idesc =
+                        idesc_bf16_f32(2 * kFM, tile_cols(t, pass, p), p.a_mn, p.b_mn);
                     // bytes from one 16-deep step to the next within a stage
                     const uint32_t a_step = p.a_mn ? 2048 : 32, b_step = p.b_mn ? 2048 : 32;
                     const uint32_t a_lbo = p.a_mn ? 8192 : 16, b_lbo = p.b_mn ? 8192 : 16;
-                    uint32_t d_tmem;
-                    if (MODE != FFN_GRAD) {
-                        // accumulator it % 2: drained of unit it - 2
-                        if (!mbar_wait(&bars->tempty[it & 1], ((it >> 1) & 1) ^ 1, abort, tmo))
-                            ok = false;
-                        d_tmem = tmem_base + (uint32_t)(it & 1) * 256;
-                    } else if (pass == 0) {
-                        // da, buffer it % 2: its unit it - 2 was drained before the g, u
-                        // products of unit it - 1 began
-                        d_tmem = tmem_base + (uint32_t)(it & 1) * 128;
-                    } else {
-                        // g and u: drained of unit it - 1
-                        if (!mbar_wait(&bars->tempty[0], (it & 1) ^ 1, abort, tmo)) ok = false;
-                        d_tmem = tmem_base + 256;
-                    }
+                    // the accumulator: it % 2, drained of unit it - 2; FFN_GRAD: 0 (g and u) or
+                    // 1 (da), drained of its last pass
+                    const int acc = MODE == FFN_GRAD ? pass & 1 : it & 1;
+                    const int use = MODE != FFN_GRAD ? it >> 1 : acc ? it : ig++;
+                    if (!mbar_wait(&bars->tempty[acc], (use & 1) ^ 1, abort, tmo)) ok = false;
+                    const uint32_t d_tmem = tmem_base + (uint32_t)acc * 256;
                     if (!ok) break;
                     tc_fence_after();
                     for (int kb = kb0; kb < kb1; ++kb) {
@@ -301,8 +316,8 @@ __global__ void __launch_bounds__(kFThreads, 1) ffn_pair_kernel(const __grid_con
                             phase ^= 1;
                         }
                     }
+                    if (ok) mma_commit_pair(&bars->tfull[acc], 3);
                 }
-                if (ok) mma_commit_pair(&bars->tfull[it & 1], 3);
             }
             if (any) {
                 // the pair's MMAs have completed before TMEM can be freed
@@ -344,21 +359,99 @@ __global__ void __launch_bounds__(kFThreads, 1) ffn_pair_kernel(const __grid_con
                 bulk_commit();
             }
         };
-        int it = 0;
-        for (int v = pair; v < a.n_units; v += n_pairs, ++it) {
+        // accumulator i has been read by this warp
+        auto release = [&](int i) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_remote_tmem(mapa_shared(&bars->tempty[i], 0));
+        };
+        int it = 0, ig = 0;
+        bool ok = true;
+        for (int v = pair; v < a.n_units && ok; v += n_pairs, ++it) {
             const Unit t = unit(v);
+            if constexpr (MODE == FFN_GRAD) {
+                const int row0 = (2 * t.mi + (int)rank) * kFM + quarter * 32;
+#pragma unroll 1
+                for (int half = 0; half < (t.wide ? 2 : 1) && ok; ++half, ++ig) {
+                    const int col = (t.ni + half) * 128 + chalf * 64;   // the warp's 64 columns
+                    const bool st = row0 < a.p[0].M && col < a.h;       // warp-uniform
+                    // g and u go to registers at once: the next pass takes their place while
+                    // these are worked on
+                    const uint32_t tg = tmem_base + lanes + (uint32_t)(chalf * 64);
+                    const uint32_t td = tg + 256u + (uint32_t)(half * 128);
+                    uint32_t g[64], u[64];
+                    ok = __all_sync(0xffffffffu, mbar_wait(&bars->tfull[0], ig & 1, abort, tmo));
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (st) {
+#pragma unroll
+                        for (int c = 0; c < 64; c += 32) {
+                            tmem_ld_32x32b_x32(tg + (uint32_t)c,
+                                               *reinterpret_cast<uint32_t(*)[32]>(g + c));
+                            tmem_ld_32x32b_x32(tg + (uint32_t)(128 + c),
+                                               *reinterpret_cast<uint32_t(*)[32]>(u + c));
+                        }
+#pragma unroll
+                        for (int c = 0; c < 64; c += 32) {
+                            tmem_ld_wait_regs(*reinterpret_cast<uint32_t(*)[32]>(g + c));
+                            tmem_ld_wait_regs(*reinterpret_cast<uint32_t(*)[32]>(u + c));
+                        }
+                    }
+                    release(0);
+                    if (half == 0) {
+                        ok = __all_sync(0xffffffffu, mbar_wait(&bars->tfull[1], it & 1, abort, tmo));
+                        if (!ok) break;
+                        tc_fence_after();
+                    }
+#pragma unroll
+                    for (int c = 0; c < 64; c += 32) {
+                        if (!st || col + c >= a.h) break;   // warp-uniform
+                        patches_free();
+                        uint8_t *const bg = patch(), *const bu = patch(), *const ba = patch();
+                        uint32_t d[16];
+#pragma unroll
+                        for (int m = 0; m < 4; ++m) {
+                            uint32_t wg[4], wu[4], wa[4];
+                            if (m % 2 == 0) {
+                                __syncwarp();
+                                tmem_ld_32x32b_x16(td + (uint32_t)(c + 8 * m), d);
+                                tmem_ld_wait_regs(d);
+                            }
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                float og[2], ou[2], oa[2];
+#pragma unroll
+                                for (int i = 0; i < 2; ++i) {
+                                    const int q = 8 * m + 2 * j + i;
+                                    const float da = __uint_as_float(d[q & 15]);
+                                    const float uu = __uint_as_float(u[c + q]);
+                                    float dact;
+                                    const float ag = ffn_act<ACT>(__uint_as_float(g[c + q]), &dact);
+                                    og[i] = da * uu * dact;
+                                    ou[i] = da * ag;
+                                    oa[i] = ag * uu;
+                                }
+                                wg[j] = pack_bf16x2(og[0], og[1]);
+                                wu[j] = pack_bf16x2(ou[0], ou[1]);
+                                wa[j] = pack_bf16x2(oa[0], oa[1]);
+                            }
+                            *chunk(bg, m) = make_uint4(wg[0], wg[1], wg[2], wg[3]);
+                            *chunk(bu, m) = make_uint4(wu[0], wu[1], wu[2], wu[3]);
+                            *chunk(ba, m) = make_uint4(wa[0], wa[1], wa[2], wa[3]);
+                        }
+                        store_2d(&a.p[0].mOut, bg, col + c, row0);
+                        store_2d(&a.p[1].mOut, bu, col + c, row0);
+                        store_2d(&a.p[2].mOut, ba, col + c, row0);
+                    }
+                    if (half == (t.wide ? 1 : 0)) release(1);
+                }
+                continue;
+            }
             const FfnProd& p = a.p[MODE == FFN_GEMM ? t.q : 0];
             const int row0 = (2 * t.mi + (int)rank) * kFM + quarter * 32;
             const bool okw = mbar_wait(&bars->tfull[it & 1], (it >> 1) & 1, abort, tmo);
             if (!__all_sync(0xffffffffu, okw)) break;
             tc_fence_after();
-            const uint32_t tempty =
-                mapa_shared(&bars->tempty[MODE == FFN_GRAD ? 0 : it & 1], 0);
-            auto release = [&]() {   // this warp has read the unit's accumulators
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive_remote_tmem(tempty);
-            };
             if (MODE == FFN_GEMM) {
                 const int cw = p.bn / 2;                       // the warp's columns
                 const int colw = t.ni * p.bn + chalf * cw;
@@ -372,7 +465,7 @@ __global__ void __launch_bounds__(kFThreads, 1) ffn_pair_kernel(const __grid_con
                         tmem_ld_32x32b_x32(tb + (uint32_t)c, r);
                         tmem_ld_wait_regs(r);
                     }
-                    if (c + 32 == cw) release();
+                    if (c + 32 == cw) release(it & 1);
                     if (!st) continue;
                     if (p.f32) {
 #pragma unroll
@@ -411,10 +504,10 @@ __global__ void __launch_bounds__(kFThreads, 1) ffn_pair_kernel(const __grid_con
             const int col = t.ni * 128 + chalf * 64;   // the warp's 64 hidden columns
             const bool st = row0 < p.M && col < a.h;
             if (!st) {
-                release();
+                release(it & 1);
                 continue;
             }
-            if (MODE == FFN_GATE) {
+            if constexpr (MODE == FFN_GATE) {
                 const uint32_t tg = tmem_base + lanes + (uint32_t)((it & 1) * 256 + chalf * 64);
 #pragma unroll 1
                 for (int c = 0; c < 64; c += 32) {
@@ -424,7 +517,7 @@ __global__ void __launch_bounds__(kFThreads, 1) ffn_pair_kernel(const __grid_con
                     tmem_ld_32x32b_x32(tg + (uint32_t)(128 + c), u);
                     tmem_ld_wait_regs(g);
                     tmem_ld_wait_regs(u);
-                    if (c) release();
+                    if (c) release(it & 1);
                     if (col + c >= a.h) continue;   // warp-uniform
                     patches_free();
                     uint8_t* buf = patch();
@@ -442,51 +535,6 @@ __global__ void __launch_bounds__(kFThreads, 1) ffn_pair_kernel(const __grid_con
                         *chunk(buf, m) = make_uint4(w[0], w[1], w[2], w[3]);
                     }
                     store_2d(&p.mOut, buf, col + c, row0);
-                }
-            } else {
-                const uint32_t td = tmem_base + lanes + (uint32_t)((it & 1) * 128 + chalf * 64);
-                const uint32_t tg = tmem_base + lanes + (uint32_t)(256 + chalf * 64);
-#pragma unroll 1
-                for (int c = 0; c < 64; c += 32) {
-                    uint32_t d[32], g[32], u[32];
-                    __syncwarp();
-                    tmem_ld_32x32b_x32(td + (uint32_t)c, d);
-                    tmem_ld_32x32b_x32(tg + (uint32_t)c, g);
-                    tmem_ld_32x32b_x32(tg + (uint32_t)(128 + c), u);
-                    tmem_ld_wait_regs(d);
-                    tmem_ld_wait_regs(g);
-                    tmem_ld_wait_regs(u);
-                    if (c) release();
-                    if (col + c >= a.h) continue;   // warp-uniform
-                    patches_free();
-                    uint8_t *const bg = patch(), *const bu = patch(), *const ba = patch();
-#pragma unroll
-                    for (int m = 0; m < 4; ++m) {
-                        uint32_t wg[4], wu[4], wa[4];
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            float og[2], ou[2], oa[2];
-#pragma unroll
-                            for (int i = 0; i < 2; ++i) {
-                                const int q = 8 * m + 2 * j + i;
-                                const float da = __uint_as_float(d[q]), uu = __uint_as_float(u[q]);
-                                float dact;
-                                const float ag = ffn_act<ACT>(__uint_as_float(g[q]), &dact);
-                                og[i] = da * uu * dact;
-                                ou[i] = da * ag;
-                                oa[i] = ag * uu;
-                            }
-                            wg[j] = pack_bf16x2(og[0], og[1]);
-                            wu[j] = pack_bf16x2(ou[0], ou[1]);
-                            wa[j] = pack_bf16x2(oa[0], oa[1]);
-                        }
-                        *chunk(bg, m) = make_uint4(wg[0], wg[1], wg[2], wg[3]);
-                        *chunk(bu, m) = make_uint4(wu[0], wu[1], wu[2], wu[3]);
-                        *chunk(ba, m) = make_uint4(wa[0], wa[1], wa[2], wa[3]);
-                    }
-                    store_2d(&a.p[0].mOut, bg, col + c, row0);
-                    store_2d(&a.p[1].mOut, bu, col + c, row0);
-                    store_2d(&a.p[2].mOut, ba, col + c, row0);
                 }
             }
         }
@@ -996,6 +1044,32 @@ size_t ffn_part_bytes(const FfnShape* s, int n) {
     return b;
 }
 
+// Units of the gradient pass: 256 hidden columns, whose da runs at the rate of 256-column
+// products (of 128 columns a K step takes 0.75 of that time, not half), and 128 columns for odd
+// ends.  The last round's units are cut in two where that shortens the busiest pair's share.
+void ffn_grad_units(FfnArgs& a, int pairs) {
+    const int mt = a.p[0].mt, nt = a.p[0].nt, all = mt * (nt / 2), odd = mt * (nt & 1);
+    const double k = a.p[0].nkb, whole = 3 * k + 3, half = 1.75 * k + 2;
+    double best = 0;
+    for (int i = 0; i < 3; ++i) {
+        const int cut = i == 0 ? 0 : i == 1 ? all % pairs : all;
+        const int wide = all - cut, units = all + cut + odd;
+        double most = 0;
+        for (int p = 0; p < pairs; ++p) {   // pair p: units p, p + pairs, ...
+            const int n = units > p ? (units - p + pairs - 1) / pairs : 0;
+            const int w = wide > p ? (wide - p + pairs - 1) / pairs : 0;
+            const double t = w * whole + (n - w) * half;
+            most = t > most ? t : most;
+        }
+        if (i == 0 || most < best) {
+            best = most;
+            a.wide = wide;
+            a.cut = cut;
+            a.n_units = units;
+        }
+    }
+}
+
 struct FfnOperands {
     const void* A;
     bool a_mn;
@@ -1276,7 +1350,7 @@ int hcw_gated_ffn_bwd(const void* x, const void* dy, const void* W1, const void*
         p.nt = (h + 127) / 128;
     }
     a.n_prod = 2;
-    a.n_units = a.p[0].mt * a.p[0].nt;
+    ffn_grad_units(a, pairs);
     a.h = h;
     a.timeout_ns = kFTimeoutNs;
     if (!ffn_operand(&a.p[0].mA, dy, T, d, false, kFM) ||
