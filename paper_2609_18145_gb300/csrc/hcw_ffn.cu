@@ -19,10 +19,10 @@
 //   grad    the same tile, three accumulators: da (128 columns), then g and u.  da has a
 //           second buffer (512 TMEM columns in all), so that the next tile's da
 //           products run under this tile's epilogue, which writes dg, du and a.
-//   gemm    y, or dx, dW1 and dW2 together: a list of up to three products in one launch,
-//           the units of the longest K first.  A product with few tiles and a long
-//           K splits it; the splits' fp32 partial sums are added in split order by
-//           a second kernel.
+//   gemm    y, or dx, dW1 and dW2 together: up to three products in one launch.  Each pair
+//           takes the same number of whole tiles; the tiles left over form a line of K
+//           steps that is cut into even shares.  A tile that was cut is added up from its
+//           parts' fp32 sums, in the order of K, by a second kernel.
 //
 // g, u and da stay in fp32; a, dg and du are rounded to bf16 once, because they are the
 // next products' operands; y, dx, dW1 and dW2 once more when they are stored (dW in fp32
@@ -77,21 +77,36 @@ static_assert(ffn_smem(FFN_GEMM) <= 232448 && ffn_smem(FFN_GRAD) <= 232448, "sha
 // (box 64 x 128), or MN-major (_mn: a row-major [K][cols] matrix in 64 x 64 boxes).
 struct FfnProd {
     CUtensorMap mA, mB;
-    CUtensorMap mOut;     // bf16 (N, M) box (32, 32), or fp32 (N, M, splits) box (16, 32, 1)
+    CUtensorMap mOut;     // bf16 (N, M) box (32, 32), or fp32 (N, M, 1) box (16, 32, 1)
     int a_mn, b_mn;
     int M, N;
     int bn;               // tile columns: 256 or 128
-    int nkb, kps, splits; // K steps, K steps of a split, splits
+    int nkb;              // K steps
     int mt, nt;           // tiles
-    int unit0;            // first unit
+    int unit0, whole;     // first unit of the tiles taken whole, their number
+    int line0;            // place on the line of the first tile left over
     int f32;              // fp32 output (mOut)
+};
+
+constexpr int kFCuts = 256;   // shares of the line at most
+constexpr int kFSlot = 256 * 256;   // floats of a part's sums
+
+// Where the line's shares begin: a tile (by its place on the line) and a K step in it.  Share j
+// ends where share j + 1 begins.  Tiles cut alike (`each` parts of each of `tiles`) are taken
+// part by part: the pairs that run together then read the same K steps.
+struct FfnLine {
+    int shares, each, tiles;
+    unsigned short tile[kFCuts + 1];
+    int step[kFCuts + 1];
 };
 
 struct FfnArgs {
     // FFN_GATE: p[0] = (x, W1) -> a.  FFN_GRAD: p[0] = (dy, W2) with mOut dg,
     // p[1] = (x, W1) with mOut du, p[2].mOut a.
     FfnProd p[3];
-    int n_prod, n_units;
+    int n_prod, n_units;  // units: whole tiles
+    CUtensorMap mPart;    // FFN_GEMM: the parts' sums, fp32 (256, 256, slots) box (16, 32, 1)
+    FfnLine line;
     int h;                // FFN_GATE / FFN_GRAD: hidden columns (first up row of W1)
     int wide, cut;        // FFN_GRAD: units of 256 hidden columns, and those cut into two of 128
     unsigned long long timeout_ns;
@@ -165,41 +180,76 @@ __global__ void __launch_bounds__(kFThreads, 1) ffn_pair_kernel(const __grid_con
     const uint32_t tmem_base = bars->tmem_base;
     volatile int* abort = &bars->abort;
 
-    // unit -> product, split, row tile, column tile (columns fastest: the pairs that run
-    // together share rows of A)
+    // A unit: a tile (columns fastest: the pairs that run together share rows of A), or K steps
+    // [kb0, kb1) of one, whose sums go to a slot.
     struct Unit {
-        int q, s, mi, ni;
-        bool wide;
+        int q, mi, ni;
+        int kb0, kb1, slot;   // FFN_GEMM; slot -1: the whole tile
+        bool wide;            // FFN_GRAD
     };
-    auto unit = [&](int v) {
-        Unit t;
-        t.q = t.s = 0;
+    // The pair's units in turn: whole tiles, then its shares of the line.
+    struct Walk {
+        int v, turn, j, tile, step;
+        bool open;   // inside share j (the turn's), at (tile, step)
+    };
+    auto next = [&](Walk& w, Unit& t) {
+        t.q = t.kb0 = 0;
+        t.slot = -1;
         t.wide = false;
-        if (MODE == FFN_GRAD) {
-            // ni: the first block of 128 hidden columns; last the odd block of each row tile
-            const int cols = a.p[0].nt / 2, k = v - a.wide;
-            if (k < 2 * a.cut) {
-                t.wide = k < 0;
-                const int w = t.wide ? v : a.wide + (k >> 1);
-                t.mi = w / cols;
-                t.ni = 2 * (w - t.mi * cols) + (t.wide ? 0 : k & 1);
-            } else {
-                t.mi = k - 2 * a.cut;
-                t.ni = a.p[0].nt - 1;
+        int v = w.v;
+        if (v < a.n_units) {
+            w.v += n_pairs;
+            if (MODE == FFN_GRAD) {
+                // ni: the first block of 128 hidden columns; last the odd block of each row
+                // tile
+                const int cols = a.p[0].nt / 2, k = v - a.wide;
+                if (k < 2 * a.cut) {
+                    t.wide = k < 0;
+                    const int x = t.wide ? v : a.wide + (k >> 1);
+                    t.mi = x / cols;
+                    t.ni = 2 * (x - t.mi * cols) + (t.wide ? 0 : k & 1);
+                } else {
+                    t.mi = k - 2 * a.cut;
+                    t.ni = a.p[0].nt - 1;
+                }
+                return true;
             }
-            return t;
+            if (MODE == FFN_GEMM) {
+                while (t.q + 1 < a.n_prod && v >= a.p[t.q + 1].unit0) ++t.q;
+                v -= a.p[t.q].unit0;
+            }
+            t.kb1 = a.p[t.q].nkb;
+        } else {
+            if (MODE != FFN_GEMM) return false;
+            for (;;) {
+                if (w.turn >= a.line.shares) return false;
+                if (!w.open) {
+                    w.j = a.line.each ? w.turn % a.line.tiles * a.line.each + w.turn / a.line.tiles
+                                      : w.turn;
+                    w.tile = a.line.tile[w.j];
+                    w.step = a.line.step[w.j];
+                    w.open = true;
+                }
+                if (w.tile < a.line.tile[w.j + 1] ||
+                    (w.tile == a.line.tile[w.j + 1] && w.step < a.line.step[w.j + 1]))
+                    break;
+                w.turn += n_pairs;
+                w.open = false;
+            }
+            while (t.q + 1 < a.n_prod && w.tile >= a.p[t.q + 1].line0) ++t.q;
+            v = a.p[t.q].whole + w.tile - a.p[t.q].line0;
+            const int nkb = a.p[t.q].nkb;
+            t.kb0 = w.step;
+            t.kb1 = w.tile < a.line.tile[w.j + 1] ? nkb : a.line.step[w.j + 1];
+            if (t.kb0 > 0 || t.kb1 < nkb) t.slot = w.tile + w.j;
+            ++w.tile;
+            w.step = 0;
         }
-        if (MODE == FFN_GEMM)
-            while (t.q + 1 < a.n_prod && v >= a.p[t.q + 1].unit0) ++t.q;
-        const FfnProd& p = a.p[t.q];
-        if (MODE == FFN_GEMM) v -= p.unit0;
-        const int tiles = p.mt * p.nt;
-        t.s = v / tiles;
-        const int rem = v - t.s * tiles;
-        t.mi = rem / p.nt;
-        t.ni = rem - t.mi * p.nt;
-        return t;
+        t.mi = v / a.p[t.q].nt;
+        t.ni = v - t.mi * a.p[t.q].nt;
+        return true;
     };
+    const Walk start = {pair, pair, 0, 0, 0, false};
     // A unit's passes over K: one product; FFN_GRAD: g and u of the first 128 hidden columns,
     // da of all (under which the first g and u are drained), g and u of the second 128.
     auto passes = [&](const Unit& t) { return MODE != FFN_GRAD ? 1 : t.wide ? 3 : 2; };
@@ -209,9 +259,9 @@ __global__ void __launch_bounds__(kFThreads, 1) ffn_pair_kernel(const __grid_con
     auto tile_cols = [&](const Unit& t, int pass, const FfnProd& p) {
         return MODE == FFN_GRAD && pass == 1 ? (t.wide ? 256 : 128) : p.bn;
     };
-    auto k_range = [&](const FfnProd& p, int s, int& kb0, int& kb1) {
-        kb0 = MODE == FFN_GEMM ? s * p.kps : 0;
-        kb1 = MODE == FFN_GEMM && kb0 + p.kps < p.nkb ? kb0 + p.kps : p.nkb;
+    auto k_range = [&](const Unit& t, const FfnProd& p, int& kb0, int& kb1) {
+        kb0 = t.kb0;
+        kb1 = MODE == FFN_GEMM ? t.kb1 : p.nkb;
     };
 
     if (warp == 0) {
@@ -220,12 +270,12 @@ __global__ void __launch_bounds__(kFThreads, 1) ffn_pair_kernel(const __grid_con
             int stage = 0;
             uint32_t phase = 0, issued_mask = 0, issued_phase = 0;
             bool ok = true;
-            for (int v = pair; v < a.n_units && ok; v += n_pairs) {
-                const Unit t = unit(v);
+            Walk walk = start;
+            for (Unit t; ok && next(walk, t);) {
                 for (int pass = 0; pass < passes(t) && ok; ++pass) {
                     const FfnProd& p = product(t, pass);
                     int kb0, kb1;
-                    k_range(p, t.s, kb0, kb1);
+                    k_range(t, p, kb0, kb1);
                     const int a_mn = p.a_mn, b_mn = p.b_mn;
                     const int bc = tile_cols(t, pass, p) / 2;   // this CTA's columns of B
                     // g and u: gate rows on one CTA, up rows on the other
@@ -277,12 +327,12 @@ __global__ void __launch_bounds__(kFThreads, 1) ffn_pair_kernel(const __grid_con
             int stage = 0, it = 0, ig = 0;   // ig: passes of g and u
             uint32_t phase = 0;
             bool ok = true, any = false;
-            for (int v = pair; v < a.n_units && ok; v += n_pairs, ++it) {
-                const Unit t = unit(v);
+            Walk walk = start;
+            for (Unit t; ok && next(walk, t); ++it) {
                 for (int pass = 0; pass < passes(t) && ok; ++pass) {
                     const FfnProd& p = product(t, pass);
                     int kb0, kb1;
-                    k_range(p, t.s, kb0, kb1);
+                    k_range(t, p, kb0, kb1);
                     const uint32_t idesc =
                         idesc_bf16_f32(2 * kFM, tile_cols(t, pass, p), p.a_mn, p.b_mn);
                     // bytes from one 16-deep step to the next within a stage
@@ -367,8 +417,8 @@ __global__ void __launch_bounds__(kFThreads, 1) ffn_pair_kernel(const __grid_con
         };
         int it = 0, ig = 0;
         bool ok = true;
-        for (int v = pair; v < a.n_units && ok; v += n_pairs, ++it) {
-            const Unit t = unit(v);
+        Walk walk = start;
+        for (Unit t; ok && next(walk, t); ++it) {
             if constexpr (MODE == FFN_GRAD) {
                 const int row0 = (2 * t.mi + (int)rank) * kFM + quarter * 32;
 #pragma unroll 1
@@ -467,7 +517,7 @@ __global__ void __launch_bounds__(kFThreads, 1) ffn_pair_kernel(const __grid_con
                     }
                     if (c + 32 == cw) release(it & 1);
                     if (!st) continue;
-                    if (p.f32) {
+                    if (p.f32 || t.slot >= 0) {
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
                             if (colw + c + 16 * h >= p.N) break;   // warp-uniform
@@ -480,7 +530,11 @@ __global__ void __launch_bounds__(kFThreads, 1) ffn_pair_kernel(const __grid_con
                             fence_proxy_async_smem();
                             __syncwarp();
                             if (lane == 0) {
-                                tma_store_3d(&p.mOut, buf, colw + c + 16 * h, row0, t.s);
+                                if (t.slot >= 0)
+                                    tma_store_3d(&a.mPart, buf, chalf * cw + c + 16 * h,
+                                                 (int)rank * kFM + quarter * 32, t.slot);
+                                else
+                                    tma_store_3d(&p.mOut, buf, colw + c + 16 * h, row0, 0);
                                 bulk_commit();
                             }
                         }
@@ -553,39 +607,57 @@ __global__ void __launch_bounds__(kFThreads, 1) ffn_pair_kernel(const __grid_con
     }
 }
 
-// out[i] = sum over the splits, in order, of part[s][i] (zero without splits), for up to
-// three matrices of a multiple of four elements, one after the other.
+// The tiles that were cut, from their parts in the order of K: slots [slot, slot + parts) of tile
+// `tile` (by its place on the line).  A block adds 4 rows of a tile; 64 blocks a tile.
 struct FfnReduce {
+    const float* part;
     struct {
-        const float* part;
         void* out;
-        size_t count4;   // groups of four
-        int splits, f32;
-    } m[3];
+        int M, N, bn, nt, whole, line0, f32;
+    } p[3];
+    int n_prod;
+    struct {
+        unsigned short tile, slot, parts;
+    } t[kFCuts];
 };
 
-__global__ void __launch_bounds__(256) ffn_reduce_kernel(const FfnReduce a) {
+__global__ void __launch_bounds__(256) ffn_reduce_kernel(const __grid_constant__ FfnReduce a) {
     pdl_wait();
     pdl_trigger();
-    for (int q = 0; q < 3; ++q) {
-        const auto& m = a.m[q];
-        for (size_t i = blockIdx.x * (size_t)blockDim.x + threadIdx.x; i < m.count4;
-             i += (size_t)gridDim.x * blockDim.x) {
-            float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
-            for (int s = 0; s < m.splits; ++s) {
-                const float4 v = reinterpret_cast<const float4*>(m.part)[(size_t)s * m.count4 + i];
-                t.x += v.x;
-                t.y += v.y;
-                t.z += v.z;
-                t.w += v.w;
-            }
-            if (m.f32)
-                reinterpret_cast<float4*>(m.out)[i] = t;
-            else
-                reinterpret_cast<uint2*>(m.out)[i] =
-                    make_uint2(pack_bf16x2(t.x, t.y), pack_bf16x2(t.z, t.w));
-        }
+    const auto& t = a.t[blockIdx.x >> 6];
+    int q = 0;
+    while (q + 1 < a.n_prod && t.tile >= a.p[q + 1].line0) ++q;
+    const auto& p = a.p[q];
+    const int v = p.whole + t.tile - p.line0, mi = v / p.nt, ni = v - mi * p.nt;
+    const int r = (int)(blockIdx.x & 63) * 4 + (int)(threadIdx.x >> 6), row = mi * 256 + r;
+    const int c = (threadIdx.x & 63) * 4, col = ni * p.bn + c;
+    if (c >= p.bn || col >= p.N || row >= p.M) return;
+    const float4* src =
+        reinterpret_cast<const float4*>(a.part + (size_t)t.slot * kFSlot + r * 256 + c);
+    float4 s = *src;
+#pragma unroll 4
+    for (int i = 1; i < t.parts; ++i) {
+        const float4 x = src[(size_t)i * (kFSlot / 4)];
+        s.x += x.x;
+        s.y += x.y;
+        s.z += x.z;
+        s.w += x.w;
     }
+    const size_t at = (size_t)row * p.N + col;
+    if (p.f32)
+        *reinterpret_cast<float4*>(static_cast<float*>(p.out) + at) = s;
+    else
+        *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.out) + at) =
+            make_uint2(pack_bf16x2(s.x, s.y), pack_bf16x2(s.z, s.w));
+}
+
+// Zeros (the weight gradients of no tokens).
+__global__ void __launch_bounds__(256) ffn_zero_kernel(uint4* a, size_t na, uint4* b, size_t nb) {
+    pdl_wait();
+    pdl_trigger();
+    for (size_t i = blockIdx.x * (size_t)blockDim.x + threadIdx.x; i < na + nb;
+         i += (size_t)gridDim.x * blockDim.x)
+        (i < na ? a[i] : b[i - na]) = make_uint4(0u, 0u, 0u, 0u);
 }
 
 // ------------------------------------------------------------------ few tokens
@@ -995,54 +1067,170 @@ struct FfnShape {
     long long M, N, K;
     int out_f32;       // the output itself is fp32
     // filled by the plan
-    int bn, nkb, kps, splits;
+    int bn, nkb, mt, nt;
+    int whole, line0;  // tiles taken whole; place on the line of the first of the others
+    int tiles() const { return mt * nt; }
+    double step() const { return bn == 256 ? 1.0 : 0.75; }   // time of a K step
 };
 
-// Tile columns and K splits of the products of one launch on `pairs` pairs: over a range of
-// unit lengths L (K steps), the least of
-//   the units' K steps spread over the pairs, half a longest unit for the uneven end, no
-//   less than one longest unit, at 0.3 us a step (256 columns), and
-//   the fp32 partials written and read at 6 TB/s, and 3 us for the kernel that adds them.
-void ffn_plan(FfnShape* s, int n, int pairs) {
-    double best = 1e30;
-    for (int L = 4; L <= 1 << 20; L = L < 64 ? L + 4 : L * 2) {
-        double total = 0, longest = 0, bytes = 0;
-        bool capped = true;
-        FfnShape t[3];
-        for (int i = 0; i < n; ++i) {
-            t[i] = s[i];
-            t[i].bn = s[i].N <= 128 ? 128 : 256;
-            t[i].nkb = (int)((s[i].K + kFK - 1) / kFK);
-            int sp = (t[i].nkb + L - 1) / L;
-            if (sp > 64) sp = 64;
-            t[i].kps = (t[i].nkb + sp - 1) / sp;
-            t[i].splits = (t[i].nkb + t[i].kps - 1) / t[i].kps;
-            const double tiles = (double)((s[i].M + 255) / 256) * ((s[i].N + t[i].bn - 1) / t[i].bn);
-            const double step = t[i].bn == 256 ? 1.0 : 0.75;
-            total += tiles * t[i].nkb * step + tiles * t[i].splits * 2;   // 2: a unit's own part
-            if (t[i].kps * step + 2 > longest) longest = t[i].kps * step + 2;
-            if (t[i].splits > 1) {
-                bytes += (double)t[i].splits * s[i].M * s[i].N * 8;
-                capped = false;
+// The products of one launch: s in the order in which the caller named them, order[] in that of
+// the launch (the longest tiles first).
+struct FfnPlan {
+    FfnShape s[3];
+    int n, order[3];
+    int on_line, slots;
+    FfnLine line;
+};
+
+// Cuts the line into `shares`: evenly, or (`each` > 0) every tile into that many parts.  No part
+// is shorter than kFLeast steps: a cut nearer to a tile's end moves there, one nearer to the cut
+// before it (or on it) is left out.
+constexpr int kFLeast = 3;
+void ffn_cut(FfnPlan& p, int shares, int each) {
+    int n = 0;
+    double total = 0;
+    for (int i = 0; i < p.n; ++i) {
+        const FfnShape& s = p.s[p.order[i]];
+        total += (double)(s.tiles() - s.whole) * s.nkb * s.step();
+    }
+    int i = 0;
+    double before = 0;   // the line's length up to product i's first tile
+    for (int j = 0; j <= shares; ++j) {
+        int tile = p.on_line, step = 0;
+        if (j < shares && each > 0) {
+            tile = j / each;
+            while (tile >= p.s[p.order[i]].line0 + p.s[p.order[i]].tiles() - p.s[p.order[i]].whole) ++i;
+            step = (int)((long long)p.s[p.order[i]].nkb * (j - tile * each) / each);
+        } else if (j < shares) {
+            const double at = total * j / shares;
+            const FfnShape* s = &p.s[p.order[i]];
+            for (;;) {
+                const double len = (double)(s->tiles() - s->whole) * s->nkb * s->step();
+                if (at < before + len || i + 1 == p.n) break;
+                before += len;
+                s = &p.s[p.order[++i]];
+            }
+            const long long steps = (long long)((at - before) / s->step());
+            tile = s->line0 + (int)(steps / s->nkb);
+            step = (int)(steps % s->nkb);
+        }
+        if (tile >= p.on_line) {
+            tile = p.on_line;
+            step = 0;
+        } else {
+            const int nkb = p.s[p.order[i]].nkb;
+            if (step < kFLeast) step = 0;
+            if (step > 0 && nkb - step < kFLeast) {
+                step = 0;
+                ++tile;
             }
         }
-        double us = total / pairs + 0.5 * longest;
-        if (us < longest) us = longest;
-        us = us * 0.3 + bytes / 6.0e6 + (bytes > 0 ? 3.0 : 0.0);
-        if (us < best) {
-            best = us;
-            for (int i = 0; i < n; ++i) s[i] = t[i];
+        if (n && tile == p.line.tile[n - 1] && step - p.line.step[n - 1] < kFLeast) continue;
+        p.line.tile[n] = (unsigned short)tile;
+        p.line.step[n++] = step;
+    }
+    p.line.shares = n - 1;
+    p.line.tiles = p.on_line;
+    p.line.each = each > 0 && n - 1 == each * p.on_line ? each : 0;
+}
+
+// Time of a plan: the busiest pair's K steps (and 2 a unit) at 0.3 us, the parts' sums written
+// and read at 15 TB/s where they stay in L2 and at 6 elsewhere, and 3 us for the kernel that adds them.
+double ffn_plan_us(FfnPlan& p, int pairs) {
+    double most = 0, bytes = 0;
+    p.slots = 0;
+    for (int pair = 0; pair < pairs; ++pair) {
+        double steps = 0;
+        int unit0 = 0;
+        for (int i = 0; i < p.n; ++i) {   // units pair, pair + pairs, ... of the whole tiles
+            const FfnShape& s = p.s[p.order[i]];
+            const int first = ((pair - unit0) % pairs + pairs) % pairs;
+            if (s.whole > first)
+                steps += ((s.whole - first + pairs - 1) / pairs) * (s.nkb * s.step() + 2);
+            unit0 += s.whole;
         }
-        if (capped) break;   // longer units change nothing
+        for (int turn = pair; turn < p.line.shares; turn += pairs) {
+            const int j = p.line.each ? turn % p.line.tiles * p.line.each + turn / p.line.tiles : turn;
+            int tile = p.line.tile[j], step = p.line.step[j], i = 0;
+            const int end = p.line.tile[j + 1], last = p.line.step[j + 1];
+            for (; tile < end || (tile == end && step < last); ++tile, step = 0) {
+                while (i + 1 < p.n && tile >= p.s[p.order[i + 1]].line0) ++i;
+                const FfnShape& s = p.s[p.order[i]];
+                const int to = tile < end ? s.nkb : last;
+                steps += (to - step) * s.step() + 2;
+                if (step > 0 || to < s.nkb) {
+                    bytes += 8.0 * s.M * s.N / s.tiles();
+                    if (p.slots < tile + j + 1) p.slots = tile + j + 1;
+                }
+            }
+        }
+        most = steps > most ? steps : most;
+    }
+    return most * 0.3 + (bytes > 0 ? bytes / (bytes < 100e6 ? 15.0e6 : 6.0e6) + 3.0 : 0.0);
+}
+
+// Every pair takes the same number of whole tiles of each product, and the rest is cut evenly or
+// into equal parts of each tile; or all tiles are taken whole.  The least time of these.
+// (Backward with even shares, and with dW1's and dW2's tiles in equal parts and all of dx's whole:
+// 16384 x 512 x 1024 116 us, 120; 1000 x 2048 x 5632 157, 164; 2048 x 1024 x 2816 101, 107.)
+void ffn_plan(FfnPlan& best, int pairs) {
+    FfnPlan p = best;
+    for (int i = 0; i < p.n; ++i) {
+        FfnShape& s = p.s[i];
+        s.bn = s.N <= 128 ? 128 : 256;
+        s.nkb = (int)((s.K + kFK - 1) / kFK);
+        s.mt = (int)((s.M + 255) / 256);
+        s.nt = (int)((s.N + s.bn - 1) / s.bn);
+        p.order[i] = i;
+    }
+    for (int i = 0; i < p.n; ++i)
+        for (int j = i + 1; j < p.n; ++j)
+            if (p.s[p.order[j]].nkb > p.s[p.order[i]].nkb) {
+                const int k = p.order[i];
+                p.order[i] = p.order[j];
+                p.order[j] = k;
+            }
+    auto lay = [&](bool all) {
+        p.on_line = 0;
+        for (int i = 0; i < p.n; ++i) {
+            FfnShape& s = p.s[p.order[i]];
+            s.whole = all ? s.tiles() : s.tiles() / pairs * pairs;
+            s.line0 = p.on_line;
+            p.on_line += s.tiles() - s.whole;
+        }
+    };
+    double least = -1;
+    auto offer = [&]() {
+        const double us = ffn_plan_us(p, pairs);
+        if (least < 0 || us < least) {
+            least = us;
+            best = p;
+        }
+    };
+    lay(true);
+    ffn_cut(p, 0, 0);
+    offer();
+    lay(false);
+    if (p.on_line < 1 || p.on_line > kFCuts) return;
+    // (even shares read K steps all over the operands at a time: only where a product's operands
+    // stay in L2.  16384 x 1024 x 2816 backward, 218 MB: 474 us with whole tiles, 511 so)
+    double operands = 0;
+    for (int i = 0; i < p.n; ++i) {
+        const double b = 2.0 * (double)(p.s[i].M + p.s[i].N) * (double)p.s[i].K;
+        operands = b > operands ? b : operands;
+    }
+    if (pairs <= kFCuts && operands < 120e6) {
+        ffn_cut(p, pairs, 0);
+        offer();
+    }
+    for (int each = 2; each * p.on_line <= kFCuts && each <= 64; ++each) {
+        ffn_cut(p, each * p.on_line, each);
+        offer();
     }
 }
 
-size_t ffn_part_bytes(const FfnShape* s, int n) {
-    size_t b = 0;
-    for (int i = 0; i < n; ++i)
-        if (s[i].splits > 1) b += ffn_round((size_t)s[i].splits * s[i].M * s[i].N * 4);
-    return b;
-}
+// The parts' slots.
+size_t ffn_part_bytes(const FfnPlan& p) { return (size_t)p.slots * kFSlot * sizeof(float); }
 
 // Units of the gradient pass: 256 hidden columns, whose da runs at the rate of 256-column
 // products (of 128 columns a K step takes 0.75 of that time, not half), and 128 columns for odd
@@ -1078,26 +1266,17 @@ struct FfnOperands {
     void* out;
 };
 
-// The products of one launch (planned), and the launch that adds their splits.
-int ffn_gemms(const FfnShape* s, const FfnOperands* o, int n, uint8_t* part, cudaStream_t st) {
+// The products of one launch (planned), and the launch that adds the parts of cut tiles.
+int ffn_gemms(const FfnPlan& pl, const FfnOperands* o, uint8_t* part, cudaStream_t st) {
     FfnArgs a;
     memset(&a, 0, sizeof(a));
     FfnReduce r;
-    memset(&r, 0, sizeof(r));
-    // the products with the longest units first
-    int order[3] = {0, 1, 2};
-    for (int i = 0; i < n; ++i)
-        for (int j = i + 1; j < n; ++j)
-            if (s[order[j]].kps > s[order[i]].kps) {
-                const int k = order[i];
-                order[i] = order[j];
-                order[j] = k;
-            }
-    int units = 0, n_red = 0;
-    size_t most = 0;
-    for (int i = 0; i < n; ++i) {
-        const FfnShape& t = s[order[i]];
-        const FfnOperands& q = o[order[i]];
+    r.part = reinterpret_cast<const float*>(part);
+    r.n_prod = pl.n;
+    int units = 0;
+    for (int i = 0; i < pl.n; ++i) {
+        const FfnShape& t = pl.s[pl.order[i]];
+        const FfnOperands& q = o[pl.order[i]];
         FfnProd& p = a.p[i];
         p.a_mn = q.a_mn;
         p.b_mn = q.b_mn;
@@ -1105,94 +1284,96 @@ int ffn_gemms(const FfnShape* s, const FfnOperands* o, int n, uint8_t* part, cud
         p.N = (int)t.N;
         p.bn = t.bn;
         p.nkb = t.nkb;
-        p.kps = t.kps;
-        p.splits = t.splits;
-        p.mt = (int)((t.M + 255) / 256);
-        p.nt = (int)((t.N + t.bn - 1) / t.bn);
+        p.mt = t.mt;
+        p.nt = t.nt;
         p.unit0 = units;
-        units += p.mt * p.nt * p.splits;
-        void* out = q.out;
-        p.f32 = t.out_f32 || t.splits > 1;
-        if (t.splits > 1) {
-            auto& m = r.m[n_red++];
-            m.part = reinterpret_cast<const float*>(part);
-            m.out = q.out;
-            m.count4 = (size_t)t.M * t.N / 4;
-            m.splits = t.splits;
-            m.f32 = t.out_f32;
-            most = m.count4 > most ? m.count4 : most;
-            out = part;
-            part += ffn_round((size_t)t.splits * t.M * t.N * 4);
-        }
+        p.whole = t.whole;
+        p.line0 = t.line0;
+        p.f32 = t.out_f32;
+        units += t.whole;
+        r.p[i] = {q.out, p.M, p.N, p.bn, p.nt, p.whole, p.line0, p.f32};
         if (!ffn_operand(&p.mA, q.A, t.M, t.K, q.a_mn, kFM) ||
             !ffn_operand(&p.mB, q.B, t.N, t.K, q.b_mn, t.bn / 2) ||
-            !(p.f32 ? ffn_map_f32(&p.mOut, out, p.M, p.N, p.splits)
-                    : ffn_map_out(&p.mOut, out, p.M, p.N, p.N)))
+            !(p.f32 ? ffn_map_f32(&p.mOut, q.out, p.M, p.N, 1)
+                    : ffn_map_out(&p.mOut, q.out, p.M, p.N, p.N)))
             return HCW_ERR_CUDA;
     }
-    a.n_prod = n;
+    a.n_prod = pl.n;
     a.n_units = units;
+    a.line = pl.line;
+    if (pl.slots && !ffn_map_f32(&a.mPart, part, 256, 256, pl.slots)) return HCW_ERR_CUDA;
     a.timeout_ns = kFTimeoutNs;
-    const int sms = device_sms();
-    int rc = count_launch(ffn_launch<FFN_GEMM, 0>(a, units < sms / 2 ? units : sms / 2, st), 1);
-    if (rc || !n_red) return rc;
-    const size_t want = (most + 255) / 256, cap = (size_t)sms * 8;
-    return count_launch(launch_pdl(ffn_reduce_kernel, dim3((unsigned)(want < cap ? want : cap)),
-                                   dim3(256), 0, st, r), 1);
+    // the tiles that share j + 1 continues, with all their parts
+    int cut = 0;
+    for (int j = 1; j < pl.line.shares; ++j) {
+        if (!pl.line.step[j]) continue;
+        const int tile = pl.line.tile[j];
+        if (cut && r.t[cut - 1].tile == tile) {
+            r.t[cut - 1].parts = (unsigned short)(tile + j - r.t[cut - 1].slot + 1);
+        } else {
+            r.t[cut].tile = (unsigned short)tile;
+            r.t[cut].slot = (unsigned short)(tile + j - 1);
+            r.t[cut++].parts = 2;
+        }
+    }
+    const int pairs = device_sms() / 2, most = units > pl.line.shares ? units : pl.line.shares;
+    const int rc = count_launch(ffn_launch<FFN_GEMM, 0>(a, most < pairs ? most : pairs, st), 1);
+    if (rc || !cut) return rc;
+    return count_launch(launch_pdl(ffn_reduce_kernel, dim3((unsigned)cut * 64u), dim3(256), 0, st, r), 1);
 }
 
-// The plan of these products, kept by its sizes: the thread's last few (a plan costs a few us
-// of the host's time, and a training step or a served model repeats the same ones).
-void ffn_plan_kept(FfnShape* s, int n, int pairs) {
+// The plan of these products (their sizes in `want`), kept by its sizes: the thread's last few
+// (a plan costs some us of the host's time, and a training step or a served model repeats the
+// same ones).
+const FfnPlan& ffn_planned(const FfnShape* want, int n, int pairs) {
     struct Entry {
-        FfnShape s[3];
-        int n, pairs;
+        FfnPlan p;
+        int pairs;
     };
     constexpr int kEntries = 8;
     thread_local Entry kept[kEntries];
     thread_local int next = 0;
     for (const Entry& e : kept) {
-        bool same = e.n == n && e.pairs == pairs;
+        bool same = e.p.n == n && e.pairs == pairs;
         for (int i = 0; i < n && same; ++i)
-            same = e.s[i].M == s[i].M && e.s[i].N == s[i].N && e.s[i].K == s[i].K &&
-                   e.s[i].out_f32 == s[i].out_f32;
-        if (!same) continue;
-        for (int i = 0; i < n; ++i) s[i] = e.s[i];
-        return;
+            same = e.p.s[i].M == want[i].M && e.p.s[i].N == want[i].N && e.p.s[i].K == want[i].K &&
+                   e.p.s[i].out_f32 == want[i].out_f32;
+        if (same) return e.p;
     }
-    ffn_plan(s, n, pairs);
     Entry& e = kept[next];
     next = (next + 1) % kEntries;
-    e.n = n;
+    memset(&e.p, 0, sizeof(e.p));
     e.pairs = pairs;
-    for (int i = 0; i < n; ++i) e.s[i] = s[i];
+    e.p.n = n;
+    for (int i = 0; i < n; ++i) e.p.s[i] = want[i];
+    ffn_plan(e.p, pairs);
+    return e.p;
 }
 
-// Forward workspace: a [T][h] bf16, then the partial sums of y.
-FfnShape ffn_down_shape(int T, int d, int h) {
-    FfnShape s = {T, d, h, 0, 0, 0, 0, 0};
-    ffn_plan_kept(&s, 1, device_sms() / 2);
-    return s;
+// Forward workspace: a [T][h] bf16, then the parts of y.
+const FfnPlan& ffn_down_plan(int T, int d, int h) {
+    const FfnShape s = {T, d, h};
+    return ffn_planned(&s, 1, device_sms() / 2);
 }
 
 struct FfnBwdWs {
     size_t act, part, bytes;   // dgu at 0
-    FfnShape s[3];
-    int n;
+    const FfnPlan* plan;       // until the thread's next plan
 };
 
 FfnBwdWs ffn_bwd_ws(int T, int d, int h, bool dx, bool dw, bool f32) {
     FfnBwdWs w;
-    w.n = 0;
-    if (dx) w.s[w.n++] = {T, d, 2ll * h, 0, 0, 0, 0, 0};
+    FfnShape s[3] = {};
+    int n = 0;
+    if (dx) s[n++] = {T, d, 2ll * h};
     if (dw) {
-        w.s[w.n++] = {2ll * h, d, T, f32, 0, 0, 0, 0};
-        w.s[w.n++] = {d, h, T, f32, 0, 0, 0, 0};
+        s[n++] = {2ll * h, d, T, f32};
+        s[n++] = {d, h, T, f32};
     }
-    ffn_plan_kept(w.s, w.n, device_sms() / 2);
+    w.plan = &ffn_planned(s, n, device_sms() / 2);
     w.act = ffn_round((size_t)T * 2 * h * 2);
     w.part = w.act + ffn_round((size_t)T * h * 2);
-    w.bytes = w.part + ffn_part_bytes(w.s, w.n);
+    w.bytes = w.part + ffn_part_bytes(*w.plan);
     return w;
 }
 
@@ -1249,8 +1430,7 @@ extern "C" {
 size_t hcw_gated_ffn_fwd_workspace_bytes(int T, int d, int h) {
     if (T < 1 || ffn_sizes(T, d, h, HCW_GATE_SILU)) return 0;
     if (ffn_few(T, d, h)) return ffn_rows_ws(T, h);
-    const FfnShape s = ffn_down_shape(T, d, h);
-    return ffn_round((size_t)T * h * 2) + ffn_part_bytes(&s, 1);
+    return ffn_round((size_t)T * h * 2) + ffn_part_bytes(ffn_down_plan(T, d, h));
 }
 
 int hcw_gated_ffn_fwd(const void* x, const void* W1, const void* W2, int T, int d, int h, int act,
@@ -1270,8 +1450,8 @@ int hcw_gated_ffn_fwd(const void* x, const void* W1, const void* W2, int T, int 
         if (!workspace || ws_bytes < ffn_rows_ws(T, h)) return HCW_ERR_WORKSPACE;
         return ffn_rows_fwd(x, W1, W2, T, d, h, act, y, workspace, st);
     }
-    FfnShape s = ffn_down_shape(T, d, h);
-    if (!workspace || ws_bytes < act_bytes + ffn_part_bytes(&s, 1)) return HCW_ERR_WORKSPACE;
+    const FfnPlan& plan = ffn_down_plan(T, d, h);
+    if (!workspace || ws_bytes < act_bytes + ffn_part_bytes(plan)) return HCW_ERR_WORKSPACE;
     const int pairs = device_sms() / 2;
     FfnArgs a;
     memset(&a, 0, sizeof(a));
@@ -1292,7 +1472,7 @@ int hcw_gated_ffn_fwd(const void* x, const void* W1, const void* W2, int T, int 
     rc = count_launch(ffn_launch_act<FFN_GATE>(act, a, a.n_units < pairs ? a.n_units : pairs, st), 1);
     if (rc) return rc;
     const FfnOperands o = {workspace, false, W2, false, y};
-    return ffn_gemms(&s, &o, 1, static_cast<uint8_t*>(workspace) + act_bytes, st);
+    return ffn_gemms(plan, &o, static_cast<uint8_t*>(workspace) + act_bytes, st);
 }
 
 size_t hcw_gated_ffn_bwd_workspace_bytes(int T, int d, int h) {
@@ -1322,15 +1502,9 @@ int hcw_gated_ffn_bwd(const void* x, const void* dy, const void* W1, const void*
     const cudaStream_t st = (cudaStream_t)stream;
     if (T == 0) {
         if (!dW1) return HCW_OK;
-        FfnReduce r;   // no tokens: the weight gradients are zero
-        memset(&r, 0, sizeof(r));
-        r.m[0].out = dW1;
-        r.m[0].count4 = (size_t)2 * d * h / 4;
-        r.m[1].out = dW2;
-        r.m[1].count4 = (size_t)d * h / 4;
-        r.m[0].f32 = r.m[1].f32 = f32;
-        return count_launch(launch_pdl(ffn_reduce_kernel, dim3((unsigned)device_sms() * 4), dim3(256), 0,
-                                       st, r), 1);
+        return count_launch(launch_pdl(ffn_zero_kernel, dim3((unsigned)device_sms() * 4), dim3(256), 0,
+                                       st, static_cast<uint4*>(dW1), 2 * gb / 16,
+                                       static_cast<uint4*>(dW2), gb / 16), 1);
     }
     if (!x || !dy || !W1 || !W2 || (!dx && !dW1)) return HCW_ERR_INVALID_ARG;
     const FfnBwdWs w = ffn_bwd_ws(T, d, h, dx != nullptr, dW1 != nullptr, f32);
@@ -1370,7 +1544,7 @@ int hcw_gated_ffn_bwd(const void* x, const void* dy, const void* W1, const void*
         o[n++] = {ws, true, x, true, dW1};
         o[n++] = {dy, true, ws + w.act, true, dW2};
     }
-    return ffn_gemms(w.s, o, n, ws + w.part, st);
+    return ffn_gemms(*w.plan, o, ws + w.part, st);
 }
 
 }  // extern "C"
