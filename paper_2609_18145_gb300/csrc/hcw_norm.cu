@@ -487,10 +487,6 @@ __global__ void __launch_bounds__(kNormThreads) norm_fwd_kernel(const NormArgs a
     const uint8_t* const par = norm_smem + (size_t)a.bufs * 2 * a.piece;
     const uint32_t pw = C.own(par, C.l), gw = pw + C.OWN * nl, pb = gw + C.OWN * nl,
                    gb = pb + C.OWN * nl;
-    if (grp == n_grp - 1) {
-        C.fill(pw, a.pre_w, nullptr, 1.f);
-        if (LN) C.fill(pb, a.pre_b, nullptr, 0.f);
-    }
     int b = 0;
     uint32_t round = 0;
     bool ok = true;
@@ -498,10 +494,14 @@ __global__ void __launch_bounds__(kNormThreads) norm_fwd_kernel(const NormArgs a
         int g, r0, r1;
         item_rows(a, item, g, r0, r1);
         const float* gate = a.gate ? a.gate + (size_t)g * d : nullptr;
-        __syncthreads();   // the item before has been worked through
-        if (grp == n_grp - 1) {
-            C.fill(gw, a.post_w, gate, 1.f);
-            if (LN) C.fill(gb, a.post_b, gate, 0.f);
+        const bool fresh = item == (int)blockIdx.x;
+        if (!fresh) __syncthreads();   // the item before has been worked through
+        // a vector a row group: their loads wait side by side
+        for (int k = n_grp - 1 - grp; k < (fresh ? 4 : 2); k += n_grp) {
+            if (k == 0) C.fill(gw, a.post_w, gate, 1.f);
+            if (LN && k == 1) C.fill(gb, a.post_b, gate, 0.f);
+            if (k == 2) C.fill(pw, a.pre_w, nullptr, 1.f);
+            if (LN && k == 3) C.fill(pb, a.pre_b, nullptr, 0.f);
         }
         __syncthreads();
         for (int row0 = r0; row0 < r1 && ok; row0 += a.rows) {
@@ -689,7 +689,6 @@ __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const NormArgs a
     const int items = a.groups * a.slices;
     RowSum rs(&sh, nl, warp, lane);
     const Cols<T, VW, E> C(l, nl, d, sh.zero);
-    if (grp == n_grp - 1) C.fill(pw, a.pre_w, nullptr, 1.f);
     // sums over all of the CTA's rows: dx shat, dx
     uint64_t c_w[H];
     pairs_zero(c_w);
@@ -715,8 +714,12 @@ __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const NormArgs a
         int g, r0, r1;
         item_rows(a, item, g, r0, r1);
         const float* gate = a.gate ? a.gate + (size_t)g * d : nullptr;
-        __syncthreads();   // the item before has been worked through
-        if (grp == n_grp - 1) C.fill(gp, a.post_w, gate, 1.f);
+        const bool fresh = item == (int)blockIdx.x;
+        if (!fresh) __syncthreads();   // the item before has been worked through
+        for (int k = n_grp - 1 - grp; k < (fresh ? 2 : 1); k += n_grp) {
+            if (k == 0) C.fill(gp, a.post_w, gate, 1.f);
+            if (k == 1) C.fill(pw, a.pre_w, nullptr, 1.f);
+        }
         __syncthreads();
         // sums over the item's rows: ds fhat, ds
         uint64_t i_w[H];
@@ -980,7 +983,6 @@ __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const NormArgs a
         if (a.cpart || a.gpart) {
             // the CTA's sums of gate ds fhat and gate ds build up in its partial row; dgate's of
             // ds v = ds (fhat post_w + post_b) are the item's alone
-            const bool fresh = item == (int)blockIdx.x;
             float* const grow = a.gpart ? a.gpart + (size_t)item * d : nullptr;
             uint64_t b_[H];
             if (SM) own_sums(b_, i_b);
