@@ -664,7 +664,7 @@ int hcw_residual_norm_bwd(const void* dr_out, const void* dx_out, const void* s,
  *            probabilities add up).
  *   target   [T] int32 or NULL: the hard label; negative: the row has none.
  *   weight   [T] fp32 or NULL (ones), e.g. 1 / (rows that count).  A row of weight 0 gives
- *            loss and gradient 0 whatever its logits are, NaN included; they are not read.
+ *            loss and gradient 0 whatever its logits are, NaN included.
  *   loss     [T] fp32, dz [T][V] (dtype): outputs; one may be NULL.
  * Logits of -inf are symbols that cannot occur (gradient 0 unless the teacher or the label
  * names them, then the loss is +inf); a row of -inf alone gives 0 and 0.  NaN or +inf in a row

@@ -8,8 +8,8 @@
 //
 // (P = 1, or 0 for a row without slots).  Bound by memory: the logits are read once and
 // the gradient is written once, 4 bytes a symbol in bf16.  A row stays on chip between
-// its sums and its gradient: short rows (V <= 1024) in a warp's registers, long ones in
-// the shared memory of a cluster of up to 8 CTAs, each summing its slice against its own
+// its sums and its gradient: rows of a few thousand symbols in the registers of 1 to 8 warps,
+// longer ones in the shared memory of a cluster of up to 8 CTAs, each summing its slice against its own
 // maximum, the parts joined through distributed shared memory.  The dense part
 // of the gradient goes out first; then the symbols that the teacher or the label names
 // are written again with their share taken off, each by the one thread that owns the
@@ -33,9 +33,9 @@ constexpr int kDMaxK = 1024;          // slots of a row
 constexpr int kDMaxV = 262144;        // 8 CTAs x 128 KB of fp32 logits
 constexpr size_t kDSmem = 232448;     // shared memory of an SM
 constexpr long long kDSlice = 65536;  // bytes of a row a CTA takes by choice
-constexpr int kDWarpV = 1024;         // a warp a row up to here,
+constexpr int kDWarpV = 8192;         // rows in registers up to here (bf16: half as many),
 constexpr int kDWarpK = 64;           // and up to this many slots
-constexpr int kDWarps = 8;            // rows of a CTA of the warp kernel
+constexpr int kDWarps = 8;            // warps of a CTA of the kernel for rows in registers
 constexpr int kErrInvalid = 1;        // HCW_ERR_INVALID_ARG in the error word
 
 struct DistillArgs {
@@ -126,9 +126,8 @@ __device__ __forceinline__ void put(float* p, float v) { *p = v; }
 __device__ __forceinline__ void put(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
 
 // The row's slots, in the caller's shared arrays: p[k] (0 for an empty slot), the symbol
-// id[k] (-1), and after it p_own[k]: the slots' sum for the symbol where slot k is its first
-// one, else -1.  `threads` threads of index `t` take part, `sync` orders them.  An index at
-// or past V is reported and counts as empty.
+// id[k] (-1), own[k]: the slots' sum for the symbol where slot k is its first one, else -1, and
+// zk[k], the symbol's logit.  An index at or past V is reported and counts as empty.
 struct Slots {
     float *p, *own, *zk;
     int* id;
@@ -196,9 +195,9 @@ __device__ __forceinline__ float slot_owned(const Slots& s, int K, int k) {
     return t;
 }
 
-// One warp: fills own, above 32 slots through a table of the symbols (open addressing, `size` a power of two
-// of at least 2 K entries of symbol and first slot).  Which entry a symbol gets depends on
-// the order of the threads, what is found there does not.
+// One warp: fills own, above 32 slots through a table of the symbols (open addressing, `size` a
+// power of two of at least 2 K entries of symbol and first slot).  Which entry a symbol gets
+// depends on the order of the threads, what is found there does not.
 __device__ __forceinline__ void slots_own(const Slots& s, int K, int* table, int size, int lane) {
     if (K <= 32) {   // a slot a lane: the lanes with the same symbol
         const int id = lane < K ? s.id[lane] : -1;
@@ -255,18 +254,26 @@ __device__ __forceinline__ void slots_own(const Slots& s, int K, int* table, int
     __syncwarp();
 }
 
-// ------------------------------------------------------------------ a warp a row
-// NE symbols a lane, symbol lane + 32 e: coalesced whatever the row's alignment.  Everything
-// the row needs from its index alone is loaded at once; the named symbols' logits come
-// after the row, from L1.  Slots lane and lane + 32 stay in registers.
-template <typename T, int NE, int EXPS>
-__global__ void __launch_bounds__(32 * kDWarps) distill_warp_kernel(const DistillArgs a) {
+// ------------------------------------------------------------------ W warps a row
+// NE symbols a lane: symbol lane + 32 W e (lane: of the row's 32 W), in bf16 above 256 symbols two
+// neighbours at a time, from the even place at or before the row's start: coalesced whatever
+// the row's alignment.  Everything the row needs from its index alone is loaded at once; the named
+// symbols' logits come after the row, from L1.  Slots lane and lane + 32 stay in registers, in
+// each of the row's warps; the first one writes the loss and the named symbols.
+template <typename T, int NE, int EXPS, int W>
+__global__ void __launch_bounds__(32 * kDWarps, NE == 8 ? 6 : 4) distill_warp_kernel(const DistillArgs a) {
     __shared__ float sp[kDWarps][kDWarpK];
     __shared__ int si[kDWarps][kDWarpK];
+    __shared__ float red[3][kDWarps];   // the warps' maxima and sums
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int part = warp % W, first = lane + 32 * part;   // the row's warp and lane
+    // all of the row's warps are here
+    auto meet = [&]() {
+        if (W > 1) asm volatile("bar.sync %0, %1;" ::"r"(1 + warp / W), "n"(32 * W) : "memory");
+    };
     pdl_wait();
     pdl_trigger();
-    const long long row = (long long)blockIdx.x * kDWarps + warp;
+    const long long row = (long long)blockIdx.x * (kDWarps / W) + warp / W;
     if (row >= a.T) return;
     const T* z = static_cast<const T*>(a.z) + (size_t)row * a.V;
     T* dz = a.dz ? static_cast<T*>(a.dz) + (size_t)row * a.V : nullptr;
@@ -280,13 +287,35 @@ __global__ void __launch_bounds__(32 * kDWarps) distill_warp_kernel(const Distil
         id[q] = k < a.K ? a.idx[row * a.K + k] : -1;
         p[q] = k < a.K ? a.teacher[row * a.K + k] : 0.f;
     }
+    constexpr bool kPairs = sizeof(T) == 2 && NE > 8;
+    const int odd = kPairs ? (int)(row & a.V & 1) : 0;   // the row starts at an odd place
+    // the lane's pair e: its first symbol (-1: the second alone lies in the row)
+    auto pair_at = [&](int e) { return 2 * (first + 32 * W * e) - odd; };
     float v[NE];
+    if constexpr (kPairs) {
+        // whole pairs, and apart from them a first or a last symbol on its own
+        uint32_t q[NE / 2];
 #pragma unroll
-    for (int e = 0; e < NE; ++e) v[e] = lane + 32 * e < a.V ? logit(z + lane + 32 * e) : -INFINITY;
+        for (int e = 0; e < NE / 2; ++e) {
+            const int j = pair_at(e);
+            q[e] = j >= 0 && j + 1 < a.V ? *reinterpret_cast<const uint32_t*>(z + j) : 0xff80ff80u;
+        }
+        const float head = odd ? logit(z) : -INFINITY, tail = logit(z + a.V - 1);
+#pragma unroll
+        for (int e = 0; e < NE / 2; ++e) {
+            v[2 * e] = pair_at(e) == a.V - 1 ? tail : __uint_as_float(q[e] << 16);
+            v[2 * e + 1] = __uint_as_float(q[e] & 0xffff0000u);
+        }
+        if (first == 0 && odd) v[1] = head;
+    } else {
+#pragma unroll
+        for (int e = 0; e < NE; ++e)
+            v[e] = first + 32 * W * e < a.V ? logit(z + first + 32 * W * e) : -INFINITY;
+    }
     if (w == 0.f) {   // whatever the row holds
         if (dz)
-            for (int j = lane; j < a.V; j += 32) put(dz + j, 0.f);
-        if (lane == 0 && a.loss) a.loss[row] = 0.f;
+            for (int j = first; j < a.V; j += 32 * W) put(dz + j, 0.f);
+        if (first == 0 && a.loss) a.loss[row] = 0.f;
         return;
     }
     if (y >= a.V || id[0] >= a.V || id[1] >= a.V) atomicExch(&g_error_word, kErrInvalid);
@@ -305,6 +334,13 @@ __global__ void __launch_bounds__(32 * kDWarps) distill_warp_kernel(const Distil
     for (int o = 16; o > 0; o >>= 1) {
         mz = fmaxf(mz, __shfl_xor_sync(0xffffffffu, mz, o));
         mt = fmaxf(mt, __shfl_xor_sync(0xffffffffu, mt, o));
+    }
+    if (W > 1) {
+        if (lane == 0) red[0][warp] = mz;
+        meet();
+        mz = red[0][warp - part];
+#pragma unroll
+        for (int i = 1; i < W; ++i) mz = fmaxf(mz, red[0][warp - part + i]);
     }
     const float c = a.inv_tau * kLog2e;
     const float base = stat_base(mz), bt = stat_base(mt);
@@ -335,6 +371,20 @@ __global__ void __launch_bounds__(32 * kDWarps) distill_warp_kernel(const Distil
         stt += __shfl_xor_sync(0xffffffffu, stt, o);
         if (EXPS != kOne) s1 += __shfl_xor_sync(0xffffffffu, s1, o);
     }
+    if (W > 1) {
+        if (lane == 0) {
+            red[1][warp] = s;
+            red[2][warp] = s1;
+        }
+        meet();
+        s = red[1][warp - part];
+        s1 = red[2][warp - part];
+#pragma unroll
+        for (int i = 1; i < W; ++i) {
+            s += red[1][warp - part + i];
+            s1 += red[2][warp - part + i];
+        }
+    }
     if (EXPS == kOne) s1 = s;
     bool any = st != 0.f;   // NaN counts: it belongs in the result
     if (s == 0.f) {         // no logit above -inf: nothing to learn from
@@ -343,7 +393,7 @@ __global__ void __launch_bounds__(32 * kDWarps) distill_warp_kernel(const Distil
         s = s1 = 1.f;
     }
     const float inv_t = any ? 1.f / st : 0.f;
-    if (lane == 0 && a.loss) {
+    if (first == 0 && a.loss) {
         // sum p (log p - log q) with log p = t - bt - log st, log q = (z - base) / tau - log s
         const float kl = any ? stt * inv_t - logf(st) + logf(s) : 0.f;
         a.loss[row] = w * (a.kl * kl + (y >= 0 ? a.ce * (logf(s1) - (zy - base)) : 0.f));
@@ -355,9 +405,23 @@ __global__ void __launch_bounds__(32 * kDWarps) distill_warp_kernel(const Distil
         if (EXPS == kOne) return (fq + f1) * e;
         return fq * e + f1 * (EXPS == kSquare ? e * e : ex2((x - base) * kLog2e));
     };
+    if constexpr (kPairs) {
 #pragma unroll
-    for (int e = 0; e < NE; ++e)
-        if (lane + 32 * e < a.V) put(dz + lane + 32 * e, dense(v[e]));
+        for (int e = 0; e < NE / 2; ++e) {
+            const int j = pair_at(e);
+            const float x = dense(v[2 * e]);
+            if (j >= 0 && j + 1 < a.V)
+                *reinterpret_cast<uint32_t*>(dz + j) = pack_bf16x2(x, dense(v[2 * e + 1]));
+            if (j == a.V - 1) put(dz + j, x);
+        }
+        if (first == 0 && odd) put(dz, dense(v[1]));
+    } else {
+#pragma unroll
+        for (int e = 0; e < NE; ++e)
+            if (first + 32 * W * e < a.V) put(dz + first + 32 * W * e, dense(v[e]));
+    }
+    meet();   // the dense values are in place
+    if (part) return;
     bool named = false;
     if (any) {
         // a slot's share of its symbol: every slot its own, as a rule
@@ -951,10 +1015,22 @@ cudaError_t launch_distill_rows(const DistillArgs& a, DistillPlan pl, cudaStream
 
 template <typename T, int EXPS>
 cudaError_t launch_distill(const DistillArgs& a, cudaStream_t st) {
-    if (a.V <= kDWarpV && a.K <= kDWarpK) {
-        const dim3 grid((unsigned)((a.T + kDWarps - 1) / kDWarps)), block(32 * kDWarps);
-        if (a.V <= 256) return launch_pdl(distill_warp_kernel<T, 8, EXPS>, grid, block, 0, st, a);
-        return launch_pdl(distill_warp_kernel<T, 32, EXPS>, grid, block, 0, st, a);
+    // Rows in registers or in a cluster's shared memory (us, 16384 rows of bf16, 8192 of fp32; K = 32
+    // at one temperature, K = 64 at two): bf16 V = 2048: 46, 73 and 70, 191; 4096: 74, 78 and 111,
+    // 177; 8192: 125, 101 and 177, 178; fp32 4096: 46, 51; 8192: 83, 95.
+    if (a.V <= (sizeof(T) == 2 ? kDWarpV / 2 : kDWarpV) && a.K <= kDWarpK) {
+        const dim3 block(32 * kDWarps);
+        auto grid = [&](int w) { return dim3((unsigned)(((long long)a.T * w + kDWarps - 1) / kDWarps)); };
+        if (a.V <= 256)
+            return launch_pdl(distill_warp_kernel<T, 8, EXPS, 1>, grid(1), block, 0, st, a);
+        if (a.V <= 1024)
+            return launch_pdl(distill_warp_kernel<T, 32, EXPS, 1>, grid(1), block, 0, st, a);
+        if (a.V <= 2048)
+            return launch_pdl(distill_warp_kernel<T, 32, EXPS, 2>, grid(2), block, 0, st, a);
+        if (a.V <= 4096)
+            return launch_pdl(distill_warp_kernel<T, 32, EXPS, 4>, grid(4), block, 0, st, a);
+        if constexpr (sizeof(T) == 4)
+            return launch_pdl(distill_warp_kernel<T, 32, EXPS, 8>, grid(8), block, 0, st, a);
     }
     const int sms = device_sms();
     const long long bytes = (long long)a.V * (int)sizeof(T) + 32;

@@ -197,3 +197,43 @@ def test_another_stream_and_the_same_bits(H, V):
     args = (z.cuda(), a(idx), a(teacher), a(target), a(weight), 2.0, 0.7, 0.3)
     one, two = H.hcw_distill_loss(*args), H.hcw_distill_loss(*args)
     assert torch.equal(one[0], two[0]) and torch.equal(one[1], two[1])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("V", [256, 257, 1023, 1025, 2047, 2048, 2049, 4095, 4096, 4097, 8191, 8193])
+def test_rows_of_several_warps(H, V, dtype):
+    """Every number of warps a row, rows that start at odd places, named ends."""
+    z, idx, teacher, target, weight = make(11, V, 40, dtype, V)
+    idx[1, 0], idx[1, 1] = 0, V - 1          # the row's ends are named ...
+    target[1], target[2] = V - 1, 0          # ... and labels
+    idx[2, 5] = 0
+    idx[3, 1] = idx[3, 39] = idx[3, 0]       # a symbol three times, far apart
+    weight[4] = 0.0
+    z[4, :] = float("nan")
+    z[5, : V // 2] = -float("inf")
+    z[6, :] = -float("inf")
+    z[6, V - 1] = 1.0
+    target[5] = target[6] = V - 1
+    idx[5], idx[6] = -1, -1
+    for tau in (1.0, 2.0, 3.5):
+        check(H, z[:4], idx[:4], teacher[:4], target[:4], weight[:4], tau, 0.7, 0.3)
+        check(H, z[5:], idx[5:], teacher[5:], target[5:], weight[5:], tau, 0.7, 0.3)
+    a = lambda x: torch.from_numpy(x).cuda()  # noqa: E731
+    loss, dz = H.hcw_distill_loss(z.cuda(), a(idx), a(teacher), a(target), a(weight), 2.0, 0.7, 0.3)
+    torch.cuda.synchronize()
+    assert float(loss[4]) == 0.0 and bool((dz[4] == 0).all())
+    assert bool(torch.isfinite(dz[3]).all()) and bool(torch.isfinite(dz[5]).all())
+
+
+@pytest.mark.parametrize("tau", [1.0, 2.0])
+def test_empty_slots_in_long_rows(H, tau):
+    test_slots_and_rows_that_are_empty(H, 9001, 12, tau)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+def test_masked_symbols_in_long_rows(H, dtype):
+    test_masked_symbols(H, 9001, dtype)
+
+
+def test_symbols_past_a_long_vocabulary_are_reported(H):
+    test_symbols_past_the_vocabulary_are_reported(H, 9001)
