@@ -1015,9 +1015,9 @@ cudaError_t launch_distill_rows(const DistillArgs& a, DistillPlan pl, cudaStream
 
 template <typename T, int EXPS>
 cudaError_t launch_distill(const DistillArgs& a, cudaStream_t st) {
-    // Rows in registers or in a cluster's shared memory (us, 16384 rows of bf16, 8192 of fp32; K = 32
-    // at one temperature, K = 64 at two): bf16 V = 2048: 46, 73 and 70, 191; 4096: 74, 78 and 111,
-    // 177; 8192: 125, 101 and 177, 178; fp32 4096: 46, 51; 8192: 83, 95.
+    // Rows in registers, or in a cluster's shared memory (us, 16384 rows of bf16, 8192 of fp32; K = 32
+    // at one temperature and K = 64 at two): bf16 V = 2048: 33, 72 and 41, 129; 4096: 64, 78 and 77,
+    // 133; 8192: 125, 101; fp32 4096: 44, 51; 8192: 81, 95.
     if (a.V <= (sizeof(T) == 2 ? kDWarpV / 2 : kDWarpV) && a.K <= kDWarpK) {
         const dim3 block(32 * kDWarps);
         auto grid = [&](int w) { return dim3((unsigned)(((long long)a.T * w + kDWarps - 1) / kDWarps)); };
