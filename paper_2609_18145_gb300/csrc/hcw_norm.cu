@@ -449,7 +449,8 @@ struct RowSum {
 };
 
 // LN: some norm is a LayerNorm (means, centred values and biases).  R: rows a row group works
-// on at once.
+// on at once.  bf16, us and TB/s: 32768 x 4096 RMS 188, 5.7, LayerNorms 182, 5.9; 16384 x 512
+// LayerNorms 17, 4.0 (108 rows an SM: a start and an end of about 5 us).
 template <typename T, int VW, bool LN, int R>
 __global__ void __launch_bounds__(kNormThreads) norm_fwd_kernel(const NormArgs a) {
     extern __shared__ __align__(128) uint8_t norm_smem[];
@@ -646,6 +647,9 @@ __device__ __forceinline__ void group_sum(const C& cols, const uint64_t (&v)[H],
 // SM: with LayerNorms, the sums of dx and ds in shared memory (16 columns' sums have no room in
 // the registers; without SM they are there all the same, for rows whose ring leaves no room
 // either).
+// bf16, with the second launch, us and TB/s: 32768 x 4096 RMS 317, 5.1, LayerNorms 432, 3.7;
+// 65536 x 1024 RMS 143, 5.6; 16384 x 512 RMS 27, 3.7, LayerNorms 36, 2.8: the LayerNorms by the
+// issue of their instructions (0.47 a cycle with the 16 warps that the registers allow).
 template <typename T, int VW, bool LN, bool SM, int E, int R>
 __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const NormArgs a) {
     extern __shared__ __align__(128) uint8_t norm_smem[];
