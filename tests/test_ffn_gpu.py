@@ -198,3 +198,44 @@ def test_the_same_bits_over_many_runs(H, T, d, h):
         if first is None:
             first = got
         assert all(torch.equal(a, b) for a, b in zip(first, got))
+
+
+@pytest.mark.parametrize("T,d,h", [(20000, 64, 264), (9000, 64, 2056), (1000, 520, 1416), (333, 128, 2744)])
+def test_every_way_tiles_are_shared_out(H, T, d, h):
+    """Whole tiles and cut ones, units of 256 and 128 hidden columns, an odd end."""
+    check(H, T, d, h, S.SILU, h)
+    check(H, T, d, h, S.GELU, h + 1, dw=F32)
+
+
+@pytest.mark.parametrize("T,d,h", [(1, 512, 1024), (20, 128, 264), (333, 128, 2744), (4100, 256, 1024)])
+def test_nothing_is_read_from_the_workspace_before_it_is_written(H, T, d, h):
+    x, dy, W1, W2 = make(T, d, h, 11)
+    got = []
+    for fill in (0, 255):   # zeros, and NaN in every type
+        ws = [torch.full((max(n, 1),), fill, dtype=torch.uint8, device="cuda")
+              for n in (H.hcw_gated_ffn_fwd_workspace_bytes(T, d, h),
+                        H.hcw_gated_ffn_bwd_workspace_bytes(T, d, h))]
+        got.append((H.hcw_gated_ffn_fwd(x, W1, W2, workspace=ws[0]),
+                    *H.hcw_gated_ffn_bwd(x, dy, W1, W2, dw_dtype=BF16, workspace=ws[1])))
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+@pytest.mark.parametrize("act", [S.SILU, S.GELU, S.RELU])
+@pytest.mark.parametrize("T,d,h", [(1, 512, 1024), (3, 72, 200), (8, 1024, 2744)])
+def test_few_tokens_round_the_output_alone(H, T, d, h, act):
+    """Up to 8 tokens a is kept in two bf16 parts: off by 2^-16 of itself."""
+    x, _, W1, W2 = make(T, d, h, T + act)
+    x64, w1, w2 = np64(x), np64(W1), np64(W2)
+    g, u = x64 @ w1[:h].T, x64 @ w1[h:].T
+    eg, eu = (2 * (d + 8) * U * (np.abs(x64) @ np.abs(w).T) for w in (w1[:h], w1[h:]))
+    ag, _ = S.act(act, g)
+    eag = 1.13 * eg + 16 * U * np.abs(g)
+    a = ag * u
+    ea = eag * np.abs(u) + (np.abs(ag) + eag) * eu
+    ea = ea + 2.0 ** -16 * (np.abs(a) + ea)
+    y = a @ w2.T
+    ey = ea @ np.abs(w2).T + 2 * (2 * h + 8) * U * ((np.abs(a) + ea) @ np.abs(w2).T)
+    close(H.hcw_gated_ffn_fwd(x, W1, W2, act), y, ey, "y")
+    big = (W1.float() * 1e15).to(BF16)   # a = 1e30 and more: an infinite sum stays one
+    got = H.hcw_gated_ffn_fwd((x.float() * 1e8).to(BF16), big, W2, S.RELU)
+    assert not torch.isfinite(got).all()
