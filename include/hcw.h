@@ -565,9 +565,10 @@ int hcw_gemm_bf16_batched(int M, int N, int K, const void* A, long long a_stride
  *   workspace  hcw_gated_ffn_fwd_workspace_bytes(...) bytes, contents need not be
  *       initialised (HCW_ERR_WORKSPACE when NULL or smaller).
  * Products accumulate in fp32; g and u stay in fp32, a is rounded to bf16 once (it is the
- * second product's operand), y once.  T >= 0 (0 does nothing), d and h multiples of 8
- * (HCW_ERR_UNSUPPORTED otherwise, and above 2^20); pointers are 16-byte aligned; an output
- * or the workspace over an input is HCW_ERR_ALIASING.  The same inputs give the same bits.
+ * second product's operand; for few tokens it may be kept in two bf16 parts), y once.
+ * T >= 0 (0 does nothing), d and h multiples of 8 (HCW_ERR_UNSUPPORTED otherwise, and above
+ * 2^20); pointers are 16-byte aligned; an output or the workspace over an input is
+ * HCW_ERR_ALIASING.  The same inputs give the same bits.
  */
 #define HCW_GATE_SILU 0
 #define HCW_GATE_GELU 1

@@ -16,9 +16,11 @@
 //           of W1, the second the up rows, so one MMA of N = 256 gives both projections
 //           of the tile side by side, and the epilogue writes act(g) u, rounded once.
 //           Two accumulators: a tile's epilogue runs under the next tile's products.
-//   grad    the same tile, three accumulators: da (128 columns), then g and u.  da has a
-//           second buffer (512 TMEM columns in all), so that the next tile's da
-//           products run under this tile's epilogue, which writes dg, du and a.
+//   grad    256 rows x 256 hidden columns, two accumulators of 256 columns: g and u of the
+//           first 128, da of all, g and u of the second 128.  (Of 128 columns a K step of da
+//           takes 0.75 of the time of 256, not half: at 8192 x 2048 x 2816 this pass took 214 us
+//           so and takes 177.)  The epilogue draws g and u into registers at once, so that
+//           the next products run under it, and writes dg, du and a.
 //   gemm    y, or dx, dW1 and dW2 together: up to three products in one launch.  Each pair
 //           takes the same number of whole tiles; the tiles left over form a line of K
 //           steps that is cut into even shares.  A tile that was cut is added up from its
@@ -225,8 +227,9 @@ __global__ void __launch_bounds__(kFThreads, 1) ffn_pair_kernel(const __grid_con
                 v -= a.p[t.q].unit0;
             }
             t.kb1 = a.p[t.q].nkb;
+        } else if constexpr (MODE != FFN_GEMM) {
+            return false;
         } else {
-            if (MODE != FFN_GEMM) return false;
             for (;;) {
                 if (w.turn >= a.line.shares) return false;
                 if (!w.open) {

@@ -15,12 +15,13 @@
 // writes two.  Runs of consecutive rows are always on their way into a ring in shared memory
 // (bulk copies: consecutive rows are one piece, whatever their width and alignment), so the
 // reductions of one row never hold up the loads of the next.  A row belongs to `nl`
-// threads (16 columns each: up to 512 columns no two warps share a row), whose columns stay
-// the same from row to row: a thread's share of the parameter gradients stays in registers
-// over all rows of its CTA, the parameters in shared memory.  The sums of a row go through
+// threads (16 columns each, in the backward 8 up to 4096 columns: up to 512 and 256 columns no
+// two warps share a row), whose columns stay the same from row to row: a thread's share of the
+// parameter gradients stays in registers over all rows of its CTA, the parameters in shared
+// memory.  The sums of a row go through
 // shuffles that halve the number of values at each step and, between the warps of a row,
-// through shared memory behind a barrier of those warps.  The arithmetic is in packed pairs (two fp32
-// operations an instruction).  Parameter gradients: each CTA writes one row of partial
+// through shared memory behind a barrier of those warps.  The arithmetic is in packed pairs (two
+// fp32 operations an instruction).  Parameter gradients: each CTA writes one row of partial
 // sums, a second kernel adds the rows in a fixed order, so the same inputs give the same
 // bits.
 //
