@@ -1296,6 +1296,11 @@ int hcw_residual_norm_fwd(const void* r, const void* f, const float* gate, int r
     if (x_out && pre == HCW_NORM_NONE) return HCW_ERR_INVALID_ARG;
     if (T == 0) return HCW_OK;
     if ((!r && !f) || (!r_out && !x_out)) return HCW_ERR_INVALID_ARG;
+    // without a branch there is nothing that its gate and its norm's parameters apply to
+    if (!f) {
+        post = HCW_NORM_NONE;
+        gate = nullptr;
+    }
     const NormPlan p = norm_plan(false, post == HCW_NORM_LAYER || pre == HCW_NORM_LAYER, T, d,
                                  dtype == HCW_F32 ? 4 : 2, rows_per_gate);
     NormArgs a = {};
@@ -1315,7 +1320,7 @@ int hcw_residual_norm_fwd(const void* r, const void* f, const float* gate, int r
     a.rows_per_gate = rows_per_gate > 0 && rows_per_gate < T ? rows_per_gate : T;
     a.groups = p.groups;
     a.slices = p.slices;
-    a.post = f ? post : HCW_NORM_NONE;
+    a.post = post;
     a.pre = x_out ? pre : HCW_NORM_NONE;
     norm_geometry(a, p);
     return count_launch(launch_norm_any(false, dtype, p, a, (cudaStream_t)stream), 1);
