@@ -1152,7 +1152,7 @@ NormPlan norm_plan(bool bwd, bool ln, int T, int d, int elem, int rows_per_gate)
     p.slices = 1;
     if (p.groups > 0) {
         long long best = -1;
-        const int runs = (rows + n_grp - 1) / n_grp;
+        const int runs = rows > 0 ? (rows + n_grp - 1) / n_grp : 1;
         for (int per = 1; per <= 8; ++per) {
             long long k = (long long)most * per / p.groups;
             k = k < 1 ? 1 : k < runs ? k : runs;
