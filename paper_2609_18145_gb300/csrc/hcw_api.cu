@@ -2609,7 +2609,7 @@ unsigned long long hcw_launch_count(void) { return g_launches.load(); }
 int hcw_sync_status(void* stream) {
     if (cudaStreamSynchronize((cudaStream_t)stream) != cudaSuccess) return HCW_ERR_CUDA;
     int word = 0, word_res = 0, word_dec = 0, word_blk = 0, word_gemm = 0, word_small = 0,
-        word_dst = 0, word_ffn = 0;
+        word_dst = 0, word_ffn = 0, word_norm = 0;
     if (error_word_read_clear(&word) != cudaSuccess ||
         small_error_word_read_clear(&word_small) != cudaSuccess ||
         res_error_word_read_clear(&word_res) != cudaSuccess ||
@@ -2617,6 +2617,7 @@ int hcw_sync_status(void* stream) {
         block_error_word_read_clear(&word_blk) != cudaSuccess ||
         gemm_error_word_read_clear(&word_gemm) != cudaSuccess ||
         ffn_error_word_read_clear(&word_ffn) != cudaSuccess ||
+        norm_error_word_read_clear(&word_norm) != cudaSuccess ||
         distill_error_word_read_clear(&word_dst) != cudaSuccess)
         return HCW_ERR_CUDA;
     if (!word) word = word_res;
@@ -2625,6 +2626,7 @@ int hcw_sync_status(void* stream) {
     if (!word) word = word_gemm;
     if (!word) word = word_small;
     if (!word) word = word_ffn;
+    if (!word) word = word_norm;
     if (!word) word = word_dst;
     if (word == HCW_ERR_INVALID_ARG) return HCW_ERR_INVALID_ARG;
     if (word) return word == HCW_ERR_TIMEOUT ? HCW_ERR_TIMEOUT : HCW_ERR_CUDA;

@@ -376,6 +376,10 @@ inline int device_sms() {
 // Read its kernels' error word and reset it to 0 (synchronous).
 cudaError_t ffn_error_word_read_clear(int* word);
 
+// ---- Residual norms (hcw_norm.cu) ----
+// Read their kernels' error word and reset it to 0 (synchronous).
+cudaError_t norm_error_word_read_clear(int* word);
+
 // ---- Distillation loss (hcw_distill.cu) ----
 // Read its kernels' error word and reset it to 0 (synchronous).
 cudaError_t distill_error_word_read_clear(int* word);

@@ -1275,6 +1275,13 @@ NormWs norm_ws(const NormPlan& p, int d) {
 
 }  // namespace
 
+cudaError_t norm_error_word_read_clear(int* word) {
+    const int zero = 0;
+    cudaError_t e = cudaMemcpyFromSymbol(word, g_error_word, sizeof(int));
+    if (e == cudaSuccess && *word) e = cudaMemcpyToSymbol(g_error_word, &zero, sizeof(int));
+    return e;
+}
+
 }  // namespace hcw
 
 using namespace hcw;

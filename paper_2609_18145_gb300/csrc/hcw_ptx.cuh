@@ -14,7 +14,7 @@ namespace hcw {
 // bounded wait write a non-zero code here; hcw_sync_status reads and clears
 // the word of every translation unit that includes this header (hcw_tc.cu,
 // hcw_res.cu, hcw_small.cu, hcw_decode.cu, hcw_block.cu, hcw_gemm.cu, hcw_ffn.cu,
-// hcw_distill.cu), each through its own
+// hcw_norm.cu, hcw_distill.cu), each through its own
 // read-and-clear function.
 namespace {
 __device__ int g_error_word = 0;

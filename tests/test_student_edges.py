@@ -1,12 +1,17 @@
 """Calls of the student block's operators that need no GPU to go wrong: those without rows, the
 sizes of workspaces, what the status read covers."""
 import ctypes
+import glob
+import os
+import re
 import subprocess
 import sys
 
 import pytest
 
 P = ctypes.c_void_p
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))),
+                    "paper_2609_18145_gb300", "csrc")
 
 
 @pytest.fixture(scope="module")
@@ -32,3 +37,24 @@ assert H.hcw_launch_count() == before
 """ % (rows, kind, kind)
     r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True)
     assert r.returncode == 0, (r.returncode, r.stderr[-500:])
+
+
+def test_every_unit_that_can_give_up_is_read_by_the_status():
+    """The error word exists once a translation unit: the unit that waits has to hand out its own,
+    and hcw_sync_status has to read it."""
+    units = {}
+    for path in glob.glob(os.path.join(CSRC, "*.cu")):
+        text = re.sub(r"//[^\n]*|/\*.*?\*/", "", open(path).read(), flags=re.S)
+        units[os.path.basename(path)] = text
+    m = re.search(r"int hcw_sync_status\(.*?\n\}", units["hcw_api.cu"], flags=re.S)
+    seen = 0
+    for name, text in units.items():
+        if not re.search(r"\bmbar_wait|\bg_error_word\b|\bhcw_ptx\.cuh\b", text):
+            continue
+        seen += 1
+        own = re.search(r"cudaError_t (\w*error_word_read_clear)\(int\* word\) \{", text)
+        assert own, name
+        assert re.search(r"\b%s\(" % own.group(1), m.group(0)), (name, own.group(1))
+        # and the header that declares the word names the unit
+        assert name in open(os.path.join(CSRC, "hcw_ptx.cuh")).read().split("namespace {")[0], name
+    assert seen >= 9
