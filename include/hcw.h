@@ -696,6 +696,14 @@ int hcw_sync_status(void* stream);
  */
 int hcw_selftest_wait(long long timeout_ns, void* stream);
 
+/*
+ * Self-test of the same path in the residual norm's kernels: from now on every CTA's loads
+ * give up after `fetches` (> 0) of them, as if the wait for a free buffer had run out: the
+ * launch ends, its outputs are incomplete and hcw_sync_status reports HCW_ERR_TIMEOUT.
+ * 0 (the default): never.  For this process; returns the value before.
+ */
+int hcw_selftest_norm_starve(int fetches);
+
 #ifdef __cplusplus
 }
 #endif

@@ -74,6 +74,7 @@ struct NormArgs {
     int rows;             // rows of a buffer
     int bufs;
     int piece;            // bytes of a tensor in a buffer
+    uint32_t starve;      // self-test: thread 0 gives up after so many fetches (0: never)
 };
 
 struct __align__(16) NormShared {
@@ -101,10 +102,11 @@ struct NormFeed {
     int b;                 // buffer they go to
     uint32_t round;        // how often the ring has been gone through
     size_t at;             // where they start in a tensor, in elements
+    uint32_t fetches;
     __device__ __forceinline__ void start(const NormArgs& a) {
         item = blockIdx.x;
         b = 0;
-        round = 0;
+        round = fetches = 0;
         row = r1 = 0;
         if (item < a.groups * a.slices) {
             int g;
@@ -122,12 +124,18 @@ struct NormFeed {
             if (item < items) item_rows(a, item, g, row, r1);
         }
     }
-    // Fetches the next rows into the next buffer, which must be free (false: gave up).
+    // Fetches the next rows into the next buffer, which must be free.  Where it gives up the
+    // buffer stays empty, and who waits for it sees `abort`.
     template <typename T, int NIN>
-    __device__ __forceinline__ bool fetch(const NormArgs& a, uint8_t* ring, NormShared* sh) {
-        if (item >= a.groups * a.slices) return true;
+    __device__ __forceinline__ void fetch(const NormArgs& a, uint8_t* ring, NormShared* sh) {
+        if (item >= a.groups * a.slices) return;
+        if (a.starve && fetches++ >= a.starve) {   // as if the wait below had run out
+            atomicExch(&g_error_word, kErrTimeout);
+            *(volatile int*)&sh->abort = 1;
+            return;
+        }
         if (round && !mbar_wait(&sh->empty[b], (round & 1) ^ 1, &sh->abort, kNormTimeoutNs))
-            return false;
+            return;
         const int n = r1 - row < a.rows ? r1 - row : a.rows;
         // the 16-byte pieces the rows touch, those wholly inside the tensor in one copy and
         // the last few bytes of the tensor element by element
@@ -169,7 +177,6 @@ struct NormFeed {
             b = 0;
             ++round;
         }
-        return true;
     }
     // Every copy has landed before the CTA leaves, also after giving up.
     __device__ __forceinline__ void drain(const NormArgs& a, NormShared* sh) const {
@@ -178,6 +185,13 @@ struct NormFeed {
                 mbar_wait_drain(&sh->full[i], (i < b ? round : round - 1) & 1, kNormTimeoutNs);
     }
 };
+
+// A warp's wait for the rows of buffer b.  false: the warp has given up.  It then takes its part in every later step all the same, without waiting,
+// storing or handing buffers back: the other warps of its rows, which may find buffers that
+// are full already, meet it at the barrier of each sum, and an item's end is every warp's.
+__device__ __forceinline__ bool norm_rows_landed(NormShared& sh, int b, uint32_t round) {
+    return __all_sync(0xffffffffu, mbar_wait(&sh.full[b], round & 1, &sh.abort, kNormTimeoutNs));
+}
 
 // Shared memory by its 32-bit address.
 __device__ __forceinline__ uint4 lds128(uint32_t at) {
@@ -472,10 +486,9 @@ __global__ void __launch_bounds__(kNormThreads) norm_fwd_kernel(const NormArgs a
     pdl_wait();
     pdl_trigger();
     NormFeed feed;
-    bool fed = true;
     if (threadIdx.x == 0) {
         feed.start(a);
-        for (int i = 0; i < a.bufs; ++i) fed = fed && feed.fetch<T, 2>(a, norm_smem, &sh);
+        for (int i = 0; i < a.bufs; ++i) feed.fetch<T, 2>(a, norm_smem, &sh);
     }
     const int grp = (int)threadIdx.x / nl, n_grp = nt / nl;
     const float inv_d = 1.f / (float)d;
@@ -506,13 +519,11 @@ __global__ void __launch_bounds__(kNormThreads) norm_fwd_kernel(const NormArgs a
             if (LN && k == 3) C.fill(pb, a.pre_b, nullptr, 0.f);
         }
         __syncthreads();
-        for (int row0 = r0; row0 < r1 && ok; row0 += a.rows) {
-            const bool okw = mbar_wait(&sh.full[b], round & 1, &sh.abort, kNormTimeoutNs);
-            ok = __all_sync(0xffffffffu, okw && fed);
-            if (!ok) break;
+        for (int row0 = r0; row0 < r1; row0 += a.rows) {
+            ok = ok && norm_rows_landed(sh, b, round);
             // a group's rows past the buffer's n hold what was there before: they are worked
             // on and not stored
-            const int n = r1 - row0 < a.rows ? r1 - row0 : a.rows;
+            const int n = !ok ? 0 : r1 - row0 < a.rows ? r1 - row0 : a.rows;
             const uint32_t buf = smem_u32(norm_smem) + b * 2 * a.piece +
                                  ((uint32_t)row0 * (uint32_t)d * (uint32_t)sizeof(T) & 15) + first;
             uint64_t v[R][H];
@@ -583,7 +594,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_fwd_kernel(const NormArgs a
                 }
             }
             __syncwarp();
-            if (lane == 0) mbar_arrive(&sh.empty[b]);   // the buffer has been read
+            if (ok && lane == 0) mbar_arrive(&sh.empty[b]);   // the buffer has been read
             if (a.o0)
 #pragma unroll
                 for (int r = 0; r < R; ++r)
@@ -608,7 +619,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_fwd_kernel(const NormArgs a
                     }
                 }
             }
-            if (threadIdx.x == 0) fed = feed.fetch<T, 2>(a, norm_smem, &sh);
+            if (ok && threadIdx.x == 0) feed.fetch<T, 2>(a, norm_smem, &sh);
             __syncwarp();
             if (++b == a.bufs) {
                 b = 0;
@@ -682,10 +693,9 @@ __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const NormArgs a
     pdl_wait();
     pdl_trigger();
     NormFeed feed;
-    bool fed = true;
     if (threadIdx.x == 0) {
         feed.start(a);
-        for (int i = 0; i < a.bufs; ++i) fed = fed && feed.fetch<T, 4>(a, norm_smem, &sh);
+        for (int i = 0; i < a.bufs; ++i) feed.fetch<T, 4>(a, norm_smem, &sh);
     }
     const int l = (int)threadIdx.x % nl, grp = (int)threadIdx.x / nl, n_grp = nt / nl;
     const float inv_d = 1.f / (float)d;
@@ -733,11 +743,9 @@ __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const NormArgs a
 #pragma unroll
             for (int k = 0; k < H / Q; ++k) C.put8(i_b, k, none);
         if constexpr (LN && !SM) pairs_zero(i_r);
-        for (int row0 = r0; row0 < r1 && ok; row0 += a.rows) {
-            const bool okw = mbar_wait(&sh.full[b], round & 1, &sh.abort, kNormTimeoutNs);
-            ok = __all_sync(0xffffffffu, okw && fed);
-            if (!ok) break;
-            const int n = r1 - row0 < a.rows ? r1 - row0 : a.rows;
+        for (int row0 = r0; row0 < r1; row0 += a.rows) {
+            ok = ok && norm_rows_landed(sh, b, round);
+            const int n = !ok ? 0 : r1 - row0 < a.rows ? r1 - row0 : a.rows;
             const uint32_t buf = smem_u32(norm_smem) + b * 4 * a.piece +
                                  ((uint32_t)row0 * (uint32_t)d * (uint32_t)sizeof(T) & 15) + first;
             // 8 columns at a time, in passes over the rows: the sums over the rows take the
@@ -908,7 +916,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const NormArgs a
             }
             auto read = [&]() {   // the buffer has been read
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&sh.empty[b]);
+                if (ok && lane == 0) mbar_arrive(&sh.empty[b]);
             };
             if (KF) read();
 #pragma unroll
@@ -978,7 +986,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const NormArgs a
                         if (grp + n_grp * r < n) C.store8(a.o0, row0 + grp + n_grp * r, k, v);
                     }
             }
-            if (threadIdx.x == 0) fed = feed.fetch<T, 4>(a, norm_smem, &sh);
+            if (ok && threadIdx.x == 0) feed.fetch<T, 4>(a, norm_smem, &sh);
             __syncwarp();
             if (++b == a.bufs) {
                 b = 0;
@@ -1252,7 +1260,10 @@ int norm_check(int T, int d, int dtype, int post, int pre, int rows_per_gate, fl
     return HCW_OK;
 }
 
+std::atomic<int> g_starve{0};
+
 void norm_geometry(NormArgs& a, const NormPlan& p) {
+    a.starve = (uint32_t)g_starve.load(std::memory_order_relaxed);
     a.ln = p.ln;
     a.nl = p.nl;
     a.rows = p.rows;
@@ -1332,6 +1343,8 @@ int hcw_residual_norm_fwd(const void* r, const void* f, const float* gate, int r
     norm_geometry(a, p);
     return count_launch(launch_norm_any(false, dtype, p, a, (cudaStream_t)stream), 1);
 }
+
+int hcw_selftest_norm_starve(int fetches) { return g_starve.exchange(fetches > 0 ? fetches : 0); }
 
 size_t hcw_residual_norm_bwd_workspace_bytes(int T, int d, int rows_per_gate) {
     if (T < 1 || d < 1 || d > kNormMaxD || rows_per_gate < 0) return 0;

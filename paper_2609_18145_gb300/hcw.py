@@ -121,6 +121,7 @@ _SIGNATURES = {
     "hcw_stack_kernels_used": ([_I, _I, _I, _I], _I),
     "hcw_sync_status": ([_P], _I),
     "hcw_selftest_wait": ([_LL, _P], _I),
+    "hcw_selftest_norm_starve": ([_I], _I),
 }
 
 EXPORTED = tuple(_SIGNATURES)
@@ -870,3 +871,7 @@ def hcw_sync_status(stream=None) -> int:
 
 def hcw_selftest_wait(timeout_ns: int, stream=None):
     _check(lib().hcw_selftest_wait(int(timeout_ns), _stream(stream)), "hcw_selftest_wait")
+
+
+def hcw_selftest_norm_starve(fetches: int) -> int:
+    return int(lib().hcw_selftest_norm_starve(int(fetches)))

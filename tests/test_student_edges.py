@@ -9,6 +9,8 @@ import sys
 
 import pytest
 
+from test_dependent_kernels import kernels
+
 P = ctypes.c_void_p
 CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))),
                     "paper_2609_18145_gb300", "csrc")
@@ -58,3 +60,19 @@ def test_every_unit_that_can_give_up_is_read_by_the_status():
         # and the header that declares the word names the unit
         assert name in open(os.path.join(CSRC, "hcw_ptx.cuh")).read().split("namespace {")[0], name
     assert seen >= 9
+
+
+@pytest.mark.parametrize("name", ["norm_fwd_kernel", "norm_bwd_kernel"])
+def test_no_warp_of_a_norm_leaves_its_rows_early(name):
+    """The sums of a row meet at a barrier of the row's warps: a warp that gave up and left the
+    loop over the rows would leave the others there for good."""
+    body = dict(kernels(open(os.path.join(CSRC, "hcw_norm.cu")).read()))[name]
+    heads = list(re.finditer(r"for \(int row0\b[^;]*;([^;]*);[^{]*\{", body))
+    assert len(heads) == 1
+    assert heads[0].group(1).strip() == "row0 < r1"
+    depth, i = 1, heads[0].end()
+    while depth:
+        depth += {"{": 1, "}": -1}.get(body[i], 0)
+        i += 1
+    assert not re.search(r"\b(break|return|continue|goto)\b", body[heads[0].end():i].replace(
+        "return pack_bf16x2", ""))

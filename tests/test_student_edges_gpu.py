@@ -3,6 +3,7 @@ are not finite, extreme sizes, other streams than the current one."""
 import pytest
 import torch
 
+from oracle import student as S
 from test_norm_gpu import Problem, check_fwd
 
 pytestmark = pytest.mark.gpu
@@ -23,3 +24,29 @@ def test_without_a_branch_its_gate_and_norm_are_not_read(H, post, pre):
     check_fwd(H, p, post, pre, f=False)
     p.gate[0, 5], p.post_w[7], p.post_b[9] = float("nan"), float("inf"), float("nan")
     check_fwd(H, p, post, pre, f=False)
+
+
+@pytest.mark.parametrize("T,d,rows", [(200000, 64, 0), (40000, 512, 256), (8000, 2048, 0),
+                                      (4000, 8192, 100)])
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("kind", [S.RMS, S.LAYER])
+def test_a_norm_that_gives_up_ends_and_says_so(H, T, d, rows, dtype, kind):
+    p = Problem(T, d, dtype, d, rows=rows)
+    par = dict(gate=p.gate, rows_per_gate=rows, alpha=p.alpha, post=kind, post_w=p.post_w,
+               post_b=p.post_b, pre=kind, pre_w=p.pre_w)
+    calls = (lambda: H.hcw_residual_norm_fwd(p.r, p.f, pre_b=p.pre_b, **par),
+             lambda: tuple(H.hcw_residual_norm_bwd(p.dr_out, p.dx_out, p.s, p.f,
+                                                   want_bias=kind == S.LAYER, **par).values()))
+    for call in calls:
+        whole = call()
+        assert H.hcw_sync_status() == H.HCW_OK
+        for fetches in (1, 3, 5):
+            H.hcw_selftest_norm_starve(fetches)
+            try:
+                call()
+            finally:
+                assert H.hcw_selftest_norm_starve(0) == fetches
+            assert H.hcw_sync_status() == H.HCW_ERR_TIMEOUT
+        again = call()
+        assert H.hcw_sync_status() == H.HCW_OK
+        assert all(torch.equal(a, b) for a, b in zip(whole, again))
