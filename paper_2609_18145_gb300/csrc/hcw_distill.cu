@@ -199,6 +199,7 @@ __device__ __forceinline__ float slot_owned(const Slots& s, int K, int k) {
 // power of two of at least 2 K entries of symbol and first slot).  Which entry a symbol gets
 // depends on the order of the threads, what is found there does not.
 __device__ __forceinline__ void slots_own(const Slots& s, int K, int* table, int size, int lane) {
+    __syncwarp();    // the lanes' p and id are there for the others
     if (K <= 32) {   // a slot a lane: the lanes with the same symbol
         const int id = lane < K ? s.id[lane] : -1;
         const uint32_t same = __match_any_sync(0xffffffffu, id);
@@ -270,9 +271,12 @@ __global__ void __launch_bounds__(32 * kDWarps, NE == 8 ? 6 : 4) distill_warp_ke
     __shared__ float red[3][kDWarps];   // the warps' maxima and sums
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int part = warp % W, first = lane + 32 * part;   // the row's warp and lane
-    // all of the row's warps are here
+    // all of the row's threads are here, and what they wrote before is there for the others
     auto meet = [&]() {
-        if (W > 1) asm volatile("bar.sync %0, %1;" ::"r"(1 + warp / W), "n"(32 * W) : "memory");
+        if (W > 1)
+            asm volatile("bar.sync %0, %1;" ::"r"(1 + warp / W), "n"(32 * W) : "memory");
+        else
+            __syncwarp();
     };
     pdl_wait();
     pdl_trigger();
@@ -451,7 +455,6 @@ __global__ void __launch_bounds__(32 * kDWarps, NE == 8 ? 6 : 4) distill_warp_ke
 #pragma unroll
             for (int q = 0; q < 2; ++q) own[q] = slot_owned(sl, kDWarpK, lane + 32 * q);
         }
-        __syncwarp();   // the dense values are in place
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
             if (own[q] < 0.f) continue;
@@ -873,7 +876,10 @@ __global__ void __launch_bounds__(NT + 32 + 32 * slot_warps(NT), NT == 512 ? 1 :
                 }
             }
             st = stat_warp<EXPS>(st, c);
-            if (!gb && lane == 0) mbar_arrive(&bars->empty[b]);   // read once
+            if (!gb) {   // read once
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bars->empty[b]);
+            }
             uint64_t* const bar = &bars->stat[n % kDStats];
             float4* const at = stats + (n % kDStats) * parts + rank * NW + warp;
             if (tid == 0) mbar_arrive_expect_tx(bar, (uint32_t)(parts * sizeof(float4)));

@@ -76,3 +76,24 @@ def test_no_warp_of_a_norm_leaves_its_rows_early(name):
         i += 1
     assert not re.search(r"\b(break|return|continue|goto)\b", body[heads[0].end():i].replace(
         "return pack_bf16x2", ""))
+
+
+def test_lanes_that_read_or_overwrite_each_others_values_are_ordered():
+    """Votes and shuffles are no memory barriers: before a lane writes a named symbol over
+    another lane's dense value, or reads another lane's slot, there is a barrier on every way
+    there."""
+    text = re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, "hcw_distill.cu")).read())
+    kernel = dict(kernels(text))["distill_warp_kernel"]
+    meet = re.search(r"auto meet = \[&\]\(\) \{(.*?)\};", kernel, flags=re.S).group(1)
+    assert re.search(r"if \(W > 1\)\s+asm volatile\(\"bar.sync[^;]*;[^;]*;\s+else\s+__syncwarp\(\);",
+                     meet)
+    # the dense values, a meeting of all, the named symbols
+    assert re.search(r"dense\(v\[e\]\)\);\s*\}\s*meet\(\);\s*if \(part\) return;", kernel)
+    own = re.search(r"void slots_own\([^{]*\{(.*?)\n\}", text, flags=re.S).group(1)
+    assert own.lstrip().startswith("__syncwarp();")
+    # a buffer is handed back when every lane has read it
+    row = dict(kernels(text))["distill_row_kernel"]
+    gives = list(re.finditer(r"mbar_arrive\(&bars->empty\[", row))
+    assert len(gives) == 2
+    for m in gives:
+        assert re.search(r"__syncwarp\(\);\s*if \(lane == 0\)( \{\s*if \(gb\))? $", row[:m.start()])

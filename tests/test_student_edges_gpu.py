@@ -4,6 +4,7 @@ import pytest
 import torch
 
 from oracle import student as S
+from test_distill_gpu import check as distill_check, make as distill_problem
 from test_norm_gpu import Problem, check_fwd
 
 pytestmark = pytest.mark.gpu
@@ -50,3 +51,21 @@ def test_a_norm_that_gives_up_ends_and_says_so(H, T, d, rows, dtype, kind):
         again = call()
         assert H.hcw_sync_status() == H.HCW_OK
         assert all(torch.equal(a, b) for a, b in zip(whole, again))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("V", [1, 2, 31, 33, 201, 256, 257, 1000, 1024])
+def test_rows_with_a_label_and_no_teacher(H, V, dtype):
+    z, idx, teacher, target, weight = distill_problem(700, V, 3, dtype, V)
+    distill_check(H, z, None, None, target, weight, 1.0, 1.0, 0.4)
+    idx[:] = -1
+    distill_check(H, z, idx, teacher, target, weight, 2.0, 0.7, 0.3)
+
+
+@pytest.mark.parametrize("V,K", [(5000, 32), (5000, 7), (9001, 32)])
+def test_slots_that_name_the_same_symbols(H, V, K):
+    """Every symbol by two slots or more, in rows of a cluster."""
+    z, idx, teacher, target, weight = distill_problem(400, V, K, BF16, V + K)
+    idx[:, K // 2:] = idx[:, : K - K // 2]
+    idx[::3, 1:] = idx[::3, :1]
+    distill_check(H, z, idx, teacher, target, weight, 1.0, 0.7, 0.3)
