@@ -134,7 +134,8 @@ struct Slots {
 };
 
 // One warp: fills p and id from the row's slots; returns sum_k p_k log p_k, and in *any
-// whether there is a slot with any probability.
+// whether there is a slot with any probability.  The teacher's logits count by their distance
+// from the largest, taken before anything is rounded at their own size.
 __device__ __forceinline__ float slots_read(const DistillArgs& a, size_t row, const Slots& s,
                                             int lane, bool* any) {
     const int* idx = a.idx + row * a.K;
@@ -158,7 +159,7 @@ __device__ __forceinline__ float slots_read(const DistillArgs& a, size_t row, co
                 atomicExch(&g_error_word, kErrInvalid);
                 i[q] = -1;
             }
-            const float x = i[q] >= 0 ? t[q] * c : -INFINITY;
+            const float x = i[q] >= 0 ? t[q] : -INFINITY;
             s.id[k] = i[q];
             s.p[k] = x;
             m = fmaxf(m, x);
@@ -167,16 +168,17 @@ __device__ __forceinline__ float slots_read(const DistillArgs& a, size_t row, co
     m = warp_max(m);
     const float b = stat_base(m);
     float sum = 0.f;
-    for (int k = lane; k < a.K; k += 32) sum += s.id[k] >= 0 ? ex2((s.p[k] - b) * kLog2e) : 0.f;
+    for (int k = lane; k < a.K; k += 32)
+        sum += s.id[k] >= 0 ? ex2((s.p[k] - b) * (c * kLog2e)) : 0.f;
     sum = warp_sum(sum);
     *any = sum != 0.f;   // NaN counts: it belongs in the result
-    const float lse = *any ? b + logf(sum) : 0.f, inv = *any ? 1.f / sum : 0.f;
+    const float ls = *any ? logf(sum) : 0.f, inv = *any ? 1.f / sum : 0.f;
     float ent = 0.f;
     for (int k = lane; k < a.K; k += 32) {
-        const float t = s.p[k];
-        const float p = *any && s.id[k] >= 0 ? ex2((t - b) * kLog2e) * inv : 0.f;
+        const float t = s.p[k] - b;
+        const float p = *any && s.id[k] >= 0 ? ex2(t * (c * kLog2e)) * inv : 0.f;
         s.p[k] = p;
-        if (p != 0.f) ent += p * (t - lse);
+        if (p != 0.f) ent += p * (t * c - ls);
     }
     return warp_sum(ent);
 }
@@ -332,7 +334,7 @@ __global__ void __launch_bounds__(32 * kDWarps, NE == 8 ? 6 : 4) distill_warp_ke
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
         if (id[q] >= a.V) id[q] = -1;
-        p[q] = id[q] >= 0 ? p[q] * a.inv_tau : -INFINITY;
+        p[q] = id[q] >= 0 ? p[q] : -INFINITY;
         mt = fmaxf(mt, p[q]);
     }
 #pragma unroll
@@ -355,7 +357,7 @@ __global__ void __launch_bounds__(32 * kDWarps, NE == 8 ? 6 : 4) distill_warp_ke
     float zk[2];
 #pragma unroll
     for (int q = 0; q < 2; ++q) zk[q] = id[q] >= 0 ? logit(z + id[q]) : 0.f;
-    // sums: the row's exponentials, the teacher's, and its sum of exp(t) t
+    // sums: the row's exponentials, the teacher's, and its sum of exp(t / tau) (t - z)
     float s = 0.f, s1 = 0.f, st = 0.f, stt = 0.f;
 #pragma unroll
     for (int e = 0; e < NE; ++e) {
@@ -367,9 +369,9 @@ __global__ void __launch_bounds__(32 * kDWarps, NE == 8 ? 6 : 4) distill_warp_ke
     float et[2];
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-        et[q] = id[q] >= 0 ? ex2((p[q] - bt) * kLog2e) : 0.f;
+        et[q] = id[q] >= 0 ? ex2((p[q] - bt) * c) : 0.f;
         st += et[q];
-        if (et[q] != 0.f) stt += et[q] * (p[q] - bt - (zk[q] - base) * a.inv_tau);
+        if (et[q] != 0.f) stt += et[q] * ((p[q] - bt) - (zk[q] - base));
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
@@ -401,8 +403,9 @@ __global__ void __launch_bounds__(32 * kDWarps, NE == 8 ? 6 : 4) distill_warp_ke
     }
     const float inv_t = any ? 1.f / st : 0.f;
     if (first == 0 && a.loss) {
-        // sum p (log p - log q) with log p = t - bt - log st, log q = (z - base) / tau - log s
-        const float kl = any ? stt * inv_t - logf(st) + logf(s) : 0.f;
+        // sum p (log p - log q) with log p = (t - bt) / tau - log st and log q = (z - base) / tau
+        // - log s
+        const float kl = any ? stt * inv_t * a.inv_tau - logf(st) + logf(s) : 0.f;
         a.loss[row] = w * (a.kl * kl + (y >= 0 ? a.ce * (logf(s1) - (zy - base)) : 0.f));
     }
     if (!dz) return;

@@ -1,5 +1,6 @@
 """Calls of the student block's operators at their edges: parts that are not there, values that
 are not finite, extreme sizes, other streams than the current one."""
+import numpy as np
 import pytest
 import torch
 
@@ -69,3 +70,20 @@ def test_slots_that_name_the_same_symbols(H, V, K):
     idx[:, K // 2:] = idx[:, : K - K // 2]
     idx[::3, 1:] = idx[::3, :1]
     distill_check(H, z, idx, teacher, target, weight, 1.0, 0.7, 0.3)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("V,K", [(100, 12), (1000, 40), (3001, 12), (5000, 50), (3000, 200), (33001, 64)])
+@pytest.mark.parametrize("tau", [1.0, 2.0, 3.5])
+def test_the_teachers_logits_count_by_their_differences(H, V, K, tau, dtype):
+    """Logits in quarters, and the same ones 2^20 higher and lower: exact in fp32, and so are
+    their differences, from which everything follows.  The same bits."""
+    z, idx, teacher, target, weight = distill_problem(9, V, K, dtype, V)
+    teacher = np.round(teacher * 4) / 4
+    dev = lambda x: torch.from_numpy(x).cuda()  # noqa: E731
+    got = [H.hcw_distill_loss(z.cuda(), dev(idx), dev((teacher + c).astype(np.float32)), dev(target),
+                              dev(weight), tau, 0.7, 0.3) for c in (0.0, 2.0 ** 20, -2.0 ** 20)]
+    assert bool(torch.isfinite(got[0][0]).all())
+    for loss, dz in got[1:]:
+        assert torch.equal(loss, got[0][0]) and torch.equal(dz, got[0][1])
+    distill_check(H, z, idx, teacher.astype(np.float32), target, weight, tau, 0.7, 0.3)
