@@ -143,8 +143,9 @@ __device__ __forceinline__ float ffn_act(float g, float* d) {
         if (d) *d = c + g * 0.39894228040143268f * ffn_ex2(g * g * -0.72134752044448170f);
         return g * c;
     }
-    if (d) *d = g > 0.f ? 1.f : 0.f;
-    return g > 0.f ? g : 0.f;
+    // (NaN stays NaN, here and in the derivative)
+    if (d) *d = g > 0.f ? 1.f : g <= 0.f ? 0.f : g;
+    return g <= 0.f ? 0.f : g;
 }
 
 // Warp 0 loads, warp 1 issues the products (the pair's leader), eight warps drain TMEM.

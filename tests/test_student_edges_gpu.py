@@ -6,6 +6,7 @@ import torch
 
 from oracle import student as S
 from test_distill_gpu import check as distill_check, make as distill_problem
+from test_ffn_gpu import make as ffn_problem
 from test_norm_gpu import Problem, check_fwd
 
 pytestmark = pytest.mark.gpu
@@ -87,3 +88,27 @@ def test_the_teachers_logits_count_by_their_differences(H, V, K, tau, dtype):
     for loss, dz in got[1:]:
         assert torch.equal(loss, got[0][0]) and torch.equal(dz, got[0][1])
     distill_check(H, z, idx, teacher.astype(np.float32), target, weight, tau, 0.7, 0.3)
+
+
+@pytest.mark.parametrize("act", [S.SILU, S.GELU, S.RELU])
+@pytest.mark.parametrize("T", [4, 20, 200])
+def test_a_nan_in_a_gate_row_is_not_hidden(H, T, act):
+    """NaN in one gate: in every output that this hidden column enters, and in no other."""
+    d, h, at = 128, 136, 3
+    x, dy, W1, W2 = ffn_problem(T, d, h, T)
+    W1[at, 5] = float("nan")
+    assert H.hcw_gated_ffn_fwd(x, W1, W2, act).isnan().all()
+    dx, dW1, dW2 = H.hcw_gated_ffn_bwd(x, dy, W1, W2, act)
+    assert dx.isnan().all() and dW2[:, at].isnan().all()
+    assert dW1[at].isnan().all() and dW1[h + at].isnan().all()
+    keep = [i for i in range(h) if i != at]
+    assert dW2[:, keep].isfinite().all()
+    assert dW1[keep].isfinite().all() and dW1[[h + i for i in keep]].isfinite().all()
+    # a token's: in its own row alone
+    x, dy, W1, W2 = ffn_problem(T, d, h, T)
+    x[2, 5] = float("nan")
+    y = H.hcw_gated_ffn_fwd(x, W1, W2, act)
+    dx = H.hcw_gated_ffn_bwd(x, dy, W1, W2, act, want_dw=False)[0]
+    rows = [i for i in range(T) if i != 2]
+    for t in (y, dx):
+        assert t[2].isnan().all() and t[rows].isfinite().all()
