@@ -179,6 +179,33 @@ def _stream(stream):
     return _raw_stream(torch.cuda.current_device())
 
 
+# What a wrapper allocates belongs to the stream it launches on: a block is handed out again in
+# the order of the stream it was allocated under, so memory of the current stream could still
+# be in use there before the launch, or be given away while the launch on `stream` goes on.
+def _empty(stream, *size, **kw):
+    """torch.empty of an output; the caller may go on with it on the current stream."""
+    if stream is None:
+        return torch.empty(*size, **kw)
+    with torch.cuda.stream(stream):
+        t = torch.empty(*size, **kw)
+    t.record_stream(torch.cuda.current_stream())
+    return t
+
+
+def _empty_like(stream, t):
+    if stream is None:
+        return torch.empty_like(t)
+    return _empty(stream, t.shape, dtype=t.dtype, device=t.device)
+
+
+def _scratch(stream, nbytes, device):
+    """Bytes that the launch alone uses."""
+    if stream is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
 def _dtype_code(t: torch.Tensor) -> int:
     if t.dtype == torch.bfloat16:
         return HCW_BF16
@@ -210,7 +237,7 @@ def hcw_partner_table(layer: int, n: int, flags: int = 0, dim_override: int = -1
 
 def hcw_partner_table_device(layer: int, n: int, flags: int = 0, dim_override: int = -1,
                              device=None, stream=None) -> torch.Tensor:
-    out = torch.empty(n, dtype=torch.int32, device=device or "cuda")
+    out = _empty(stream, n, dtype=torch.int32, device=device or "cuda")
     _check(lib().hcw_partner_table_device(layer, dim_override, n, flags, _ptr(out),
                                           _stream(stream)), "hcw_partner_table_device")
     return out
@@ -222,9 +249,9 @@ def hcw_layer_fwd(x, W_self, W_nbr, bias=None, layer: int = 0, dim_override: int
     _dev(x, W_self, W_nbr, bias, y, z_save)
     B, n, d = x.shape
     if y is None:
-        y = torch.empty_like(x)
+        y = _empty_like(stream, x)
     if want_z and z_save is None:
-        z_save = torch.empty_like(x)
+        z_save = _empty_like(stream, x)
     _check(lib().hcw_layer_fwd(_ptr(x), _ptr(W_self), _ptr(W_nbr), _ptr(bias), layer,
                                dim_override, B, n, d, _dtype_code(x), flags, _ptr(y),
                                _ptr(z_save), _stream(stream)), "hcw_layer_fwd")
@@ -239,10 +266,10 @@ def hcw_stack_workspace_bytes(B: int, n: int, d: int, dtype: int, flags: int, L:
     return int(lib().hcw_stack_workspace_bytes(B, n, d, dtype, flags, L))
 
 
-def _workspace(nbytes, device, workspace):
+def _workspace(stream, nbytes, device, workspace):
     if workspace is not None:
         return workspace
-    return torch.empty(max(nbytes, 1), dtype=torch.uint8, device=device)
+    return _scratch(stream, max(nbytes, 1), device)
 
 
 def hcw_layer_bwd(x, z_save, dy, W_self, W_nbr, layer: int = 0, dim_override: int = -1,
@@ -253,13 +280,13 @@ def hcw_layer_bwd(x, z_save, dy, W_self, W_nbr, layer: int = 0, dim_override: in
     B, n, d = x.shape
     dt = _dtype_code(x)
     f32 = dict(dtype=torch.float32, device=x.device)
-    dx = torch.empty_like(x) if dx is None else dx
-    dW_self = torch.empty(d, d, **f32) if dW_self is None else dW_self
-    dW_nbr = torch.empty(d, d, **f32) if dW_nbr is None else dW_nbr
+    dx = _empty_like(stream, x) if dx is None else dx
+    dW_self = _empty(stream, d, d, **f32) if dW_self is None else dW_self
+    dW_nbr = _empty(stream, d, d, **f32) if dW_nbr is None else dW_nbr
     if dbias is None and want_dbias:
-        dbias = torch.empty(d, **f32)
+        dbias = _empty(stream, d, **f32)
     need = hcw_workspace_bytes(B, n, d, dt, flags)
-    ws = _workspace(need, x.device, workspace)
+    ws = _workspace(stream, need, x.device, workspace)
     _check(lib().hcw_layer_bwd(_ptr(x), _ptr(z_save), _ptr(dy), _ptr(W_self), _ptr(W_nbr),
                                layer, dim_override, B, n, d, dt, flags, _ptr(dx),
                                _ptr(dW_self), _ptr(dW_nbr), _ptr(dbias), _ptr(ws),
@@ -272,7 +299,7 @@ def hcw_layer_bwd_data(dz, dy, W_self, W_nbr, layer: int = 0, dim_override: int 
     """Input gradient of one layer from dz = dy * act'(z); returns dx."""
     _dev(dz, dy, W_self, W_nbr, dx)
     B, n, d = dz.shape
-    dx = torch.empty_like(dz) if dx is None else dx
+    dx = _empty_like(stream, dz) if dx is None else dx
     _check(lib().hcw_layer_bwd_data(_ptr(dz), _ptr(dy), _ptr(W_self), _ptr(W_nbr), layer,
                                     dim_override, B, n, d, _dtype_code(dz), flags, _ptr(dx),
                                     _stream(stream)), "hcw_layer_bwd_data")
@@ -291,11 +318,11 @@ def hcw_layer_bwd_weight(x, dz, layer: int = 0, dim_override: int = -1, flags: i
     B, n, d = x.shape
     dt = _dtype_code(x)
     f32 = dict(dtype=torch.float32, device=x.device)
-    dW_self = torch.empty(d, d, **f32) if dW_self is None else dW_self
-    dW_nbr = torch.empty(d, d, **f32) if dW_nbr is None else dW_nbr
+    dW_self = _empty(stream, d, d, **f32) if dW_self is None else dW_self
+    dW_nbr = _empty(stream, d, d, **f32) if dW_nbr is None else dW_nbr
     if dbias is None and want_dbias:
-        dbias = torch.empty(d, **f32)
-    ws = _workspace(hcw_layer_bwd_weight_workspace_bytes(B, n, d, dt, flags), x.device,
+        dbias = _empty(stream, d, **f32)
+    ws = _workspace(stream, hcw_layer_bwd_weight_workspace_bytes(B, n, d, dt, flags), x.device,
                     workspace)
     _check(lib().hcw_layer_bwd_weight(_ptr(x), _ptr(dz), layer, dim_override, B, n, d, dt, flags,
                                       _ptr(dW_self), _ptr(dW_nbr), _ptr(dbias), _ptr(ws),
@@ -316,7 +343,7 @@ def hcw_decode_step(x_t, W_self, W_nbr, bias, t: int, n: int, cache, flags: int,
     _dev(x_t, W_self, W_nbr, bias, cache, y)
     B, d = x_t.shape
     L = W_self.shape[0]
-    y = torch.empty_like(x_t) if y is None else y
+    y = _empty_like(stream, x_t) if y is None else y
     arr = None if dims is None else _dims_array(dims, L)
     _check(lib().hcw_decode_step(_ptr(x_t), _ptr(W_self), _ptr(W_nbr), _ptr(bias),
                                  None if arr is None else ctypes.cast(arr, _P), layer0, L, t, B,
@@ -351,10 +378,10 @@ def hcw_block_step(ids, params: dict, grads: dict | None = None, loss=None, work
     L, h = params["W1"].shape[0], params["W1"].shape[1]
     dev = ids.device
     if grads is None:
-        grads = {f: torch.empty(tuple(params[f].shape), dtype=torch.float32, device=dev)
+        grads = {f: _empty(stream, tuple(params[f].shape), dtype=torch.float32, device=dev)
                  for f in BLOCK_FIELDS}
-    loss = torch.empty(1, dtype=torch.float32, device=dev) if loss is None else loss
-    ws = _workspace(hcw_block_workspace_bytes(B, n, d, h, V, L), dev, workspace)
+    loss = _empty(stream, 1, dtype=torch.float32, device=dev) if loss is None else loss
+    ws = _workspace(stream, hcw_block_workspace_bytes(B, n, d, h, V, L), dev, workspace)
     P = _BlockPtrs(*[params[f].data_ptr() for f in BLOCK_FIELDS])
     G = _BlockPtrs(*[grads[f].data_ptr() for f in BLOCK_FIELDS])
     _check(lib().hcw_block_step(_ptr(ids), ctypes.byref(P), ctypes.byref(G), B, n, d, h, V, L,
@@ -379,9 +406,9 @@ def hcw_gemm_bf16(A, B, ta: bool = False, tb: bool = False, C=None, workspace=No
     Kb, N = (B.shape[1], B.shape[0]) if tb else (B.shape[0], B.shape[1])
     if Kb != K:
         raise ValueError("hcw_gemm_bf16: inner sizes differ (%d, %d)" % (K, Kb))
-    C = torch.empty(M, N, dtype=torch.float32, device=A.device) if C is None else C
+    C = _empty(stream, M, N, dtype=torch.float32, device=A.device) if C is None else C
     if split:
-        ws = _workspace(hcw_gemm_workspace_bytes(M, N, K), A.device, workspace)
+        ws = _workspace(stream, hcw_gemm_workspace_bytes(M, N, K), A.device, workspace)
         wp, wn = _ptr(ws), ws.numel()
     else:
         wp, wn = None, 0
@@ -407,7 +434,7 @@ def hcw_gemm_bf16_batched(A, B, C=None, stream=None):
     N = B.shape[2]
     if A.stride(2) != 1 or A.stride(1) != M or B.stride(2) != 1 or B.stride(1) != N:
         raise ValueError("hcw_gemm_bf16_batched: each product's rows must be contiguous")
-    C = torch.empty(batch, M, N, dtype=torch.float32, device=A.device) if C is None else C
+    C = _empty(stream, batch, M, N, dtype=torch.float32, device=A.device) if C is None else C
     _check(lib().hcw_gemm_bf16_batched(M, N, K, _ptr(A), A.stride(0), _ptr(B), B.stride(0),
                                        _ptr(C), batch, _stream(stream)), "hcw_gemm_bf16_batched")
     return C
@@ -468,10 +495,10 @@ def hcw_gated_ffn_fwd(x, W1, W2, act: int = HCW_GATE_SILU, y=None, workspace=Non
     _dev(x, W1, W2, y, workspace)
     _bf16("hcw_gated_ffn_fwd: tensors", x, W1, W2, y)
     T, d, h = _ffn_sizes("hcw_gated_ffn_fwd", x, W1, W2)
-    y = torch.empty_like(x) if y is None else y
+    y = _empty_like(stream, x) if y is None else y
     _like(x, "hcw_gated_ffn_fwd", y)
     if workspace is None:
-        workspace = _workspace(hcw_gated_ffn_fwd_workspace_bytes(T, d, h), x.device, None)
+        workspace = _workspace(stream, hcw_gated_ffn_fwd_workspace_bytes(T, d, h), x.device, None)
     _check(lib().hcw_gated_ffn_fwd(_ptr(x), _ptr(W1), _ptr(W2), T, d, h, act, _ptr(y),
                                    _ptr(workspace), workspace.numel(), _stream(stream)),
            "hcw_gated_ffn_fwd")
@@ -492,13 +519,13 @@ def hcw_gated_ffn_bwd(x, dy, W1, W2, act: int = HCW_GATE_SILU, dx=None, dW1=None
     _bf16("hcw_gated_ffn_bwd: tensors", x, dy, W1, W2, dx)
     T, d, h = _ffn_sizes("hcw_gated_ffn_bwd", x, W1, W2)
     if want_dx and dx is None:
-        dx = torch.empty_like(x)
+        dx = _empty_like(stream, x)
     _like(x, "hcw_gated_ffn_bwd", dy, dx)
     if want_dw:
         if dW1 is not None or dW2 is not None:
             dw_dtype = (dW1 if dW1 is not None else dW2).dtype
-        dW1 = torch.empty(2 * h, d, dtype=dw_dtype, device=x.device) if dW1 is None else dW1
-        dW2 = torch.empty(d, h, dtype=dw_dtype, device=x.device) if dW2 is None else dW2
+        dW1 = _empty(stream, 2 * h, d, dtype=dw_dtype, device=x.device) if dW1 is None else dW1
+        dW2 = _empty(stream, d, h, dtype=dw_dtype, device=x.device) if dW2 is None else dW2
         if dW1.shape != W1.shape or dW2.shape != W2.shape or dW1.dtype != dW2.dtype:
             raise ValueError("hcw_gated_ffn_bwd: dW1 and dW2 have the weights' shapes and one dtype")
         code = _dtype_code(dW1)
@@ -506,7 +533,7 @@ def hcw_gated_ffn_bwd(x, dy, W1, W2, act: int = HCW_GATE_SILU, dx=None, dW1=None
         dW1 = dW2 = None
         code = HCW_BF16
     if workspace is None:
-        workspace = _workspace(hcw_gated_ffn_bwd_workspace_bytes(T, d, h), x.device, None)
+        workspace = _workspace(stream, hcw_gated_ffn_bwd_workspace_bytes(T, d, h), x.device, None)
     _check(lib().hcw_gated_ffn_bwd(_ptr(x), _ptr(dy), _ptr(W1), _ptr(W2), T, d, h, act, code,
                                    _ptr(dx), _ptr(dW1), _ptr(dW2), _ptr(workspace),
                                    workspace.numel(), _stream(stream)), "hcw_gated_ffn_bwd")
@@ -535,9 +562,9 @@ def hcw_residual_norm_fwd(r, f, gate=None, rows_per_gate: int = 0, alpha: float 
     if gate is not None:
         _params("hcw_residual_norm_fwd: gate", _gates(T, rows_per_gate) * d, gate)
     if want_r and r_out is None:
-        r_out = torch.empty_like(ref)
+        r_out = _empty_like(stream, ref)
     if want_x and x_out is None:
-        x_out = torch.empty_like(ref)
+        x_out = _empty_like(stream, ref)
     _like(ref, "hcw_residual_norm_fwd", f, r_out, x_out)
     _check(lib().hcw_residual_norm_fwd(_ptr(r), _ptr(f), _ptr(gate), rows_per_gate, alpha, post,
                                        _ptr(post_w), _ptr(post_b), pre, _ptr(pre_w), _ptr(pre_b),
@@ -571,26 +598,26 @@ def hcw_residual_norm_bwd(dr_out, dx_out, s, f, gate=None, rows_per_gate: int = 
     has_pre = dx_out is not None and pre != HCW_NORM_NONE
     out = {}
     if want_dr:
-        out["dr"] = torch.empty_like(ref) if dr is None else dr
+        out["dr"] = _empty_like(stream, ref) if dr is None else dr
     if f is not None:
-        out["df"] = torch.empty_like(ref) if df is None else df
+        out["df"] = _empty_like(stream, ref) if df is None else df
     _like(ref, "hcw_residual_norm_bwd", dr_out, s if dx_out is not None else None, f,
           out.get("dr"), out.get("df"))
     if want_params:
         f32 = dict(dtype=torch.float32, device=ref.device)
         if f is not None and gate is not None:
-            out["dgate"] = torch.empty(G, d, **f32)
+            out["dgate"] = _empty(stream, G, d, **f32)
         if has_post:
-            out["dpost_w"] = torch.empty(d, **f32)
+            out["dpost_w"] = _empty(stream, d, **f32)
             if want_bias and post == HCW_NORM_LAYER:
-                out["dpost_b"] = torch.empty(d, **f32)
+                out["dpost_b"] = _empty(stream, d, **f32)
         if has_pre:
-            out["dpre_w"] = torch.empty(d, **f32)
+            out["dpre_w"] = _empty(stream, d, **f32)
             if want_bias and pre == HCW_NORM_LAYER:
-                out["dpre_b"] = torch.empty(d, **f32)
+                out["dpre_b"] = _empty(stream, d, **f32)
         if workspace is None:
-            workspace = _workspace(hcw_residual_norm_bwd_workspace_bytes(T, d, rows_per_gate),
-                                   ref.device, None)
+            need = hcw_residual_norm_bwd_workspace_bytes(T, d, rows_per_gate)
+            workspace = _workspace(stream, need, ref.device, None)
     get = lambda k: _ptr(out.get(k))  # noqa: E731
     _check(lib().hcw_residual_norm_bwd(_ptr(dr_out), _ptr(dx_out), _ptr(s), _ptr(f), _ptr(gate),
                                        rows_per_gate, alpha, post, _ptr(post_w), _ptr(post_b),
@@ -626,9 +653,9 @@ def hcw_distill_loss(z, idx=None, teacher=None, target=None, weight=None,
     _params("hcw_distill_loss: weight and loss", T, weight, loss)
     _numel("hcw_distill_loss: target", T, target)
     if loss is None:
-        loss = torch.empty(T, dtype=torch.float32, device=z.device)
+        loss = _empty(stream, T, dtype=torch.float32, device=z.device)
     if want_grad and dz is None:
-        dz = torch.empty_like(z)
+        dz = _empty_like(stream, z)
     _like(z, "hcw_distill_loss", dz)
     _check(lib().hcw_distill_loss(_ptr(z), _ptr(idx) if K else None, _ptr(teacher) if K else None,
                                   _ptr(target), _ptr(weight), T, V, K, _dtype_code(z),
@@ -693,14 +720,15 @@ def hcw_stack_fwd(x, W_self, W_nbr, bias=None, layer0: int = 0, dim_override: in
     B, n, d = x.shape
     L = W_self.shape[0]
     dt = _dtype_code(x)
-    y = torch.empty_like(x) if y is None else y
+    y = _empty_like(stream, x) if y is None else y
     if acts is None and L > 1:
-        acts = torch.empty((L - 1, B, n, d), dtype=x.dtype, device=x.device)
+        acts = _empty(stream, (L - 1, B, n, d), dtype=x.dtype, device=x.device)
     if want_masks is None:
         want_masks = bool(flags & HCW_ACT_RELU)
     if masks is None and want_masks:
-        masks = torch.empty((L, B, n, (d + 31) // 32), dtype=torch.int32, device=x.device)
-    ws = _workspace(hcw_stack_fwd_workspace_bytes(B, n, d, dt, flags, L), x.device, workspace)
+        masks = _empty(stream, (L, B, n, (d + 31) // 32), dtype=torch.int32, device=x.device)
+    ws = _workspace(stream, hcw_stack_fwd_workspace_bytes(B, n, d, dt, flags, L), x.device,
+                    workspace)
     if dims is not None:
         arr = _dims_array(dims, L)
         _check(lib().hcw_stack_fwd_dims(_ptr(x), _ptr(W_self), _ptr(W_nbr), _ptr(bias),
@@ -730,13 +758,13 @@ def hcw_stack_bwd(x, acts, masks, dy, W_self, W_nbr, layer0: int = 0, dim_overri
     L = W_self.shape[0]
     dt = _dtype_code(x)
     f32 = dict(dtype=torch.float32, device=x.device)
-    dx = torch.empty_like(x) if dx is None else dx
-    dW_self = torch.empty(L, d, d, **f32) if dW_self is None else dW_self
-    dW_nbr = torch.empty(L, d, d, **f32) if dW_nbr is None else dW_nbr
+    dx = _empty_like(stream, x) if dx is None else dx
+    dW_self = _empty(stream, L, d, d, **f32) if dW_self is None else dW_self
+    dW_nbr = _empty(stream, L, d, d, **f32) if dW_nbr is None else dW_nbr
     if dbias is None and want_dbias:
-        dbias = torch.empty(L, d, **f32)
+        dbias = _empty(stream, L, d, **f32)
     need = hcw_stack_workspace_bytes(B, n, d, dt, flags, L)
-    ws = _workspace(need, x.device, workspace)
+    ws = _workspace(stream, need, x.device, workspace)
     if dims is not None:
         arr = _dims_array(dims, L)
         _check(lib().hcw_stack_bwd_dims(_ptr(x), _ptr(acts), _ptr(masks), _ptr(dy),
@@ -772,18 +800,18 @@ def hcw_stack_train_step(x, W_self, W_nbr, bias, dy, layer0: int = 0, dim_overri
     L = W_self.shape[0]
     dt = _dtype_code(x)
     f32 = dict(dtype=torch.float32, device=x.device)
-    y = torch.empty_like(x) if y is None else y
+    y = _empty_like(stream, x) if y is None else y
     if acts is None and L > 1:
-        acts = torch.empty((L - 1, B, n, d), dtype=x.dtype, device=x.device)
+        acts = _empty(stream, (L - 1, B, n, d), dtype=x.dtype, device=x.device)
     if masks is None and flags & HCW_ACT_RELU:
-        masks = torch.empty((L, B, n, (d + 31) // 32), dtype=torch.int32, device=x.device)
-    dx = torch.empty_like(x) if dx is None else dx
+        masks = _empty(stream, (L, B, n, (d + 31) // 32), dtype=torch.int32, device=x.device)
+    dx = _empty_like(stream, x) if dx is None else dx
     if want_dw:
-        dW_self = torch.empty(L, d, d, **f32) if dW_self is None else dW_self
-        dW_nbr = torch.empty(L, d, d, **f32) if dW_nbr is None else dW_nbr
+        dW_self = _empty(stream, L, d, d, **f32) if dW_self is None else dW_self
+        dW_nbr = _empty(stream, L, d, d, **f32) if dW_nbr is None else dW_nbr
         if dbias is None and want_dbias:
-            dbias = torch.empty(L, d, **f32)
-    ws = _workspace(hcw_stack_train_step_workspace_bytes(B, n, d, dt, flags, L), x.device,
+            dbias = _empty(stream, L, d, **f32)
+    ws = _workspace(stream, hcw_stack_train_step_workspace_bytes(B, n, d, dt, flags, L), x.device,
                     workspace)
     if dims is not None:
         arr = _dims_array(dims, L)
@@ -824,10 +852,10 @@ def hcw_stack_bwd_data(masks, dy, W_self, W_nbr, layer0: int = 0, dim_override: 
     B, n, d = dy.shape
     L = W_self.shape[0]
     dt = _dtype_code(dy)
-    dx = torch.empty_like(dy) if dx is None else dx
-    dz = torch.empty((L, B, n, d), dtype=dy.dtype, device=dy.device) if dz is None else dz
+    dx = _empty_like(stream, dy) if dx is None else dx
+    dz = _empty(stream, (L, B, n, d), dtype=dy.dtype, device=dy.device) if dz is None else dz
     need = hcw_stack_bwd_data_workspace_bytes(B, n, d, dt, flags, L)
-    ws = _workspace(need, dy.device, workspace)
+    ws = _workspace(stream, need, dy.device, workspace)
     _check(lib().hcw_stack_bwd_data(_ptr(masks), _ptr(dy), _ptr(W_self), _ptr(W_nbr), layer0, L,
                                     dim_override, B, n, d, dt, flags, _ptr(dx), _ptr(dz),
                                     _ptr(ws), ws.numel(), _stream(stream)), "hcw_stack_bwd_data")
@@ -845,12 +873,12 @@ def hcw_stack_bwd_weight(x, acts, dz, layer0: int = 0, dim_override: int = -1, f
     L = dz.shape[0]
     dt = _dtype_code(x)
     f32 = dict(dtype=torch.float32, device=x.device)
-    dW_self = torch.empty(L, d, d, **f32) if dW_self is None else dW_self
-    dW_nbr = torch.empty(L, d, d, **f32) if dW_nbr is None else dW_nbr
+    dW_self = _empty(stream, L, d, d, **f32) if dW_self is None else dW_self
+    dW_nbr = _empty(stream, L, d, d, **f32) if dW_nbr is None else dW_nbr
     if dbias is None and want_dbias:
-        dbias = torch.empty(L, d, **f32)
+        dbias = _empty(stream, L, d, **f32)
     need = hcw_stack_bwd_weight_workspace_bytes(B, n, d, dt, flags, L)
-    ws = _workspace(need, x.device, workspace)
+    ws = _workspace(stream, need, x.device, workspace)
     if dims is not None:
         _check(lib().hcw_stack_bwd_weight_dims(_ptr(x), _ptr(acts), _ptr(dz), _dims_array(dims, L),
                                                L, B, n, d, dt, flags, _ptr(dW_self),

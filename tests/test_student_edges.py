@@ -1,5 +1,6 @@
 """Calls of the student block's operators that need no GPU to go wrong: those without rows, the
 sizes of workspaces, what the status read covers."""
+import ast
 import ctypes
 import glob
 import os
@@ -97,3 +98,42 @@ def test_lanes_that_read_or_overwrite_each_others_values_are_ordered():
     assert len(gives) == 2
     for m in gives:
         assert re.search(r"__syncwarp\(\);\s*if \(lane == 0\)( \{\s*if \(gb\))? $", row[:m.start()])
+
+
+def test_what_a_call_allocates_belongs_to_its_stream(H, monkeypatch):
+    """Memory of the current stream may still be in use there when another stream's launch writes
+    it, or be handed out again while that launch goes on."""
+    tree = ast.parse(open(H.__file__).read())
+    for f in [n for n in tree.body if isinstance(n, ast.FunctionDef)]:
+        made = [n for n in ast.walk(f) if isinstance(n, ast.Call) and
+                re.fullmatch(r"torch\.(empty|zeros|ones|full)(_like)?", ast.unparse(n.func))]
+        assert not made or f.name in ("_empty", "_empty_like", "_scratch"), f.name
+
+    log = []
+
+    class Under:
+        def __init__(self, stream):
+            self.stream = stream
+
+        def __enter__(self):
+            log.append(("under", self.stream))
+
+        def __exit__(self, *_):
+            log.append(("back", self.stream))
+
+    class Memory:
+        def record_stream(self, stream):
+            log.append(("also used on", stream))
+
+    monkeypatch.setattr(H.torch.cuda, "stream", Under)
+    monkeypatch.setattr(H.torch.cuda, "current_stream", lambda: "current")
+    monkeypatch.setattr(H.torch, "empty", lambda *a, **k: log.append("made") or Memory())
+    H._empty("side", 4)
+    assert log == [("under", "side"), "made", ("back", "side"), ("also used on", "current")]
+    del log[:]
+    H._scratch("side", 4, "cuda")
+    assert log == [("under", "side"), "made", ("back", "side")]
+    del log[:]
+    H._empty(None, 4)
+    H._scratch(None, 4, "cuda")
+    assert log == ["made", "made"]

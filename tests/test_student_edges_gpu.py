@@ -112,3 +112,43 @@ def test_a_nan_in_a_gate_row_is_not_hidden(H, T, act):
     rows = [i for i in range(T) if i != 2]
     for t in (y, dx):
         assert t[2].isnan().all() and t[rows].isfinite().all()
+
+
+def test_memory_of_a_call_on_another_stream_is_its_own(H):
+    """While the side stream is busy the current one goes on: it gets none of the memory of the
+    calls that wait there, and gives them none that it still works on."""
+    x, dy, W1, W2 = ffn_problem(700, 128, 264, 1)
+    p = Problem(700, 128, BF16, 2, rows=64)
+    par = dict(gate=p.gate, rows_per_gate=64, post=S.RMS, post_w=p.post_w, pre=S.RMS, pre_w=p.pre_w)
+    z = distill_problem(700, 500, 3, BF16, 3)
+    zs = [torch.as_tensor(t).cuda() for t in z]
+
+    def calls(stream=None):
+        y = H.hcw_gated_ffn_fwd(x, W1, W2, stream=stream)
+        dx, dW1, dW2 = H.hcw_gated_ffn_bwd(x, dy, W1, W2, stream=stream)
+        r, v = H.hcw_residual_norm_fwd(p.r, p.f, stream=stream, **par)
+        g = H.hcw_residual_norm_bwd(p.dr_out, p.dx_out, p.s, p.f, stream=stream, **par)
+        loss, dz = H.hcw_distill_loss(*zs, stream=stream)
+        return (y, dx, dW1, dW2, r, v, *g.values(), loss, dz)
+
+    want = calls()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        # blocks of many sizes that the current stream has in use, and then lets go of
+        sizes = [1 << k for k in range(9, 23)] + [t.numel() * t.element_size() for t in want]
+        torch.cuda._sleep(2_000_000)
+        for t in [torch.empty(n, dtype=torch.uint8, device="cuda") for n in sizes for _ in range(3)]:
+            t.fill_(255)
+        del t
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(20_000_000)
+        got = calls(side)
+        dropped = calls(side)
+        del dropped
+        mine = [torch.full((n,), 255, dtype=torch.uint8, device="cuda") for n in sizes
+                for _ in range(3)]
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, got))
+        assert all(bool((t == 255).all()) for t in mine)
+        del got, mine
