@@ -13,6 +13,7 @@ torch.float32 -> HCW_F32.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 import threading
 
@@ -446,28 +447,50 @@ def _rows(t):
     return (t.numel() // d if d else 0), d
 
 
+def _same_rows(a, b):
+    """Whether leading sizes a and b number the same rows in the same order: equal up to sizes of
+    1, or one of them a single run of rows."""
+    a, b = [n for n in a if n != 1], [n for n in b if n != 1]
+    return a == b or (len(a) < 2 or len(b) < 2) and math.prod(a) == math.prod(b)
+
+
 def _like(ref, what, *ts):
-    """ts (None allowed) have ref's dtype and number of elements."""
+    """ts (None allowed) have ref's dtype and rows, or all its elements in one dimension."""
+    dtype, n, d, deep = ref.dtype, ref.numel(), ref.size(-1), ref.dim() > 2
     for t in ts:
-        if t is not None and (t.dtype != ref.dtype or t.numel() != ref.numel()):
+        if t is None:
+            continue
+        k = t.dim()
+        if t.dtype != dtype or t.numel() != n or k > 1 and (
+                t.size(-1) != d or
+                k > 2 and deep and not _same_rows(t.shape[:-1], ref.shape[:-1])):
             raise ValueError("%s: %s %s does not match %s %s"
                              % (what, tuple(t.shape), t.dtype, tuple(ref.shape), ref.dtype))
 
 
-def _params(what, n, *ts):
-    """ts (None allowed) are fp32 with n elements."""
+def _params(what, G, d, *ts):
+    """ts (None allowed) are fp32: d elements where G is 1, else [G, d] or all in one dimension."""
     for t in ts:
-        if t is not None:
-            if t.dtype != torch.float32:
-                raise TypeError("%s must be float32, got %s" % (what, t.dtype))
-            if t.numel() != n:
-                raise ValueError("%s: expected %d elements, got %s" % (what, n, tuple(t.shape)))
+        if t is None:
+            continue
+        if t.dtype != torch.float32:
+            raise TypeError("%s must be float32, got %s" % (what, t.dtype))
+        if t.numel() != G * d or G > 1 and t.dim() > 1 and t.shape[-1] != d:
+            raise ValueError("%s: expected %s, got %s"
+                             % (what, (G, d) if G != 1 else (d,), tuple(t.shape)))
 
 
-def _numel(what, n, *ts):
+def _row_values(what, dtype, z, T, *ts):
+    """ts (None allowed) hold a value of this dtype for every row of z [..., V]."""
     for t in ts:
-        if t is not None and t.numel() != n:
-            raise ValueError("%s: expected %d elements, got %s" % (what, n, tuple(t.shape)))
+        if t is None:
+            continue
+        if t.dtype != dtype:
+            raise TypeError("%s must be %s, got %s" % (what, str(dtype)[6:], t.dtype))
+        if t.numel() != T or (t.dim() > 1 and z.dim() > 2 and
+                              not _same_rows(t.shape, z.shape[:-1])):
+            raise ValueError("%s: %s does not match the rows of %s"
+                             % (what, tuple(t.shape), tuple(z.shape)))
 
 
 def _bf16(what, *ts):
@@ -558,9 +581,9 @@ def hcw_residual_norm_fwd(r, f, gate=None, rows_per_gate: int = 0, alpha: float 
     if ref is None:
         raise ValueError("hcw_residual_norm_fwd: r or f is needed")
     T, d = _rows(ref)
-    _params("hcw_residual_norm_fwd: weights and biases", d, post_w, post_b, pre_w, pre_b)
+    _params("hcw_residual_norm_fwd: weights and biases", 1, d, post_w, post_b, pre_w, pre_b)
     if gate is not None:
-        _params("hcw_residual_norm_fwd: gate", _gates(T, rows_per_gate) * d, gate)
+        _params("hcw_residual_norm_fwd: gate", _gates(T, rows_per_gate), d, gate)
     if want_r and r_out is None:
         r_out = _empty_like(stream, ref)
     if want_x and x_out is None:
@@ -592,8 +615,8 @@ def hcw_residual_norm_bwd(dr_out, dx_out, s, f, gate=None, rows_per_gate: int = 
         raise ValueError("hcw_residual_norm_bwd: dr_out or dx_out is needed")
     T, d = _rows(ref)
     G = _gates(T, rows_per_gate)
-    _params("hcw_residual_norm_bwd: weights and biases", d, post_w, post_b, pre_w)
-    _params("hcw_residual_norm_bwd: gate", G * d, gate)
+    _params("hcw_residual_norm_bwd: weights and biases", 1, d, post_w, post_b, pre_w)
+    _params("hcw_residual_norm_bwd: gate", G, d, gate)
     has_post = f is not None and post != HCW_NORM_NONE
     has_pre = dx_out is not None and pre != HCW_NORM_NONE
     out = {}
@@ -640,18 +663,21 @@ def hcw_distill_loss(z, idx=None, teacher=None, target=None, weight=None,
     T, V = _rows(z)
     K = 0
     if idx is not None:
-        if teacher is None or idx.shape != teacher.shape:
+        if teacher is None or not idx.dim() or idx.shape != teacher.shape:
             raise ValueError("hcw_distill_loss: idx and teacher must have the same shape")
         if idx.dtype != torch.int32:
             raise TypeError("hcw_distill_loss: idx must be int32, got %s" % idx.dtype)
+        if teacher.dtype != torch.float32:
+            raise TypeError("hcw_distill_loss: teacher must be float32, got %s" % teacher.dtype)
         K = idx.shape[-1]
+        if idx.numel() != T * K or (idx.dim() > 2 and z.dim() > 2 and
+                                    not _same_rows(idx.shape[:-1], z.shape[:-1])):
+            raise ValueError("hcw_distill_loss: idx and teacher %s do not match z %s"
+                             % (tuple(idx.shape), tuple(z.shape)))
     elif teacher is not None:
         raise ValueError("hcw_distill_loss: teacher logits without their symbols")
-    if target is not None and target.dtype != torch.int32:
-        raise TypeError("hcw_distill_loss: target must be int32, got %s" % target.dtype)
-    _params("hcw_distill_loss: teacher", T * K, teacher)
-    _params("hcw_distill_loss: weight and loss", T, weight, loss)
-    _numel("hcw_distill_loss: target", T, target)
+    _row_values("hcw_distill_loss: target", torch.int32, z, T, target)
+    _row_values("hcw_distill_loss: weight and loss", torch.float32, z, T, weight, loss)
     if loss is None:
         loss = _empty(stream, T, dtype=torch.float32, device=z.device)
     if want_grad and dz is None:

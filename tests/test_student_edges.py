@@ -3,6 +3,7 @@ sizes of workspaces, what the status read covers."""
 import ast
 import ctypes
 import glob
+import math
 import os
 import re
 import subprocess
@@ -137,3 +138,34 @@ def test_what_a_call_allocates_belongs_to_its_stream(H, monkeypatch):
     H._empty(None, 4)
     H._scratch(None, 4, "cuda")
     assert log == ["made", "made"]
+
+
+def test_the_bindings_shape_checks(H):
+    """What numbers the same rows in the same order passes, what has the same number of elements
+    in another order does not."""
+    torch = H.torch
+    e = lambda *s: torch.empty(s, device="meta")  # noqa: E731
+    like = [((6, 8), (6, 8)), ((2, 3, 8), (6, 8)), ((6, 8), (2, 3, 8)), ((2, 1, 3, 8), (2, 3, 8)),
+            ((6, 8), (48,)), ((0, 8), (0, 8)), ((8,), (1, 8))]
+    for a, b in like:
+        H._like(e(*a), "x", e(*b), None)
+    for a, b in [((6, 8), (8, 6)), ((6, 8), (6, 4)), ((6, 8), (12, 4)), ((2, 3, 8), (3, 2, 8)),
+                 ((2, 3, 8), (3, 16)), ((6, 8), ())]:
+        with pytest.raises(ValueError, match="does not match"):
+            H._like(e(*a), "x", e(*b))
+    with pytest.raises(ValueError, match="does not match"):
+        H._like(e(6, 8), "x", e(6, 8).half())
+    for G, d, b in [(1, 8, (8,)), (1, 8, (1, 8)), (1, 8, (8, 1)), (3, 8, (3, 8)), (3, 8, (24,)),
+                    (0, 8, (0, 8))]:
+        H._params("x", G, d, e(*b), None)
+    for G, d, b in [(1, 8, (6,)), (3, 8, (8, 3)), (3, 8, (8,)), (3, 8, (2, 8))]:
+        with pytest.raises(ValueError, match="expected"):
+            H._params("x", G, d, e(*b))
+    for lead, b in [((6,), (6,)), ((6,), (6, 1)), ((2, 3), (6,)), ((2, 3), (2, 3)), ((6,), (2, 3)),
+                    ((), (1,)), ((0,), (0,))]:
+        H._row_values("x", torch.float32, e(*lead, 9), math.prod(lead), e(*b), None)
+    for lead, b in [((6,), (5,)), ((2, 3), (3, 2)), ((2, 3), (2,)), ((2, 3), (5,))]:
+        with pytest.raises(ValueError, match="does not match"):
+            H._row_values("x", torch.float32, e(*lead, 9), math.prod(lead), e(*b))
+    with pytest.raises(TypeError, match="int32"):
+        H._row_values("x", torch.int32, e(6, 9), 6, e(6))

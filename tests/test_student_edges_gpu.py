@@ -152,3 +152,35 @@ def test_memory_of_a_call_on_another_stream_is_its_own(H):
         assert all(torch.equal(a, b) for a, b in zip(want, got))
         assert all(bool((t == 255).all()) for t in mine)
         del got, mine
+
+
+def test_rows_in_another_order_are_refused(H):
+    """As many elements are not enough."""
+    t = lambda *s, dtype=BF16: torch.zeros(*s, dtype=dtype, device="cuda")  # noqa: E731
+    par = dict(rows_per_gate=2, post=S.RMS, pre=S.RMS)
+    r, f, gate = t(6, 8), t(6, 8), t(3, 8, dtype=F32)
+    H.hcw_residual_norm_fwd(r.view(2, 3, 8), f, gate, **par)
+    H.hcw_residual_norm_bwd(r.view(2, 3, 8), f, r, f, gate, **par)
+    for bad in (dict(f=t(8, 6)), dict(gate=t(8, 3, dtype=F32)), dict(r_out=t(4, 12))):
+        with pytest.raises(ValueError):
+            H.hcw_residual_norm_fwd(**{"r": r, "f": f, "gate": gate, **par, **bad})
+    for bad in (dict(s=t(8, 6)), dict(gate=t(8, 3, dtype=F32)), dict(df=t(12, 4))):
+        with pytest.raises(ValueError):
+            H.hcw_residual_norm_bwd(**{"dr_out": r, "dx_out": r, "s": r, "f": f, "gate": gate, **par,
+                                       **bad})
+    W1, W2 = t(32, 8), t(8, 16)
+    for bad in (t(8, 6), t(3, 16)):
+        with pytest.raises(ValueError):
+            H.hcw_gated_ffn_fwd(r, W1, W2, y=bad)
+        with pytest.raises(ValueError):
+            H.hcw_gated_ffn_bwd(r, bad, W1, W2)
+    z = t(2, 3, 40)
+    ok = dict(idx=t(2, 3, 4, dtype=torch.int32), teacher=t(2, 3, 4, dtype=F32),
+              target=t(6, dtype=torch.int32), weight=t(2, 3, dtype=F32))
+    H.hcw_distill_loss(z, **ok)
+    for bad in (dict(target=t(3, 2, dtype=torch.int32)), dict(weight=t(3, 2, dtype=F32)),
+                dict(idx=t(3, 2, 4, dtype=torch.int32), teacher=t(3, 2, 4, dtype=F32)),
+                dict(dz=t(3, 2, 40)), dict(loss=t(3, 2, dtype=F32))):
+        with pytest.raises(ValueError):
+            H.hcw_distill_loss(z, **{**ok, **bad})
+    assert H.hcw_sync_status() == H.HCW_OK
