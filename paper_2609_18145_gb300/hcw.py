@@ -183,20 +183,25 @@ def _stream(stream):
 # What a wrapper allocates belongs to the stream it launches on: a block is handed out again in
 # the order of the stream it was allocated under, so memory of the current stream could still
 # be in use there before the launch, or be given away while the launch on `stream` goes on.
-def _empty(stream, *size, **kw):
-    """torch.empty of an output; the caller may go on with it on the current stream."""
-    if stream is None:
-        return torch.empty(*size, **kw)
-    with torch.cuda.stream(stream):
-        t = torch.empty(*size, **kw)
-    t.record_stream(torch.cuda.current_stream())
-    return t
+class _Memory:
+    """torch.empty and torch.empty_like for the outputs of a call on `stream`; the caller may go on
+    with them on the current stream."""
+
+    def __init__(self, stream):
+        self.stream = stream
+
+    def empty(self, *size, **kw):
+        with torch.cuda.stream(self.stream):
+            t = torch.empty(*size, **kw)
+        t.record_stream(torch.cuda.current_stream())
+        return t
+
+    def empty_like(self, t):
+        return self.empty(t.shape, dtype=t.dtype, device=t.device)
 
 
-def _empty_like(stream, t):
-    if stream is None:
-        return torch.empty_like(t)
-    return _empty(stream, t.shape, dtype=t.dtype, device=t.device)
+def _memory(stream):
+    return torch if stream is None else _Memory(stream)
 
 
 def _scratch(stream, nbytes, device):
@@ -238,7 +243,8 @@ def hcw_partner_table(layer: int, n: int, flags: int = 0, dim_override: int = -1
 
 def hcw_partner_table_device(layer: int, n: int, flags: int = 0, dim_override: int = -1,
                              device=None, stream=None) -> torch.Tensor:
-    out = _empty(stream, n, dtype=torch.int32, device=device or "cuda")
+    mem = _memory(stream)
+    out = mem.empty(n, dtype=torch.int32, device=device or "cuda")
     _check(lib().hcw_partner_table_device(layer, dim_override, n, flags, _ptr(out),
                                           _stream(stream)), "hcw_partner_table_device")
     return out
@@ -249,10 +255,11 @@ def hcw_layer_fwd(x, W_self, W_nbr, bias=None, layer: int = 0, dim_override: int
     """One layer forward; returns y (and z_save if want_z or given)."""
     _dev(x, W_self, W_nbr, bias, y, z_save)
     B, n, d = x.shape
+    mem = _memory(stream)
     if y is None:
-        y = _empty_like(stream, x)
+        y = mem.empty_like(x)
     if want_z and z_save is None:
-        z_save = _empty_like(stream, x)
+        z_save = mem.empty_like(x)
     _check(lib().hcw_layer_fwd(_ptr(x), _ptr(W_self), _ptr(W_nbr), _ptr(bias), layer,
                                dim_override, B, n, d, _dtype_code(x), flags, _ptr(y),
                                _ptr(z_save), _stream(stream)), "hcw_layer_fwd")
@@ -281,11 +288,12 @@ def hcw_layer_bwd(x, z_save, dy, W_self, W_nbr, layer: int = 0, dim_override: in
     B, n, d = x.shape
     dt = _dtype_code(x)
     f32 = dict(dtype=torch.float32, device=x.device)
-    dx = _empty_like(stream, x) if dx is None else dx
-    dW_self = _empty(stream, d, d, **f32) if dW_self is None else dW_self
-    dW_nbr = _empty(stream, d, d, **f32) if dW_nbr is None else dW_nbr
+    mem = _memory(stream)
+    dx = mem.empty_like(x) if dx is None else dx
+    dW_self = mem.empty(d, d, **f32) if dW_self is None else dW_self
+    dW_nbr = mem.empty(d, d, **f32) if dW_nbr is None else dW_nbr
     if dbias is None and want_dbias:
-        dbias = _empty(stream, d, **f32)
+        dbias = mem.empty(d, **f32)
     need = hcw_workspace_bytes(B, n, d, dt, flags)
     ws = _workspace(stream, need, x.device, workspace)
     _check(lib().hcw_layer_bwd(_ptr(x), _ptr(z_save), _ptr(dy), _ptr(W_self), _ptr(W_nbr),
@@ -300,7 +308,8 @@ def hcw_layer_bwd_data(dz, dy, W_self, W_nbr, layer: int = 0, dim_override: int 
     """Input gradient of one layer from dz = dy * act'(z); returns dx."""
     _dev(dz, dy, W_self, W_nbr, dx)
     B, n, d = dz.shape
-    dx = _empty_like(stream, dz) if dx is None else dx
+    mem = _memory(stream)
+    dx = mem.empty_like(dz) if dx is None else dx
     _check(lib().hcw_layer_bwd_data(_ptr(dz), _ptr(dy), _ptr(W_self), _ptr(W_nbr), layer,
                                     dim_override, B, n, d, _dtype_code(dz), flags, _ptr(dx),
                                     _stream(stream)), "hcw_layer_bwd_data")
@@ -319,10 +328,11 @@ def hcw_layer_bwd_weight(x, dz, layer: int = 0, dim_override: int = -1, flags: i
     B, n, d = x.shape
     dt = _dtype_code(x)
     f32 = dict(dtype=torch.float32, device=x.device)
-    dW_self = _empty(stream, d, d, **f32) if dW_self is None else dW_self
-    dW_nbr = _empty(stream, d, d, **f32) if dW_nbr is None else dW_nbr
+    mem = _memory(stream)
+    dW_self = mem.empty(d, d, **f32) if dW_self is None else dW_self
+    dW_nbr = mem.empty(d, d, **f32) if dW_nbr is None else dW_nbr
     if dbias is None and want_dbias:
-        dbias = _empty(stream, d, **f32)
+        dbias = mem.empty(d, **f32)
     ws = _workspace(stream, hcw_layer_bwd_weight_workspace_bytes(B, n, d, dt, flags), x.device,
                     workspace)
     _check(lib().hcw_layer_bwd_weight(_ptr(x), _ptr(dz), layer, dim_override, B, n, d, dt, flags,
@@ -344,7 +354,8 @@ def hcw_decode_step(x_t, W_self, W_nbr, bias, t: int, n: int, cache, flags: int,
     _dev(x_t, W_self, W_nbr, bias, cache, y)
     B, d = x_t.shape
     L = W_self.shape[0]
-    y = _empty_like(stream, x_t) if y is None else y
+    mem = _memory(stream)
+    y = mem.empty_like(x_t) if y is None else y
     arr = None if dims is None else _dims_array(dims, L)
     _check(lib().hcw_decode_step(_ptr(x_t), _ptr(W_self), _ptr(W_nbr), _ptr(bias),
                                  None if arr is None else ctypes.cast(arr, _P), layer0, L, t, B,
@@ -378,10 +389,11 @@ def hcw_block_step(ids, params: dict, grads: dict | None = None, loss=None, work
     V, d = params["E"].shape
     L, h = params["W1"].shape[0], params["W1"].shape[1]
     dev = ids.device
+    mem = _memory(stream)
     if grads is None:
-        grads = {f: _empty(stream, tuple(params[f].shape), dtype=torch.float32, device=dev)
+        grads = {f: mem.empty(tuple(params[f].shape), dtype=torch.float32, device=dev)
                  for f in BLOCK_FIELDS}
-    loss = _empty(stream, 1, dtype=torch.float32, device=dev) if loss is None else loss
+    loss = mem.empty(1, dtype=torch.float32, device=dev) if loss is None else loss
     ws = _workspace(stream, hcw_block_workspace_bytes(B, n, d, h, V, L), dev, workspace)
     P = _BlockPtrs(*[params[f].data_ptr() for f in BLOCK_FIELDS])
     G = _BlockPtrs(*[grads[f].data_ptr() for f in BLOCK_FIELDS])
@@ -407,7 +419,8 @@ def hcw_gemm_bf16(A, B, ta: bool = False, tb: bool = False, C=None, workspace=No
     Kb, N = (B.shape[1], B.shape[0]) if tb else (B.shape[0], B.shape[1])
     if Kb != K:
         raise ValueError("hcw_gemm_bf16: inner sizes differ (%d, %d)" % (K, Kb))
-    C = _empty(stream, M, N, dtype=torch.float32, device=A.device) if C is None else C
+    mem = _memory(stream)
+    C = mem.empty(M, N, dtype=torch.float32, device=A.device) if C is None else C
     if split:
         ws = _workspace(stream, hcw_gemm_workspace_bytes(M, N, K), A.device, workspace)
         wp, wn = _ptr(ws), ws.numel()
@@ -435,7 +448,8 @@ def hcw_gemm_bf16_batched(A, B, C=None, stream=None):
     N = B.shape[2]
     if A.stride(2) != 1 or A.stride(1) != M or B.stride(2) != 1 or B.stride(1) != N:
         raise ValueError("hcw_gemm_bf16_batched: each product's rows must be contiguous")
-    C = _empty(stream, batch, M, N, dtype=torch.float32, device=A.device) if C is None else C
+    mem = _memory(stream)
+    C = mem.empty(batch, M, N, dtype=torch.float32, device=A.device) if C is None else C
     _check(lib().hcw_gemm_bf16_batched(M, N, K, _ptr(A), A.stride(0), _ptr(B), B.stride(0),
                                        _ptr(C), batch, _stream(stream)), "hcw_gemm_bf16_batched")
     return C
@@ -456,14 +470,12 @@ def _same_rows(a, b):
 
 def _like(ref, what, *ts):
     """ts (None allowed) have ref's dtype and rows, or all its elements in one dimension."""
-    dtype, n, d, deep = ref.dtype, ref.numel(), ref.size(-1), ref.dim() > 2
+    dtype, shape = ref.dtype, ref.shape
     for t in ts:
-        if t is None:
+        if t is None or t.shape == shape and t.dtype == dtype:
             continue
-        k = t.dim()
-        if t.dtype != dtype or t.numel() != n or k > 1 and (
-                t.size(-1) != d or
-                k > 2 and deep and not _same_rows(t.shape[:-1], ref.shape[:-1])):
+        if t.dtype != dtype or t.numel() != ref.numel() or t.dim() > 1 and (
+                t.shape[-1] != shape[-1] or not _same_rows(t.shape[:-1], shape[:-1])):
             raise ValueError("%s: %s %s does not match %s %s"
                              % (what, tuple(t.shape), t.dtype, tuple(ref.shape), ref.dtype))
 
@@ -480,17 +492,17 @@ def _params(what, G, d, *ts):
                              % (what, (G, d) if G != 1 else (d,), tuple(t.shape)))
 
 
-def _row_values(what, dtype, z, T, *ts):
-    """ts (None allowed) hold a value of this dtype for every row of z [..., V]."""
+def _row_values(what, dtype, T, rows, *ts):
+    """ts (None allowed) hold a value of this dtype for each of T rows, of leading sizes `rows`
+    (None: one run of rows)."""
     for t in ts:
         if t is None:
             continue
         if t.dtype != dtype:
             raise TypeError("%s must be %s, got %s" % (what, str(dtype)[6:], t.dtype))
-        if t.numel() != T or (t.dim() > 1 and z.dim() > 2 and
-                              not _same_rows(t.shape, z.shape[:-1])):
-            raise ValueError("%s: %s does not match the rows of %s"
-                             % (what, tuple(t.shape), tuple(z.shape)))
+        if t.numel() != T or rows is not None and not _same_rows(t.shape, rows):
+            raise ValueError("%s: %s does not match rows of %s"
+                             % (what, tuple(t.shape), T if rows is None else tuple(rows)))
 
 
 def _bf16(what, *ts):
@@ -518,7 +530,8 @@ def hcw_gated_ffn_fwd(x, W1, W2, act: int = HCW_GATE_SILU, y=None, workspace=Non
     _dev(x, W1, W2, y, workspace)
     _bf16("hcw_gated_ffn_fwd: tensors", x, W1, W2, y)
     T, d, h = _ffn_sizes("hcw_gated_ffn_fwd", x, W1, W2)
-    y = _empty_like(stream, x) if y is None else y
+    mem = _memory(stream)
+    y = mem.empty_like(x) if y is None else y
     _like(x, "hcw_gated_ffn_fwd", y)
     if workspace is None:
         workspace = _workspace(stream, hcw_gated_ffn_fwd_workspace_bytes(T, d, h), x.device, None)
@@ -541,14 +554,15 @@ def hcw_gated_ffn_bwd(x, dy, W1, W2, act: int = HCW_GATE_SILU, dx=None, dW1=None
     _dev(x, dy, W1, W2, dx, dW1, dW2, workspace)
     _bf16("hcw_gated_ffn_bwd: tensors", x, dy, W1, W2, dx)
     T, d, h = _ffn_sizes("hcw_gated_ffn_bwd", x, W1, W2)
+    mem = _memory(stream)
     if want_dx and dx is None:
-        dx = _empty_like(stream, x)
+        dx = mem.empty_like(x)
     _like(x, "hcw_gated_ffn_bwd", dy, dx)
     if want_dw:
         if dW1 is not None or dW2 is not None:
             dw_dtype = (dW1 if dW1 is not None else dW2).dtype
-        dW1 = _empty(stream, 2 * h, d, dtype=dw_dtype, device=x.device) if dW1 is None else dW1
-        dW2 = _empty(stream, d, h, dtype=dw_dtype, device=x.device) if dW2 is None else dW2
+        dW1 = mem.empty(2 * h, d, dtype=dw_dtype, device=x.device) if dW1 is None else dW1
+        dW2 = mem.empty(d, h, dtype=dw_dtype, device=x.device) if dW2 is None else dW2
         if dW1.shape != W1.shape or dW2.shape != W2.shape or dW1.dtype != dW2.dtype:
             raise ValueError("hcw_gated_ffn_bwd: dW1 and dW2 have the weights' shapes and one dtype")
         code = _dtype_code(dW1)
@@ -584,10 +598,11 @@ def hcw_residual_norm_fwd(r, f, gate=None, rows_per_gate: int = 0, alpha: float 
     _params("hcw_residual_norm_fwd: weights and biases", 1, d, post_w, post_b, pre_w, pre_b)
     if gate is not None:
         _params("hcw_residual_norm_fwd: gate", _gates(T, rows_per_gate), d, gate)
+    mem = _memory(stream)
     if want_r and r_out is None:
-        r_out = _empty_like(stream, ref)
+        r_out = mem.empty_like(ref)
     if want_x and x_out is None:
-        x_out = _empty_like(stream, ref)
+        x_out = mem.empty_like(ref)
     _like(ref, "hcw_residual_norm_fwd", f, r_out, x_out)
     _check(lib().hcw_residual_norm_fwd(_ptr(r), _ptr(f), _ptr(gate), rows_per_gate, alpha, post,
                                        _ptr(post_w), _ptr(post_b), pre, _ptr(pre_w), _ptr(pre_b),
@@ -620,24 +635,25 @@ def hcw_residual_norm_bwd(dr_out, dx_out, s, f, gate=None, rows_per_gate: int = 
     has_post = f is not None and post != HCW_NORM_NONE
     has_pre = dx_out is not None and pre != HCW_NORM_NONE
     out = {}
+    mem = _memory(stream)
     if want_dr:
-        out["dr"] = _empty_like(stream, ref) if dr is None else dr
+        out["dr"] = mem.empty_like(ref) if dr is None else dr
     if f is not None:
-        out["df"] = _empty_like(stream, ref) if df is None else df
+        out["df"] = mem.empty_like(ref) if df is None else df
     _like(ref, "hcw_residual_norm_bwd", dr_out, s if dx_out is not None else None, f,
           out.get("dr"), out.get("df"))
     if want_params:
         f32 = dict(dtype=torch.float32, device=ref.device)
         if f is not None and gate is not None:
-            out["dgate"] = _empty(stream, G, d, **f32)
+            out["dgate"] = mem.empty(G, d, **f32)
         if has_post:
-            out["dpost_w"] = _empty(stream, d, **f32)
+            out["dpost_w"] = mem.empty(d, **f32)
             if want_bias and post == HCW_NORM_LAYER:
-                out["dpost_b"] = _empty(stream, d, **f32)
+                out["dpost_b"] = mem.empty(d, **f32)
         if has_pre:
-            out["dpre_w"] = _empty(stream, d, **f32)
+            out["dpre_w"] = mem.empty(d, **f32)
             if want_bias and pre == HCW_NORM_LAYER:
-                out["dpre_b"] = _empty(stream, d, **f32)
+                out["dpre_b"] = mem.empty(d, **f32)
         if workspace is None:
             need = hcw_residual_norm_bwd_workspace_bytes(T, d, rows_per_gate)
             workspace = _workspace(stream, need, ref.device, None)
@@ -661,7 +677,7 @@ def hcw_distill_loss(z, idx=None, teacher=None, target=None, weight=None,
     Returns (loss [T] fp32, dz like z, or None with want_grad=False)."""
     _dev(z, idx, teacher, target, weight, loss, dz)
     T, V = _rows(z)
-    K = 0
+    rows, K = z.shape[:-1] if z.dim() > 2 else None, 0
     if idx is not None:
         if teacher is None or not idx.dim() or idx.shape != teacher.shape:
             raise ValueError("hcw_distill_loss: idx and teacher must have the same shape")
@@ -670,18 +686,18 @@ def hcw_distill_loss(z, idx=None, teacher=None, target=None, weight=None,
         if teacher.dtype != torch.float32:
             raise TypeError("hcw_distill_loss: teacher must be float32, got %s" % teacher.dtype)
         K = idx.shape[-1]
-        if idx.numel() != T * K or (idx.dim() > 2 and z.dim() > 2 and
-                                    not _same_rows(idx.shape[:-1], z.shape[:-1])):
+        if idx.numel() != T * K or rows is not None and not _same_rows(idx.shape[:-1], rows):
             raise ValueError("hcw_distill_loss: idx and teacher %s do not match z %s"
                              % (tuple(idx.shape), tuple(z.shape)))
     elif teacher is not None:
         raise ValueError("hcw_distill_loss: teacher logits without their symbols")
-    _row_values("hcw_distill_loss: target", torch.int32, z, T, target)
-    _row_values("hcw_distill_loss: weight and loss", torch.float32, z, T, weight, loss)
+    _row_values("hcw_distill_loss: target", torch.int32, T, rows, target)
+    _row_values("hcw_distill_loss: weight and loss", torch.float32, T, rows, weight, loss)
+    mem = _memory(stream)
     if loss is None:
-        loss = _empty(stream, T, dtype=torch.float32, device=z.device)
+        loss = mem.empty(T, dtype=torch.float32, device=z.device)
     if want_grad and dz is None:
-        dz = _empty_like(stream, z)
+        dz = mem.empty_like(z)
     _like(z, "hcw_distill_loss", dz)
     _check(lib().hcw_distill_loss(_ptr(z), _ptr(idx) if K else None, _ptr(teacher) if K else None,
                                   _ptr(target), _ptr(weight), T, V, K, _dtype_code(z),
@@ -746,13 +762,14 @@ def hcw_stack_fwd(x, W_self, W_nbr, bias=None, layer0: int = 0, dim_override: in
     B, n, d = x.shape
     L = W_self.shape[0]
     dt = _dtype_code(x)
-    y = _empty_like(stream, x) if y is None else y
+    mem = _memory(stream)
+    y = mem.empty_like(x) if y is None else y
     if acts is None and L > 1:
-        acts = _empty(stream, (L - 1, B, n, d), dtype=x.dtype, device=x.device)
+        acts = mem.empty((L - 1, B, n, d), dtype=x.dtype, device=x.device)
     if want_masks is None:
         want_masks = bool(flags & HCW_ACT_RELU)
     if masks is None and want_masks:
-        masks = _empty(stream, (L, B, n, (d + 31) // 32), dtype=torch.int32, device=x.device)
+        masks = mem.empty((L, B, n, (d + 31) // 32), dtype=torch.int32, device=x.device)
     ws = _workspace(stream, hcw_stack_fwd_workspace_bytes(B, n, d, dt, flags, L), x.device,
                     workspace)
     if dims is not None:
@@ -784,11 +801,12 @@ def hcw_stack_bwd(x, acts, masks, dy, W_self, W_nbr, layer0: int = 0, dim_overri
     L = W_self.shape[0]
     dt = _dtype_code(x)
     f32 = dict(dtype=torch.float32, device=x.device)
-    dx = _empty_like(stream, x) if dx is None else dx
-    dW_self = _empty(stream, L, d, d, **f32) if dW_self is None else dW_self
-    dW_nbr = _empty(stream, L, d, d, **f32) if dW_nbr is None else dW_nbr
+    mem = _memory(stream)
+    dx = mem.empty_like(x) if dx is None else dx
+    dW_self = mem.empty(L, d, d, **f32) if dW_self is None else dW_self
+    dW_nbr = mem.empty(L, d, d, **f32) if dW_nbr is None else dW_nbr
     if dbias is None and want_dbias:
-        dbias = _empty(stream, L, d, **f32)
+        dbias = mem.empty(L, d, **f32)
     need = hcw_stack_workspace_bytes(B, n, d, dt, flags, L)
     ws = _workspace(stream, need, x.device, workspace)
     if dims is not None:
@@ -826,17 +844,18 @@ def hcw_stack_train_step(x, W_self, W_nbr, bias, dy, layer0: int = 0, dim_overri
     L = W_self.shape[0]
     dt = _dtype_code(x)
     f32 = dict(dtype=torch.float32, device=x.device)
-    y = _empty_like(stream, x) if y is None else y
+    mem = _memory(stream)
+    y = mem.empty_like(x) if y is None else y
     if acts is None and L > 1:
-        acts = _empty(stream, (L - 1, B, n, d), dtype=x.dtype, device=x.device)
+        acts = mem.empty((L - 1, B, n, d), dtype=x.dtype, device=x.device)
     if masks is None and flags & HCW_ACT_RELU:
-        masks = _empty(stream, (L, B, n, (d + 31) // 32), dtype=torch.int32, device=x.device)
-    dx = _empty_like(stream, x) if dx is None else dx
+        masks = mem.empty((L, B, n, (d + 31) // 32), dtype=torch.int32, device=x.device)
+    dx = mem.empty_like(x) if dx is None else dx
     if want_dw:
-        dW_self = _empty(stream, L, d, d, **f32) if dW_self is None else dW_self
-        dW_nbr = _empty(stream, L, d, d, **f32) if dW_nbr is None else dW_nbr
+        dW_self = mem.empty(L, d, d, **f32) if dW_self is None else dW_self
+        dW_nbr = mem.empty(L, d, d, **f32) if dW_nbr is None else dW_nbr
         if dbias is None and want_dbias:
-            dbias = _empty(stream, L, d, **f32)
+            dbias = mem.empty(L, d, **f32)
     ws = _workspace(stream, hcw_stack_train_step_workspace_bytes(B, n, d, dt, flags, L), x.device,
                     workspace)
     if dims is not None:
@@ -878,8 +897,9 @@ def hcw_stack_bwd_data(masks, dy, W_self, W_nbr, layer0: int = 0, dim_override: 
     B, n, d = dy.shape
     L = W_self.shape[0]
     dt = _dtype_code(dy)
-    dx = _empty_like(stream, dy) if dx is None else dx
-    dz = _empty(stream, (L, B, n, d), dtype=dy.dtype, device=dy.device) if dz is None else dz
+    mem = _memory(stream)
+    dx = mem.empty_like(dy) if dx is None else dx
+    dz = mem.empty((L, B, n, d), dtype=dy.dtype, device=dy.device) if dz is None else dz
     need = hcw_stack_bwd_data_workspace_bytes(B, n, d, dt, flags, L)
     ws = _workspace(stream, need, dy.device, workspace)
     _check(lib().hcw_stack_bwd_data(_ptr(masks), _ptr(dy), _ptr(W_self), _ptr(W_nbr), layer0, L,
@@ -899,10 +919,11 @@ def hcw_stack_bwd_weight(x, acts, dz, layer0: int = 0, dim_override: int = -1, f
     L = dz.shape[0]
     dt = _dtype_code(x)
     f32 = dict(dtype=torch.float32, device=x.device)
-    dW_self = _empty(stream, L, d, d, **f32) if dW_self is None else dW_self
-    dW_nbr = _empty(stream, L, d, d, **f32) if dW_nbr is None else dW_nbr
+    mem = _memory(stream)
+    dW_self = mem.empty(L, d, d, **f32) if dW_self is None else dW_self
+    dW_nbr = mem.empty(L, d, d, **f32) if dW_nbr is None else dW_nbr
     if dbias is None and want_dbias:
-        dbias = _empty(stream, L, d, **f32)
+        dbias = mem.empty(L, d, **f32)
     need = hcw_stack_bwd_weight_workspace_bytes(B, n, d, dt, flags, L)
     ws = _workspace(stream, need, x.device, workspace)
     if dims is not None:

@@ -108,7 +108,7 @@ def test_what_a_call_allocates_belongs_to_its_stream(H, monkeypatch):
     for f in [n for n in tree.body if isinstance(n, ast.FunctionDef)]:
         made = [n for n in ast.walk(f) if isinstance(n, ast.Call) and
                 re.fullmatch(r"torch\.(empty|zeros|ones|full)(_like)?", ast.unparse(n.func))]
-        assert not made or f.name in ("_empty", "_empty_like", "_scratch"), f.name
+        assert not made or f.name == "_scratch", f.name
 
     log = []
 
@@ -129,13 +129,14 @@ def test_what_a_call_allocates_belongs_to_its_stream(H, monkeypatch):
     monkeypatch.setattr(H.torch.cuda, "stream", Under)
     monkeypatch.setattr(H.torch.cuda, "current_stream", lambda: "current")
     monkeypatch.setattr(H.torch, "empty", lambda *a, **k: log.append("made") or Memory())
-    H._empty("side", 4)
+    H._memory("side").empty(4)
     assert log == [("under", "side"), "made", ("back", "side"), ("also used on", "current")]
     del log[:]
     H._scratch("side", 4, "cuda")
     assert log == [("under", "side"), "made", ("back", "side")]
     del log[:]
-    H._empty(None, 4)
+    assert H._memory(None) is H.torch
+    H._memory(None).empty(4)
     H._scratch(None, 4, "cuda")
     assert log == ["made", "made"]
 
@@ -163,9 +164,9 @@ def test_the_bindings_shape_checks(H):
             H._params("x", G, d, e(*b))
     for lead, b in [((6,), (6,)), ((6,), (6, 1)), ((2, 3), (6,)), ((2, 3), (2, 3)), ((6,), (2, 3)),
                     ((), (1,)), ((0,), (0,))]:
-        H._row_values("x", torch.float32, e(*lead, 9), math.prod(lead), e(*b), None)
+        H._row_values("x", torch.float32, math.prod(lead), lead, e(*b), None)
     for lead, b in [((6,), (5,)), ((2, 3), (3, 2)), ((2, 3), (2,)), ((2, 3), (5,))]:
         with pytest.raises(ValueError, match="does not match"):
-            H._row_values("x", torch.float32, e(*lead, 9), math.prod(lead), e(*b))
+            H._row_values("x", torch.float32, math.prod(lead), lead, e(*b))
     with pytest.raises(TypeError, match="int32"):
-        H._row_values("x", torch.int32, e(6, 9), 6, e(6))
+        H._row_values("x", torch.int32, 6, None, e(6))
