@@ -325,8 +325,9 @@ __global__ void __launch_bounds__(kFThreads, 1) ffn_pair_kernel(const __grid_con
                     }
                 }
             }
-            if (!ok && rank == 0)
-                // every copy of the pair completes on the leader's barriers
+            if (rank == 0)
+                // every copy of the pair completes on the leader's barriers; also when this
+                // warp has issued them all and the one that reads them gave up
                 for (int s = 0; s < kStages; ++s)
                     if (issued_mask & (1u << s))
                         mbar_wait_drain(&bars->full[s], (issued_phase >> s) & 1u, tmo);
@@ -610,6 +611,7 @@ __global__ void __launch_bounds__(kFThreads, 1) ffn_pair_kernel(const __grid_con
     tc_fence_before();
     __syncthreads();
     cluster_sync_all();   // neither CTA frees the pair's TMEM while the other uses it
+    if (*abort) settle_after_abort();   // copies of one CTA that the leader did not get to count
     if (warp == 1) {
         __syncwarp();
         tc_fence_after();

@@ -130,6 +130,15 @@ __device__ __forceinline__ bool mbar_wait_drain(uint64_t* bar, uint32_t parity,
     return true;
 }
 
+// After giving up, once no CTA of the cluster starts anything more: time (1 ms, where a copy
+// takes microseconds) for what is on its way into this CTA's shared memory and is counted by no
+// barrier that it could wait for.
+__device__ __forceinline__ void settle_after_abort() {
+    const uint64_t t0 = globaltimer_ns();
+    while (globaltimer_ns() - t0 < 1000000u) {
+    }
+}
+
 // ------------------------------------------------------------------ TMA
 __device__ __forceinline__ void tma_prefetch_desc(const CUtensorMap* m) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(m)) : "memory");

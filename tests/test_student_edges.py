@@ -170,3 +170,13 @@ def test_the_bindings_shape_checks(H):
             H._row_values("x", torch.float32, math.prod(lead), lead, e(*b))
     with pytest.raises(TypeError, match="int32"):
         H._row_values("x", torch.int32, 6, None, e(6))
+
+
+def test_a_pair_that_gives_up_waits_for_its_copies():
+    """The copies' landing is waited for whichever warp gave up, not only where the one that starts
+    them did."""
+    body = dict(kernels(open(os.path.join(CSRC, "hcw_ffn.cu")).read()))["ffn_pair_kernel"]
+    drain = body.index("mbar_wait_drain(&bars->full[s]")
+    cond = re.findall(r"if \(([^;{}]*)\)\s+for \(int s = 0;", body[:drain])[-1]
+    assert cond == "rank == 0"
+    assert re.search(r"cluster_sync_all\(\);\s+if \(\*abort\) settle_after_abort\(\);", body)
