@@ -968,9 +968,11 @@ __global__ void __launch_bounds__(NT + 32 + 32 * slot_warps(NT), NT == 512 ? 1 :
             ++nb;
         }
     }
-    // no CTA leaves while another may still send to it
+    // No CTA leaves while another may still send to it.  A sent part that was waited for has come
+    // by then; after giving up some were not.
     __syncwarp();
     cluster_sync_all();
+    if (*abort) settle_after_abort();
 }
 
 template <typename T, int NT, int EXPS>

@@ -180,3 +180,9 @@ def test_a_pair_that_gives_up_waits_for_its_copies():
     cond = re.findall(r"if \(([^;{}]*)\)\s+for \(int s = 0;", body[:drain])[-1]
     assert cond == "rank == 0"
     assert re.search(r"cluster_sync_all\(\);\s+if \(\*abort\) settle_after_abort\(\);", body)
+
+
+def test_a_cluster_that_gives_up_waits_for_what_was_sent():
+    """Parts that another CTA sent are counted by barriers that are no longer waited for."""
+    body = dict(kernels(open(os.path.join(CSRC, "hcw_distill.cu")).read()))["distill_row_kernel"]
+    assert re.search(r"cluster_sync_all\(\);\s+if \(\*abort\) settle_after_abort\(\);\s*\}$", body)
