@@ -88,11 +88,17 @@ struct __align__(16) NormShared {
 __device__ __forceinline__ void item_rows(const NormArgs& a, int item, int& g, int& r0, int& r1) {
     g = item / a.slices;
     const int first = g * a.rows_per_gate;
-    const int n = a.T - first < a.rows_per_gate ? a.T - first : a.rows_per_gate;
-    const int len = (n + a.slices - 1) / a.slices;
-    const int sl = item - g * a.slices;
-    r0 = first + (sl * len < n ? sl * len : n);
-    r1 = first + (sl * len < n - len ? sl * len + len : n);
+    // (unsigned: up to slices - 1 more than the rows, of which there may be 2^31 - 1)
+    const unsigned n = a.T - first < a.rows_per_gate ? a.T - first : a.rows_per_gate;
+    const unsigned len = (n + a.slices - 1) / a.slices;
+    const unsigned at = (unsigned)(item - g * a.slices) * len;
+    r0 = first + (int)(at < n ? at : n);
+    r1 = first + (int)(at < n - len ? at + len : n);
+}
+
+// `step` on from i, or to the end
+__device__ __forceinline__ int norm_next(int i, int step, int end) {
+    return step < end - i ? i + step : end;
 }
 
 // The ring's source: thread 0 walks the same items and rows as the CTA works through, up
@@ -119,7 +125,7 @@ struct NormFeed {
     __device__ __forceinline__ void settle(const NormArgs& a) {
         const int items = a.groups * a.slices;
         while (item < items && row >= r1) {
-            item += gridDim.x;
+            item = norm_next(item, (int)gridDim.x, items);
             int g;
             if (item < items) item_rows(a, item, g, row, r1);
         }
@@ -505,7 +511,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_fwd_kernel(const NormArgs a
     int b = 0;
     uint32_t round = 0;
     bool ok = true;
-    for (int item = blockIdx.x; item < items; item += gridDim.x) {
+    for (int item = blockIdx.x; item < items; item = norm_next(item, (int)gridDim.x, items)) {
         int g, r0, r1;
         item_rows(a, item, g, r0, r1);
         const float* gate = a.gate ? a.gate + (size_t)g * d : nullptr;
@@ -519,7 +525,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_fwd_kernel(const NormArgs a
             if (LN && k == 3) C.fill(pb, a.pre_b, nullptr, 0.f);
         }
         __syncthreads();
-        for (int row0 = r0; row0 < r1; row0 += a.rows) {
+        for (int row0 = r0; row0 < r1; row0 = norm_next(row0, a.rows, r1)) {
             ok = ok && norm_rows_landed(sh, b, round);
             // a group's rows past the buffer's n hold what was there before: they are worked
             // on and not stored
@@ -725,7 +731,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const NormArgs a
     int b = 0;
     uint32_t round = 0;
     bool ok = true;
-    for (int item = blockIdx.x; item < items; item += gridDim.x) {
+    for (int item = blockIdx.x; item < items; item = norm_next(item, (int)gridDim.x, items)) {
         int g, r0, r1;
         item_rows(a, item, g, r0, r1);
         const float* gate = a.gate ? a.gate + (size_t)g * d : nullptr;
@@ -743,7 +749,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const NormArgs a
 #pragma unroll
             for (int k = 0; k < H / Q; ++k) C.put8(i_b, k, none);
         if constexpr (LN && !SM) pairs_zero(i_r);
-        for (int row0 = r0; row0 < r1; row0 += a.rows) {
+        for (int row0 = r0; row0 < r1; row0 = norm_next(row0, a.rows, r1)) {
             ok = ok && norm_rows_landed(sh, b, round);
             const int n = !ok ? 0 : r1 - row0 < a.rows ? r1 - row0 : a.rows;
             const uint32_t buf = smem_u32(norm_smem) + b * 4 * a.piece +
@@ -1127,7 +1133,7 @@ NormPlan norm_plan(bool bwd, bool ln, int T, int d, int elem, int rows_per_gate)
     // one CTA an SM, row groups of 512 threads in all; fewer where the rows do not go round,
     // but whole warps
     int n_grp = p.nl < kNormThreads ? kNormThreads / p.nl : 1;
-    const int least = p.nl < 32 ? 32 / p.nl : 1, share = (T + sms - 1) / sms;
+    const int least = p.nl < 32 ? 32 / p.nl : 1, share = (int)(((long long)T + sms - 1) / sms);
     while (n_grp / 2 >= least && n_grp / 2 >= share) n_grp /= 2;
     p.threads = n_grp * p.nl;
     const int n_in = bwd ? 4 : 2;
@@ -1160,7 +1166,7 @@ NormPlan norm_plan(bool bwd, bool ln, int T, int d, int elem, int rows_per_gate)
     p.slices = 1;
     if (p.groups > 0) {
         long long best = -1;
-        const int runs = rows > 0 ? (rows + n_grp - 1) / n_grp : 1;
+        const int runs = rows > 0 ? (int)(((long long)rows + n_grp - 1) / n_grp) : 1;
         for (int per = 1; per <= 8; ++per) {
             long long k = (long long)most * per / p.groups;
             k = k < 1 ? 1 : k < runs ? k : runs;

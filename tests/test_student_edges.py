@@ -186,3 +186,11 @@ def test_a_cluster_that_gives_up_waits_for_what_was_sent():
     """Parts that another CTA sent are counted by barriers that are no longer waited for."""
     body = dict(kernels(open(os.path.join(CSRC, "hcw_distill.cu")).read()))["distill_row_kernel"]
     assert re.search(r"cluster_sync_all\(\);\s+if \(\*abort\) settle_after_abort\(\);\s*\}$", body)
+
+
+def test_the_norms_count_rows_and_items_without_passing_an_int():
+    """Rows and items may number 2^31 - 1: a step past the end must not wrap."""
+    text = re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, "hcw_norm.cu")).read())
+    assert not re.search(r"\b(item|row0)\s*\+=", text)
+    assert len(re.findall(r"\b(?:item|row0) = norm_next\(", text)) == 5
+    assert "return step < end - i ? i + step : end;" in text

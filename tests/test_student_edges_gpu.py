@@ -184,3 +184,33 @@ def test_rows_in_another_order_are_refused(H):
         with pytest.raises(ValueError):
             H.hcw_distill_loss(z, **{**ok, **bad})
     assert H.hcw_sync_status() == H.HCW_OK
+
+
+@pytest.mark.parametrize("rows", [0, 1 << 30])
+def test_norms_of_as_many_rows_as_an_int_counts(H, rows):
+    T, last = 2 ** 31 - 1, 700
+    if torch.cuda.mem_get_info()[0] < 60e9:
+        pytest.skip("needs 60 GB on the device")
+    new = lambda: torch.empty(T, 1, dtype=BF16, device="cuda").normal_()  # noqa: E731
+    cut = lambda t: t[T - last:].clone()  # noqa: E731
+    r, f = new(), new()
+    gate = torch.rand(-(-T // rows) if rows else 1, 1, device="cuda")
+    one = dict(alpha=0.9, post=S.RMS, pre=S.RMS)
+    par = dict(gate=gate, rows_per_gate=rows, **one)
+    s, x = H.hcw_residual_norm_fwd(r, f, **par)
+    s1, x1 = H.hcw_residual_norm_fwd(cut(r), cut(f), gate=gate[-1:].clone(), **one)
+    assert torch.equal(cut(s), s1) and torch.equal(cut(x), x1)
+    got = H.hcw_residual_norm_bwd(r, x, s, f, **par)
+    part = H.hcw_residual_norm_bwd(cut(r), x1, s1, cut(f), gate=gate[-1:].clone(), **one)
+    assert torch.equal(cut(got["dr"]), part["dr"]) and torch.equal(cut(got["df"]), part["df"])
+    # the sums: dpre_w = sum x shat over blocks of rows in fp64, within 2^16 fp32 roundings (a
+    # thread adds up its CTA's rows one after the other, 2^31 / 152 / 64 of them and more)
+    want = size = 0.0
+    for i in range(0, T, 1 << 27):
+        b = slice(i, min(i + (1 << 27), T))
+        sd = s[b].double()
+        t = x[b].double() * sd * torch.rsqrt(sd * sd + 1e-5)
+        want, size = want + float(t.sum()), size + float(t.abs().sum())
+        del sd, t
+    assert abs(float(got["dpre_w"]) - want) <= 2.0 ** -24 * (2 ** 31 / 152 / 64) * size
+    assert H.hcw_sync_status() == H.HCW_OK
