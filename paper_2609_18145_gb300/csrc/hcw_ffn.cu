@@ -1054,6 +1054,9 @@ bool ffn_few(int T, int d, int h) {
     return T <= 16 ? work <= 1 << 28 : T <= kRowMax && work <= 1 << 27;
 }
 
+// row tiles of T rows (T up to 2^31 - 1)
+int ffn_row_tiles(int T) { return (int)(((long long)T + 255) / 256); }
+
 size_t ffn_round(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // a of a few tokens, and its remainders
@@ -1472,7 +1475,7 @@ int hcw_gated_ffn_fwd(const void* x, const void* W1, const void* W2, int T, int 
     p.N = h;
     p.bn = 256;
     p.nkb = (d + kFK - 1) / kFK;
-    p.mt = (T + 255) / 256;
+    p.mt = ffn_row_tiles(T);
     p.nt = (h + 127) / 128;
     a.n_prod = 1;
     a.n_units = p.mt * p.nt;
@@ -1532,7 +1535,7 @@ int hcw_gated_ffn_bwd(const void* x, const void* dy, const void* W1, const void*
         p.bn = i == 0 ? 128 : 256;
         p.b_mn = i == 0;
         p.nkb = (d + kFK - 1) / kFK;
-        p.mt = (T + 255) / 256;
+        p.mt = ffn_row_tiles(T);
         p.nt = (h + 127) / 128;
     }
     a.n_prod = 2;

@@ -194,3 +194,8 @@ def test_the_norms_count_rows_and_items_without_passing_an_int():
     assert not re.search(r"\b(item|row0)\s*\+=", text)
     assert len(re.findall(r"\b(?:item|row0) = norm_next\(", text)) == 5
     assert "return step < end - i ? i + step : end;" in text
+
+
+def test_the_feed_forward_block_counts_its_row_tiles_without_passing_an_int():
+    text = re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, "hcw_ffn.cu")).read())
+    assert "(T + 255)" not in text and "((long long)T + 255) / 256" in text

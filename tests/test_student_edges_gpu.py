@@ -214,3 +214,21 @@ def test_norms_of_as_many_rows_as_an_int_counts(H, rows):
         del sd, t
     assert abs(float(got["dpre_w"]) - want) <= 2.0 ** -24 * (2 ** 31 / 152 / 64) * size
     assert H.hcw_sync_status() == H.HCW_OK
+
+
+def test_a_feed_forward_block_of_as_many_rows_as_an_int_counts(H):
+    T, d, h, last = 2 ** 31 - 1, 8, 8, 999
+    if torch.cuda.mem_get_info()[0] < 215e9:
+        pytest.skip("needs 215 GB on the device")
+    _, _, W1, W2 = ffn_problem(1, d, h, 5)
+    x = torch.empty(T, d, dtype=BF16, device="cuda").normal_()
+    end = x[T - last:].clone()
+    y = H.hcw_gated_ffn_fwd(x, W1, W2)
+    assert torch.equal(y[T - last:], H.hcw_gated_ffn_fwd(end, W1, W2))
+    del y
+    dx, none, _ = H.hcw_gated_ffn_bwd(x, x, W1, W2, want_dw=False)
+    assert none is None
+    assert torch.equal(dx[T - last:], H.hcw_gated_ffn_bwd(end, end, W1, W2, want_dw=False)[0])
+    assert H.hcw_sync_status() == H.HCW_OK
+    del dx, x
+    torch.cuda.empty_cache()
