@@ -563,7 +563,8 @@ int hcw_gemm_bf16_batched(int M, int N, int K, const void* A, long long a_stride
  *       or HCW_GATE_RELU max(g, 0) (derivative 0 at 0)
  *   y   [T][d] output (no residual: hcw_residual_norm_fwd adds it)
  *   workspace  hcw_gated_ffn_fwd_workspace_bytes(...) bytes, contents need not be
- *       initialised (HCW_ERR_WORKSPACE when NULL or smaller).
+ *       initialised (HCW_ERR_WORKSPACE when NULL or smaller).  The bytes never fall with T: a
+ *       workspace for T rows does for fewer.
  * Products accumulate in fp32; g and u stay in fp32, a is rounded to bf16 once (it is the
  * second product's operand; for few tokens it may be kept in two bf16 parts), y once.
  * T >= 0 (0 does nothing), d and h multiples of 8 (HCW_ERR_UNSUPPORTED otherwise, and above
@@ -587,7 +588,7 @@ int hcw_gated_ffn_fwd(const void* x, const void* W1, const void* W2, int T, int 
  *       or HCW_F32 (to be accumulated further)
  *   dx = NULL: the weight gradients alone; dW1 = dW2 = NULL: dx alone (frozen weights).
  *       With T = 0 the weight gradients are zeros.
- *   workspace  hcw_gated_ffn_bwd_workspace_bytes(...) bytes.
+ *   workspace  hcw_gated_ffn_bwd_workspace_bytes(...) bytes, which never fall with T either.
  * dg, du and a are rounded to bf16 once, as the products' operands.  Partial sums of a
  * split sum over the tokens are added in a fixed order: the same inputs give the same
  * bits.  Requirements and errors as for the forward.

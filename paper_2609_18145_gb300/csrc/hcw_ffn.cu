@@ -1059,8 +1059,11 @@ int ffn_row_tiles(int T) { return (int)(((long long)T + 255) / 256); }
 
 size_t ffn_round(size_t n) { return (n + 255) & ~(size_t)255; }
 
-// a of a few tokens, and its remainders
-size_t ffn_rows_ws(int T, int h) { return ffn_round((size_t)(T <= kRowLo ? 2 * T : T) * h * 2); }
+// a of up to T tokens: its rows and, up to kRowLo tokens, those of the remainders
+size_t ffn_rows_ws_up_to(int T, int h) {
+    const size_t two = T < kRowLo ? 2 * T : 2 * kRowLo, rows = (size_t)T > two ? (size_t)T : two;
+    return ffn_round(rows * h * 2);
+}
 
 // The forward of a few tokens: two launches.
 int ffn_rows_fwd(const void* x, const void* W1, const void* W2, int T, int d, int h, int act,
@@ -1247,6 +1250,23 @@ void ffn_plan(FfnPlan& best, int pairs) {
 // The parts' slots.
 size_t ffn_part_bytes(const FfnPlan& p) { return (size_t)p.slots * kFSlot * sizeof(float); }
 
+// The most slots of any plan of these products and of ones with smaller M and K (a workspace for
+// the longest batch then does for every shorter one, whose tiles may be cut where the longest's
+// are not).  On the line lie at most pairs - 1 tiles of a product; a slot is a place on the line
+// plus a share, and there are at most kFCuts shares, each with kFLeast steps of a tile at least
+// or the tile itself.
+size_t ffn_part_bytes_up_to(const FfnShape* s, int n, int pairs) {
+    long long line = 0, shares = 0;
+    for (int i = 0; i < n; ++i) {
+        const long long bn = s[i].N <= 128 ? 128 : 256, nkb = (s[i].K + kFK - 1) / kFK;
+        const long long tiles = ((s[i].M + 255) / 256) * ((s[i].N + bn - 1) / bn);
+        const long long left = tiles < pairs - 1 ? tiles : pairs - 1;
+        line += left;
+        shares += left * (nkb < 2 * kFLeast ? 1 : nkb / kFLeast);
+    }
+    return (size_t)(line + (shares < kFCuts ? shares : kFCuts)) * kFSlot * sizeof(float);
+}
+
 // Units of the gradient pass: 256 hidden columns, whose da runs at the rate of 256-column
 // products (of 128 columns a K step takes 0.75 of that time, not half), and 128 columns for odd
 // ends.  The last round's units are cut in two where that shortens the busiest pair's share.
@@ -1371,25 +1391,45 @@ const FfnPlan& ffn_down_plan(int T, int d, int h) {
     return ffn_planned(&s, 1, device_sms() / 2);
 }
 
+size_t ffn_fwd_ws_bytes(int T, int d, int h) {
+    const size_t rows = ffn_rows_ws_up_to(T, h);
+    if (ffn_few(T, d, h)) return rows;   // and so are fewer tokens
+    const FfnShape s = {T, d, h};
+    return rows + ffn_part_bytes_up_to(&s, 1, device_sms() / 2);
+}
+
+// Backward workspace: [dg | du] [T][2h] and a [T][h] bf16, then the parts of dx, dW1 and dW2.
 struct FfnBwdWs {
     size_t act, part, bytes;   // dgu at 0
     const FfnPlan* plan;       // until the thread's next plan
 };
 
-FfnBwdWs ffn_bwd_ws(int T, int d, int h, bool dx, bool dw, bool f32) {
-    FfnBwdWs w;
-    FfnShape s[3] = {};
+int ffn_bwd_shapes(FfnShape (&s)[3], int T, int d, int h, bool dx, bool dw, bool f32) {
     int n = 0;
     if (dx) s[n++] = {T, d, 2ll * h};
     if (dw) {
         s[n++] = {2ll * h, d, T, f32};
         s[n++] = {d, h, T, f32};
     }
+    return n;
+}
+
+FfnBwdWs ffn_bwd_ws(int T, int d, int h, bool dx, bool dw, bool f32) {
+    FfnBwdWs w;
+    FfnShape s[3] = {};
+    const int n = ffn_bwd_shapes(s, T, d, h, dx, dw, f32);
     w.plan = &ffn_planned(s, n, device_sms() / 2);
     w.act = ffn_round((size_t)T * 2 * h * 2);
     w.part = w.act + ffn_round((size_t)T * h * 2);
     w.bytes = w.part + ffn_part_bytes(*w.plan);
     return w;
+}
+
+size_t ffn_bwd_ws_bytes(int T, int d, int h) {
+    FfnShape s[3] = {};
+    const int n = ffn_bwd_shapes(s, T, d, h, true, true, false);
+    return ffn_round((size_t)T * 2 * h * 2) + ffn_round((size_t)T * h * 2) +
+           ffn_part_bytes_up_to(s, n, device_sms() / 2);
 }
 
 bool ffn_aligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -1443,9 +1483,7 @@ using namespace hcw;
 extern "C" {
 
 size_t hcw_gated_ffn_fwd_workspace_bytes(int T, int d, int h) {
-    if (T < 1 || ffn_sizes(T, d, h, HCW_GATE_SILU)) return 0;
-    if (ffn_few(T, d, h)) return ffn_rows_ws(T, h);
-    return ffn_round((size_t)T * h * 2) + ffn_part_bytes(ffn_down_plan(T, d, h));
+    return T < 1 || ffn_sizes(T, d, h, HCW_GATE_SILU) ? 0 : ffn_fwd_ws_bytes(T, d, h);
 }
 
 int hcw_gated_ffn_fwd(const void* x, const void* W1, const void* W2, int T, int d, int h, int act,
@@ -1459,14 +1497,12 @@ int hcw_gated_ffn_fwd(const void* x, const void* W1, const void* W2, int T, int 
     if (rc) return rc;
     if (T == 0) return HCW_OK;
     if (!x || !W1 || !W2 || !y) return HCW_ERR_INVALID_ARG;
+    if (!workspace || ws_bytes < ffn_fwd_ws_bytes(T, d, h)) return HCW_ERR_WORKSPACE;
     const size_t act_bytes = ffn_round((size_t)T * h * 2);
     const cudaStream_t st = (cudaStream_t)stream;
-    if (ffn_few(T, d, h)) {
-        if (!workspace || ws_bytes < ffn_rows_ws(T, h)) return HCW_ERR_WORKSPACE;
-        return ffn_rows_fwd(x, W1, W2, T, d, h, act, y, workspace, st);
-    }
+    if (ffn_few(T, d, h)) return ffn_rows_fwd(x, W1, W2, T, d, h, act, y, workspace, st);
     const FfnPlan& plan = ffn_down_plan(T, d, h);
-    if (!workspace || ws_bytes < act_bytes + ffn_part_bytes(plan)) return HCW_ERR_WORKSPACE;
+    if (ws_bytes < act_bytes + ffn_part_bytes(plan)) return HCW_ERR_WORKSPACE;
     const int pairs = device_sms() / 2;
     FfnArgs a;
     memset(&a, 0, sizeof(a));
@@ -1491,14 +1527,7 @@ int hcw_gated_ffn_fwd(const void* x, const void* W1, const void* W2, int T, int 
 }
 
 size_t hcw_gated_ffn_bwd_workspace_bytes(int T, int d, int h) {
-    if (T < 1 || ffn_sizes(T, d, h, HCW_GATE_SILU)) return 0;
-    size_t most = 0;
-    // whichever outputs a call asks for
-    for (int k = 1; k < 4; ++k) {
-        const size_t b = ffn_bwd_ws(T, d, h, k & 1, k & 2, false).bytes;
-        most = b > most ? b : most;
-    }
-    return most;
+    return T < 1 || ffn_sizes(T, d, h, HCW_GATE_SILU) ? 0 : ffn_bwd_ws_bytes(T, d, h);
 }
 
 int hcw_gated_ffn_bwd(const void* x, const void* dy, const void* W1, const void* W2, int T, int d,
@@ -1523,7 +1552,8 @@ int hcw_gated_ffn_bwd(const void* x, const void* dy, const void* W1, const void*
     }
     if (!x || !dy || !W1 || !W2 || (!dx && !dW1)) return HCW_ERR_INVALID_ARG;
     const FfnBwdWs w = ffn_bwd_ws(T, d, h, dx != nullptr, dW1 != nullptr, f32);
-    if (!workspace || ws_bytes < w.bytes) return HCW_ERR_WORKSPACE;
+    if (!workspace || ws_bytes < ffn_bwd_ws_bytes(T, d, h) || ws_bytes < w.bytes)
+        return HCW_ERR_WORKSPACE;
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     const int pairs = device_sms() / 2;
     FfnArgs a;

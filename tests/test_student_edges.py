@@ -199,3 +199,13 @@ def test_the_norms_count_rows_and_items_without_passing_an_int():
 def test_the_feed_forward_block_counts_its_row_tiles_without_passing_an_int():
     text = re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, "hcw_ffn.cu")).read())
     assert "(T + 255)" not in text and "((long long)T + 255) / 256" in text
+
+
+@pytest.mark.parametrize("d,h", [(64, 72), (512, 1024), (1024, 2744), (2048, 5632), (4096, 14336)])
+def test_a_feed_forward_workspace_does_for_fewer_tokens(H, d, h):
+    for size in (H.hcw_gated_ffn_fwd_workspace_bytes, H.hcw_gated_ffn_bwd_workspace_bytes):
+        last = 0
+        for T in [*range(1, 700), *range(700, 20000, 97)]:
+            need = size(T, d, h)
+            assert need >= last, (T, need, last)
+            last = need
