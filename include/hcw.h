@@ -640,7 +640,8 @@ int hcw_residual_norm_fwd(const void* r, const void* f, const float* gate, int r
  *            not there has no gradients, RMS no bias gradient (HCW_ERR_INVALID_ARG).  With
  *            T = 0 the parameter gradients are zeros.
  *   workspace  hcw_residual_norm_bwd_workspace_bytes(...) bytes for the parameter gradients'
- *            partial sums; not needed without them.
+ *            partial sums; not needed without them.  The bytes never fall with T: a workspace
+ *            for T rows does for fewer.
  * The sums over the rows have a fixed order: the same inputs give the same bits.
  */
 size_t hcw_residual_norm_bwd_workspace_bytes(int T, int d, int rows_per_gate);

@@ -1117,6 +1117,8 @@ int norm_groups(int T, int rows_per_gate) {
     return rows_per_gate > 0 ? (int)(((long long)T + rows_per_gate - 1) / rows_per_gate) : 1;
 }
 
+constexpr int kNormPerCta = 8;   // items a CTA takes of groups that are cut, at most
+
 // rows a row group works on at once in the forward, and in the backward with 8 columns a thread
 constexpr int kNormRows = 2;
 
@@ -1167,7 +1169,7 @@ NormPlan norm_plan(bool bwd, bool ln, int T, int d, int elem, int rows_per_gate)
     if (p.groups > 0) {
         long long best = -1;
         const int runs = rows > 0 ? (int)(((long long)rows + n_grp - 1) / n_grp) : 1;
-        for (int per = 1; per <= 8; ++per) {
+        for (int per = 1; per <= kNormPerCta; ++per) {
             long long k = (long long)most * per / p.groups;
             k = k < 1 ? 1 : k < runs ? k : runs;
             const long long busiest = (p.groups * k + most - 1) / most;
@@ -1290,6 +1292,18 @@ NormWs norm_ws(const NormPlan& p, int d) {
     return w;
 }
 
+// The most of that for up to T rows (a workspace for the longest batch does for every shorter
+// one, whose groups may be cut where the longest's are not): a partial row a CTA, of which
+// there are no more than SMs or than items, and no more items than the groups have rows; and a
+// row for every item of groups that are cut, of which each CTA takes kNormPerCta.
+size_t norm_ws_up_to(int T, int d, int rows_per_gate) {
+    const int rows = rows_per_gate > 0 && rows_per_gate < T ? rows_per_gate : T;
+    const long long all = (long long)norm_groups(T, rows_per_gate) * rows, sms = device_sms();
+    const long long ctas = all < sms ? all : sms, most = sms * kNormPerCta;
+    return round256((size_t)ctas * kNormPar * d * sizeof(float)) +
+           (rows > 1 ? round256((size_t)(all < most ? all : most) * d * sizeof(float)) : 0);
+}
+
 }  // namespace
 
 cudaError_t norm_error_word_read_clear(int* word) {
@@ -1354,7 +1368,7 @@ int hcw_selftest_norm_starve(int fetches) { return g_starve.exchange(fetches > 0
 
 size_t hcw_residual_norm_bwd_workspace_bytes(int T, int d, int rows_per_gate) {
     if (T < 1 || d < 1 || d > kNormMaxD || rows_per_gate < 0) return 0;
-    return norm_ws(norm_plan(true, false, T, d, 2, rows_per_gate), d).bytes;
+    return norm_ws_up_to(T, d, rows_per_gate);
 }
 
 int hcw_residual_norm_bwd(const void* dr_out, const void* dx_out, const void* s, const void* f,
@@ -1392,7 +1406,8 @@ int hcw_residual_norm_bwd(const void* dr_out, const void* dx_out, const void* s,
     const bool ws_needed = T > 0 && (params || (dgate && p.slices > 1));
     if (ws_needed) {
         w = norm_ws(p, d);
-        if (!workspace || ws_bytes < w.bytes) return HCW_ERR_WORKSPACE;
+        if (!workspace || ws_bytes < norm_ws_up_to(T, d, rows_per_gate) || ws_bytes < w.bytes)
+            return HCW_ERR_WORKSPACE;
     }
     float* part = static_cast<float*>(workspace);
     float* gpart = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + w.gpart);

@@ -209,3 +209,13 @@ def test_a_feed_forward_workspace_does_for_fewer_tokens(H, d, h):
             need = size(T, d, h)
             assert need >= last, (T, need, last)
             last = need
+
+
+@pytest.mark.parametrize("d", [1, 64, 512, 4097, 8192])
+@pytest.mark.parametrize("rows", [0, 1, 2, 7, 64, 256, 5000])
+def test_a_norm_workspace_does_for_fewer_rows(H, d, rows):
+    last = 0
+    for T in [*range(1, 700), *range(700, 40000, 97)]:
+        need = H.hcw_residual_norm_bwd_workspace_bytes(T, d, rows)
+        assert need >= last, (T, need, last)
+        last = need
