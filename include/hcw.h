@@ -566,7 +566,9 @@ int hcw_gemm_bf16_batched(int M, int N, int K, const void* A, long long a_stride
  *       initialised (HCW_ERR_WORKSPACE when NULL or smaller).  The bytes never fall with T: a
  *       workspace for T rows does for fewer.
  * Products accumulate in fp32; g and u stay in fp32, a is rounded to bf16 once (it is the
- * second product's operand; for few tokens it may be kept in two bf16 parts), y once.
+ * second product's operand), y once.  Up to 8 tokens, while T d h <= 2^28, a is kept in two bf16
+ * parts, 16 bits together, so that y is off by its own rounding alone: a token's y may then change
+ * by a little more than that rounding when a ninth one joins the batch.
  * T >= 0 (0 does nothing), d and h multiples of 8 (HCW_ERR_UNSUPPORTED otherwise, and above
  * 2^20); pointers are 16-byte aligned; an output or the workspace over an input is
  * HCW_ERR_ALIASING.  The same inputs give the same bits.

@@ -665,9 +665,10 @@ __device__ __forceinline__ void group_sum(const C& cols, const uint64_t (&v)[H],
 // SM: with LayerNorms, the sums of dx and ds in shared memory (16 columns' sums have no room in
 // the registers; without SM they are there all the same, for rows whose ring leaves no room
 // either).
-// bf16, with the second launch, us and TB/s: 32768 x 4096 RMS 317, 5.1, LayerNorms 432, 3.7;
-// 65536 x 1024 RMS 143, 5.6; 16384 x 512 RMS 27, 3.7, LayerNorms 36, 2.8: the LayerNorms by the
-// issue of their instructions (0.47 a cycle with the 16 warps that the registers allow).
+// bf16, with the second launch, us and TB/s: 32768 x 4096 RMS 324, 5.0, LayerNorms 432, 3.7;
+// 65536 x 1024 RMS 148, 5.4; 16384 x 512 RMS 27, 3.7, LayerNorms 34, 3.0: bound by waiting at
+// the barriers of the sums, two in sequence (LayerNorms: three) for the 16 warps that the
+// registers allow; under half of the issue slots are used (0.47 a cycle).
 template <typename T, int VW, bool LN, bool SM, int E, int R>
 __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const NormArgs a) {
     extern __shared__ __align__(128) uint8_t norm_smem[];

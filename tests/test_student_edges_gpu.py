@@ -189,6 +189,7 @@ def test_rows_in_another_order_are_refused(H):
 @pytest.mark.parametrize("rows", [0, 1 << 30])
 def test_norms_of_as_many_rows_as_an_int_counts(H, rows):
     T, last = 2 ** 31 - 1, 700
+    torch.cuda.empty_cache()
     if torch.cuda.mem_get_info()[0] < 60e9:
         pytest.skip("needs 60 GB on the device")
     new = lambda: torch.empty(T, 1, dtype=BF16, device="cuda").normal_()  # noqa: E731
@@ -218,6 +219,7 @@ def test_norms_of_as_many_rows_as_an_int_counts(H, rows):
 
 def test_a_feed_forward_block_of_as_many_rows_as_an_int_counts(H):
     T, d, h, last = 2 ** 31 - 1, 8, 8, 999
+    torch.cuda.empty_cache()
     if torch.cuda.mem_get_info()[0] < 215e9:
         pytest.skip("needs 215 GB on the device")
     _, _, W1, W2 = ffn_problem(1, d, h, 5)
@@ -232,3 +234,18 @@ def test_a_feed_forward_block_of_as_many_rows_as_an_int_counts(H):
     assert H.hcw_sync_status() == H.HCW_OK
     del dx, x
     torch.cuda.empty_cache()
+
+
+def test_the_example_learns_with_the_stacks_usual_activation(monkeypatch):
+    """The step's gradients are held to fp64 without a ReLU (whose decisions near 0 differ); with it
+    the same calls have to bring the loss down clearly."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples",
+                        "student.py")
+    spec = importlib.util.spec_from_file_location("student_relu", path)
+    student = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(student)
+    monkeypatch.setattr(student, "FLAGS", student.H.HCW_CAUSAL | student.H.HCW_ACT_RELU)
+    losses = student.train(steps=60, say=None)
+    assert all(v == v for v in losses) and sum(losses[-5:]) / 5 < 0.8 * losses[0]
