@@ -666,9 +666,9 @@ __device__ __forceinline__ void group_sum(const C& cols, const uint64_t (&v)[H],
 // the registers; without SM they are there all the same, for rows whose ring leaves no room
 // either).
 // bf16, with the second launch, us and TB/s: 32768 x 4096 RMS 324, 5.0, LayerNorms 432, 3.7;
-// 65536 x 1024 RMS 148, 5.4; 16384 x 512 RMS 27, 3.7, LayerNorms 34, 3.0: bound by waiting at
-// the barriers of the sums, two in sequence (LayerNorms: three) for the 16 warps that the
-// registers allow; under half of the issue slots are used (0.47 a cycle).
+// 65536 x 1024 RMS 148, 5.4; 16384 x 512 RMS 27, 3.7, LayerNorms 34, 3.0: bound by waiting, at
+// the barriers of the sums, two in sequence (LayerNorms: three), and for shared memory, with the
+// 16 warps that the registers allow; about half of the issue slots are used (0.45 to 0.51 a cycle).
 template <typename T, int VW, bool LN, bool SM, int E, int R>
 __global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const NormArgs a) {
     extern __shared__ __align__(128) uint8_t norm_smem[];
