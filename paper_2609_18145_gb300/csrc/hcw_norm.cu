@@ -520,7 +520,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_fwd_kernel(const NormArgs a
         // a vector a row group: their loads wait side by side
         for (int k = n_grp - 1 - grp; k < (fresh ? 4 : 2); k += n_grp) {
             if (k == 0) C.fill(gw, a.post_w, gate, 1.f);
-            if (LN && k == 1) C.fill(gb, a.post_b, gate, 0.f);
+            if (LN && k == 1) C.fill(gb, a.post_b, a.post_b ? gate : nullptr, 0.f);
             if (k == 2) C.fill(pw, a.pre_w, nullptr, 1.f);
             if (LN && k == 3) C.fill(pb, a.pre_b, nullptr, 0.f);
         }

@@ -249,3 +249,13 @@ def test_the_example_learns_with_the_stacks_usual_activation(monkeypatch):
     monkeypatch.setattr(student, "FLAGS", student.H.HCW_CAUSAL | student.H.HCW_ACT_RELU)
     losses = student.train(steps=60, say=None)
     assert all(v == v for v in losses) and sum(losses[-5:]) / 5 < 0.8 * losses[0]
+
+
+@pytest.mark.parametrize("post", [S.NONE, S.RMS, S.LAYER])
+def test_an_infinite_gate_gives_infinities(H, post):
+    """gate v alone: no bias that is not there times the gate."""
+    p = Problem(9, 264, F32, 3)
+    p.gate[0, 5] = float("inf")
+    s, _ = H.hcw_residual_norm_fwd(p.r, p.f, p.gate, alpha=0.5, post=post, post_w=p.post_w,
+                                   pre=S.LAYER)
+    assert s[:, 5].isinf().all() and not s.isnan().any()
