@@ -682,6 +682,111 @@ int hcw_distill_loss(const void* z, const int* idx, const float* teacher, const 
                      const float* weight, int T, int V, int K, int dtype, float temperature,
                      float kl_scale, float ce_scale, float* loss, void* dz, void* stream);
 
+/*
+ * Lookup of symbols: x_t = scale E[id_t].
+ *   ids   [T] int32;  a negative id is padding: its row of x is zeros
+ *   E     [V][d] (dtype);  x [T][d] (dtype) output, rounded once
+ * An id >= V counts as padding and is reported by hcw_sync_status as HCW_ERR_INVALID_ARG.
+ * Any T >= 0 up to 2^28 (0 does nothing), V up to 2^23, d up to 2^20 (HCW_ERR_UNSUPPORTED above;
+ * d needs no multiple: rows of 16-byte pieces are the faster ones); scale is finite; pointers are
+ * 16-byte aligned; x over an input is HCW_ERR_ALIASING.  One launch, no workspace.
+ */
+int hcw_embed_fwd(const int* ids, const void* E, int T, int V, int d, int dtype, float scale, void* x,
+                  void* stream);
+
+/*
+ * Its gradient: dE_v = scale * sum over {t: id_t = v} of dx_t.
+ *   dx    [T][d] (dtype);  dE [V][d] in de_dtype (HCW_BF16 or HCW_F32)
+ *   accumulate  0: every row of dE is written, zeros where no token names the symbol;
+ *         1: the sums are added to what dE holds (the gradient of a head that shares the table),
+ *         rows that no token names are neither read nor written.
+ *   workspace  hcw_embed_bwd_workspace_bytes(...) bytes (on the device in use), contents need not
+ *         be initialised; the bytes never fall with T.
+ * Padding and ids >= V as for the lookup: they have no part in any sum.  Sums are fp32, rounded
+ * once, in an order that depends on the ids and sizes alone: the same inputs give the same bits.
+ * With T = 0 dE is zeros, or stays as it is.  Sizes, alignment and errors as for the lookup.
+ */
+size_t hcw_embed_bwd_workspace_bytes(int T, int V, int d);
+int hcw_embed_bwd(const int* ids, const void* dx, int T, int V, int d, int dtype, float scale,
+                  int accumulate, int de_dtype, void* dE, void* workspace, size_t ws_bytes,
+                  void* stream);
+
+/*
+ * The norm over the gradients of all parameters, and clipping by it:
+ *   n = sqrt(sum over tensors i, elements j of g_ij^2);  c = n > max_norm ? max_norm / n : 1;
+ *   out_ij = c g_ij, rounded once
+ *   grads, out   host arrays of `count` device pointers, read during the call; out = NULL: in
+ *                place.  Contiguous tensors, aligned to their elements (16 bytes where speed counts).
+ *   sizes, dtypes  host arrays: elements (0 is allowed, the pointer is then not looked at) and
+ *                HCW_BF16 or HCW_F32 of each tensor.
+ *   max_norm     >= 0; infinity: nothing is clipped (in place only the norm is taken).
+ *   norm         [2] fp32 on the device, written: n and c.
+ *   workspace    hcw_clip_grads_workspace_bytes(count) bytes, contents need not be initialised.
+ * Any finite gradients have their norm (squares that leave fp32's range are scaled); beyond fp32's
+ * largest number norm[0] is infinite while c still is max_norm / n.  Where an element is infinite or
+ * NaN so is norm[0], and c = 1: the gradients stay as they are, for the caller to skip the step.
+ * In place with c = 1 nothing is written.  Sums above 32 squares are fp64, in a fixed order: the
+ * same inputs give the same bits.  An output or the workspace that overlaps another tensor (in
+ * place: two tensors that share memory) is HCW_ERR_ALIASING.  Two launches for up to 512 tensors.
+ */
+size_t hcw_clip_grads_workspace_bytes(int count);
+int hcw_clip_grads(const void* const* grads, void* const* out, const long long* sizes,
+                   const int* dtypes, int count, float max_norm, float* norm, void* workspace,
+                   size_t ws_bytes, void* stream);
+
+/*
+ * Products of a few tokens with weights of 4 bits, one scale for each `group` of neighbours in a
+ * row (32, 64 or 128; the last group of a row may be shorter):
+ *   y_to = sum over k of x_tk w_ok (+ b_o),   w_ok = scales[o][k / group] codes[o][k]
+ *   codes   [N][K] int8, -8 .. 7;  scales [N][ceil(K / group)] bf16
+ *   packed  hcw_q4_bytes(N, K, group) bytes: the same weights as hcw_q4_matmul reads them
+ *   x [T][K] bf16;  bias [N] fp32 or NULL;  y [T][N] in y_dtype (HCW_BF16 or HCW_F32)
+ * hcw_q4_quantize makes codes and scales from finite W [N][K] (dtype): s = max |w| / 7 over the
+ * group, rounded to bf16; code = w / s to the nearest integer, ties to even, within -8 .. 7 (0
+ * where s is 0).  hcw_q4_pack lays codes and scales from there or elsewhere out; of a code only the
+ * low four bits count.  Sums and scales are fp32, y is rounded once; a token's y does not
+ * depend on the other tokens of the call, and the same inputs give the same bits.  Made for up to 16
+ * tokens, which read the weights once; more read them again for every 16.
+ * T >= 0 up to 2^19 (0 does nothing), N up to 2^24, K a multiple of 8 up to 2^20
+ * (HCW_ERR_UNSUPPORTED otherwise); pointers are 16-byte aligned; an output over an input is
+ * HCW_ERR_ALIASING.  One launch each, no workspace.
+ */
+size_t hcw_q4_bytes(int N, int K, int group);
+int hcw_q4_quantize(const void* W, int N, int K, int group, int dtype, signed char* codes,
+                    void* scales, void* stream);
+int hcw_q4_pack(const signed char* codes, const void* scales, int N, int K, int group, void* packed,
+                void* stream);
+int hcw_q4_matmul(const void* x, const void* packed, const float* bias, int T, int N, int K, int group,
+                  int y_dtype, void* y, void* stream);
+
+/*
+ * Edits of a batch's logits before a symbol is drawn.  For symbol j of row b, n_j its occurrences
+ * in history[b] from prompt[b] on and s_j whether it occurs in history[b] at all:
+ *   z'  = s_j ? (z > 0 ? z / repetition[b] : z repetition[b]) : z
+ *   z'' = z' - frequency[b] n_j - (n_j > 0 ? presence[b] : 0) + sum of bias[b][k] with bias_idx[b][k] = j
+ *   out = bit j of mask[b] set ? z'' : -inf
+ *   z, out   [B][V] (dtype); out = z edits in place
+ *   history  [B][H] int32, or NULL with H = 0: prompt and own symbols of each row, the first
+ *            lengths[b] of them (NULL: H; taken to 0 .. H); negative entries are empty
+ *   prompt   [B] int32 or NULL (0): where the row's own symbols begin
+ *   repetition, frequency, presence  [B] fp32 or NULL (1, 0, 0)
+ *   bias_idx, bias  [B][M] int32 and fp32, or NULL with M = 0; a negative symbol is an empty slot,
+ *            one that occurs in several slots gets their sum
+ *   mask     [B][ceil(V / 32)] words or NULL: bit j % 32 of word j / 32 lets symbol j through.  A
+ *            row that lets nothing through is -inf throughout.
+ * Products and sums are fp32 (past its largest number: infinite), each output is rounded once; a
+ * symbol without edits keeps its bits;
+ * what the mask takes out is -inf whatever it was, NaN included.  A symbol >= V in the history or a
+ * slot counts as empty and is reported by hcw_sync_status as HCW_ERR_INVALID_ARG.  The same inputs
+ * give the same bits.  B >= 0 up to 2^20 (0 does nothing), V up to 2^24, H up to 2^28, M up to
+ * 1024, B V up to 2^40 (HCW_ERR_UNSUPPORTED above); pointers are 16-byte aligned; out over an input, or
+ * over z other than in place, is HCW_ERR_ALIASING.  One launch, no workspace.
+ */
+int hcw_logits_edit(const void* z, int B, int V, int dtype, const int* history, const int* lengths,
+                    const int* prompt, int H, const float* repetition, const float* frequency,
+                    const float* presence, const int* bias_idx, const float* bias, int M,
+                    const unsigned* mask, void* out, void* stream);
+
 /* Number of kernels this library has launched in this process (all devices). */
 unsigned long long hcw_launch_count(void);
 

@@ -21,7 +21,8 @@ LIB = os.path.join(PKG, "libhcw.so")
 BUILD_DIR = os.path.join(PKG, "_build")
 
 SOURCES = ["hcw_api.cu", "hcw_tc.cu", "hcw_res.cu", "hcw_small.cu", "hcw_simt.cu", "hcw_decode.cu",
-           "hcw_block.cu", "hcw_gemm.cu", "hcw_ffn.cu", "hcw_norm.cu", "hcw_distill.cu"]
+           "hcw_block.cu", "hcw_gemm.cu", "hcw_ffn.cu", "hcw_norm.cu", "hcw_distill.cu",
+           "hcw_embed.cu", "hcw_clip.cu", "hcw_q4.cu", "hcw_logits.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-O2",
               "--expt-relaxed-constexpr", "-I", INCLUDE, "-I", CSRC]

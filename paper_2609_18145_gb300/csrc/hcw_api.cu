@@ -2609,7 +2609,7 @@ unsigned long long hcw_launch_count(void) { return g_launches.load(); }
 int hcw_sync_status(void* stream) {
     if (cudaStreamSynchronize((cudaStream_t)stream) != cudaSuccess) return HCW_ERR_CUDA;
     int word = 0, word_res = 0, word_dec = 0, word_blk = 0, word_gemm = 0, word_small = 0,
-        word_dst = 0, word_ffn = 0, word_norm = 0;
+        word_dst = 0, word_ffn = 0, word_norm = 0, word_emb = 0, word_log = 0;
     if (error_word_read_clear(&word) != cudaSuccess ||
         small_error_word_read_clear(&word_small) != cudaSuccess ||
         res_error_word_read_clear(&word_res) != cudaSuccess ||
@@ -2618,7 +2618,9 @@ int hcw_sync_status(void* stream) {
         gemm_error_word_read_clear(&word_gemm) != cudaSuccess ||
         ffn_error_word_read_clear(&word_ffn) != cudaSuccess ||
         norm_error_word_read_clear(&word_norm) != cudaSuccess ||
-        distill_error_word_read_clear(&word_dst) != cudaSuccess)
+        distill_error_word_read_clear(&word_dst) != cudaSuccess ||
+        embed_error_word_read_clear(&word_emb) != cudaSuccess ||
+        logits_error_word_read_clear(&word_log) != cudaSuccess)
         return HCW_ERR_CUDA;
     if (!word) word = word_res;
     if (!word) word = word_dec;
@@ -2628,6 +2630,8 @@ int hcw_sync_status(void* stream) {
     if (!word) word = word_ffn;
     if (!word) word = word_norm;
     if (!word) word = word_dst;
+    if (!word) word = word_emb;
+    if (!word) word = word_log;
     if (word == HCW_ERR_INVALID_ARG) return HCW_ERR_INVALID_ARG;
     if (word) return word == HCW_ERR_TIMEOUT ? HCW_ERR_TIMEOUT : HCW_ERR_CUDA;
     return HCW_OK;

@@ -1,0 +1,417 @@
+// hcw_clip.cu -- the norm over the gradients of all parameters, and clipping by it
+// (hcw_clip_grads):
+//
+//   n = sqrt(sum over tensors i and elements j of g_ij^2),  c = min(1, max_norm / n),
+//   out_ij = c g_ij
+//
+// Bound by memory: every element is read for the norm and, as the factor is not known before
+// the last of them, read again and written for the product.  Two launches for up to 512 tensors,
+// whatever their sizes: each tensor is cut into chunks, the chunks of all tensors are numbered
+// through, and the CTAs take them in turn.  The second launch goes through them backwards, so that
+// what the first one read last is found in L2.
+//
+// The squares of a thread's elements of one chunk (32 of them) are added in fp32, everything above
+// in fp64.  Squares of fp32 or bf16 gradients may leave fp32's range: a thread whose sum did, or
+// lies where squares lose their last bits, takes its elements again with a power of two before
+// them, so the norm is right to a few parts in 2^24 for any finite gradients.
+#include "hcw.h"
+#include "hcw_internal.h"
+
+#include <math.h>
+
+#include <algorithm>
+#include <new>
+
+namespace hcw {
+
+namespace {
+
+constexpr int kCThreads = 512;
+constexpr int kCPer = 32;                        // elements of a chunk for a thread
+constexpr int kCChunk = kCThreads * kCPer;
+constexpr int kCParts = 1024;                    // CTAs of a launch at most
+constexpr int kCTensors = 512;                   // tensors of a launch at most
+constexpr long long kCMaxChunks = 1ll << 30;     // of a launch
+
+struct ClipTensor {
+    const void* g;
+    void* out;
+    long long n;
+};
+
+// The tensors of a launch, passed by value: 32 of them or 512.
+template <int N>
+struct ClipArgs {
+    ClipTensor t[N];
+    int first[N + 1];        // the tensor's first chunk; first[count]: chunks in all
+    unsigned char f32[N];
+    int count;
+    double* parts;           // sums of squares, one of each CTA
+    int n_parts;             // of all launches (second kernel)
+    float max_norm;
+    float* norm;             // null: another launch writes it
+    int in_place;
+};
+
+// Elements before p's first 16-byte boundary (as many as the tensor has, at most).
+__device__ __forceinline__ int head_of(const void* p, int es, long long n) {
+    const int h = (int)((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / es;
+    return h < n ? h : (int)n;
+}
+
+// The chunk's tensor: the last one whose first chunk is not past it.
+template <int N>
+__device__ __forceinline__ int tensor_of(const ClipArgs<N>& a, int chunk) {
+    int lo = 0, hi = a.count - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (a.first[mid] <= chunk)
+            lo = mid;
+        else
+            hi = mid - 1;
+    }
+    return lo;
+}
+
+template <typename T>
+struct Vec {   // 16 bytes of T
+    static constexpr int n = 16 / sizeof(T);
+};
+
+__device__ __forceinline__ void unpack(const uint4& q, float (&v)[4]) {
+    v[0] = __uint_as_float(q.x);
+    v[1] = __uint_as_float(q.y);
+    v[2] = __uint_as_float(q.z);
+    v[3] = __uint_as_float(q.w);
+}
+__device__ __forceinline__ void unpack(const uint4& q, float (&v)[8]) {
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __uint_as_float(w[i] << 16);
+        v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ float value(const float* p) { return *p; }
+__device__ __forceinline__ float value(const __nv_bfloat16* p) { return __bfloat162float(*p); }
+__device__ __forceinline__ void put(float* p, float v) { *p = v; }
+__device__ __forceinline__ void put(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
+
+// The thread's share of the elements [lo, hi) of g, whose vectors start at its element `head`:
+// the sum of (f g)^2, and in *any whether one of them is not zero.
+template <typename T>
+__device__ __forceinline__ float squares(const T* g, long long lo, long long hi, float f, bool* any) {
+    constexpr int VE = Vec<T>::n, NV = kCPer / VE;
+    float s0 = 0.f, s1 = 0.f;
+    uint32_t bits = 0;
+    const long long vecs = (hi - lo) / VE;   // lo is on a boundary
+    uint4 q[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const long long k = threadIdx.x + (long long)i * kCThreads;
+        q[i] = k < vecs ? reinterpret_cast<const uint4*>(g + lo)[k] : make_uint4(0, 0, 0, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        float v[VE];
+        unpack(q[i], v);
+        bits |= q[i].x | q[i].y | q[i].z | q[i].w;
+#pragma unroll
+        for (int e = 0; e < VE; e += 2) {
+            const float x = v[e] * f, y = v[e + 1] * f;
+            s0 = fmaf(x, x, s0);
+            s1 = fmaf(y, y, s1);
+        }
+    }
+    const long long rest = lo + vecs * VE + threadIdx.x;
+    if (rest < hi) {
+        const float x = value(g + rest) * f;
+        bits |= __float_as_uint(x) | (uint32_t)(x != 0.f);
+        s0 = fmaf(x, x, s0);
+    }
+    *any = bits != 0;
+    return s0 + s1;
+}
+
+// The elements of chunk c of a tensor of n: chunk 0 takes those before the first boundary too.
+__device__ __forceinline__ void chunk_span(long long c, int head, long long n, long long* lo,
+                                           long long* hi) {
+    *lo = head + c * kCChunk;
+    *hi = *lo + kCChunk < n ? *lo + kCChunk : n;
+    if (*lo > n) *lo = n;
+}
+
+template <typename T>
+__device__ __forceinline__ double chunk_squares(const ClipTensor& t, int c) {
+    const T* g = static_cast<const T*>(t.g);
+    const int head = head_of(g, sizeof(T), t.n);
+    long long lo, hi;
+    chunk_span(c, head, t.n, &lo, &hi);
+    float edge = 0.f;
+    if (c == 0 && (int)threadIdx.x < head) edge = value(g + threadIdx.x);
+    bool any;
+    const float s = squares(g, lo, hi, 1.f, &any) + edge * edge;
+    // 2^-60 and above: what a square lost below 2^-149 is nothing beside it
+    if (s >= 0x1p-60f && s < INFINITY) return (double)s;
+    if (!any && edge == 0.f) return 0.0;
+    // squares that fp32 does not hold: with 2^90 (elements below 2^-30) or 2^-70 before the
+    // elements; infinities and NaN stay
+    const float f = s < 1.f ? 0x1p90f : 0x1p-70f;
+    const float again = squares(g, lo, hi, f, &any) + (edge * f) * (edge * f);
+    return (double)again * (s < 1.f ? 0x1p-180 : 0x1p140);
+}
+
+// Sum over the block in a fixed order, on every thread.
+__device__ __forceinline__ double block_sum(double v) {
+    __shared__ double part[kCThreads / 32];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
+    __syncthreads();
+    double s = 0.0;
+    for (int i = 0; i < kCThreads / 32; ++i) s += part[i];
+    return s;
+}
+
+template <int N>
+__global__ void __launch_bounds__(kCThreads) clip_norm_kernel(const __grid_constant__ ClipArgs<N> a) {
+    pdl_wait();
+    pdl_trigger();
+    double sum = 0.0;
+    const int chunks = a.first[a.count];
+    for (int c = blockIdx.x; c < chunks; c += gridDim.x) {
+        const int i = tensor_of(a, c);
+        sum += a.f32[i] ? chunk_squares<float>(a.t[i], c - a.first[i])
+                        : chunk_squares<__nv_bfloat16>(a.t[i], c - a.first[i]);
+    }
+    sum = block_sum(sum);
+    if (threadIdx.x == 0) a.parts[blockIdx.x] = sum;
+}
+
+template <typename T>
+__device__ __forceinline__ void chunk_scale(const ClipTensor& t, int c, float pre, float f) {
+    constexpr int VE = Vec<T>::n, NV = kCPer / VE;
+    const T* g = static_cast<const T*>(t.g);
+    T* out = static_cast<T*>(t.out);
+    const int head = head_of(g, sizeof(T), t.n);
+    long long lo, hi;
+    chunk_span(c, head, t.n, &lo, &hi);
+    if (c == 0 && (int)threadIdx.x < head) put(out + threadIdx.x, value(g + threadIdx.x) * pre * f);
+    const bool same = ((reinterpret_cast<uintptr_t>(out + lo)) & 15) == 0;
+    const long long vecs = (hi - lo) / VE;
+    uint4 q[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const long long k = threadIdx.x + (long long)i * kCThreads;
+        if (k < vecs) q[i] = reinterpret_cast<const uint4*>(g + lo)[k];
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const long long k = threadIdx.x + (long long)i * kCThreads;
+        if (k >= vecs) continue;
+        float v[VE];
+        unpack(q[i], v);
+#pragma unroll
+        for (int e = 0; e < VE; ++e) v[e] *= pre;
+        if (same) {
+            uint4 r;
+            if constexpr (VE == 4) {
+                r = make_uint4(__float_as_uint(v[0] * f), __float_as_uint(v[1] * f),
+                               __float_as_uint(v[2] * f), __float_as_uint(v[3] * f));
+            } else {
+                uint32_t w[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const __nv_bfloat162 p = __floats2bfloat162_rn(v[2 * e] * f, v[2 * e + 1] * f);
+                    w[e] = *reinterpret_cast<const uint32_t*>(&p);
+                }
+                r = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+            reinterpret_cast<uint4*>(out + lo)[k] = r;
+        } else {   // the output lies otherwise than the input
+#pragma unroll
+            for (int e = 0; e < VE; ++e) put(out + lo + k * VE + e, v[e] * f);
+        }
+    }
+    const long long rest = lo + vecs * VE + threadIdx.x;
+    if (rest < hi) put(out + rest, value(g + rest) * pre * f);
+}
+
+template <int N>
+__global__ void __launch_bounds__(kCThreads) clip_scale_kernel(const __grid_constant__ ClipArgs<N> a) {
+    pdl_wait();
+    pdl_trigger();
+    double sum = 0.0;
+    for (int i = threadIdx.x; i < a.n_parts; i += kCThreads) sum += a.parts[i];
+    const double norm = sqrt(block_sum(sum));
+    // a norm that is not finite, or not above the limit: as they are
+    const double factor = norm > (double)a.max_norm && norm < INFINITY ? (double)a.max_norm / norm : 1.0;
+    const float f = (float)factor;
+    // a factor that fp32 would hold in fewer bits: 2^-40 of it apart (elements it takes below fp32's
+    // normal numbers end at zero)
+    const float pre = factor < 0x1p-80 ? 0x1p-40f : 1.f;
+    const float rest = (float)(factor / (double)pre);
+    if (a.norm && blockIdx.x == 0 && threadIdx.x == 0) {
+        a.norm[0] = (float)norm;
+        a.norm[1] = f;
+    }
+    if (a.in_place && f == 1.f) return;
+    const int chunks = a.first[a.count];
+    for (int c = chunks - 1 - blockIdx.x; c >= 0; c -= gridDim.x) {
+        const int i = tensor_of(a, c);
+        if (a.f32[i])
+            chunk_scale<float>(a.t[i], c - a.first[i], pre, rest);
+        else
+            chunk_scale<__nv_bfloat16>(a.t[i], c - a.first[i], pre, rest);
+    }
+}
+
+size_t clip_ws_bytes(int count) {
+    const size_t launches = count > 0 ? ((size_t)count + kCTensors - 1) / kCTensors : 1;
+    return launches * kCParts * sizeof(double);
+}
+
+struct ClipCall {
+    const void* const* grads;
+    void* const* out;
+    const long long* sizes;
+    const int* dtypes;
+    int count;
+    float max_norm;
+    float* norm;
+    double* parts;
+};
+
+// Chunks of the tensors [t0, t1).
+long long chunks_of(const ClipCall& c, int t0, int t1) {
+    long long n = 0;
+    for (int i = t0; i < t1; ++i) n += (c.sizes[i] + kCChunk - 1) / kCChunk + 1;
+    return n;
+}
+
+// The launches for the tensors [t0, t0 + count): the norm's, or the product's.
+template <int N>
+cudaError_t clip_launch(const ClipCall& c, int t0, int count, bool scale, double* parts, int* n_parts,
+                        float* norm, cudaStream_t st) {
+    ClipArgs<N> a;
+    a.count = count;
+    int chunks = 0;
+    for (int i = 0; i < count; ++i) {
+        const int k = t0 + i, es = c.dtypes[k] == HCW_F32 ? 4 : 2;
+        a.t[i].g = c.grads[k];
+        a.t[i].out = c.out ? c.out[k] : const_cast<void*>(c.grads[k]);
+        a.t[i].n = c.sizes[k];
+        a.f32[i] = c.dtypes[k] == HCW_F32;
+        a.first[i] = chunks;
+        // the elements before the first boundary come on top of the first chunk's
+        const uintptr_t at = reinterpret_cast<uintptr_t>(c.grads[k]);
+        const long long head = std::min<long long>((long long)((16 - (at & 15)) & 15) / es, c.sizes[k]);
+        const long long body = c.sizes[k] - head;
+        chunks += (int)(body > 0 ? (body + kCChunk - 1) / kCChunk : c.sizes[k] > 0);
+    }
+    a.first[count] = chunks;
+    a.parts = scale ? c.parts : parts;
+    a.max_norm = c.max_norm;
+    a.norm = norm;
+    a.in_place = c.out == nullptr;
+    const int most = std::min(kCParts, 4 * device_sms());
+    const int grid = std::max(1, std::min(chunks, most));
+    if (!scale) {
+        *n_parts += grid;
+        a.n_parts = 0;
+        return launch_pdl(clip_norm_kernel<N>, dim3(grid), dim3(kCThreads), 0, st, a);
+    }
+    a.n_parts = *n_parts;
+    return launch_pdl(clip_scale_kernel<N>, dim3(grid), dim3(kCThreads), 0, st, a);
+}
+
+}  // namespace
+
+}  // namespace hcw
+
+using namespace hcw;
+
+extern "C" size_t hcw_clip_grads_workspace_bytes(int count) {
+    return count < 0 ? 0 : clip_ws_bytes(count);
+}
+
+extern "C" int hcw_clip_grads(const void* const* grads, void* const* out, const long long* sizes,
+                              const int* dtypes, int count, float max_norm, float* norm,
+                              void* workspace, size_t ws_bytes, void* stream) {
+    if (count < 0 || !norm || !(max_norm >= 0.f)) return HCW_ERR_INVALID_ARG;
+    if (count > 0 && (!grads || !sizes || !dtypes)) return HCW_ERR_INVALID_ARG;
+    const size_t need = clip_ws_bytes(count);
+    // the tensors' spans (inputs, outputs, then norm and workspace): no two share a byte
+    struct Span {
+        uintptr_t a, b;
+        bool out;
+    };
+    const bool apart = out != nullptr;
+    const size_t room = (size_t)count * (apart ? 2 : 1) + 2;
+    for (int i = 0; i < count; ++i) {
+        if (sizes[i] < 0 || (dtypes[i] != HCW_BF16 && dtypes[i] != HCW_F32)) return HCW_ERR_INVALID_ARG;
+        if (sizes[i] > 0 && (!grads[i] || (apart && !out[i]))) return HCW_ERR_INVALID_ARG;
+        if (sizes[i] > 1ll << 44) return HCW_ERR_UNSUPPORTED;
+        const uintptr_t mask = dtypes[i] == HCW_F32 ? 3 : 1;
+        if ((reinterpret_cast<uintptr_t>(grads[i]) & mask) ||
+            (apart && (reinterpret_cast<uintptr_t>(out[i]) & mask)))
+            return HCW_ERR_ALIGNMENT;
+    }
+    if (!on_16_bytes(workspace) || (reinterpret_cast<uintptr_t>(norm) & 3)) return HCW_ERR_ALIGNMENT;
+    if (!workspace || ws_bytes < need) return HCW_ERR_WORKSPACE;
+    ClipCall c = {grads, out, sizes, dtypes, count, max_norm, norm, static_cast<double*>(workspace)};
+    for (int t = 0; t < count; t += kCTensors)
+        if (chunks_of(c, t, std::min(count, t + kCTensors)) > kCMaxChunks) return HCW_ERR_UNSUPPORTED;
+    Span few[160];
+    Span* s = room <= 160 ? few : new (std::nothrow) Span[room];
+    if (!s) return HCW_ERR_UNSUPPORTED;
+    size_t k = 0;
+    bool sorted = true;
+    const auto add = [&](const void* p, size_t bytes, bool o) {
+        if (!bytes) return;
+        const uintptr_t a = reinterpret_cast<uintptr_t>(p);
+        s[k] = {a, a + bytes, o};
+        if (k && s[k - 1].a > a) sorted = false;
+        ++k;
+    };
+    for (int i = 0; i < count; ++i) add(grads[i], (size_t)sizes[i] * (dtypes[i] == HCW_F32 ? 4 : 2), !apart);
+    if (apart)
+        for (int i = 0; i < count; ++i)
+            add(out[i], (size_t)sizes[i] * (dtypes[i] == HCW_F32 ? 4 : 2), true);
+    add(norm, 8, true);
+    add(workspace, need, true);
+    if (!sorted) std::sort(s, s + k, [](const Span& x, const Span& y) { return x.a < y.a; });
+    // inputs that are only read may share memory
+    uintptr_t in_end = 0, out_end = 0;
+    bool meet = false;
+    for (size_t i = 0; i < k; ++i) {
+        if (s[i].a < out_end || (s[i].out && s[i].a < in_end)) meet = true;
+        uintptr_t& end = s[i].out ? out_end : in_end;
+        if (s[i].b > end) end = s[i].b;
+    }
+    if (s != few) delete[] s;
+    if (meet) return HCW_ERR_ALIASING;
+
+    const cudaStream_t st = (cudaStream_t)stream;
+    int launches = 0, n_parts = 0;
+    cudaError_t e = cudaSuccess;
+    const auto all = [&](bool scale) {
+        for (int t = 0; t == 0 || t < count; t += kCTensors) {
+            const int n = std::min(count - t, kCTensors);
+            double* parts = c.parts + n_parts;
+            float* first = scale && t == 0 ? norm : nullptr;
+            e = n <= 32 ? clip_launch<32>(c, t, n, scale, parts, &n_parts, first, st)
+                        : clip_launch<kCTensors>(c, t, n, scale, parts, &n_parts, first, st);
+            if (e != cudaSuccess) return;
+            ++launches;
+        }
+    };
+    all(false);
+    if (e == cudaSuccess) {
+        // the norm alone: one CTA without tensors writes it
+        if (isinf(max_norm) && !apart)
+            c.count = count = 0;
+        all(true);
+    }
+    return count_launch(e, launches);
+}

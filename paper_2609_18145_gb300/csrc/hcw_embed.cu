@@ -1,0 +1,675 @@
+// hcw_embed.cu -- the lookup of symbols (hcw_embed_fwd) and its gradient (hcw_embed_bwd):
+//
+//   x_t = scale E[id_t]                         (zeros for a negative id)
+//   dE_v (+)= scale sum over {t: id_t = v} of dx_t
+//
+// Both are bound by memory: the lookup reads and writes T rows, the gradient reads T rows and
+// writes V (or, added to what is there, reads and writes the rows that are named).
+//
+// Text names a few symbols thousands of times and most of them never, so the gradient goes by the
+// sorted tokens: the positions in the order of their symbols, cut into chunks of equal length, a
+// chunk's rows added by one warp for each block of columns.  A symbol whose positions lie in one
+// chunk is written there; one that reaches over a chunk's end leaves a partial sum in the
+// workspace at each, and a last launch adds these in the order of the chunks.  No atomics on
+// numbers: the order of every sum depends on the ids and the sizes alone.
+//
+// The sort is one launch without any exchange between its CTAs.  Each owns a range of symbols and
+// goes through all ids: it counts those of smaller symbols (where its own begin in the sorted
+// order) and collects its own in their order; then it sorts its own, 8 bits of the symbol a pass,
+// each warp counting and placing a run of them.
+#include "hcw.h"
+#include "hcw_internal.h"
+#include "hcw_ptx.cuh"
+
+#include <algorithm>
+
+namespace hcw {
+
+namespace {
+
+constexpr int kErrInvalid = 1;            // HCW_ERR_INVALID_ARG in the error word
+constexpr int kSortWarps = 32;
+constexpr int kSortThreads = 32 * kSortWarps;
+constexpr int kDigits = 256;              // values of a sorting pass's digit
+constexpr int kMaxRange = 65536;          // symbols of a CTA: two passes, 8 KB of flags
+constexpr int kMaxV = 1 << 23;
+constexpr int kMaxD = 1 << 20;
+constexpr int kSumWarps = 8;
+
+__device__ __forceinline__ float to_f32(float v) { return v; }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ void put(float* p, float v) { *p = v; }
+__device__ __forceinline__ void put(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
+
+// E elements of a row for a lane: one load where the rows lie on 16 bytes (WIDE), else every
+// 32nd element.  `left`: elements of the row from the block's first one.
+template <typename T, int E, bool WIDE>
+__device__ __forceinline__ void load_row(const T* p, int lane, int left, float (&v)[E]) {
+    if constexpr (WIDE) {
+        static_assert(E * sizeof(T) == 16, "a vector");
+        uint4 q = make_uint4(0, 0, 0, 0);
+        if (lane * E < left) q = *reinterpret_cast<const uint4*>(p + lane * E);
+        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (E == 8) {
+                v[2 * i] = __uint_as_float(w[i] << 16);
+                v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+            } else {
+                v[i] = __uint_as_float(w[i]);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            v[e] = lane + 32 * e < left ? to_f32(p[lane + 32 * e]) : 0.f;
+    }
+}
+
+// The lane's E elements of an output row (of type O, rounded here).
+template <typename O, int E, bool WIDE>
+__device__ __forceinline__ void store_row(O* p, int lane, int left, const float (&v)[E]) {
+    if constexpr (WIDE) {
+        if (lane * E >= left) return;
+        if constexpr (sizeof(O) == 4) {
+#pragma unroll
+            for (int i = 0; i < E / 4; ++i)
+                reinterpret_cast<float4*>(p + lane * E)[i] =
+                    make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+        } else {
+            uint32_t w[E / 2];
+#pragma unroll
+            for (int i = 0; i < E / 2; ++i) w[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
+            if constexpr (E == 8)
+                *reinterpret_cast<uint4*>(p + lane * E) = make_uint4(w[0], w[1], w[2], w[3]);
+            else
+                *reinterpret_cast<uint2*>(p + lane * E) = make_uint2(w[0], w[1]);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (lane + 32 * e < left) put(p + lane + 32 * e, v[e]);
+    }
+}
+
+// ------------------------------------------------------------------ lookup
+// A warp takes R rows, 32 E columns of them at a time.
+template <typename T, int E, bool WIDE, int R>
+__global__ void __launch_bounds__(256) embed_fwd_kernel(const int* ids, const T* table, long long T_,
+                                                        int V, int d, float scale, T* x) {
+    pdl_wait();
+    pdl_trigger();
+    const int lane = threadIdx.x & 31;
+    const long long row0 = ((long long)blockIdx.x * 8 + (threadIdx.x >> 5)) * R;
+    const int col = blockIdx.y * (32 * E);
+    int id[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) id[r] = row0 + r < T_ ? ids[row0 + r] : -1;
+    float v[R][E];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const bool there = id[r] >= 0 && id[r] < V;
+        if (id[r] >= V && lane == 0) atomicExch(&g_error_word, kErrInvalid);
+        load_row<T, E, WIDE>(table + (size_t)(there ? id[r] : 0) * d + col, lane, there ? d - col : 0,
+                             v[r]);
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        if (row0 + r >= T_) break;
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[r][e] *= scale;
+        store_row<T, E, WIDE>(x + (size_t)(row0 + r) * d + col, lane, d - col, v[r]);
+    }
+}
+
+// ------------------------------------------------------------------ the sorted tokens
+struct SortArgs {
+    const int* ids;
+    int T, V, range;          // symbols of a CTA
+    int* key[2];              // [T] symbols and [T] positions, two of each
+    int* pos[2];
+    int* count;               // tokens that name a symbol
+    void* dE;                 // null: no zeros
+    size_t row_bytes;
+};
+
+// The ids i .. i + 3, i a multiple of four; -1 from `end` on.
+__device__ __forceinline__ void ids_at(const int* ids, long long i, long long end, int (&id)[4]) {
+    if (i + 3 < end) {
+        const int4 q = *reinterpret_cast<const int4*>(ids + i);
+        id[0] = q.x;
+        id[1] = q.y;
+        id[2] = q.z;
+        id[3] = q.w;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) id[e] = i + e < end ? ids[i + e] : -1;
+    }
+}
+
+// Exclusive prefix of v over the block's threads; the total in *total.
+__device__ __forceinline__ int block_prefix(int v, int* scratch, int* total) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int s = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int u = __shfl_up_sync(0xffffffffu, s, o);
+        if (lane >= o) s += u;
+    }
+    __syncthreads();   // scratch's last use
+    if (lane == 31) scratch[warp] = s;
+    __syncthreads();
+    int before = 0, all = 0;
+    for (int i = 0; i < kSortWarps; ++i) {
+        const int c = scratch[i];
+        if (i < warp) before += c;
+        all += c;
+    }
+    *total = all;
+    return before + s - v;
+}
+
+__global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const SortArgs a) {
+    __shared__ int hist[kDigits * kSortWarps];
+    __shared__ uint32_t named[kMaxRange / 32];
+    __shared__ int scratch[kSortWarps];
+    pdl_wait();
+    pdl_trigger();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int lo = blockIdx.x * a.range, hi = min(a.V, lo + a.range);
+    for (int i = threadIdx.x; i < (a.range + 31) / 32; i += kSortThreads) named[i] = 0;
+    __syncthreads();
+    // each warp goes through a run of ids, four a lane at a time
+    const int run = ((a.T + kSortThreads - 1) / kSortThreads) * 32;   // of a warp, before rounding to 128
+    const long long w0 = (long long)warp * ((run + 127) / 128 * 128);
+    const long long w1 = min((long long)a.T, w0 + (run + 127) / 128 * 128);
+    int below = 0, mine = 0;
+    for (long long i = w0 + 4 * lane; i < w1; i += 128) {
+        int id[4];
+        ids_at(a.ids, i, w1, id);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            below += id[e] >= 0 && id[e] < lo;
+            if (id[e] >= lo && id[e] < hi) {
+                ++mine;
+                atomicOr(&named[(id[e] - lo) >> 5], 1u << ((id[e] - lo) & 31));
+            }
+            if (id[e] >= a.V) atomicExch(&g_error_word, kErrInvalid);
+        }
+    }
+    int m, base;
+    (void)block_prefix(below, scratch, &base);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+    int at = block_prefix(lane == 0 ? mine : 0, scratch, &m);
+    at = __shfl_sync(0xffffffffu, at, 0);
+    if (threadIdx.x == 0 && hi == a.V) *a.count = base + m;
+    // its own, in order
+    if (m > 0) {
+        int *key = a.key[0] + base, *pos = a.pos[0] + base;
+        int *key_to = a.key[1] + base, *pos_to = a.pos[1] + base;
+        for (long long i0 = w0; i0 < w1; i0 += 128) {
+            const long long i = i0 + 4 * lane;
+            int id[4];
+            uint32_t have[4];
+            ids_at(a.ids, i, w1, id);
+            int before = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                have[e] = __ballot_sync(0xffffffffu, id[e] >= lo && id[e] < hi);
+                before += __popc(have[e] & ((1u << lane) - 1));
+            }
+            int k = at + before;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (id[e] >= lo && id[e] < hi) {
+                    key[k] = id[e];
+                    pos[k] = (int)(i + e);
+                    ++k;
+                }
+                at += __popc(have[e]);
+            }
+        }
+        const int own = ((m + kSortThreads - 1) / kSortThreads) * 32;   // of a warp
+        const int m0 = min(m, warp * own), m1 = min(m, m0 + own);
+        for (int shift = 0; shift == 0 || (a.range - 1) >> shift; shift += 8) {
+            for (int i = threadIdx.x; i < kDigits * kSortWarps; i += kSortThreads) hist[i] = 0;
+            __syncthreads();   // and the list is there
+            for (int i = m0 + lane; i < m1; i += 32)
+                atomicAdd(&hist[(((key[i] - lo) >> shift) & (kDigits - 1)) * kSortWarps + warp], 1);
+            __syncthreads();
+            // places: by digit, then by warp
+            int c[kDigits * kSortWarps / kSortThreads], sum = 0, all;
+#pragma unroll
+            for (int j = 0; j < kDigits * kSortWarps / kSortThreads; ++j) {
+                c[j] = hist[threadIdx.x * (kDigits * kSortWarps / kSortThreads) + j];
+                sum += c[j];
+            }
+            int p = block_prefix(sum, scratch, &all);
+#pragma unroll
+            for (int j = 0; j < kDigits * kSortWarps / kSortThreads; ++j) {
+                hist[threadIdx.x * (kDigits * kSortWarps / kSortThreads) + j] = p;
+                p += c[j];
+            }
+            __syncthreads();
+            for (int i0 = m0; i0 < m1; i0 += 32) {
+                const int i = i0 + lane;
+                const bool on = i < m1;
+                const int k = on ? key[i] : 0, q = on ? pos[i] : 0;
+                const int d = on ? ((k - lo) >> shift) & (kDigits - 1) : kDigits;
+                const uint32_t same = __match_any_sync(0xffffffffu, d);
+                const int rank = __popc(same & ((1u << lane) - 1));
+                const int place = on ? hist[d * kSortWarps + warp] + rank : 0;
+                __syncwarp();
+                if (on && rank == 0) hist[d * kSortWarps + warp] += __popc(same);
+                __syncwarp();
+                if (on) {
+                    key_to[place] = k;
+                    pos_to[place] = q;
+                }
+            }
+            __syncthreads();
+            int* t = key;
+            key = key_to;
+            key_to = t;
+            t = pos;
+            pos = pos_to;
+            pos_to = t;
+        }
+    }
+    // rows that no token names
+    if (a.dE) {
+        char* rows = static_cast<char*>(a.dE);
+        const bool wide = a.row_bytes % 16 == 0;
+        for (int v = lo + warp; v < hi; v += kSortWarps) {
+            if (named[(v - lo) >> 5] >> ((v - lo) & 31) & 1) continue;
+            char* r = rows + (size_t)v * a.row_bytes;
+            if (wide)
+                for (size_t i = 16 * lane; i < a.row_bytes; i += 512)
+                    *reinterpret_cast<uint4*>(r + i) = make_uint4(0, 0, 0, 0);
+            else if (a.row_bytes % 4 == 0)
+                for (size_t i = 4 * lane; i < a.row_bytes; i += 128)
+                    *reinterpret_cast<uint32_t*>(r + i) = 0;
+            else
+                for (size_t i = 2 * lane; i < a.row_bytes; i += 64)
+                    *reinterpret_cast<unsigned short*>(r + i) = 0;
+        }
+    }
+}
+
+// ------------------------------------------------------------------ the sums
+struct SumArgs {
+    const int* key;       // the sorted tokens: symbols and positions
+    const int* pos;
+    const int* count;
+    const void* dx;
+    void* dE;
+    float* part;          // [chunks][2][d]: of the run that came in from before, and of the one that goes on
+    int d;
+    int chunk_log2;       // tokens of a chunk
+    int chunks, tiles;    // chunks at most, blocks of columns
+    float scale;
+    int add;
+};
+
+// Writes a symbol's sum: scale sum, or that on top of what is there, rounded once.
+template <typename O, int E, bool WIDE>
+__device__ __forceinline__ void write_sum(const SumArgs& a, int symbol, int col, int lane,
+                                          const float (&s)[E]) {
+    O* row = static_cast<O*>(a.dE) + (size_t)symbol * a.d + col;
+    const int left = a.d - col;
+    float v[E];
+    if (a.add) {
+        if constexpr (WIDE && sizeof(O) * E == 16) {
+            load_row<O, E, true>(row, lane, left, v);
+        } else if constexpr (WIDE) {   // the lane's E neighbours, not one vector
+#pragma unroll
+            for (int e = 0; e < E; ++e) v[e] = lane * E < left ? to_f32(row[lane * E + e]) : 0.f;
+        } else {
+            load_row<O, E, false>(row, lane, left, v);
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] = fmaf(a.scale, s[e], v[e]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] = a.scale * s[e];
+    }
+    store_row<O, E, WIDE>(row, lane, left, v);
+}
+
+// A warp adds the rows of one chunk, 32 E columns of them, eight rows on their way at once.
+template <typename T, typename O, int E, bool WIDE>
+__global__ void __launch_bounds__(32 * kSumWarps) embed_sum_kernel(const SumArgs a) {
+    pdl_wait();
+    pdl_trigger();
+    const int lane = threadIdx.x & 31;
+    const long long item = (long long)blockIdx.x * kSumWarps + (threadIdx.x >> 5);
+    const int chunk = (int)(item / a.tiles), col = (int)(item % a.tiles) * (32 * E);
+    const int count = *a.count;
+    const long long first = (long long)chunk << a.chunk_log2;
+    if (chunk >= a.chunks || first >= count) return;
+    const int n = (int)min((long long)(1 << a.chunk_log2), count - first);
+    const int before = first > 0 ? a.key[first - 1] : -1;
+    const int after = first + n < count ? a.key[first + n] : -1;
+    const T* dx = static_cast<const T*>(a.dx) + col;
+    const int left = a.d - col;
+    float* part = a.part + ((size_t)chunk * 2 * a.d + col);
+    float s[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) s[e] = 0.f;
+    bool from_before = a.key[first] == before;
+    for (int i0 = 0; i0 < n; i0 += 32) {
+        const int k = i0 + lane;
+        const int key = k < n ? a.key[first + k] : -1, pos = k < n ? a.pos[first + k] : 0;
+        // the symbol behind the lane's: the next lane's, or the next 32 tokens' first
+        const int next_first = i0 + 32 < n ? a.key[first + i0 + 32] : after;
+        int next = __shfl_down_sync(0xffffffffu, key, 1);
+        if (lane == 31 || k + 1 >= n) next = next_first;
+        const uint32_t last = __ballot_sync(0xffffffffu, k < n && (next != key || k + 1 == n));
+        const int rows = min(32, n - i0);
+        for (int r0 = 0; r0 < rows; r0 += 8) {
+            float v[8][E];
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+                const int t = __shfl_sync(0xffffffffu, pos, (r0 + r) & 31);
+                load_row<T, E, WIDE>(dx + (size_t)t * a.d, lane, r0 + r < rows ? left : 0, v[r]);
+            }
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+                if (r0 + r >= rows) break;
+#pragma unroll
+                for (int e = 0; e < E; ++e) s[e] += v[r][e];
+                if (!(last >> (r0 + r) & 1)) continue;
+                const int symbol = __shfl_sync(0xffffffffu, key, r0 + r);
+                const bool goes_on = i0 + r0 + r + 1 == n && after == symbol;
+                if (from_before)
+                    store_row<float, E, WIDE>(part, lane, left, s);
+                else if (goes_on)
+                    store_row<float, E, WIDE>(part + a.d, lane, left, s);
+                else
+                    write_sum<O, E, WIDE>(a, symbol, col, lane, s);
+                from_before = false;
+#pragma unroll
+                for (int e = 0; e < E; ++e) s[e] = 0.f;
+            }
+        }
+    }
+}
+
+// A run over several chunks: the warp of the chunk it starts in adds the parts, in order.
+template <typename T, typename O, int E, bool WIDE>
+__global__ void __launch_bounds__(32 * kSumWarps) embed_join_kernel(const SumArgs a) {
+    pdl_wait();
+    pdl_trigger();
+    const int lane = threadIdx.x & 31;
+    const long long item = (long long)blockIdx.x * kSumWarps + (threadIdx.x >> 5);
+    const int chunk = (int)(item / a.tiles), col = (int)(item % a.tiles) * (32 * E);
+    const int count = *a.count;
+    const int size = 1 << a.chunk_log2;
+    const long long first = (long long)chunk << a.chunk_log2;
+    if (chunk >= a.chunks || first + size >= count) return;   // no chunk behind it
+    const int symbol = a.key[first + size - 1];
+    if (a.key[first + size] != symbol) return;
+    if (a.key[first] == symbol && first > 0 && a.key[first - 1] == symbol) return;   // started before
+    // the chunks behind it that the run reaches into
+    int more = 0;
+    for (;;) {
+        const long long end = first + (long long)size * (more + lane + 2);   // the end of one of them
+        const bool on = end < count && a.key[end] == symbol && a.key[end - 1] == symbol;
+        const uint32_t stop = __ballot_sync(0xffffffffu, !on);
+        if (stop) {
+            more += __ffs(stop);
+            break;
+        }
+        more += 32;
+    }
+    const int left = a.d - col;
+    const float* part = a.part + ((size_t)chunk * 2 * a.d + col);
+    float s[E];
+    const auto load = [&](const float* p, float (&v)[E]) {
+        if constexpr (WIDE) {
+#pragma unroll
+            for (int i = 0; i < E / 4; ++i) {
+                const float4 q = lane * E < left ? reinterpret_cast<const float4*>(p + lane * E)[i]
+                                                 : make_float4(0.f, 0.f, 0.f, 0.f);
+                v[4 * i] = q.x;
+                v[4 * i + 1] = q.y;
+                v[4 * i + 2] = q.z;
+                v[4 * i + 3] = q.w;
+            }
+        } else {
+            load_row<float, E, false>(p, lane, left, v);
+        }
+    };
+    load(part + a.d, s);
+    for (int j0 = 0; j0 < more; j0 += 4) {
+        float v[4][E];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (j0 + j < more) {
+                load(part + (size_t)(j0 + j + 1) * 2 * a.d, v[j]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; ++e) v[j][e] = 0.f;
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (j0 + j < more) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) s[e] += v[j][e];
+            }
+    }
+    write_sum<O, E, WIDE>(a, symbol, col, lane, s);
+}
+
+// ------------------------------------------------------------------ host
+size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
+
+// Tokens of a chunk: 8 to 256, so that the chunks' warps fill the machine about once.
+int chunk_log2_of(int T, int tiles, int sms) {
+    int l = 3;
+    while (l < 8 && ((long long)T * tiles >> (l + 1)) >= 16ll * sms) ++l;
+    return l;
+}
+
+struct BwdPlan {
+    int tiles, chunk_log2, chunks;
+    size_t key[2], pos[2], count, part, bytes;
+};
+
+// The workspace's parts.  Chunks grow with T, so that a shorter batch's parts may be more of
+// them: the room for the parts is that of any batch up to T.
+BwdPlan bwd_plan(int T, int d, int elems) {
+    BwdPlan p;
+    p.tiles = (d + 32 * elems - 1) / (32 * elems);
+    const int sms = device_sms();
+    p.chunk_log2 = chunk_log2_of(T, p.tiles, sms);
+    p.chunks = (int)(((long long)T + (1 << p.chunk_log2) - 1) >> p.chunk_log2);
+    const size_t list = up((size_t)T * 4);
+    size_t at = 0;
+    for (int i = 0; i < 2; ++i) {
+        p.key[i] = at;
+        at += list;
+        p.pos[i] = at;
+        at += list;
+    }
+    p.count = at;
+    at += 256;
+    p.part = at;
+    p.bytes = at + (size_t)p.chunks * 2 * d * 4;
+    return p;
+}
+
+// At least what any batch of up to T tokens of width d takes, whatever its type: with chunks of
+// 2^l tokens there are at most those of the longest batch that takes them.
+size_t bwd_ws_bytes(int T, int d) {
+    size_t most = 0;
+    const int sms = device_sms();
+    for (int elems = 4; elems <= 8; elems += 4) {
+        const int tiles = (d + 32 * elems - 1) / (32 * elems);
+        long long parts = 0;
+        for (int l = 3; l <= 8; ++l) {
+            // the longest batch with chunks of 2^l: one token fewer than takes the next size
+            const long long next = ((16ll * sms << (l + 1)) + tiles - 1) / tiles;
+            const long long longest = l == 8 || next > T ? T : next - 1;
+            if (longest > 0) parts = std::max(parts, (longest + (1 << l) - 1) >> l);
+        }
+        most = std::max(most, (size_t)parts * 2 * d * 4);
+    }
+    return 4 * up((size_t)T * 4) + 256 + most;
+}
+
+template <typename T, int E, bool WIDE>
+cudaError_t fwd(const int* ids, const void* table, int tokens, int V, int d, float scale, void* x,
+                cudaStream_t st) {
+    const int tiles = (d + 32 * E - 1) / (32 * E);
+    const T* t = static_cast<const T*>(table);
+    // four rows a warp once that leaves 16 warps an SM
+    if ((long long)tokens * tiles >= 64ll * device_sms()) {
+        const dim3 grid((unsigned)(((long long)tokens + 31) / 32), tiles);
+        return launch_pdl(embed_fwd_kernel<T, E, WIDE, 4>, grid, dim3(256), 0, st, ids, t,
+                          (long long)tokens, V, d, scale, static_cast<T*>(x));
+    }
+    const dim3 grid((unsigned)(((long long)tokens + 7) / 8), tiles);
+    return launch_pdl(embed_fwd_kernel<T, E, WIDE, 1>, grid, dim3(256), 0, st, ids, t,
+                      (long long)tokens, V, d, scale, static_cast<T*>(x));
+}
+
+template <typename T, typename O, int E, bool WIDE>
+cudaError_t bwd(SortArgs& so, SumArgs& su, int tokens, char* ws, cudaStream_t st, int* launches) {
+    const BwdPlan p = bwd_plan(tokens, su.d, E);
+    for (int i = 0; i < 2; ++i) {
+        so.key[i] = reinterpret_cast<int*>(ws + p.key[i]);
+        so.pos[i] = reinterpret_cast<int*>(ws + p.pos[i]);
+    }
+    so.count = reinterpret_cast<int*>(ws + p.count);
+    const int last = so.range > kDigits ? 0 : 1;   // after two passes, or one
+    su.key = so.key[last];
+    su.pos = so.pos[last];
+    su.count = so.count;
+    su.part = reinterpret_cast<float*>(ws + p.part);
+    su.chunk_log2 = p.chunk_log2;
+    su.chunks = p.chunks;
+    su.tiles = p.tiles;
+    const int owners = (so.V + so.range - 1) / so.range;
+    cudaError_t e = launch_pdl(embed_sort_kernel, dim3(owners), dim3(kSortThreads), 0, st, so);
+    if (e != cudaSuccess) return e;
+    ++*launches;
+    const dim3 grid((unsigned)(((long long)p.chunks * p.tiles + kSumWarps - 1) / kSumWarps));
+    e = launch_pdl(embed_sum_kernel<T, O, E, WIDE>, grid, dim3(32 * kSumWarps), 0, st, su);
+    if (e != cudaSuccess) return e;
+    ++*launches;
+    e = launch_pdl(embed_join_kernel<T, O, E, WIDE>, grid, dim3(32 * kSumWarps), 0, st, su);
+    if (e != cudaSuccess) return e;
+    ++*launches;
+    return cudaSuccess;
+}
+
+int check_sizes(int T, int V, int d, int dtype) {
+    if (T < 0 || V < 1 || d < 1 || (dtype != HCW_BF16 && dtype != HCW_F32)) return HCW_ERR_INVALID_ARG;
+    if (V > kMaxV || d > kMaxD || T > 1 << 28) return HCW_ERR_UNSUPPORTED;
+    return HCW_OK;
+}
+
+}  // namespace
+
+cudaError_t embed_error_word_read_clear(int* word) {
+    const int zero = 0;
+    cudaError_t e = cudaMemcpyFromSymbol(word, g_error_word, sizeof(int));
+    if (e == cudaSuccess && *word) e = cudaMemcpyToSymbol(g_error_word, &zero, sizeof(int));
+    return e;
+}
+
+}  // namespace hcw
+
+using namespace hcw;
+
+extern "C" int hcw_embed_fwd(const int* ids, const void* E, int T, int V, int d, int dtype, float scale,
+                             void* x, void* stream) {
+    const int rc = check_sizes(T, V, d, dtype);
+    if (rc) return rc;
+    if (!(scale - scale == 0.f)) return HCW_ERR_INVALID_ARG;   // infinite or NaN
+    if (!on_16_bytes(ids) || !on_16_bytes(E) || !on_16_bytes(x)) return HCW_ERR_ALIGNMENT;
+    const size_t es = dtype == HCW_F32 ? 4 : 2, xb = (size_t)T * d * es;
+    if (spans_meet(x, xb, ids, (size_t)T * 4) || spans_meet(x, xb, E, (size_t)V * d * es))
+        return HCW_ERR_ALIASING;
+    if (T == 0) return HCW_OK;
+    if (!ids || !E || !x) return HCW_ERR_INVALID_ARG;
+    const cudaStream_t st = (cudaStream_t)stream;
+    const bool wide = d * es % 16 == 0;
+    cudaError_t e;
+    if (dtype == HCW_BF16)
+        e = wide ? fwd<__nv_bfloat16, 8, true>(ids, E, T, V, d, scale, x, st)
+                 : fwd<__nv_bfloat16, 8, false>(ids, E, T, V, d, scale, x, st);
+    else
+        e = wide ? fwd<float, 4, true>(ids, E, T, V, d, scale, x, st)
+                 : fwd<float, 4, false>(ids, E, T, V, d, scale, x, st);
+    return count_launch(e, 1);
+}
+
+extern "C" size_t hcw_embed_bwd_workspace_bytes(int T, int V, int d) {
+    if (check_sizes(T, V, d, HCW_BF16) || T == 0) return 0;
+    return bwd_ws_bytes(T, d);
+}
+
+extern "C" int hcw_embed_bwd(const int* ids, const void* dx, int T, int V, int d, int dtype, float scale,
+                             int accumulate, int de_dtype, void* dE, void* workspace,
+                             size_t ws_bytes, void* stream) {
+    const int rc = check_sizes(T, V, d, dtype);
+    if (rc) return rc;
+    if (!(scale - scale == 0.f) || (accumulate != 0 && accumulate != 1) ||
+        (de_dtype != HCW_BF16 && de_dtype != HCW_F32))
+        return HCW_ERR_INVALID_ARG;
+    if (!on_16_bytes(ids) || !on_16_bytes(dx) || !on_16_bytes(dE) || !on_16_bytes(workspace))
+        return HCW_ERR_ALIGNMENT;
+    if (!dE || (T > 0 && (!ids || !dx))) return HCW_ERR_INVALID_ARG;
+    const size_t es = dtype == HCW_F32 ? 4 : 2, oes = de_dtype == HCW_F32 ? 4 : 2;
+    const size_t ob = (size_t)V * d * oes, need = T > 0 ? bwd_ws_bytes(T, d) : 0;
+    if (need && (!workspace || ws_bytes < need)) return HCW_ERR_WORKSPACE;
+    const struct {
+        const void* p;
+        size_t n;
+    } in[] = {{ids, (size_t)T * 4}, {dx, (size_t)T * d * es}};
+    for (const auto& q : in)
+        if (spans_meet(dE, ob, q.p, q.n) || spans_meet(workspace, need, q.p, q.n)) return HCW_ERR_ALIASING;
+    if (spans_meet(dE, ob, workspace, need)) return HCW_ERR_ALIASING;
+    const cudaStream_t st = (cudaStream_t)stream;
+    if (T == 0) {
+        if (accumulate) return HCW_OK;
+        return cudaMemsetAsync(dE, 0, ob, st) == cudaSuccess ? HCW_OK : HCW_ERR_CUDA;
+    }
+    const int sms = device_sms();
+    if ((V + sms - 1) / sms > kMaxRange) return HCW_ERR_UNSUPPORTED;
+    SortArgs so = {};
+    so.ids = ids;
+    so.T = T;
+    so.V = V;
+    so.range = (V + sms - 1) / sms;
+    so.dE = accumulate ? nullptr : dE;
+    so.row_bytes = (size_t)d * oes;
+    SumArgs su = {};
+    su.dx = dx;
+    su.dE = dE;
+    su.d = d;
+    su.scale = scale;
+    su.add = accumulate;
+    int launches = 0;
+    cudaError_t e;
+    char* ws = static_cast<char*>(workspace);
+    const bool wide = d * es % 16 == 0;
+    using B = __nv_bfloat16;
+    if (dtype == HCW_BF16 && de_dtype == HCW_BF16)
+        e = wide ? bwd<B, B, 8, true>(so, su, T, ws, st, &launches)
+                 : bwd<B, B, 8, false>(so, su, T, ws, st, &launches);
+    else if (dtype == HCW_BF16)
+        e = wide ? bwd<B, float, 8, true>(so, su, T, ws, st, &launches)
+                 : bwd<B, float, 8, false>(so, su, T, ws, st, &launches);
+    else if (de_dtype == HCW_BF16)
+        e = wide ? bwd<float, B, 4, true>(so, su, T, ws, st, &launches)
+                 : bwd<float, B, 4, false>(so, su, T, ws, st, &launches);
+    else
+        e = wide ? bwd<float, float, 4, true>(so, su, T, ws, st, &launches)
+                 : bwd<float, float, 4, false>(so, su, T, ws, st, &launches);
+    return count_launch(e, launches);
+}

@@ -384,6 +384,20 @@ cudaError_t norm_error_word_read_clear(int* word);
 // Read its kernels' error word and reset it to 0 (synchronous).
 cudaError_t distill_error_word_read_clear(int* word);
 
+// ---- The model's two ends (hcw_embed.cu, hcw_clip.cu, hcw_q4.cu, hcw_logits.cu) ----
+// Read the kernels' error words and reset them to 0 (synchronous); the clipping and the 4-bit
+// products wait for nothing and check nothing on the device, so they have none.
+cudaError_t embed_error_word_read_clear(int* word);
+cudaError_t logits_error_word_read_clear(int* word);
+
+// Argument checks of those files: 16-byte alignment, and whether two spans share a byte.
+inline bool on_16_bytes(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+inline bool spans_meet(const void* a, size_t na, const void* b, size_t nb) {
+    if (!a || !b || !na || !nb) return false;
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return x < y + nb && y < x + na;
+}
+
 // Dynamic shared memory the tensor-core kernel uses for this N tile.
 size_t tc_smem_bytes(int BN);
 int tc_stages(int BN);

@@ -117,6 +117,16 @@ _SIGNATURES = {
     "hcw_residual_norm_bwd": ([_P, _P, _P, _P, _P, _I, _F, _I, _P, _P, _I, _P, _F, _I, _I, _I, _P,
                                _P, _P, _P, _P, _P, _P, _P, _SZ, _P], _I),
     "hcw_distill_loss": ([_P, _P, _P, _P, _P, _I, _I, _I, _I, _F, _F, _F, _P, _P, _P], _I),
+    "hcw_embed_fwd": ([_P, _P, _I, _I, _I, _I, _F, _P, _P], _I),
+    "hcw_embed_bwd_workspace_bytes": ([_I, _I, _I], _SZ),
+    "hcw_embed_bwd": ([_P, _P, _I, _I, _I, _I, _F, _I, _I, _P, _P, _SZ, _P], _I),
+    "hcw_clip_grads_workspace_bytes": ([_I], _SZ),
+    "hcw_clip_grads": ([_P, _P, _P, _P, _I, _F, _P, _P, _SZ, _P], _I),
+    "hcw_q4_bytes": ([_I, _I, _I], _SZ),
+    "hcw_q4_quantize": ([_P, _I, _I, _I, _I, _P, _P, _P], _I),
+    "hcw_q4_pack": ([_P, _P, _I, _I, _I, _P, _P], _I),
+    "hcw_q4_matmul": ([_P, _P, _P, _I, _I, _I, _I, _I, _P, _P], _I),
+    "hcw_logits_edit": ([_P, _I, _I, _I, _P, _P, _P, _I, _P, _P, _P, _P, _P, _I, _P, _P, _P], _I),
     "hcw_set_stack_kernels": ([_I], _I),
     "hcw_set_decode_kernel": ([_I], _I),
     "hcw_stack_kernels_used": ([_I, _I, _I, _I], _I),
@@ -704,6 +714,245 @@ def hcw_distill_loss(z, idx=None, teacher=None, target=None, weight=None,
                                   temperature, kl_scale, ce_scale, _ptr(loss), _ptr(dz),
                                   _stream(stream)), "hcw_distill_loss")
     return loss, dz
+
+
+def _here(what, *ts):
+    """ts (None allowed) are contiguous tensors of the current device, where the launch goes."""
+    dev = None
+    for t in ts:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError("%s: all tensors must be CUDA tensors" % what)
+        if not t.is_contiguous():
+            raise ValueError("%s: all tensors must be contiguous" % what)
+        if dev is None:
+            dev = torch.cuda.current_device()
+        if t.get_device() != dev:
+            raise ValueError("%s: a tensor of %s, but the current device is cuda:%d"
+                             % (what, t.device, dev))
+
+
+def _typed(what, dtype, *ts):
+    for t in ts:
+        if t is not None and t.dtype != dtype:
+            raise TypeError("%s must be %s, got %s" % (what, str(dtype)[6:], t.dtype))
+
+
+def hcw_embed_fwd(ids, E, scale: float = 1.0, x=None, stream=None):
+    """x[t] = scale E[ids[t]]: rows of E [V, d] for ids [...] int32 (negative: zeros).
+    Returns x [..., d]."""
+    _here("hcw_embed_fwd", ids, E, x)
+    _typed("hcw_embed_fwd: ids", torch.int32, ids)
+    if E.dim() != 2:
+        raise ValueError("hcw_embed_fwd: E must be [V, d], got %s" % (tuple(E.shape),))
+    V, d = E.shape
+    if x is None:
+        x = _memory(stream).empty((*ids.shape, d), dtype=E.dtype, device=E.device)
+    elif x.dtype != E.dtype or x.numel() != ids.numel() * d or x.dim() > 1 and (
+            x.shape[-1] != d or not _same_rows(x.shape[:-1], ids.shape)):
+        raise ValueError("hcw_embed_fwd: x %s %s does not match ids %s and E %s %s"
+                         % (tuple(x.shape), x.dtype, tuple(ids.shape), tuple(E.shape), E.dtype))
+    _check(lib().hcw_embed_fwd(_ptr(ids), _ptr(E), ids.numel(), V, d, _dtype_code(E), scale, _ptr(x),
+                               _stream(stream)), "hcw_embed_fwd")
+    return x
+
+
+def hcw_embed_bwd_workspace_bytes(T: int, V: int, d: int) -> int:
+    return int(lib().hcw_embed_bwd_workspace_bytes(T, V, d))
+
+
+def hcw_embed_bwd(ids, dx, V: int, scale: float = 1.0, dE=None, de_dtype=torch.float32,
+                  accumulate: bool = False, workspace=None, stream=None):
+    """Gradient of hcw_embed_fwd: dE[v] = scale * the sum of dx's rows with ids = v.
+    dE [V, d] in its own type (new: de_dtype); accumulate=True adds to the dE given.
+    Returns dE."""
+    _here("hcw_embed_bwd", ids, dx, dE, workspace)
+    _typed("hcw_embed_bwd: ids", torch.int32, ids)
+    if not dx.dim():
+        raise ValueError("hcw_embed_bwd: dx must be [..., d]")
+    T, d = ids.numel(), dx.shape[-1]
+    if dx.numel() != T * d or dx.dim() > 1 and not _same_rows(dx.shape[:-1], ids.shape):
+        raise ValueError("hcw_embed_bwd: dx %s does not match ids %s"
+                         % (tuple(dx.shape), tuple(ids.shape)))
+    if dE is None:
+        if accumulate:
+            raise ValueError("hcw_embed_bwd: accumulate needs the dE to add to")
+        dE = _memory(stream).empty(V, d, dtype=de_dtype, device=dx.device)
+    elif tuple(dE.shape) != (V, d):
+        raise ValueError("hcw_embed_bwd: dE %s is not [%d, %d]" % (tuple(dE.shape), V, d))
+    if workspace is None:
+        workspace = _workspace(stream, hcw_embed_bwd_workspace_bytes(T, V, d), dx.device, None)
+    _check(lib().hcw_embed_bwd(_ptr(ids), _ptr(dx), T, V, d, _dtype_code(dx), scale,
+                               int(bool(accumulate)), _dtype_code(dE), _ptr(dE), _ptr(workspace),
+                               workspace.nbytes, _stream(stream)), "hcw_embed_bwd")
+    return dE
+
+
+class GradList:
+    """The tensors of hcw_clip_grads with the arrays that describe them: made once for gradients
+    that keep their memory from step to step.  out: tensors of the same sizes and types for the
+    clipped gradients (None: in place).  Holds the tensors; to be made again when one is replaced."""
+
+    def __init__(self, grads, out=None):
+        self.grads = list(grads)
+        self.out = None if out is None else list(out)
+        _here("GradList", *self.grads, *(self.out or ()))
+        n = len(self.grads)
+        if self.out is not None:
+            if len(self.out) != n:
+                raise ValueError("GradList: %d outputs for %d gradients" % (len(self.out), n))
+            for g, o in zip(self.grads, self.out):
+                if o.dtype != g.dtype or o.shape != g.shape:
+                    raise ValueError("GradList: output %s %s does not match gradient %s %s"
+                                     % (tuple(o.shape), o.dtype, tuple(g.shape), g.dtype))
+        self.device = self.grads[0].device if n else None
+        self.count = n
+        self._grads = (_P * n)(*[_ptr(g) for g in self.grads])
+        self._out = None if self.out is None else (_P * n)(*[_ptr(o) for o in self.out])
+        self._sizes = (_LL * n)(*[g.numel() for g in self.grads])
+        self._dtypes = (_I * n)(*[_dtype_code(g) for g in self.grads])
+
+
+def hcw_clip_grads_workspace_bytes(count: int) -> int:
+    return int(lib().hcw_clip_grads_workspace_bytes(count))
+
+
+def hcw_clip_grads(grads, max_norm: float, norm=None, workspace=None, stream=None):
+    """Scales the gradients (a GradList, or tensors that are clipped in place) by
+    min(1, max_norm / norm over all of them); max_norm = inf takes the norm alone.  Returns
+    the tensor [2] fp32 of the norm and the factor (on the device: nothing waits)."""
+    q = grads if isinstance(grads, GradList) else GradList(grads)
+    _here("hcw_clip_grads", norm, workspace)
+    if q.device is not None and q.device.index != torch.cuda.current_device():
+        raise ValueError("hcw_clip_grads: gradients of %s, but the current device is cuda:%d"
+                         % (q.device, torch.cuda.current_device()))
+    if norm is None:
+        norm = _memory(stream).empty(2, dtype=torch.float32, device=q.device or "cuda")
+    elif norm.dtype != torch.float32 or norm.numel() != 2:
+        raise ValueError("hcw_clip_grads: norm must be 2 float32 values")
+    if workspace is None:
+        workspace = _workspace(stream, hcw_clip_grads_workspace_bytes(q.count), norm.device, None)
+    _check(lib().hcw_clip_grads(q._grads, q._out, q._sizes, q._dtypes, q.count, max_norm, _ptr(norm),
+                                _ptr(workspace), workspace.nbytes, _stream(stream)),
+           "hcw_clip_grads")
+    return norm
+
+
+def hcw_q4_bytes(N: int, K: int, group: int) -> int:
+    return int(lib().hcw_q4_bytes(N, K, group))
+
+
+def hcw_q4_quantize(W, group: int = 64, codes=None, scales=None, stream=None):
+    """Codes [N, K] int8 (-8 .. 7) and scales [N, ceil(K / group)] bf16 of weights W [N, K]."""
+    _here("hcw_q4_quantize", W, codes, scales)
+    _typed("hcw_q4_quantize: codes", torch.int8, codes)
+    _typed("hcw_q4_quantize: scales", torch.bfloat16, scales)
+    if W.dim() != 2:
+        raise ValueError("hcw_q4_quantize: W must be [N, K], got %s" % (tuple(W.shape),))
+    N, K = W.shape
+    G = -(-K // group) if group > 0 else 0
+    mem = _memory(stream)
+    codes = mem.empty(N, K, dtype=torch.int8, device=W.device) if codes is None else codes
+    scales = mem.empty(N, G, dtype=torch.bfloat16, device=W.device) if scales is None else scales
+    if tuple(codes.shape) != (N, K) or tuple(scales.shape) != (N, G):
+        raise ValueError("hcw_q4_quantize: codes %s and scales %s do not match W %s"
+                         % (tuple(codes.shape), tuple(scales.shape), tuple(W.shape)))
+    _check(lib().hcw_q4_quantize(_ptr(W), N, K, group, _dtype_code(W), _ptr(codes), _ptr(scales),
+                                 _stream(stream)), "hcw_q4_quantize")
+    return codes, scales
+
+
+def hcw_q4_pack(codes, scales, group: int = 64, packed=None, stream=None):
+    """The weights scales * codes as hcw_q4_matmul reads them (uint8 [hcw_q4_bytes])."""
+    _here("hcw_q4_pack", codes, scales, packed)
+    _typed("hcw_q4_pack: codes", torch.int8, codes)
+    _typed("hcw_q4_pack: scales", torch.bfloat16, scales)
+    _typed("hcw_q4_pack: packed", torch.uint8, packed)
+    if codes.dim() != 2:
+        raise ValueError("hcw_q4_pack: codes must be [N, K], got %s" % (tuple(codes.shape),))
+    N, K = codes.shape
+    if group > 0 and tuple(scales.shape) != (N, -(-K // group)):
+        raise ValueError("hcw_q4_pack: scales %s do not match codes %s in groups of %d"
+                         % (tuple(scales.shape), tuple(codes.shape), group))
+    need = hcw_q4_bytes(N, K, group)
+    if packed is None:
+        packed = _memory(stream).empty(need, dtype=torch.uint8, device=codes.device)
+    elif packed.numel() != need:
+        raise ValueError("hcw_q4_pack: packed has %d bytes, not %d" % (packed.numel(), need))
+    _check(lib().hcw_q4_pack(_ptr(codes), _ptr(scales), N, K, group, _ptr(packed), _stream(stream)),
+           "hcw_q4_pack")
+    return packed
+
+
+def hcw_q4_matmul(x, packed, N: int, group: int = 64, bias=None, y=None, y_dtype=torch.bfloat16,
+                  stream=None):
+    """y = x W^T (+ bias) of a few tokens x [..., K] bf16 with the packed weights of N rows in
+    groups of `group`; y [..., N] is bf16 or fp32 (y's type, or y_dtype for a new one)."""
+    _here("hcw_q4_matmul", x, packed, bias, y)
+    _typed("hcw_q4_matmul: x", torch.bfloat16, x)
+    _typed("hcw_q4_matmul: packed", torch.uint8, packed)
+    if not x.dim():
+        raise ValueError("hcw_q4_matmul: x must be [..., K]")
+    T, K = _rows(x)
+    if bias is not None:
+        _params("hcw_q4_matmul: bias", 1, N, bias)
+    need = hcw_q4_bytes(N, K, group)
+    if packed.numel() != need:
+        raise ValueError("hcw_q4_matmul: packed has %d bytes, weights [%d, %d] in groups of %d %d"
+                         % (packed.numel(), N, K, group, need))
+    if y is None:
+        y = _memory(stream).empty((*x.shape[:-1], N), dtype=y_dtype, device=x.device)
+    elif y.numel() != T * N or y.dim() > 1 and (y.shape[-1] != N or
+                                                not _same_rows(y.shape[:-1], x.shape[:-1])):
+        raise ValueError("hcw_q4_matmul: y %s does not match x %s and N = %d"
+                         % (tuple(y.shape), tuple(x.shape), N))
+    _check(lib().hcw_q4_matmul(_ptr(x), _ptr(packed), _ptr(bias), T, N, K, group, _dtype_code(y),
+                               _ptr(y), _stream(stream)), "hcw_q4_matmul")
+    return y
+
+
+def hcw_logits_edit(z, history=None, lengths=None, prompt=None, repetition=None, frequency=None,
+                    presence=None, bias_idx=None, bias=None, mask=None, out=None, stream=None):
+    """Logits z [B, V] with penalties for the symbols of history [B, H], biases in slots
+    (bias_idx, bias [B, M]) and a mask of bits [B, ceil(V / 32)] int32; see hcw.h.  out = z
+    edits in place.  Returns out."""
+    _here("hcw_logits_edit", z, history, lengths, prompt, repetition, frequency, presence, bias_idx,
+          bias, mask, out)
+    if z.dim() != 2:
+        raise ValueError("hcw_logits_edit: z must be [B, V], got %s" % (tuple(z.shape),))
+    B, V = z.shape
+    H = M = 0
+    if history is not None:
+        _typed("hcw_logits_edit: history", torch.int32, history)
+        if history.dim() != 2 or history.shape[0] != B:
+            raise ValueError("hcw_logits_edit: history %s is not [%d, H]" % (tuple(history.shape), B))
+        H = history.shape[1]
+    if bias_idx is not None or bias is not None:
+        if bias_idx is None or bias is None or bias_idx.shape != bias.shape or \
+                bias.dim() != 2 or bias.shape[0] != B:
+            raise ValueError("hcw_logits_edit: bias_idx and bias must both be [%d, M]" % B)
+        _typed("hcw_logits_edit: bias_idx", torch.int32, bias_idx)
+        _typed("hcw_logits_edit: bias", torch.float32, bias)
+        M = bias.shape[1]
+    _row_values("hcw_logits_edit: lengths and prompt", torch.int32, B, None, lengths, prompt)
+    _row_values("hcw_logits_edit: penalties", torch.float32, B, None, repetition, frequency, presence)
+    if mask is not None:
+        _typed("hcw_logits_edit: mask", torch.int32, mask)
+        if tuple(mask.shape) != (B, -(-V // 32)):
+            raise ValueError("hcw_logits_edit: mask %s is not [%d, %d]"
+                             % (tuple(mask.shape), B, -(-V // 32)))
+    if out is None:
+        out = _memory(stream).empty_like(z)
+    elif out.shape != z.shape or out.dtype != z.dtype:
+        raise ValueError("hcw_logits_edit: out %s %s does not match z %s %s"
+                         % (tuple(out.shape), out.dtype, tuple(z.shape), z.dtype))
+    _check(lib().hcw_logits_edit(
+        _ptr(z), B, V, _dtype_code(z), _ptr(history) if H else None, _ptr(lengths) if H else None,
+        _ptr(prompt) if H else None, H, _ptr(repetition), _ptr(frequency), _ptr(presence),
+        _ptr(bias_idx) if M else None, _ptr(bias) if M else None, M, _ptr(mask), _ptr(out),
+        _stream(stream)), "hcw_logits_edit")
+    return out
 
 
 def hcw_set_decode_kernel(mode: int) -> int:
