@@ -112,7 +112,7 @@ def test_packed_weight_refusals(H):
     N, K = 40, 264
     W, q, s, p = places(4)
     need = H.hcw_q4_bytes(N, K, 64)
-    assert need == 3 * 5 * 512 + 3 * 5 * 32
+    assert need == 3 * 3 * (1024 + 2 * 32)
     assert H.hcw_q4_bytes(N, K, 48) == H.hcw_q4_bytes(N, K + 4, 64) == H.hcw_q4_bytes(0, K, 64) == 0
 
     def quant(W=W, N=N, K=K, g=64, dt=0, q=q, s=s):

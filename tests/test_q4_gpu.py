@@ -60,7 +60,9 @@ def check(H, codes, scales, x, bias, group, dtype, stream=None):
 
 
 SIZES = [(1, 1, 8), (1, 16, 64), (1, 17, 72), (3, 33, 200), (8, 64, 256), (9, 40, 1000), (16, 100, 2048),
-         (1, 2048, 512), (5, 3203, 1000), (16, 48, 8192), (17, 50, 136), (40, 31, 640), (2, 5000, 4096)]
+         (1, 2048, 512), (5, 3203, 1000), (16, 48, 8192), (17, 50, 136), (40, 31, 640), (2, 5000, 4096),
+         (1, 40000, 64), (9, 30000, 320), (3, 40, 5000), (16, 33, 9000), (10, 6000, 4232), (2, 20, 33800),
+         (12, 40, 66000)]
 
 
 @pytest.mark.parametrize("group", [32, 64, 128])
