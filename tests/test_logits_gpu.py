@@ -216,3 +216,53 @@ def test_shapes_are_checked(H):
                dict(bias_idx=i(3, 2), bias=i(3, 2))):
         with pytest.raises(TypeError):
             H.hcw_logits_edit(z, **kw)
+
+
+LARGE = [(60, 50001, 300, 64), (200, 20003, 4000, 90), (3, 1500001, 40, 1024), (40, 131072, 4097, 5),
+         (900, 8191, 60, 20), (40, 131072, 0, 30), (40, 131072, 700, 0)]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("B,V,Hn,M", LARGE)
+def test_large_batches(H, B, V, Hn, M, dtype):
+    """Sizes at which the named symbols have a launch of their own, with and without a mask."""
+    z, a = make(B, V, Hn, M, dtype, seed=V)
+    if Hn > 100:
+        a["history"][0] = a["history"][0, 5]                       # one symbol all along
+        a["history"][1] = np.arange(Hn) * 31 % V                   # every symbol another one
+        a["lengths"][:2], a["prompt"][:2] = Hn, (Hn // 2, 0)
+    if M > 4:
+        a["bias_idx"][0] = 5                                       # one symbol in every slot
+        a["bias_idx"][1, ::2] = V - 1
+        a["bias_idx"][2, 1] = a["history"][2, 0] if Hn else 0      # a symbol of the history too
+    a["mask"][0] = -1
+    a["mask"][1, : 9] = 0
+    a["mask"][2] = 0
+    check(H, z, a)
+    del a["mask"]
+    check(H, z, a)
+
+
+def test_rows_at_odd_places_in_large_batches(H):
+    for V in (16385, 16386, 16391, 33003):
+        for dtype in (BF16, F32):
+            z, a = make(257, V, 5, 2, dtype, seed=V)
+            check(H, z, a)
+
+
+def test_a_large_batch_in_a_graph(H):
+    z, a = make(64, 50001, 300, 64, F32)
+    one = check(H, z, a).clone()
+    dev = {k: torch.from_numpy(v).cuda() for k, v in a.items()}
+    zd, out, st = z.cuda(), torch.empty(64, 50001, device="cuda"), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=st):
+        # the history is written right before the call that reads it
+        past = dev["history"] + 0
+        H.hcw_logits_edit(zd, out=out, **dict(dev, history=past))
+    for _ in range(3):
+        out.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, one)
