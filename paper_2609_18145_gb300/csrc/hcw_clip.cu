@@ -10,10 +10,10 @@
 // through, and the CTAs take them in turn.  The second launch goes through them backwards, so that
 // what the first one read last is found in L2.
 //
-// The squares of a thread's elements of one chunk (32 of them) are added in fp32, everything above
-// in fp64.  Squares of fp32 or bf16 gradients may leave fp32's range: a thread whose sum did, or
-// lies where squares lose their last bits, takes its elements again with a power of two before
-// them, so the norm is right to a few parts in 2^24 for any finite gradients.
+// The squares of a warp's elements of one chunk (8 or 32 a thread) are added in fp32, everything above in
+// fp64.  Squares of fp32 or bf16 gradients may leave fp32's range: a warp whose sum did, or lies where
+// squares lose their last bits, takes its elements again with a power of two before them, so the norm
+// is right to a few parts in 2^24 for any finite gradients.
 #include "hcw.h"
 #include "hcw_internal.h"
 
@@ -27,8 +27,6 @@ namespace hcw {
 namespace {
 
 constexpr int kCThreads = 512;
-constexpr int kCPer = 32;                        // elements of a chunk for a thread
-constexpr int kCChunk = kCThreads * kCPer;
 constexpr int kCParts = 1024;                    // CTAs of a launch at most
 constexpr int kCTensors = 512;                   // tensors of a launch at most
 constexpr long long kCMaxChunks = 1ll << 30;     // of a launch
@@ -39,7 +37,7 @@ struct ClipTensor {
     long long n;
 };
 
-// The tensors of a launch, passed by value: 32 of them or 512.
+// The tensors of a launch, passed by value: 32 of them or 512.  Chunks have PER elements a thread.
 template <int N>
 struct ClipArgs {
     ClipTensor t[N];
@@ -99,9 +97,9 @@ __device__ __forceinline__ void put(__nv_bfloat16* p, float v) { *p = __float2bf
 
 // The thread's share of the elements [lo, hi) of g, whose vectors start at its element `head`:
 // the sum of (f g)^2, and in *any whether one of them is not zero.
-template <typename T>
+template <typename T, int PER>
 __device__ __forceinline__ float squares(const T* g, long long lo, long long hi, float f, bool* any) {
-    constexpr int VE = Vec<T>::n, NV = kCPer / VE;
+    constexpr int VE = Vec<T>::n, NV = PER / VE;
     float s0 = 0.f, s1 = 0.f;
     uint32_t bits = 0;
     const long long vecs = (hi - lo) / VE;   // lo is on a boundary
@@ -134,68 +132,102 @@ __device__ __forceinline__ float squares(const T* g, long long lo, long long hi,
 }
 
 // The elements of chunk c of a tensor of n: chunk 0 takes those before the first boundary too.
+template <int PER>
 __device__ __forceinline__ void chunk_span(long long c, int head, long long n, long long* lo,
                                            long long* hi) {
-    *lo = head + c * kCChunk;
-    *hi = *lo + kCChunk < n ? *lo + kCChunk : n;
+    *lo = head + c * (kCThreads * PER);
+    *hi = *lo + kCThreads * PER < n ? *lo + kCThreads * PER : n;
     if (*lo > n) *lo = n;
 }
 
-template <typename T>
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+__device__ __forceinline__ double warp_sum(double v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+
+// The warp's share of a chunk, on every lane (fp64 is slow here: one sum a warp and chunk).
+template <typename T, int PER>
 __device__ __forceinline__ double chunk_squares(const ClipTensor& t, int c) {
     const T* g = static_cast<const T*>(t.g);
     const int head = head_of(g, sizeof(T), t.n);
     long long lo, hi;
-    chunk_span(c, head, t.n, &lo, &hi);
+    chunk_span<PER>(c, head, t.n, &lo, &hi);
     float edge = 0.f;
     if (c == 0 && (int)threadIdx.x < head) edge = value(g + threadIdx.x);
     bool any;
-    const float s = squares(g, lo, hi, 1.f, &any) + edge * edge;
+    const float s = warp_sum(squares<T, PER>(g, lo, hi, 1.f, &any) + edge * edge);
     // 2^-60 and above: what a square lost below 2^-149 is nothing beside it
     if (s >= 0x1p-60f && s < INFINITY) return (double)s;
-    if (!any && edge == 0.f) return 0.0;
+    if (!__any_sync(0xffffffffu, any || edge != 0.f)) return 0.0;
     // squares that fp32 does not hold: with 2^90 (elements below 2^-30) or 2^-70 before the
     // elements; infinities and NaN stay
     const float f = s < 1.f ? 0x1p90f : 0x1p-70f;
-    const float again = squares(g, lo, hi, f, &any) + (edge * f) * (edge * f);
+    const float again = warp_sum(squares<T, PER>(g, lo, hi, f, &any) + (edge * f) * (edge * f));
     return (double)again * (s < 1.f ? 0x1p-180 : 0x1p140);
 }
 
-// Sum over the block in a fixed order, on every thread.
-__device__ __forceinline__ double block_sum(double v) {
-    __shared__ double part[kCThreads / 32];
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
-    __syncthreads();
-    double s = 0.0;
-    for (int i = 0; i < kCThreads / 32; ++i) s += part[i];
-    return s;
-}
-
-template <int N>
+template <int N, int PER>
 __global__ void __launch_bounds__(kCThreads) clip_norm_kernel(const __grid_constant__ ClipArgs<N> a) {
     pdl_wait();
     pdl_trigger();
+    __shared__ double part[kCThreads / 32];
+    const int lane = threadIdx.x & 31;
     double sum = 0.0;
     const int chunks = a.first[a.count];
     for (int c = blockIdx.x; c < chunks; c += gridDim.x) {
         const int i = tensor_of(a, c);
-        sum += a.f32[i] ? chunk_squares<float>(a.t[i], c - a.first[i])
-                        : chunk_squares<__nv_bfloat16>(a.t[i], c - a.first[i]);
+        const double s = a.f32[i] ? chunk_squares<float, PER>(a.t[i], c - a.first[i])
+                                  : chunk_squares<__nv_bfloat16, PER>(a.t[i], c - a.first[i]);
+        if (lane == 0) sum += s;
     }
-    sum = block_sum(sum);
-    if (threadIdx.x == 0) a.parts[blockIdx.x] = sum;
+    if (lane == 0) part[threadIdx.x >> 5] = sum;
+    __syncthreads();
+    if (threadIdx.x >= 32) return;
+    sum = warp_sum(lane < kCThreads / 32 ? part[lane] : 0.0);
+    if (lane == 0) a.parts[blockIdx.x] = sum;
 }
 
-template <typename T>
+// What the sum of squares says: the norm, the factor, and the factor as two (pre = 2^-40 apart where
+// fp32 would hold the factor in fewer bits; what that takes below fp32's normal numbers ends at zero).
+// The root is that of the sum's leading digits, in fp32.
+struct Clip {
+    float norm, factor, pre, rest;
+};
+__device__ __forceinline__ Clip clip_of(double sum, float max_norm) {
+    Clip c = {(float)sum, 1.f, 1.f, 1.f};   // 0, infinity or NaN
+    if (sum > 0.0 && sum < INFINITY) {
+        const int e = ((__double2hiint(sum) >> 20) - 1023) & ~1, h = e / 2;
+        const float root = sqrtf((float)(sum * __hiloint2double((1023 - e) << 20, 0)));   // of 1 .. 4
+        c.norm = scalbnf(root, h);
+        if (c.norm > max_norm) {
+            // (a limit of few bits is scaled before the quotient would lose its own)
+            const bool small = max_norm < 0x1p-60f;
+            const float q = (small ? max_norm * 0x1p64f : max_norm) / root;
+            const int shift = small ? -h - 64 : -h;
+            c.factor = c.rest = scalbnf(q, shift);
+            if (c.factor < 0x1p-80f) {
+                c.pre = 0x1p-40f;
+                c.rest = scalbnf(q, shift + 40);
+            }
+        }
+    }
+    return c;
+}
+
+template <typename T, int PER>
 __device__ __forceinline__ void chunk_scale(const ClipTensor& t, int c, float pre, float f) {
-    constexpr int VE = Vec<T>::n, NV = kCPer / VE;
+    constexpr int VE = Vec<T>::n, NV = PER / VE;
     const T* g = static_cast<const T*>(t.g);
     T* out = static_cast<T*>(t.out);
     const int head = head_of(g, sizeof(T), t.n);
     long long lo, hi;
-    chunk_span(c, head, t.n, &lo, &hi);
+    chunk_span<PER>(c, head, t.n, &lo, &hi);
     if (c == 0 && (int)threadIdx.x < head) put(out + threadIdx.x, value(g + threadIdx.x) * pre * f);
     const bool same = ((reinterpret_cast<uintptr_t>(out + lo)) & 15) == 0;
     const long long vecs = (hi - lo) / VE;
@@ -237,32 +269,34 @@ __device__ __forceinline__ void chunk_scale(const ClipTensor& t, int c, float pr
     if (rest < hi) put(out + rest, value(g + rest) * pre * f);
 }
 
-template <int N>
+template <int N, int PER>
 __global__ void __launch_bounds__(kCThreads) clip_scale_kernel(const __grid_constant__ ClipArgs<N> a) {
     pdl_wait();
     pdl_trigger();
-    double sum = 0.0;
-    for (int i = threadIdx.x; i < a.n_parts; i += kCThreads) sum += a.parts[i];
-    const double norm = sqrt(block_sum(sum));
-    // a norm that is not finite, or not above the limit: as they are
-    const double factor = norm > (double)a.max_norm && norm < INFINITY ? (double)a.max_norm / norm : 1.0;
-    const float f = (float)factor;
-    // a factor that fp32 would hold in fewer bits: 2^-40 of it apart (elements it takes below fp32's
-    // normal numbers end at zero)
-    const float pre = factor < 0x1p-80 ? 0x1p-40f : 1.f;
-    const float rest = (float)(factor / (double)pre);
-    if (a.norm && blockIdx.x == 0 && threadIdx.x == 0) {
-        a.norm[0] = (float)norm;
-        a.norm[1] = f;
+    __shared__ Clip shared_clip;
+    if (threadIdx.x < 32) {
+        double sum = 0.0;
+        for (int i = threadIdx.x; i < a.n_parts; i += 32) sum += a.parts[i];
+        sum = warp_sum(sum);
+        if (threadIdx.x == 0) {
+            const Clip c = clip_of(sum, a.max_norm);
+            shared_clip = c;
+            if (a.norm && blockIdx.x == 0) {
+                a.norm[0] = c.norm;
+                a.norm[1] = c.factor;
+            }
+        }
     }
+    __syncthreads();
+    const float f = shared_clip.factor, pre = shared_clip.pre, rest = shared_clip.rest;
     if (a.in_place && f == 1.f) return;
     const int chunks = a.first[a.count];
     for (int c = chunks - 1 - blockIdx.x; c >= 0; c -= gridDim.x) {
         const int i = tensor_of(a, c);
         if (a.f32[i])
-            chunk_scale<float>(a.t[i], c - a.first[i], pre, rest);
+            chunk_scale<float, PER>(a.t[i], c - a.first[i], pre, rest);
         else
-            chunk_scale<__nv_bfloat16>(a.t[i], c - a.first[i], pre, rest);
+            chunk_scale<__nv_bfloat16, PER>(a.t[i], c - a.first[i], pre, rest);
     }
 }
 
@@ -282,17 +316,18 @@ struct ClipCall {
     double* parts;
 };
 
-// Chunks of the tensors [t0, t1).
-long long chunks_of(const ClipCall& c, int t0, int t1) {
+// Chunks of the tensors [t0, t1), at most.
+long long chunks_of(const ClipCall& c, int t0, int t1, int chunk) {
     long long n = 0;
-    for (int i = t0; i < t1; ++i) n += (c.sizes[i] + kCChunk - 1) / kCChunk + 1;
+    for (int i = t0; i < t1; ++i) n += (c.sizes[i] + chunk - 1) / chunk + 1;
     return n;
 }
 
 // The launches for the tensors [t0, t0 + count): the norm's, or the product's.
-template <int N>
+template <int N, int PER>
 cudaError_t clip_launch(const ClipCall& c, int t0, int count, bool scale, double* parts, int* n_parts,
                         float* norm, cudaStream_t st) {
+    constexpr int kChunk = kCThreads * PER;
     ClipArgs<N> a;
     a.count = count;
     int chunks = 0;
@@ -307,7 +342,7 @@ cudaError_t clip_launch(const ClipCall& c, int t0, int count, bool scale, double
         const uintptr_t at = reinterpret_cast<uintptr_t>(c.grads[k]);
         const long long head = std::min<long long>((long long)((16 - (at & 15)) & 15) / es, c.sizes[k]);
         const long long body = c.sizes[k] - head;
-        chunks += (int)(body > 0 ? (body + kCChunk - 1) / kCChunk : c.sizes[k] > 0);
+        chunks += (int)(body > 0 ? (body + kChunk - 1) / kChunk : c.sizes[k] > 0);
     }
     a.first[count] = chunks;
     a.parts = scale ? c.parts : parts;
@@ -319,10 +354,10 @@ cudaError_t clip_launch(const ClipCall& c, int t0, int count, bool scale, double
     if (!scale) {
         *n_parts += grid;
         a.n_parts = 0;
-        return launch_pdl(clip_norm_kernel<N>, dim3(grid), dim3(kCThreads), 0, st, a);
+        return launch_pdl(clip_norm_kernel<N, PER>, dim3(grid), dim3(kCThreads), 0, st, a);
     }
     a.n_parts = *n_parts;
-    return launch_pdl(clip_scale_kernel<N>, dim3(grid), dim3(kCThreads), 0, st, a);
+    return launch_pdl(clip_scale_kernel<N, PER>, dim3(grid), dim3(kCThreads), 0, st, a);
 }
 
 }  // namespace
@@ -361,7 +396,8 @@ extern "C" int hcw_clip_grads(const void* const* grads, void* const* out, const 
     if (!workspace || ws_bytes < need) return HCW_ERR_WORKSPACE;
     ClipCall c = {grads, out, sizes, dtypes, count, max_norm, norm, static_cast<double*>(workspace)};
     for (int t = 0; t < count; t += kCTensors)
-        if (chunks_of(c, t, std::min(count, t + kCTensors)) > kCMaxChunks) return HCW_ERR_UNSUPPORTED;
+        if (chunks_of(c, t, std::min(count, t + kCTensors), kCThreads * 32) > kCMaxChunks)
+            return HCW_ERR_UNSUPPORTED;
     Span few[160];
     Span* s = room <= 160 ? few : new (std::nothrow) Span[room];
     if (!s) return HCW_ERR_UNSUPPORTED;
@@ -400,8 +436,12 @@ extern "C" int hcw_clip_grads(const void* const* grads, void* const* out, const 
             const int n = std::min(count - t, kCTensors);
             double* parts = c.parts + n_parts;
             float* first = scale && t == 0 ? norm : nullptr;
-            e = n <= 32 ? clip_launch<32>(c, t, n, scale, parts, &n_parts, first, st)
-                        : clip_launch<kCTensors>(c, t, n, scale, parts, &n_parts, first, st);
+            // shorter chunks while the longer ones would leave SMs with fewer than four CTAs
+            const bool few = chunks_of(c, t, t + n, kCThreads * 32) < 4ll * device_sms();
+            e = n <= 32 ? few ? clip_launch<32, 8>(c, t, n, scale, parts, &n_parts, first, st)
+                              : clip_launch<32, 32>(c, t, n, scale, parts, &n_parts, first, st)
+                : few   ? clip_launch<kCTensors, 8>(c, t, n, scale, parts, &n_parts, first, st)
+                        : clip_launch<kCTensors, 32>(c, t, n, scale, parts, &n_parts, first, st);
             if (e != cudaSuccess) return;
             ++launches;
         }
