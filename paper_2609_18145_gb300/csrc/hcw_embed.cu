@@ -7,9 +7,10 @@
 // writes V (or, added to what is there, reads and writes the rows that are named).
 //
 // Text names a few symbols thousands of times and most of them never, so the gradient goes by the
-// sorted tokens: the positions in the order of their symbols, cut into chunks of equal length, a
-// chunk's rows added by one warp for each block of columns.  A symbol whose positions lie in one
-// chunk is written there; one that reaches over a chunk's end leaves a partial sum in the
+// sorted tokens: the positions in the order of their symbols, cut into chunks of equal length.  A CTA
+// takes a chunk for a block of columns, each of its 8 warps adds an eighth of the rows, and the warps'
+// sums of a symbol that lies in several of them are joined in shared memory.  A symbol whose positions
+// lie in one chunk is written there; one that reaches over a chunk's end leaves a partial sum in the
 // workspace at each, and a last launch adds these in the order of the chunks.  No atomics on
 // numbers: the order of every sum depends on the ids and the sizes alone.
 //
@@ -22,6 +23,7 @@
 #include "hcw_ptx.cuh"
 
 #include <algorithm>
+#include <mutex>
 
 namespace hcw {
 
@@ -35,6 +37,8 @@ constexpr int kMaxRange = 65536;          // symbols of a CTA: two passes, 8 KB 
 constexpr int kMaxV = 1 << 23;
 constexpr int kMaxD = 1 << 20;
 constexpr int kSumWarps = 8;
+constexpr int kZeroBytes = 4096;          // of a bulk copy of zeros at most
+constexpr int kBulkRow = 512;             // bytes of the rows that bulk copies zero
 
 __device__ __forceinline__ float to_f32(float v) { return v; }
 __device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
@@ -65,6 +69,39 @@ __device__ __forceinline__ void load_row(const T* p, int lane, int left, float (
             v[e] = lane + 32 * e < left ? to_f32(p[lane + 32 * e]) : 0.f;
     }
 }
+
+// The lane's E elements of a row on their way: as they lie there where one load takes them.
+template <typename T, int E, bool WIDE>
+struct Row {
+    float v[E];
+    __device__ __forceinline__ void load(const T* p, int lane, int left) {
+        load_row<T, E, false>(p, lane, left, v);
+    }
+    __device__ __forceinline__ void add_to(float (&s)[E]) const {
+#pragma unroll
+        for (int e = 0; e < E; ++e) s[e] += v[e];
+    }
+};
+template <typename T, int E>
+struct Row<T, E, true> {
+    uint4 q;
+    __device__ __forceinline__ void load(const T* p, int lane, int left) {
+        q = make_uint4(0, 0, 0, 0);
+        if (lane * E < left) q = *reinterpret_cast<const uint4*>(p + lane * E);
+    }
+    __device__ __forceinline__ void add_to(float (&s)[E]) const {
+        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (E == 8) {
+                s[2 * i] += __uint_as_float(w[i] << 16);
+                s[2 * i + 1] += __uint_as_float(w[i] & 0xffff0000u);
+            } else {
+                s[i] += __uint_as_float(w[i]);
+            }
+        }
+    }
+};
 
 // The lane's E elements of an output row (of type O, rounded here).
 template <typename O, int E, bool WIDE>
@@ -126,8 +163,9 @@ __global__ void __launch_bounds__(256) embed_fwd_kernel(const int* ids, const T*
 struct SortArgs {
     const int* ids;
     int T, V, range;          // symbols of a CTA
-    int* key[2];              // [T] symbols and [T] positions, two of each
-    int* pos[2];
+    int split;                // CTAs of a range, which share the tokens (1, 2, 4 or 8)
+    int* key[3];              // [T] symbols and [T] positions: two for the passes, and the sorted ones
+    int* pos[3];
     int* count;               // tokens that name a symbol
     void* dE;                 // null: no zeros
     size_t row_bytes;
@@ -159,103 +197,222 @@ __device__ __forceinline__ int block_prefix(int v, int* scratch, int* total) {
     __syncthreads();   // scratch's last use
     if (lane == 31) scratch[warp] = s;
     __syncthreads();
-    int before = 0, all = 0;
-    for (int i = 0; i < kSortWarps; ++i) {
-        const int c = scratch[i];
-        if (i < warp) before += c;
-        all += c;
+    int w = scratch[lane];   // every warp: the warps' sums, added up
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int u = __shfl_up_sync(0xffffffffu, w, o);
+        if (lane >= o) w += u;
     }
-    *total = all;
-    return before + s - v;
+    *total = __shfl_sync(0xffffffffu, w, 31);
+    const int before = __shfl_sync(0xffffffffu, w, (warp + 31) & 31);
+    return (warp ? before : 0) + s - v;
 }
 
+__device__ __forceinline__ bool is_named(const uint32_t* named, int i) { return named[i >> 5] >> (i & 31) & 1; }
+
+// One warp, rows of kBulkRow bytes or more: starts the zeros of every row of [z0, z1) that is not
+// named (flags from symbol lo on), a lane a row.  Bulk copies take what lies between 16-byte boundaries, plain stores the edges.
+__device__ __forceinline__ void start_zeros(const SortArgs& a, int z0, int z1, int lo,
+                                            const uint32_t* named, const uint4* zeros) {
+    for (int v = z0 + (threadIdx.x & 31); v < z1; v += 32) {
+        if (is_named(named, v - lo)) continue;
+        char* p = static_cast<char*>(a.dE) + (size_t)v * a.row_bytes;
+        char* const end = p + a.row_bytes;
+        for (; reinterpret_cast<uintptr_t>(p) & 15; p += 2) *reinterpret_cast<short*>(p) = 0;
+        size_t left = (size_t)(end - p) & ~(size_t)15;
+        while (left) {
+            const uint32_t bytes = left < kZeroBytes ? (uint32_t)left : (uint32_t)kZeroBytes;
+            asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(p),
+                         "r"(smem_u32(zeros)), "r"(bytes)
+                         : "memory");
+            p += bytes;
+            left -= bytes;
+        }
+        for (; p < end; p += 2) *reinterpret_cast<short*>(p) = 0;
+    }
+    bulk_commit();
+}
+
+// All warps, shorter rows: the same with plain stores, a warp a row.
+__device__ __forceinline__ void zero_rows(const SortArgs& a, int z0, int z1, int lo, const uint32_t* named) {
+    const int lane = threadIdx.x & 31;
+    for (int v = z0 + (threadIdx.x >> 5); v < z1; v += kSortWarps) {
+        if (is_named(named, v - lo)) continue;
+        char* const p = static_cast<char*>(a.dE) + (size_t)v * a.row_bytes;
+        const int bytes = (int)a.row_bytes;
+        if (bytes % 16 == 0) {
+            if (16 * lane < bytes) *reinterpret_cast<uint4*>(p + 16 * lane) = make_uint4(0, 0, 0, 0);
+        } else {
+            for (int i = 2 * lane; i < bytes; i += 64) *reinterpret_cast<short*>(p + i) = 0;
+        }
+    }
+}
+
+// SPLIT: a range has several CTAs, each with some of the warps' runs of tokens (a frequent symbol's
+// tokens would keep one CTA busy long after the others).  Each counts, for every symbol of the range,
+// the tokens before its share, in it and after it, and so knows where its own of a symbol go.
+template <bool SPLIT>
 __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const SortArgs a) {
-    __shared__ int hist[kDigits * kSortWarps];
+    extern __shared__ int counts[];                        // SPLIT: [3][range]
+    __shared__ __align__(16) int hist[kDigits * kSortWarps];
     __shared__ uint32_t named[kMaxRange / 32];
     __shared__ int scratch[kSortWarps];
+    __shared__ __align__(16) uint4 zeros[kZeroBytes / 16];
+    if (threadIdx.x < kZeroBytes / 16) zeros[threadIdx.x] = make_uint4(0, 0, 0, 0);
+    fence_proxy_async_smem();   // before the barriers that come first, for the bulk copies that read them
     pdl_wait();
     pdl_trigger();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int lo = blockIdx.x * a.range, hi = min(a.V, lo + a.range);
-    for (int i = threadIdx.x; i < (a.range + 31) / 32; i += kSortThreads) named[i] = 0;
+    const int lo = blockIdx.x / a.split * a.range, hi = min(a.V, lo + a.range);
+    const int part = blockIdx.x % a.split, kind = warp * a.split / kSortWarps;   // the warp's share
+    int* const tally = counts + (kind < part ? 0 : kind == part ? 1 : 2) * a.range;
+    if (SPLIT)
+        for (int i = threadIdx.x; i < 3 * a.range; i += kSortThreads) counts[i] = 0;
+    else
+        for (int i = threadIdx.x; i < (a.range + 31) / 32; i += kSortThreads) named[i] = 0;
     __syncthreads();
     // each warp goes through a run of ids, four a lane at a time
-    const int run = ((a.T + kSortThreads - 1) / kSortThreads) * 32;   // of a warp, before rounding to 128
-    const long long w0 = (long long)warp * ((run + 127) / 128 * 128);
-    const long long w1 = min((long long)a.T, w0 + (run + 127) / 128 * 128);
-    int below = 0, mine = 0;
-    for (long long i = w0 + 4 * lane; i < w1; i += 128) {
-        int id[4];
-        ids_at(a.ids, i, w1, id);
+    const int run = ((a.T + kSortThreads - 1) / kSortThreads * 32 + 127) / 128 * 128;   // of a warp
+    const long long w0 = (long long)warp * run, w1 = min((long long)a.T, w0 + run);
+    int below = 0, mine = 0, earlier = 0;
+    for (long long i0 = w0; i0 < w1; i0 += 512) {
+        int id[4][4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            below += id[e] >= 0 && id[e] < lo;
-            if (id[e] >= lo && id[e] < hi) {
-                ++mine;
-                atomicOr(&named[(id[e] - lo) >> 5], 1u << ((id[e] - lo) & 31));
+        for (int q = 0; q < 4; ++q) ids_at(a.ids, i0 + 128 * q + 4 * lane, w1, id[q]);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int v = id[q][e];
+                below += v >= 0 && v < lo;
+                if (v >= lo && v < hi) {
+                    ++mine;
+                    if (SPLIT) {
+                        atomicAdd(&tally[v - lo], 1);
+                    } else {
+                        // (a frequent symbol is looked for before it is marked again)
+                        const uint32_t bit = 1u << ((v - lo) & 31);
+                        if (!(*(volatile uint32_t*)&named[(v - lo) >> 5] & bit))
+                            atomicOr(&named[(v - lo) >> 5], bit);
+                    }
+                }
+                if (v >= a.V) atomicExch(&g_error_word, kErrInvalid);
             }
-            if (id[e] >= a.V) atomicExch(&g_error_word, kErrInvalid);
-        }
     }
-    int m, base;
+    if (SPLIT && kind != part) {
+        if (kind < part) earlier = mine;
+        mine = 0;
+    }
+    int m, base, all = 0;
     (void)block_prefix(below, scratch, &base);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
     int at = block_prefix(lane == 0 ? mine : 0, scratch, &m);
     at = __shfl_sync(0xffffffffu, at, 0);
-    if (threadIdx.x == 0 && hi == a.V) *a.count = base + m;
+    // (the prefixes were behind a barrier: the counts are complete)
+    int list = base;     // where the CTA's lists lie
+    if (SPLIT) {
+        (void)block_prefix(earlier, scratch, &list);
+        list += base;
+        for (int i = threadIdx.x; i < (a.range + 31) / 32 * 32; i += kSortThreads) {
+            const bool on = i < a.range && (counts[i] | counts[a.range + i] | counts[2 * a.range + i]);
+            const uint32_t word = __ballot_sync(0xffffffffu, on);
+            if (lane == 0) named[i >> 5] = word;
+        }
+        // a symbol's place in the whole order, less that among the CTA's own
+        const int per = (a.range + kSortThreads - 1) / kSortThreads;
+        const int v0 = min((int)threadIdx.x * per, a.range), v1 = min(v0 + per, a.range);
+        int total = 0, own = 0;
+        for (int v = v0; v < v1; ++v) {
+            own += counts[a.range + v];
+            total += counts[v] + counts[a.range + v] + counts[2 * a.range + v];
+        }
+        int unused, before_all = block_prefix(total, scratch, &all);
+        int before_own = block_prefix(own, scratch, &unused);
+        for (int v = v0; v < v1; ++v) {
+            const int c0 = counts[v], c1 = counts[a.range + v], c2 = counts[2 * a.range + v];
+            counts[v] = base + before_all + c0 - before_own;
+            before_all += c0 + c1 + c2;
+            before_own += c1;
+        }
+        __syncthreads();
+    } else {
+        all = m;
+    }
+    if (threadIdx.x == 0 && hi == a.V && part == 0) *a.count = base + all;
+    if (a.dE) {
+        // the CTAs of a range share its rows
+        const int share = (a.range + a.split - 1) / a.split;
+        const int z0 = min(lo + part * share, hi), z1 = min(z0 + share, hi);
+        if (a.row_bytes >= kBulkRow) {
+            if (warp == kSortWarps - 1) start_zeros(a, z0, z1, lo, named, zeros);
+        } else {
+            zero_rows(a, z0, z1, lo, named);
+        }
+    }
     // its own, in order
     if (m > 0) {
-        int *key = a.key[0] + base, *pos = a.pos[0] + base;
-        int *key_to = a.key[1] + base, *pos_to = a.pos[1] + base;
-        for (long long i0 = w0; i0 < w1; i0 += 128) {
-            const long long i = i0 + 4 * lane;
-            int id[4];
-            uint32_t have[4];
-            ids_at(a.ids, i, w1, id);
-            int before = 0;
+        int *key = a.key[0] + list, *pos = a.pos[0] + list;
+        int *key_to = a.key[1] + list, *pos_to = a.pos[1] + list;
+        for (long long i0 = w0; i0 < w1 && kind == part; i0 += 512) {
+            int id[4][4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                have[e] = __ballot_sync(0xffffffffu, id[e] >= lo && id[e] < hi);
-                before += __popc(have[e] & ((1u << lane) - 1));
-            }
-            int k = at + before;
+            for (int q = 0; q < 4; ++q) ids_at(a.ids, i0 + 128 * q + 4 * lane, w1, id[q]);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if (id[e] >= lo && id[e] < hi) {
-                    key[k] = id[e];
-                    pos[k] = (int)(i + e);
-                    ++k;
+            for (int q = 0; q < 4; ++q) {
+                bool in[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) in[e] = id[q][e] >= lo && id[q][e] < hi;
+                if (!__any_sync(0xffffffffu, in[0] || in[1] || in[2] || in[3])) continue;
+                uint32_t have[4];
+                int before = 0;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    have[e] = __ballot_sync(0xffffffffu, in[e]);
+                    before += __popc(have[e] & ((1u << lane) - 1));
                 }
-                at += __popc(have[e]);
+                int k = at + before;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (in[e]) {
+                        key[k] = id[q][e];
+                        pos[k] = (int)(i0 + 128 * q + 4 * lane + e);
+                        ++k;
+                    }
+                    at += __popc(have[e]);
+                }
             }
         }
         const int own = ((m + kSortThreads - 1) / kSortThreads) * 32;   // of a warp
         const int m0 = min(m, warp * own), m1 = min(m, m0 + own);
         for (int shift = 0; shift == 0 || (a.range - 1) >> shift; shift += 8) {
-            for (int i = threadIdx.x; i < kDigits * kSortWarps; i += kSortThreads) hist[i] = 0;
+            const bool last = !((a.range - 1) >> (shift + 8));
+            // (counters of the digits that occur: 8 a thread, two vectors)
+            const int used = min(kDigits, a.range) * kSortWarps;
+            int4* const my = reinterpret_cast<int4*>(hist) + 2 * threadIdx.x;
+            const bool in = 8 * (int)threadIdx.x < used;
+            if (in) my[0] = my[1] = make_int4(0, 0, 0, 0);
             __syncthreads();   // and the list is there
             for (int i = m0 + lane; i < m1; i += 32)
                 atomicAdd(&hist[(((key[i] - lo) >> shift) & (kDigits - 1)) * kSortWarps + warp], 1);
             __syncthreads();
             // places: by digit, then by warp
-            int c[kDigits * kSortWarps / kSortThreads], sum = 0, all;
-#pragma unroll
-            for (int j = 0; j < kDigits * kSortWarps / kSortThreads; ++j) {
-                c[j] = hist[threadIdx.x * (kDigits * kSortWarps / kSortThreads) + j];
-                sum += c[j];
+            int4 c = make_int4(0, 0, 0, 0), e = c;
+            if (in) {
+                c = my[0];
+                e = my[1];
             }
-            int p = block_prefix(sum, scratch, &all);
-#pragma unroll
-            for (int j = 0; j < kDigits * kSortWarps / kSortThreads; ++j) {
-                hist[threadIdx.x * (kDigits * kSortWarps / kSortThreads) + j] = p;
-                p += c[j];
+            int unused, p = block_prefix(c.x + c.y + c.z + c.w + e.x + e.y + e.z + e.w, scratch, &unused);
+            const int q = p + c.x + c.y + c.z + c.w;
+            if (in) {
+                my[0] = make_int4(p, p + c.x, p + c.x + c.y, p + c.x + c.y + c.z);
+                my[1] = make_int4(q, q + e.x, q + e.x + e.y, q + e.x + e.y + e.z);
             }
             __syncthreads();
             for (int i0 = m0; i0 < m1; i0 += 32) {
                 const int i = i0 + lane;
                 const bool on = i < m1;
-                const int k = on ? key[i] : 0, q = on ? pos[i] : 0;
+                const int k = on ? key[i] : 0, t = on ? pos[i] : 0;
                 const int d = on ? ((k - lo) >> shift) & (kDigits - 1) : kDigits;
                 const uint32_t same = __match_any_sync(0xffffffffu, d);
                 const int rank = __popc(same & ((1u << lane) - 1));
@@ -263,9 +420,13 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const SortArgs
                 __syncwarp();
                 if (on && rank == 0) hist[d * kSortWarps + warp] += __popc(same);
                 __syncwarp();
-                if (on) {
+                if (on && last) {
+                    const int to = place + (SPLIT ? counts[k - lo] : base);
+                    a.key[2][to] = k;
+                    a.pos[2][to] = t;
+                } else if (on) {
                     key_to[place] = k;
-                    pos_to[place] = q;
+                    pos_to[place] = t;
                 }
             }
             __syncthreads();
@@ -277,24 +438,7 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const SortArgs
             pos_to = t;
         }
     }
-    // rows that no token names
-    if (a.dE) {
-        char* rows = static_cast<char*>(a.dE);
-        const bool wide = a.row_bytes % 16 == 0;
-        for (int v = lo + warp; v < hi; v += kSortWarps) {
-            if (named[(v - lo) >> 5] >> ((v - lo) & 31) & 1) continue;
-            char* r = rows + (size_t)v * a.row_bytes;
-            if (wide)
-                for (size_t i = 16 * lane; i < a.row_bytes; i += 512)
-                    *reinterpret_cast<uint4*>(r + i) = make_uint4(0, 0, 0, 0);
-            else if (a.row_bytes % 4 == 0)
-                for (size_t i = 4 * lane; i < a.row_bytes; i += 128)
-                    *reinterpret_cast<uint32_t*>(r + i) = 0;
-            else
-                for (size_t i = 2 * lane; i < a.row_bytes; i += 64)
-                    *reinterpret_cast<unsigned short*>(r + i) = 0;
-        }
-    }
+    bulk_wait<0>();   // (the threads that copied zeros)
 }
 
 // ------------------------------------------------------------------ the sums
@@ -305,7 +449,7 @@ struct SumArgs {
     const void* dx;
     void* dE;
     float* part;          // [chunks][2][d]: of the run that came in from before, and of the one that goes on
-    int d;
+    int d, T;
     int chunk_log2;       // tokens of a chunk
     int chunks, tiles;    // chunks at most, blocks of columns
     float scale;
@@ -337,63 +481,106 @@ __device__ __forceinline__ void write_sum(const SumArgs& a, int symbol, int col,
     store_row<O, E, WIDE>(row, lane, left, v);
 }
 
-// A warp adds the rows of one chunk, 32 E columns of them, eight rows on their way at once.
+// A CTA adds the rows of one chunk, 32 E columns of them, each warp an eighth.
 template <typename T, typename O, int E, bool WIDE>
 __global__ void __launch_bounds__(32 * kSumWarps) embed_sum_kernel(const SumArgs a) {
+    __shared__ __align__(16) float head[kSumWarps][32 * E], tail[kSumWarps][32 * E];
+    __shared__ int state[kSumWarps], head_symbol[kSumWarps];
+    constexpr int kRows = WIDE || E == 4 ? 8 : 4;   // on their way at once
+    // of a warp: has a run that came in from before it, which goes on behind it; another one that does
+    constexpr int kFrom = 1, kThrough = 2, kOn = 4;
     pdl_wait();
     pdl_trigger();
-    const int lane = threadIdx.x & 31;
-    const long long item = (long long)blockIdx.x * kSumWarps + (threadIdx.x >> 5);
-    const int chunk = (int)(item / a.tiles), col = (int)(item % a.tiles) * (32 * E);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int chunk = blockIdx.x / a.tiles, col = blockIdx.x % a.tiles * (32 * E);
+    const long long chunk0 = (long long)chunk << a.chunk_log2;
+    const int share = 1 << (a.chunk_log2 - 3);   // a warp's, 32 at most
+    const long long first = chunk0 + warp * share;
+    // everything that depends on the place alone (behind the count the lists hold nothing of use)
     const int count = *a.count;
-    const long long first = (long long)chunk << a.chunk_log2;
-    if (chunk >= a.chunks || first >= count) return;
-    const int n = (int)min((long long)(1 << a.chunk_log2), count - first);
-    const int before = first > 0 ? a.key[first - 1] : -1;
-    const int after = first + n < count ? a.key[first + n] : -1;
+    const int at = (int)min(first + lane, (long long)a.T - 1);
+    int key = a.key[at];
+    const int pos = a.pos[at];
+    const int before = first > 0 && first - 1 < a.T ? a.key[first - 1] : -1;
+    const int behind = first + share < a.T ? a.key[first + share] : -1;
+    if (chunk0 >= count) return;
+    const int n = (int)max(0ll, min((long long)share, count - first));
     const T* dx = static_cast<const T*>(a.dx) + col;
     const int left = a.d - col;
-    float* part = a.part + ((size_t)chunk * 2 * a.d + col);
-    float s[E];
+    if (n > 0) {
+        if (lane >= n) key = -1;
+        const int after = first + n < count ? behind : -1;
+        float s[E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) s[e] = 0.f;
-    bool from_before = a.key[first] == before;
-    for (int i0 = 0; i0 < n; i0 += 32) {
-        const int k = i0 + lane;
-        const int key = k < n ? a.key[first + k] : -1, pos = k < n ? a.pos[first + k] : 0;
-        // the symbol behind the lane's: the next lane's, or the next 32 tokens' first
-        const int next_first = i0 + 32 < n ? a.key[first + i0 + 32] : after;
+        for (int e = 0; e < E; ++e) s[e] = 0.f;
+        const int first_symbol = __shfl_sync(0xffffffffu, key, 0);
+        bool from_before = first > 0 && first_symbol == before;
+        int flags = 0;
+        // the lanes whose symbol is another one behind them
         int next = __shfl_down_sync(0xffffffffu, key, 1);
-        if (lane == 31 || k + 1 >= n) next = next_first;
-        const uint32_t last = __ballot_sync(0xffffffffu, k < n && (next != key || k + 1 == n));
-        const int rows = min(32, n - i0);
-        for (int r0 = 0; r0 < rows; r0 += 8) {
-            float v[8][E];
+        if (lane + 1 >= n) next = after;
+        const uint32_t last = __ballot_sync(0xffffffffu, lane < n && (next != key || lane + 1 == n));
+        for (int r0 = 0; r0 < n; r0 += kRows) {
+            Row<T, E, WIDE> v[kRows];
 #pragma unroll
-            for (int r = 0; r < 8; ++r) {
+            for (int r = 0; r < kRows; ++r) {
                 const int t = __shfl_sync(0xffffffffu, pos, (r0 + r) & 31);
-                load_row<T, E, WIDE>(dx + (size_t)t * a.d, lane, r0 + r < rows ? left : 0, v[r]);
+                v[r].load(dx + (size_t)(r0 + r < n ? t : 0) * a.d, lane, r0 + r < n ? left : 0);
             }
 #pragma unroll
-            for (int r = 0; r < 8; ++r) {
-                if (r0 + r >= rows) break;
-#pragma unroll
-                for (int e = 0; e < E; ++e) s[e] += v[r][e];
+            for (int r = 0; r < kRows; ++r) {
+                if (r0 + r >= n) break;
+                v[r].add_to(s);
                 if (!(last >> (r0 + r) & 1)) continue;
                 const int symbol = __shfl_sync(0xffffffffu, key, r0 + r);
-                const bool goes_on = i0 + r0 + r + 1 == n && after == symbol;
-                if (from_before)
-                    store_row<float, E, WIDE>(part, lane, left, s);
-                else if (goes_on)
-                    store_row<float, E, WIDE>(part + a.d, lane, left, s);
-                else
+                const bool goes_on = r0 + r + 1 == n && after == symbol;
+                if (from_before || goes_on) {
+                    float* const to = from_before ? head[warp] : tail[warp];
+                    flags |= from_before ? (goes_on ? kFrom | kThrough : kFrom) : kOn;
+#pragma unroll
+                    for (int e = 0; e < E; ++e) to[WIDE ? lane * E + e : lane + 32 * e] = s[e];
+                } else {
                     write_sum<O, E, WIDE>(a, symbol, col, lane, s);
+                }
                 from_before = false;
 #pragma unroll
                 for (int e = 0; e < E; ++e) s[e] = 0.f;
             }
         }
+        if (lane == 0) {
+            state[warp] = flags;
+            head_symbol[warp] = first_symbol;
+        }
+    } else if (lane == 0) {
+        state[warp] = 0;
     }
+    __syncthreads();
+    // a thread a column: the runs over several warps, or over an end of the chunk
+    const int c = threadIdx.x;
+    if (c >= 32 * E || c >= left) return;
+    float* const part = a.part + (size_t)chunk * 2 * a.d + col + c;
+    float s = 0.f;
+    bool open = state[0] & kFrom, came = open;   // a run is under way, and was before the chunk
+    for (int w = 0; w < kSumWarps; ++w) {
+        const int f = state[w];
+        if (f & kFrom) {
+            s += head[w][c];
+            if (!(f & kThrough)) {
+                if (came) {
+                    part[0] = s;
+                } else {
+                    O* const to = static_cast<O*>(a.dE) + (size_t)head_symbol[w] * a.d + col + c;
+                    put(to, a.add ? fmaf(a.scale, s, to_f32(*to)) : a.scale * s);
+                }
+                open = came = false;
+            }
+        }
+        if (f & kOn) {
+            s = tail[w][c];
+            open = true;
+        }
+    }
+    if (open) part[came ? 0 : a.d] = s;
 }
 
 // A run over several chunks: the warp of the chunk it starts in adds the parts, in order.
@@ -407,10 +594,11 @@ __global__ void __launch_bounds__(32 * kSumWarps) embed_join_kernel(const SumArg
     const int count = *a.count;
     const int size = 1 << a.chunk_log2;
     const long long first = (long long)chunk << a.chunk_log2;
-    if (chunk >= a.chunks || first + size >= count) return;   // no chunk behind it
-    const int symbol = a.key[first + size - 1];
-    if (a.key[first + size] != symbol) return;
-    if (a.key[first] == symbol && first > 0 && a.key[first - 1] == symbol) return;   // started before
+    if (chunk >= a.chunks || first + size >= a.T) return;   // no chunk behind it
+    const int symbol = a.key[first + size - 1], behind = a.key[first + size], start = a.key[first],
+              before = first > 0 ? a.key[first - 1] : -1;
+    if (first + size >= count || behind != symbol) return;
+    if (first > 0 && start == symbol && before == symbol) return;   // started before
     // the chunks behind it that the run reaches into
     int more = 0;
     for (;;) {
@@ -442,10 +630,10 @@ __global__ void __launch_bounds__(32 * kSumWarps) embed_join_kernel(const SumArg
         }
     };
     load(part + a.d, s);
-    for (int j0 = 0; j0 < more; j0 += 4) {
-        float v[4][E];
+    for (int j0 = 0; j0 < more; j0 += 8) {
+        float v[8][E];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < 8; ++j) {
             if (j0 + j < more) {
                 load(part + (size_t)(j0 + j + 1) * 2 * a.d, v[j]);
             } else {
@@ -454,7 +642,7 @@ __global__ void __launch_bounds__(32 * kSumWarps) embed_join_kernel(const SumArg
             }
         }
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < 8; ++j)
             if (j0 + j < more) {
 #pragma unroll
                 for (int e = 0; e < E; ++e) s[e] += v[j][e];
@@ -466,16 +654,17 @@ __global__ void __launch_bounds__(32 * kSumWarps) embed_join_kernel(const SumArg
 // ------------------------------------------------------------------ host
 size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
 
-// Tokens of a chunk: 8 to 256, so that the chunks' warps fill the machine about once.
+// Tokens of a chunk: 64 to 256, as few as leave every SM eight CTAs at most, where that can be.
+constexpr int kChunkMin = 6, kChunkMax = 8;
 int chunk_log2_of(int T, int tiles, int sms) {
-    int l = 3;
-    while (l < 8 && ((long long)T * tiles >> (l + 1)) >= 16ll * sms) ++l;
+    int l = kChunkMin;
+    while (l < kChunkMax && ((long long)T * tiles >> l) >= 8ll * sms) ++l;
     return l;
 }
 
 struct BwdPlan {
     int tiles, chunk_log2, chunks;
-    size_t key[2], pos[2], count, part, bytes;
+    size_t key[3], pos[3], count, part, bytes;
 };
 
 // The workspace's parts.  Chunks grow with T, so that a shorter batch's parts may be more of
@@ -488,7 +677,7 @@ BwdPlan bwd_plan(int T, int d, int elems) {
     p.chunks = (int)(((long long)T + (1 << p.chunk_log2) - 1) >> p.chunk_log2);
     const size_t list = up((size_t)T * 4);
     size_t at = 0;
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < 3; ++i) {
         p.key[i] = at;
         at += list;
         p.pos[i] = at;
@@ -509,15 +698,15 @@ size_t bwd_ws_bytes(int T, int d) {
     for (int elems = 4; elems <= 8; elems += 4) {
         const int tiles = (d + 32 * elems - 1) / (32 * elems);
         long long parts = 0;
-        for (int l = 3; l <= 8; ++l) {
+        for (int l = kChunkMin; l <= kChunkMax; ++l) {
             // the longest batch with chunks of 2^l: one token fewer than takes the next size
-            const long long next = ((16ll * sms << (l + 1)) + tiles - 1) / tiles;
-            const long long longest = l == 8 || next > T ? T : next - 1;
+            const long long next = ((8ll * sms << l) + tiles - 1) / tiles;
+            const long long longest = l == kChunkMax || next > T ? T : next - 1;
             if (longest > 0) parts = std::max(parts, (longest + (1 << l) - 1) >> l);
         }
         most = std::max(most, (size_t)parts * 2 * d * 4);
     }
-    return 4 * up((size_t)T * 4) + 256 + most;
+    return 6 * up((size_t)T * 4) + 256 + most;
 }
 
 template <typename T, int E, bool WIDE>
@@ -536,31 +725,56 @@ cudaError_t fwd(const int* ids, const void* table, int tokens, int V, int d, flo
                       (long long)tokens, V, d, scale, static_cast<T*>(x));
 }
 
+constexpr int kSplitSmem = 160 * 1024;    // of counts at most
+
+// The ranges, and the CTAs of each: eight once there are tokens enough for a frequent symbol's share
+// of them to be worth it (32000 symbols, 16384 tokens, d = 512: 41 us with one, 34 with eight), fewer where a range's counts would not fit.
+cudaError_t launch_sort(SortArgs& a, cudaStream_t st) {
+    const int sms = device_sms();
+    a.split = a.T > 8192 ? 8 : 1;
+    const auto range = [&]() { return (int)(((long long)a.V * a.split + sms - 1) / sms); };
+    while (a.split > 1 && range() * 12ll > kSplitSmem) a.split /= 2;
+    a.range = range();
+    const dim3 grid((unsigned)((a.V + a.range - 1) / a.range * a.split)), block(kSortThreads);
+    if (a.split == 1) return launch_pdl(embed_sort_kernel<false>, grid, block, 0, st, a);
+    static std::once_flag once[64];
+    static cudaError_t set_err[64];
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+    std::call_once(once[dev], [&] {
+        set_err[dev] = cudaFuncSetAttribute(embed_sort_kernel<true>,
+                                            cudaFuncAttributeMaxDynamicSharedMemorySize, kSplitSmem);
+    });
+    if (set_err[dev] != cudaSuccess) return set_err[dev];
+    return launch_pdl(embed_sort_kernel<true>, grid, block, (size_t)a.range * 12, st, a);
+}
+
 template <typename T, typename O, int E, bool WIDE>
 cudaError_t bwd(SortArgs& so, SumArgs& su, int tokens, char* ws, cudaStream_t st, int* launches) {
     const BwdPlan p = bwd_plan(tokens, su.d, E);
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < 3; ++i) {
         so.key[i] = reinterpret_cast<int*>(ws + p.key[i]);
         so.pos[i] = reinterpret_cast<int*>(ws + p.pos[i]);
     }
     so.count = reinterpret_cast<int*>(ws + p.count);
-    const int last = so.range > kDigits ? 0 : 1;   // after two passes, or one
-    su.key = so.key[last];
-    su.pos = so.pos[last];
+    su.key = so.key[2];
+    su.pos = so.pos[2];
     su.count = so.count;
     su.part = reinterpret_cast<float*>(ws + p.part);
     su.chunk_log2 = p.chunk_log2;
     su.chunks = p.chunks;
     su.tiles = p.tiles;
-    const int owners = (so.V + so.range - 1) / so.range;
-    cudaError_t e = launch_pdl(embed_sort_kernel, dim3(owners), dim3(kSortThreads), 0, st, so);
+    cudaError_t e = launch_sort(so, st);
     if (e != cudaSuccess) return e;
     ++*launches;
-    const dim3 grid((unsigned)(((long long)p.chunks * p.tiles + kSumWarps - 1) / kSumWarps));
-    e = launch_pdl(embed_sum_kernel<T, O, E, WIDE>, grid, dim3(32 * kSumWarps), 0, st, su);
+    const long long items = (long long)p.chunks * p.tiles;
+    e = launch_pdl(embed_sum_kernel<T, O, E, WIDE>, dim3((unsigned)items), dim3(32 * kSumWarps), 0, st, su);
     if (e != cudaSuccess) return e;
     ++*launches;
-    e = launch_pdl(embed_join_kernel<T, O, E, WIDE>, grid, dim3(32 * kSumWarps), 0, st, su);
+    e = launch_pdl(embed_join_kernel<T, O, E, WIDE>, dim3((unsigned)((items + kSumWarps - 1) / kSumWarps)),
+                   dim3(32 * kSumWarps), 0, st, su);
     if (e != cudaSuccess) return e;
     ++*launches;
     return cudaSuccess;
@@ -639,19 +853,18 @@ extern "C" int hcw_embed_bwd(const int* ids, const void* dx, int T, int V, int d
         if (accumulate) return HCW_OK;
         return cudaMemsetAsync(dE, 0, ob, st) == cudaSuccess ? HCW_OK : HCW_ERR_CUDA;
     }
-    const int sms = device_sms();
-    if ((V + sms - 1) / sms > kMaxRange) return HCW_ERR_UNSUPPORTED;
+    if ((V + device_sms() - 1) / device_sms() > kMaxRange) return HCW_ERR_UNSUPPORTED;
     SortArgs so = {};
     so.ids = ids;
     so.T = T;
     so.V = V;
-    so.range = (V + sms - 1) / sms;
     so.dE = accumulate ? nullptr : dE;
     so.row_bytes = (size_t)d * oes;
     SumArgs su = {};
     su.dx = dx;
     su.dE = dE;
     su.d = d;
+    su.T = T;
     su.scale = scale;
     su.add = accumulate;
     int launches = 0;
