@@ -14,10 +14,9 @@
 // workspace at each, and a last launch adds these in the order of the chunks.  No atomics on
 // numbers: the order of every sum depends on the ids and the sizes alone.
 //
-// The sort is one launch without any exchange between its CTAs.  Each owns a range of symbols and
-// goes through all ids: it counts those of smaller symbols (where its own begin in the sorted
-// order) and collects its own in their order; then it sorts its own, 8 bits of the symbol a pass,
-// each warp counting and placing a run of them.
+// The sort is one launch without any exchange between its CTAs.  Each owns a range of symbols and goes
+// through all ids: it counts those of smaller symbols, where its own begin in the sorted order, and
+// its own by symbol.  The rows of symbols that do not occur are zeroed on the way, by bulk copies.
 #include "hcw.h"
 #include "hcw_internal.h"
 #include "hcw_ptx.cuh"
@@ -38,7 +37,6 @@ constexpr int kMaxV = 1 << 23;
 constexpr int kMaxD = 1 << 20;
 constexpr int kSumWarps = 8;
 constexpr int kZeroBytes = 4096;          // of a bulk copy of zeros at most
-constexpr int kBulkRow = 512;             // bytes of the rows that bulk copies zero
 
 __device__ __forceinline__ float to_f32(float v) { return v; }
 __device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
@@ -163,7 +161,6 @@ __global__ void __launch_bounds__(256) embed_fwd_kernel(const int* ids, const T*
 struct SortArgs {
     const int* ids;
     int T, V, range;          // symbols of a CTA
-    int split;                // CTAs of a range, which share the tokens (1, 2, 4 or 8)
     int* key[3];              // [T] symbols and [T] positions: two for the passes, and the sorted ones
     int* pos[3];
     int* count;               // tokens that name a symbol
@@ -208,73 +205,153 @@ __device__ __forceinline__ int block_prefix(int v, int* scratch, int* total) {
     return (warp ? before : 0) + s - v;
 }
 
-__device__ __forceinline__ bool is_named(const uint32_t* named, int i) { return named[i >> 5] >> (i & 31) & 1; }
-
-// One warp, rows of kBulkRow bytes or more: starts the zeros of every row of [z0, z1) that is not
-// named (flags from symbol lo on), a lane a row.  Bulk copies take what lies between 16-byte boundaries, plain stores the edges.
+// `warps` warps, this one being the w-th: start the zeros of the rows of [z0, z1) that are not named
+// (flags from symbol lo on).  Rows of whole 32-byte sectors by bulk copies, a row a lane; others by
+// plain stores, a row a warp (4099 tokens, 32003 x 777 fp32: 39 us, by bulk copies between 16-byte
+// boundaries 41).
 __device__ __forceinline__ void start_zeros(const SortArgs& a, int z0, int z1, int lo,
-                                            const uint32_t* named, const uint4* zeros) {
-    for (int v = z0 + (threadIdx.x & 31); v < z1; v += 32) {
-        if (is_named(named, v - lo)) continue;
-        char* p = static_cast<char*>(a.dE) + (size_t)v * a.row_bytes;
-        char* const end = p + a.row_bytes;
-        for (; reinterpret_cast<uintptr_t>(p) & 15; p += 2) *reinterpret_cast<short*>(p) = 0;
-        size_t left = (size_t)(end - p) & ~(size_t)15;
-        while (left) {
-            const uint32_t bytes = left < kZeroBytes ? (uint32_t)left : (uint32_t)kZeroBytes;
-            asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(p),
-                         "r"(smem_u32(zeros)), "r"(bytes)
-                         : "memory");
-            p += bytes;
-            left -= bytes;
+                                            const uint32_t* named, const uint4* source, int w, int warps) {
+    const auto is_named = [&](int v) { return named[(v - lo) >> 5] >> ((v - lo) & 31) & 1; };
+    const int lane = threadIdx.x & 31;
+    if (a.row_bytes % 32) {
+        for (int v = z0 + w; v < z1; v += warps) {
+            if (is_named(v)) continue;
+            char* const p = static_cast<char*>(a.dE) + (size_t)v * a.row_bytes;
+            char* const end = p + a.row_bytes;
+            char* const in = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(p) + 15) & ~(uintptr_t)15);
+            char* const out = reinterpret_cast<char*>(reinterpret_cast<uintptr_t>(end) & ~(uintptr_t)15);
+            if (p + 2 * lane < (in < end ? in : end)) *reinterpret_cast<short*>(p + 2 * lane) = 0;
+            for (char* q = in + 16 * lane; q < out; q += 512) *reinterpret_cast<uint4*>(q) = make_uint4(0, 0, 0, 0);
+            if (out >= in && out + 2 * lane < end) *reinterpret_cast<short*>(out + 2 * lane) = 0;
         }
-        for (; p < end; p += 2) *reinterpret_cast<short*>(p) = 0;
+        return;
+    }
+    for (int v = z0 + 32 * w + lane; v < z1; v += 32 * warps) {
+        if (is_named(v)) continue;
+        char* const p = static_cast<char*>(a.dE) + (size_t)v * a.row_bytes;
+        for (size_t at = 0; at < a.row_bytes; at += kZeroBytes)
+            asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(p + at),
+                         "r"(smem_u32(source)),
+                         "r"((uint32_t)(a.row_bytes - at < kZeroBytes ? a.row_bytes - at : kZeroBytes))
+                         : "memory");
     }
     bulk_commit();
 }
 
-// All warps, shorter rows: the same with plain stores, a warp a row.
-__device__ __forceinline__ void zero_rows(const SortArgs& a, int z0, int z1, int lo, const uint32_t* named) {
-    const int lane = threadIdx.x & 31;
-    for (int v = z0 + (threadIdx.x >> 5); v < z1; v += kSortWarps) {
-        if (is_named(named, v - lo)) continue;
-        char* const p = static_cast<char*>(a.dE) + (size_t)v * a.row_bytes;
-        const int bytes = (int)a.row_bytes;
-        if (bytes % 16 == 0) {
-            if (16 * lane < bytes) *reinterpret_cast<uint4*>(p + 16 * lane) = make_uint4(0, 0, 0, 0);
-        } else {
-            for (int i = 2 * lane; i < bytes; i += 64) *reinterpret_cast<short*>(p + i) = 0;
-        }
-    }
-}
+// Where a range's counts fit into shared memory.  A range has kSplit CTAs, each with the runs of
+// kOwn warps (a frequent symbol's tokens would keep one CTA busy long after the others).  Each counts, for
+// every symbol of the range, the tokens before its runs, in each of them and after them: so it knows
+// where those of each run go, and the run's warp puts them there, 32 at a time.
+constexpr int kSplit = 8, kOwn = kSortWarps / kSplit, kTallies = kOwn + 2;
 
-// SPLIT: a range has several CTAs, each with some of the warps' runs of tokens (a frequent symbol's
-// tokens would keep one CTA busy long after the others).  Each counts, for every symbol of the range,
-// the tokens before its share, in it and after it, and so knows where its own of a symbol go.
-template <bool SPLIT>
-__global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const SortArgs a) {
-    extern __shared__ int counts[];                        // SPLIT: [3][range]
-    __shared__ __align__(16) int hist[kDigits * kSortWarps];
-    __shared__ uint32_t named[kMaxRange / 32];
+__global__ void __launch_bounds__(kSortThreads) embed_place_kernel(const SortArgs a) {
+    extern __shared__ int counts[];                 // [kTallies][range]: before, own .., after
     __shared__ int scratch[kSortWarps];
-    __shared__ __align__(16) uint4 zeros[kZeroBytes / 16];
-    if (threadIdx.x < kZeroBytes / 16) zeros[threadIdx.x] = make_uint4(0, 0, 0, 0);
+    __shared__ __align__(16) uint4 source[kZeroBytes / 16];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, range = a.range;
+    uint32_t* const named = reinterpret_cast<uint32_t*>(counts + kTallies * range);
+    if (threadIdx.x < kZeroBytes / 16) source[threadIdx.x] = make_uint4(0, 0, 0, 0);
     fence_proxy_async_smem();   // before the barriers that come first, for the bulk copies that read them
+    for (int i = threadIdx.x; i < kTallies * range; i += kSortThreads) counts[i] = 0;
     pdl_wait();
     pdl_trigger();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int lo = blockIdx.x / a.split * a.range, hi = min(a.V, lo + a.range);
-    const int part = blockIdx.x % a.split, kind = warp * a.split / kSortWarps;   // the warp's share
-    int* const tally = counts + (kind < part ? 0 : kind == part ? 1 : 2) * a.range;
-    if (SPLIT)
-        for (int i = threadIdx.x; i < 3 * a.range; i += kSortThreads) counts[i] = 0;
-    else
-        for (int i = threadIdx.x; i < (a.range + 31) / 32; i += kSortThreads) named[i] = 0;
+    const int lo = blockIdx.x / kSplit * range, hi = min(a.V, lo + range);
+    const int part = blockIdx.x % kSplit, own = warp - part * kOwn;
+    int* const tally = counts + (own < 0 ? 0 : own < kOwn ? 1 + own : kOwn + 1) * range;
     __syncthreads();
     // each warp goes through a run of ids, four a lane at a time
     const int run = ((a.T + kSortThreads - 1) / kSortThreads * 32 + 127) / 128 * 128;   // of a warp
     const long long w0 = (long long)warp * run, w1 = min((long long)a.T, w0 + run);
-    int below = 0, mine = 0, earlier = 0;
+    int below = 0;
+    for (long long i0 = w0; i0 < w1; i0 += 512) {
+        int id[4][4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) ids_at(a.ids, i0 + 128 * q + 4 * lane, w1, id[q]);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int v = id[q][e];
+                below += v >= 0 && v < lo;
+                if (v >= lo && v < hi) atomicAdd(&tally[v - lo], 1);
+                if (v >= a.V) atomicExch(&g_error_word, kErrInvalid);
+            }
+    }
+    int base, all;
+    (void)block_prefix(below, scratch, &base);   // (and the counts are complete)
+    const int per = (range + kSortThreads - 1) / kSortThreads;
+    const int v0 = min((int)threadIdx.x * per, range), v1 = min(v0 + per, range);
+    int total = 0;
+    for (int v = v0; v < v1; ++v)
+#pragma unroll
+        for (int k = 0; k < kTallies; ++k) total += counts[k * range + v];
+    for (int i = threadIdx.x; i < (range + 31) / 32 * 32; i += kSortThreads) {
+        int any = 0;
+#pragma unroll
+        for (int k = 0; k < kTallies; ++k) any |= i < range ? counts[k * range + i] : 0;
+        const uint32_t word = __ballot_sync(0xffffffffu, any != 0);
+        if (lane == 0) named[i >> 5] = word;
+    }
+    int at = base + block_prefix(total, scratch, &all);
+    for (int v = v0; v < v1; ++v) {
+#pragma unroll
+        for (int k = 0; k < kTallies; ++k) {   // the first place of the symbol's tokens in each part
+            const int c = counts[k * range + v];
+            counts[k * range + v] = at;
+            at += c;
+        }
+    }
+    if (threadIdx.x == 0 && hi == a.V && part == 0) *a.count = base + all;
+    __syncthreads();
+    if (own >= 0 && own < kOwn) {
+        for (long long i0 = w0; i0 < w1; i0 += 512) {
+            int id[16];
+#pragma unroll
+            for (int q = 0; q < 16; ++q) id[q] = i0 + 32 * q + lane < w1 ? a.ids[i0 + 32 * q + lane] : -1;
+#pragma unroll
+            for (int q = 0; q < 16; ++q) {
+                const bool in = id[q] >= lo && id[q] < hi;
+                if (!__any_sync(0xffffffffu, in)) continue;
+                const uint32_t same = __match_any_sync(0xffffffffu, in ? id[q] : -1);
+                const int rank = __popc(same & ((1u << lane) - 1));
+                const int to = in ? tally[id[q] - lo] + rank : 0;
+                __syncwarp();
+                if (in && rank == 0) tally[id[q] - lo] += __popc(same);
+                __syncwarp();
+                if (in) {
+                    a.key[2][to] = id[q];
+                    a.pos[2][to] = (int)(i0 + 32 * q + lane);
+                }
+            }
+        }
+    } else if (a.dE) {
+        // the other warps: zeros; the CTAs of a range share its rows
+        const int share = (range + kSplit - 1) / kSplit;
+        const int z0 = min(lo + part * share, hi), z1 = min(z0 + share, hi);
+        start_zeros(a, z0, z1, lo, named, source, own < 0 ? warp : warp - kOwn, kSortWarps - kOwn);
+        bulk_wait<0>();
+    }
+}
+
+// For larger vocabularies: a CTA a range, which collects its own in their order and sorts them, 8 bits
+// of the symbol a pass, each warp counting and placing a run of them.
+__global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const SortArgs a) {
+    __shared__ __align__(16) int hist[kDigits * kSortWarps];
+    __shared__ uint32_t named[kMaxRange / 32];
+    __shared__ int scratch[kSortWarps];
+    __shared__ __align__(16) uint4 source[kZeroBytes / 16];
+    if (threadIdx.x < kZeroBytes / 16) source[threadIdx.x] = make_uint4(0, 0, 0, 0);
+    fence_proxy_async_smem();   // before the barriers that come first, for the bulk copies that read them
+    pdl_wait();
+    pdl_trigger();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int lo = blockIdx.x * a.range, hi = min(a.V, lo + a.range);
+    for (int i = threadIdx.x; i < (a.range + 31) / 32; i += kSortThreads) named[i] = 0;
+    __syncthreads();
+    // each warp goes through a run of ids, four a lane at a time
+    const int run = ((a.T + kSortThreads - 1) / kSortThreads * 32 + 127) / 128 * 128;   // of a warp
+    const long long w0 = (long long)warp * run, w1 = min((long long)a.T, w0 + run);
+    int below = 0, mine = 0;
     for (long long i0 = w0; i0 < w1; i0 += 512) {
         int id[4][4];
 #pragma unroll
@@ -287,74 +364,27 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const SortArgs
                 below += v >= 0 && v < lo;
                 if (v >= lo && v < hi) {
                     ++mine;
-                    if (SPLIT) {
-                        atomicAdd(&tally[v - lo], 1);
-                    } else {
-                        // (a frequent symbol is looked for before it is marked again)
-                        const uint32_t bit = 1u << ((v - lo) & 31);
-                        if (!(*(volatile uint32_t*)&named[(v - lo) >> 5] & bit))
-                            atomicOr(&named[(v - lo) >> 5], bit);
-                    }
+                    // (a frequent symbol is looked for before it is marked again)
+                    const uint32_t bit = 1u << ((v - lo) & 31);
+                    if (!(*(volatile uint32_t*)&named[(v - lo) >> 5] & bit)) atomicOr(&named[(v - lo) >> 5], bit);
                 }
                 if (v >= a.V) atomicExch(&g_error_word, kErrInvalid);
             }
     }
-    if (SPLIT && kind != part) {
-        if (kind < part) earlier = mine;
-        mine = 0;
-    }
-    int m, base, all = 0;
+    int m, base;
     (void)block_prefix(below, scratch, &base);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
     int at = block_prefix(lane == 0 ? mine : 0, scratch, &m);
     at = __shfl_sync(0xffffffffu, at, 0);
-    // (the prefixes were behind a barrier: the counts are complete)
-    int list = base;     // where the CTA's lists lie
-    if (SPLIT) {
-        (void)block_prefix(earlier, scratch, &list);
-        list += base;
-        for (int i = threadIdx.x; i < (a.range + 31) / 32 * 32; i += kSortThreads) {
-            const bool on = i < a.range && (counts[i] | counts[a.range + i] | counts[2 * a.range + i]);
-            const uint32_t word = __ballot_sync(0xffffffffu, on);
-            if (lane == 0) named[i >> 5] = word;
-        }
-        // a symbol's place in the whole order, less that among the CTA's own
-        const int per = (a.range + kSortThreads - 1) / kSortThreads;
-        const int v0 = min((int)threadIdx.x * per, a.range), v1 = min(v0 + per, a.range);
-        int total = 0, own = 0;
-        for (int v = v0; v < v1; ++v) {
-            own += counts[a.range + v];
-            total += counts[v] + counts[a.range + v] + counts[2 * a.range + v];
-        }
-        int unused, before_all = block_prefix(total, scratch, &all);
-        int before_own = block_prefix(own, scratch, &unused);
-        for (int v = v0; v < v1; ++v) {
-            const int c0 = counts[v], c1 = counts[a.range + v], c2 = counts[2 * a.range + v];
-            counts[v] = base + before_all + c0 - before_own;
-            before_all += c0 + c1 + c2;
-            before_own += c1;
-        }
-        __syncthreads();
-    } else {
-        all = m;
-    }
-    if (threadIdx.x == 0 && hi == a.V && part == 0) *a.count = base + all;
-    if (a.dE) {
-        // the CTAs of a range share its rows
-        const int share = (a.range + a.split - 1) / a.split;
-        const int z0 = min(lo + part * share, hi), z1 = min(z0 + share, hi);
-        if (a.row_bytes >= kBulkRow) {
-            if (warp == kSortWarps - 1) start_zeros(a, z0, z1, lo, named, zeros);
-        } else {
-            zero_rows(a, z0, z1, lo, named);
-        }
-    }
+    if (threadIdx.x == 0 && hi == a.V) *a.count = base + m;
+    // (the prefixes above were behind a barrier: the flags are complete)
+    if (a.dE) start_zeros(a, lo, hi, lo, named, source, warp, kSortWarps);
     // its own, in order
     if (m > 0) {
-        int *key = a.key[0] + list, *pos = a.pos[0] + list;
-        int *key_to = a.key[1] + list, *pos_to = a.pos[1] + list;
-        for (long long i0 = w0; i0 < w1 && kind == part; i0 += 512) {
+        int *key = a.key[0] + base, *pos = a.pos[0] + base;
+        int *key_to = a.key[1] + base, *pos_to = a.pos[1] + base;
+        for (long long i0 = w0; i0 < w1; i0 += 512) {
             int id[4][4];
 #pragma unroll
             for (int q = 0; q < 4; ++q) ids_at(a.ids, i0 + 128 * q + 4 * lane, w1, id[q]);
@@ -402,7 +432,7 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const SortArgs
                 c = my[0];
                 e = my[1];
             }
-            int unused, p = block_prefix(c.x + c.y + c.z + c.w + e.x + e.y + e.z + e.w, scratch, &unused);
+            int all, p = block_prefix(c.x + c.y + c.z + c.w + e.x + e.y + e.z + e.w, scratch, &all);
             const int q = p + c.x + c.y + c.z + c.w;
             if (in) {
                 my[0] = make_int4(p, p + c.x, p + c.x + c.y, p + c.x + c.y + c.z);
@@ -420,13 +450,9 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const SortArgs
                 __syncwarp();
                 if (on && rank == 0) hist[d * kSortWarps + warp] += __popc(same);
                 __syncwarp();
-                if (on && last) {
-                    const int to = place + (SPLIT ? counts[k - lo] : base);
-                    a.key[2][to] = k;
-                    a.pos[2][to] = t;
-                } else if (on) {
-                    key_to[place] = k;
-                    pos_to[place] = t;
+                if (on) {
+                    (last ? a.key[2] + base : key_to)[place] = k;
+                    (last ? a.pos[2] + base : pos_to)[place] = t;
                 }
             }
             __syncthreads();
@@ -438,7 +464,7 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const SortArgs
             pos_to = t;
         }
     }
-    bulk_wait<0>();   // (the threads that copied zeros)
+    bulk_wait<0>();   // the zeros
 }
 
 // ------------------------------------------------------------------ the sums
@@ -662,6 +688,16 @@ int chunk_log2_of(int T, int tiles, int sms) {
     return l;
 }
 
+// Symbols of a range, and whether the counts of its tokens fit into shared memory: up to about 160000
+// symbols (16384 tokens of 32000 symbols: 13 us, where collecting and sorting took 18).
+constexpr size_t kPlaceSmem = 200 * 1024;   // of counts at most
+size_t place_bytes(int range) { return ((size_t)kTallies * range + (range + 31) / 32) * 4; }
+int range_of(int V, bool* counted) {
+    const long long sms = device_sms();
+    const int range = (int)((V * (long long)kSplit + sms - 1) / sms);
+    *counted = place_bytes(range) <= kPlaceSmem;
+    return *counted ? range : (int)((V + sms - 1) / sms);
+}
 struct BwdPlan {
     int tiles, chunk_log2, chunks;
     size_t key[3], pos[3], count, part, bytes;
@@ -725,18 +761,9 @@ cudaError_t fwd(const int* ids, const void* table, int tokens, int V, int d, flo
                       (long long)tokens, V, d, scale, static_cast<T*>(x));
 }
 
-constexpr int kSplitSmem = 160 * 1024;    // of counts at most
-
-// The ranges, and the CTAs of each: eight once there are tokens enough for a frequent symbol's share
-// of them to be worth it (32000 symbols, 16384 tokens, d = 512: 41 us with one, 34 with eight), fewer where a range's counts would not fit.
-cudaError_t launch_sort(SortArgs& a, cudaStream_t st) {
-    const int sms = device_sms();
-    a.split = a.T > 8192 ? 8 : 1;
-    const auto range = [&]() { return (int)(((long long)a.V * a.split + sms - 1) / sms); };
-    while (a.split > 1 && range() * 12ll > kSplitSmem) a.split /= 2;
-    a.range = range();
-    const dim3 grid((unsigned)((a.V + a.range - 1) / a.range * a.split)), block(kSortThreads);
-    if (a.split == 1) return launch_pdl(embed_sort_kernel<false>, grid, block, 0, st, a);
+cudaError_t launch_sort(const SortArgs& a, bool counted, cudaStream_t st) {
+    const unsigned ranges = (unsigned)((a.V + a.range - 1) / a.range);
+    if (!counted) return launch_pdl(embed_sort_kernel, dim3(ranges), dim3(kSortThreads), 0, st, a);
     static std::once_flag once[64];
     static cudaError_t set_err[64];
     int dev = 0;
@@ -744,11 +771,12 @@ cudaError_t launch_sort(SortArgs& a, cudaStream_t st) {
     if (e != cudaSuccess) return e;
     if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
     std::call_once(once[dev], [&] {
-        set_err[dev] = cudaFuncSetAttribute(embed_sort_kernel<true>,
-                                            cudaFuncAttributeMaxDynamicSharedMemorySize, kSplitSmem);
+        set_err[dev] = cudaFuncSetAttribute(embed_place_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                            (int)kPlaceSmem);
     });
     if (set_err[dev] != cudaSuccess) return set_err[dev];
-    return launch_pdl(embed_sort_kernel<true>, grid, block, (size_t)a.range * 12, st, a);
+    return launch_pdl(embed_place_kernel, dim3(ranges * kSplit), dim3(kSortThreads),
+                      place_bytes(a.range), st, a);
 }
 
 template <typename T, typename O, int E, bool WIDE>
@@ -766,13 +794,16 @@ cudaError_t bwd(SortArgs& so, SumArgs& su, int tokens, char* ws, cudaStream_t st
     su.chunk_log2 = p.chunk_log2;
     su.chunks = p.chunks;
     su.tiles = p.tiles;
-    cudaError_t e = launch_sort(so, st);
+    bool counted;
+    so.range = range_of(so.V, &counted);
+    cudaError_t e = launch_sort(so, counted, st);
     if (e != cudaSuccess) return e;
     ++*launches;
     const long long items = (long long)p.chunks * p.tiles;
     e = launch_pdl(embed_sum_kernel<T, O, E, WIDE>, dim3((unsigned)items), dim3(32 * kSumWarps), 0, st, su);
     if (e != cudaSuccess) return e;
     ++*launches;
+    if (p.chunks == 1) return cudaSuccess;   // no run over a chunk's end
     e = launch_pdl(embed_join_kernel<T, O, E, WIDE>, dim3((unsigned)((items + kSumWarps - 1) / kSumWarps)),
                    dim3(32 * kSumWarps), 0, st, su);
     if (e != cudaSuccess) return e;

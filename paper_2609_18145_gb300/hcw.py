@@ -182,6 +182,10 @@ def _ptr(t):
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
+# the current device's number, likewise (for a tensor of a device that is in use already)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
 def _stream(stream):
     if stream is not None:
         return stream.cuda_stream
@@ -727,7 +731,7 @@ def _here(what, *ts):
         if not t.is_contiguous():
             raise ValueError("%s: all tensors must be contiguous" % what)
         if dev is None:
-            dev = torch.cuda.current_device()
+            dev = _current_device()
         if t.get_device() != dev:
             raise ValueError("%s: a tensor of %s, but the current device is cuda:%d"
                              % (what, t.device, dev))
@@ -824,9 +828,9 @@ def hcw_clip_grads(grads, max_norm: float, norm=None, workspace=None, stream=Non
     the tensor [2] fp32 of the norm and the factor (on the device: nothing waits)."""
     q = grads if isinstance(grads, GradList) else GradList(grads)
     _here("hcw_clip_grads", norm, workspace)
-    if q.device is not None and q.device.index != torch.cuda.current_device():
+    if q.device is not None and q.device.index != _current_device():
         raise ValueError("hcw_clip_grads: gradients of %s, but the current device is cuda:%d"
-                         % (q.device, torch.cuda.current_device()))
+                         % (q.device, _current_device()))
     if norm is None:
         norm = _memory(stream).empty(2, dtype=torch.float32, device=q.device or "cuda")
     elif norm.dtype != torch.float32 or norm.numel() != 2:
