@@ -1,4 +1,5 @@
-"""A student block around the mixing stack, trained from a teacher's top logits.
+"""A student block around the mixing stack, trained from a teacher's top logits, then run one
+symbol at a time.
 
     python examples/student.py [--steps 40] [--tokens 256] [--width 256]
 
@@ -7,7 +8,7 @@ the block around them as it was: norms before and after each sublayer, a gate on
 what the sublayer adds to the residual stream, a gated feed-forward block.  And
 it leaves a teacher: the model before the replacement.  One training step here is
 
-    x   = N(E[ids])
+    x   = N(E[ids])                               hcw_embed_fwd
     m   = mixing stack of x                       hcw_stack_fwd
     r,x = r + g1 N(m), N(r)                       hcw_residual_norm_fwd
     f   = W2 (silu(Wg x) * Wu x)                  hcw_gated_ffn_fwd
@@ -15,10 +16,15 @@ it leaves a teacher: the model before the replacement.  One training step here i
     z   = Wh x                                    hcw_gemm_bf16
     loss against the teacher's top logits and the next symbol, dz      hcw_distill_loss
 
-and the same calls' backward passes in reverse.  Weights, activations and their
+and the same calls' backward passes in reverse (hcw_embed_bwd last), before the gradients
+of all parameters are clipped together (hcw_clip_grads).  Weights, activations and their
 gradients are bf16, norm weights, gates, the logits and the weight gradients
 fp32.  The teacher is a frozen table: its top logits for the next symbol given the
 current one and the one 4 positions before, which the mixing layer can see.
+
+Run one symbol at a time the same block takes hcw_embed_fwd for the symbol, hcw_decode_step for
+the mixing, the head's weights in 4 bits (hcw_q4_matmul) and, before the next symbol is drawn, the
+penalties for symbols that occurred already (hcw_logits_edit).
 """
 import argparse
 import os
@@ -59,15 +65,21 @@ def join(p, i):
                 pre_w=p["n%d" % i], eps=EPS)
 
 
+def links(L):
+    """The layers' links: 4, 8, ... positions back."""
+    return [2 + l for l in range(L)]
+
+
 def step(p, ids, teacher, target, weight, temperature=2.0):
     """Loss of every position and the gradient of every parameter.  ids [B, n],
     teacher (symbols, logits) [B n, K], target and weight [B n]."""
     B, n = ids.shape
     V, d = p["E"].shape
     L = p["W_self"].shape[0]
-    dims = [2 + l for l in range(L)]                    # links 4, 8, ... positions back
+    dims = links(L)
+    ids = ids.reshape(-1).to(torch.int32)
     # forward
-    r0, x0 = H.hcw_residual_norm_fwd(p["E"][ids.view(-1)], None, pre_w=p["n0"], eps=EPS)
+    r0, x0 = H.hcw_residual_norm_fwd(H.hcw_embed_fwd(ids, p["E"]), None, pre_w=p["n0"], eps=EPS)
     m, acts, masks = H.hcw_stack_fwd(x0.view(B, n, d), p["W_self"], p["W_nbr"], flags=FLAGS,
                                      dims=dims)
     m = m.view(B * n, d)
@@ -92,7 +104,7 @@ def step(p, ids, teacher, target, weight, temperature=2.0):
         want_dbias=False, dims=dims)
     b = H.hcw_residual_norm_bwd(b["dr"], dx0.view(B * n, d), r0, None, pre_w=p["n0"], eps=EPS)
     g["n0"] = b["dpre_w"]
-    g["E"] = torch.zeros(V, d, device=ids.device).index_add_(0, ids.view(-1).long(), b["dr"].float())
+    g["E"] = H.hcw_embed_bwd(ids, b["dr"], V)
     return loss, g
 
 
@@ -105,12 +117,58 @@ def batch(table, V, B, n, K, gen):
         logits[:, t] = table[0, ids[:, t]] + table[1, before]
         ids[:, t + 1] = torch.multinomial(logits[:, t].softmax(-1), 1, generator=gen)[:, 0]
     top, at = logits.view(B * n, V).topk(K)
-    return (ids[:, :n].contiguous(), (at.to(torch.int32).contiguous(), top.contiguous()),
+    return (ids[:, :n].to(torch.int32).contiguous(), (at.to(torch.int32).contiguous(), top.contiguous()),
             ids[:, 1:].reshape(-1).to(torch.int32).contiguous())
 
 
-def train(steps=40, B=8, n=32, V=97, d=256, h=512, L=1, K=16, lr=3e-3, seed=0, say=print):
-    """Adam on fp32 copies of the parameters; returns the mean loss of every step."""
+def packed_head(p, group=64):
+    """The head's weights as hcw_q4_matmul reads them."""
+    return H.hcw_q4_pack(*H.hcw_q4_quantize(p["Wh"], group), group)
+
+
+def cache_for(p, B, n):
+    """What hcw_decode_step keeps of the positions before."""
+    L, d = p["W_self"].shape[:2]
+    return torch.empty(H.hcw_decode_cache_bytes(L, B, n, d, links(L)), dtype=torch.uint8,
+                       device=p["E"].device)
+
+
+def next_logits(p, head, symbols, t, n, cache, group=64):
+    """Logits [B, V] fp32 for what follows symbols [B] int32 at position t of a window of n, after
+    the positions before it in their order."""
+    L = p["W_self"].shape[0]
+    r, x = H.hcw_residual_norm_fwd(H.hcw_embed_fwd(symbols, p["E"]), None, pre_w=p["n0"], eps=EPS)
+    m = H.hcw_decode_step(x, p["W_self"], p["W_nbr"], None, t, n, cache, FLAGS, dims=links(L))
+    r, x = H.hcw_residual_norm_fwd(r, m, **join(p, 1))
+    f = H.hcw_gated_ffn_fwd(x, p["W1"], p["W2"])
+    r, x = H.hcw_residual_norm_fwd(r, f, **join(p, 2))
+    return H.hcw_q4_matmul(x, head, p["E"].shape[0], group, y_dtype=torch.float32)
+
+
+def generate(p, prompt, n, repetition=1.1, frequency=0.05, gen=None):
+    """prompt [B, at least 1] int32 continued to n symbols, drawn with penalties for those that a
+    sequence holds already."""
+    dev, (B, given) = prompt.device, prompt.shape
+    head, cache = packed_head(p), cache_for(p, B, n)
+    out = torch.full((B, n), -1, dtype=torch.int32, device=dev)
+    out[:, :given] = prompt
+    row = lambda v, dt: torch.full((B,), v, dtype=dt, device=dev)  # noqa: E731
+    own, rep, freq = row(given, torch.int32), row(repetition, torch.float32), \
+        row(frequency, torch.float32)
+    for t in range(n - 1):
+        z = next_logits(p, head, out[:, t].contiguous(), t, n, cache)
+        if t + 1 < given:
+            continue
+        # symbols that are not there yet are -1: empty
+        z = H.hcw_logits_edit(z, history=out, prompt=own, repetition=rep, frequency=freq, out=z)
+        out[:, t + 1] = torch.multinomial(z.softmax(-1), 1, generator=gen)[:, 0].to(torch.int32)
+    return out
+
+
+def train(steps=40, B=8, n=32, V=97, d=256, h=512, L=1, K=16, lr=3e-3, seed=0, clip=1.0, say=print,
+          keep=None):
+    """Adam on fp32 copies of the parameters; returns the mean loss of every step.  keep: a dict that
+    gets the trained parameters."""
     dev = "cuda"
     gen = torch.Generator(device=dev).manual_seed(seed)
     table = 2.0 * torch.randn(2, V, V, generator=gen, device=dev)
@@ -123,6 +181,7 @@ def train(steps=40, B=8, n=32, V=97, d=256, h=512, L=1, K=16, lr=3e-3, seed=0, s
     for s in range(1, steps + 1):
         ids, teacher, target = batch(table, V, B, n, K, gen)
         loss, g = step(p, ids, teacher, target, weight)
+        H.hcw_clip_grads(g.values(), clip)
         for k, w in master.items():
             m1[k].lerp_(g[k], 0.1)
             m2[k].lerp_(g[k] * g[k], 0.05)
@@ -133,6 +192,8 @@ def train(steps=40, B=8, n=32, V=97, d=256, h=512, L=1, K=16, lr=3e-3, seed=0, s
             say("step %3d  loss %.4f" % (s, float(losses[-1])))
     if H.hcw_sync_status() != H.HCW_OK:
         raise RuntimeError("the device reported an error")
+    if keep is not None:
+        keep.update(p)
     return [float(v) for v in losses]
 
 
@@ -142,4 +203,8 @@ if __name__ == "__main__":
     ap.add_argument("--tokens", type=int, default=256, help="positions a step (windows of 32)")
     ap.add_argument("--width", type=int, default=256, help="a multiple of 64")
     a = ap.parse_args()
-    train(a.steps, B=max(1, a.tokens // 32), d=a.width, h=2 * a.width)
+    params = {}
+    train(a.steps, B=max(1, a.tokens // 32), d=a.width, h=2 * a.width, keep=params)
+    start = torch.arange(2, dtype=torch.int32, device="cuda")[:, None]
+    for line in generate(params, start, 32).tolist():
+        print("symbols", *line)

@@ -688,8 +688,8 @@ int hcw_distill_loss(const void* z, const int* idx, const float* teacher, const 
  *   E     [V][d] (dtype);  x [T][d] (dtype) output, rounded once
  * An id >= V counts as padding and is reported by hcw_sync_status as HCW_ERR_INVALID_ARG.
  * Any T >= 0 up to 2^28 (0 does nothing), V up to 2^23, d up to 2^20 (HCW_ERR_UNSUPPORTED above;
- * d needs no multiple: rows of 16-byte pieces are the faster ones); scale is finite; pointers are
- * 16-byte aligned; x over an input is HCW_ERR_ALIASING.  One launch, no workspace.
+ * d needs no multiple: rows of 16-byte pieces are the faster ones); scale is finite; ids is 4-byte,
+ * the rest 16-byte aligned; x over an input is HCW_ERR_ALIASING.  One launch, no workspace.
  */
 int hcw_embed_fwd(const int* ids, const void* E, int T, int V, int d, int dtype, float scale, void* x,
                   void* stream);
@@ -748,8 +748,8 @@ int hcw_clip_grads(const void* const* grads, void* const* out, const long long* 
  * depend on the other tokens of the call, and the same inputs give the same bits.  Made for up to 16
  * tokens, which read the weights once; more read them again for every 16.
  * T >= 0 up to 2^19 (0 does nothing), N up to 2^24, K a multiple of 8 up to 2^20
- * (HCW_ERR_UNSUPPORTED otherwise); pointers are 16-byte aligned; an output over an input is
- * HCW_ERR_ALIASING.  One launch each, no workspace.
+ * (HCW_ERR_UNSUPPORTED otherwise); bias is 4-byte, the rest 16-byte aligned; an output over an
+ * input is HCW_ERR_ALIASING.  One launch each, no workspace.
  */
 size_t hcw_q4_bytes(int N, int K, int group);
 int hcw_q4_quantize(const void* W, int N, int K, int group, int dtype, signed char* codes,
@@ -779,8 +779,9 @@ int hcw_q4_matmul(const void* x, const void* packed, const float* bias, int T, i
  * what the mask takes out is -inf whatever it was, NaN included.  A symbol >= V in the history or a
  * slot counts as empty and is reported by hcw_sync_status as HCW_ERR_INVALID_ARG.  The same inputs
  * give the same bits.  B >= 0 up to 2^20 (0 does nothing), V up to 2^24, H up to 2^28, M up to
- * 1024, B V up to 2^40 (HCW_ERR_UNSUPPORTED above); pointers are 16-byte aligned; out over an input, or
- * over z other than in place, is HCW_ERR_ALIASING.  One launch, no workspace.
+ * 1024, B V up to 2^40 (HCW_ERR_UNSUPPORTED above); z and out are 16-byte, the rest 4-byte aligned;
+ * out over an input, or over z other than in place, is HCW_ERR_ALIASING.  One or two launches, no
+ * workspace.
  */
 int hcw_logits_edit(const void* z, int B, int V, int dtype, const int* history, const int* lengths,
                     const int* prompt, int H, const float* repetition, const float* frequency,

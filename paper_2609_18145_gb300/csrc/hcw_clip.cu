@@ -392,7 +392,7 @@ extern "C" int hcw_clip_grads(const void* const* grads, void* const* out, const 
             (apart && (reinterpret_cast<uintptr_t>(out[i]) & mask)))
             return HCW_ERR_ALIGNMENT;
     }
-    if (!on_16_bytes(workspace) || (reinterpret_cast<uintptr_t>(norm) & 3)) return HCW_ERR_ALIGNMENT;
+    if (!on_16_bytes(workspace) || !on_4_bytes(norm)) return HCW_ERR_ALIGNMENT;
     if (!workspace || ws_bytes < need) return HCW_ERR_WORKSPACE;
     ClipCall c = {grads, out, sizes, dtypes, count, max_norm, norm, static_cast<double*>(workspace)};
     for (int t = 0; t < count; t += kCTensors)

@@ -170,7 +170,7 @@ struct SortArgs {
 
 // The ids i .. i + 3, i a multiple of four; -1 from `end` on.
 __device__ __forceinline__ void ids_at(const int* ids, long long i, long long end, int (&id)[4]) {
-    if (i + 3 < end) {
+    if (i + 3 < end && (reinterpret_cast<uintptr_t>(ids) & 15) == 0) {
         const int4 q = *reinterpret_cast<const int4*>(ids + i);
         id[0] = q.x;
         id[1] = q.y;
@@ -835,7 +835,7 @@ extern "C" int hcw_embed_fwd(const int* ids, const void* E, int T, int V, int d,
     const int rc = check_sizes(T, V, d, dtype);
     if (rc) return rc;
     if (!(scale - scale == 0.f)) return HCW_ERR_INVALID_ARG;   // infinite or NaN
-    if (!on_16_bytes(ids) || !on_16_bytes(E) || !on_16_bytes(x)) return HCW_ERR_ALIGNMENT;
+    if (!on_4_bytes(ids) || !on_16_bytes(E) || !on_16_bytes(x)) return HCW_ERR_ALIGNMENT;
     const size_t es = dtype == HCW_F32 ? 4 : 2, xb = (size_t)T * d * es;
     if (spans_meet(x, xb, ids, (size_t)T * 4) || spans_meet(x, xb, E, (size_t)V * d * es))
         return HCW_ERR_ALIASING;
@@ -866,7 +866,7 @@ extern "C" int hcw_embed_bwd(const int* ids, const void* dx, int T, int V, int d
     if (!(scale - scale == 0.f) || (accumulate != 0 && accumulate != 1) ||
         (de_dtype != HCW_BF16 && de_dtype != HCW_F32))
         return HCW_ERR_INVALID_ARG;
-    if (!on_16_bytes(ids) || !on_16_bytes(dx) || !on_16_bytes(dE) || !on_16_bytes(workspace))
+    if (!on_4_bytes(ids) || !on_16_bytes(dx) || !on_16_bytes(dE) || !on_16_bytes(workspace))
         return HCW_ERR_ALIGNMENT;
     if (!dE || (T > 0 && (!ids || !dx))) return HCW_ERR_INVALID_ARG;
     const size_t es = dtype == HCW_F32 ? 4 : 2, oes = de_dtype == HCW_F32 ? 4 : 2;

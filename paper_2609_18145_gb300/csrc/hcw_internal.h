@@ -390,8 +390,9 @@ cudaError_t distill_error_word_read_clear(int* word);
 cudaError_t embed_error_word_read_clear(int* word);
 cudaError_t logits_error_word_read_clear(int* word);
 
-// Argument checks of those files: 16-byte alignment, and whether two spans share a byte.
+// Argument checks of those files: alignment, and whether two spans share a byte.
 inline bool on_16_bytes(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+inline bool on_4_bytes(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 inline bool spans_meet(const void* a, size_t na, const void* b, size_t nb) {
     if (!a || !b || !na || !nb) return false;
     const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);

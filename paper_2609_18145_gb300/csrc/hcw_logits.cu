@@ -546,10 +546,10 @@ extern "C" int hcw_logits_edit(const void* z, int B, int V, int dtype, const int
         return HCW_ERR_INVALID_ARG;
     if (V > 1 << 24 || B > 1 << 20 || H > 1 << 28 || M > kLMaxSlots || (long long)B * V > 1ll << 40)
         return HCW_ERR_UNSUPPORTED;
-    const void* all[] = {z, history, lengths, prompt, repetition, frequency, presence, bias_idx,
-                         bias, mask, out};
+    const void* all[] = {history, lengths, prompt, repetition, frequency, presence, bias_idx, bias, mask};
     for (const void* p : all)
-        if (!on_16_bytes(p)) return HCW_ERR_ALIGNMENT;
+        if (!on_4_bytes(p)) return HCW_ERR_ALIGNMENT;
+    if (!on_16_bytes(z) || !on_16_bytes(out)) return HCW_ERR_ALIGNMENT;
     const size_t zb = (size_t)B * V * (dtype == HCW_F32 ? 4 : 2), b4 = (size_t)B * 4;
     const struct {
         const void* p;

@@ -498,7 +498,7 @@ extern "C" int hcw_q4_matmul(const void* x, const void* packed, const float* bia
     const int rc = check_weights(N, K, group);
     if (rc) return rc;
     if (T > kQMaxT) return HCW_ERR_UNSUPPORTED;
-    if (!on_16_bytes(x) || !on_16_bytes(packed) || !on_16_bytes(bias) || !on_16_bytes(y))
+    if (!on_16_bytes(x) || !on_16_bytes(packed) || !on_4_bytes(bias) || !on_16_bytes(y))
         return HCW_ERR_ALIGNMENT;
     const size_t yb = (size_t)T * N * (y_dtype == HCW_F32 ? 4 : 2);
     if (spans_meet(y, yb, x, (size_t)T * K * 2) || spans_meet(y, yb, packed, packed_bytes(N, K, group)) ||

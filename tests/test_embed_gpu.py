@@ -212,3 +212,14 @@ def test_shapes_of_batches(H):
         H.hcw_embed_fwd(ids.long(), table)
     with pytest.raises(ValueError):
         H.hcw_embed_fwd(ids, table.t())
+
+
+@pytest.mark.parametrize("at", [1, 2, 3])
+def test_ids_that_start_anywhere(H, at):
+    rng = np.random.default_rng(at)
+    for T in (1, 5, 3000):
+        ids = torch.from_numpy(symbols(rng, 500, T + at)).cuda()
+        table, dx = torch.randn(500, 40, device="cuda"), torch.randn(T, 40, device="cuda")
+        apart = ids[at:].clone()
+        assert torch.equal(H.hcw_embed_fwd(ids[at:], table), H.hcw_embed_fwd(apart, table))
+        assert torch.equal(H.hcw_embed_bwd(ids[at:], dx, 500), H.hcw_embed_bwd(apart, dx, 500))

@@ -41,7 +41,8 @@ def test_lookup_refusals(H):
         H.HCW_ERR_UNSUPPORTED
     for k in "iEx":
         assert call(**{k: None}) == H.HCW_ERR_INVALID_ARG, k
-        assert call(**{k: P(8)}) == H.HCW_ERR_ALIGNMENT, k
+        assert call(**{k: P(6)}) == H.HCW_ERR_ALIGNMENT, k
+    assert call(E=P(8)) == call(x=P(8)) == H.HCW_ERR_ALIGNMENT
     assert call(x=E) == call(x=i) == call(x=P(E.value + V * d * 2 - 16)) == H.HCW_ERR_ALIASING
     assert call(T=0, i=None, E=None, x=None) == H.HCW_OK
 
@@ -60,7 +61,8 @@ def test_lookup_gradient_refusals(H):
     assert call(V=(1 << 23) + 1) == call(T=(1 << 28) + 1) == H.HCW_ERR_UNSUPPORTED
     for k, v in dict(i=i, dx=dx, dE=dE).items():
         assert call(**{k: None}) == H.HCW_ERR_INVALID_ARG, k
-        assert call(**{k: P(v.value + 8)}) == H.HCW_ERR_ALIGNMENT, k
+        assert call(**{k: P(v.value + 2)}) == H.HCW_ERR_ALIGNMENT, k
+    assert call(dx=P(dx.value + 8)) == call(dE=P(dE.value + 8)) == H.HCW_ERR_ALIGNMENT
     assert call(w=P(w.value + 8)) == H.HCW_ERR_ALIGNMENT
     assert call(w=None) == call(n=ws - 1) == H.HCW_ERR_WORKSPACE
     assert call(dE=dx) == call(dE=i) == call(w=dE) == call(w=dx) == H.HCW_ERR_ALIASING
@@ -142,8 +144,9 @@ def test_packed_product_refusals(H):
     assert call(K=12) == call(T=(1 << 19) + 1) == H.HCW_ERR_UNSUPPORTED
     for k in "xpy":
         assert call(**{k: None}) == H.HCW_ERR_INVALID_ARG, k
-    for k in "xpby":
+    for k in "xpy":
         assert call(**{k: P(8)}) == H.HCW_ERR_ALIGNMENT, k
+    assert call(b=P(6)) == H.HCW_ERR_ALIGNMENT
     assert call(y=x) == call(y=p) == call(y=b) == H.HCW_ERR_ALIASING
     assert call(y=P(x.value - T * N * 4 + 16), dt=1) == H.HCW_ERR_ALIASING
     assert call(T=0, x=None, y=None) == H.HCW_OK
@@ -164,7 +167,8 @@ def test_logits_refusals(H):
     assert call(M=1025) == call(V=(1 << 24) + 1) == call(B=(1 << 20) + 1) == H.HCW_ERR_UNSUPPORTED
     assert call(B=1 << 20, V=(1 << 20) + 1) == H.HCW_ERR_UNSUPPORTED
     for k, v in dict(z=z, h=h, n=n, q=q, r=r, f=f, e=e, bi=bi, b=b, m=m, o=o).items():
-        assert call(**{k: P(v.value + 4)}) == H.HCW_ERR_ALIGNMENT, k
+        assert call(**{k: P(v.value + 2)}) == H.HCW_ERR_ALIGNMENT, k
+    assert call(z=P(z.value + 4)) == call(o=P(o.value + 4)) == H.HCW_ERR_ALIGNMENT
     for v in (h, n, q, r, f, e, bi, b, m):
         assert call(o=v) == H.HCW_ERR_ALIASING
     assert call(o=P(z.value + 16)) == H.HCW_ERR_ALIASING      # neither in place nor apart

@@ -1,0 +1,100 @@
+"""The operators at the model's two ends together, as examples/student.py uses them: one symbol at a
+time against the same block in fp64 over the whole window, the gradients of a training step with
+their common norm, and a sequence that is drawn."""
+import importlib.util
+import os
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import ends as E
+
+pytestmark = pytest.mark.gpu
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+U = 2.0 ** -24
+# From the symbol to the logits about 8 tensors are rounded to bf16 one after the other (2^-9 of
+# their size as a root mean square: half a step of 8 bits over sqrt 3 is below that), independently:
+# 8^(1/2) 2^-9 = 0.6 %, with what each norm and product passes on.  Held to 3 % of the norm.
+TOL = 3e-2
+
+
+@pytest.fixture(scope="module")
+def student():
+    spec = importlib.util.spec_from_file_location("student", os.path.join(ROOT, "examples", "student.py"))
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    return m
+
+
+def window_logits(student, p, Wh, ids):
+    """Logits [B, n, V] of whole windows, fp64, with the head Wh."""
+    q = {k: v.double() for k, v in p.items()}
+    B, n = ids.shape
+    d = q["E"].shape[1]
+    rms = lambda v, w: v * torch.rsqrt((v * v).mean(-1, keepdim=True) + student.EPS) * w  # noqa: E731
+    r = q["E"][ids.long()]
+    x = rms(r, q["n0"])
+    for l, dim in enumerate(student.links(q["W_self"].shape[0])):
+        k = 1 << dim
+        takes = ((torch.arange(n, device=ids.device) // k) % 2 == 1).double()[None, :, None]
+        x = x @ q["W_self"][l].T + (torch.roll(x, k, dims=1) * takes) @ q["W_nbr"][l].T
+    r = r + q["g1"] * rms(x, q["m1"])
+    x = rms(r, q["n1"])
+    gu = x @ q["W1"].T
+    h = q["W2"].shape[1]
+    f = (torch.nn.functional.silu(gu[..., :h]) * gu[..., h:]) @ q["W2"].T
+    r = r + q["g2"] * rms(f, q["m2"])
+    return rms(r, q["n2"]) @ Wh.double().T
+
+
+@pytest.mark.parametrize("B,n,V,d,h,L", [(1, 16, 97, 64, 136, 1), (5, 32, 203, 192, 256, 2)])
+def test_one_symbol_at_a_time(student, B, n, V, d, h, L):
+    H = student.H
+    p = student.init(V, d, h, L, seed=5)
+    ids = torch.randint(V, (B, n), dtype=torch.int32, device="cuda",
+                        generator=torch.Generator(device="cuda").manual_seed(V))
+    codes, scales = H.hcw_q4_quantize(p["Wh"], 64)
+    Wh = torch.from_numpy(E.q4_weights(codes.cpu().numpy().astype(np.float64),
+                                       scales.double().cpu().numpy(), 64)).cuda()
+    want = window_logits(student, p, Wh, ids)
+    head, cache = student.packed_head(p), student.cache_for(p, B, n)
+    for t in range(n):
+        z = student.next_logits(p, head, ids[:, t].contiguous(), t, n, cache)
+        err = float((z.double() - want[:, t]).norm() / want[:, t].norm())
+        assert err < TOL, (t, err)
+    # the edits of these logits, from what has been seen
+    past = ids.cpu().numpy()
+    rep = np.full(B, 1.3, np.float32)
+    out = H.hcw_logits_edit(z, history=ids, repetition=torch.from_numpy(rep).cuda())
+    ref, mag = E.edit(z.double().cpu().numpy(), past, rep=rep.astype(np.float64))
+    assert (np.abs(out.double().cpu().numpy() - ref) <= 7 * U * mag + 1e-37).all()
+    assert H.hcw_sync_status() == H.HCW_OK
+
+
+def test_a_steps_gradients_are_clipped_together(student):
+    H = student.H
+    B, n, V, d = 3, 32, 97, 64
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    table = 2.0 * torch.randn(2, V, V, generator=gen, device="cuda")
+    p = student.init(V, d, 136, 1, seed=3)
+    ids, teacher, target = student.batch(table, V, B, n, 12, gen)
+    weight = torch.full((B * n,), 1.0 / (B * n), device="cuda")
+    _, g = student.step(p, ids, teacher, target, weight)
+    before = {k: v.double().clone() for k, v in g.items()}
+    total = float(torch.sqrt(sum((v * v).sum() for v in before.values())))
+    limit = 0.25 * total
+    norm, factor = H.hcw_clip_grads(g.values(), limit).tolist()
+    assert abs(norm - total) <= 13 * U * total and abs(factor - 0.25) <= 16 * U
+    for k, v in g.items():
+        assert bool(((v.double() - 0.25 * before[k]).abs() <= 18 * U * before[k].abs() + 1e-44).all()), k
+
+
+def test_a_sequence_is_drawn(student):
+    p = student.init(97, 64, 136, 1, seed=2)
+    prompt = torch.randint(97, (3, 4), dtype=torch.int32, device="cuda")
+    out = student.generate(p, prompt, 16)
+    assert out.shape == (3, 16) and torch.equal(out[:, :4], prompt)
+    assert bool(((out >= 0) & (out < 97)).all())
+    assert student.H.hcw_sync_status() == student.H.HCW_OK
