@@ -704,7 +704,8 @@ int hcw_embed_fwd(const int* ids, const void* E, int T, int V, int d, int dtype,
  *         be initialised; the bytes never fall with T.
  * Padding and ids >= V as for the lookup: they have no part in any sum.  Sums are fp32, rounded
  * once, in an order that depends on the ids and sizes alone: the same inputs give the same bits.
- * With T = 0 dE is zeros, or stays as it is.  Sizes, alignment and errors as for the lookup.
+ * With T = 0 dE is zeros, or stays as it is.  Sizes, alignment and errors as for the lookup, and
+ * T d / 2^15 up to 2^31 (HCW_ERR_UNSUPPORTED above).
  */
 size_t hcw_embed_bwd_workspace_bytes(int T, int V, int d);
 int hcw_embed_bwd(const int* ids, const void* dx, int T, int V, int d, int dtype, float scale,

@@ -385,7 +385,8 @@ extern "C" int hcw_clip_grads(const void* const* grads, void* const* out, const 
     const size_t room = (size_t)count * (apart ? 2 : 1) + 2;
     for (int i = 0; i < count; ++i) {
         if (sizes[i] < 0 || (dtypes[i] != HCW_BF16 && dtypes[i] != HCW_F32)) return HCW_ERR_INVALID_ARG;
-        if (sizes[i] > 0 && (!grads[i] || (apart && !out[i]))) return HCW_ERR_INVALID_ARG;
+        if (!sizes[i]) continue;
+        if (!grads[i] || (apart && !out[i])) return HCW_ERR_INVALID_ARG;
         if (sizes[i] > 1ll << 44) return HCW_ERR_UNSUPPORTED;
         const uintptr_t mask = dtypes[i] == HCW_F32 ? 3 : 1;
         if ((reinterpret_cast<uintptr_t>(grads[i]) & mask) ||

@@ -884,7 +884,10 @@ extern "C" int hcw_embed_bwd(const int* ids, const void* dx, int T, int V, int d
         if (accumulate) return HCW_OK;
         return cudaMemsetAsync(dE, 0, ob, st) == cudaSuccess ? HCW_OK : HCW_ERR_CUDA;
     }
-    if ((V + device_sms() - 1) / device_sms() > kMaxRange) return HCW_ERR_UNSUPPORTED;
+    const int elems = dtype == HCW_BF16 ? 8 : 4;
+    const BwdPlan plan = bwd_plan(T, d, elems);
+    if ((V + device_sms() - 1) / device_sms() > kMaxRange || (long long)plan.chunks * plan.tiles > 0x7fffffff)
+        return HCW_ERR_UNSUPPORTED;
     SortArgs so = {};
     so.ids = ids;
     so.T = T;

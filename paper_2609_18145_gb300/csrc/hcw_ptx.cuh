@@ -500,12 +500,6 @@ __device__ __forceinline__ int ld_acquire_cluster_remote(uint32_t cluster_addr) 
     return v;
 }
 
-__device__ __forceinline__ float ld_remote_f32(uint32_t cluster_addr) {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(cluster_addr) : "memory");
-    return v;
-}
-
 __device__ __forceinline__ void st_remote(uint32_t cluster_addr, int v) {
     asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(cluster_addr), "r"(v) : "memory");
 }

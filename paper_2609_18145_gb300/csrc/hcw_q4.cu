@@ -20,7 +20,6 @@
 // its scale, in fp32; the factor 2^6 comes last.
 #include "hcw.h"
 #include "hcw_internal.h"
-#include "hcw_ptx.cuh"
 
 #include <math.h>
 
@@ -175,6 +174,9 @@ __host__ __device__ constexpr int part_floats(int rt, int nt) { return rt * nt *
 // byte reads of neighbouring tokens fall into different banks.
 __host__ __device__ constexpr int x_stride(int pieces) { return pieces * 256 + 64; }
 
+__device__ __forceinline__ uint32_t shared_at(const void* p) {
+    return static_cast<uint32_t>(__cvta_generic_to_shared(p));
+}
 __device__ __forceinline__ void copy_async(uint32_t to, const void* from) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
 }
@@ -218,7 +220,7 @@ __global__ void __launch_bounds__(32 * kQWarps, 1) q4_kernel(const Q4Args a) {
         const int vecs = (min(a.pieces, p0 + kPer) - p0) * 16;   // of a token
         for (int i = threadIdx.x; i < rows * vecs; i += blockDim.x) {
             const int row = i / vecs, v = i % vecs, k = p0 * 128 + v * 8;
-            copy_async_or_zero(smem_u32(xs + row * stride + v * 16),
+            copy_async_or_zero(shared_at(xs + row * stride + v * 16),
                                a.x + (size_t)(tok0 + row) * a.K + (k < a.K ? k : 0), k < a.K);
         }
         copies_commit();
@@ -232,7 +234,7 @@ __global__ void __launch_bounds__(32 * kQWarps, 1) q4_kernel(const Q4Args a) {
         for (int r = 0; r < RT; ++r)
             from[r] = a.packed + min(next_set * RT + r, tiles - 1) * row_bytes + next_piece * PB + 16 * lane;
     };
-    const uint32_t ring_at = smem_u32(ring) + 16 * lane;
+    const uint32_t ring_at = shared_at(ring) + 16 * lane;
     const int ahead = a.team * PB;
     const auto issue = [&](int place) {
         if (next_set < sets) {

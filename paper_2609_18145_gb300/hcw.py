@@ -737,6 +737,13 @@ def _here(what, *ts):
                              % (what, t.device, dev))
 
 
+def _counts(what, *ns):
+    """ns are sizes that arrive in an int."""
+    for n in ns:
+        if n > 0x7fffffff:
+            raise ValueError("%s: a size of %d" % (what, n))
+
+
 def _typed(what, dtype, *ts):
     for t in ts:
         if t is not None and t.dtype != dtype:
@@ -751,6 +758,7 @@ def hcw_embed_fwd(ids, E, scale: float = 1.0, x=None, stream=None):
     if E.dim() != 2:
         raise ValueError("hcw_embed_fwd: E must be [V, d], got %s" % (tuple(E.shape),))
     V, d = E.shape
+    _counts("hcw_embed_fwd", ids.numel(), V, d)
     if x is None:
         x = _memory(stream).empty((*ids.shape, d), dtype=E.dtype, device=E.device)
     elif x.dtype != E.dtype or x.numel() != ids.numel() * d or x.dim() > 1 and (
@@ -779,6 +787,7 @@ def hcw_embed_bwd(ids, dx, V: int, scale: float = 1.0, dE=None, de_dtype=torch.f
     if dx.numel() != T * d or dx.dim() > 1 and not _same_rows(dx.shape[:-1], ids.shape):
         raise ValueError("hcw_embed_bwd: dx %s does not match ids %s"
                          % (tuple(dx.shape), tuple(ids.shape)))
+    _counts("hcw_embed_bwd", T, V, d)
     if dE is None:
         if accumulate:
             raise ValueError("hcw_embed_bwd: accumulate needs the dE to add to")
@@ -855,6 +864,7 @@ def hcw_q4_quantize(W, group: int = 64, codes=None, scales=None, stream=None):
     if W.dim() != 2:
         raise ValueError("hcw_q4_quantize: W must be [N, K], got %s" % (tuple(W.shape),))
     N, K = W.shape
+    _counts("hcw_q4_quantize", N, K)
     G = -(-K // group) if group > 0 else 0
     mem = _memory(stream)
     codes = mem.empty(N, K, dtype=torch.int8, device=W.device) if codes is None else codes
@@ -876,6 +886,7 @@ def hcw_q4_pack(codes, scales, group: int = 64, packed=None, stream=None):
     if codes.dim() != 2:
         raise ValueError("hcw_q4_pack: codes must be [N, K], got %s" % (tuple(codes.shape),))
     N, K = codes.shape
+    _counts("hcw_q4_pack", N, K)
     if group > 0 and tuple(scales.shape) != (N, -(-K // group)):
         raise ValueError("hcw_q4_pack: scales %s do not match codes %s in groups of %d"
                          % (tuple(scales.shape), tuple(codes.shape), group))
@@ -899,6 +910,7 @@ def hcw_q4_matmul(x, packed, N: int, group: int = 64, bias=None, y=None, y_dtype
     if not x.dim():
         raise ValueError("hcw_q4_matmul: x must be [..., K]")
     T, K = _rows(x)
+    _counts("hcw_q4_matmul", T, N, K)
     if bias is not None:
         _params("hcw_q4_matmul: bias", 1, N, bias)
     need = hcw_q4_bytes(N, K, group)
@@ -939,6 +951,7 @@ def hcw_logits_edit(z, history=None, lengths=None, prompt=None, repetition=None,
         _typed("hcw_logits_edit: bias_idx", torch.int32, bias_idx)
         _typed("hcw_logits_edit: bias", torch.float32, bias)
         M = bias.shape[1]
+    _counts("hcw_logits_edit", B, V, H, M)
     _row_values("hcw_logits_edit: lengths and prompt", torch.int32, B, None, lengths, prompt)
     _row_values("hcw_logits_edit: penalties", torch.float32, B, None, repetition, frequency, presence)
     if mask is not None:

@@ -68,6 +68,8 @@ def test_lookup_gradient_refusals(H):
     assert call(dE=dx) == call(dE=i) == call(w=dE) == call(w=dx) == H.HCW_ERR_ALIASING
     # fp32 gradients are twice as long
     assert call(dE=P(dx.value - V * d * 2)) == H.HCW_ERR_ALIASING
+    assert call(T=1 << 28, d=1 << 20, n=1 << 60, i=P(1 << 40), dx=P(1 << 50), dE=P(1 << 44),
+                w=P(1 << 55)) == H.HCW_ERR_UNSUPPORTED     # more chunks than a grid holds
     assert call(T=0, add=1, i=None, dx=None, w=None, n=0) == H.HCW_OK
     assert H.hcw_embed_bwd_workspace_bytes(0, V, d) == 0
     assert H.hcw_embed_bwd_workspace_bytes(T, V, 0) == 0
@@ -99,6 +101,9 @@ def test_clipping_refusals(H):
     assert call(g=(a, None)) == call(o=(c, None)) == H.HCW_ERR_INVALID_ARG
     assert H.lib().hcw_clip_grads(None, None, None, None, 1, 1.0, n, w, ws, None) == \
         H.HCW_ERR_INVALID_ARG
+    # (what an empty tensor's pointer is does not matter; the other one is refused)
+    assert call(g=(P(3), P(b.value + 2)), sizes=(0, 8)) == H.HCW_ERR_ALIGNMENT
+    assert call(g=(P(3), None), sizes=(0, 8)) == H.HCW_ERR_INVALID_ARG
     assert call(sizes=(1 << 45, 5)) == H.HCW_ERR_UNSUPPORTED
     assert call(g=(P(a.value + 1), b)) == call(g=(a, P(b.value + 2))) == H.HCW_ERR_ALIGNMENT
     assert call(n=P(n.value + 2)) == call(w=P(w.value + 8)) == H.HCW_ERR_ALIGNMENT
