@@ -726,7 +726,7 @@ int hcw_embed_bwd(const int* ids, const void* dx, int T, int V, int d, int dtype
  * Any finite gradients have their norm (squares that leave fp32's range are scaled); beyond fp32's
  * largest number norm[0] is infinite while c still is max_norm / n.  Where an element is infinite or
  * NaN so is norm[0], and c = 1: the gradients stay as they are, for the caller to skip the step.
- * In place with c = 1 nothing is written.  Sums above 1024 squares are fp64, in a fixed order: the
+ * In place with c = 1 nothing is written.  Sums above 2048 squares are fp64, in a fixed order: the
  * same inputs give the same bits.  An output or the workspace that overlaps another tensor (in
  * place: two tensors that share memory) is HCW_ERR_ALIASING.  Two launches for up to 512 tensors.
  */

@@ -1,9 +1,9 @@
 """GPU parity of hcw_clip_grads with the fp64 oracle.
 
-Tolerances, u = 2^-24.  A thread adds 32 squares in two chains of 16 multiply-adds and two additions,
-a warp its threads in 5 more: every term is positive, so the sum is off by at most 23 u relative, its
-root by half of that, by another half for the sum's rounding to fp32 before it and u for its own: 13 u.
-The factor is a quotient with that root: 14 u.  Below
+Tolerances, u = 2^-24.  A thread adds up to 64 squares in four chains of 16 multiply-adds and three
+additions, a warp its threads in 5 more: every term is positive, so the sum is off by at most 24 u
+relative, its root by half of that, by another half for the sum's rounding to fp32 before it and u for
+its own: 13.5 u.  The factor is a quotient with that root: 14.5 u.  Below
 2^-126 fp32's half step is 2^-150 whatever the value: norm and factor, which are returned in fp32, are
 off by that there.  An output is one product (u) rounded once (half a step).
 """
@@ -58,11 +58,11 @@ def check(H, sizes, dtypes, limit, seed=0, std=1.0, at=0, apart=None, stream=Non
     torch.cuda.synchronize()
     assert bool((ws[need:] == 0xFF).all())
     n, c = norm.double().cpu().tolist()
-    assert abs(n - n64) <= 13 * U * n64 + 2.0 ** -150 and \
-        abs(c - c64) <= 14 * U * c64 + 2.0 ** -150, (n, n64, c, c64)
+    assert abs(n - n64) <= 14 * U * n64 + 2.0 ** -150 and \
+        abs(c - c64) <= 15 * U * c64 + 2.0 ** -150, (n, n64, c, c64)
     for k, (o, b, r, old, dt) in enumerate(zip(outs, obufs, ref, before, dtypes)):
         got = o.double().cpu().numpy()
-        bound = 15 * U * np.abs(r)
+        bound = 16 * U * np.abs(r)
         bound = bound + HALF[dt] * (np.abs(r) + bound) + 1e-44
         assert (np.abs(got - r) <= bound).all(), k
         if c64 == 1.0:
@@ -126,7 +126,7 @@ def test_squares_that_leave_the_range(H, std):
 def test_small_and_large_side_by_side(H):
     g = torch.cat([torch.full((16384 * 2,), 1e-25), torch.full((3,), 1e25)]).cuda()
     norm = H.hcw_clip_grads([g], 1.0)
-    assert abs(float(norm[0]) - math.sqrt(3) * 1e25) <= 13 * U * 2e25
+    assert abs(float(norm[0]) - math.sqrt(3) * 1e25) <= 14 * U * 2e25
     assert bool((g[:5] == 0).all()) or float(g[:5].max()) < 1e-44
     assert abs(float(g[-1]) - 3 ** -0.5) < 1e-6
 
@@ -159,7 +159,7 @@ def test_zeros_no_tensors_and_the_norm_alone(H):
     r = torch.randn(40000, device="cuda")
     old = r.clone()
     n = H.hcw_clip_grads([r], float("inf"))
-    assert abs(float(n[0]) - float(old.double().norm())) <= 13 * U * float(n[0]) and float(n[1]) == 1.0
+    assert abs(float(n[0]) - float(old.double().norm())) <= 14 * U * float(n[0]) and float(n[1]) == 1.0
     assert torch.equal(r, old)
     out = torch.full_like(r, 7.0)
     H.hcw_clip_grads(H.GradList([r], [out]), float("inf"))
