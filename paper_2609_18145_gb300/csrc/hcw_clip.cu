@@ -195,7 +195,8 @@ __global__ void __launch_bounds__(kCThreads, 2) clip_norm_kernel(const __grid_co
 
 // What the sum of squares says: the norm, the factor, and the factor as two (pre = 2^-40 apart where
 // fp32 would hold the factor in fewer bits; what that takes below fp32's normal numbers ends at zero).
-// The root is that of the sum's leading digits, in fp32.
+// fp64's own root and quotient take about a microsecond here: fp32's, with one correction each from their
+// remainder in fp64, are right to their last bit but for ties.
 struct Clip {
     float norm, factor, pre, rest;
 };
@@ -203,12 +204,15 @@ __device__ __forceinline__ Clip clip_of(double sum, float max_norm) {
     Clip c = {(float)sum, 1.f, 1.f, 1.f};   // 0, infinity or NaN
     if (sum > 0.0 && sum < INFINITY) {
         const int e = ((__double2hiint(sum) >> 20) - 1023) & ~1, h = e / 2;
-        const float root = sqrtf((float)(sum * __hiloint2double((1023 - e) << 20, 0)));   // of 1 .. 4
-        c.norm = scalbnf(root, h);
+        const double lead = sum * __hiloint2double((1023 - e) << 20, 0);   // 1 .. 4
+        const float r = sqrtf((float)lead);
+        const double root = (double)r + (double)((float)(lead - (double)r * r) * 0.5f / r);
+        c.norm = scalbnf((float)root, h);
         if (c.norm > max_norm) {
             // (a limit of few bits is scaled before the quotient would lose its own)
             const bool small = max_norm < 0x1p-60f;
-            const float q = (small ? max_norm * 0x1p64f : max_norm) / root;
+            const float limit = small ? max_norm * 0x1p64f : max_norm, q0 = limit / r;
+            const float q = (float)((double)q0 + (double)((float)((double)limit - q0 * root) / r));
             const int shift = small ? -h - 64 : -h;
             c.factor = c.rest = scalbnf(q, shift);
             if (c.factor < 0x1p-80f) {
