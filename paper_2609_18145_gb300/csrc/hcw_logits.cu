@@ -91,7 +91,8 @@ struct Penalty {
 // ------------------------------------------------------------------ one launch
 // A slice of 256 vectors of 16 bytes, from the boundary at or before the row's start, for a CTA of as
 // many threads.  What it needs is asked for at once, before the counters are cleared: its logits, its
-// words of the mask, the first 1024 symbols of the history, the first 256 slots.
+// words of the mask, the first 1024 symbols of the history, the first 256 slots.  Bound by latency: a
+// launch, one round of loads, three barriers (1 x 201 fp32 2.4 us, 8 x 131072 bf16 5.2).
 template <typename T>
 __global__ void __launch_bounds__(256) logits_edit_kernel(const LogitsArgs a) {
     constexpr int NT = 256, NH = 4, VE = 16 / sizeof(T), S = NT * VE;
@@ -250,7 +251,8 @@ __global__ void __launch_bounds__(256) logits_edit_kernel(const LogitsArgs a) {
 
 // ------------------------------------------------------------------ two launches
 // The whole row first: logits and mask, four vectors a thread.  A vector that the mask takes out
-// entirely is not read; in place one that it lets through entirely is not touched.
+// entirely is not read; in place one that it lets through entirely is not touched.  Bound by memory:
+// 256 x 131072 fp32 without a mask 43 us, 6.2 TB/s.
 template <typename T>
 __global__ void __launch_bounds__(256) logits_mask_kernel(const LogitsArgs a) {
     constexpr int VE = 16 / sizeof(T), NV = 4;

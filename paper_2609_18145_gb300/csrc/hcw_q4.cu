@@ -195,6 +195,12 @@ __device__ __forceinline__ void copies_wait() {
 // through a ring of each warp's own, by asynchronous copies, D pieces of its RT tiles ahead; the
 // activations are in shared memory, kQChunk of the k range at a time.  Tiles and tokens past the last
 // ones are computed as something, and not written.
+//
+// Where there are many row tiles a warp has two of them to itself: no sums to join, and the activations'
+// way from shared memory serves both.  131072 x 4096, groups of 128: one token 52 us (5.4 TB/s), 8 54, 16
+// 65; bound by the issue of instructions, nine for every eight weights of a lane, and with 16 tokens
+// by the MMA too (46 % of its cycles).  A k range shared by 8 warps took 74 and 94 us: joining the
+// sums and reading the activations again and again cost as much as the products.
 template <int RT, int NT, int GROUP, int D>
 __global__ void __launch_bounds__(32 * kQWarps, 1) q4_kernel(const Q4Args a) {
     constexpr int GM = GROUP / 16;                 // MMAs of a group
