@@ -338,7 +338,7 @@ __global__ void __launch_bounds__(kSortThreads) embed_place_kernel(const SortArg
 }
 
 // For larger vocabularies: a CTA a range, which collects its own in their order and sorts them, 8 bits
-// of the symbol a pass, each warp counting and placing a run of them.
+// of the symbol in each of two passes, each warp counting and placing a run of them.
 __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const SortArgs a) {
     __shared__ __align__(16) int hist[kDigits * kSortWarps];
     __shared__ uint32_t named[kMaxRange / 32];
@@ -419,29 +419,22 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const SortArgs
         }
         const int own = ((m + kSortThreads - 1) / kSortThreads) * 32;   // of a warp
         const int m0 = min(m, warp * own), m1 = min(m, m0 + own);
-        for (int shift = 0; shift == 0 || (a.range - 1) >> shift; shift += 8) {
-            const bool last = !((a.range - 1) >> (shift + 8));
-            // (counters of the digits that occur: 8 a thread, two vectors)
-            const int used = min(kDigits, a.range) * kSortWarps;
+        for (int shift = 0; shift < 16; shift += 8) {
+            const bool last = shift == 8;
+            // (8 counters a thread, two vectors)
+            static_assert(kDigits * kSortWarps == 8 * kSortThreads, "a thread's counters");
             int4* const my = reinterpret_cast<int4*>(hist) + 2 * threadIdx.x;
-            const bool in = 8 * (int)threadIdx.x < used;
-            if (in) my[0] = my[1] = make_int4(0, 0, 0, 0);
+            my[0] = my[1] = make_int4(0, 0, 0, 0);
             __syncthreads();   // and the list is there
             for (int i = m0 + lane; i < m1; i += 32)
                 atomicAdd(&hist[(((key[i] - lo) >> shift) & (kDigits - 1)) * kSortWarps + warp], 1);
             __syncthreads();
             // places: by digit, then by warp
-            int4 c = make_int4(0, 0, 0, 0), e = c;
-            if (in) {
-                c = my[0];
-                e = my[1];
-            }
+            const int4 c = my[0], e = my[1];
             int all, p = block_prefix(c.x + c.y + c.z + c.w + e.x + e.y + e.z + e.w, scratch, &all);
             const int q = p + c.x + c.y + c.z + c.w;
-            if (in) {
-                my[0] = make_int4(p, p + c.x, p + c.x + c.y, p + c.x + c.y + c.z);
-                my[1] = make_int4(q, q + e.x, q + e.x + e.y, q + e.x + e.y + e.z);
-            }
+            my[0] = make_int4(p, p + c.x, p + c.x + c.y, p + c.x + c.y + c.z);
+            my[1] = make_int4(q, q + e.x, q + e.x + e.y, q + e.x + e.y + e.z);
             __syncthreads();
             for (int i0 = m0; i0 < m1; i0 += 32) {
                 const int i = i0 + lane;

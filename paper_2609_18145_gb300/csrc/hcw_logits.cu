@@ -78,6 +78,19 @@ __device__ __forceinline__ uint4 pack(const float (&v)[VE]) {
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+// f(symbol, t) for the history's entries from `from` on, eight of a thread's on their way at once.
+template <int NT, typename F>
+__device__ __forceinline__ void rest_of_history(const int* h, int from, int n, F f) {
+    for (long long t0 = from + (int)threadIdx.x; t0 < n; t0 += 8 * NT) {
+        int v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = t0 + i * NT < n ? h[t0 + i * NT] : -1;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (t0 + i * NT < n) f(v[i], (int)t0 + i * NT);
+    }
+}
+
 struct Penalty {
     float rep, freq, pres;
     __device__ __forceinline__ float operator()(float z, uint32_t c) const {
@@ -156,7 +169,7 @@ __global__ void __launch_bounds__(256) logits_edit_kernel(const LogitsArgs a) {
 #pragma unroll
     for (int i = 0; i < NH; ++i)
         if ((int)threadIdx.x + i * NT < n) mark(past[i], threadIdx.x + i * NT);
-    for (int t = threadIdx.x + NH * NT; t < n; t += NT) mark(h[t], t);
+    rest_of_history<NT>(h, NH * NT, n, mark);
     // the slice's slots, in their order
     int slots = 0;
     for (int k0 = 0; k0 < a.M; k0 += NT) {
@@ -396,10 +409,10 @@ __global__ void __launch_bounds__(NT) logits_named_kernel(const LogitsArgs a, in
         if (past[i] >= 0) mark(past[i], t);
     }
     if (!HASH)
-        for (int t = threadIdx.x + kLNames; t < n; t += NT) {
-            const int p = place(h[t]);
+        rest_of_history<NT>(h, kLNames, n, [&](int symbol, int t) {
+            const int p = place(symbol);
             if (p >= 0) mark(p, t);
-        }
+        });
 #pragma unroll
     for (int i = 0; i < NS; ++i) {
         const int symbol = slot[i];
@@ -460,12 +473,11 @@ __global__ void __launch_bounds__(NT) logits_named_kernel(const LogitsArgs a, in
     for (int i = 0; i < NS; ++i)
         if (at[i] >= 0) put(out + at[i], pen(sv[i], sc[i] & ~kMore) + sum[i]);
     if (!HASH)
-        for (int t = threadIdx.x + kLNames; t < n; t += NT) {
-            const int symbol = h[t];
+        rest_of_history<NT>(h, kLNames, n, [&](int symbol, int) {
             uint32_t m;
             const int j = symbol >= lo && symbol < hi ? taken(symbol - lo, &m) : -1;
             if (j >= 0 && passes(j)) put(out + j, pen(value(z + j), m));
-        }
+        });
 }
 
 template <typename T, bool HASH, int NT>

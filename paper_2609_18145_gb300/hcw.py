@@ -13,6 +13,7 @@ torch.float32 -> HCW_F32.
 from __future__ import annotations
 
 import ctypes
+import functools
 import math
 import os
 import threading
@@ -720,28 +721,40 @@ def hcw_distill_loss(z, idx=None, teacher=None, target=None, weight=None,
     return loss, dz
 
 
+def _refuse(what, t, dev):
+    if not t.is_cuda:
+        raise ValueError("%s: all tensors must be CUDA tensors" % what)
+    if not t.is_contiguous():
+        raise ValueError("%s: all tensors must be contiguous" % what)
+    raise ValueError("%s: a tensor of %s, but the current device is cuda:%d" % (what, t.device, dev))
+
+
 def _here(what, *ts):
-    """ts (None allowed) are contiguous tensors of the current device, where the launch goes."""
-    dev = None
+    """ts (None allowed) are contiguous tensors of the current device, where the launch goes.
+    Returns its number."""
+    try:
+        dev = _current_device()
+    except RuntimeError:   # no device: no tensor is there
+        dev = -2
     for t in ts:
-        if t is None:
-            continue
-        if not t.is_cuda:
-            raise ValueError("%s: all tensors must be CUDA tensors" % what)
-        if not t.is_contiguous():
-            raise ValueError("%s: all tensors must be contiguous" % what)
-        if dev is None:
-            dev = _current_device()
-        if t.get_device() != dev:
-            raise ValueError("%s: a tensor of %s, but the current device is cuda:%d"
-                             % (what, t.device, dev))
+        if t is not None and (t.get_device() != dev or not t.is_contiguous()):
+            _refuse(what, t, dev)
+    return dev
+
+
+def _on(stream, dev):
+    """The handle of `stream`, or of the current stream of device dev."""
+    if stream is not None:
+        return stream.cuda_stream
+    if _raw_stream is None:
+        return torch.cuda.current_stream().cuda_stream
+    return _raw_stream(dev)
 
 
 def _counts(what, *ns):
     """ns are sizes that arrive in an int."""
-    for n in ns:
-        if n > 0x7fffffff:
-            raise ValueError("%s: a size of %d" % (what, n))
+    if max(ns) > 0x7fffffff:
+        raise ValueError("%s: a size of %d" % (what, max(ns)))
 
 
 def _typed(what, dtype, *ts):
@@ -753,20 +766,21 @@ def _typed(what, dtype, *ts):
 def hcw_embed_fwd(ids, E, scale: float = 1.0, x=None, stream=None):
     """x[t] = scale E[ids[t]]: rows of E [V, d] for ids [...] int32 (negative: zeros).
     Returns x [..., d]."""
-    _here("hcw_embed_fwd", ids, E, x)
+    dev = _here("hcw_embed_fwd", ids, E, x)
     _typed("hcw_embed_fwd: ids", torch.int32, ids)
     if E.dim() != 2:
         raise ValueError("hcw_embed_fwd: E must be [V, d], got %s" % (tuple(E.shape),))
     V, d = E.shape
-    _counts("hcw_embed_fwd", ids.numel(), V, d)
+    T, dtype = ids.numel(), E.dtype
+    _counts("hcw_embed_fwd", T, V, d)
     if x is None:
-        x = _memory(stream).empty((*ids.shape, d), dtype=E.dtype, device=E.device)
-    elif x.dtype != E.dtype or x.numel() != ids.numel() * d or x.dim() > 1 and (
+        x = _memory(stream).empty((*ids.shape, d), dtype=dtype, device=E.device)
+    elif x.dtype != dtype or x.numel() != T * d or x.dim() > 1 and (
             x.shape[-1] != d or not _same_rows(x.shape[:-1], ids.shape)):
         raise ValueError("hcw_embed_fwd: x %s %s does not match ids %s and E %s %s"
-                         % (tuple(x.shape), x.dtype, tuple(ids.shape), tuple(E.shape), E.dtype))
-    _check(lib().hcw_embed_fwd(_ptr(ids), _ptr(E), ids.numel(), V, d, _dtype_code(E), scale, _ptr(x),
-                               _stream(stream)), "hcw_embed_fwd")
+                         % (tuple(x.shape), x.dtype, tuple(ids.shape), tuple(E.shape), dtype))
+    _check(lib().hcw_embed_fwd(ids.data_ptr(), E.data_ptr(), T, V, d, _dtype_code(E), scale,
+                               x.data_ptr(), _on(stream, dev)), "hcw_embed_fwd")
     return x
 
 
@@ -779,7 +793,7 @@ def hcw_embed_bwd(ids, dx, V: int, scale: float = 1.0, dE=None, de_dtype=torch.f
     """Gradient of hcw_embed_fwd: dE[v] = scale * the sum of dx's rows with ids = v.
     dE [V, d] in its own type (new: de_dtype); accumulate=True adds to the dE given.
     Returns dE."""
-    _here("hcw_embed_bwd", ids, dx, dE, workspace)
+    dev = _here("hcw_embed_bwd", ids, dx, dE, workspace)
     _typed("hcw_embed_bwd: ids", torch.int32, ids)
     if not dx.dim():
         raise ValueError("hcw_embed_bwd: dx must be [..., d]")
@@ -796,9 +810,10 @@ def hcw_embed_bwd(ids, dx, V: int, scale: float = 1.0, dE=None, de_dtype=torch.f
         raise ValueError("hcw_embed_bwd: dE %s is not [%d, %d]" % (tuple(dE.shape), V, d))
     if workspace is None:
         workspace = _workspace(stream, hcw_embed_bwd_workspace_bytes(T, V, d), dx.device, None)
-    _check(lib().hcw_embed_bwd(_ptr(ids), _ptr(dx), T, V, d, _dtype_code(dx), scale,
-                               int(bool(accumulate)), _dtype_code(dE), _ptr(dE), _ptr(workspace),
-                               workspace.nbytes, _stream(stream)), "hcw_embed_bwd")
+    _check(lib().hcw_embed_bwd(ids.data_ptr(), dx.data_ptr(), T, V, d, _dtype_code(dx), scale,
+                               int(bool(accumulate)), _dtype_code(dE), dE.data_ptr(),
+                               workspace.data_ptr(), workspace.nbytes, _on(stream, dev)),
+           "hcw_embed_bwd")
     return dE
 
 
@@ -820,6 +835,7 @@ class GradList:
                     raise ValueError("GradList: output %s %s does not match gradient %s %s"
                                      % (tuple(o.shape), o.dtype, tuple(g.shape), g.dtype))
         self.device = self.grads[0].device if n else None
+        self._dev = self.grads[0].get_device() if n else None
         self.count = n
         self._grads = (_P * n)(*[_ptr(g) for g in self.grads])
         self._out = None if self.out is None else (_P * n)(*[_ptr(o) for o in self.out])
@@ -836,22 +852,23 @@ def hcw_clip_grads(grads, max_norm: float, norm=None, workspace=None, stream=Non
     min(1, max_norm / norm over all of them); max_norm = inf takes the norm alone.  Returns
     the tensor [2] fp32 of the norm and the factor (on the device: nothing waits)."""
     q = grads if isinstance(grads, GradList) else GradList(grads)
-    _here("hcw_clip_grads", norm, workspace)
-    if q.device is not None and q.device.index != _current_device():
+    dev = _here("hcw_clip_grads", norm, workspace)
+    if q._dev is not None and q._dev != dev:
         raise ValueError("hcw_clip_grads: gradients of %s, but the current device is cuda:%d"
-                         % (q.device, _current_device()))
+                         % (q.device, dev))
     if norm is None:
         norm = _memory(stream).empty(2, dtype=torch.float32, device=q.device or "cuda")
     elif norm.dtype != torch.float32 or norm.numel() != 2:
         raise ValueError("hcw_clip_grads: norm must be 2 float32 values")
     if workspace is None:
         workspace = _workspace(stream, hcw_clip_grads_workspace_bytes(q.count), norm.device, None)
-    _check(lib().hcw_clip_grads(q._grads, q._out, q._sizes, q._dtypes, q.count, max_norm, _ptr(norm),
-                                _ptr(workspace), workspace.nbytes, _stream(stream)),
-           "hcw_clip_grads")
+    _check(lib().hcw_clip_grads(q._grads, q._out, q._sizes, q._dtypes, q.count, max_norm,
+                                norm.data_ptr(), workspace.data_ptr(), workspace.nbytes,
+                                _on(stream, dev)), "hcw_clip_grads")
     return norm
 
 
+@functools.lru_cache(maxsize=1024)
 def hcw_q4_bytes(N: int, K: int, group: int) -> int:
     return int(lib().hcw_q4_bytes(N, K, group))
 
@@ -904,7 +921,7 @@ def hcw_q4_matmul(x, packed, N: int, group: int = 64, bias=None, y=None, y_dtype
                   stream=None):
     """y = x W^T (+ bias) of a few tokens x [..., K] bf16 with the packed weights of N rows in
     groups of `group`; y [..., N] is bf16 or fp32 (y's type, or y_dtype for a new one)."""
-    _here("hcw_q4_matmul", x, packed, bias, y)
+    dev = _here("hcw_q4_matmul", x, packed, bias, y)
     _typed("hcw_q4_matmul: x", torch.bfloat16, x)
     _typed("hcw_q4_matmul: packed", torch.uint8, packed)
     if not x.dim():
@@ -923,8 +940,8 @@ def hcw_q4_matmul(x, packed, N: int, group: int = 64, bias=None, y=None, y_dtype
                                                 not _same_rows(y.shape[:-1], x.shape[:-1])):
         raise ValueError("hcw_q4_matmul: y %s does not match x %s and N = %d"
                          % (tuple(y.shape), tuple(x.shape), N))
-    _check(lib().hcw_q4_matmul(_ptr(x), _ptr(packed), _ptr(bias), T, N, K, group, _dtype_code(y),
-                               _ptr(y), _stream(stream)), "hcw_q4_matmul")
+    _check(lib().hcw_q4_matmul(x.data_ptr(), packed.data_ptr(), _ptr(bias), T, N, K, group,
+                               _dtype_code(y), y.data_ptr(), _on(stream, dev)), "hcw_q4_matmul")
     return y
 
 
@@ -933,42 +950,45 @@ def hcw_logits_edit(z, history=None, lengths=None, prompt=None, repetition=None,
     """Logits z [B, V] with penalties for the symbols of history [B, H], biases in slots
     (bias_idx, bias [B, M]) and a mask of bits [B, ceil(V / 32)] int32; see hcw.h.  out = z
     edits in place.  Returns out."""
-    _here("hcw_logits_edit", z, history, lengths, prompt, repetition, frequency, presence, bias_idx,
-          bias, mask, out)
+    what = "hcw_logits_edit"
+    dev = _here(what, z, history, lengths, prompt, repetition, frequency, presence, bias_idx, bias,
+                mask, out)
     if z.dim() != 2:
-        raise ValueError("hcw_logits_edit: z must be [B, V], got %s" % (tuple(z.shape),))
+        raise ValueError("%s: z must be [B, V], got %s" % (what, tuple(z.shape)))
     B, V = z.shape
     H = M = 0
     if history is not None:
         _typed("hcw_logits_edit: history", torch.int32, history)
         if history.dim() != 2 or history.shape[0] != B:
-            raise ValueError("hcw_logits_edit: history %s is not [%d, H]" % (tuple(history.shape), B))
+            raise ValueError("%s: history %s is not [%d, H]" % (what, tuple(history.shape), B))
         H = history.shape[1]
     if bias_idx is not None or bias is not None:
         if bias_idx is None or bias is None or bias_idx.shape != bias.shape or \
                 bias.dim() != 2 or bias.shape[0] != B:
-            raise ValueError("hcw_logits_edit: bias_idx and bias must both be [%d, M]" % B)
+            raise ValueError("%s: bias_idx and bias must both be [%d, M]" % (what, B))
         _typed("hcw_logits_edit: bias_idx", torch.int32, bias_idx)
         _typed("hcw_logits_edit: bias", torch.float32, bias)
         M = bias.shape[1]
-    _counts("hcw_logits_edit", B, V, H, M)
+    _counts(what, B, V, H, M)
     _row_values("hcw_logits_edit: lengths and prompt", torch.int32, B, None, lengths, prompt)
     _row_values("hcw_logits_edit: penalties", torch.float32, B, None, repetition, frequency, presence)
     if mask is not None:
         _typed("hcw_logits_edit: mask", torch.int32, mask)
-        if tuple(mask.shape) != (B, -(-V // 32)):
-            raise ValueError("hcw_logits_edit: mask %s is not [%d, %d]"
-                             % (tuple(mask.shape), B, -(-V // 32)))
+        if mask.shape != (B, -(-V // 32)):
+            raise ValueError("%s: mask %s is not [%d, %d]" % (what, tuple(mask.shape), B, -(-V // 32)))
     if out is None:
         out = _memory(stream).empty_like(z)
     elif out.shape != z.shape or out.dtype != z.dtype:
-        raise ValueError("hcw_logits_edit: out %s %s does not match z %s %s"
-                         % (tuple(out.shape), out.dtype, tuple(z.shape), z.dtype))
-    _check(lib().hcw_logits_edit(
-        _ptr(z), B, V, _dtype_code(z), _ptr(history) if H else None, _ptr(lengths) if H else None,
-        _ptr(prompt) if H else None, H, _ptr(repetition), _ptr(frequency), _ptr(presence),
-        _ptr(bias_idx) if M else None, _ptr(bias) if M else None, M, _ptr(mask), _ptr(out),
-        _stream(stream)), "hcw_logits_edit")
+        raise ValueError("%s: out %s %s does not match z %s %s"
+                         % (what, tuple(out.shape), out.dtype, tuple(z.shape), z.dtype))
+    if not H:
+        history = lengths = prompt = None
+    if not M:
+        bias_idx = bias = None
+    _check(lib().hcw_logits_edit(z.data_ptr(), B, V, _dtype_code(z), _ptr(history), _ptr(lengths),
+                                 _ptr(prompt), H, _ptr(repetition), _ptr(frequency), _ptr(presence),
+                                 _ptr(bias_idx), _ptr(bias), M, _ptr(mask), out.data_ptr(),
+                                 _on(stream, dev)), what)
     return out
 
 

@@ -219,7 +219,7 @@ def test_shapes_are_checked(H):
 
 
 LARGE = [(60, 50001, 300, 64), (200, 20003, 4000, 90), (3, 1500001, 40, 1024), (40, 131072, 4097, 5),
-         (900, 8191, 60, 20), (40, 131072, 0, 30), (40, 131072, 700, 0)]
+         (900, 8191, 60, 20), (40, 131072, 0, 30), (40, 131072, 700, 0), (30, 60001, 20000, 40)]
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
