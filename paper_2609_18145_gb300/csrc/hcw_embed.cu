@@ -43,119 +43,156 @@ __device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162flo
 __device__ __forceinline__ void put(float* p, float v) { *p = v; }
 __device__ __forceinline__ void put(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
 
-// E elements of a row for a lane: one load where the rows lie on 16 bytes (WIDE), else every
-// 32nd element.  `left`: elements of the row from the block's first one.
-template <typename T, int E, bool WIDE>
-__device__ __forceinline__ void load_row(const T* p, int lane, int left, float (&v)[E]) {
-    if constexpr (WIDE) {
-        static_assert(E * sizeof(T) == 16, "a vector");
-        uint4 q = make_uint4(0, 0, 0, 0);
-        if (lane * E < left) q = *reinterpret_cast<const uint4*>(p + lane * E);
-        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+// A row's elements as a warp takes them, 16 bytes a lane in loads of W bytes: 16 where the rows lie
+// on 16 bytes, else as much as all of them lie on (4, or 2 for bf16 rows of odd width).
+template <int W>
+struct Raw;
+template <>
+struct Raw<16> {
+    using type = uint4;
+};
+template <>
+struct Raw<4> {
+    using type = uint32_t;
+};
+template <>
+struct Raw<2> {
+    using type = unsigned short;
+};
+template <typename T, int W>
+struct Cols {
+    static constexpr int E = 16 / sizeof(T);   // elements of a lane, of 32 E
+    static constexpr int P = W / sizeof(T);    // neighbours among them
+    static constexpr int L = E / P;            // loads
+    static __device__ __forceinline__ int at(int lane, int e) { return (lane + 32 * (e / P)) * P + e % P; }
+};
+
+// A lane's elements of a row on their way, as they lie there.  `left`: elements of the row from the
+// block's first one, a multiple of P; what would lie behind them is the last P again (loads under a
+// condition waited one for another: gradient of 65536 tokens, 32000 x 1023 fp32, 259 us, without 101).
+template <typename T, int W>
+struct Row {
+    using C = Cols<T, W>;
+    typename Raw<W>::type q[C::L];
+    __device__ __forceinline__ void load(const T* p, int lane, int left) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if constexpr (E == 8) {
-                v[2 * i] = __uint_as_float(w[i] << 16);
-                v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-            } else {
-                v[i] = __uint_as_float(w[i]);
-            }
+        for (int l = 0; l < C::L; ++l)
+            q[l] = *reinterpret_cast<const typename Raw<W>::type*>(p + min((lane + 32 * l) * C::P, left - C::P));
+    }
+    __device__ __forceinline__ void get(float (&v)[C::E]) const {
+        if constexpr (W == 16) {
+            const uint32_t w[4] = {q[0].x, q[0].y, q[0].z, q[0].w};
+#pragma unroll
+            for (int e = 0; e < C::E; ++e) v[e] = part(w[e * sizeof(T) / 4], e);
+        } else {
+#pragma unroll
+            for (int e = 0; e < C::E; ++e) v[e] = part(q[e / C::P], e);
         }
-    } else {
+    }
+    // element e of the row in the word that holds it
+    __device__ __forceinline__ static float part(uint32_t w, int e) {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w);
+        return __uint_as_float(W != 2 && (e & 1) ? w & 0xffff0000u : w << 16);
+    }
+};
+
+// P neighbours of a row of type O: 16 bytes at a time at most.
+template <int P>
+__device__ __forceinline__ void get_piece(const float* p, float* v) {
+    if constexpr (P >= 4) {
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-            v[e] = lane + 32 * e < left ? to_f32(p[lane + 32 * e]) : 0.f;
+        for (int i = 0; i < P / 4; ++i) {
+            const float4 q = reinterpret_cast<const float4*>(p)[i];
+            v[4 * i] = q.x;
+            v[4 * i + 1] = q.y;
+            v[4 * i + 2] = q.z;
+            v[4 * i + 3] = q.w;
+        }
+    } else if constexpr (P == 2) {
+        const float2 q = *reinterpret_cast<const float2*>(p);
+        v[0] = q.x;
+        v[1] = q.y;
+    } else {
+        v[0] = p[0];
     }
 }
-
-// The lane's E elements of a row on their way: as they lie there where one load takes them.
-template <typename T, int E, bool WIDE>
-struct Row {
-    float v[E];
-    __device__ __forceinline__ void load(const T* p, int lane, int left) {
-        load_row<T, E, false>(p, lane, left, v);
-    }
-    __device__ __forceinline__ void add_to(float (&s)[E]) const {
+template <int P>
+__device__ __forceinline__ void get_piece(const __nv_bfloat16* p, float* v) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) s[e] += v[e];
-    }
-};
-template <typename T, int E>
-struct Row<T, E, true> {
-    uint4 q;
-    __device__ __forceinline__ void load(const T* p, int lane, int left) {
-        q = make_uint4(0, 0, 0, 0);
-        if (lane * E < left) q = *reinterpret_cast<const uint4*>(p + lane * E);
-    }
-    __device__ __forceinline__ void add_to(float (&s)[E]) const {
-        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+    for (int i = 0; i < P; ++i) v[i] = to_f32(p[i]);
+}
+template <int P>
+__device__ __forceinline__ void put_piece(float* p, const float* v) {
+    if constexpr (P >= 4) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if constexpr (E == 8) {
-                s[2 * i] += __uint_as_float(w[i] << 16);
-                s[2 * i + 1] += __uint_as_float(w[i] & 0xffff0000u);
-            } else {
-                s[i] += __uint_as_float(w[i]);
-            }
-        }
-    }
-};
-
-// The lane's E elements of an output row (of type O, rounded here).
-template <typename O, int E, bool WIDE>
-__device__ __forceinline__ void store_row(O* p, int lane, int left, const float (&v)[E]) {
-    if constexpr (WIDE) {
-        if (lane * E >= left) return;
-        if constexpr (sizeof(O) == 4) {
-#pragma unroll
-            for (int i = 0; i < E / 4; ++i)
-                reinterpret_cast<float4*>(p + lane * E)[i] =
-                    make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
-        } else {
-            uint32_t w[E / 2];
-#pragma unroll
-            for (int i = 0; i < E / 2; ++i) w[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
-            if constexpr (E == 8)
-                *reinterpret_cast<uint4*>(p + lane * E) = make_uint4(w[0], w[1], w[2], w[3]);
-            else
-                *reinterpret_cast<uint2*>(p + lane * E) = make_uint2(w[0], w[1]);
-        }
+        for (int i = 0; i < P / 4; ++i)
+            reinterpret_cast<float4*>(p)[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+    } else if constexpr (P == 2) {
+        *reinterpret_cast<float2*>(p) = make_float2(v[0], v[1]);
     } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-            if (lane + 32 * e < left) put(p + lane + 32 * e, v[e]);
+        p[0] = v[0];
     }
+}
+template <int P>
+__device__ __forceinline__ void put_piece(__nv_bfloat16* p, const float* v) {
+    if constexpr (P == 8)
+        *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]),
+                                                  pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+    else if constexpr (P == 4)
+        *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+    else if constexpr (P == 2)
+        *reinterpret_cast<uint32_t*>(p) = pack_bf16x2(v[0], v[1]);
+    else
+        put(p, v[0]);
+}
+// The lane's elements of an output row (of type O, rounded here).
+template <typename C, typename O>
+__device__ __forceinline__ void store_row(O* p, int lane, int left, const float (&v)[C::E]) {
+#pragma unroll
+    for (int l = 0; l < C::L; ++l) {
+        const int j = (lane + 32 * l) * C::P;
+        if (j < left) put_piece<C::P>(p + j, v + l * C::P);
+    }
+}
+template <typename C, typename O>
+__device__ __forceinline__ void load_out(const O* p, int lane, int left, float (&v)[C::E]) {
+#pragma unroll
+    for (int l = 0; l < C::L; ++l) get_piece<C::P>(p + min((lane + 32 * l) * C::P, left - C::P), v + l * C::P);
 }
 
 // ------------------------------------------------------------------ lookup
 // A warp takes R rows, 32 E columns of them: all R rows' loads on their way at once, as nothing but
 // memory bounds it (65536 of 131072 x 2048 bf16: 56 us, 6.2 TB/s of rows read and written; 64 of
 // 32000 x 512, where the wait for a row after its id counts: 1.2 us).
-template <typename T, int E, bool WIDE, int R>
+template <typename T, int W, int R>
 __global__ void __launch_bounds__(256) embed_fwd_kernel(const int* ids, const T* table, long long T_,
                                                         int V, int d, float scale, T* x) {
+    using C = Cols<T, W>;
     pdl_wait();
     pdl_trigger();
     const int lane = threadIdx.x & 31;
     const long long row0 = ((long long)blockIdx.x * 8 + (threadIdx.x >> 5)) * R;
-    const int col = blockIdx.y * (32 * E);
+    const int col = blockIdx.y * (32 * C::E);
     int id[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) id[r] = row0 + r < T_ ? ids[row0 + r] : -1;
-    float v[R][E];
+    Row<T, W> q[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        const bool there = id[r] >= 0 && id[r] < V;
-        if (id[r] >= V && lane == 0) atomicExch(&g_error_word, kErrInvalid);
-        load_row<T, E, WIDE>(table + (size_t)(there ? id[r] : 0) * d + col, lane, there ? d - col : 0,
-                             v[r]);
+        if (id[r] >= V) {
+            if (lane == 0) atomicExch(&g_error_word, kErrInvalid);
+            id[r] = -1;
+        }
+        q[r].load(table + (size_t)max(id[r], 0) * d + col, lane, d - col);
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         if (row0 + r >= T_) break;
+        float v[C::E];
+        q[r].get(v);
 #pragma unroll
-        for (int e = 0; e < E; ++e) v[r][e] *= scale;
-        store_row<T, E, WIDE>(x + (size_t)(row0 + r) * d + col, lane, d - col, v[r]);
+        for (int e = 0; e < C::E; ++e) v[e] = id[r] >= 0 ? v[e] * scale : 0.f;
+        store_row<C>(x + (size_t)(row0 + r) * d + col, lane, d - col, v);
     }
 }
 
@@ -210,7 +247,7 @@ __device__ __forceinline__ int block_prefix(int v, int* scratch, int* total) {
 // `warps` warps, this one being the w-th: start the zeros of the rows of [z0, z1) that are not named
 // (flags from symbol lo on).  Rows of whole 32-byte sectors by bulk copies, a row a lane; others by
 // plain stores, a row a warp (4099 tokens, 32003 x 777 fp32: 39 us, by bulk copies between 16-byte
-// boundaries 41).
+// boundaries 41, when the sums took 9 more than now).
 __device__ __forceinline__ void start_zeros(const SortArgs& a, int z0, int z1, int lo,
                                             const uint32_t* named, const uint4* source, int w, int warps) {
     const auto is_named = [&](int v) { return named[(v - lo) >> 5] >> ((v - lo) & 31) & 1; };
@@ -480,39 +517,33 @@ struct SumArgs {
 };
 
 // Writes a symbol's sum: scale sum, or that on top of what is there, rounded once.
-template <typename O, int E, bool WIDE>
+template <typename C, typename O>
 __device__ __forceinline__ void write_sum(const SumArgs& a, int symbol, int col, int lane,
-                                          const float (&s)[E]) {
+                                          const float (&s)[C::E]) {
     O* row = static_cast<O*>(a.dE) + (size_t)symbol * a.d + col;
     const int left = a.d - col;
-    float v[E];
+    float v[C::E];
     if (a.add) {
-        if constexpr (WIDE && sizeof(O) * E == 16) {
-            load_row<O, E, true>(row, lane, left, v);
-        } else if constexpr (WIDE) {   // the lane's E neighbours, not one vector
+        load_out<C>(row, lane, left, v);
 #pragma unroll
-            for (int e = 0; e < E; ++e) v[e] = lane * E < left ? to_f32(row[lane * E + e]) : 0.f;
-        } else {
-            load_row<O, E, false>(row, lane, left, v);
-        }
-#pragma unroll
-        for (int e = 0; e < E; ++e) v[e] = fmaf(a.scale, s[e], v[e]);
+        for (int e = 0; e < C::E; ++e) v[e] = fmaf(a.scale, s[e], v[e]);
     } else {
 #pragma unroll
-        for (int e = 0; e < E; ++e) v[e] = a.scale * s[e];
+        for (int e = 0; e < C::E; ++e) v[e] = a.scale * s[e];
     }
-    store_row<O, E, WIDE>(row, lane, left, v);
+    store_row<C>(row, lane, left, v);
 }
 
 // A CTA adds the rows of one chunk, 32 E columns of them, each warp an eighth: at most 32 rows, in an
-// order that the lanes hold, 8 of them on their way at once in registers (65536 x 1024 bf16: 48 us with
-// cold caches, 3.3 TB/s, 24 warps an SM; chunks of 64 tokens throughout take 87 us where these take
-// 80 for the whole gradient).
-template <typename T, typename O, int E, bool WIDE>
+// order that the lanes hold, 8 of them on their way at once in registers (65536 tokens, 32000 x 1024
+// bf16: 75 us for the whole gradient; with chunks of 64 tokens throughout 7 more).
+template <typename T, typename O, int W>
 __global__ void __launch_bounds__(32 * kSumWarps) embed_sum_kernel(const SumArgs a) {
+    using C = Cols<T, W>;
+    constexpr int E = C::E;
     __shared__ __align__(16) float head[kSumWarps][32 * E], tail[kSumWarps][32 * E];
     __shared__ int state[kSumWarps], head_symbol[kSumWarps];
-    constexpr int kRows = WIDE || E == 4 ? 8 : 4;   // on their way at once
+    constexpr int kRows = W == 2 ? 4 : 8;   // on their way at once
     // of a warp: has a run that came in from before it, which goes on behind it; another one that does
     constexpr int kFrom = 1, kThrough = 2, kOn = 4;
     pdl_wait();
@@ -547,16 +578,19 @@ __global__ void __launch_bounds__(32 * kSumWarps) embed_sum_kernel(const SumArgs
         if (lane + 1 >= n) next = after;
         const uint32_t last = __ballot_sync(0xffffffffu, lane < n && (next != key || lane + 1 == n));
         for (int r0 = 0; r0 < n; r0 += kRows) {
-            Row<T, E, WIDE> v[kRows];
+            Row<T, W> q[kRows];
 #pragma unroll
-            for (int r = 0; r < kRows; ++r) {
-                const int t = __shfl_sync(0xffffffffu, pos, (r0 + r) & 31);
-                v[r].load(dx + (size_t)(r0 + r < n ? t : 0) * a.d, lane, r0 + r < n ? left : 0);
+            for (int r = 0; r < kRows; ++r) {   // (past the chunk's last row that one again)
+                const int t = __shfl_sync(0xffffffffu, pos, min(r0 + r, n - 1));
+                q[r].load(dx + (size_t)t * a.d, lane, left);
             }
 #pragma unroll
             for (int r = 0; r < kRows; ++r) {
                 if (r0 + r >= n) break;
-                v[r].add_to(s);
+                float v[E];
+                q[r].get(v);
+#pragma unroll
+                for (int e = 0; e < E; ++e) s[e] += v[e];
                 if (!(last >> (r0 + r) & 1)) continue;
                 const int symbol = __shfl_sync(0xffffffffu, key, r0 + r);
                 const bool goes_on = r0 + r + 1 == n && after == symbol;
@@ -564,9 +598,9 @@ __global__ void __launch_bounds__(32 * kSumWarps) embed_sum_kernel(const SumArgs
                     float* const to = from_before ? head[warp] : tail[warp];
                     flags |= from_before ? (goes_on ? kFrom | kThrough : kFrom) : kOn;
 #pragma unroll
-                    for (int e = 0; e < E; ++e) to[WIDE ? lane * E + e : lane + 32 * e] = s[e];
+                    for (int e = 0; e < E; ++e) to[C::at(lane, e)] = s[e];
                 } else {
-                    write_sum<O, E, WIDE>(a, symbol, col, lane, s);
+                    write_sum<C, O>(a, symbol, col, lane, s);
                 }
                 from_before = false;
 #pragma unroll
@@ -612,8 +646,10 @@ __global__ void __launch_bounds__(32 * kSumWarps) embed_sum_kernel(const SumArgs
 // A run over several chunks: the warp of the chunk it starts in adds the parts, in order, eight of
 // them on their way at once (16384 tokens of 201 symbols: about 4 us, a launch and loads that wait for
 // one another; no chunk's CTA can do it, as none knows when the others are done).
-template <typename T, typename O, int E, bool WIDE>
+template <typename T, typename O, int W>
 __global__ void __launch_bounds__(32 * kSumWarps) embed_join_kernel(const SumArgs a) {
+    using C = Cols<T, W>;
+    constexpr int E = C::E;
     pdl_wait();
     pdl_trigger();
     const int lane = threadIdx.x & 31;
@@ -642,33 +678,12 @@ __global__ void __launch_bounds__(32 * kSumWarps) embed_join_kernel(const SumArg
     const int left = a.d - col;
     const float* part = a.part + ((size_t)chunk * 2 * a.d + col);
     float s[E];
-    const auto load = [&](const float* p, float (&v)[E]) {
-        if constexpr (WIDE) {
-#pragma unroll
-            for (int i = 0; i < E / 4; ++i) {
-                const float4 q = lane * E < left ? reinterpret_cast<const float4*>(p + lane * E)[i]
-                                                 : make_float4(0.f, 0.f, 0.f, 0.f);
-                v[4 * i] = q.x;
-                v[4 * i + 1] = q.y;
-                v[4 * i + 2] = q.z;
-                v[4 * i + 3] = q.w;
-            }
-        } else {
-            load_row<float, E, false>(p, lane, left, v);
-        }
-    };
-    load(part + a.d, s);
+    load_out<C>(part + a.d, lane, left, s);
     for (int j0 = 0; j0 < more; j0 += 8) {
         float v[8][E];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            if (j0 + j < more) {
-                load(part + (size_t)(j0 + j + 1) * 2 * a.d, v[j]);
-            } else {
-#pragma unroll
-                for (int e = 0; e < E; ++e) v[j][e] = 0.f;
-            }
-        }
+        for (int j = 0; j < 8; ++j)
+            load_out<C>(part + (size_t)(min(j0 + j, more - 1) + 1) * 2 * a.d, lane, left, v[j]);
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             if (j0 + j < more) {
@@ -676,7 +691,7 @@ __global__ void __launch_bounds__(32 * kSumWarps) embed_join_kernel(const SumArg
                 for (int e = 0; e < E; ++e) s[e] += v[j][e];
             }
     }
-    write_sum<O, E, WIDE>(a, symbol, col, lane, s);
+    write_sum<C, O>(a, symbol, col, lane, s);
 }
 
 // ------------------------------------------------------------------ host
@@ -747,19 +762,20 @@ size_t bwd_ws_bytes(int T, int d) {
     return 6 * up((size_t)T * 4) + 256 + most;
 }
 
-template <typename T, int E, bool WIDE>
+template <typename T, int W>
 cudaError_t fwd(const int* ids, const void* table, int tokens, int V, int d, float scale, void* x,
                 cudaStream_t st) {
-    const int tiles = (d + 32 * E - 1) / (32 * E);
+    constexpr int kCols = 32 * Cols<T, W>::E;
+    const int tiles = (d + kCols - 1) / kCols;
     const T* t = static_cast<const T*>(table);
     // four rows a warp once that leaves 16 warps an SM
     if ((long long)tokens * tiles >= 64ll * device_sms()) {
         const dim3 grid((unsigned)(((long long)tokens + 31) / 32), tiles);
-        return launch_pdl(embed_fwd_kernel<T, E, WIDE, 4>, grid, dim3(256), 0, st, ids, t,
+        return launch_pdl(embed_fwd_kernel<T, W, 4>, grid, dim3(256), 0, st, ids, t,
                           (long long)tokens, V, d, scale, static_cast<T*>(x));
     }
     const dim3 grid((unsigned)(((long long)tokens + 7) / 8), tiles);
-    return launch_pdl(embed_fwd_kernel<T, E, WIDE, 1>, grid, dim3(256), 0, st, ids, t,
+    return launch_pdl(embed_fwd_kernel<T, W, 1>, grid, dim3(256), 0, st, ids, t,
                       (long long)tokens, V, d, scale, static_cast<T*>(x));
 }
 
@@ -781,9 +797,9 @@ cudaError_t launch_sort(const SortArgs& a, bool counted, cudaStream_t st) {
                       place_bytes(a.range), st, a);
 }
 
-template <typename T, typename O, int E, bool WIDE>
+template <typename T, typename O, int W>
 cudaError_t bwd(SortArgs& so, SumArgs& su, int tokens, char* ws, cudaStream_t st, int* launches) {
-    const BwdPlan p = bwd_plan(tokens, su.d, E);
+    const BwdPlan p = bwd_plan(tokens, su.d, Cols<T, W>::E);
     for (int i = 0; i < 3; ++i) {
         so.key[i] = reinterpret_cast<int*>(ws + p.key[i]);
         so.pos[i] = reinterpret_cast<int*>(ws + p.pos[i]);
@@ -802,15 +818,24 @@ cudaError_t bwd(SortArgs& so, SumArgs& su, int tokens, char* ws, cudaStream_t st
     if (e != cudaSuccess) return e;
     ++*launches;
     const long long items = (long long)p.chunks * p.tiles;
-    e = launch_pdl(embed_sum_kernel<T, O, E, WIDE>, dim3((unsigned)items), dim3(32 * kSumWarps), 0, st, su);
+    e = launch_pdl(embed_sum_kernel<T, O, W>, dim3((unsigned)items), dim3(32 * kSumWarps), 0, st, su);
     if (e != cudaSuccess) return e;
     ++*launches;
     if (p.chunks == 1) return cudaSuccess;   // no run over a chunk's end
-    e = launch_pdl(embed_join_kernel<T, O, E, WIDE>, dim3((unsigned)((items + kSumWarps - 1) / kSumWarps)),
+    e = launch_pdl(embed_join_kernel<T, O, W>, dim3((unsigned)((items + kSumWarps - 1) / kSumWarps)),
                    dim3(32 * kSumWarps), 0, st, su);
     if (e != cudaSuccess) return e;
     ++*launches;
     return cudaSuccess;
+}
+
+template <typename T, typename O>
+cudaError_t bwd_by_width(SortArgs& so, SumArgs& su, int tokens, char* ws, cudaStream_t st, int* launches) {
+    const size_t row = (size_t)su.d * sizeof(T);
+    if (row % 16 == 0) return bwd<T, O, 16>(so, su, tokens, ws, st, launches);
+    if constexpr (sizeof(T) == 2)
+        if (row % 4) return bwd<T, O, 2>(so, su, tokens, ws, st, launches);
+    return bwd<T, O, 4>(so, su, tokens, ws, st, launches);
 }
 
 int check_sizes(int T, int V, int d, int dtype) {
@@ -844,14 +869,15 @@ extern "C" int hcw_embed_fwd(const int* ids, const void* E, int T, int V, int d,
     if (T == 0) return HCW_OK;
     if (!ids || !E || !x) return HCW_ERR_INVALID_ARG;
     const cudaStream_t st = (cudaStream_t)stream;
-    const bool wide = d * es % 16 == 0;
+    const int bytes = (int)(d * es % 16 == 0 ? 16 : d * es % 4 == 0 ? 4 : 2);
     cudaError_t e;
     if (dtype == HCW_BF16)
-        e = wide ? fwd<__nv_bfloat16, 8, true>(ids, E, T, V, d, scale, x, st)
-                 : fwd<__nv_bfloat16, 8, false>(ids, E, T, V, d, scale, x, st);
+        e = bytes == 16  ? fwd<__nv_bfloat16, 16>(ids, E, T, V, d, scale, x, st)
+            : bytes == 4 ? fwd<__nv_bfloat16, 4>(ids, E, T, V, d, scale, x, st)
+                         : fwd<__nv_bfloat16, 2>(ids, E, T, V, d, scale, x, st);
     else
-        e = wide ? fwd<float, 4, true>(ids, E, T, V, d, scale, x, st)
-                 : fwd<float, 4, false>(ids, E, T, V, d, scale, x, st);
+        e = bytes == 16 ? fwd<float, 16>(ids, E, T, V, d, scale, x, st)
+                        : fwd<float, 4>(ids, E, T, V, d, scale, x, st);
     return count_launch(e, 1);
 }
 
@@ -906,19 +932,11 @@ extern "C" int hcw_embed_bwd(const int* ids, const void* dx, int T, int V, int d
     int launches = 0;
     cudaError_t e;
     char* ws = static_cast<char*>(workspace);
-    const bool wide = d * es % 16 == 0;
-    using B = __nv_bfloat16;
-    if (dtype == HCW_BF16 && de_dtype == HCW_BF16)
-        e = wide ? bwd<B, B, 8, true>(so, su, T, ws, st, &launches)
-                 : bwd<B, B, 8, false>(so, su, T, ws, st, &launches);
-    else if (dtype == HCW_BF16)
-        e = wide ? bwd<B, float, 8, true>(so, su, T, ws, st, &launches)
-                 : bwd<B, float, 8, false>(so, su, T, ws, st, &launches);
-    else if (de_dtype == HCW_BF16)
-        e = wide ? bwd<float, B, 4, true>(so, su, T, ws, st, &launches)
-                 : bwd<float, B, 4, false>(so, su, T, ws, st, &launches);
+    if (dtype == HCW_BF16)
+        e = de_dtype == HCW_BF16 ? bwd_by_width<__nv_bfloat16, __nv_bfloat16>(so, su, T, ws, st, &launches)
+                                 : bwd_by_width<__nv_bfloat16, float>(so, su, T, ws, st, &launches);
     else
-        e = wide ? bwd<float, float, 4, true>(so, su, T, ws, st, &launches)
-                 : bwd<float, float, 4, false>(so, su, T, ws, st, &launches);
+        e = de_dtype == HCW_BF16 ? bwd_by_width<float, __nv_bfloat16>(so, su, T, ws, st, &launches)
+                                 : bwd_by_width<float, float>(so, su, T, ws, st, &launches);
     return count_launch(e, launches);
 }

@@ -125,9 +125,10 @@ __global__ void __launch_bounds__(256) logits_edit_kernel(const LogitsArgs a) {
     const int lo = max(j0, 0), hi = (int)min((long long)a.V, (long long)j0 + S);
     const int* h = a.history ? a.history + (size_t)row * a.H : nullptr;
     int past[NH];
+    if (h) {   // (no condition at a load: those wait one for another; entries past n are not looked at)
 #pragma unroll
-    for (int i = 0; i < NH; ++i)
-        past[i] = h && (int)threadIdx.x + i * NT < a.H ? h[threadIdx.x + i * NT] : -1;
+        for (int i = 0; i < NH; ++i) past[i] = h[min((int)threadIdx.x + i * NT, a.H - 1)];
+    }
     const int n = !h ? 0 : a.lengths ? min(max(a.lengths[row], 0), a.H) : a.H;
     const int own = a.prompt ? a.prompt[row] : 0;
     int id = -1;
@@ -360,16 +361,15 @@ __global__ void __launch_bounds__(NT) logits_named_kernel(const LogitsArgs a, in
     const float* bias = a.bias + (size_t)row * a.M;
     const uint32_t* mask = a.mask ? a.mask + (size_t)row * ((a.V + 31) / 32) : nullptr;
     // everything asked for at once
+    // (no condition at a load: those wait one for another)
     int past[NH], slot[NS];
 #pragma unroll
-    for (int i = 0; i < NH; ++i) {
-        const int t = threadIdx.x + i * NT;
-        past[i] = h && t < a.H ? h[t] : -1;
-    }
+    for (int i = 0; i < NH; ++i) past[i] = h ? h[min((int)threadIdx.x + i * NT, a.H - 1)] : -1;
 #pragma unroll
     for (int i = 0; i < NS; ++i) {
         const int k = threadIdx.x + i * NT;
-        slot[i] = k < a.M ? bias_idx[k] : -1;
+        slot[i] = a.M ? bias_idx[min(k, a.M - 1)] : -1;
+        if (k >= a.M) slot[i] = -1;
     }
     const int n = !h ? 0 : a.lengths ? min(max(a.lengths[row], 0), a.H) : a.H;
     const int own = a.prompt ? a.prompt[row] : 0;
@@ -448,18 +448,27 @@ __global__ void __launch_bounds__(NT) logits_named_kernel(const LogitsArgs a, in
         sc[i] = count[p];
     }
 #pragma unroll
-    for (int i = 0; i < NH; ++i) v[i] = past[i] >= 0 ? value(z + past[i]) : 0.f;
+    for (int i = 0; i < NH; ++i) v[i] = value(z + max(past[i], 0));
 #pragma unroll
     for (int i = 0; i < NS; ++i) {
-        sum[i] = at[i] >= 0 ? bias[threadIdx.x + i * NT] : 0.f;
-        sv[i] = at[i] >= 0 ? value(z + at[i]) : 0.f;
+        sum[i] = a.M ? bias[min((int)threadIdx.x + i * NT, a.M - 1)] : 0.f;
+        sv[i] = value(z + max(at[i], 0));
+    }
+    if (mask) {
+        uint32_t w[NH], sw[NS];
+#pragma unroll
+        for (int i = 0; i < NH; ++i) w[i] = mask[max(past[i], 0) >> 5];
+#pragma unroll
+        for (int i = 0; i < NS; ++i) sw[i] = mask[max(at[i], 0) >> 5];
+#pragma unroll
+        for (int i = 0; i < NH; ++i)
+            if (!(w[i] >> (past[i] & 31) & 1)) past[i] = -1;
+#pragma unroll
+        for (int i = 0; i < NS; ++i)
+            if (!(sw[i] >> (at[i] & 31) & 1)) at[i] = -1;
     }
 #pragma unroll
-    for (int i = 0; i < NH; ++i)
-        if (past[i] >= 0 && !passes(past[i])) past[i] = -1;
-#pragma unroll
     for (int i = 0; i < NS; ++i) {
-        if (at[i] >= 0 && !passes(at[i])) at[i] = -1;
         if (at[i] < 0 || !(sc[i] & kMore)) continue;
         for (int m = threadIdx.x + i * NT + 1; m < a.M; ++m)
             if (bias_idx[m] == at[i]) sum[i] += bias[m];
