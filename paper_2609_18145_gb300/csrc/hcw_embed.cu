@@ -37,6 +37,7 @@ constexpr int kMaxV = 1 << 23;
 constexpr int kMaxD = 1 << 20;
 constexpr int kSumWarps = 8;
 constexpr int kZeroBytes = 4096;          // of a bulk copy of zeros at most
+constexpr int kLongRow = 512;             // bytes of a row that a warp zeroes on its own
 
 __device__ __forceinline__ float to_f32(float v) { return v; }
 __device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
@@ -244,35 +245,55 @@ __device__ __forceinline__ int block_prefix(int v, int* scratch, int* total) {
     return (warp ? before : 0) + s - v;
 }
 
+// Starts bytes of zeros at p, on 16-byte boundaries both.
+__device__ __forceinline__ void bulk_zeros(char* p, size_t bytes, const uint4* source) {
+    for (size_t at = 0; at < bytes; at += kZeroBytes)
+        asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(p + at),
+                     "r"(smem_u32(source)),
+                     "r"((uint32_t)(bytes - at < kZeroBytes ? bytes - at : kZeroBytes))
+                     : "memory");
+}
+
 // `warps` warps, this one being the w-th: start the zeros of the rows of [z0, z1) that are not named
-// (flags from symbol lo on).  Rows of whole 32-byte sectors by bulk copies, a row a lane; others by
-// plain stores, a row a warp (4099 tokens, 32003 x 777 fp32: 39 us, by bulk copies between 16-byte
-// boundaries 41, when the sums took 9 more than now).
+// (flags from symbol lo on).  Rows of whole 32-byte sectors by bulk copies, a row a lane
+// (1000 tokens, 131072 x 16 fp32: 14 us, by plain stores 27; 2^20 x 16: 25 against 130).  Others of
+// kLongRow bytes or more by plain stores, a row a warp (4099 tokens, 32003 x 777 fp32: 39 us, by bulk
+// copies between 16-byte boundaries 41, when the sums took 9 more than now); shorter ones by bulk copies
+// again, 8 rows a lane with those next to one another as one piece (1000 tokens, 131072 x 9 fp32: 19 us,
+// by plain stores 27; 2^20 x 9: 27 against 125; from 131072 x 201 on plain stores win, 30 against 34).
 __device__ __forceinline__ void start_zeros(const SortArgs& a, int z0, int z1, int lo,
                                             const uint32_t* named, const uint4* source, int w, int warps) {
     const auto is_named = [&](int v) { return named[(v - lo) >> 5] >> ((v - lo) & 31) & 1; };
     const int lane = threadIdx.x & 31;
-    if (a.row_bytes % 32) {
+    char* const rows = static_cast<char*>(a.dE);
+    if (a.row_bytes % 32 == 0) {
+        for (int v = z0 + 32 * w + lane; v < z1; v += 32 * warps)
+            if (!is_named(v)) bulk_zeros(rows + (size_t)v * a.row_bytes, a.row_bytes, source);
+    } else if (a.row_bytes >= kLongRow) {
         for (int v = z0 + w; v < z1; v += warps) {
             if (is_named(v)) continue;
-            char* const p = static_cast<char*>(a.dE) + (size_t)v * a.row_bytes;
+            char* const p = rows + (size_t)v * a.row_bytes;
             char* const end = p + a.row_bytes;
             char* const in = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(p) + 15) & ~(uintptr_t)15);
             char* const out = reinterpret_cast<char*>(reinterpret_cast<uintptr_t>(end) & ~(uintptr_t)15);
-            if (p + 2 * lane < (in < end ? in : end)) *reinterpret_cast<short*>(p + 2 * lane) = 0;
+            if (p + 2 * lane < in) *reinterpret_cast<short*>(p + 2 * lane) = 0;
             for (char* q = in + 16 * lane; q < out; q += 512) *reinterpret_cast<uint4*>(q) = make_uint4(0, 0, 0, 0);
-            if (out >= in && out + 2 * lane < end) *reinterpret_cast<short*>(out + 2 * lane) = 0;
+            if (out + 2 * lane < end) *reinterpret_cast<short*>(out + 2 * lane) = 0;
         }
-        return;
-    }
-    for (int v = z0 + 32 * w + lane; v < z1; v += 32 * warps) {
-        if (is_named(v)) continue;
-        char* const p = static_cast<char*>(a.dE) + (size_t)v * a.row_bytes;
-        for (size_t at = 0; at < a.row_bytes; at += kZeroBytes)
-            asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(p + at),
-                         "r"(smem_u32(source)),
-                         "r"((uint32_t)(a.row_bytes - at < kZeroBytes ? a.row_bytes - at : kZeroBytes))
-                         : "memory");
+    } else {
+        for (int v0 = z0 + 8 * (32 * w + lane); v0 < z1; v0 += 8 * 32 * warps) {
+            const int v1 = min(v0 + 8, z1);
+            for (int v = v0; v < v1; ++v) {
+                if (is_named(v)) continue;
+                char* p = rows + (size_t)v * a.row_bytes;
+                while (v + 1 < v1 && !is_named(v + 1)) ++v;
+                char* const end = rows + (size_t)(v + 1) * a.row_bytes;
+                for (; p < end && (reinterpret_cast<uintptr_t>(p) & 15); p += 2) *reinterpret_cast<short*>(p) = 0;
+                const size_t whole = (size_t)(end - p) & ~(size_t)15;
+                bulk_zeros(p, whole, source);
+                for (p += whole; p < end; p += 2) *reinterpret_cast<short*>(p) = 0;
+            }
+        }
     }
     bulk_commit();
 }
