@@ -233,7 +233,9 @@ __global__ void __launch_bounds__(32 * kQWarps, 1) q4_kernel(const Q4Args a) {
     };
     activations(0);
     // the next copy: a piece of a set, and the lane's first 16 bytes of it in each of the set's tiles
-    int next_set = set0, next_piece = part;
+    // (a team, of which there is none where RT is 2, may have more warps than a tile has pieces: the others
+    // copy nothing)
+    int next_set = RT > 1 || part < a.pieces ? set0 : sets, next_piece = part;
     const char* from[RT];
     const auto aim = [&]() {
 #pragma unroll

@@ -158,3 +158,17 @@ def test_shapes_are_checked(H):
                 lambda: H.hcw_q4_pack(codes.cuda().float(), scales.cuda(), 64)):
         with pytest.raises(TypeError):
             bad()
+
+
+@pytest.mark.parametrize("T", [1, 9])
+@pytest.mark.parametrize("N,K", [(16, 264), (40, 520), (24, 1096), (3, 1920)])
+def test_fewer_pieces_than_warps_at_the_end_of_an_allocation(H, N, K, T):
+    """Rows of 3 to 15 pieces, which fewer warps take than share them: what is read ends with the weights."""
+    group = 64
+    codes, scales, x, bias = make(T, N, K, group, seed=5)
+    need = H.hcw_q4_bytes(N, K, group)
+    room = torch.empty(32 << 20, dtype=torch.uint8, device="cuda")
+    packed = H.hcw_q4_pack(codes.cuda(), scales.cuda(), group, packed=room[-need:])
+    y = H.hcw_q4_matmul(x.cuda(), packed, N, group, bias=bias.cuda(), y_dtype=F32)
+    want = check(H, codes, scales, x, bias, group, F32)
+    assert torch.equal(y, want)
