@@ -776,9 +776,9 @@ int hcw_q4_matmul(const void* x, const void* packed, const float* bias, int T, i
  *   mask     [B][ceil(V / 32)] words or NULL: bit j % 32 of word j / 32 lets symbol j through.  A
  *            row that lets nothing through is -inf throughout.
  * Products and sums are fp32 (past its largest number: infinite), each output is rounded once; a
- * symbol without edits keeps its bits;
- * what the mask takes out is -inf whatever it was, NaN included.  A symbol >= V in the history or a
- * slot counts as empty and is reported by hcw_sync_status as HCW_ERR_INVALID_ARG.  The same inputs
+ * symbol without edits keeps its value (a NaN stays one); what the mask takes out is -inf whatever it
+ * was, NaN included.  A symbol >= V in the history (which is read where a penalty is given) or a slot
+ * counts as empty and is reported by hcw_sync_status as HCW_ERR_INVALID_ARG.  The same inputs
  * give the same bits.  B >= 0 up to 2^20 (0 does nothing), V up to 2^24, H up to 2^28, M up to
  * 1024, B V up to 2^40 (HCW_ERR_UNSUPPORTED above); z and out are 16-byte, the rest 4-byte aligned;
  * out over an input, or over z other than in place, is HCW_ERR_ALIASING.  One or two launches, no
