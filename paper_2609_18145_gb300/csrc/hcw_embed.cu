@@ -664,55 +664,83 @@ __global__ void __launch_bounds__(32 * kSumWarps) embed_sum_kernel(const SumArgs
     if (open) part[came ? 0 : a.d] = s;
 }
 
-// A run over several chunks: the warp of the chunk it starts in adds the parts, in order, eight of
-// them on their way at once (16384 tokens of 201 symbols: about 4 us, a launch and loads that wait for
-// one another; no chunk's CTA can do it, as none knows when the others are done).
-template <typename T, typename O, int W>
+// A run over several chunks: TEAM warps of the chunk it starts in add the parts, in order, each warp eight
+// or its share of them, eight on their way at once (no chunk's CTA can do it, as none knows when the
+// others are done).  Eight warps where the symbols' runs fill a chunk on average (the gradient of 16384
+// tokens, 201 x 512 bf16: 16.9 us, with one warp 18.1; 262144 tokens 133, with one 148); one where most chunks
+// have none to join (65536 tokens, 131072 x 2048: 243, with eight 248).
+template <typename T, typename O, int W, int TEAM>
 __global__ void __launch_bounds__(32 * kSumWarps) embed_join_kernel(const SumArgs a) {
+    static_assert(TEAM == 1 || TEAM == kSumWarps, "a warp or a CTA for a run");
     using C = Cols<T, W>;
     constexpr int E = C::E;
+    __shared__ float sums[TEAM][32 * E];
     pdl_wait();
     pdl_trigger();
-    const int lane = threadIdx.x & 31;
-    const long long item = (long long)blockIdx.x * kSumWarps + (threadIdx.x >> 5);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part_of = TEAM > 1 ? warp : 0;
+    const long long item = TEAM > 1 ? (long long)blockIdx.x : (long long)blockIdx.x * kSumWarps + warp;
     const int chunk = (int)(item / a.tiles), col = (int)(item % a.tiles) * (32 * E);
     const int count = *a.count;
     const int size = 1 << a.chunk_log2;
     const long long first = (long long)chunk << a.chunk_log2;
-    if (chunk >= a.chunks || first + size >= a.T) return;   // no chunk behind it
+    if (first + size >= a.T) return;   // no chunk behind it
     const int symbol = a.key[first + size - 1], behind = a.key[first + size], start = a.key[first],
               before = first > 0 ? a.key[first - 1] : -1;
+    // the symbols around the ends of the 32 chunks from the from-th behind it on (behind the count the list
+    // holds nothing of use); the first ones at once with those above, where they are needed as a rule
+    int k[2];
+    const auto ends = [&](int from) {
+        const long long end = min(first + (long long)size * (from + lane + 2), (long long)a.T - 1);
+        k[0] = a.key[end - 1];
+        k[1] = a.key[end];
+    };
+    if (TEAM > 1) ends(0);
     if (first + size >= count || behind != symbol) return;
     if (first > 0 && start == symbol && before == symbol) return;   // started before
+    if (TEAM == 1) ends(0);
     // the chunks behind it that the run reaches into
     int more = 0;
     for (;;) {
-        const long long end = first + (long long)size * (more + lane + 2);   // the end of one of them
-        const bool on = end < count && a.key[end] == symbol && a.key[end - 1] == symbol;
+        const bool on = first + (long long)size * (more + lane + 2) < count && k[0] == symbol && k[1] == symbol;
         const uint32_t stop = __ballot_sync(0xffffffffu, !on);
         if (stop) {
             more += __ffs(stop);
             break;
         }
         more += 32;
+        ends(more);
     }
     const int left = a.d - col;
     const float* part = a.part + ((size_t)chunk * 2 * a.d + col);
     float s[E];
-    load_out<C>(part + a.d, lane, left, s);
-    for (int j0 = 0; j0 < more; j0 += 8) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) s[e] = 0.f;
+    if (part_of == 0) load_out<C>(part + a.d, lane, left, s);
+    const int share = TEAM > 1 ? max(8, (more + TEAM - 1) / TEAM) : more;
+    const int j1 = min(more, (part_of + 1) * share);
+    for (int j0 = part_of * share; j0 < j1; j0 += 8) {
         float v[8][E];
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-            load_out<C>(part + (size_t)(min(j0 + j, more - 1) + 1) * 2 * a.d, lane, left, v[j]);
+            load_out<C>(part + (size_t)(min(j0 + j, j1 - 1) + 1) * 2 * a.d, lane, left, v[j]);
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-            if (j0 + j < more) {
+            if (j0 + j < j1) {
 #pragma unroll
                 for (int e = 0; e < E; ++e) s[e] += v[j][e];
             }
     }
-    write_sum<C, O>(a, symbol, col, lane, s);
+    if (TEAM > 1 && more > 8) {   // (the same for the whole CTA)
+#pragma unroll
+        for (int e = 0; e < E; ++e) sums[part_of][lane + 32 * e] = s[e];
+        __syncthreads();
+        if (part_of == 0) {
+            for (int w = 1; w < TEAM; ++w)
+#pragma unroll
+                for (int e = 0; e < E; ++e) s[e] += sums[w][lane + 32 * e];
+        }
+    }
+    if (part_of == 0) write_sum<C, O>(a, symbol, col, lane, s);
 }
 
 // ------------------------------------------------------------------ host
@@ -843,8 +871,12 @@ cudaError_t bwd(SortArgs& so, SumArgs& su, int tokens, char* ws, cudaStream_t st
     if (e != cudaSuccess) return e;
     ++*launches;
     if (p.chunks == 1) return cudaSuccess;   // no run over a chunk's end
-    e = launch_pdl(embed_join_kernel<T, O, W>, dim3((unsigned)((items + kSumWarps - 1) / kSumWarps)),
-                   dim3(32 * kSumWarps), 0, st, su);
+    if ((long long)so.V << p.chunk_log2 <= tokens)
+        e = launch_pdl(embed_join_kernel<T, O, W, kSumWarps>, dim3((unsigned)items), dim3(32 * kSumWarps), 0,
+                       st, su);
+    else
+        e = launch_pdl(embed_join_kernel<T, O, W, 1>, dim3((unsigned)((items + kSumWarps - 1) / kSumWarps)),
+                       dim3(32 * kSumWarps), 0, st, su);
     if (e != cudaSuccess) return e;
     ++*launches;
     return cudaSuccess;

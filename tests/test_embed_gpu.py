@@ -77,7 +77,7 @@ def check_bwd(H, ids, dx, V, scale, out=F32, base=None, stream=None, poison=0.0)
 
 SIZES = [(1, 1, 1), (1, 5, 8), (3, 2, 7), (33, 300, 64), (64, 31, 513), (257, 1000, 24), (100, 151, 2048),
          (1000, 152, 40), (1000, 153, 256), (2049, 40000, 33), (4099, 3203, 777), (5000, 17, 96),
-         (700, 9001, 9), (90, 5003, 1), (1500, 4001, 63), (300, 2503, 130)]
+         (700, 9001, 9), (90, 5003, 1), (1500, 4001, 63), (300, 2503, 130), (400, 200003, 7)]
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
