@@ -14,9 +14,9 @@
 // workspace at each, and a last launch adds these in the order of the chunks.  No atomics on
 // numbers: the order of every sum depends on the ids and the sizes alone.
 //
-// The sort is one launch without any exchange between its CTAs.  Each owns a range of symbols and goes
-// through all ids: it counts those of smaller symbols, where its own begin in the sorted order, and
-// its own by symbol.  The rows of symbols that do not occur are zeroed on the way, by bulk copies.
+// The sort is one launch.  Each CTA, or some CTAs together, own a range of symbols and go through all
+// ids: they count those of smaller symbols, where their own begin in the sorted order, and their own
+// by symbol.  The rows of symbols that do not occur are zeroed on the way, by bulk copies.
 #include "hcw.h"
 #include "hcw_internal.h"
 #include "hcw_ptx.cuh"
@@ -200,7 +200,7 @@ __global__ void __launch_bounds__(256) embed_fwd_kernel(const int* ids, const T*
 // ------------------------------------------------------------------ the sorted tokens
 struct SortArgs {
     const int* ids;
-    int T, V, range;          // symbols of a CTA
+    int T, V, range;          // symbols of a CTA, or of several that share them
     int* key[3];              // [T] symbols and [T] positions: two for the passes, and the sorted ones
     int* pos[3];
     int* count;               // tokens that name a symbol
@@ -298,6 +298,55 @@ __device__ __forceinline__ void start_zeros(const SortArgs& a, int z0, int z1, i
     bulk_commit();
 }
 
+// A warp goes through the tokens [w0, w1), four a lane at a time: counts those of the range's symbols.
+// Returns how many of the lane's have a smaller symbol.
+__device__ __forceinline__ int count_tokens(const SortArgs& a, long long w0, long long w1, int lo, int hi,
+                                            int* tally) {
+    const int lane = threadIdx.x & 31;
+    int below = 0;
+    for (long long i0 = w0; i0 < w1; i0 += 512) {
+        int id[4][4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) ids_at(a.ids, i0 + 128 * q + 4 * lane, w1, id[q]);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int v = id[q][e];
+                below += v >= 0 && v < lo;
+                if (v >= lo && v < hi) atomicAdd(&tally[v - lo], 1);
+                if (v >= a.V) atomicExch(&g_error_word, kErrInvalid);
+            }
+    }
+    return below;
+}
+
+// A warp goes through them again, 32 at a time, and puts each where the range's tallies say.
+__device__ __forceinline__ void place_tokens(const SortArgs& a, long long w0, long long w1, int lo, int hi,
+                                             int* tally) {
+    const int lane = threadIdx.x & 31;
+    for (long long i0 = w0; i0 < w1; i0 += 512) {
+        int id[16];
+#pragma unroll
+        for (int q = 0; q < 16; ++q) id[q] = i0 + 32 * q + lane < w1 ? a.ids[i0 + 32 * q + lane] : -1;
+#pragma unroll
+        for (int q = 0; q < 16; ++q) {
+            const bool in = id[q] >= lo && id[q] < hi;
+            if (!__any_sync(0xffffffffu, in)) continue;
+            const uint32_t same = __match_any_sync(0xffffffffu, in ? id[q] : -1);
+            const int rank = __popc(same & ((1u << lane) - 1));
+            const int to = in ? tally[id[q] - lo] + rank : 0;
+            __syncwarp();
+            if (in && rank == 0) tally[id[q] - lo] += __popc(same);
+            __syncwarp();
+            if (in) {
+                a.key[2][to] = id[q];
+                a.pos[2][to] = (int)(i0 + 32 * q + lane);
+            }
+        }
+    }
+}
+
 // Where a range's counts fit into shared memory.  A range has kSplit CTAs, each with the runs of
 // kOwn warps (a frequent symbol's tokens would keep one CTA busy long after the others).  Each counts, for
 // every symbol of the range, the tokens before its runs, in each of them and after them: so it knows
@@ -324,21 +373,7 @@ __global__ void __launch_bounds__(kSortThreads) embed_place_kernel(const SortArg
     // each warp goes through a run of ids, four a lane at a time
     const int run = ((a.T + kSortThreads - 1) / kSortThreads * 32 + 127) / 128 * 128;   // of a warp
     const long long w0 = (long long)warp * run, w1 = min((long long)a.T, w0 + run);
-    int below = 0;
-    for (long long i0 = w0; i0 < w1; i0 += 512) {
-        int id[4][4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) ids_at(a.ids, i0 + 128 * q + 4 * lane, w1, id[q]);
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int v = id[q][e];
-                below += v >= 0 && v < lo;
-                if (v >= lo && v < hi) atomicAdd(&tally[v - lo], 1);
-                if (v >= a.V) atomicExch(&g_error_word, kErrInvalid);
-            }
-    }
+    const int below = count_tokens(a, w0, w1, lo, hi, tally);
     int base, all;
     (void)block_prefix(below, scratch, &base);   // (and the counts are complete)
     const int per = (range + kSortThreads - 1) / kSortThreads;
@@ -366,26 +401,7 @@ __global__ void __launch_bounds__(kSortThreads) embed_place_kernel(const SortArg
     if (threadIdx.x == 0 && hi == a.V && part == 0) *a.count = base + all;
     __syncthreads();
     if (own >= 0 && own < kOwn) {
-        for (long long i0 = w0; i0 < w1; i0 += 512) {
-            int id[16];
-#pragma unroll
-            for (int q = 0; q < 16; ++q) id[q] = i0 + 32 * q + lane < w1 ? a.ids[i0 + 32 * q + lane] : -1;
-#pragma unroll
-            for (int q = 0; q < 16; ++q) {
-                const bool in = id[q] >= lo && id[q] < hi;
-                if (!__any_sync(0xffffffffu, in)) continue;
-                const uint32_t same = __match_any_sync(0xffffffffu, in ? id[q] : -1);
-                const int rank = __popc(same & ((1u << lane) - 1));
-                const int to = in ? tally[id[q] - lo] + rank : 0;
-                __syncwarp();
-                if (in && rank == 0) tally[id[q] - lo] += __popc(same);
-                __syncwarp();
-                if (in) {
-                    a.key[2][to] = id[q];
-                    a.pos[2][to] = (int)(i0 + 32 * q + lane);
-                }
-            }
-        }
+        place_tokens(a, w0, w1, lo, hi, tally);
     } else if (a.dE) {
         // the other warps: zeros; the CTAs of a range share its rows
         const int share = (range + kSplit - 1) / kSplit;
@@ -393,6 +409,107 @@ __global__ void __launch_bounds__(kSortThreads) embed_place_kernel(const SortArg
         start_zeros(a, z0, z1, lo, named, source, own < 0 ? warp : warp - kOwn, kSortWarps - kOwn);
         bulk_wait<0>();
     }
+}
+
+// The same for many tokens, where what takes the time is that each of 152 CTAs goes through all of them
+// (65536: 22 us, 262144: 68).  A cluster of kCluster CTAs has a range, each of its CTAs a part of the
+// tokens; they count those of kRuns runs of neighbours each and read each other's sums.  The gradient of
+// 65536 tokens, 32000 x 1024 bf16: 71 us, without clusters 75; 500 x 128: 27 and 36; 262144 tokens, 201 x
+// 512: 97 and 133.  Few tokens wait longer for the cluster than for the counts (4096 tokens, 201 x 512: 13.2
+// and 12.4; 16384 the same).  Of 8 CTAs fewer clusters run at once, which the zeros feel (16384
+// tokens, 32000 x 512: 34, of 4 29).
+constexpr int kCluster = 4, kRuns = 16;
+
+__device__ __forceinline__ int from_cta(const int* p, int rank) {
+    int v;
+    asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(mapa_shared(p, rank)) : "memory");
+    return v;
+}
+
+__global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kSortThreads)
+    embed_place_cluster_kernel(const SortArgs a) {
+    extern __shared__ int counts[];                 // [kRuns][range], then the sums, [range] each:
+    __shared__ int scratch[kSortWarps];
+    __shared__ int below_here;
+    __shared__ __align__(16) uint4 source[kZeroBytes / 16];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, range = a.range;
+    int* const here = counts + kRuns * range;       // of this CTA's tokens
+    int* const all = here + range;                  // of all tokens
+    int* const before = all + range;                // of those of the CTAs before this one
+    uint32_t* const named = reinterpret_cast<uint32_t*>(before + range);
+    if (threadIdx.x < kZeroBytes / 16) source[threadIdx.x] = make_uint4(0, 0, 0, 0);
+    fence_proxy_async_smem();   // before the barriers that come first, for the bulk copies that read them
+    for (int i = threadIdx.x; i < kRuns * range; i += kSortThreads) counts[i] = 0;
+    pdl_wait();
+    pdl_trigger();
+    const int part = (int)cluster_ctarank();
+    const int lo = blockIdx.x / kCluster * range, hi = min(a.V, lo + range);
+    __syncthreads();
+    // a warp's share of the tokens (a multiple of four), of which a run has several
+    const long long share = ((a.T + kCluster * kSortWarps - 1) / (kCluster * kSortWarps) + 3) & ~3;
+    constexpr int kShares = kSortWarps / kRuns;
+    const long long first = part * kSortWarps * share;
+    const int below = count_tokens(a, first + warp * share, min((long long)a.T, first + (warp + 1) * share), lo,
+                                   hi, counts + warp / kShares * range);
+    int base, sum;
+    (void)block_prefix(below, scratch, &base);   // (and the counts are complete)
+    if (threadIdx.x == 0) below_here = base;
+    for (int v = threadIdx.x; v < range; v += kSortThreads) {
+        int n = 0;
+#pragma unroll
+        for (int k = 0; k < kRuns; ++k) n += counts[k * range + v];
+        here[v] = n;
+    }
+    cluster_sync_all();
+    base = lane < kCluster ? from_cta(&below_here, lane) : 0;
+    for (int v = threadIdx.x; v < range; v += kSortThreads) {
+        int n = 0, ahead = 0;
+#pragma unroll
+        for (int q = 0; q < kCluster; ++q) {
+            const int c = from_cta(here + v, q);
+            n += c;
+            ahead += q < part ? c : 0;
+        }
+        all[v] = n;
+        before[v] = ahead;
+    }
+    // (the others' sums have been read; a CTA leaves once its own have been)
+    asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) base += __shfl_xor_sync(0xffffffffu, base, o);
+    __syncthreads();
+    for (int i = threadIdx.x; i < (range + 31) / 32 * 32; i += kSortThreads) {
+        const uint32_t word = __ballot_sync(0xffffffffu, i < range && all[i] != 0);
+        if (lane == 0) named[i >> 5] = word;
+    }
+    const int per = (range + kSortThreads - 1) / kSortThreads;
+    const int v0 = min((int)threadIdx.x * per, range), v1 = min(v0 + per, range);
+    int total = 0;
+    for (int v = v0; v < v1; ++v) total += all[v];
+    int at = base + block_prefix(total, scratch, &sum);
+    for (int v = v0; v < v1; ++v) {
+        int to = at + before[v];
+#pragma unroll
+        for (int k = 0; k < kRuns; ++k) {   // the first place of the symbol's tokens in each run
+            const int c = counts[k * range + v];
+            counts[k * range + v] = to;
+            to += c;
+        }
+        at += all[v];
+    }
+    if (threadIdx.x == 0 && hi == a.V && part == 0) *a.count = base + sum;
+    __syncthreads();
+    if (warp < kRuns) {
+        const long long w0 = first + warp * kShares * share;
+        place_tokens(a, w0, min((long long)a.T, w0 + kShares * share), lo, hi, counts + warp * range);
+    } else if (a.dE) {
+        // the other warps: zeros; the CTAs of a cluster share the range's rows
+        const int rows = (range + kCluster - 1) / kCluster;
+        const int z0 = min(lo + part * rows, hi), z1 = min(z0 + rows, hi);
+        start_zeros(a, z0, z1, lo, named, source, warp - kRuns, kSortWarps - kRuns);
+        bulk_wait<0>();
+    }
+    asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
 }
 
 // For larger vocabularies: a CTA a range, which collects its own in their order and sorts them, 8 bits
@@ -754,16 +871,9 @@ int chunk_log2_of(int T, int tiles, int sms) {
     return l;
 }
 
-// Symbols of a range, and whether the counts of its tokens fit into shared memory: up to about 160000
-// symbols (16384 tokens of 32000 symbols: 13 us, where collecting and sorting took 18).
+// Bytes of `tallies` counts for each symbol of a range, and of the flags.
 constexpr size_t kPlaceSmem = 200 * 1024;   // of counts at most
-size_t place_bytes(int range) { return ((size_t)kTallies * range + (range + 31) / 32) * 4; }
-int range_of(int V, bool* counted) {
-    const long long sms = device_sms();
-    const int range = (int)((V * (long long)kSplit + sms - 1) / sms);
-    *counted = place_bytes(range) <= kPlaceSmem;
-    return *counted ? range : (int)((V + sms - 1) / sms);
-}
+size_t place_bytes(int range, int tallies) { return ((size_t)tallies * range + (range + 31) / 32) * 4; }
 struct BwdPlan {
     int tiles, chunk_log2, chunks;
     size_t key[3], pos[3], count, part, bytes;
@@ -828,22 +938,54 @@ cudaError_t fwd(const int* ids, const void* table, int tokens, int V, int d, flo
                       (long long)tokens, V, d, scale, static_cast<T*>(x));
 }
 
-cudaError_t launch_sort(const SortArgs& a, bool counted, cudaStream_t st) {
-    const unsigned ranges = (unsigned)((a.V + a.range - 1) / a.range);
-    if (!counted) return launch_pdl(embed_sort_kernel, dim3(ranges), dim3(kSortThreads), 0, st, a);
+// Orders the tokens, and zeros the rows that none names.  More of them than a CTA's warps ask for at once:
+// by clusters, as many as run at the same time, while their counts fit into shared memory (about 100000
+// symbols); else without, while those do (about 160000 symbols: 16384 tokens of 32000 13 us, where
+// collecting and sorting took 18).
+constexpr int kManyTokens = kSortWarps * 512;
+cudaError_t launch_sort(SortArgs& a, cudaStream_t st) {
     static std::once_flag once[64];
     static cudaError_t set_err[64];
+    static int clusters[64];
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
     std::call_once(once[dev], [&] {
-        set_err[dev] = cudaFuncSetAttribute(embed_place_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                            (int)kPlaceSmem);
+        cudaError_t& err = set_err[dev];
+        err = cudaFuncSetAttribute(embed_place_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                   (int)kPlaceSmem);
+        if (err == cudaSuccess)
+            err = cudaFuncSetAttribute(embed_place_cluster_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                       (int)kPlaceSmem);
+        if (err != cudaSuccess) return;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(kCluster);
+        cfg.blockDim = dim3(kSortThreads);
+        cfg.dynamicSmemBytes = kPlaceSmem;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = kCluster;
+        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        err = cudaOccupancyMaxActiveClusters(&clusters[dev], embed_place_cluster_kernel, &cfg);
+        if (err == cudaSuccess && clusters[dev] < 1) err = cudaErrorInvalidConfiguration;
     });
     if (set_err[dev] != cudaSuccess) return set_err[dev];
-    return launch_pdl(embed_place_kernel, dim3(ranges * kSplit), dim3(kSortThreads),
-                      place_bytes(a.range), st, a);
+    const long long sms = device_sms();
+    const auto launch = [&](void (*kern)(const SortArgs), int ctas_of_range, size_t smem) {
+        const unsigned ranges = (unsigned)((a.V + a.range - 1) / a.range);
+        return launch_pdl(kern, dim3(ranges * ctas_of_range), dim3(kSortThreads), smem, st, a);
+    };
+    a.range = (a.V + clusters[dev] - 1) / clusters[dev];
+    if (a.T > kManyTokens && place_bytes(a.range, kRuns + 3) <= kPlaceSmem)
+        return launch(embed_place_cluster_kernel, kCluster, place_bytes(a.range, kRuns + 3));
+    a.range = (int)((a.V * (long long)kSplit + sms - 1) / sms);
+    if (place_bytes(a.range, kTallies) <= kPlaceSmem)
+        return launch(embed_place_kernel, kSplit, place_bytes(a.range, kTallies));
+    a.range = (int)((a.V + sms - 1) / sms);
+    return launch(embed_sort_kernel, 1, 0);
 }
 
 template <typename T, typename O, int W>
@@ -861,9 +1003,7 @@ cudaError_t bwd(SortArgs& so, SumArgs& su, int tokens, char* ws, cudaStream_t st
     su.chunk_log2 = p.chunk_log2;
     su.chunks = p.chunks;
     su.tiles = p.tiles;
-    bool counted;
-    so.range = range_of(so.V, &counted);
-    cudaError_t e = launch_sort(so, counted, st);
+    cudaError_t e = launch_sort(so, st);
     if (e != cudaSuccess) return e;
     ++*launches;
     const long long items = (long long)p.chunks * p.tiles;

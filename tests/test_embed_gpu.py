@@ -108,6 +108,25 @@ def test_runs_over_chunks(H, T):
         check_bwd(H, ids.astype(np.int32), dx, V, 1.0, poison=float("nan"))
 
 
+@pytest.mark.parametrize("T", [16384, 16385, 24577, 40001, 100000])
+@pytest.mark.parametrize("V,d", [(1, 8), (3, 24), (201, 16), (5003, 9), (40000, 8), (99000, 4), (120000, 4)])
+def test_many_tokens(H, T, V, d):
+    rng = np.random.default_rng(T + V)
+    ids = symbols(rng, V, T)
+    ids[::11] = ids[0]
+    ids[T - 100:] = V - 1
+    dx = torch.from_numpy(rng.normal(size=(T, d)).astype(np.float32))
+    at = torch.from_numpy(np.where(ids < 0, V, ids)).long()
+    want = torch.zeros(V + 1, d, dtype=torch.float64).index_add_(0, at, dx.double())[:V]
+    mag = torch.zeros(V + 1, d, dtype=torch.float64).index_add_(0, at, dx.double().abs())[:V]
+    dE = torch.full((V, d), float("nan"), device="cuda")
+    H.hcw_embed_bwd(torch.from_numpy(ids).cuda(), dx.cuda(), V, dE=dE)
+    assert bool(((dE.double().cpu() - want).abs() <= T * U * mag).all())
+    again = H.hcw_embed_bwd(torch.from_numpy(ids).cuda(), dx.cuda(), V)
+    assert torch.equal(again, dE)
+    assert H.hcw_sync_status() == H.HCW_OK
+
+
 @pytest.mark.parametrize("V", [256 * 152 - 1, 256 * 152 + 1, 131072, 262144, 1 << 20])
 def test_vocabularies_of_one_and_two_sorting_passes(H, V):
     rng = np.random.default_rng(V)
