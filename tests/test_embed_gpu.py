@@ -215,6 +215,34 @@ def test_the_same_bits_another_stream_and_a_graph(H, dtype):
     assert torch.equal(dE, check_bwd(H, other, dx, V, 1.5))
 
 
+def test_many_tokens_on_two_streams_and_in_a_graph(H):
+    rng = np.random.default_rng(12)
+    T, V, d = 40000, 900, 24
+    ids = [torch.from_numpy(symbols(rng, V, T)).cuda() for _ in range(2)]
+    dx = [torch.randn(T, d, device="cuda") for _ in range(2)]
+    want = [H.hcw_embed_bwd(i, x, V) for i, x in zip(ids, dx)]
+    got = [torch.full((V, d), float("nan"), device="cuda") for _ in range(2)]
+    ws = [torch.empty(H.hcw_embed_bwd_workspace_bytes(T, V, d), dtype=torch.uint8, device="cuda")
+          for _ in range(2)]
+    st = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for k in range(2):
+            H.hcw_embed_bwd(ids[k], dx[k], V, dE=got[k], workspace=ws[k], stream=st[k])
+    torch.cuda.synchronize()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=st[0]):
+        H.hcw_embed_bwd(ids[0], dx[0], V, dE=got[0], workspace=ws[0])
+    ids[0].copy_(ids[1])
+    dx[0].copy_(dx[1])
+    for _ in range(3):
+        got[0].fill_(float("nan"))
+        g.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(got[0], want[1])
+
+
 def test_shapes_of_batches(H):
     ids = torch.randint(0, 50, (4, 7), dtype=torch.int32, device="cuda")
     table = torch.randn(50, 24, device="cuda")
