@@ -336,21 +336,27 @@ __global__ void __launch_bounds__(256) logits_mask_kernel(const LogitsArgs a) {
 // slot.  Which place a symbol gets depends on the order of the threads, what is found there does not.
 // Where a row has more names than the table takes (HASH false) the table is indexed by the symbol,
 // and CTAs share a row's symbols in ranges of kLRange.
-// The table is filled while the launch before may still be under way: that one began after what lies
-// before it had ended, and does not change a logit that is read here.
+// The table is cleared while the launch before may still be under way; everything else waits for it:
+// what lies before that launch has ended by then, but only the wait makes its memory visible here.
 constexpr int kLRange = 8192;
 constexpr int kLNames = 4096;         // of a row's history, for the hashed table
 constexpr int kLPlaces = 8192;        // of that table: five eighths of them taken at most
 constexpr int kNoSlot = 0x7fffffff;
 
 template <typename T, bool HASH, int NT>
-__global__ void __launch_bounds__(NT) logits_named_kernel(const LogitsArgs a, int size, int behind_mask) {
+__global__ void __launch_bounds__(NT) logits_named_kernel(const LogitsArgs a, int size) {
     constexpr int NH = kLNames / NT, NS = kLMaxSlots / NT;   // names a thread
     extern __shared__ __align__(16) int table[];   // [size]: counts, first slots, symbols
     uint32_t* const count = reinterpret_cast<uint32_t*>(table);
     int* const low = table + size;
     int* const key = table + 2 * size;             // HASH
-    if (!behind_mask) pdl_wait();
+    for (int i = threadIdx.x; i < size / 4; i += NT) {
+        reinterpret_cast<uint4*>(count)[i] = make_uint4(0, 0, 0, 0);
+        reinterpret_cast<int4*>(low)[i] = make_int4(kNoSlot, kNoSlot, kNoSlot, kNoSlot);
+        if (HASH) reinterpret_cast<int4*>(key)[i] = make_int4(-1, -1, -1, -1);
+    }
+    pdl_wait();
+    pdl_trigger();
     const int row = HASH ? blockIdx.x : blockIdx.x / a.slices;
     const int lo = HASH ? 0 : blockIdx.x % a.slices * kLRange;
     const int hi = HASH ? a.V : min(a.V, lo + kLRange);
@@ -377,11 +383,6 @@ __global__ void __launch_bounds__(NT) logits_named_kernel(const LogitsArgs a, in
     pen.rep = a.rep ? a.rep[row] : 1.f;
     pen.freq = a.freq ? a.freq[row] : 0.f;
     pen.pres = a.pres ? a.pres[row] : 0.f;
-    for (int i = threadIdx.x; i < size / 4; i += NT) {
-        reinterpret_cast<uint4*>(count)[i] = make_uint4(0, 0, 0, 0);
-        reinterpret_cast<int4*>(low)[i] = make_int4(kNoSlot, kNoSlot, kNoSlot, kNoSlot);
-        if (HASH) reinterpret_cast<int4*>(key)[i] = make_int4(-1, -1, -1, -1);
-    }
     __syncthreads();
     // the symbol's place (made if it has none), or -1
     const auto place = [&](int symbol) {
@@ -473,8 +474,6 @@ __global__ void __launch_bounds__(NT) logits_named_kernel(const LogitsArgs a, in
         for (int m = threadIdx.x + i * NT + 1; m < a.M; ++m)
             if (bias_idx[m] == at[i]) sum[i] += bias[m];
     }
-    if (behind_mask) pdl_wait();
-    pdl_trigger();
 #pragma unroll
     for (int i = 0; i < NH; ++i)
         if (past[i] >= 0) put(out + past[i], pen(v[i], c[i]));
@@ -490,7 +489,7 @@ __global__ void __launch_bounds__(NT) logits_named_kernel(const LogitsArgs a, in
 }
 
 template <typename T, bool HASH, int NT>
-cudaError_t launch_named(const LogitsArgs& a, long long ctas, int size, bool behind, cudaStream_t st) {
+cudaError_t launch_named(const LogitsArgs& a, long long ctas, int size, cudaStream_t st) {
     auto kern = logits_named_kernel<T, HASH, NT>;
     static std::once_flag once[64];
     static cudaError_t set_err[64];
@@ -503,8 +502,7 @@ cudaError_t launch_named(const LogitsArgs& a, long long ctas, int size, bool beh
                                             HASH ? kLPlaces * 12 : kLRange * 8);
     });
     if (set_err[dev] != cudaSuccess) return set_err[dev];
-    return launch_pdl(kern, dim3((unsigned)ctas), dim3(NT), (size_t)size * (HASH ? 12 : 8), st, a, size,
-                      (int)behind);
+    return launch_pdl(kern, dim3((unsigned)ctas), dim3(NT), (size_t)size * (HASH ? 12 : 8), st, a, size);
 }
 
 // One launch up to 2.5 MB of logits, where it is the shorter wait (1 x 201 2.4 us, 8 x 131072 bf16 5.2
@@ -538,13 +536,13 @@ cudaError_t edit(LogitsArgs& a, cudaStream_t st, int* launches) {
         a.slices = (a.V + kLRange - 1) / kLRange;
         const long long ctas = (long long)a.B * a.slices;
         const int size = std::min((a.V + 3) / 4 * 4, kLRange);
-        return ctas <= sms ? launch_named<T, false, 1024>(a, ctas, size, whole, st)
-                           : launch_named<T, false, 512>(a, ctas, size, whole, st);
+        return ctas <= sms ? launch_named<T, false, 1024>(a, ctas, size, st)
+                           : launch_named<T, false, 512>(a, ctas, size, st);
     }
     int size = 256;
     while (5 * size < 8 * names) size *= 2;
-    return a.B <= sms ? launch_named<T, true, 1024>(a, a.B, size, whole, st)
-                      : launch_named<T, true, 512>(a, a.B, size, whole, st);
+    return a.B <= sms ? launch_named<T, true, 1024>(a, a.B, size, st)
+                      : launch_named<T, true, 512>(a, a.B, size, st);
 }
 
 }  // namespace
