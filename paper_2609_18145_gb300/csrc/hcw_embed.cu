@@ -649,7 +649,7 @@ struct SumArgs {
     float* part;          // [chunks][2][d]: of the run that came in from before, and of the one that goes on
     int d, T;
     int chunk_log2;       // tokens of a chunk
-    int chunks, tiles;    // chunks at most, blocks of columns
+    int tiles;            // blocks of columns
     float scale;
     int add;
 };
@@ -1001,7 +1001,6 @@ cudaError_t bwd(SortArgs& so, SumArgs& su, int tokens, char* ws, cudaStream_t st
     su.count = so.count;
     su.part = reinterpret_cast<float*>(ws + p.part);
     su.chunk_log2 = p.chunk_log2;
-    su.chunks = p.chunks;
     su.tiles = p.tiles;
     cudaError_t e = launch_sort(so, st);
     if (e != cudaSuccess) return e;
@@ -1093,6 +1092,9 @@ extern "C" int hcw_embed_bwd(const int* ids, const void* dx, int T, int V, int d
     const size_t es = dtype == HCW_F32 ? 4 : 2, oes = de_dtype == HCW_F32 ? 4 : 2;
     const size_t ob = (size_t)V * d * oes, need = T > 0 ? bwd_ws_bytes(T, d) : 0;
     if (need && (!workspace || ws_bytes < need)) return HCW_ERR_WORKSPACE;
+    const BwdPlan plan = bwd_plan(T, d, dtype == HCW_BF16 ? 8 : 4);
+    // (`need` is that of any batch up to T, so no less than this one's parts take)
+    if (T > 0 && plan.bytes > ws_bytes) return HCW_ERR_WORKSPACE;
     const struct {
         const void* p;
         size_t n;
@@ -1105,8 +1107,6 @@ extern "C" int hcw_embed_bwd(const int* ids, const void* dx, int T, int V, int d
         if (accumulate) return HCW_OK;
         return cudaMemsetAsync(dE, 0, ob, st) == cudaSuccess ? HCW_OK : HCW_ERR_CUDA;
     }
-    const int elems = dtype == HCW_BF16 ? 8 : 4;
-    const BwdPlan plan = bwd_plan(T, d, elems);
     if ((V + device_sms() - 1) / device_sms() > kMaxRange || (long long)plan.chunks * plan.tiles > 0x7fffffff)
         return HCW_ERR_UNSUPPORTED;
     SortArgs so = {};
